@@ -402,6 +402,213 @@ tss_status tss_linear_static_status(void* stream);
  * returned.  Synchronises the device. */
 tss_status tss_read_trace(tss_ctx* ctx, unsigned long long* host, size_t capacity, size_t* n_out);
 
+/* ------------------------------------------------------------------------------------------------
+ * A KV cache in pages, held in 4 bits, and the operators around it.  The paper keeps its base methods'
+ * 16-bit cache; these calls serve the same drafts (chains and trees, App. "Models" heads, grouped
+ * heads too) where contexts or hypotheses are too many for it.  They need no tss_ctx.
+ *
+ * Page layout.  A page holds TSS_PAGE_TOKENS = 64 tokens of every KV head of one layer: a block of
+ * 64 * head_dim + 512 * (head_dim / 64) bytes per head, heads consecutive (head_dim 64 or 128).  The 64
+ * neighbouring dims 64 g .. 64 g + 63 of a token's head share a scale s and a minimum z, both fp16; a
+ * 4-bit code c stands for s c + z.  With G = head_dim / 64, a block is
+ *   K codes     [64 tokens][4 quarters t][G groups][16 dims], two to a byte, the even one low;
+ *               dim = 64 g + 16 t + index
+ *   V codes     [2 halves][head_dim / 4][4 t][4 e] 32-bit words; nibble b + 4 i of a word is token
+ *               32 half + 8 b + 2 t + i, dim 4 (third index) + e
+ *   K params    [64 tokens][G] pairs (s, z) of fp16
+ *   V params    the same
+ * Quantisation of a token's group x: z = fp16(min x), s = fp16(max(0, max x - z) / 15), both at most
+ * 65504 in magnitude, c = (x - z) / s rounded to the nearest (ties to even) and kept in [0, 15], 0 where
+ * s = 0; all in fp32.  A group that holds a NaN or an infinity gets s = NaN and reads back as NaN.
+ * ------------------------------------------------------------------------------------------------ */
+#define TSS_DTYPE_BF16 0
+#define TSS_DTYPE_F16 1
+#define TSS_DTYPE_F32 2
+#define TSS_PAGE_TOKENS 64
+
+/* Per-head norms of queries and keys and their rotary positions in one pass:
+ *   x' = x * rsqrt(mean(x^2) + eps) * gain over the head (only where a gain is given), then the pairs
+ *   (a, b) of the first rot_dim dims become (a cos - b sin, b cos + a sin).
+ * interleaved = 0 pairs dims (i, i + rot_dim / 2), 1 pairs (2 i, 2 i + 1); the other dims pass.
+ * table [max_positions][rot_dim / 2][2] fp32 holds (cos, sin) of pair i at a position, any scaling for
+ * long contexts included (tss_rope_frequencies, tss_rope_table).  All arithmetic is fp32; one rounding
+ * at the end.
+ *   q [n_rows][n_q_heads][head_dim], k [n_rows][n_k_heads][head_dim], DEVICE, dtype TSS_DTYPE_*; strides
+ *   are elements between rows (slices of a fused projection qualify); heads are contiguous.  Either side
+ *   may have 0 heads.  q_out / k_out may be q / k with the same stride; otherwise outputs overlap no input.
+ *   q_gain / k_gain [head_dim] of the same dtype, or NULL.  positions [n_rows] int32 DEVICE.
+ *   status: DEVICE int32 or NULL; a position outside the table records TSS_ERR_DEVICE_CHECK there (if it
+ *   was 0), and the row is rotated as at the nearest position of the table.
+ * head_dim a multiple of 16 up to 256; rot_dim a multiple of 16 in [0, head_dim]; pointers and rows
+ * aligned to 16 bytes.  Asynchronous on `stream`; any number of calls may overlap.  Errors: INVALID_ARG,
+ * CUDA. */
+typedef struct {
+  int n_rows, n_q_heads, n_k_heads, head_dim, rot_dim, interleaved, dtype;
+  const void* q;
+  const void* k;
+  void* q_out;
+  void* k_out;
+  int64_t q_stride, k_stride, q_out_stride, k_out_stride;
+  const void* q_gain;
+  const void* k_gain;
+  float eps;
+  const float* table;
+  int max_positions;
+  const int32_t* positions;
+  int32_t* status;
+} tss_rope_args;
+tss_status tss_qk_rope(const tss_rope_args* args, void* stream);
+
+/* Frequencies of rot_dim / 2 rotary pairs, theta^(-2 i / rot_dim), scaled for contexts `factor` times the
+ * `original` one.  Host arithmetic in double; inv_freq (HOST) receives rot_dim / 2 values and
+ * *attention_factor what the table's entries are multiplied by (1 but for YARN).
+ *   NONE
+ *   LINEAR  every frequency divided by factor (position interpolation)
+ *   NTK     theta replaced by theta * factor^(rot_dim / (rot_dim - 2))
+ *   YARN    pairs that turn more than fast = 32 times within `original` stay, those that turn less than
+ *           slow = 1 times are divided by factor, a linear ramp over the pair index between;
+ *           attention_factor = 0.1 ln(factor) + 1
+ *   BANDS   wavelengths under original / 4 stay, those over `original` are divided by factor, between
+ *           them the two are blended in original / wavelength
+ * Errors: INVALID_ARG (NULL, rot_dim odd or < 2, theta <= 1, factor < 1, original < 1 where it is used,
+ * rot_dim < 4 for NTK). */
+#define TSS_ROPE_NONE 0
+#define TSS_ROPE_LINEAR 1
+#define TSS_ROPE_NTK 2
+#define TSS_ROPE_YARN 3
+#define TSS_ROPE_BANDS 4
+tss_status tss_rope_frequencies(int kind, int rot_dim, double theta, double factor, double original, double* inv_freq,
+                                double* attention_factor);
+
+/* table[p][i] = attention_factor * (cos, sin)(p * inv_freq[i]) for p in [0, max_positions) and i in
+ * [0, n_pairs), computed in double and rounded to fp32; inv_freq HOST, n_pairs in [1, 128], table DEVICE
+ * fp32 (8-byte aligned).  Asynchronous on `stream` (the frequencies are read before the call returns).
+ * Errors: INVALID_ARG, CUDA. */
+tss_status tss_rope_table(const double* inv_freq, int n_pairs, double attention_factor, int max_positions, float* table,
+                          void* stream);
+
+/* Bytes of one page (0 for a shape that is not supported: head_dim 64 or 128, n_kv_heads in [1, 1024]). */
+size_t tss_paged_page_bytes(int n_kv_heads, int head_dim);
+
+/* Workspace of the calls on 4-bit pages, for one shape: n_q_heads a multiple of n_kv_heads, at most 64
+ * query heads per KV head, head_dim 64 or 128; on the current device (sm_103).  It holds the attention's
+ * partial results and a status word; calls that share one must not overlap on different streams.  Errors:
+ * INVALID_ARG, UNSUPPORTED_ARCH, OUT_OF_MEMORY, CUDA. */
+typedef struct tss_paged tss_paged;
+tss_status tss_paged_create(int n_q_heads, int n_kv_heads, int head_dim, tss_paged** out);
+/* After the caller's streams are idle; NULL is a no-op. */
+void tss_paged_destroy(tss_paged* p);
+/* Synchronise `stream`, then return and clear the status word: TSS_OK, TSS_ERR_DEVICE_CHECK (a page table
+ * entry outside [0, n_pages) where a page was needed: nothing was read or written there) or
+ * TSS_ERR_TIMEOUT. */
+tss_status tss_paged_sync_status(tss_paged* p, void* stream);
+
+/* Caller-owned cache: layer is a HOST array of n_layers DEVICE pointers to [n_pages][page bytes] (16-byte
+ * aligned); table [n_seqs][max_pages] int32 DEVICE lists each sequence's pages in order.  Sequences may
+ * share pages that nobody appends to. */
+typedef struct {
+  void* const* layer;
+  int n_layers, n_pages;
+  const int32_t* table;
+  int n_seqs, max_pages;
+} tss_paged_cache;
+
+/* Blocks of n_req requests (1..64), HOST arrays: request b is the tokens [first[b], first[b] + n_tokens[b])
+ * of sequence seq[b] (n_tokens[b] >= 0).  Rows of q, k, v and the outputs are the requests' tokens laid
+ * end to end.  first + n_tokens above 64 * max_pages returns TSS_ERR_KV_CAPACITY. */
+typedef struct {
+  int n_req;
+  const int32_t* seq;
+  const int32_t* first;
+  const int32_t* n_tokens;
+} tss_paged_batch;
+
+/* Quantise k, v [rows][n_kv_heads][head_dim] (DEVICE, TSS_DTYPE_*, strides in elements between rows, rows
+ * 16-byte aligned) into the pages of their tokens in `layer`.  A sequence may appear once.  Other tokens
+ * of those pages keep their values.  Asynchronous on `stream`. */
+tss_status tss_paged_append(tss_paged* p, const tss_paged_cache* cache, int layer, const tss_paged_batch* batch,
+                            const void* k, const void* v, int64_t k_stride, int64_t v_stride, int dtype, void* stream);
+
+/* The reverse: the values of the batch's tokens, s c + z, to k, v (either may be NULL). */
+tss_status tss_paged_read(tss_paged* p, const tss_paged_cache* cache, int layer, const tss_paged_batch* batch, void* k,
+                          void* v, int64_t k_stride, int64_t v_stride, int dtype, void* stream);
+
+/* Attention of draft blocks over the cached keys and values of `layer`.  Request b's rows are the tokens
+ * [first, first + n_tokens) (n_tokens <= 128), already appended; a row sees the keys [0, first) and, of
+ * its own block, the rows of its mask, or (mask NULL) itself and those before it.
+ *   q, out [rows][n_q_heads][head_dim] DEVICE, TSS_DTYPE_BF16 or _F16, strides in elements between rows,
+ *     rows 16-byte aligned; query head h reads KV head h / (n_q_heads / n_kv_heads).
+ *   scale: of the scores (1 / sqrt(head_dim) as a rule).
+ *   mask: DEVICE uint64 [rows][2] or NULL; bit j of the pair: the row sees row j of its block.
+ *   window > 0: a key is seen only where position(row) - position(key) < window, or its index in the
+ *     sequence is below n_sinks.  positions: DEVICE int32 [rows], at least first[b] (a smaller one counts
+ *     as first[b]); NULL: the rows' indices.  A context key's position is its index.  Read only where
+ *     window > 0.
+ *   lse: DEVICE fp32 [rows][n_q_heads] or NULL: ln sum exp(scale q.k) over the keys seen.
+ * A row that sees nothing gets zeros and lse = -infinity.  Values of keys that a row does not see do not
+ * reach it, whatever they are.  Scores, sums and accumulators are fp32; the weights enter the second
+ * product as fp16.  Asynchronous on `stream`.  Errors: INVALID_ARG, KV_CAPACITY, CUDA. */
+typedef struct {
+  const void* q;
+  int64_t q_stride;
+  void* out;
+  int64_t out_stride;
+  float* lse;
+  int dtype;
+  float scale;
+  int window, n_sinks;
+  const uint64_t* mask;
+  const int32_t* positions;
+} tss_paged_attn;
+tss_status tss_paged_attention(tss_paged* p, const tss_paged_cache* cache, int layer, const tss_paged_batch* batch,
+                               const tss_paged_attn* args, void* stream);
+
+/* Bookkeeping of pages of any content, entirely on the device (no host wait): the caller's arrays
+ *   table [n_seqs][max_pages]  page ids of each sequence, -1 past held[seq]
+ *   held [n_seqs]              pages of each sequence
+ *   refs [n_pages]             sequences that hold each page; 0 = free
+ * all int32 DEVICE.  A page that is needed is the free one of lowest id, in the order of the request:
+ * results do not depend on timing.  tss_pages_create makes the workspace for these sizes (n_pages at most
+ * 2^20; n_seqs * max_pages below 2^31); calls that share one must not overlap on different streams.
+ * `layer` arguments are HOST arrays of DEVICE pointers to [n_pages][page_bytes] (1..128 layers, 16-byte
+ * aligned, page_bytes a multiple of 16).  seq, src, dst and the counts are HOST arrays of n entries, n in
+ * [0, 64].  Failures seen on the device leave the arrays as they were and record a code for
+ * tss_pages_sync_status: TSS_ERR_KV_CAPACITY (not enough free pages: the whole call did nothing),
+ * TSS_ERR_DEVICE_CHECK (an id outside the pool, a count that the arrays contradict; tss_pages_free drops
+ * such an entry alone).  Asynchronous on `stream`.  Errors: INVALID_ARG, UNSUPPORTED_ARCH, OUT_OF_MEMORY, CUDA. */
+typedef struct tss_pages tss_pages;
+typedef struct {
+  int32_t* table;
+  int32_t* held;
+  int32_t* refs;
+} tss_page_tables;
+tss_status tss_pages_create(int n_seqs, int max_pages, int n_pages, tss_pages** out);
+void tss_pages_destroy(tss_pages* h);
+tss_status tss_pages_sync_status(tss_pages* h, void* stream);
+
+/* Give sequence seq[i] new pages until it holds want[i] (nothing where it already does).  Sequences are
+ * distinct. */
+tss_status tss_pages_reserve(tss_pages* h, const tss_page_tables* t, int n, const int32_t* seq, const int32_t* want,
+                             void* stream);
+/* Drop the pages of seq[i] past the first keep[i] (keep NULL: all).  Sequences are distinct. */
+tss_status tss_pages_free(tss_pages* h, const tss_page_tables* t, int n, const int32_t* seq, const int32_t* keep,
+                          void* stream);
+/* Sequence dst[i], which holds nothing, becomes a copy of the first total[i] pages of src[i]: the first
+ * shared[i] of them are the same pages (refs + 1), the rest are copied into new ones in every layer.
+ * dst are distinct and none is a src. */
+tss_status tss_pages_fork(tss_pages* h, const tss_page_tables* t, void* const* layer, int n_layers, size_t page_bytes,
+                          int n, const int32_t* src, const int32_t* dst, const int32_t* shared, const int32_t* total,
+                          void* stream);
+/* Move the pages in use to the ids below their number, in every layer: the lowest page past it to the
+ * lowest free one, and so on; the other pages stay.  The new table and counts go to table_out and
+ * refs_out, which may be t's own (held does not change). */
+tss_status tss_pages_compact(tss_pages* h, const tss_page_tables* t, int32_t* table_out, int32_t* refs_out,
+                             void* const* layer, int n_layers, size_t page_bytes, void* stream);
+/* Copy page src[i] over page dst[i] in every layer; src, dst int32 DEVICE of n entries, in [0, n_pages)
+ * (others are skipped and recorded); no dst is another entry's src or dst. */
+tss_status tss_pages_copy(tss_pages* h, void* const* layer, int n_layers, size_t page_bytes, int n, const int32_t* src,
+                          const int32_t* dst, void* stream);
+
 const char* tss_status_string(tss_status s);
 /* Message of the last error reported to the calling thread ("" if none). */
 const char* tss_last_error(void);

@@ -1,0 +1,130 @@
+// What the stand-alone operators (rope.cu, paged.cu, paged_attn.cu, pages.cu) share: element types,
+// vectors of eight elements, the layout of a 4-bit page, host-side refusals.
+#pragma once
+
+#include <new>
+#include <string>
+
+#include "internal.h"
+
+namespace tss {
+
+// ------------------------------------------------------------------------------------------
+// Host
+// ------------------------------------------------------------------------------------------
+inline tss_status refuse(tss_status s, const char* msg) noexcept {
+  try {
+    set_last_error(msg);
+  } catch (...) {  // no memory for the message: the status stands
+  }
+  return s;
+}
+inline tss_status refuse_cuda(cudaError_t e, const char* what) noexcept {
+  cudaGetLastError();  // (a launch error is not sticky; leave none for the next call)
+  try {
+    set_last_error(std::string(what) + ": " + cudaGetErrorString(e));
+  } catch (...) {
+  }
+  return TSS_ERR_CUDA;
+}
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline int dtype_bytes(int dtype) { return dtype == TSS_DTYPE_F32 ? 4 : 2; }
+inline bool known_dtype(int dtype) { return dtype == TSS_DTYPE_BF16 || dtype == TSS_DTYPE_F16 || dtype == TSS_DTYPE_F32; }
+// A row stride (elements) of rows of `width` elements that keeps them apart and 16-byte aligned.
+inline bool good_stride(int64_t stride, int64_t width, int dtype) {
+  return stride >= width && stride < (int64_t(1) << 40) && (stride * dtype_bytes(dtype)) % 16 == 0;
+}
+// The current device's SM count, if it is an sm_103.
+inline tss_status this_device(int* sms) {
+  int dev = 0, major = 0, minor = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, dev);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev);
+  if (e != cudaSuccess) return refuse_cuda(e, "device query");
+  if (major != 10 || minor != 3) return refuse(TSS_ERR_UNSUPPORTED_ARCH, "needs an sm_103 GPU");
+  return TSS_OK;
+}
+
+// ------------------------------------------------------------------------------------------
+// Vectors of N elements (N * element size a multiple of 4 bytes, addresses aligned to it) as fp32
+// ------------------------------------------------------------------------------------------
+__device__ __forceinline__ float to_f32(float x) { return x; }
+__device__ __forceinline__ float to_f32(__half x) { return __half2float(x); }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
+template <typename T>
+__device__ __forceinline__ T from_f32(float x);
+template <>
+__device__ __forceinline__ float from_f32<float>(float x) { return x; }
+template <>
+__device__ __forceinline__ __half from_f32<__half>(float x) { return __float2half_rn(x); }
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+
+template <int BYTES>
+struct RawVec;
+template <>
+struct RawVec<4> { using type = uint32_t; };
+template <>
+struct RawVec<8> { using type = uint2; };
+template <>
+struct RawVec<16> { using type = uint4; };
+
+template <typename T, int N>
+__device__ __forceinline__ void load_vec(const T* p, float* x) {
+  constexpr int kPart = N * sizeof(T) < 16 ? N * sizeof(T) : 16;
+  constexpr int kPer = kPart / sizeof(T);
+#pragma unroll
+  for (int i = 0; i < N / kPer; ++i) {
+    const typename RawVec<kPart>::type raw = *reinterpret_cast<const typename RawVec<kPart>::type*>(p + i * kPer);
+    T t[kPer];
+    memcpy(t, &raw, kPart);
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) x[i * kPer + j] = to_f32(t[j]);
+  }
+}
+template <typename T, int N>
+__device__ __forceinline__ void store_vec(T* p, const float* x) {
+  constexpr int kPart = N * sizeof(T) < 16 ? N * sizeof(T) : 16;
+  constexpr int kPer = kPart / sizeof(T);
+#pragma unroll
+  for (int i = 0; i < N / kPer; ++i) {
+    T t[kPer];
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) t[j] = from_f32<T>(x[i * kPer + j]);
+    typename RawVec<kPart>::type raw;
+    memcpy(&raw, t, kPart);
+    *reinterpret_cast<typename RawVec<kPart>::type*>(p + i * kPer) = raw;
+  }
+}
+
+// ------------------------------------------------------------------------------------------
+// A page of the 4-bit cache: one block per KV head (K codes, V codes, K parameters, V parameters;
+// tss.h gives the order inside each)
+// ------------------------------------------------------------------------------------------
+constexpr int kPgTokens = TSS_PAGE_TOKENS;
+constexpr int kPgGroup = 64;      // dims that share a scale and a minimum
+constexpr int kPgMaxReq = 64;     // requests of a call
+constexpr int kPgMaxRows = 128;   // rows of one request's block in the attention
+template <int D>
+struct PgBlock {
+  static constexpr int kGroups = D / kPgGroup;
+  static constexpr int kCodes = kPgTokens * D / 2;
+  static constexpr int kK = 0, kV = kCodes, kKParams = 2 * kCodes;
+  static constexpr int kParams = kPgTokens * kGroups * 4;
+  static constexpr int kVParams = kKParams + kParams;
+  static constexpr int kBytes = kVParams + kParams;
+};
+inline size_t pg_block_bytes(int head_dim) {
+  return head_dim == 64 ? PgBlock<64>::kBytes : head_dim == 128 ? PgBlock<128>::kBytes : 0;
+}
+
+struct PgReq {
+  int seq, first, n, row;  // sequence, first token, tokens, first row of the caller's arrays
+};
+struct PgBatch {
+  int n_req;
+  PgReq r[kPgMaxReq];
+};
+
+}  // namespace tss

@@ -1,0 +1,31 @@
+// The 4-bit paged cache's workspace and the attention's launch interface.
+#pragma once
+
+#include "ops.cuh"
+
+// (opaque in tss.h)
+struct tss_paged {
+  int hq, hk, d, sms;
+  int* status;  // device
+};
+
+namespace tss {
+
+struct PgAttnParams {
+  int hq, hk, d, n_pages, max_pages;
+  const uint8_t* pool;      // the layer's pages
+  const int* table;
+  const void* q;
+  void* out;
+  float* lse;
+  long long qs, os;
+  float scale_log2;         // scale * log2(e)
+  int window, sinks, is_half;
+  const unsigned long long* mask;
+  const int* positions;
+  int* status;
+  PgBatch batch;
+};
+cudaError_t launch_paged_attention(const tss_paged* h, const PgAttnParams& p, int rows, cudaStream_t s);
+
+}  // namespace tss

@@ -29,7 +29,17 @@ EXPORTS = (
     "tss_linear", "tss_linear_static", "tss_read_trace", "tss_status_string", "tss_last_error",
     "tss_estimate_step_bytes", "tss_persistent_plan", "tss_inject_timeout", "tss_philox_uniforms",
     "tss_linear_static_status", "tss_verify_grouped", "tss_attention_kernel",
+    "tss_qk_rope", "tss_rope_frequencies", "tss_rope_table",
+    "tss_paged_page_bytes", "tss_paged_create", "tss_paged_destroy", "tss_paged_sync_status", "tss_paged_append",
+    "tss_paged_read", "tss_paged_attention",
+    "tss_pages_create", "tss_pages_destroy", "tss_pages_sync_status", "tss_pages_reserve", "tss_pages_free",
+    "tss_pages_fork", "tss_pages_compact", "tss_pages_copy",
 )
+TSS_DTYPE_BF16 = 0
+TSS_DTYPE_F16 = 1
+TSS_DTYPE_F32 = 2
+PAGE_TOKENS = 64
+ROPE_KINDS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3, "bands": 4}
 
 _P = ctypes.c_void_p
 _I32P = ctypes.POINTER(ctypes.c_int32)
@@ -81,6 +91,33 @@ class TssVerifyResult(ctypes.Structure):
                 ("new_ctx_len", _P), ("logits", _P)]
 
 
+class TssRopeArgs(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("n_rows", "n_q_heads", "n_k_heads", "head_dim", "rot_dim", "interleaved", "dtype")] + [
+        (n, _P) for n in ("q", "k", "q_out", "k_out")] + [
+        (n, ctypes.c_int64) for n in ("q_stride", "k_stride", "q_out_stride", "k_out_stride")] + [
+        ("q_gain", _P), ("k_gain", _P), ("eps", ctypes.c_float), ("table", _P), ("max_positions", ctypes.c_int),
+        ("positions", _P), ("status", _P)]
+
+
+class TssPagedCache(ctypes.Structure):
+    _fields_ = [("layer", ctypes.POINTER(_P)), ("n_layers", ctypes.c_int), ("n_pages", ctypes.c_int), ("table", _P),
+                ("n_seqs", ctypes.c_int), ("max_pages", ctypes.c_int)]
+
+
+class TssPagedBatch(ctypes.Structure):
+    _fields_ = [("n_req", ctypes.c_int), ("seq", _P), ("first", _P), ("n_tokens", _P)]
+
+
+class TssPagedAttn(ctypes.Structure):
+    _fields_ = [("q", _P), ("q_stride", ctypes.c_int64), ("out", _P), ("out_stride", ctypes.c_int64), ("lse", _P),
+                ("dtype", ctypes.c_int), ("scale", ctypes.c_float), ("window", ctypes.c_int), ("n_sinks", ctypes.c_int),
+                ("mask", _P), ("positions", _P)]
+
+
+class TssPageTables(ctypes.Structure):
+    _fields_ = [("table", _P), ("held", _P), ("refs", _P)]
+
+
 _lib = None
 
 
@@ -124,6 +161,34 @@ def lib() -> ctypes.CDLL:
                                          ctypes.POINTER(_P)]
         L.tss_attention_kernel.argtypes = [_P]
         L.tss_attention_kernel.restype = ctypes.c_int
+        I, L64, PP = ctypes.c_int, ctypes.c_int64, ctypes.POINTER(_P)
+        D = ctypes.POINTER(ctypes.c_double)
+        cache, batch, tables = ctypes.POINTER(TssPagedCache), ctypes.POINTER(TssPagedBatch), ctypes.POINTER(TssPageTables)
+        L.tss_qk_rope.argtypes = [ctypes.POINTER(TssRopeArgs), _P]
+        L.tss_rope_frequencies.argtypes = [I, I, ctypes.c_double, ctypes.c_double, ctypes.c_double, D, D]
+        L.tss_rope_table.argtypes = [D, I, ctypes.c_double, I, _P, _P]
+        L.tss_paged_page_bytes.argtypes = [I, I]
+        L.tss_paged_page_bytes.restype = ctypes.c_size_t
+        L.tss_paged_create.argtypes = [I, I, I, PP]
+        L.tss_paged_sync_status.argtypes = [_P, _P]
+        L.tss_paged_append.argtypes = [_P, cache, I, batch, _P, _P, L64, L64, I, _P]
+        L.tss_paged_read.argtypes = L.tss_paged_append.argtypes
+        L.tss_paged_attention.argtypes = [_P, cache, I, batch, ctypes.POINTER(TssPagedAttn), _P]
+        L.tss_pages_create.argtypes = [I, I, I, PP]
+        L.tss_pages_sync_status.argtypes = [_P, _P]
+        L.tss_pages_reserve.argtypes = [_P, tables, I, _P, _P, _P]
+        L.tss_pages_free.argtypes = [_P, tables, I, _P, _P, _P]
+        L.tss_pages_fork.argtypes = [_P, tables, PP, I, ctypes.c_size_t, I, _P, _P, _P, _P, _P]
+        L.tss_pages_compact.argtypes = [_P, tables, _P, _P, PP, I, ctypes.c_size_t, _P]
+        L.tss_pages_copy.argtypes = [_P, PP, I, ctypes.c_size_t, I, _P, _P, _P]
+        for name in ("tss_paged_destroy", "tss_pages_destroy"):
+            getattr(L, name).argtypes = [_P]
+            getattr(L, name).restype = None
+        for name in ("tss_qk_rope", "tss_rope_frequencies", "tss_rope_table", "tss_paged_create", "tss_paged_sync_status",
+                     "tss_paged_append", "tss_paged_read", "tss_paged_attention", "tss_pages_create",
+                     "tss_pages_sync_status", "tss_pages_reserve", "tss_pages_free", "tss_pages_fork", "tss_pages_compact",
+                     "tss_pages_copy"):
+            getattr(L, name).restype = ctypes.c_int
         for name in ("tss_create", "tss_set_skip_config", "tss_clear_skip_config", "tss_sparsity_ratio",
                      "tss_active_layer_count", "tss_verify", "tss_verify_profiled", "tss_prefill", "tss_sync_status",
                      "tss_linear", "tss_linear_static", "tss_read_trace", "tss_estimate_step_bytes",
@@ -177,6 +242,97 @@ def estimate_step_bytes(arch, masks: Sequence[int], ctx_len: Sequence[int], n_no
                                         ctypes.cast(_i32(n_nodes), _I32P), ctypes.byref(out)), "tss_estimate_step_bytes")
     return {"weights": out.weights, "kv_read": out.kv_read, "kv_write": out.kv_write, "total": out.total,
             "active_union": out.active_union}
+
+
+def dtype_code(t) -> int:
+    """TSS_DTYPE_* of a torch tensor."""
+    name = str(t.dtype)
+    codes = {"torch.bfloat16": TSS_DTYPE_BF16, "torch.float16": TSS_DTYPE_F16, "torch.float32": TSS_DTYPE_F32}
+    if name not in codes:
+        raise TypeError(f"bfloat16, float16 or float32 is wanted, not {name}")
+    return codes[name]
+
+
+def _rows(t, what: str):
+    """(rows, heads, head_dim, row stride) of a tensor [rows][heads][head_dim] whose heads are contiguous."""
+    if t.dim() != 3:
+        raise ValueError(f"{what}: [rows][heads][head_dim] is wanted")
+    n, h, d = t.shape
+    if n and h and (t.stride(2) != 1 or (h > 1 and t.stride(1) != d)):
+        raise ValueError(f"{what}: the heads of a row must be contiguous")
+    return n, h, d, t.stride(0) if n > 1 else max(t.stride(0), h * d)
+
+
+def _same(a, b, what: str) -> None:
+    if a.shape != b.shape or a.dtype != b.dtype or a.device != b.device:
+        raise ValueError(f"{what}: the output's shape, type and device must be the input's")
+
+
+def rope_frequencies(rot_dim: int, theta: float = 10000.0, kind: str = "none", factor: float = 1.0, original: float = 0.0):
+    """tss_rope_frequencies: (list of rot_dim / 2 frequencies, attention factor); kind one of ROPE_KINDS."""
+    n = max(int(rot_dim) // 2, 1)
+    f, a = (ctypes.c_double * n)(), ctypes.c_double()
+    check(lib().tss_rope_frequencies(ROPE_KINDS[kind], rot_dim, theta, factor, original, f, ctypes.byref(a)),
+          "tss_rope_frequencies")
+    return list(f), a.value
+
+
+def rope_table(inv_freq: Sequence[float], table, attention_factor: float = 1.0, stream=None) -> None:
+    """tss_rope_table into the float32 device tensor table [positions][len(inv_freq)][2]."""
+    n = len(inv_freq)
+    if tuple(table.shape[1:]) != (n, 2) or dtype_code(table) != TSS_DTYPE_F32 or not table.is_contiguous():
+        raise ValueError("table: contiguous float32 [positions][pairs][2] is wanted")
+    check(lib().tss_rope_table((ctypes.c_double * n)(*inv_freq), n, attention_factor, table.shape[0], table.data_ptr(), stream),
+          "tss_rope_table")
+
+
+def rope_args(q, k, q_out, k_out, positions, table, q_gain=None, k_gain=None, eps: float = 1e-6, interleaved: bool = False,
+              status=None) -> TssRopeArgs:
+    """Arguments of tss_qk_rope from tensors: q, k [rows][heads][head_dim] (either may be None) and their
+    outputs (q_out may be q), positions int32 [rows], table [positions][pairs][2] float32 (None: no rotation),
+    gains [head_dim] (None: no norm).  The structure keeps the tensors alive."""
+    one = q if q is not None else k
+    if one is None:
+        raise ValueError("q or k is wanted")
+    a = TssRopeArgs()
+    a.n_rows, _, a.head_dim, _ = _rows(one, "q")
+    a.dtype, a.interleaved, a.eps = dtype_code(one), int(interleaved), eps
+    for name, x, y, gain in (("q", q, q_out, q_gain), ("k", k, k_out, k_gain)):
+        if x is None:
+            continue
+        n, h, d, stride = _rows(x, name)
+        _same(x, y, name)
+        if (n, d, dtype_code(x)) != (a.n_rows, a.head_dim, a.dtype):
+            raise ValueError("q and k must agree in rows, head_dim and type")
+        setattr(a, f"n_{name}_heads", h)
+        setattr(a, name, x.data_ptr())
+        setattr(a, name + "_stride", stride)
+        setattr(a, name + "_out", y.data_ptr())
+        setattr(a, name + "_out_stride", _rows(y, name + "_out")[3])
+        if gain is not None:
+            if tuple(gain.shape) != (d,) or gain.dtype != x.dtype or not gain.is_contiguous():
+                raise ValueError(f"{name}_gain: contiguous [head_dim] of the same type is wanted")
+            setattr(a, name + "_gain", gain.data_ptr())
+    if table is not None:
+        if table.dim() != 3 or table.shape[2] != 2 or dtype_code(table) != TSS_DTYPE_F32 or not table.is_contiguous():
+            raise ValueError("table: contiguous float32 [positions][pairs][2] is wanted")
+        if str(positions.dtype) != "torch.int32" or positions.numel() != a.n_rows or not positions.is_contiguous():
+            raise ValueError("positions: contiguous int32 [rows] is wanted")
+        a.table, a.max_positions, a.rot_dim = table.data_ptr(), table.shape[0], 2 * table.shape[1]
+        a.positions = positions.data_ptr()
+    a.status = _ptr(status)
+    a._keep = (q, k, q_out, k_out, positions, table, q_gain, k_gain, status)
+    return a
+
+
+def current_stream() -> int:
+    import torch
+    return torch.cuda.current_stream().cuda_stream
+
+
+def qk_rope(args: TssRopeArgs, stream=None) -> None:
+    """tss_qk_rope on the given stream (None: torch's current one)."""
+    check(lib().tss_qk_rope(ctypes.byref(args), current_stream() if stream is None else stream), "tss_qk_rope")
 
 
 class TssError(RuntimeError):

@@ -1,0 +1,228 @@
+"""The paged 4-bit KV cache for PyTorch users: tensors and streams are torch's, all work runs in
+libtss.so (tss_paged_*, tss_pages_*).
+
+``PagePool`` keeps the books of pages of any content (page table, pages held, reference counts, all on the
+device); ``Kv4Cache`` appends to, reads and attends over pages held in 4 bits.  Both work on the caller's
+tensors; ``Kv4Cache.allocate`` makes a set that fits together.
+"""
+from __future__ import annotations
+
+import ctypes
+import math
+from typing import Optional, Sequence
+
+import torch
+
+from . import native
+from .native import _P, _i32, _ptr, _rows, check, lib
+
+PAGE_TOKENS = native.PAGE_TOKENS
+
+
+def page_bytes(n_kv_heads: int, head_dim: int) -> int:
+    """Bytes of one 4-bit page (64 tokens of every KV head of one layer)."""
+    n = lib().tss_paged_page_bytes(n_kv_heads, head_dim)
+    if n == 0:
+        raise ValueError(f"no 4-bit page for {n_kv_heads} heads of {head_dim}")
+    return n
+
+
+def pages_for(tokens: int) -> int:
+    return -(-int(tokens) // PAGE_TOKENS)
+
+
+def _ints(t: torch.Tensor, shape, what: str) -> None:
+    if tuple(t.shape) != tuple(shape) or t.dtype != torch.int32 or not t.is_contiguous():
+        raise ValueError(f"{what}: contiguous int32 {list(shape)} is wanted")
+
+
+def _layers(pool: torch.Tensor):
+    """(array of each layer's address, layers, pages, bytes of a page) of a tensor [layers][pages][...]."""
+    if pool.dim() < 3 or not pool.is_contiguous():
+        raise ValueError("pool: contiguous [layers][pages][...] is wanted")
+    n, step = pool.shape[0], pool.stride(0) * pool.element_size()
+    ptrs = (_P * n)(*[pool.data_ptr() + i * step for i in range(n)])
+    return ptrs, n, pool.shape[1], pool.stride(1) * pool.element_size()
+
+
+class PagePool:
+    """Page table [seqs][max_pages], pages held [seqs] and reference counts [pages] (int32, on the GPU) of a
+    pool [layers][pages][...].  Calls are enqueued on torch's current stream (or `stream`); a failure that
+    only the device sees is reported by sync_status()."""
+
+    def __init__(self, pool: torch.Tensor, table: torch.Tensor, held: torch.Tensor, refs: torch.Tensor):
+        self._ptrs, self.n_layers, self.n_pages, self.page_bytes = _layers(pool)
+        if table.dim() != 2:
+            raise ValueError("table: int32 [seqs][max_pages] is wanted")
+        self.n_seqs, self.max_pages = table.shape
+        _ints(table, (self.n_seqs, self.max_pages), "table")
+        _ints(held, (self.n_seqs,), "held")
+        _ints(refs, (self.n_pages,), "refs")
+        self.pool, self.table, self.held, self.refs = pool, table, held, refs
+        self._tables = native.TssPageTables(table.data_ptr(), held.data_ptr(), refs.data_ptr())
+        h = _P()
+        check(lib().tss_pages_create(self.n_seqs, self.max_pages, self.n_pages, ctypes.byref(h)), "tss_pages_create")
+        self._h = h
+
+    def close(self) -> None:
+        if getattr(self, "_h", None):
+            lib().tss_pages_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _stream(self, stream):
+        return native.current_stream() if stream is None else stream
+
+    def reserve(self, seqs: Sequence[int], tokens: Sequence[int], stream=None) -> None:
+        """Pages for tokens[i] tokens of seqs[i] (those it holds stay)."""
+        if len(seqs) != len(tokens):
+            raise ValueError("seqs and tokens differ in length")
+        check(lib().tss_pages_reserve(self._h, ctypes.byref(self._tables), len(seqs), _i32(seqs),
+                                      _i32([pages_for(t) for t in tokens]), self._stream(stream)), "tss_pages_reserve")
+
+    def free(self, seqs: Sequence[int], tokens: Optional[Sequence[int]] = None, stream=None) -> None:
+        """Give back the pages of seqs[i] past its first tokens[i] tokens (None: all)."""
+        if tokens is not None and len(seqs) != len(tokens):
+            raise ValueError("seqs and tokens differ in length")
+        keep = _i32([pages_for(t) for t in tokens]) if tokens is not None else None
+        check(lib().tss_pages_free(self._h, ctypes.byref(self._tables), len(seqs), _i32(seqs), keep, self._stream(stream)),
+              "tss_pages_free")
+
+    def fork(self, src: Sequence[int], dst: Sequence[int], tokens: Sequence[int], stream=None) -> None:
+        """dst[i] (which holds nothing) becomes the first tokens[i] tokens of src[i]: full pages are shared, a
+        part-filled last one is copied."""
+        n = len(src)
+        if len(dst) != n or len(tokens) != n:
+            raise ValueError("src, dst and tokens differ in length")
+        check(lib().tss_pages_fork(self._h, ctypes.byref(self._tables), self._ptrs, self.n_layers, self.page_bytes, n, _i32(src),
+                                   _i32(dst), _i32([int(t) // PAGE_TOKENS for t in tokens]),
+                                   _i32([pages_for(t) for t in tokens]), self._stream(stream)), "tss_pages_fork")
+
+    def compact(self, table_out: Optional[torch.Tensor] = None, refs_out: Optional[torch.Tensor] = None, stream=None) -> None:
+        """Move the pages in use to the lowest ids; the new table and counts replace the pool's, or go to the
+        given tensors."""
+        t, r = (self.table if table_out is None else table_out), (self.refs if refs_out is None else refs_out)
+        _ints(t, self.table.shape, "table_out")
+        _ints(r, self.refs.shape, "refs_out")
+        check(lib().tss_pages_compact(self._h, ctypes.byref(self._tables), t.data_ptr(), r.data_ptr(), self._ptrs, self.n_layers,
+                                      self.page_bytes, self._stream(stream)), "tss_pages_compact")
+
+    def copy(self, src: torch.Tensor, dst: torch.Tensor, stream=None) -> None:
+        """Copy page src[i] over page dst[i] in every layer (int32 tensors on the GPU)."""
+        _ints(src, (src.numel(),), "src")
+        _ints(dst, (src.numel(),), "dst")
+        check(lib().tss_pages_copy(self._h, self._ptrs, self.n_layers, self.page_bytes, src.numel(), _ptr(src), _ptr(dst),
+                                   self._stream(stream)), "tss_pages_copy")
+
+    def sync_status(self, stream=None) -> int:
+        return lib().tss_pages_sync_status(self._h, self._stream(stream))
+
+
+class Kv4Cache:
+    """A KV cache in 4 bits: pool uint8 [layers][pages][page bytes], table int32 [seqs][max_pages]."""
+
+    def __init__(self, pool: torch.Tensor, table: torch.Tensor, *, n_q_heads: int, n_kv_heads: int, head_dim: int):
+        if pool.dtype != torch.uint8 or pool.dim() != 3 or pool.shape[2] != page_bytes(n_kv_heads, head_dim):
+            raise ValueError("pool: uint8 [layers][pages][page bytes] is wanted")
+        if table.dim() != 2:
+            raise ValueError("table: int32 [seqs][max_pages] is wanted")
+        _ints(table, table.shape, "table")
+        self.n_q_heads, self.n_kv_heads, self.head_dim = n_q_heads, n_kv_heads, head_dim
+        self.pool, self.table = pool, table
+        self._ptrs, n_layers, n_pages, _ = _layers(pool)
+        self._cache = native.TssPagedCache(ctypes.cast(self._ptrs, ctypes.POINTER(_P)), n_layers, n_pages, table.data_ptr(),
+                                           table.shape[0], table.shape[1])
+        self.pages: Optional[PagePool] = None
+        h = _P()
+        check(lib().tss_paged_create(n_q_heads, n_kv_heads, head_dim, ctypes.byref(h)), "tss_paged_create")
+        self._h = h
+
+    @classmethod
+    def allocate(cls, *, n_layers: int, n_pages: int, n_seqs: int, max_pages: int, n_q_heads: int, n_kv_heads: int,
+                 head_dim: int, device: str = "cuda") -> "Kv4Cache":
+        """An empty cache with its page books (the result's `pages`)."""
+        pool = torch.zeros((n_layers, n_pages, page_bytes(n_kv_heads, head_dim)), dtype=torch.uint8, device=device)
+        table = torch.full((n_seqs, max_pages), -1, dtype=torch.int32, device=device)
+        c = cls(pool, table, n_q_heads=n_q_heads, n_kv_heads=n_kv_heads, head_dim=head_dim)
+        c.pages = PagePool(pool, table, torch.zeros(n_seqs, dtype=torch.int32, device=device),
+                           torch.zeros(n_pages, dtype=torch.int32, device=device))
+        return c
+
+    def close(self) -> None:
+        if self.pages is not None:
+            self.pages.close()
+        if getattr(self, "_h", None):
+            lib().tss_paged_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    @staticmethod
+    def batch(seqs: Sequence[int], first: Sequence[int], n_tokens: Sequence[int]) -> native.TssPagedBatch:
+        """Request i is the tokens [first[i], first[i] + n_tokens[i]) of sequence seqs[i]."""
+        if not len(seqs) == len(first) == len(n_tokens):
+            raise ValueError("seqs, first and n_tokens differ in length")
+        keep = [_i32(seqs), _i32(first), _i32(n_tokens)]
+        b = native.TssPagedBatch(len(seqs), *[ctypes.cast(a, _P) for a in keep])
+        b._keep = keep
+        b.rows = sum(int(n) for n in n_tokens)
+        return b
+
+    def _kv(self, t: torch.Tensor, batch, what: str) -> int:
+        n, h, d, stride = _rows(t, what)
+        if (n, h, d) != (batch.rows, self.n_kv_heads, self.head_dim):
+            raise ValueError(f"{what}: [{batch.rows}][{self.n_kv_heads}][{self.head_dim}] is wanted")
+        return stride
+
+    def append(self, layer: int, batch, k: torch.Tensor, v: torch.Tensor, stream=None) -> None:
+        """Quantise k, v [rows][kv heads][head_dim] into the pages of the batch's tokens."""
+        if k.dtype != v.dtype:
+            raise ValueError("k and v differ in type")
+        check(lib().tss_paged_append(self._h, ctypes.byref(self._cache), layer, ctypes.byref(batch), k.data_ptr(), v.data_ptr(),
+                                     self._kv(k, batch, "k"), self._kv(v, batch, "v"), native.dtype_code(k),
+                                     native.current_stream() if stream is None else stream), "tss_paged_append")
+
+    def read(self, layer: int, batch, k: Optional[torch.Tensor], v: Optional[torch.Tensor], stream=None) -> None:
+        """The values that the batch's tokens are held as, to k and v (either may be None)."""
+        one = k if k is not None else v
+        if one is None or (k is not None and v is not None and k.dtype != v.dtype):
+            raise ValueError("k or v is wanted, of one type")
+        strides = [self._kv(t, batch, w) if t is not None else 0 for t, w in ((k, "k"), (v, "v"))]
+        check(lib().tss_paged_read(self._h, ctypes.byref(self._cache), layer, ctypes.byref(batch), _ptr(k), _ptr(v), *strides,
+                                   native.dtype_code(one), native.current_stream() if stream is None else stream),
+              "tss_paged_read")
+
+    def attention(self, layer: int, batch, q: torch.Tensor, out: torch.Tensor, lse: Optional[torch.Tensor] = None, *,
+                  scale: Optional[float] = None, window: int = 0, sinks: int = 0, mask: Optional[torch.Tensor] = None,
+                  positions: Optional[torch.Tensor] = None, stream=None) -> None:
+        """Attention of the batch's rows (already appended) over their sequences: q, out [rows][heads][head_dim];
+        lse float32 [rows][heads]; mask int64 [rows][2] (bits of the block's rows that a row sees; None: a chain);
+        window and sinks as in tss_paged_attention, positions int32 [rows]."""
+        n, h, d, stride = _rows(q, "q")
+        if (n, h, d) != (batch.rows, self.n_q_heads, self.head_dim):
+            raise ValueError(f"q: [{batch.rows}][{self.n_q_heads}][{self.head_dim}] is wanted")
+        if out.shape != q.shape or out.dtype != q.dtype or out.device != q.device:
+            raise ValueError("out: the shape, type and device of q are wanted")
+        if lse is not None and (tuple(lse.shape) != (n, h) or lse.dtype != torch.float32 or not lse.is_contiguous()):
+            raise ValueError("lse: contiguous float32 [rows][heads] is wanted")
+        if mask is not None and (tuple(mask.shape) != (n, 2) or mask.dtype not in (torch.int64, torch.uint64)
+                                 or not mask.is_contiguous()):
+            raise ValueError("mask: contiguous 64-bit [rows][2] is wanted")
+        if positions is not None:
+            _ints(positions, (n,), "positions")
+        a = native.TssPagedAttn(q.data_ptr(), stride, out.data_ptr(), _rows(out, "out")[3], _ptr(lse), native.dtype_code(q),
+                                1.0 / math.sqrt(d) if scale is None else scale, window, sinks, _ptr(mask), _ptr(positions))
+        check(lib().tss_paged_attention(self._h, ctypes.byref(self._cache), layer, ctypes.byref(batch), ctypes.byref(a),
+                                        native.current_stream() if stream is None else stream), "tss_paged_attention")
+
+    def sync_status(self, stream=None) -> int:
+        return lib().tss_paged_sync_status(self._h, native.current_stream() if stream is None else stream)
