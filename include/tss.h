@@ -547,7 +547,7 @@ tss_status tss_paged_read(tss_paged* p, const tss_paged_cache* cache, int layer,
  *   lse: DEVICE fp32 [rows][n_q_heads] or NULL: ln sum exp(scale q.k) over the keys seen.
  * A row that sees nothing gets zeros and lse = -infinity.  Values of keys that a row does not see do not
  * reach it, whatever they are.  Scores, sums and accumulators are fp32; the weights enter the second
- * product as fp16.  Asynchronous on `stream`.  Errors: INVALID_ARG, KV_CAPACITY, CUDA. */
+ * product as two fp16 parts (22 bits).  Asynchronous on `stream`.  Errors: INVALID_ARG, KV_CAPACITY, CUDA. */
 typedef struct {
   const void* q;
   int64_t q_stride;

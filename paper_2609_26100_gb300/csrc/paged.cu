@@ -347,8 +347,14 @@ extern "C" tss_status tss_paged_create(int n_q_heads, int n_kv_heads, int head_d
   h->hk = n_kv_heads;
   h->d = head_dim;
   h->sms = sms;
-  cudaError_t e = cudaMalloc(&h->status, 256);
+  const size_t rows = pa_partial_rows(sms);
+  cudaError_t e = pa_prepare_all();
+  if (e == cudaSuccess) e = cudaMalloc(&h->status, 256);
   if (e == cudaSuccess) e = cudaMemset(h->status, 0, 256);
+  if (e == cudaSuccess) e = cudaMalloc(&h->part_o, rows * head_dim * sizeof(float));
+  if (e == cudaSuccess) e = cudaMalloc(&h->part_ml, rows * sizeof(float2));
+  if (e == cudaSuccess) e = cudaMalloc(&h->counters, sms * sizeof(int));
+  if (e == cudaSuccess) e = cudaMemset(h->counters, 0, sms * sizeof(int));
   if (e != cudaSuccess) {
     tss_paged_destroy(h);
     const tss_status r = refuse_cuda(e, "workspace");
@@ -361,6 +367,9 @@ extern "C" tss_status tss_paged_create(int n_q_heads, int n_kv_heads, int head_d
 extern "C" void tss_paged_destroy(tss_paged* h) {
   if (!h) return;
   cudaFree(h->status);
+  cudaFree(h->part_o);
+  cudaFree(h->part_ml);
+  cudaFree(h->counters);
   delete h;
 }
 
@@ -425,6 +434,8 @@ extern "C" tss_status tss_paged_attention(tss_paged* h, const tss_paged_cache* c
   p.mask = reinterpret_cast<const unsigned long long*>(a->mask);
   p.positions = a->window ? a->positions : nullptr;
   p.status = h->status;
-  const cudaError_t e = launch_paged_attention(h, p, static_cast<int>(rows), static_cast<cudaStream_t>(stream));
+  bool too_large = false;
+  const cudaError_t e = launch_paged_attention(h, p, static_cast<cudaStream_t>(stream), &too_large);
+  if (too_large) return refuse(TSS_ERR_INVALID_ARG, "more than 2^30 (page, head, row tile) units in one call");
   return e == cudaSuccess ? TSS_OK : refuse_cuda(e, "launch");
 }

@@ -6,7 +6,10 @@
 // (opaque in tss.h)
 struct tss_paged {
   int hq, hk, d, sms;
-  int* status;  // device
+  int* status;      // device
+  float* part_o;    // device: partial results of items that several CTAs share
+  float2* part_ml;
+  int* counters;    // device [sms], zero between launches
 };
 
 namespace tss {
@@ -26,6 +29,9 @@ struct PgAttnParams {
   int* status;
   PgBatch batch;
 };
-cudaError_t launch_paged_attention(const tss_paged* h, const PgAttnParams& p, int rows, cudaStream_t s);
+size_t pa_partial_rows(int sms);
+cudaError_t pa_prepare_all();
+// *too_large: more work than one launch counts (nothing was launched).
+cudaError_t launch_paged_attention(const tss_paged* h, const PgAttnParams& p, cudaStream_t s, bool* too_large);
 
 }  // namespace tss
