@@ -252,6 +252,7 @@ tss_status take_batch(const tss_paged* h, const tss_paged_cache* c, int layer, c
   if (!c->layer || c->n_layers < 1 || layer < 0 || layer >= c->n_layers)
     return refuse(TSS_ERR_INVALID_ARG, "layer must be in [0, n_layers)");
   if (!c->layer[layer] || !aligned16(c->layer[layer])) return refuse(TSS_ERR_INVALID_ARG, "the layer's pages must be 16-byte aligned device memory");
+  if (static_cast<long long>(c->n_pages) * h->hk >= 1 << 30) return refuse(TSS_ERR_INVALID_ARG, "n_pages * n_kv_heads must be below 2^30");
   if (!c->table || c->n_pages < 1 || c->n_seqs < 1 || c->max_pages < 1 || c->max_pages > (1 << 24))
     return refuse(TSS_ERR_INVALID_ARG, "the cache needs a table, n_pages and n_seqs >= 1 and max_pages in [1, 2^24]");
   if (b->n_req < 1 || b->n_req > kPgMaxReq) return refuse(TSS_ERR_INVALID_ARG, "n_req must be in [1, 64]");
@@ -353,8 +354,8 @@ extern "C" tss_status tss_paged_create(int n_q_heads, int n_kv_heads, int head_d
   if (e == cudaSuccess) e = cudaMemset(h->status, 0, 256);
   if (e == cudaSuccess) e = cudaMalloc(&h->part_o, rows * head_dim * sizeof(float));
   if (e == cudaSuccess) e = cudaMalloc(&h->part_ml, rows * sizeof(float2));
-  if (e == cudaSuccess) e = cudaMalloc(&h->counters, sms * sizeof(int));
-  if (e == cudaSuccess) e = cudaMemset(h->counters, 0, sms * sizeof(int));
+  if (e == cudaSuccess) e = cudaMalloc(&h->counters, pa_counters(sms) * sizeof(int));
+  if (e == cudaSuccess) e = cudaMemset(h->counters, 0, pa_counters(sms) * sizeof(int));
   if (e != cudaSuccess) {
     tss_paged_destroy(h);
     const tss_status r = refuse_cuda(e, "workspace");
@@ -397,14 +398,15 @@ extern "C" tss_status tss_paged_read(tss_paged* h, const tss_paged_cache* cache,
 
 extern "C" tss_status tss_paged_attention(tss_paged* h, const tss_paged_cache* cache, int layer, const tss_paged_batch* batch,
                                           const tss_paged_attn* a, void* stream) {
-  PgAttnParams p{};
+  PgAttnArgs p{};
+  PgBatch b;
   long long rows = 0;
-  const tss_status st = take_batch(h, cache, layer, batch, &p.batch, &rows);
+  const tss_status st = take_batch(h, cache, layer, batch, &b, &rows);
   if (st != TSS_OK) return st;
   if (!a) return refuse(TSS_ERR_INVALID_ARG, "NULL argument");
   if (a->dtype != TSS_DTYPE_BF16 && a->dtype != TSS_DTYPE_F16) return refuse(TSS_ERR_INVALID_ARG, "dtype must be bf16 or fp16");
-  for (int i = 0; i < p.batch.n_req; ++i)
-    if (p.batch.r[i].n > kPgMaxRows) return refuse(TSS_ERR_INVALID_ARG, "a request's block has more than 128 rows");
+  for (int i = 0; i < b.n_req; ++i)
+    if (b.r[i].n > kPgMaxRows) return refuse(TSS_ERR_INVALID_ARG, "a request's block has more than 128 rows");
   if (!(a->scale > 0.f) || !(a->scale < INFINITY)) return refuse(TSS_ERR_INVALID_ARG, "scale must be positive and finite");
   if (a->window < 0 || a->n_sinks < 0) return refuse(TSS_ERR_INVALID_ARG, "window and n_sinks must be >= 0");
   if (rows == 0) return TSS_OK;
@@ -435,7 +437,7 @@ extern "C" tss_status tss_paged_attention(tss_paged* h, const tss_paged_cache* c
   p.positions = a->window ? a->positions : nullptr;
   p.status = h->status;
   bool too_large = false;
-  const cudaError_t e = launch_paged_attention(h, p, static_cast<cudaStream_t>(stream), &too_large);
+  const cudaError_t e = launch_paged_attention(h, p, b, static_cast<cudaStream_t>(stream), &too_large);
   if (too_large) return refuse(TSS_ERR_INVALID_ARG, "more than 2^30 (page, head, row tile) units in one call");
   return e == cudaSuccess ? TSS_OK : refuse_cuda(e, "launch");
 }

@@ -9,12 +9,12 @@ struct tss_paged {
   int* status;      // device
   float* part_o;    // device: partial results of items that several CTAs share
   float2* part_ml;
-  int* counters;    // device [sms], zero between launches
+  int* counters;    // device [pa_counters], zero between launches
 };
 
 namespace tss {
 
-struct PgAttnParams {
+struct PgAttnArgs {
   int hq, hk, d, n_pages, max_pages;
   const uint8_t* pool;      // the layer's pages
   const int* table;
@@ -27,11 +27,11 @@ struct PgAttnParams {
   const unsigned long long* mask;
   const int* positions;
   int* status;
-  PgBatch batch;
 };
 size_t pa_partial_rows(int sms);
+int pa_counters(int sms);
 cudaError_t pa_prepare_all();
 // *too_large: more work than one launch counts (nothing was launched).
-cudaError_t launch_paged_attention(const tss_paged* h, const PgAttnParams& p, cudaStream_t s, bool* too_large);
+cudaError_t launch_paged_attention(const tss_paged* h, const PgAttnArgs& a, const PgBatch& batch, cudaStream_t s, bool* too_large);
 
 }  // namespace tss

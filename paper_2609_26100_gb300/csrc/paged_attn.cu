@@ -19,10 +19,11 @@
 // need no reduction over tokens.  In terms of p s' rather than p, it keeps the weights in fp16's range
 // whatever the values' scales.
 //
-// Work split: the pages of all (request, row tile, KV head) items laid end to end and cut evenly, one CTA
-// per SM.  A CTA's pages go round its warps, each with its own ring of bulk copies (a page of a head is one
-// contiguous block, 9 KiB at head_dim 128).  At an item's end the warps' parts are joined in shared memory;
-// items that several CTAs share leave partials, which the last one to arrive joins in CTA order.
+// Work split.  A unit is 32 tokens (half a page) of one item: a request's row tile and KV head.  CTAs of
+// four warps, three to an SM (two with 16 rows), take runs of units; a run's units go round its warps,
+// each with its own ring of bulk copies.  Several small CTAs rather than one: while one ends an item the
+// others stream.  At an item's end the warps' parts are joined in shared memory; items that several CTAs
+// share leave partials, which the last CTA to arrive joins in CTA order (results do not depend on timing).
 #include <type_traits>
 
 #include "paged.h"
@@ -32,12 +33,16 @@ namespace {
 
 struct PaReq {
   int seq, first, n, row;
-  int pages, sink, lo;   // pages in sight: [0, sink) and [lo, ...); their number
-  int off;               // units (page, head, row tile) before the request
+  int units;             // of one item: those in sight, [0, sink) and [lo, ...)
+  int sink, lo;
+  int off;               // units of all items before the request
+  int cta, splits;       // aligned runs: CTAs before the request, CTAs of one item
 };
 struct PaParams {
-  PgAttnParams a;        // (batch unused)
+  PgAttnArgs a;
   int n_req, total;      // units in all
+  int aligned;           // a CTA's run lies within one item
+  int halves;            // 32-token halves of a unit: 2 (a page) or 1
   float* part_o;         // [grid][2][rows][D]
   float2* part_ml;       // [grid][2][rows]
   int* counters;         // [grid], zero between launches
@@ -55,20 +60,51 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
+// d = a b (mma_f16_16816 without an accumulator to clear)
+__device__ __forceinline__ void mma_f16_first(float* d, const uint32_t* a, const uint32_t* b) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+      "{%10, %10, %10, %10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]), "f"(0.f));
+}
+
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n\t.reg .b64 x, y, z, w;\n\t"
+      "mov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
+      "fma.rn.f32x2 w, x, y, z;\n\t"
+      "mov.b64 {%0, %1}, w;\n\t}\n"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 x, y, w;\n\t"
+      "mov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t"
+      "add.rn.f32x2 w, x, y;\n\t"
+      "mov.b64 {%0, %1}, w;\n\t}\n"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
 constexpr float kTop = 32768.f;         // p s' that raises the reference
 constexpr float kLeast = 5.9604645e-8f; // fp16's smallest scale
 
+// A ring stage holds a page's block (or half of each of its parts).
 template <int D, int NT>
 struct PaShape {
   static constexpr int kRows = 8 * NT;
-  static constexpr int kWarps = NT == 1 ? 12 : 8;
+  static constexpr int kWarps = 4;
+  static constexpr int kCtas = NT == 1 ? 3 : 2;  // resident on an SM
   static constexpr int kStages = NT == 1 ? 2 : 3;
-  static constexpr int kRing = kWarps * kStages * PgBlock<D>::kBytes;
-  static constexpr size_t kSmem = kRing + 128;
+  static constexpr size_t kSmem = kWarps * kStages * PgBlock<D>::kBytes;
 };
 
 // Whether row i (position qp, mask words anc or null) of request r sees key j.
-__device__ __forceinline__ bool sees(const PgAttnParams& a, const PaReq& r, int i, int qp, const unsigned long long* anc, int j) {
+__device__ __forceinline__ bool sees(const PgAttnArgs& a, const PaReq& r, int i, int qp, const unsigned long long* anc, int j) {
   if (j >= r.first + r.n) return false;
   int kp = j;
   if (j >= r.first) {
@@ -80,34 +116,43 @@ __device__ __forceinline__ bool sees(const PgAttnParams& a, const PaReq& r, int 
 }
 
 template <int D, int NT>
-__global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, 1) paged_attn_kernel(const __grid_constant__ PaParams p) {
+__global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::kCtas) paged_attn_kernel(const __grid_constant__ PaParams p) {
   using B = PgBlock<D>;
   using S = PaShape<D, NT>;
   constexpr int G = B::kGroups, W = S::kWarps, ST = S::kStages, R = S::kRows, DB = D / 32;
-  extern __shared__ uint8_t pa_dyn[];
+  extern __shared__ __align__(128) uint8_t pa_dyn[];
   __shared__ uint64_t bars[W][ST];
-  __shared__ int s_off[kPgMaxReq], s_pages[kPgMaxReq], s_sink[kPgMaxReq], s_lo[kPgMaxReq], s_seq[kPgMaxReq];
+  __shared__ int s_off[kPgMaxReq];
   __shared__ float2 s_ml[W][R];
-  __shared__ int s_has[W], abort_s, s_last;
+  __shared__ int s_has[W], abort_s, s_last;  // s_has: the stage of a warp's part, plus one; 0 without
+  __shared__ __align__(16) float s_x[W][D];  // parts of rows that several warps gather from other CTAs' partials
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
-  uint8_t* ring_all = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(pa_dyn) + 127) & ~uintptr_t(127));
-  uint8_t* ring = ring_all + warp * (ST * B::kBytes);
-  const PgAttnParams& a = p.a;
-  const int gq = a.hq / a.hk;
-  const int u0 = static_cast<int>(static_cast<long long>(p.total) * blockIdx.x / gridDim.x);
-  const int u1 = static_cast<int>(static_cast<long long>(p.total) * (blockIdx.x + 1) / gridDim.x);
-  if (tid < p.n_req) {
-    s_off[tid] = p.r[tid].off;
-    s_pages[tid] = p.r[tid].pages;
-    s_sink[tid] = p.r[tid].sink;
-    s_lo[tid] = p.r[tid].lo;
-    s_seq[tid] = p.r[tid].seq;
-  }
+  uint8_t* ring = pa_dyn + warp * (ST * B::kBytes);
+  const PgAttnArgs& a = p.a;
+  const int gq = a.hq / a.hk, halves = p.halves, unit = 32 * halves;  // tokens of a unit
+  if (tid < p.n_req) s_off[tid] = p.r[tid].off;
   if (lane == 0)
     for (int i = 0; i < ST; ++i) mbar_init(&bars[warp][i], 1);
   if (tid == 0) abort_s = 0;
   fence_mbar_init();
+  // the CTA's run of units [u0, u1)
+  int u0, u1, first_cta = 0, splits = 0;  // (of an aligned run: its item's CTAs)
+  if (p.aligned) {
+    int b = 0;
+    while (b + 1 < p.n_req && p.r[b + 1].cta <= static_cast<int>(blockIdx.x)) ++b;
+    const PaReq& r = p.r[b];
+    const int c = blockIdx.x - r.cta, item = c / r.splits, j = c - item * r.splits, at = r.off + item * r.units;
+    u0 = at + static_cast<int>(static_cast<long long>(r.units) * j / r.splits);
+    u1 = at + static_cast<int>(static_cast<long long>(r.units) * (j + 1) / r.splits);
+    first_cta = blockIdx.x - j;
+    splits = r.splits;
+  } else {
+    u0 = static_cast<int>(static_cast<long long>(p.total) * blockIdx.x / gridDim.x);
+    u1 = static_cast<int>(static_cast<long long>(p.total) * (blockIdx.x + 1) / gridDim.x);
+  }
   __syncthreads();
+  griddep_wait();    // (nothing before this reads or writes what another kernel may)
+  griddep_launch();
   volatile int* abort = &abort_s;
 
   const int mine = u0 + warp < u1 ? (u1 - u0 - warp + W - 1) / W : 0;  // the warp's units: u0 + warp + k W
@@ -118,59 +163,67 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, 1) paged_attn_ker
       if (b + s < p.n_req && s_off[b + s] <= u) b += s;
     return b;
   };
-  // Lane l: block of unit k0 + l in the pool; -1 where the table names no page, -2 past the end.
-  const auto blocks_from = [&](int k0) -> long long {
+  // Lane l: half block of unit k0 + l in the pool; -1 where the table names no page, -2 past the end.
+  const auto blocks_from = [&](int k0) -> int {
     if (k0 + lane >= mine) return -2;
     const int u = u0 + warp + (k0 + lane) * W, b = request_of(u), v = u - s_off[b];
-    const int item = v / s_pages[b], pg = v - item * s_pages[b];
-    const int h = item % a.hk, at = pg < s_sink[b] ? pg : pg - s_sink[b] + s_lo[b];
-    const int page = __ldg(a.table + static_cast<long long>(s_seq[b]) * a.max_pages + at);
+    const PaReq& r = p.r[b];
+    const int item = v / r.units, x = v - item * r.units;
+    const int h = item % a.hk, at = x < r.sink ? x : x - r.sink + r.lo;
+    const int half = halves == 1 ? at & 1 : 0;
+    const int page = __ldg(a.table + static_cast<long long>(r.seq) * a.max_pages + (halves == 1 ? at >> 1 : at));
     if (page < 0 || page >= a.n_pages) {
       report(a.status, kStatusCheck);
       return -1;
     }
-    return static_cast<long long>(page) * a.hk + h;
+    return (page * a.hk + h) * 2 + half;  // (below 2^31: the host checks)
   };
-  long long ids = blocks_from(0), ids_next = blocks_from(32);
-  int ids_at = 0, issued = 0;
+  int ids = blocks_from(0), ids_next = -2;
+  int issued = 0, issue_at = 0;  // units asked for, the stage of the next
   uint32_t no_page = 0;  // bit s: stage s's unit has no page
+  // a unit's copies: lane 0 K codes, 1 V codes, 2 K parameters, 3 V parameters
+  const int piece_half = (lane < 2 ? B::kCodes : B::kParams) / 2, piece = piece_half * halves;
+  const int piece_at = lane < 2 ? lane * B::kCodes : B::kKParams + (lane - 2) * B::kParams;
   const auto issue = [&]() {  // the warp's next unit into stage issued % ST
     if (issued >= mine) return;
-    if (issued - ids_at == 32) {
-      ids = ids_next;
-      ids_at += 32;
-      ids_next = blocks_from(ids_at + 32);
+    if ((issued & 31) == 0) {
+      if (issued > 0) ids = ids_next;
+      ids_next = blocks_from(issued + 32);
     }
-    const long long blk = __shfl_sync(0xffffffffu, ids, issued - ids_at);
-    const int s = issued % ST;
+    const int blk = __shfl_sync(0xffffffffu, ids, issued & 31), s = issue_at;
+    issue_at = s + 1 == ST ? 0 : s + 1;
     if (blk < 0) {
       no_page |= 1u << s;
       if (lane == 0) mbar_arrive(&bars[warp][s]);
     } else {
       no_page &= ~(1u << s);
-      if (lane == 0) {
-        mbar_arrive_expect_tx(&bars[warp][s], B::kBytes);
-        bulk_load(ring + s * B::kBytes, a.pool + blk * B::kBytes, B::kBytes, &bars[warp][s]);
-      }
+      uint64_t* bar = &bars[warp][s];
+      if (lane == 0) mbar_arrive_expect_tx(bar, B::kBytes / 2 * halves);
+      __syncwarp();
+      if (lane < 4)
+        bulk_load(ring + s * B::kBytes + piece_at, a.pool + static_cast<long long>(blk >> 1) * B::kBytes + piece_at + (blk & 1) * piece_half, piece,
+                  bar);
     }
     ++issued;
   };
 #pragma unroll
   for (int i = 0; i < ST; ++i) issue();
 
-  int done = 0;  // the warp's units processed
+  int done = 0, stage = 0;  // the warp's units so far, the stage of the next
+  uint32_t parity = 0;
   bool ok = true;
   for (int u = u0; u < u1;) {
-    // ---- a segment: this CTA's pages [pg0, pg1) of an item ----
+    // ---- a segment: this CTA's units [x0, x1) of an item ----
     const int b = request_of(u);
     const PaReq& r = p.r[b];
-    const int v = u - r.off, item = v / r.pages, pg0 = v - item * r.pages;
-    const int seg_end = min(u1, u - pg0 + r.pages), pg1 = pg0 + seg_end - u;
+    const int v = u - r.off, item = v / r.units, x0 = v - item * r.units;
+    const int seg_end = min(u1, u - x0 + r.units), x1 = x0 + seg_end - u;
     const int h = item % a.hk, row0 = item / a.hk * R, rows = min(R, r.n * gq - row0);
     // Q: thread (g, t) holds row g's dims 64 gi + 16 t .. + 15 as the operand of 4 k-steps a group: pairs
     // (0, 4), (1, 5) and (2, 6), (3, 7) of each 8 dims, odd ones / 16 (their codes stand four bits up)
     uint32_t qf[NT][G][2][4];
-    float f[NT][2], zq[NT][G][2], ref[NT][2], l[NT][2], oz[NT][G][2], o[NT][DB][2][4];
+    float2 f2[NT], ref2[NT], l2[NT];  // (of rows 2t and 2t + 1; the reference negated)
+    float zq[NT][G][2], oz[NT][G][2], o[NT][DB][2][4];
     int pmax = 0;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
@@ -205,7 +258,7 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, 1) paged_attn_ker
         for (int i = 0; i < 16; ++i) sum[gi] += x[gi][i];
         sum[gi] += __shfl_xor_sync(0xffffffffu, sum[gi], 1);
         sum[gi] += __shfl_xor_sync(0xffffffffu, sum[gi], 2);
-        sum[gi] *= a.scale_log2;
+        sum[gi] *= up * 5.9604645e-8f;  // (f times this is scale_log2)
 #pragma unroll
         for (int w = 0; w < 2; ++w)
 #pragma unroll
@@ -215,18 +268,16 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, 1) paged_attn_ker
           }
       }
       // the accumulators' rows of a thread are 2t and 2t + 1
+      f2[nt] = make_float2(__shfl_sync(0xffffffffu, mul, 8 * t), __shfl_sync(0xffffffffu, mul, 8 * t + 4));
+      ref2[nt] = make_float2(INFINITY, INFINITY);
+      l2[nt] = make_float2(0.f, 0.f);
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int from = (2 * t + i) * 4;
-        f[nt][i] = __shfl_sync(0xffffffffu, mul, from);
+      for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int gi = 0; gi < G; ++gi) {
-          zq[nt][gi][i] = __shfl_sync(0xffffffffu, sum[gi], from);
+          zq[nt][gi][i] = __shfl_sync(0xffffffffu, sum[gi], 8 * t + 4 * i);
           oz[nt][gi][i] = 0.f;
         }
-        ref[nt][i] = -INFINITY;
-        l[nt][i] = 0.f;
-      }
 #pragma unroll
       for (int x2 = 0; x2 < DB; ++x2)
 #pragma unroll
@@ -240,35 +291,37 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, 1) paged_attn_ker
 #pragma unroll
       for (int x2 = 16; x2 > 0; x2 >>= 1) pmax = max(pmax, __shfl_xor_sync(0xffffffffu, pmax, x2));
     }
+    // units whose keys every row sees: [0, all0), the sinks, and [all1, all2)
+    const int all0 = a.window ? min(r.sink, a.sinks / unit) : 0;
+    const int all1 = r.sink + (a.window ? max(0, (pmax - a.window + unit) / unit - r.lo) : 0);
+    const int all2 = r.sink + r.first / unit - r.lo;
     const int done0 = done;
-    for (int uu = u0 + warp + done * W; uu < seg_end; uu += W) {
-      if (done > 0 && ok) issue();  // into the stage of the unit before this one
-      const int s = done % ST;
-      ok = __all_sync(0xffffffffu, ok && mbar_wait(&bars[warp][s], (done / ST) & 1, abort, a.status));
+    for (int x = u0 + warp + done * W - u + x0; x < x1; x += W) {
+      if (done > 0) issue();  // into the stage of the unit before (every lane has read it: the last loop's end)
+      const int s = stage;
+      if (!__all_sync(0xffffffffu, mbar_try_wait(&bars[warp][s], parity))) {
+        ok = __all_sync(0xffffffffu, ok && mbar_wait(&bars[warp][s], parity, abort, a.status));
+        if (!ok) break;
+      }
       ++done;
-      if (!ok || (no_page >> s & 1u)) continue;
-      const int pg = uu - u + pg0, key0 = (pg < r.sink ? pg : pg - r.sink + r.lo) * kPgTokens;
-      const uint8_t* blk = ring + s * B::kBytes;
+      stage = s + 1 == ST ? 0 : s + 1;
+      parity ^= stage == 0;
+      const bool full = no_page == 0 && (x < all0 || (x >= all1 && x < all2));
+      if (no_page >> s & 1u) continue;
 #pragma unroll 1
-      for (int kg = 0; kg < 2; ++kg) {
-        const int kb = key0 + 32 * kg;
-        // every row sees all 32 keys?
-        const bool full = kb + 32 <= r.first && (!a.window || kb > pmax - a.window || kb + 32 <= a.sinks);
-        if (kb >= r.first + r.n) break;
-        float sc[NT][2][4];  // scores: [16-key tile][key g, rows 2t and 2t + 1; key g + 8, the same]
+      for (int kg = 0; kg < halves; ++kg) {
+        const uint8_t* blk = ring + s * B::kBytes;
+        const uint8_t *kcodes = blk + B::kK + kg * (B::kCodes / 2), *vcodes = blk + B::kV + kg * (B::kCodes / 2);
+        const __half2* kparams = reinterpret_cast<const __half2*>(blk + B::kKParams) + kg * 32 * G;
+        const __half2* vparams = reinterpret_cast<const __half2*>(blk + B::kVParams) + kg * 32 * G;
+        float sc[NT][2][4];  // scores / f: [16-key tile][key g, rows 2t and 2t + 1; key g + 8, the same]
 #pragma unroll
         for (int mt = 0; mt < 2; ++mt) {
           float acc[NT][G][4];
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int gi = 0; gi < G; ++gi)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) acc[nt][gi][i] = 0.f;
           uint32_t kw[2][G][2];
 #pragma unroll
           for (int x2 = 0; x2 < 2; ++x2) {
-            const uint8_t* kp = blk + B::kK + (kg * 32 + mt * 16 + x2 * 8 + g) * (D / 2) + t * (D / 8);
+            const uint8_t* kp = kcodes + (mt * 16 + x2 * 8 + g) * (D / 2) + t * (D / 8);
             if constexpr (G == 2) {
               const uint4 w = *reinterpret_cast<const uint4*>(kp);
               kw[x2][0][0] = w.x, kw[x2][0][1] = w.y, kw[x2][G - 1][0] = w.z, kw[x2][G - 1][1] = w.w;
@@ -286,14 +339,17 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, 1) paged_attn_ker
               const uint32_t a1[4] = {y0 & 0x000f000fu, y1 & 0x000f000fu, y0 & 0x00f000f0u, y1 & 0x00f000f0u};
 #pragma unroll
               for (int nt = 0; nt < NT; ++nt) {
-                mma_f16_16816(acc[nt][gi], a0, &qf[nt][gi][w][0]);
+                if (w == 0)
+                  mma_f16_first(acc[nt][gi], a0, &qf[nt][gi][w][0]);
+                else
+                  mma_f16_16816(acc[nt][gi], a0, &qf[nt][gi][w][0]);
                 mma_f16_16816(acc[nt][gi], a1, &qf[nt][gi][w][2]);
               }
             }
           // scores from the codes' sums
 #pragma unroll
           for (int x2 = 0; x2 < 2; ++x2) {
-            const __half2* pr = reinterpret_cast<const __half2*>(blk + B::kKParams) + (kg * 32 + mt * 16 + x2 * 8 + g) * G;
+            const __half2* pr = kparams + (mt * 16 + x2 * 8 + g) * G;
             float2 sz[G];
 #pragma unroll
             for (int gi = 0; gi < G; ++gi) sz[gi] = __half22float2(pr[gi]);
@@ -301,35 +357,37 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, 1) paged_attn_ker
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
               for (int i = 0; i < 2; ++i) {
-                float c = 0.f, z = 0.f;
+                float c = sz[0].x * acc[nt][0][2 * x2 + i];
+                if constexpr (G == 2) c = fmaf(sz[G - 1].x, acc[nt][G - 1][2 * x2 + i], c);
 #pragma unroll
-                for (int gi = 0; gi < G; ++gi) {
-                  c = fmaf(sz[gi].x, acc[nt][gi][2 * x2 + i], c);
-                  z = fmaf(sz[gi].y, zq[nt][gi][i], z);
-                }
-                sc[nt][mt][2 * x2 + i] = fmaf(c, f[nt][i], z);
+                for (int gi = 0; gi < G; ++gi) c = fmaf(sz[gi].y, zq[nt][gi][i], c);
+                sc[nt][mt][2 * x2 + i] = c;
               }
           }
         }
         float2 vz[2][2][G];
-        float smax[2][2];
+        float smax = kLeast;  // the largest scale among the thread's keys
 #pragma unroll
-        for (int mt = 0; mt < 2; ++mt)
+        for (int k = 0; k < 4; ++k) {
+          const __half2* pr = vparams + (k * 8 + g) * G;
 #pragma unroll
-          for (int x2 = 0; x2 < 2; ++x2) {
-            const __half2* pr = reinterpret_cast<const __half2*>(blk + B::kVParams) + (kg * 32 + mt * 16 + x2 * 8 + g) * G;
-            smax[mt][x2] = kLeast;
-#pragma unroll
-            for (int gi = 0; gi < G; ++gi) {
-              vz[mt][x2][gi] = __half22float2(pr[gi]);
-              smax[mt][x2] = fmaxf(smax[mt][x2], vz[mt][x2][gi].x);
-            }
+          for (int gi = 0; gi < G; ++gi) {
+            vz[k >> 1][k & 1][gi] = __half22float2(pr[gi]);
+            smax = fmaxf(smax, vz[k >> 1][k & 1][gi].x);
           }
+        }
+        const auto key_scale = [&](int mt, int x2) {
+          float x = kLeast;
+#pragma unroll
+          for (int gi = 0; gi < G; ++gi) x = fmaxf(x, vz[mt][x2][gi].x);
+          return x;
+        };
         uint32_t pf[NT][G][2][4];  // the weights times the values' scales, fp16 parts hi and lo, [8-key block]
         const auto weigh = [&](auto all) {
           constexpr bool kAll = decltype(all)::value;  // every (key, row) pair counts
           uint32_t vis = 0;  // else: bit nt * 8 + mt * 4 + (key half) * 2 + row
           if constexpr (!kAll) {
+            const int kb = (x < r.sink ? x : x - r.sink + r.lo) * unit + kg * 32;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -345,21 +403,25 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, 1) paged_attn_ker
               }
           }
           const auto on = [&](int nt, int mt, int i) { return kAll || (vis >> (nt * 8 + mt * 4 + i) & 1u); };
-          // weights, in units of 2^ref; twice where the reference has to rise first
-          float w[NT][2][4];
-#pragma unroll 1
-          for (int again = 0; again < 2; ++again) {
-            bool high = false;
+          // weights, in units of 2^ref; again where the reference has to rise first
+          float w[NT][2][4], wmax;
+          const auto weights = [&]() {
+            wmax = 0.f;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-              for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                  w[nt][mt][i] = on(nt, mt, i) ? ex2(sc[nt][mt][i] - ref[nt][i & 1]) : 0.f;
-                  high |= w[nt][mt][i] * smax[mt][i >> 1] > kTop;
-                }
-            if (again || !__any_sync(0xffffffffu, high)) break;
+              for (int k = 0; k < 4; ++k) {
+                float* sp = &sc[nt][k >> 1][(k & 1) * 2];
+                float* wp = &w[nt][k >> 1][(k & 1) * 2];
+                const float2 e = fma2(make_float2(sp[0], sp[1]), f2[nt], ref2[nt]);
+                wp[0] = on(nt, k >> 1, (k & 1) * 2) ? ex2(e.x) : 0.f;
+                wp[1] = on(nt, k >> 1, (k & 1) * 2 + 1) ? ex2(e.y) : 0.f;
+                wmax = fmaxf(wmax, fmaxf(wp[0], wp[1]));
+              }
+          };
+          weights();
+          // (the thread's largest weight and scale may be of different keys: then nothing rises below)
+          if (__any_sync(0xffffffffu, wmax * smax > kTop)) {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -371,8 +433,8 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, 1) paged_attn_ker
 #pragma unroll
                   for (int x2 = 0; x2 < 2; ++x2)
                     if (on(nt, mt, x2 * 2 + i)) {
-                      top = fmaxf(top, sc[nt][mt][2 * x2 + i] + __log2f(smax[mt][x2]));
-                      up |= w[nt][mt][2 * x2 + i] * smax[mt][x2] > kTop;
+                      top = fmaxf(top, fmaf(sc[nt][mt][2 * x2 + i], i ? f2[nt].y : f2[nt].x, __log2f(key_scale(mt, x2))));
+                      up |= w[nt][mt][2 * x2 + i] * key_scale(mt, x2) > kTop;
                     }
 #pragma unroll
                 for (int x2 = 4; x2 < 32; x2 <<= 1) {
@@ -380,9 +442,10 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, 1) paged_attn_ker
                   up |= __shfl_xor_sync(0xffffffffu, static_cast<int>(up), x2) != 0;
                 }
                 if (up) {
-                  const float now = top - 7.f, al = ref[nt][i] == -INFINITY ? 1.f : ex2(ref[nt][i] - now);
-                  ref[nt][i] = now;
-                  l[nt][i] *= al;
+                  float& ref = i ? ref2[nt].y : ref2[nt].x;
+                  const float now = 7.f - top, al = ref == INFINITY ? 1.f : ex2(now - ref);
+                  ref = now;
+                  (i ? l2[nt].y : l2[nt].x) *= al;
 #pragma unroll
                   for (int gi = 0; gi < G; ++gi) oz[nt][gi][i] *= al;
 #pragma unroll
@@ -394,6 +457,7 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, 1) paged_attn_ker
                     }
                 }
               }
+            weights();
           }
           // sums, and the second product's operand: 8-key block k = 2 mt + x2 holds nibble k of V's words,
           // odd ones four bits up
@@ -403,8 +467,7 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, 1) paged_attn_ker
             for (int k = 0; k < 4; ++k) {
               const float w0 = w[nt][k >> 1][(k & 1) * 2], w1 = w[nt][k >> 1][(k & 1) * 2 + 1];
               const bool on0 = on(nt, k >> 1, (k & 1) * 2), on1 = on(nt, k >> 1, (k & 1) * 2 + 1);
-              l[nt][0] += w0;
-              l[nt][1] += w1;
+              l2[nt] = add2(l2[nt], make_float2(w0, w1));
 #pragma unroll
               for (int gi = 0; gi < G; ++gi) {
                 const float2 sz = vz[k >> 1][k & 1][gi];
@@ -416,7 +479,8 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, 1) paged_attn_ker
                 const uint32_t hi = pack_f16(p0, p1);
                 const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&hi));
                 pf[nt][gi][0][k] = movmatrix_t(hi);
-                pf[nt][gi][1][k] = movmatrix_t(pack_f16(p0 - back.x, p1 - back.y));
+                const float2 rest = fma2(back, make_float2(-1.f, -1.f), make_float2(p0, p1));
+                pf[nt][gi][1][k] = movmatrix_t(pack_f16(rest.x, rest.y));
               }
             }
         };
@@ -426,7 +490,7 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, 1) paged_attn_ker
           weigh(std::false_type{});
 #pragma unroll
         for (int db = 0; db < DB; ++db) {
-          const uint4 vw = *reinterpret_cast<const uint4*>(blk + B::kV + ((kg * (D / 4) + db * 8 + g) * 4 + t) * 16);
+          const uint4 vw = *reinterpret_cast<const uint4*>(vcodes + ((db * 8 + g) * 4 + t) * 16);
           const uint32_t x[4] = {vw.x, vw.y, vw.z, vw.w};
 #pragma unroll
           for (int y = 0; y < 2; ++y) {
@@ -444,24 +508,26 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, 1) paged_attn_ker
           }
         }
       }
-      __syncwarp();  // every lane has read the stage
+      __syncwarp();
     }
     // ---- the segment's end: the warps' parts, joined through the stage that each read last ----
-    const bool has = done > done0;
-    float* buf = reinterpret_cast<float*>(ring + ((done + ST - 1) % ST) * B::kBytes);
-    if (has) {
+    const int last = stage == 0 ? ST - 1 : stage - 1;
+    if (lane == 0) s_has[warp] = done > done0 ? last + 1 : 0;
+    if (done > done0) {
+      float* buf = reinterpret_cast<float*>(ring + last * B::kBytes);
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
 #pragma unroll
           for (int x2 = 4; x2 < 32; x2 <<= 1) {
-            l[nt][i] += __shfl_xor_sync(0xffffffffu, l[nt][i], x2);
+            float& l = i ? l2[nt].y : l2[nt].x;
+            l += __shfl_xor_sync(0xffffffffu, l, x2);
 #pragma unroll
             for (int gi = 0; gi < G; ++gi) oz[nt][gi][i] += __shfl_xor_sync(0xffffffffu, oz[nt][gi][i], x2);
           }
           const int row = nt * 8 + 2 * t + i;
-          if (g == 0) s_ml[warp][row] = make_float2(ref[nt][i], l[nt][i]);
+          if (g == 0) s_ml[warp][row] = i ? make_float2(-ref2[nt].y, l2[nt].y) : make_float2(-ref2[nt].x, l2[nt].x);
 #pragma unroll
           for (int db = 0; db < DB; ++db) {
             float4 x;
@@ -476,19 +542,19 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, 1) paged_attn_ker
         }
       }
     }
-    if (lane == 0) s_has[warp] = has ? (done + ST - 1) % ST + 1 : 0;
     __syncthreads();
-    const bool whole = pg0 == 0 && pg1 == r.pages;
-    int c0 = 0, c1 = 0;  // CTAs that share the item
-    if (!whole) {
+    const bool whole = x0 == 0 && x1 == r.units;
+    int c0 = first_cta, c1 = first_cta + splits - 1;  // CTAs that share the item
+    if (!whole && !p.aligned) {
       const long long T = p.total, Gd = gridDim.x;
-      const int i0 = u - pg0, i1 = i0 + r.pages - 1;
+      const int i0 = u - x0, i1 = i0 + r.units - 1;
       c0 = static_cast<int>(i0 * Gd / T);
       while ((c0 + 1) * T / Gd <= i0) ++c0;
       c1 = static_cast<int>(i1 * Gd / T);
       while ((c1 + 1) * T / Gd <= i1) ++c1;
     }
-    const int slot = blockIdx.x * 2 + (pg0 == 0 ? 1 : 0);
+    // a CTA's two partials: of the item that it begins, and of the one that it ends or runs through
+    const int slot = blockIdx.x * 2 + (x0 == 0 ? 1 : 0);
     const auto finish = [&](int row, int c4, float M, float L, float4 x) {
       const float inv = L > 0.f ? 1.f / L : L == 0.f ? 0.f : L;  // (a NaN stays one)
       const float y[4] = {x.x * inv, x.y * inv, x.z * inv, x.w * inv};
@@ -502,35 +568,40 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, 1) paged_attn_ker
         store_vec<__nv_bfloat16, 4>(static_cast<__nv_bfloat16*>(a.out) + at, y);
       if (c4 == 0 && a.lse) a.lse[tok * a.hq + head] = (M + log2f(L)) * 0.6931471805599453f;
     };
-    for (int x = tid; x < rows * (D / 4); x += W * 32) {
-      const int row = x / (D / 4), c4 = x % (D / 4);
+    // the parts of (row, 4 dims), with the rows' references and sums
+    const auto joined = [&](int row, int c4, float2* ml, float4* sum) {
       float M = -INFINITY, L = 0.f;
 #pragma unroll
       for (int wi = 0; wi < W; ++wi)
         if (s_has[wi]) M = fmaxf(M, s_ml[wi][row].x);
       const float mb = M == -INFINITY ? 0.f : M;
-      float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+      *sum = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int wi = 0; wi < W; ++wi) {
-        const int st = s_has[wi];
-        if (!st) continue;
-        const float2 ml = s_ml[wi][row];
-        const float fw = ex2(ml.x - mb);
-        const float4 y = *reinterpret_cast<const float4*>(ring_all + (wi * ST + st - 1) * B::kBytes + (row * D + ((c4 ^ (2 * ((row >> 1) & 3))) << 2)) * 4);
-        L = fmaf(fw, ml.y, L);
-        sum.x = fmaf(fw, y.x, sum.x);
-        sum.y = fmaf(fw, y.y, sum.y);
-        sum.z = fmaf(fw, y.z, sum.z);
-        sum.w = fmaf(fw, y.w, sum.w);
+        if (!s_has[wi]) continue;
+        const float2 x = s_ml[wi][row];
+        const float fw = ex2(x.x - mb);
+        const float4 y = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(pa_dyn + (wi * ST + s_has[wi] - 1) * B::kBytes) + row * D + ((c4 ^ (2 * ((row >> 1) & 3))) << 2));
+        L = fmaf(fw, x.y, L);
+        sum->x = fmaf(fw, y.x, sum->x);
+        sum->y = fmaf(fw, y.y, sum->y);
+        sum->z = fmaf(fw, y.z, sum->z);
+        sum->w = fmaf(fw, y.w, sum->w);
       }
+      *ml = make_float2(M, L);
+    };
+    for (int x = tid; x < rows * (D / 4); x += W * 32) {
+      const int row = x / (D / 4), c4 = x % (D / 4);
+      float2 ml;
+      float4 sum;
+      joined(row, c4, &ml, &sum);
       if (whole) {
-        finish(row, c4, M, L, sum);
+        finish(row, c4, ml.x, ml.y, sum);
       } else {
         __stcg(reinterpret_cast<float4*>(p.part_o + (static_cast<long long>(slot) * R + row) * D) + c4, sum);
-        if (c4 == 0) __stcg(p.part_ml + slot * R + row, make_float2(M, L));
+        if (c4 == 0) __stcg(p.part_ml + slot * R + row, ml);
       }
     }
-    fence_async_smem();  // the parts in the stages, before copies write over them
     __syncthreads();
     if (!whole) {
       if (tid == 0) {
@@ -539,26 +610,77 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, 1) paged_attn_ker
       }
       __syncthreads();
       if (s_last) {
-        for (int x = tid; x < rows * (D / 4); x += W * 32) {
-          const int row = x / (D / 4), c4 = x % (D / 4);
+        // Few rows: several warps take a row, each some of its partials.
+        const int per_row = rows == 1 ? W : rows == 2 ? W / 2 : 1, slice = warp % per_row, n = c1 - c0 + 1;
+        for (int row = warp / per_row; row < rows; row += W / per_row) {
+          // lane l: reference and sum of the slice's partials l, l + 32, ...
           float M = -INFINITY, L = 0.f;
-#pragma unroll 8
-          for (int c = c0; c <= c1; ++c) M = fmaxf(M, __ldcg(p.part_ml + (c * 2 + (c == c0)) * R + row).x);
+          const int mine_n = n > slice ? (n - slice + per_row - 1) / per_row : 0;
+          const auto slot_of = [&](int k) {
+            const int c = c0 + slice + k * per_row;
+            return static_cast<long long>(c * 2 + (c == c0)) * R + row;
+          };
+          for (int k = lane; k < mine_n; k += 32) M = fmaxf(M, __ldcg(p.part_ml + slot_of(k)).x);
+#pragma unroll
+          for (int x = 16; x > 0; x >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, x));
           const float mb = M == -INFINITY ? 0.f : M;
           float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-          for (int c = c0; c <= c1; ++c) {
-            const long long sl = c * 2 + (c == c0);
-            const float2 ml = __ldcg(p.part_ml + sl * R + row);
-            const float4 y = __ldcg(reinterpret_cast<const float4*>(p.part_o + (sl * R + row) * D) + c4);
-            const float fw = ex2(ml.x - mb);
-            L = fmaf(fw, ml.y, L);
-            sum.x = fmaf(fw, y.x, sum.x);
-            sum.y = fmaf(fw, y.y, sum.y);
-            sum.z = fmaf(fw, y.z, sum.z);
-            sum.w = fmaf(fw, y.w, sum.w);
+          for (int k0 = 0; k0 < mine_n; k0 += 32) {
+            float fw = 0.f;
+            if (k0 + lane < mine_n) {
+              const float2 ml = __ldcg(p.part_ml + slot_of(k0 + lane));
+              fw = ex2(ml.x - mb);
+              L = fmaf(fw, ml.y, L);
+            }
+            const int m = min(32, mine_n - k0);
+            for (int k = 0; k < m; k += 8) {
+              float4 y[8];
+#pragma unroll
+              for (int i = 0; i < 8; ++i)
+                y[i] = k + i < m && lane < D / 4 ? __ldcg(reinterpret_cast<const float4*>(p.part_o + slot_of(k0 + k + i) * D) + lane)
+                                                 : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                const float x = __shfl_sync(0xffffffffu, fw, (k + i) & 31);
+                if (k + i >= m) continue;
+                sum.x = fmaf(x, y[i].x, sum.x);
+                sum.y = fmaf(x, y[i].y, sum.y);
+                sum.z = fmaf(x, y[i].z, sum.z);
+                sum.w = fmaf(x, y[i].w, sum.w);
+              }
+            }
           }
-          finish(row, c4, M, L, sum);
+#pragma unroll
+          for (int x = 16; x > 0; x >>= 1) L += __shfl_xor_sync(0xffffffffu, L, x);
+          if (per_row == 1) {
+            if (lane < D / 4) finish(row, lane, M, L, sum);
+          } else {
+            const int at = slice * rows + row;  // (at most W)
+            if (lane == 0) s_ml[at][0] = make_float2(M, L);
+            if (lane < D / 4) reinterpret_cast<float4*>(s_x[at])[lane] = sum;
+          }
+        }
+        __syncthreads();
+        if (per_row > 1) {
+          for (int x = tid; x < rows * (D / 4); x += W * 32) {
+            const int row = x / (D / 4), c4 = x % (D / 4);
+            float M = -INFINITY, L = 0.f;
+            for (int k = 0; k < per_row; ++k) M = fmaxf(M, s_ml[k * rows + row][0].x);
+            const float mb = M == -INFINITY ? 0.f : M;
+            float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int k = 0; k < per_row; ++k) {
+              const float2 ml = s_ml[k * rows + row][0];
+              const float4 y = reinterpret_cast<const float4*>(s_x[k * rows + row])[c4];
+              const float fw = ex2(ml.x - mb);
+              L = fmaf(fw, ml.y, L);
+              sum.x = fmaf(fw, y.x, sum.x);
+              sum.y = fmaf(fw, y.y, sum.y);
+              sum.z = fmaf(fw, y.z, sum.z);
+              sum.w = fmaf(fw, y.w, sum.w);
+            }
+            finish(row, c4, M, L, sum);
+          }
+          __syncthreads();
         }
       }
     }
@@ -570,9 +692,35 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, 1) paged_attn_ker
 }
 
 template <int D, int NT>
-cudaError_t pa_launch(const PaParams& p, int grid, cudaStream_t s) {
-  paged_attn_kernel<D, NT><<<grid, PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::kSmem, s>>>(p);
-  return cudaGetLastError();
+cudaError_t pa_launch(PaParams& p, int sms, cudaStream_t s) {
+  using S = PaShape<D, NT>;
+  // Runs of equal length, or aligned to items where one CTA's run is then not much longer (ending an item
+  // costs about as much as 8 units): every CTA ends one item instead of two or three.  At least one unit a
+  // warp.
+  const int most = sms * S::kCtas, even = (p.total + most - 1) / most;
+  int run = even > S::kWarps ? even : S::kWarps;
+  const auto ctas = [&](int len) {
+    long long n = 0;
+    for (int i = 0; i < p.n_req; ++i) {
+      const int items = (i + 1 < p.n_req ? p.r[i + 1].off : p.total) - p.r[i].off;
+      n += items / p.r[i].units * static_cast<long long>((p.r[i].units + len - 1) / len);
+    }
+    return n;
+  };
+  while (run <= even + 8 && ctas(run) > most) ++run;
+  int grid = 0;
+  p.aligned = run <= even + 8;
+  if (p.aligned) {
+    for (int i = 0; i < p.n_req; ++i) {
+      const int items = ((i + 1 < p.n_req ? p.r[i + 1].off : p.total) - p.r[i].off) / p.r[i].units;
+      p.r[i].cta = grid;
+      p.r[i].splits = (p.r[i].units + run - 1) / run;
+      grid += items * p.r[i].splits;
+    }
+  } else {
+    grid = most;
+  }
+  return launch_k(paged_attn_kernel<D, NT>, dim3(grid), dim3(S::kWarps * 32), S::kSmem, s, true, p);
 }
 template <int D, int NT>
 cudaError_t pa_prepare() {
@@ -582,7 +730,9 @@ cudaError_t pa_prepare() {
 
 }  // namespace
 
-size_t pa_partial_rows(int sms) { return static_cast<size_t>(sms) * 2 * 16; }
+// (two partials of 8 rows for four CTAs of an SM, of 16 for two)
+size_t pa_partial_rows(int sms) { return static_cast<size_t>(sms) * 2 * 32; }
+int pa_counters(int sms) { return sms * 4; }
 
 cudaError_t pa_prepare_all() {
   cudaError_t e = pa_prepare<64, 1>();
@@ -592,41 +742,50 @@ cudaError_t pa_prepare_all() {
   return e;
 }
 
-cudaError_t launch_paged_attention(const tss_paged* h, const PgAttnParams& a, cudaStream_t s, bool* too_large) {
+cudaError_t launch_paged_attention(const tss_paged* h, const PgAttnArgs& a, const PgBatch& batch, cudaStream_t s, bool* too_large) {
   *too_large = false;
-  PaParams p{};
+  PaParams p;
   p.a = a;
+  p.n_req = 0;
   p.part_o = h->part_o;
   p.part_ml = h->part_ml;
   p.counters = h->counters;
   const int gq = h->hq / h->hk;
   int most = 0;
-  for (int i = 0; i < a.batch.n_req; ++i) most = a.batch.r[i].n * gq > most ? a.batch.r[i].n * gq : most;
+  for (int i = 0; i < batch.n_req; ++i) most = batch.r[i].n * gq > most ? batch.r[i].n * gq : most;
   const int R = most <= 8 ? 8 : 16;
+  // Units of a page; of half a page where that leaves the warps less than three pages each (a warp takes about
+  // 2 us for a page, so a short launch is as long as its longest warp).
   long long at = 0;
-  for (int i = 0; i < a.batch.n_req; ++i) {
-    const PgReq& q = a.batch.r[i];
-    if (q.n == 0) continue;
-    PaReq& r = p.r[p.n_req++];
-    r = PaReq{q.seq, q.first, q.n, q.row, 0, 0, 0, static_cast<int>(at)};
-    const int end = (q.first + q.n + kPgTokens - 1) / kPgTokens;
-    if (a.window) {
-      r.lo = (q.first - a.window + 1 > 0 ? q.first - a.window + 1 : 0) / kPgTokens;
-      const int sinks = a.sinks < q.first + q.n ? a.sinks : q.first + q.n;
-      r.sink = (sinks + kPgTokens - 1) / kPgTokens;
-      if (r.sink > r.lo) r.sink = r.lo;
+  for (int halves = 2; halves > 0; --halves) {
+    const int unit = 32 * halves;
+    p.halves = halves;
+    p.n_req = 0;
+    at = 0;
+    for (int i = 0; i < batch.n_req; ++i) {
+      const PgReq& q = batch.r[i];
+      if (q.n == 0) continue;
+      PaReq& r = p.r[p.n_req++];
+      r = PaReq{q.seq, q.first, q.n, q.row, 0, 0, 0, static_cast<int>(at), 0, 1};
+      const int end = (q.first + q.n + unit - 1) / unit;
+      if (a.window) {
+        r.lo = (q.first - a.window + 1 > 0 ? q.first - a.window + 1 : 0) / unit;
+        const int sinks = a.sinks < q.first + q.n ? a.sinks : q.first + q.n;
+        r.sink = (sinks + unit - 1) / unit;
+        if (r.sink > r.lo) r.sink = r.lo;
+      }
+      r.units = r.sink + end - r.lo;
+      at += static_cast<long long>(r.units) * h->hk * ((q.n * gq + R - 1) / R);
+      if (at > 0x3fffffff) {
+        *too_large = true;
+        return cudaSuccess;
+      }
     }
-    r.pages = r.sink + end - r.lo;
-    at += static_cast<long long>(r.pages) * h->hk * ((q.n * gq + R - 1) / R);
-    if (at > 0x3fffffff) {
-      *too_large = true;
-      return cudaSuccess;
-    }
+    if (at >= 3LL * h->sms * (R == 8 ? 12 : 8)) break;
   }
   p.total = static_cast<int>(at);
-  const int grid = p.total < h->sms ? p.total : h->sms;
-  if (h->d == 64) return R == 8 ? pa_launch<64, 1>(p, grid, s) : pa_launch<64, 2>(p, grid, s);
-  return R == 8 ? pa_launch<128, 1>(p, grid, s) : pa_launch<128, 2>(p, grid, s);
+  if (h->d == 64) return R == 8 ? pa_launch<64, 1>(p, h->sms, s) : pa_launch<64, 2>(p, h->sms, s);
+  return R == 8 ? pa_launch<128, 1>(p, h->sms, s) : pa_launch<128, 2>(p, h->sms, s);
 }
 
 }  // namespace tss
