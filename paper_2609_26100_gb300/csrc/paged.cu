@@ -1,11 +1,12 @@
 // The paged 4-bit KV cache: its workspace, appending (quantising) tokens and reading them back.
 //
 // Quantisation, per token and 64 dims:  z = fp16(min), s = fp16((max - z) / 15), c = rint((x - z) / s).
-// A warp takes one (request, 32-token half page, KV head, K or V).  A lane holds D / 32 neighbouring
-// dims, so a token's row is one coalesced read and a group's minimum and maximum a butterfly over 16 or
-// 32 lanes.  K codes are stored by token; V codes share a 32-bit word between 8 tokens of a dim, which the
-// lane that owns the dim builds in registers (a half page's words all lie in one warp: tokens that the
-// call does not bring keep their nibbles, and no two warps write one word).
+// A warp takes one (request, 32-token half page, KV head, K or V).  A lane holds 8 neighbouring dims, a
+// token D / 8 lanes, so a warp's load brings two (four) whole tokens and a group's minimum and maximum
+// are a butterfly over 8 lanes.  A lane's K codes of a token are one 32-bit word.  A word of V codes is 8
+// tokens of a dim: a lane gathers those of even or of odd tokens, 16 bits of each word, and swaps half of
+// them with the lane of the same dims at the other parity.  All words of a half page lie in one warp, so
+// tokens that the call does not bring keep their nibbles and no two warps write one word.
 //
 // Bound: HBM for prompts (a token's 2 bytes a value in, half a byte out), latency for a step's few rows.
 #include "paged.h"
@@ -64,117 +65,154 @@ __device__ __forceinline__ bool pq_unit(const PqParams& p, int block_bytes, int 
   return true;
 }
 
-// Scale and minimum of the group that the lane's N values belong to, and their codes.
-template <int D, int N>
-__device__ __forceinline__ __half2 quantise(const float* x, uint32_t* code) {
-  float lo = x[0], hi = x[0];
-  bool bad = false;
+// a / b rounded as by IEEE division, for a normal b whose reciprocal r approximates to a few ulp: the quotient by
+// the reciprocal, corrected by its exact remainder (Markstein, IBM J. Res. Dev. 34, 1990).  A quotient that
+// lies so near the middle of two floats that the rounded correction could miss its side would need more
+// digits than a (24) and b (11 here) give.
+__device__ __forceinline__ float quotient(float a, float b, float r) {
+  const float q = a * r;
+  return fmaf(fmaf(-b, q, a), r, q);
+}
+
+// Scale and minimum of the group that the lane's 8 values belong to (its lanes are 8 neighbours), and their
+// codes, one to a nibble.
+__device__ __forceinline__ __half2 quantise(const float* x, uint32_t* codes) {
+  float lo = x[0], hi = x[0], odd = 0.f;
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
+  for (int i = 0; i < 8; ++i) {
     lo = fminf(lo, x[i]);
     hi = fmaxf(hi, x[i]);
-    bad |= !(fabsf(x[i]) < INFINITY);
+    odd = fmaf(x[i], 0.f, odd);  // NaN where a value is NaN or infinite
   }
 #pragma unroll
-  for (int o = kPgGroup / N / 2; o > 0; o >>= 1) {
+  for (int o = 4; o > 0; o >>= 1) {
     lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
     hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
   }
-  // a NaN or an infinity poisons its group (one ballot; the group's lanes are neighbours)
-  const uint32_t any = __ballot_sync(0xffffffffu, bad);
-  constexpr int kLanes = kPgGroup / N;
-  const int lane = threadIdx.x & 31;
-  const uint32_t mine = kLanes == 32 ? 0xffffffffu : ((1u << (kLanes & 31)) - 1u) << (lane & ~(kLanes - 1));
+  // a NaN or an infinity poisons its group
+  const bool bad = (__ballot_sync(0xffffffffu, odd != 0.f) >> (threadIdx.x & 24) & 0xffu) != 0;
   const __half z = __float2half_rn(fminf(fmaxf(lo, -65504.f), 65504.f));
   const float zf = __half2float(z);
-  __half s = __float2half_rn(fminf(fmaxf(__fdiv_rn(__fsub_rn(hi, zf), 15.f), 0.f), 65504.f));
+  const __half s = __float2half_rn(fminf(fmaxf(quotient(hi - zf, 15.f, 1.f / 15.f), 0.f), 65504.f));
   const float sf = __half2float(s);
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(sf));
+  uint32_t w = 0;
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    // (the quotient is NaN or infinite only where s = 0 or the group is poisoned)
-    const float c = sf > 0.f ? rintf(__fdiv_rn(__fsub_rn(x[i], zf), sf)) : 0.f;
-    code[i] = static_cast<uint32_t>(fminf(fmaxf(c, 0.f), 15.f));
+  for (int i = 0; i < 8; ++i) {
+    // rounded to an integer by adding 1.5 2^23: the low bits of the sum (ties to even, as rint)
+    const float c = fminf(fmaxf(quotient(x[i] - zf, sf, r), 0.f), 15.f);
+    w |= (__float_as_uint(c + 12582912.f) & 15u) << (4 * i);
   }
-  if (any & mine) {
-    s = __ushort_as_half(0x7fff);
-#pragma unroll
-    for (int i = 0; i < N; ++i) code[i] = 0;
-  }
-  return __halves2half2(s, any & mine ? __ushort_as_half(0) : z);
+  *codes = sf > 0.f && !bad ? w : 0u;
+  return bad ? __halves2half2(__ushort_as_half(0x7fff), __ushort_as_half(0)) : __halves2half2(s, z);
 }
 
-// Byte of a K row that holds dims d, d + 1 (d even).
-template <int D>
-__device__ __forceinline__ int k_byte(int d) {
-  return (d % kPgGroup) / 16 * (D / 8) + (d / kPgGroup) * 8 + (d % 16) / 2;
+// Nibbles of word t of a run (token 8 b + 2 t + i at nibble b + 4 i) that are tokens [lo, hi).
+__device__ __forceinline__ uint32_t word_mask(int t, int lo, int hi) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const int tok = 8 * (k & 3) + 2 * t + (k >> 2);
+    if (tok >= lo && tok < hi) m |= 15u << (4 * k);
+  }
+  return m;
 }
+
+template <int D>
+struct PqLane {
+  static constexpr int kLanes = D / 8;         // of a token
+  static constexpr int kTokens = 32 / kLanes;  // of a warp's step: 2 or 4
+  static constexpr int kT = 8 / kTokens;       // words (indices t) that a lane's tokens are spread over
+  int d0, sub, i, k_at;
+  __device__ explicit PqLane(int lane) {
+    d0 = 8 * (lane % kLanes);
+    sub = lane / kLanes;
+    i = sub & 1;
+    k_at = d0 % kPgGroup / 16 * (D / 8) + d0 / kPgGroup * 8 + d0 % 16 / 2;  // byte of the lane's word in a K row
+  }
+  // step j's token of the lane's is kTokens j + sub; its word t and nibble b + 4 i
+  __device__ int t(int tl) const { return kTokens == 2 ? tl : 2 * tl + (sub >> 1); }
+};
 
 template <typename T, int D>
 __global__ void __launch_bounds__(kPqThreads) append_kernel(const __grid_constant__ PqParams p) {
   using B = PgBlock<D>;
-  constexpr int N = D / 32;  // dims of a lane
-  const int lane = threadIdx.x & 31, d0 = lane * N;
+  using L = PqLane<D>;
+  const int lane = threadIdx.x & 31;
+  griddep_wait();
+  griddep_launch();
   PqUnit u;
   if (!pq_unit(p, B::kBytes, lane, &u) || !u.block) return;
+  const L at(lane);
   const T* src = u.side ? static_cast<const T*>(p.v) + u.row * p.vs : static_cast<const T*>(p.k) + u.row * p.ks;
   const long long stride = u.side ? p.vs : p.ks;
-  src += u.head * D + d0;
-  const bool head = (d0 % kPgGroup) == 0;  // the lane that writes its group's parameters
-  __half2* params = reinterpret_cast<__half2*>(u.block + (u.side ? B::kVParams : B::kKParams)) + u.tok0 * B::kGroups + d0 / kPgGroup;
-  // the lane's V words: [t][dim]; those of a run that the batch fills only in part keep the other nibbles
-  uint32_t words[4][N];
-  uint32_t* vw = reinterpret_cast<uint32_t*>(u.block + B::kV) + ((u.tok0 / 32) * (D / 4) + d0 / 4) * 16 + d0 % 4;
-  if (u.side && (u.lo > 0 || u.hi < 32)) {
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-      for (int e = 0; e < N; ++e) words[t][e] = vw[t * 4 + e];
-  } else {
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-      for (int e = 0; e < N; ++e) words[t][e] = 0u;
-  }
+  src += u.head * D + at.d0;
+  __half2* params = reinterpret_cast<__half2*>(u.block + (u.side ? B::kVParams : B::kKParams)) + u.tok0 * B::kGroups + at.d0 / kPgGroup;
+  uint8_t* krow = u.block + B::kK + u.tok0 * (D / 2) + at.k_at;
+  uint32_t acc[L::kT][4] = {};  // [t][pair of dims]: 16 bits a dim, nibble b
+  constexpr int kStep = 4;      // steps whose loads are in flight together: 8 (16) tokens
 #pragma unroll 1
-  for (int b = u.lo / 8; b * 8 < u.hi; ++b) {
-    float x[8][N];
+  for (int j0 = u.lo / (kStep * L::kTokens) * kStep; j0 * L::kTokens < u.hi; j0 += kStep) {
+    float x[kStep][8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int tok = 8 * b + i;
+    for (int j = 0; j < kStep; ++j) {
+      const int tok = (j0 + j) * L::kTokens + at.sub;
       if (tok >= u.lo && tok < u.hi) {
-        load_vec<T, N>(src + (tok - u.lo) * stride, x[i]);
+        load_vec<T, 8>(src + (tok - u.lo) * stride, x[j]);
       } else {
 #pragma unroll
-        for (int e = 0; e < N; ++e) x[i][e] = 0.f;
+        for (int e = 0; e < 8; ++e) x[j][e] = 0.f;
       }
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int tok = 8 * b + i;
-      if (tok < u.lo || tok >= u.hi) continue;  // (the same for the whole warp)
-      uint32_t c[N];
-      const __half2 sz = quantise<D, N>(x[i], c);
-      if (head) params[tok * B::kGroups] = sz;
+    for (int j = 0; j < kStep; ++j) {
+      const int tok0 = (j0 + j) * L::kTokens, tok = tok0 + at.sub;
+      if (tok0 + L::kTokens <= u.lo || tok0 >= u.hi) continue;  // (the same for the whole warp)
+      uint32_t w;
+      const __half2 sz = quantise(x[j], &w);
+      if (tok < u.lo || tok >= u.hi) continue;
+      if (at.d0 % kPgGroup == 0) params[tok * B::kGroups] = sz;
       if (u.side) {
-        const int shift = 4 * (b + 4 * (i & 1));
+        const int shift = 4 * (tok / 8);
+        constexpr int kMod = L::kT;
+        // (j0 is a multiple of kStep, a multiple of kT: the word is known at compile time)
 #pragma unroll
-        for (int e = 0; e < N; ++e) words[i / 2][e] = (words[i / 2][e] & ~(15u << shift)) | (c[e] << shift);
+        for (int e = 0; e < 4; ++e) acc[j % kMod][e] |= ((w >> (8 * e) & 15u) | (w >> (8 * e + 4) & 15u) << 16) << shift;
       } else {
-        uint8_t* dst = u.block + B::kK + (u.tok0 + tok) * (D / 2) + k_byte<D>(d0);
-        if constexpr (N == 4)
-          *reinterpret_cast<uint16_t*>(dst) = static_cast<uint16_t>(c[0] | c[1] << 4 | c[2] << 8 | c[3] << 12);
-        else
-          *dst = static_cast<uint8_t>(c[0] | c[1] << 4);
+        *reinterpret_cast<uint32_t*>(krow + tok * (D / 2)) = w;
       }
     }
   }
-  if (u.side) {
+  if (!u.side) return;
+  // A lane of even tokens finishes the first half of its words, one of odd tokens the second.
+  constexpr int kHalf = L::kT / 2;
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      if constexpr (N == 4)
-        *reinterpret_cast<uint4*>(vw + t * 4) = make_uint4(words[t][0], words[t][1], words[t][2], words[t][3]);
-      else
-        *reinterpret_cast<uint2*>(vw + t * 4) = make_uint2(words[t][0], words[t][1]);
+  for (int h = 0; h < kHalf; ++h) {
+    uint32_t lo16[4], hi16[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t keep = at.i ? acc[kHalf + h][e] : acc[h][e], give = at.i ? acc[h][e] : acc[kHalf + h][e];
+      const uint32_t got = __shfl_xor_sync(0xffffffffu, give, L::kLanes);
+      lo16[e] = at.i ? got : keep;  // even tokens: the words' low halves
+      hi16[e] = at.i ? keep : got;
+    }
+    const int t = at.t(at.i * kHalf + h);
+    const uint32_t mask = word_mask(t, u.lo, u.hi);
+    if (mask == 0) continue;
+    uint4* dst = reinterpret_cast<uint4*>(u.block + B::kV) + (u.tok0 / 32 * (D / 4) + at.d0 / 4) * 4 + t;
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      uint4 v = make_uint4(__byte_perm(lo16[2 * q], hi16[2 * q], 0x5410), __byte_perm(lo16[2 * q], hi16[2 * q], 0x7632),
+                           __byte_perm(lo16[2 * q + 1], hi16[2 * q + 1], 0x5410), __byte_perm(lo16[2 * q + 1], hi16[2 * q + 1], 0x7632));
+      if (mask != 0xffffffffu) {
+        const uint4 old = dst[4 * q];
+        v.x |= old.x & ~mask;
+        v.y |= old.y & ~mask;
+        v.z |= old.z & ~mask;
+        v.w |= old.w & ~mask;
+      }
+      dst[4 * q] = v;
     }
   }
 }
@@ -182,60 +220,71 @@ __global__ void __launch_bounds__(kPqThreads) append_kernel(const __grid_constan
 template <typename T, int D>
 __global__ void __launch_bounds__(kPqThreads) read_kernel(const __grid_constant__ PqParams p) {
   using B = PgBlock<D>;
-  constexpr int N = D / 32;
-  const int lane = threadIdx.x & 31, d0 = lane * N;
+  using L = PqLane<D>;
+  const int lane = threadIdx.x & 31;
+  griddep_wait();
+  griddep_launch();
   PqUnit u;
   if (!pq_unit(p, B::kBytes, lane, &u)) return;
   T* dst = static_cast<T*>(u.side ? p.vo : p.ko);
   if (!dst) return;
+  const L at(lane);
   const long long stride = u.side ? p.vs : p.ks;
-  dst += u.row * stride + u.head * D + d0;
-  const __half2* params = reinterpret_cast<const __half2*>(u.block + (u.side ? B::kVParams : B::kKParams)) + u.tok0 * B::kGroups + d0 / kPgGroup;
-  const uint32_t* vw = reinterpret_cast<const uint32_t*>(u.block + B::kV) + ((u.tok0 / 32) * (D / 4) + d0 / 4) * 16 + d0 % 4;
-  uint32_t words[4][N] = {};
+  dst += u.row * stride + u.head * D + at.d0;
+  const __half2* params = reinterpret_cast<const __half2*>(u.block + (u.side ? B::kVParams : B::kKParams)) + u.tok0 * B::kGroups + at.d0 / kPgGroup;
+  const uint8_t* krow = u.block + B::kK + u.tok0 * (D / 2) + at.k_at;
+  // V: 16 bits (the lane's token parity) of the words of its dims, [t][pair of dims]
+  uint32_t words[L::kT][4];
   if (u.side && u.block) {
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
+    for (int tl = 0; tl < L::kT; ++tl)
 #pragma unroll
-      for (int e = 0; e < N; ++e) words[t][e] = vw[t * 4 + e];
-  }
-#pragma unroll 1
-  for (int b = u.lo / 8; b * 8 < u.hi; ++b) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int tok = 8 * b + i;
-      if (tok < u.lo || tok >= u.hi) continue;
-      float x[N];
-      if (!u.block) {  // no such page: zeros
-#pragma unroll
-        for (int e = 0; e < N; ++e) x[e] = 0.f;
-      } else {
-        const float2 sz = __half22float2(params[tok * B::kGroups]);
-        uint32_t c;
-        if (u.side) {
-          const int shift = 4 * (b + 4 * (i & 1));
-          c = 0;
-#pragma unroll
-          for (int e = 0; e < N; ++e) c |= ((words[i / 2][e] >> shift) & 15u) << (4 * e);
-        } else {
-          const uint8_t* s = u.block + B::kK + (u.tok0 + tok) * (D / 2) + k_byte<D>(d0);
-          c = N == 4 ? *reinterpret_cast<const uint16_t*>(s) : *s;
-        }
-#pragma unroll
-        for (int e = 0; e < N; ++e) x[e] = fmaf(static_cast<float>(c >> (4 * e) & 15u), sz.x, sz.y);
+      for (int q = 0; q < 2; ++q) {
+        const uint4 v = reinterpret_cast<const uint4*>(u.block + B::kV)[(u.tok0 / 32 * (D / 4) + at.d0 / 4 + q) * 4 + at.t(tl)];
+        const uint32_t sel = at.i ? 0x7632 : 0x5410;
+        words[tl][2 * q] = __byte_perm(v.x, v.y, sel);
+        words[tl][2 * q + 1] = __byte_perm(v.z, v.w, sel);
       }
-      store_vec<T, N>(dst + (tok - u.lo) * stride, x);
+  }
+  constexpr int kStep = 4;
+#pragma unroll 1
+  for (int j0 = u.lo / (kStep * L::kTokens) * kStep; j0 * L::kTokens < u.hi; j0 += kStep) {
+    uint32_t w[kStep];
+    __half2 sz[kStep];
+#pragma unroll
+    for (int j = 0; j < kStep; ++j) {
+      const int tok = (j0 + j) * L::kTokens + at.sub;
+      w[j] = 0;
+      sz[j] = __half2half2(__ushort_as_half(0));
+      if (tok >= u.lo && tok < u.hi && u.block) {  // (no such page: zeros)
+        sz[j] = params[tok * B::kGroups];
+        if (!u.side) w[j] = *reinterpret_cast<const uint32_t*>(krow + tok * (D / 2));
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kStep; ++j) {
+      const int tok = (j0 + j) * L::kTokens + at.sub;
+      if (tok < u.lo || tok >= u.hi) continue;
+      const float2 f = __half22float2(sz[j]);
+      float x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t c = u.side && u.block ? words[j % L::kT][e / 2] >> (16 * (e & 1) + 4 * (tok / 8)) : w[j] >> (4 * e);
+        x[e] = fmaf(static_cast<float>(c & 15u), f.x, f.y);
+      }
+      store_vec<T, 8>(dst + (tok - u.lo) * stride, x);
     }
   }
 }
 
 template <int D>
-void pq_launch(const PqParams& p, bool append, int dtype, unsigned grid, cudaStream_t s) {
+cudaError_t pq_launch(const PqParams& p, bool append, int dtype, unsigned grid, cudaStream_t s) {
+  cudaError_t e;
 #define TSS_PQ(T)                                      \
   if (append)                                          \
-    append_kernel<T, D><<<grid, kPqThreads, 0, s>>>(p); \
+    e = launch_k(append_kernel<T, D>, dim3(grid), dim3(kPqThreads), 0, s, true, p); \
   else                                                 \
-    read_kernel<T, D><<<grid, kPqThreads, 0, s>>>(p)
+    e = launch_k(read_kernel<T, D>, dim3(grid), dim3(kPqThreads), 0, s, true, p)
   if (dtype == TSS_DTYPE_BF16) {
     TSS_PQ(__nv_bfloat16);
   } else if (dtype == TSS_DTYPE_F16) {
@@ -244,6 +293,7 @@ void pq_launch(const PqParams& p, bool append, int dtype, unsigned grid, cudaStr
     TSS_PQ(float);
   }
 #undef TSS_PQ
+  return e;
 }
 
 // Checks what every call on the cache has in common and copies the batch.  *rows: rows in all.
@@ -314,11 +364,7 @@ tss_status quant_call(tss_paged* h, const tss_paged_cache* cache, int layer, con
   if ((warps + per - 1) / per > 0x7fffffffLL) return refuse(TSS_ERR_INVALID_ARG, "too many rows for one launch");
   const unsigned grid = static_cast<unsigned>((warps + per - 1) / per);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (h->d == 64)
-    pq_launch<64>(p, append, dtype, grid, s);
-  else
-    pq_launch<128>(p, append, dtype, grid, s);
-  const cudaError_t e = cudaGetLastError();
+  const cudaError_t e = h->d == 64 ? pq_launch<64>(p, append, dtype, grid, s) : pq_launch<128>(p, append, dtype, grid, s);
   return e == cudaSuccess ? TSS_OK : refuse_cuda(e, "launch");
 }
 

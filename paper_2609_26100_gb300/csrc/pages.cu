@@ -106,6 +106,8 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_kernel(const __grid_cons
   __shared__ uint32_t bits[kRoundWords];
   __shared__ int scratch[kPlanThreads / 32], off[kMaxCalls + 1], from[kMaxCalls];
   const int tid = threadIdx.x;
+  griddep_wait();
+  griddep_launch();
   if (tid < list.n) {
     const int have = t.held[list.a[tid]];
     from[tid] = have;
@@ -144,6 +146,8 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_kernel(const __grid_cons
 
 // free: a CTA for each sequence a[i], which keeps b[i] pages
 __global__ void __launch_bounds__(256) free_kernel(const __grid_constant__ SeqList list, PoolTables t) {
+  griddep_wait();
+  griddep_launch();
   const int seq = list.a[blockIdx.x], keep = list.b[blockIdx.x], held = t.held[seq];
   __syncthreads();
   if (held < 0 || held > t.max_pages) {
@@ -168,6 +172,8 @@ __global__ void __launch_bounds__(kPlanThreads) fork_choose_kernel(const __grid_
   __shared__ uint32_t bits[kRoundWords];
   __shared__ int scratch[kPlanThreads / 32], bad;
   const int tid = threadIdx.x;
+  griddep_wait();
+  griddep_launch();
   if (tid == 0) bad = 0;
   __syncthreads();
   if (tid < list.n) {
@@ -221,6 +227,8 @@ __device__ __forceinline__ void copy_piece(uint8_t* base, size_t page_bytes, int
 // fork, second part: CTAs [0, n) write an entry's row and counts, the others copy pages
 __global__ void __launch_bounds__(kCopyThreads) fork_kernel(const __grid_constant__ SeqList list, PoolTables t, const __grid_constant__ Layers ly,
                                                             const int* ids, const int* go) {
+  griddep_wait();
+  griddep_launch();
   if (*go == 0) return;
   const int cta = blockIdx.x;
   if (cta < list.n) {
@@ -265,6 +273,8 @@ __global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(PoolTables t
   extern __shared__ uint32_t live[];  // a bit for every page
   __shared__ int scratch[kPlanThreads / 32];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, words = (t.n_pages + 31) / 32;
+  griddep_wait();
+  griddep_launch();
   int mine = 0;
   for (int w0 = warp; w0 < words; w0 += 8 * (kPlanThreads / 32)) {
     int v[8];
@@ -325,6 +335,8 @@ __global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(PoolTables t
 // compact, second part: CTAs [0, row_ctas) rewrite the table, the others copy pages
 __global__ void __launch_bounds__(kCopyThreads) compact_kernel(PoolTables t, const __grid_constant__ Layers ly, int* table_out, const int* moves,
                                                                const int* map, int row_ctas) {
+  griddep_wait();
+  griddep_launch();
   const int n_moves = moves[0];
   if (static_cast<int>(blockIdx.x) < row_ctas) {
     const long long n = static_cast<long long>(t.n_seqs) * t.max_pages;
@@ -345,6 +357,8 @@ __global__ void __launch_bounds__(kCopyThreads) compact_kernel(PoolTables t, con
 }
 
 __global__ void __launch_bounds__(kCopyThreads) copy_kernel(PoolTables t, const __grid_constant__ Layers ly, const int* src, const int* dst, int n) {
+  griddep_wait();
+  griddep_launch();
   const int pieces = static_cast<int>((ly.page_bytes + kPiece - 1) / kPiece);
   const long long units = static_cast<long long>(n) * ly.n * pieces;
   for (long long u = blockIdx.x; u < units; u += gridDim.x) {
@@ -394,8 +408,7 @@ unsigned copy_grid(long long pages, const Layers& ly, int sms) {
   const long long most = static_cast<long long>(sms) * 6;
   return static_cast<unsigned>(units < most ? units : most);
 }
-tss_status launched() {
-  const cudaError_t e = cudaGetLastError();
+tss_status launched(cudaError_t e) {
   return e == cudaSuccess ? TSS_OK : refuse_cuda(e, "launch");
 }
 
@@ -470,8 +483,7 @@ extern "C" tss_status tss_pages_reserve(tss_pages* h, const tss_page_tables* t, 
     list.a[i] = seq[i];
     list.b[i] = want[i];
   }
-  reserve_kernel<<<1, kPlanThreads, 0, static_cast<cudaStream_t>(stream)>>>(list, pt, h->moves + 1);
-  return launched();
+  return launched(launch_k(reserve_kernel, dim3(1), dim3(kPlanThreads), 0, static_cast<cudaStream_t>(stream), true, list, pt, h->moves + 1));
 }
 
 extern "C" tss_status tss_pages_free(tss_pages* h, const tss_page_tables* t, int n, const int32_t* seq, const int32_t* keep, void* stream) {
@@ -488,8 +500,7 @@ extern "C" tss_status tss_pages_free(tss_pages* h, const tss_page_tables* t, int
     list.a[i] = seq[i];
     list.b[i] = keep ? keep[i] : 0;
   }
-  free_kernel<<<n, 256, 0, static_cast<cudaStream_t>(stream)>>>(list, pt);
-  return launched();
+  return launched(launch_k(free_kernel, dim3(n), dim3(256), 0, static_cast<cudaStream_t>(stream), true, list, pt));
 }
 
 extern "C" tss_status tss_pages_fork(tss_pages* h, const tss_page_tables* t, void* const* layer, int n_layers, size_t page_bytes, int n,
@@ -521,11 +532,9 @@ extern "C" tss_status tss_pages_fork(tss_pages* h, const tss_page_tables* t, voi
   if (need > h->n_pages) return refuse(TSS_ERR_KV_CAPACITY, "more copies than the pool has pages");
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   int* ids = h->moves + 1;
-  fork_choose_kernel<<<1, kPlanThreads, 0, s>>>(list, pt, static_cast<int>(need), ids, h->go);
-  st = launched();
+  st = launched(launch_k(fork_choose_kernel, dim3(1), dim3(kPlanThreads), 0, s, true, list, pt, static_cast<int>(need), ids, h->go));
   if (st != TSS_OK) return st;
-  fork_kernel<<<n + copy_grid(need, ly, h->sms), kCopyThreads, 0, s>>>(list, pt, ly, ids, h->go);
-  return launched();
+  return launched(launch_k(fork_kernel, dim3(n + copy_grid(need, ly, h->sms)), dim3(kCopyThreads), 0, s, true, list, pt, ly, ids, h->go));
 }
 
 extern "C" tss_status tss_pages_compact(tss_pages* h, const tss_page_tables* t, int32_t* table_out, int32_t* refs_out, void* const* layer,
@@ -538,13 +547,12 @@ extern "C" tss_status tss_pages_compact(tss_pages* h, const tss_page_tables* t, 
   if (!table_out || !refs_out) return refuse(TSS_ERR_INVALID_ARG, "NULL argument");
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const size_t smem = static_cast<size_t>((h->n_pages + 31) / 32) * 4;
-  compact_plan_kernel<<<1, kPlanThreads, smem, s>>>(pt, refs_out, h->moves, h->map);
-  st = launched();
+  st = launched(launch_k(compact_plan_kernel, dim3(1), dim3(kPlanThreads), smem, s, true, pt, refs_out, h->moves, h->map));
   if (st != TSS_OK) return st;
   const long long entries = static_cast<long long>(h->n_seqs) * h->max_pages;
   const int row_ctas = static_cast<int>(entries < 64LL * kCopyThreads * 4 ? (entries + kCopyThreads * 4 - 1) / (kCopyThreads * 4) : 64);
-  compact_kernel<<<row_ctas + copy_grid(h->n_pages, ly, h->sms), kCopyThreads, 0, s>>>(pt, ly, table_out, h->moves, h->map, row_ctas);
-  return launched();
+  return launched(launch_k(compact_kernel, dim3(row_ctas + copy_grid(h->n_pages, ly, h->sms)), dim3(kCopyThreads), 0, s, true, pt, ly, table_out,
+                           h->moves, h->map, row_ctas));
 }
 
 extern "C" tss_status tss_pages_copy(tss_pages* h, void* const* layer, int n_layers, size_t page_bytes, int n, const int32_t* src,
@@ -557,6 +565,6 @@ extern "C" tss_status tss_pages_copy(tss_pages* h, void* const* layer, int n_lay
   if (n == 0) return TSS_OK;
   if (!src || !dst) return refuse(TSS_ERR_INVALID_ARG, "NULL argument");
   PoolTables pt{nullptr, nullptr, nullptr, h->n_seqs, h->max_pages, h->n_pages, h->status};
-  copy_kernel<<<copy_grid(n, ly, h->sms), kCopyThreads, 0, static_cast<cudaStream_t>(stream)>>>(pt, ly, src, dst, n);
-  return launched();
+  return launched(launch_k(copy_kernel, dim3(copy_grid(n, ly, h->sms)), dim3(kCopyThreads), 0, static_cast<cudaStream_t>(stream), true, pt, ly, src,
+                           dst, n));
 }

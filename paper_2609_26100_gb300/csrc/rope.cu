@@ -33,6 +33,8 @@ constexpr int kRopeThreads = 128;
 template <typename T, int LANES, bool INTER>
 __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constant__ RopeParams p) {
   constexpr int kHeads = 32 / LANES;  // heads of a group: one turn of a warp
+  griddep_wait();
+  griddep_launch();
   const int lane = threadIdx.x & 31;
   const long long w = static_cast<long long>(blockIdx.x) * (kRopeThreads / 32) + (threadIdx.x >> 5);
   const long long row = w / p.splits;
@@ -118,21 +120,18 @@ __global__ void __launch_bounds__(256) rope_table_kernel(const __grid_constant__
 }
 
 template <typename T, int LANES>
-void rope_launch(const RopeParams& p, bool inter, unsigned grid, cudaStream_t s) {
-  if (inter)
-    rope_kernel<T, LANES, true><<<grid, kRopeThreads, 0, s>>>(p);
-  else
-    rope_kernel<T, LANES, false><<<grid, kRopeThreads, 0, s>>>(p);
+cudaError_t rope_launch(const RopeParams& p, bool inter, unsigned grid, cudaStream_t s) {
+  return launch_k(inter ? rope_kernel<T, LANES, true> : rope_kernel<T, LANES, false>, dim3(grid), dim3(kRopeThreads), 0, s, true, p);
 }
 
 template <typename T>
-void rope_dispatch(const RopeParams& p, bool inter, unsigned grid, cudaStream_t s, int lanes) {
+cudaError_t rope_dispatch(const RopeParams& p, bool inter, unsigned grid, cudaStream_t s, int lanes) {
   switch (lanes) {
-    case 1: rope_launch<T, 1>(p, inter, grid, s); break;
-    case 2: rope_launch<T, 2>(p, inter, grid, s); break;
-    case 4: rope_launch<T, 4>(p, inter, grid, s); break;
-    case 8: rope_launch<T, 8>(p, inter, grid, s); break;
-    default: rope_launch<T, 16>(p, inter, grid, s);
+    case 1: return rope_launch<T, 1>(p, inter, grid, s);
+    case 2: return rope_launch<T, 2>(p, inter, grid, s);
+    case 4: return rope_launch<T, 4>(p, inter, grid, s);
+    case 8: return rope_launch<T, 8>(p, inter, grid, s);
+    default: return rope_launch<T, 16>(p, inter, grid, s);
   }
 }
 
@@ -207,13 +206,10 @@ extern "C" tss_status tss_qk_rope(const tss_rope_args* a, void* stream) {
   if ((warps + per - 1) / per > 0x7fffffffLL) return refuse(TSS_ERR_INVALID_ARG, "too many rows for one launch");
   const unsigned grid = static_cast<unsigned>((warps + per - 1) / per);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (a->dtype == TSS_DTYPE_BF16)
-    rope_dispatch<__nv_bfloat16>(p, a->interleaved != 0, grid, s, lanes);
-  else if (a->dtype == TSS_DTYPE_F16)
-    rope_dispatch<__half>(p, a->interleaved != 0, grid, s, lanes);
-  else
-    rope_dispatch<float>(p, a->interleaved != 0, grid, s, lanes);
-  const cudaError_t e = cudaGetLastError();
+  const bool inter = a->interleaved != 0;
+  const cudaError_t e = a->dtype == TSS_DTYPE_BF16  ? rope_dispatch<__nv_bfloat16>(p, inter, grid, s, lanes)
+                        : a->dtype == TSS_DTYPE_F16 ? rope_dispatch<__half>(p, inter, grid, s, lanes)
+                                                    : rope_dispatch<float>(p, inter, grid, s, lanes);
   return e == cudaSuccess ? TSS_OK : refuse_cuda(e, "launch");
 }
 

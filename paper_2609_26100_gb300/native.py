@@ -326,13 +326,16 @@ def rope_args(q, k, q_out, k_out, positions, table, q_gain=None, k_gain=None, ep
 
 
 def current_stream() -> int:
+    """torch's current stream on the current device."""
     import torch
-    return torch.cuda.current_stream().cuda_stream
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def qk_rope(args: TssRopeArgs, stream=None) -> None:
     """tss_qk_rope on the given stream (None: torch's current one)."""
-    check(lib().tss_qk_rope(ctypes.byref(args), current_stream() if stream is None else stream), "tss_qk_rope")
+    s = lib().tss_qk_rope(ctypes.byref(args), current_stream() if stream is None else stream)
+    if s:
+        check(s, "tss_qk_rope")
 
 
 class TssError(RuntimeError):
@@ -358,7 +361,7 @@ def _ptr(t) -> Optional[int]:
 
 
 def _i32(values) -> "ctypes.Array":
-    arr = (ctypes.c_int32 * len(values))(*[int(v) for v in values])
+    arr = (ctypes.c_int32 * len(values))(*map(int, values))
     return arr
 
 

@@ -8,15 +8,15 @@ tensors; ``Kv4Cache.allocate`` makes a set that fits together.
 from __future__ import annotations
 
 import ctypes
-import math
 from typing import Optional, Sequence
 
 import torch
 
 from . import native
-from .native import _P, _i32, _ptr, _rows, check, lib
+from .native import _P, _i32, _ptr, check, current_stream, lib
 
 PAGE_TOKENS = native.PAGE_TOKENS
+_CODES = {torch.bfloat16: native.TSS_DTYPE_BF16, torch.float16: native.TSS_DTYPE_F16, torch.float32: native.TSS_DTYPE_F32}
 
 
 def page_bytes(n_kv_heads: int, head_dim: int) -> int:
@@ -31,8 +31,28 @@ def pages_for(tokens: int) -> int:
     return -(-int(tokens) // PAGE_TOKENS)
 
 
+def _row_stride(t: torch.Tensor, shape, what: str) -> int:
+    """Elements between the rows of t, which has the given shape and contiguous heads."""
+    if t.shape != shape:
+        raise ValueError(f"{what}: {list(shape)} is wanted")
+    row, head, one = t.stride()
+    n, h, d = shape
+    if n == 0:
+        return h * d
+    if one != 1 or (h > 1 and head != d):
+        raise ValueError(f"{what}: the heads of a row must be contiguous")
+    return row if n > 1 else max(row, h * d)
+
+
+def _code(t: torch.Tensor) -> int:
+    try:
+        return _CODES[t.dtype]
+    except KeyError:
+        raise TypeError(f"bfloat16, float16 or float32 is wanted, not {t.dtype}") from None
+
+
 def _ints(t: torch.Tensor, shape, what: str) -> None:
-    if tuple(t.shape) != tuple(shape) or t.dtype != torch.int32 or not t.is_contiguous():
+    if t.shape != shape or t.dtype != torch.int32 or not t.is_contiguous():
         raise ValueError(f"{what}: contiguous int32 {list(shape)} is wanted")
 
 
@@ -60,6 +80,7 @@ class PagePool:
         _ints(refs, (self.n_pages,), "refs")
         self.pool, self.table, self.held, self.refs = pool, table, held, refs
         self._tables = native.TssPageTables(table.data_ptr(), held.data_ptr(), refs.data_ptr())
+        self._ref = ctypes.byref(self._tables)
         h = _P()
         check(lib().tss_pages_create(self.n_seqs, self.max_pages, self.n_pages, ctypes.byref(h)), "tss_pages_create")
         self._h = h
@@ -76,13 +97,13 @@ class PagePool:
             pass
 
     def _stream(self, stream):
-        return native.current_stream() if stream is None else stream
+        return current_stream() if stream is None else stream
 
     def reserve(self, seqs: Sequence[int], tokens: Sequence[int], stream=None) -> None:
         """Pages for tokens[i] tokens of seqs[i] (those it holds stay)."""
         if len(seqs) != len(tokens):
             raise ValueError("seqs and tokens differ in length")
-        check(lib().tss_pages_reserve(self._h, ctypes.byref(self._tables), len(seqs), _i32(seqs),
+        check(lib().tss_pages_reserve(self._h, self._ref, len(seqs), _i32(seqs),
                                       _i32([pages_for(t) for t in tokens]), self._stream(stream)), "tss_pages_reserve")
 
     def free(self, seqs: Sequence[int], tokens: Optional[Sequence[int]] = None, stream=None) -> None:
@@ -90,7 +111,7 @@ class PagePool:
         if tokens is not None and len(seqs) != len(tokens):
             raise ValueError("seqs and tokens differ in length")
         keep = _i32([pages_for(t) for t in tokens]) if tokens is not None else None
-        check(lib().tss_pages_free(self._h, ctypes.byref(self._tables), len(seqs), _i32(seqs), keep, self._stream(stream)),
+        check(lib().tss_pages_free(self._h, self._ref, len(seqs), _i32(seqs), keep, self._stream(stream)),
               "tss_pages_free")
 
     def fork(self, src: Sequence[int], dst: Sequence[int], tokens: Sequence[int], stream=None) -> None:
@@ -99,7 +120,7 @@ class PagePool:
         n = len(src)
         if len(dst) != n or len(tokens) != n:
             raise ValueError("src, dst and tokens differ in length")
-        check(lib().tss_pages_fork(self._h, ctypes.byref(self._tables), self._ptrs, self.n_layers, self.page_bytes, n, _i32(src),
+        check(lib().tss_pages_fork(self._h, self._ref, self._ptrs, self.n_layers, self.page_bytes, n, _i32(src),
                                    _i32(dst), _i32([int(t) // PAGE_TOKENS for t in tokens]),
                                    _i32([pages_for(t) for t in tokens]), self._stream(stream)), "tss_pages_fork")
 
@@ -109,7 +130,7 @@ class PagePool:
         t, r = (self.table if table_out is None else table_out), (self.refs if refs_out is None else refs_out)
         _ints(t, self.table.shape, "table_out")
         _ints(r, self.refs.shape, "refs_out")
-        check(lib().tss_pages_compact(self._h, ctypes.byref(self._tables), t.data_ptr(), r.data_ptr(), self._ptrs, self.n_layers,
+        check(lib().tss_pages_compact(self._h, self._ref, t.data_ptr(), r.data_ptr(), self._ptrs, self.n_layers,
                                       self.page_bytes, self._stream(stream)), "tss_pages_compact")
 
     def copy(self, src: torch.Tensor, dst: torch.Tensor, stream=None) -> None:
@@ -137,6 +158,8 @@ class Kv4Cache:
         self._ptrs, n_layers, n_pages, _ = _layers(pool)
         self._cache = native.TssPagedCache(ctypes.cast(self._ptrs, ctypes.POINTER(_P)), n_layers, n_pages, table.data_ptr(),
                                            table.shape[0], table.shape[1])
+        self._cache_ref = ctypes.byref(self._cache)
+        self._c_append, self._c_read, self._c_attention = lib().tss_paged_append, lib().tss_paged_read, lib().tss_paged_attention
         self.pages: Optional[PagePool] = None
         h = _P()
         check(lib().tss_paged_create(n_q_heads, n_kv_heads, head_dim, ctypes.byref(h)), "tss_paged_create")
@@ -174,32 +197,31 @@ class Kv4Cache:
         keep = [_i32(seqs), _i32(first), _i32(n_tokens)]
         b = native.TssPagedBatch(len(seqs), *[ctypes.cast(a, _P) for a in keep])
         b._keep = keep
+        b.ref = ctypes.byref(b)
         b.rows = sum(int(n) for n in n_tokens)
         return b
 
-    def _kv(self, t: torch.Tensor, batch, what: str) -> int:
-        n, h, d, stride = _rows(t, what)
-        if (n, h, d) != (batch.rows, self.n_kv_heads, self.head_dim):
-            raise ValueError(f"{what}: [{batch.rows}][{self.n_kv_heads}][{self.head_dim}] is wanted")
-        return stride
-
     def append(self, layer: int, batch, k: torch.Tensor, v: torch.Tensor, stream=None) -> None:
         """Quantise k, v [rows][kv heads][head_dim] into the pages of the batch's tokens."""
+        shape = (batch.rows, self.n_kv_heads, self.head_dim)
         if k.dtype != v.dtype:
             raise ValueError("k and v differ in type")
-        check(lib().tss_paged_append(self._h, ctypes.byref(self._cache), layer, ctypes.byref(batch), k.data_ptr(), v.data_ptr(),
-                                     self._kv(k, batch, "k"), self._kv(v, batch, "v"), native.dtype_code(k),
-                                     native.current_stream() if stream is None else stream), "tss_paged_append")
+        s = self._c_append(self._h, self._cache_ref, layer, batch.ref, k.data_ptr(), v.data_ptr(), _row_stride(k, shape, "k"),
+                           _row_stride(v, shape, "v"), _code(k), current_stream() if stream is None else stream)
+        if s:
+            check(s, "tss_paged_append")
 
     def read(self, layer: int, batch, k: Optional[torch.Tensor], v: Optional[torch.Tensor], stream=None) -> None:
         """The values that the batch's tokens are held as, to k and v (either may be None)."""
+        shape = (batch.rows, self.n_kv_heads, self.head_dim)
         one = k if k is not None else v
         if one is None or (k is not None and v is not None and k.dtype != v.dtype):
             raise ValueError("k or v is wanted, of one type")
-        strides = [self._kv(t, batch, w) if t is not None else 0 for t, w in ((k, "k"), (v, "v"))]
-        check(lib().tss_paged_read(self._h, ctypes.byref(self._cache), layer, ctypes.byref(batch), _ptr(k), _ptr(v), *strides,
-                                   native.dtype_code(one), native.current_stream() if stream is None else stream),
-              "tss_paged_read")
+        s = self._c_read(self._h, self._cache_ref, layer, batch.ref, None if k is None else k.data_ptr(),
+                         None if v is None else v.data_ptr(), 0 if k is None else _row_stride(k, shape, "k"),
+                         0 if v is None else _row_stride(v, shape, "v"), _code(one), current_stream() if stream is None else stream)
+        if s:
+            check(s, "tss_paged_read")
 
     def attention(self, layer: int, batch, q: torch.Tensor, out: torch.Tensor, lse: Optional[torch.Tensor] = None, *,
                   scale: Optional[float] = None, window: int = 0, sinks: int = 0, mask: Optional[torch.Tensor] = None,
@@ -207,22 +229,22 @@ class Kv4Cache:
         """Attention of the batch's rows (already appended) over their sequences: q, out [rows][heads][head_dim];
         lse float32 [rows][heads]; mask int64 [rows][2] (bits of the block's rows that a row sees; None: a chain);
         window and sinks as in tss_paged_attention, positions int32 [rows]."""
-        n, h, d, stride = _rows(q, "q")
-        if (n, h, d) != (batch.rows, self.n_q_heads, self.head_dim):
-            raise ValueError(f"q: [{batch.rows}][{self.n_q_heads}][{self.head_dim}] is wanted")
-        if out.shape != q.shape or out.dtype != q.dtype or out.device != q.device:
-            raise ValueError("out: the shape, type and device of q are wanted")
-        if lse is not None and (tuple(lse.shape) != (n, h) or lse.dtype != torch.float32 or not lse.is_contiguous()):
+        n, h, d = shape = (batch.rows, self.n_q_heads, self.head_dim)
+        if out.dtype != q.dtype or out.device != q.device:
+            raise ValueError("out: the type and device of q are wanted")
+        if lse is not None and (lse.shape != (n, h) or lse.dtype != torch.float32 or not lse.is_contiguous()):
             raise ValueError("lse: contiguous float32 [rows][heads] is wanted")
-        if mask is not None and (tuple(mask.shape) != (n, 2) or mask.dtype not in (torch.int64, torch.uint64)
-                                 or not mask.is_contiguous()):
+        if mask is not None and (mask.shape != (n, 2) or mask.dtype not in (torch.int64, torch.uint64) or not mask.is_contiguous()):
             raise ValueError("mask: contiguous 64-bit [rows][2] is wanted")
         if positions is not None:
             _ints(positions, (n,), "positions")
-        a = native.TssPagedAttn(q.data_ptr(), stride, out.data_ptr(), _rows(out, "out")[3], _ptr(lse), native.dtype_code(q),
-                                1.0 / math.sqrt(d) if scale is None else scale, window, sinks, _ptr(mask), _ptr(positions))
-        check(lib().tss_paged_attention(self._h, ctypes.byref(self._cache), layer, ctypes.byref(batch), ctypes.byref(a),
-                                        native.current_stream() if stream is None else stream), "tss_paged_attention")
+        a = native.TssPagedAttn(q.data_ptr(), _row_stride(q, shape, "q"), out.data_ptr(), _row_stride(out, shape, "out"),
+                                None if lse is None else lse.data_ptr(), _code(q), d ** -0.5 if scale is None else scale, window,
+                                sinks, None if mask is None else mask.data_ptr(), None if positions is None else positions.data_ptr())
+        s = self._c_attention(self._h, self._cache_ref, layer, batch.ref, ctypes.byref(a),
+                              current_stream() if stream is None else stream)
+        if s:
+            check(s, "tss_paged_attention")
 
     def sync_status(self, stream=None) -> int:
-        return lib().tss_paged_sync_status(self._h, native.current_stream() if stream is None else stream)
+        return lib().tss_paged_sync_status(self._h, current_stream() if stream is None else stream)
