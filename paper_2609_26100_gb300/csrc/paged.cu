@@ -394,7 +394,7 @@ extern "C" tss_status tss_paged_create(int n_q_heads, int n_kv_heads, int head_d
   h->hk = n_kv_heads;
   h->d = head_dim;
   h->sms = sms;
-  const size_t rows = pa_partial_rows(sms);
+  const size_t rows = pa_partial_rows(sms, head_dim);
   cudaError_t e = pa_prepare_all();
   if (e == cudaSuccess) e = cudaMalloc(&h->status, 256);
   if (e == cudaSuccess) e = cudaMemset(h->status, 0, 256);

@@ -28,7 +28,7 @@ struct PgAttnArgs {
   const int* positions;
   int* status;
 };
-size_t pa_partial_rows(int sms);
+size_t pa_partial_rows(int sms, int head_dim);
 int pa_counters(int sms);
 cudaError_t pa_prepare_all();
 // *too_large: more work than one launch counts (nothing was launched).

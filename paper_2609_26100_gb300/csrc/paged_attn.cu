@@ -26,37 +26,14 @@
 // share leave partials, which the last CTA to arrive joins in CTA order (results do not depend on timing).
 #include <type_traits>
 
-#include "paged.h"
+#include "paged_attn.cuh"
 
 namespace tss {
 namespace {
 
-struct PaReq {
-  int seq, first, n, row;
-  int units;             // of one item: those in sight, [0, sink) and [lo, ...)
-  int sink, lo;
-  int off;               // units of all items before the request
-  int cta, splits;       // aligned runs: CTAs before the request, CTAs of one item
-};
-struct PaParams {
-  PgAttnArgs a;
-  int n_req, total;      // units in all
-  int aligned;           // a CTA's run lies within one item
-  int halves;            // 32-token halves of a unit: 2 (a page) or 1
-  float* part_o;         // [grid][2][rows][D]
-  float2* part_ml;       // [grid][2][rows]
-  int* counters;         // [grid], zero between launches
-  PaReq r[kPgMaxReq];
-};
-
 __device__ __forceinline__ uint32_t movmatrix_t(uint32_t x) {
   uint32_t y;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
-  return y;
-}
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
 
@@ -69,29 +46,6 @@ __device__ __forceinline__ void mma_f16_first(float* d, const uint32_t* a, const
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]), "f"(0.f));
 }
 
-// Two fp32 operations in one instruction.
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-  float2 d;
-  asm("{\n\t.reg .b64 x, y, z, w;\n\t"
-      "mov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
-      "fma.rn.f32x2 w, x, y, z;\n\t"
-      "mov.b64 {%0, %1}, w;\n\t}\n"
-      : "=f"(d.x), "=f"(d.y)
-      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-  return d;
-}
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-  float2 d;
-  asm("{\n\t.reg .b64 x, y, w;\n\t"
-      "mov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t"
-      "add.rn.f32x2 w, x, y;\n\t"
-      "mov.b64 {%0, %1}, w;\n\t}\n"
-      : "=f"(d.x), "=f"(d.y)
-      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-  return d;
-}
-constexpr float kTop = 32768.f;         // p s' that raises the reference
-constexpr float kLeast = 5.9604645e-8f; // fp16's smallest scale
 
 // A ring stage holds a page's block (or half of each of its parts).
 template <int D, int NT>
@@ -136,20 +90,8 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
   if (tid == 0) abort_s = 0;
   fence_mbar_init();
   // the CTA's run of units [u0, u1)
-  int u0, u1, first_cta = 0, splits = 0;  // (of an aligned run: its item's CTAs)
-  if (p.aligned) {
-    int b = 0;
-    while (b + 1 < p.n_req && p.r[b + 1].cta <= static_cast<int>(blockIdx.x)) ++b;
-    const PaReq& r = p.r[b];
-    const int c = blockIdx.x - r.cta, item = c / r.splits, j = c - item * r.splits, at = r.off + item * r.units;
-    u0 = at + static_cast<int>(static_cast<long long>(r.units) * j / r.splits);
-    u1 = at + static_cast<int>(static_cast<long long>(r.units) * (j + 1) / r.splits);
-    first_cta = blockIdx.x - j;
-    splits = r.splits;
-  } else {
-    u0 = static_cast<int>(static_cast<long long>(p.total) * blockIdx.x / gridDim.x);
-    u1 = static_cast<int>(static_cast<long long>(p.total) * (blockIdx.x + 1) / gridDim.x);
-  }
+  int u0, u1, first_cta, splits;
+  cta_run(p, &u0, &u1, &first_cta, &splits);
   __syncthreads();
   griddep_wait();    // (nothing before this reads or writes what another kernel may)
   griddep_launch();
@@ -246,9 +188,7 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
       }
       big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
       big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
-      // 2^e big in [2^14, 2^15); e kept within what 2^e and 2^(24 - e) can be
-      const int e = min(100, max(-100, 14 - (static_cast<int>(__float_as_uint(big) >> 23) - 127)));
-      const float up = big > 0.f && big < INFINITY ? __uint_as_float(static_cast<uint32_t>(e + 127) << 23) : 1.f;
+      const float up = query_scale(big);
       const float mul = a.scale_log2 * 16777216.f / up;
       float sum[G];
 #pragma unroll
@@ -546,28 +486,12 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
     const bool whole = x0 == 0 && x1 == r.units;
     int c0 = first_cta, c1 = first_cta + splits - 1;  // CTAs that share the item
     if (!whole && !p.aligned) {
-      const long long T = p.total, Gd = gridDim.x;
-      const int i0 = u - x0, i1 = i0 + r.units - 1;
-      c0 = static_cast<int>(i0 * Gd / T);
-      while ((c0 + 1) * T / Gd <= i0) ++c0;
-      c1 = static_cast<int>(i1 * Gd / T);
-      while ((c1 + 1) * T / Gd <= i1) ++c1;
+      c0 = cta_of_unit(u - x0, p.total);
+      c1 = cta_of_unit(u - x0 + r.units - 1, p.total);
     }
     // a CTA's two partials: of the item that it begins, and of the one that it ends or runs through
     const int slot = blockIdx.x * 2 + (x0 == 0 ? 1 : 0);
-    const auto finish = [&](int row, int c4, float M, float L, float4 x) {
-      const float inv = L > 0.f ? 1.f / L : L == 0.f ? 0.f : L;  // (a NaN stays one)
-      const float y[4] = {x.x * inv, x.y * inv, x.z * inv, x.w * inv};
-      const int qr = row0 + row;
-      const long long tok = r.row + qr / gq;
-      const int head = h * gq + qr % gq;
-      const long long at = tok * a.os + static_cast<long long>(head) * D + c4 * 4;
-      if (a.is_half)
-        store_vec<__half, 4>(static_cast<__half*>(a.out) + at, y);
-      else
-        store_vec<__nv_bfloat16, 4>(static_cast<__nv_bfloat16*>(a.out) + at, y);
-      if (c4 == 0 && a.lse) a.lse[tok * a.hq + head] = (M + log2f(L)) * 0.6931471805599453f;
-    };
+    const auto finish = [&](int row, int c4, float M, float L, float4 x) { finish_row<D>(a, r, h, row0 + row, c4, M, L, x); };
     // the parts of (row, 4 dims), with the rows' references and sums
     const auto joined = [&](int row, int c4, float2* ml, float4* sum) {
       float M = -INFINITY, L = 0.f;
@@ -611,47 +535,11 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
       __syncthreads();
       if (s_last) {
         // Few rows: several warps take a row, each some of its partials.
-        const int per_row = rows == 1 ? W : rows == 2 ? W / 2 : 1, slice = warp % per_row, n = c1 - c0 + 1;
+        const int per_row = rows == 1 ? W : rows == 2 ? W / 2 : 1, slice = warp % per_row;
         for (int row = warp / per_row; row < rows; row += W / per_row) {
-          // lane l: reference and sum of the slice's partials l, l + 32, ...
-          float M = -INFINITY, L = 0.f;
-          const int mine_n = n > slice ? (n - slice + per_row - 1) / per_row : 0;
-          const auto slot_of = [&](int k) {
-            const int c = c0 + slice + k * per_row;
-            return static_cast<long long>(c * 2 + (c == c0)) * R + row;
-          };
-          for (int k = lane; k < mine_n; k += 32) M = fmaxf(M, __ldcg(p.part_ml + slot_of(k)).x);
-#pragma unroll
-          for (int x = 16; x > 0; x >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, x));
-          const float mb = M == -INFINITY ? 0.f : M;
-          float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-          for (int k0 = 0; k0 < mine_n; k0 += 32) {
-            float fw = 0.f;
-            if (k0 + lane < mine_n) {
-              const float2 ml = __ldcg(p.part_ml + slot_of(k0 + lane));
-              fw = ex2(ml.x - mb);
-              L = fmaf(fw, ml.y, L);
-            }
-            const int m = min(32, mine_n - k0);
-            for (int k = 0; k < m; k += 8) {
-              float4 y[8];
-#pragma unroll
-              for (int i = 0; i < 8; ++i)
-                y[i] = k + i < m && lane < D / 4 ? __ldcg(reinterpret_cast<const float4*>(p.part_o + slot_of(k0 + k + i) * D) + lane)
-                                                 : make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-              for (int i = 0; i < 8; ++i) {
-                const float x = __shfl_sync(0xffffffffu, fw, (k + i) & 31);
-                if (k + i >= m) continue;
-                sum.x = fmaf(x, y[i].x, sum.x);
-                sum.y = fmaf(x, y[i].y, sum.y);
-                sum.z = fmaf(x, y[i].z, sum.z);
-                sum.w = fmaf(x, y[i].w, sum.w);
-              }
-            }
-          }
-#pragma unroll
-          for (int x = 16; x > 0; x >>= 1) L += __shfl_xor_sync(0xffffffffu, L, x);
+          float M, L;
+          float4 sum;
+          gather_partials<D>(p, R, c0, c1, row, slice, per_row, &M, &L, &sum);
           if (per_row == 1) {
             if (lane < D / 4) finish(row, lane, M, L, sum);
           } else {
@@ -694,32 +582,8 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
 template <int D, int NT>
 cudaError_t pa_launch(PaParams& p, int sms, cudaStream_t s) {
   using S = PaShape<D, NT>;
-  // Runs of equal length, or aligned to items where one CTA's run is then not much longer (ending an item
-  // costs about as much as 8 units): every CTA ends one item instead of two or three.  At least one unit a
-  // warp.
-  const int most = sms * S::kCtas, even = (p.total + most - 1) / most;
-  int run = even > S::kWarps ? even : S::kWarps;
-  const auto ctas = [&](int len) {
-    long long n = 0;
-    for (int i = 0; i < p.n_req; ++i) {
-      const int items = (i + 1 < p.n_req ? p.r[i + 1].off : p.total) - p.r[i].off;
-      n += items / p.r[i].units * static_cast<long long>((p.r[i].units + len - 1) / len);
-    }
-    return n;
-  };
-  while (run <= even + 8 && ctas(run) > most) ++run;
-  int grid = 0;
-  p.aligned = run <= even + 8;
-  if (p.aligned) {
-    for (int i = 0; i < p.n_req; ++i) {
-      const int items = ((i + 1 < p.n_req ? p.r[i + 1].off : p.total) - p.r[i].off) / p.r[i].units;
-      p.r[i].cta = grid;
-      p.r[i].splits = (p.r[i].units + run - 1) / run;
-      grid += items * p.r[i].splits;
-    }
-  } else {
-    grid = most;
-  }
+  // (a run of a unit for each warp at least; ending an item costs about as much as 8 units)
+  const int grid = pa_cut(p, sms * S::kCtas, S::kWarps, 8);
   return launch_k(paged_attn_kernel<D, NT>, dim3(grid), dim3(S::kWarps * 32), S::kSmem, s, true, p);
 }
 template <int D, int NT>
@@ -730,15 +594,16 @@ cudaError_t pa_prepare() {
 
 }  // namespace
 
-// (two partials of 8 rows for four CTAs of an SM, of 16 for two)
-size_t pa_partial_rows(int sms) { return static_cast<size_t>(sms) * 2 * 32; }
-int pa_counters(int sms) { return sms * 4; }
+// (two partials of 8 rows for three CTAs of an SM, of 16 for two, of 128 for one of the tcgen05 kernel)
+size_t pa_partial_rows(int sms, int head_dim) { return static_cast<size_t>(sms) * 2 * (head_dim == 128 ? 128 : 32); }
+int pa_counters(int sms) { return sms * 3; }
 
 cudaError_t pa_prepare_all() {
   cudaError_t e = pa_prepare<64, 1>();
   if (e == cudaSuccess) e = pa_prepare<64, 2>();
   if (e == cudaSuccess) e = pa_prepare<128, 1>();
   if (e == cudaSuccess) e = pa_prepare<128, 2>();
+  if (e == cudaSuccess) e = paged_attn_tc_prepare();
   return e;
 }
 
@@ -746,46 +611,46 @@ cudaError_t launch_paged_attention(const tss_paged* h, const PgAttnArgs& a, cons
   *too_large = false;
   PaParams p;
   p.a = a;
-  p.n_req = 0;
   p.part_o = h->part_o;
   p.part_ml = h->part_ml;
   p.counters = h->counters;
+  // Blocks of more than kPaTcRows query rows of a KV head go to the tcgen05 kernel (head_dim 128).
   const int gq = h->hq / h->hk;
-  int most = 0;
-  for (int i = 0; i < batch.n_req; ++i) most = batch.r[i].n * gq > most ? batch.r[i].n * gq : most;
-  const int R = most <= 8 ? 8 : 16;
-  // Units of a page; of half a page where that leaves the warps less than three pages each (a warp takes about
-  // 2 us for a page, so a short launch is as long as its longest warp).
-  long long at = 0;
-  for (int halves = 2; halves > 0; --halves) {
-    const int unit = 32 * halves;
-    p.halves = halves;
-    p.n_req = 0;
-    at = 0;
-    for (int i = 0; i < batch.n_req; ++i) {
-      const PgReq& q = batch.r[i];
-      if (q.n == 0) continue;
-      PaReq& r = p.r[p.n_req++];
-      r = PaReq{q.seq, q.first, q.n, q.row, 0, 0, 0, static_cast<int>(at), 0, 1};
-      const int end = (q.first + q.n + unit - 1) / unit;
-      if (a.window) {
-        r.lo = (q.first - a.window + 1 > 0 ? q.first - a.window + 1 : 0) / unit;
-        const int sinks = a.sinks < q.first + q.n ? a.sinks : q.first + q.n;
-        r.sink = (sinks + unit - 1) / unit;
-        if (r.sink > r.lo) r.sink = r.lo;
-      }
-      r.units = r.sink + end - r.lo;
-      at += static_cast<long long>(r.units) * h->hk * ((q.n * gq + R - 1) / R);
-      if (at > 0x3fffffff) {
-        *too_large = true;
-        return cudaSuccess;
-      }
-    }
-    if (at >= 3LL * h->sms * (R == 8 ? 12 : 8)) break;
+  int most = 0, wide = 0;
+  for (int i = 0; i < batch.n_req; ++i) {
+    const int rows = batch.r[i].n * gq;
+    if (h->d == 128 && rows > kPaTcRows)
+      ++wide;
+    else
+      most = rows > most ? rows : most;
   }
-  p.total = static_cast<int>(at);
-  if (h->d == 64) return R == 8 ? pa_launch<64, 1>(p, h->sms, s) : pa_launch<64, 2>(p, h->sms, s);
-  return R == 8 ? pa_launch<128, 1>(p, h->sms, s) : pa_launch<128, 2>(p, h->sms, s);
+  if (wide) {
+    if (!pa_plan(p, batch, [&](const PgReq& q) { return q.n * gq > kPaTcRows; }, 128, 2)) {
+      *too_large = true;
+      return cudaSuccess;
+    }
+  }
+  PaParams narrow;
+  if (most) {
+    narrow.a = a;
+    narrow.part_o = p.part_o;
+    narrow.part_ml = p.part_ml;
+    narrow.counters = p.counters;
+    const int R = most <= 8 ? 8 : 16;
+    const auto take = [&](const PgReq& q) { return h->d != 128 || q.n * gq <= kPaTcRows; };
+    // Units of a page; of half a page where that leaves the warps less than three pages each (a warp takes
+    // about 2 us for a page, so a short launch is as long as its longest warp).
+    bool fits = pa_plan(narrow, batch, take, R, 2);
+    if (fits && narrow.total < 3LL * h->sms * (R == 8 ? 12 : 8)) fits = pa_plan(narrow, batch, take, R, 1);
+    if (!fits) {
+      *too_large = true;
+      return cudaSuccess;
+    }
+    const cudaError_t e = h->d == 64 ? (R == 8 ? pa_launch<64, 1>(narrow, h->sms, s) : pa_launch<64, 2>(narrow, h->sms, s))
+                                     : (R == 8 ? pa_launch<128, 1>(narrow, h->sms, s) : pa_launch<128, 2>(narrow, h->sms, s));
+    if (e != cudaSuccess) return e;
+  }
+  return wide ? launch_paged_attention_tc(p, h->sms, s) : cudaSuccess;
 }
 
 }  // namespace tss

@@ -1,0 +1,231 @@
+// What the two kernels of the paged attention share: the plan of a launch, the joining of partial results,
+// the output of a row.
+#pragma once
+
+#include "paged.h"
+
+namespace tss {
+
+struct PaReq {
+  int seq, first, n, row;
+  int units;             // of one item: those in sight, [0, sink) and [lo, ...)
+  int sink, lo;
+  int off;               // units of all items before the request
+  int cta, splits;       // aligned runs: CTAs before the request, CTAs of one item
+};
+struct PaParams {
+  PgAttnArgs a;
+  int n_req, total;      // units in all
+  int aligned;           // a CTA's run lies within one item
+  int halves;            // 32-token halves of a unit: 2 (a page) or 1
+  float* part_o;         // [grid][2][rows][D]
+  float2* part_ml;       // [grid][2][rows]
+  int* counters;         // [grid], zero between launches
+  PaReq r[kPgMaxReq];
+};
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n\t.reg .b64 x, y, z, w;\n\t"
+      "mov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
+      "fma.rn.f32x2 w, x, y, z;\n\t"
+      "mov.b64 {%0, %1}, w;\n\t}\n"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 x, y, w;\n\t"
+      "mov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t"
+      "add.rn.f32x2 w, x, y;\n\t"
+      "mov.b64 {%0, %1}, w;\n\t}\n"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+
+// The tcgen05 kernel (paged_attn_tc.cu; head_dim 128, planned with R = 128 and whole pages) and the query rows of a KV
+// head from which (exclusive) a request goes there.
+constexpr int kPaTcRows = 32;
+cudaError_t paged_attn_tc_prepare();
+cudaError_t launch_paged_attention_tc(PaParams& p, int sms, cudaStream_t s);
+
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 x, y, w;\n\t"
+      "mov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t"
+      "mul.rn.f32x2 w, x, y;\n\t"
+      "mov.b64 {%0, %1}, w;\n\t}\n"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+
+// The power of two that brings a row's largest query value `big` into [2^14, 2^15), where fp16 holds the row exactly
+// (kept within what it and its use in 2^24 / it can be; 1 for a row of zeros, or with an infinity).
+__device__ __forceinline__ float query_scale(float big) {
+  const int e = min(100, max(-100, 14 - (static_cast<int>(__float_as_uint(big) >> 23) - 127)));
+  return big > 0.f && big < INFINITY ? __uint_as_float(static_cast<uint32_t>(e + 127) << 23) : 1.f;
+}
+
+// p s' that raises a row's reference, and fp16's smallest scale.
+constexpr float kTop = 32768.f;
+constexpr float kLeast = 5.9604645e-8f;
+
+// The CTA whose even run of the launch's units holds unit u.
+__device__ __forceinline__ int cta_of_unit(int u, int total) {
+  const long long T = total, G = gridDim.x;
+  int c = static_cast<int>(u * G / T);
+  while ((c + 1) * T / G <= u) ++c;
+  return c;
+}
+
+// The CTA's run of units [u0, u1); of an aligned run, its item's first CTA and the number of them.
+__device__ __forceinline__ void cta_run(const PaParams& p, int* u0, int* u1, int* first_cta, int* splits) {
+  const int cta = blockIdx.x;
+  if (p.aligned) {
+    int b = 0;
+    while (b + 1 < p.n_req && p.r[b + 1].cta <= cta) ++b;
+    const PaReq& r = p.r[b];
+    const int c = cta - r.cta, item = c / r.splits, j = c - item * r.splits, at = r.off + item * r.units;
+    *u0 = at + static_cast<int>(static_cast<long long>(r.units) * j / r.splits);
+    *u1 = at + static_cast<int>(static_cast<long long>(r.units) * (j + 1) / r.splits);
+    *first_cta = cta - j;
+    *splits = r.splits;
+  } else {
+    *u0 = static_cast<int>(static_cast<long long>(p.total) * cta / gridDim.x);
+    *u1 = static_cast<int>(static_cast<long long>(p.total) * (cta + 1) / gridDim.x);
+    *first_cta = *splits = 0;
+  }
+}
+
+// One warp: the partials that CTAs c0 + slice, c0 + slice + step, ... up to c1 left of a row, joined: the
+// reference and sum (in all lanes) and, in lane l < D / 4, dims 4 l .. 4 l + 3 of the unnormalised output.
+// An item's first CTA left its part in its second slot, the others in their first.
+template <int D>
+__device__ __forceinline__ void gather_partials(const PaParams& p, int R, int c0, int c1, int row, int slice, int step, float* ref, float* sum,
+                                                float4* out) {
+  const int lane = threadIdx.x & 31, n = c1 - c0 + 1, mine = n > slice ? (n - slice + step - 1) / step : 0;
+  const auto slot = [&](int k) {
+    const int c = c0 + slice + k * step;
+    return static_cast<long long>(c * 2 + (c == c0)) * R + row;
+  };
+  float M = -INFINITY, L = 0.f;
+  for (int k = lane; k < mine; k += 32) M = fmaxf(M, __ldcg(p.part_ml + slot(k)).x);
+#pragma unroll
+  for (int x = 16; x > 0; x >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, x));
+  const float mb = M == -INFINITY ? 0.f : M;
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int k0 = 0; k0 < mine; k0 += 32) {
+    float fw = 0.f;
+    if (k0 + lane < mine) {
+      const float2 ml = __ldcg(p.part_ml + slot(k0 + lane));
+      fw = ex2(ml.x - mb);
+      L = fmaf(fw, ml.y, L);
+    }
+    const int m = min(32, mine - k0);
+    for (int k = 0; k < m; k += 8) {
+      float4 y[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        y[i] = k + i < m && lane < D / 4 ? __ldcg(reinterpret_cast<const float4*>(p.part_o + slot(k0 + k + i) * D) + lane)
+                                         : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float x = __shfl_sync(0xffffffffu, fw, (k + i) & 31);
+        if (k + i >= m) continue;
+        s.x = fmaf(x, y[i].x, s.x);
+        s.y = fmaf(x, y[i].y, s.y);
+        s.z = fmaf(x, y[i].z, s.z);
+        s.w = fmaf(x, y[i].w, s.w);
+      }
+    }
+  }
+#pragma unroll
+  for (int x = 16; x > 0; x >>= 1) L += __shfl_xor_sync(0xffffffffu, L, x);
+  *ref = M;
+  *sum = L;
+  *out = s;
+}
+
+// Four dims (from 4 c4) of the output of query row qr (token qr / group, query head of KV head h), and its lse.
+template <int D>
+__device__ __forceinline__ void finish_row(const PgAttnArgs& a, const PaReq& r, int h, int qr, int c4, float M, float L, float4 x) {
+  const int gq = a.hq / a.hk;
+  const float inv = L > 0.f ? 1.f / L : L == 0.f ? 0.f : L;  // (a NaN stays one)
+  const float y[4] = {x.x * inv, x.y * inv, x.z * inv, x.w * inv};
+  const long long tok = r.row + qr / gq;
+  const int head = h * gq + qr % gq;
+  const long long at = tok * a.os + static_cast<long long>(head) * D + c4 * 4;
+  if (a.is_half)
+    store_vec<__half, 4>(static_cast<__half*>(a.out) + at, y);
+  else
+    store_vec<__nv_bfloat16, 4>(static_cast<__nv_bfloat16*>(a.out) + at, y);
+  if (c4 == 0 && a.lse) a.lse[tok * a.hq + head] = (M + log2f(L)) * 0.6931471805599453f;
+}
+
+// ------------------------------------------------------------------------------------------
+// Host: the plan of a launch
+// ------------------------------------------------------------------------------------------
+// The requests of the batch that `take` picks, in row tiles of R query rows and units of `halves` 32-token
+// halves; false where the units pass 2^30.
+template <typename Take>
+inline bool pa_plan(PaParams& p, const PgBatch& batch, Take take, int R, int halves) {
+  const PgAttnArgs& a = p.a;
+  const int unit = 32 * halves, gq = a.hq / a.hk;
+  long long at = 0;
+  p.halves = halves;
+  p.n_req = 0;
+  for (int i = 0; i < batch.n_req; ++i) {
+    const PgReq& q = batch.r[i];
+    if (q.n == 0 || !take(q)) continue;
+    PaReq& r = p.r[p.n_req++];
+    r = PaReq{q.seq, q.first, q.n, q.row, 0, 0, 0, static_cast<int>(at), 0, 1};
+    const int end = (q.first + q.n + unit - 1) / unit;
+    if (a.window) {
+      r.lo = (q.first - a.window + 1 > 0 ? q.first - a.window + 1 : 0) / unit;
+      const int sinks = a.sinks < q.first + q.n ? a.sinks : q.first + q.n;
+      r.sink = (sinks + unit - 1) / unit;
+      if (r.sink > r.lo) r.sink = r.lo;
+    }
+    r.units = r.sink + end - r.lo;
+    at += static_cast<long long>(r.units) * a.hk * ((q.n * gq + R - 1) / R);
+    if (at > 0x3fffffff) return false;
+  }
+  p.total = static_cast<int>(at);
+  return true;
+}
+
+// Cuts the units into runs for at most `most` CTAs and returns their number: even runs, or, where a CTA's run
+// is then at most `slack` units longer, runs that lie within one item each (a CTA ends one item instead of two or
+// three).  Runs have at least `least` units.
+inline int pa_cut(PaParams& p, int most, int least, int slack) {
+  const int even = (p.total + most - 1) / most;
+  const auto items = [&](int i) { return ((i + 1 < p.n_req ? p.r[i + 1].off : p.total) - p.r[i].off) / p.r[i].units; };
+  const auto ctas = [&](int len) {
+    long long n = 0;
+    for (int i = 0; i < p.n_req; ++i) n += static_cast<long long>(items(i)) * ((p.r[i].units + len - 1) / len);
+    return n;
+  };
+  int run = even > least ? even : least;
+  while (run <= even + slack && ctas(run) > most) ++run;
+  p.aligned = run <= even + slack;
+  if (!p.aligned) return p.total < most ? p.total : most;
+  int grid = 0;
+  for (int i = 0; i < p.n_req; ++i) {
+    p.r[i].cta = grid;
+    p.r[i].splits = (p.r[i].units + run - 1) / run;
+    grid += items(i) * p.r[i].splits;
+  }
+  return grid;
+}
+
+}  // namespace tss
