@@ -10,12 +10,13 @@
 // ANDs and a shift; the order of the 8 within it (0, 4, 1, 5, 2, 6, 3, 7) and the factor 16 of odd nibbles are
 // matched in Q and P.
 //
-// Roles (448 threads): warp 0 copies pages (one bulk copy each), warp 1 issues MMAs, warps 2-5 expand codes
-// and parameters, warps 6-13 are the softmax: thread = (row, 32 of the 64 keys).  Two buffers of operands and
+// Roles (640 threads): warp 0 copies pages (one bulk copy each), warp 1 issues MMAs, warps 2-3 expand codes
+// and parameters, warps 4-19 are the softmax: thread = (row, 16 of the 64 keys).  Two buffers of operands and
 // scores, so that a page's expansion and scores run under the softmax before it.  Runs of pages as in
 // paged_attn.cu, one CTA an SM; partials of shared items are joined by the last CTA in CTA order.
 // Every wait is bounded; on expiry the kernel records a timeout, drains its copies and MMAs and returns.
 #include <cstddef>
+#include <type_traits>
 
 #include "paged_attn.cuh"
 
@@ -23,7 +24,8 @@ namespace tss {
 namespace {
 
 constexpr int kPtD = 128, kPtRows = 128, kPtKeys = 64;
-constexpr int kPtThreads = 448, kPtSoft = 256;    // threads; those of the softmax
+constexpr int kPtExpand = 2, kPtSoftWarps = 16;   // warps that expand codes; those of the softmax
+constexpr int kPtSoft = kPtSoftWarps * 32, kPtThreads = 64 + kPtExpand * 32 + kPtSoft;
 constexpr int kPtRaw = 4;                         // pages in the ring of copies
 using PtBlock = PgBlock<kPtD>;
 constexpr int kPtQ = kPtRows * 64 * 2;            // one group of Q: 128 rows of 128 bytes
@@ -34,11 +36,11 @@ constexpr uint32_t kPtTmem = 512;                 // S: 2 buffers x 2 groups x 6
 
 struct __align__(16) PtShared {
   float par[2][kPtParams][kPtKeys];                   // (read as 16-byte vectors)
-  uint64_t raw_full[kPtRaw], raw_free[kPtRaw], kv_full[2], kv_free[2], s_full[2], s_free[2], p_full, p_free, q_full, o_full, drain;
+  uint64_t raw_full[kPtRaw], raw_free[kPtRaw], k_full[2], k_free[2], v_full[2], v_free[2], s_full[2], s_free[2], p_full, p_free, q_full, o_full, drain;
   uint32_t tmem;
   int abort, last, bad[kPtRaw], bad_kv[2];
-  float f[kPtRows], zq[2][kPtRows], top[2][kPtRows];  // per row: factor of the scores, query sums; maxima of its halves
-  float part[2][3][kPtRows];                          // the halves' sums: p, p z'_0, p z'_1
+  float f[kPtRows], zq[2][kPtRows], top[4][kPtRows];  // per row: factor of the scores, query sums; maxima of its quarters
+  float part[4][3][kPtRows];                          // the quarters' sums: p, p z'_0, p z'_1
 };
 static_assert(offsetof(PtShared, par) % 16 == 0 && offsetof(PtShared, raw_full) % 8 == 0, "alignment of vectors and barriers");
 constexpr size_t kPtSmem = 1024 + 2 * kPtQ + 2 * 4 * kPtOp + 4 * kPtP + kPtRaw * PtBlock::kBytes;
@@ -47,32 +49,42 @@ __host__ __device__ constexpr uint32_t idesc_f16_m128(int n) {
   return (1u << 4) | (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(128 >> 4) << 24);
 }
 
+// mbar_wait, asleep between looks: sixteen warps that poll would take the issue slots of those that work.
+__device__ __forceinline__ bool quiet_wait(uint64_t* bar, uint32_t parity, volatile int* abort, int* status) {
+  if (mbar_try_wait(bar, parity)) return true;
+  const uint64_t t0 = globaltimer_ns();
+  while (!mbar_try_wait_sleep(bar, parity, 20000)) {
+    if (*abort) return false;
+    if (globaltimer_ns() - t0 > kWaitLimitNs) {
+      *abort = 1;
+      report(status, kStatusTimeout);
+      return false;
+    }
+  }
+  return true;
+}
+
 // A word's eight codes as fp16 subnormals.
 __device__ __forceinline__ uint4 expand(uint32_t x) {
   const uint32_t y = x >> 8;
   return make_uint4(x & 0x000f000fu, x & 0x00f000f0u, y & 0x000f000fu, y & 0x00f000f0u);
 }
 
-// 32 columns of a thread's TMEM lane, left in flight: tmem_wait() before they are used.
-__device__ __forceinline__ void tmem_ld32_start(uint32_t taddr, uint32_t* r) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
-        "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
-        "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-      : "r"(taddr));
+// 4 columns of a thread's TMEM lane, left in flight: tmem_wait() before they are used.
+__device__ __forceinline__ void tmem_ld4_start(uint32_t taddr, uint32_t* r) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(taddr));
 }
 __device__ __forceinline__ void tmem_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
-// OR of v over the 64 threads of named barrier id.
-__device__ __forceinline__ bool pair_or(int id, bool v) {
+// OR of v over the 128 threads of named barrier id.
+__device__ __forceinline__ bool quad_or(int id, bool v) {
   uint32_t r;
   asm volatile(
       "{\n\t.reg .pred p, q;\n\t"
       "setp.ne.u32 q, %1, 0;\n\t"
-      "bar.red.or.pred p, %2, 64, q;\n\t"
+      "bar.red.or.pred p, %2, 128, q;\n\t"
       "selp.u32 %0, 1, 0, p;\n\t}\n"
       : "=r"(r)
       : "r"(v ? 1u : 0u), "r"(id)
@@ -110,13 +122,80 @@ __device__ __forceinline__ unsigned long long row_sees(const PgAttnArgs& a, cons
   return v;
 }
 
+// The softmax team of an item's last CTA joins the partials of CTAs c0..c1: first every row's weights of them (in
+// P's and Q's shared memory: no MMA is in flight), then 4 dims of 8 rows a thread, their loads in flight together.
+__device__ __forceinline__ void join_parts(const PaParams& p, PtShared& sh, uint8_t* sq, uint8_t* sp, const PaReq& r, int h, int row0, int rows,
+                                           int c0, int c1, int sw, int qt, int row, int lane) {
+  const int parts = c1 - c0 + 1;
+  constexpr int kFirst = 4 * kPtP / (kPtRows * 4);  // weights that P's memory takes: 128 partials
+  const auto weight = [&](int x) {
+    return (x < kFirst ? reinterpret_cast<float*>(sp) + x * kPtRows : reinterpret_cast<float*>(sq) + (x - kFirst) * kPtRows);
+  };
+  const auto slot = [&](int x) { return static_cast<long long>((c0 + x) * 2 + (x == 0)) * kPtRows; };
+  float M = -INFINITY, L = 0.f;
+  if (row < rows)
+#pragma unroll 4
+    for (int x = qt; x < parts; x += 4) M = fmaxf(M, __ldcg(p.part_ml + slot(x) + row).x);
+  sh.top[qt][row] = M;
+  named_bar_sync(5, kPtSoft);
+  M = fmaxf(fmaxf(sh.top[0][row], sh.top[1][row]), fmaxf(sh.top[2][row], sh.top[3][row]));
+  const float mb = M == -INFINITY ? 0.f : M;
+  if (row < rows)
+#pragma unroll 4
+    for (int x = qt; x < parts; x += 4) {
+      const float2 ml = __ldcg(p.part_ml + slot(x) + row);
+      const float w = ex2(ml.x - mb);
+      L = fmaf(w, ml.y, L);
+      weight(x)[row] = w;
+    }
+  sh.part[qt][0][row] = L;
+  named_bar_sync(5, kPtSoft);
+  constexpr int kRowsOf = kPtRows / kPtSoftWarps;
+  float4 o[kRowsOf];
+#pragma unroll
+  for (int i = 0; i < kRowsOf; ++i) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+  for (int x = 0; x < parts; ++x) {
+    float4 y[kRowsOf];
+#pragma unroll
+    for (int i = 0; i < kRowsOf; ++i) {
+      const int q = sw + i * kPtSoftWarps;
+      y[i] = q < rows ? __ldcg(reinterpret_cast<const float4*>(p.part_o + (slot(x) + q) * kPtD) + lane) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+#pragma unroll
+    for (int i = 0; i < kRowsOf; ++i) {
+      const int q = sw + i * kPtSoftWarps;
+      if (q >= rows) continue;
+      const float w = weight(x)[q];
+      o[i].x = fmaf(w, y[i].x, o[i].x);
+      o[i].y = fmaf(w, y[i].y, o[i].y);
+      o[i].z = fmaf(w, y[i].z, o[i].z);
+      o[i].w = fmaf(w, y[i].w, o[i].w);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kRowsOf; ++i) {
+    const int q = sw + i * kPtSoftWarps;
+    if (q >= rows) continue;
+    float m = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      m = fmaxf(m, sh.top[k][q]);
+      l += sh.part[k][0][q];
+    }
+    finish_row<kPtD>(p.a, r, h, row0 + q, lane, m, l, o[i]);
+  }
+}
+
+// TWO: weights of two fp16 parts (fp16 outputs); else one (bf16 outputs: its 2^-12 is a fraction of their own 2^-9).
+template <bool TWO>
 __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __grid_constant__ PaParams p) {
   extern __shared__ uint8_t pt_dyn[];
   __shared__ PtShared sh;
   const uint32_t skew = (1024 - (smem_u32(pt_dyn) & 1023)) & 1023;
   uint8_t* sq = pt_dyn + skew;        // Q: group 0, group 1
   uint8_t* skv = sq + 2 * kPtQ;       // [buffer] C_0, C_1, C'_0, C'_1
-  uint8_t* sp = skv + 2 * 4 * kPtOp;  // P s'_0 (first part, rest), P s'_1 (first part, rest)
+  uint8_t* sp = skv + 2 * 4 * kPtOp;  // P s'_0, P s'_1; then their second parts
   uint8_t* raw = sp + 4 * kPtP;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const PgAttnArgs& a = p.a;
@@ -126,17 +205,19 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
   if (tid == 0) {
     for (int i = 0; i < kPtRaw; ++i) {
       mbar_init(&sh.raw_full[i], 1);
-      mbar_init(&sh.raw_free[i], 4);
+      mbar_init(&sh.raw_free[i], kPtExpand);
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&sh.kv_full[i], 4);
-      mbar_init(&sh.kv_free[i], 1);
+      mbar_init(&sh.k_full[i], kPtExpand);
+      mbar_init(&sh.k_free[i], 1);
+      mbar_init(&sh.v_full[i], kPtExpand);
+      mbar_init(&sh.v_free[i], 1);
       mbar_init(&sh.s_full[i], 1);
-      mbar_init(&sh.s_free[i], 8);
+      mbar_init(&sh.s_free[i], kPtSoftWarps);
     }
-    mbar_init(&sh.p_full, 8);
+    mbar_init(&sh.p_full, kPtSoftWarps);
     mbar_init(&sh.p_free, 1);
-    mbar_init(&sh.q_full, 8);
+    mbar_init(&sh.q_full, kPtSoftWarps);
     mbar_init(&sh.o_full, 1);
     mbar_init(&sh.drain, 1);
     sh.abort = 0;
@@ -179,7 +260,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
       for (int k = 0; k < 32 && t < n; ++k, ++t) {
         const long long src = __shfl_sync(0xffffffffu, blk, k);
         const int s = t % kPtRaw;
-        ok = __all_sync(0xffffffffu, t < kPtRaw || mbar_wait(&sh.raw_free[s], ((t / kPtRaw) - 1) & 1, abort, a.status));
+        ok = __all_sync(0xffffffffu, t < kPtRaw || quiet_wait(&sh.raw_free[s], ((t / kPtRaw) - 1) & 1, abort, a.status));
         if (!ok) break;
         if (lane == 0) {
           sh.bad[s] = src < 0;
@@ -203,12 +284,12 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
       for (int t = 0, seg = 0; t < n && ok; ++seg) {
         const PaReq& r = p.r[request_of(u0 + t)];
         const int len = min(n - t, r.units - (u0 + t - r.off) % r.units);
-        ok = mbar_wait(&sh.q_full, seg & 1, abort, a.status);
+        ok = quiet_wait(&sh.q_full, seg & 1, abort, a.status);
         for (int j = 0; ok && j <= len; ++j) {
           if (j < len) {
             const int u = t + j, s = u & 1;
-            if (!mbar_wait(&sh.kv_full[s], (u >> 1) & 1, abort, a.status) ||
-                (u >= 2 && !mbar_wait(&sh.s_free[s], ((u >> 1) - 1) & 1, abort, a.status))) {
+            if (!quiet_wait(&sh.k_full[s], (u >> 1) & 1, abort, a.status) ||
+                (u >= 2 && !quiet_wait(&sh.s_free[s], ((u >> 1) - 1) & 1, abort, a.status))) {
               ok = false;
               break;
             }
@@ -220,10 +301,11 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
                 umma_bf16(tm + s * 128 + g * 64, sdesc_sw128(q_a + g * kPtQ + k * 32), sdesc_sw128(kv_a + (s * 4 + g) * kPtOp + k * 32), id,
                           k ? 1u : 0u);
             umma_commit(&sh.s_full[s]);
+            umma_commit(&sh.k_free[s]);
           }
           if (j >= 1) {
             const int u = t + j - 1, s = u & 1;
-            if (!mbar_wait(&sh.p_full, u & 1, abort, a.status)) {
+            if (!quiet_wait(&sh.v_full[s], (u >> 1) & 1, abort, a.status) || !quiet_wait(&sh.p_full, u & 1, abort, a.status)) {
               ok = false;
               break;
             }
@@ -231,13 +313,13 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
 #pragma unroll
             for (int g = 0; g < 2; ++g)
 #pragma unroll
-              for (int part = 0; part < 2; ++part)
+              for (int part = 0; part < (TWO ? 2 : 1); ++part)
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
-                  umma_bf16(tm + 256 + g * 64, sdesc_sw128(p_a + (g * 2 + part) * kPtP + k * 32),
+                  umma_bf16(tm + 256 + g * 64, sdesc_sw128(p_a + (part * 2 + g) * kPtP + k * 32),
                             sdesc_sw128(kv_a + (s * 4 + 2 + g) * kPtOp + k * 32), id, (j > 1 || part || k) ? 1u : 0u);
             umma_commit(&sh.p_free);
-            umma_commit(&sh.kv_free[s]);
+            umma_commit(&sh.v_free[s]);
             if (j == len) umma_commit(&sh.o_full);
           }
         }
@@ -247,42 +329,50 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
       umma_commit(&sh.drain);
       mbar_drain(&sh.drain, 0);
     }
-  } else if (warp < 6) {
+  } else if (warp < 2 + kPtExpand) {
     // ---------------- codes to operands, parameters to fp32 ----------------
+    // A lane's units of a page are 16 keys (dims) apart, so that its chunks' places differ by constants.
     const int x = tid - 64;
+    constexpr int kTurns = 256 / (32 * kPtExpand);
+    const uint4 zero = make_uint4(0, 0, 0, 0);
     for (int t = 0; t < n; ++t) {
       const int s = t & 1, rs = t % kPtRaw;
-      const bool ok = mbar_wait(&sh.raw_full[rs], (t / kPtRaw) & 1, abort, a.status) &&
-                      (t < 2 || mbar_wait(&sh.kv_free[s], ((t >> 1) - 1) & 1, abort, a.status));
-      if (!__all_sync(0xffffffffu, ok)) break;
       const uint8_t* blk = raw + rs * PtBlock::kBytes;
-      const bool bad = sh.bad[rs];
       uint8_t* op = skv + s * 4 * kPtOp;
-      // (without a page: zeros, so that no weight meets a stale operand)
+      if (!__all_sync(0xffffffffu, quiet_wait(&sh.raw_full[rs], (t / kPtRaw) & 1, abort, a.status) &&
+                                       (t < 2 || quiet_wait(&sh.k_free[s], ((t >> 1) - 1) & 1, abort, a.status))))
+        break;
+      const bool bad = sh.bad[rs];  // without a page: zeros, so that no weight meets a stale operand
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int w = i * 128 + x;
-        const uint4 zero = make_uint4(0, 0, 0, 0);
+      for (int i = 0; i < kTurns; ++i) {
+        // unit w: key w / 4, dims 16 (w % 4) .. + 15 of each group
+        const int w = i * 32 * kPtExpand + x, key = w >> 2, c = 2 * (w & 3);
         const uint4 k = bad ? zero : *reinterpret_cast<const uint4*>(blk + PtBlock::kK + w * 16);
+        uint8_t *k0 = op + key * 128 + ((c ^ (key & 7)) << 4), *k1 = op + key * 128 + (((c + 1) ^ (key & 7)) << 4);
+        *reinterpret_cast<uint4*>(k0) = expand(k.x);
+        *reinterpret_cast<uint4*>(k1) = expand(k.y);
+        *reinterpret_cast<uint4*>(k0 + kPtOp) = expand(k.z);
+        *reinterpret_cast<uint4*>(k1 + kPtOp) = expand(k.w);
+      }
+      fence_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sh.k_full[s]);
+      if (!__all_sync(0xffffffffu, t < 2 || quiet_wait(&sh.v_free[s], ((t >> 1) - 1) & 1, abort, a.status))) break;
+#pragma unroll
+      for (int i = 0; i < kTurns; ++i) {
+        // unit w: half w / 128, dims 4 (w / 4 % 32) .. + 3, tokens 8 b + 2 (w % 4) + i of the half
+        const int w = i * 32 * kPtExpand + x, d0 = ((w >> 2) & 31) * 4, vc = (w >> 7) * 4 + (w & 3);
         const uint4 v = bad ? zero : *reinterpret_cast<const uint4*>(blk + PtBlock::kV + w * 16);
-        // K: key w / 4, dims 16 (w % 4) .. + 15 of each group
-        const int key = w >> 2, c = 2 * (w & 3);
-        uint8_t* kd = op + key * 128;
-        *reinterpret_cast<uint4*>(kd + ((c ^ (key & 7)) << 4)) = expand(k.x);
-        *reinterpret_cast<uint4*>(kd + (((c + 1) ^ (key & 7)) << 4)) = expand(k.y);
-        *reinterpret_cast<uint4*>(kd + kPtOp + ((c ^ (key & 7)) << 4)) = expand(k.z);
-        *reinterpret_cast<uint4*>(kd + kPtOp + (((c + 1) ^ (key & 7)) << 4)) = expand(k.w);
-        // V: half i, dims 4 (x / 4) .. + 3, tokens 8 b + 2 (x % 4) + i of the half
-        const int d0 = (x >> 2) * 4, vc = i * 4 + (x & 3);
         uint8_t* vd = op + (2 + d0 / 64) * kPtOp + (d0 % 64) * 128;
         const uint32_t vw[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) *reinterpret_cast<uint4*>(vd + e * 128 + ((vc ^ ((d0 + e) & 7)) << 4)) = expand(vw[e]);
       }
+      // parameters (their readers are done with the buffer's last ones: they precede P V)
       if (x < kPtKeys) {
-        const __half2* kp = reinterpret_cast<const __half2*>(blk + PtBlock::kKParams) + 2 * x;
-        const __half2* vp = reinterpret_cast<const __half2*>(blk + PtBlock::kVParams) + 2 * x;
-        const float2 k0 = __half22float2(kp[0]), k1 = __half22float2(kp[1]), v0 = __half22float2(vp[0]), v1 = __half22float2(vp[1]);
+        const uint2 kp = *reinterpret_cast<const uint2*>(blk + PtBlock::kKParams + 8 * x), vp = *reinterpret_cast<const uint2*>(blk + PtBlock::kVParams + 8 * x);
+        const auto pair = [](uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); };
+        const float2 k0 = pair(kp.x), k1 = pair(kp.y), v0 = pair(vp.x), v1 = pair(vp.y);
         const float all[kPtParams] = {k0.x, k1.x, k0.y, k1.y, v0.x, v1.x, v0.y, v1.y, __log2f(fmaxf(fmaxf(v0.x, v1.x), kLeast))};
 #pragma unroll
         for (int i = 0; i < kPtParams; ++i) sh.par[s][i][x] = all[i];
@@ -291,41 +381,47 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
       fence_async_smem();
       __syncwarp();
       if (lane == 0) {
-        mbar_arrive(&sh.kv_full[s]);
+        mbar_arrive(&sh.v_full[s]);
         mbar_arrive(&sh.raw_free[rs]);
       }
     }
   } else {
-    // ---------------- softmax: thread = (row, half of a page's keys) ----------------
+    // ---------------- softmax: thread = (row, a quarter of a page's keys) ----------------
+    // Quarter 2 half + y: keys 8 b + 4 y + {0..3}, b = 0..3, of the half, which are whole chunks of the row's P.
     // After a wait that gave up the threads go on without waiting, through the same barriers.
-    const int sw = warp - 6, qd = warp & 3, half = sw >> 2, row = qd * 32 + lane, pair = 1 + qd;
+    const int sw = warp - 2 - kPtExpand, qd = warp & 3, qt = sw >> 2, half = qt >> 1, y4 = (qt & 1) * 4;
+    const int row = qd * 32 + lane, quad = 1 + qd;
     const uint32_t lanes = static_cast<uint32_t>(qd * 32) << 16;
     bool ok = true;
     for (int t = 0, seg = 0; t < n; ++seg) {
       const PaReq& r = p.r[request_of(u0 + t)];
       const int v = u0 + t - r.off, item = v / r.units, x0 = v - item * r.units, len = min(n - t, r.units - x0);
       const int h = item % a.hk, row0 = item / a.hk * kPtRows, rows = min(kPtRows, r.n * gq - row0);
-      // Q: 16 lanes a row, 8 dims each, as chunks in the operand's order
-#pragma unroll 2
-      for (int i = 0; i < 8; ++i) {
-        const int qr = sw * 16 + i * 2 + (lane >> 4), c8 = lane & 15;
-        float x[8];
-        if (qr < rows) {
-          const int q = row0 + qr;
-          const long long at = (r.row + q / gq) * a.qs + static_cast<long long>(h * gq + q % gq) * kPtD + c8 * 8;
-          if (a.is_half)
-            load_vec<__half, 8>(static_cast<const __half*>(a.q) + at, x);
-          else
-            load_vec<__nv_bfloat16, 8>(static_cast<const __nv_bfloat16*>(a.q) + at, x);
-        } else {
+      // Q: 16 lanes a row, 8 dims each, as chunks in the operand's order; the warp's rows in flight together
+      constexpr int kTurns = kPtRows / 2 / kPtSoftWarps;
+      uint4 rawq[kTurns];
+      const int c8 = lane & 15;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] = 0.f;
-        }
-        float big = 0.f, sum = 0.f;
+      for (int i = 0; i < kTurns; ++i) {
+        const int qr = (sw * kTurns + i) * 2 + (lane >> 4), q = row0 + qr;
+        rawq[i] = make_uint4(0, 0, 0, 0);
+        if (qr < rows)
+          rawq[i] = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + (r.row + q / gq) * a.qs +
+                                                    static_cast<long long>(h * gq + q % gq) * kPtD + c8 * 8);
+      }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          big = fmaxf(big, fabsf(x[e]));
-          sum += x[e];
+      for (int i = 0; i < kTurns; ++i) {
+        const int qr = (sw * kTurns + i) * 2 + (lane >> 4);
+        const uint32_t in[4] = {rawq[i].x, rawq[i].y, rawq[i].z, rawq[i].w};
+        float x[8], big = 0.f, sum = 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float2 f = a.is_half ? __half22float2(*reinterpret_cast<const __half2*>(&in[e]))
+                                     : make_float2(__uint_as_float(in[e] << 16), __uint_as_float(in[e] & 0xffff0000u));
+          x[2 * e] = f.x;
+          x[2 * e + 1] = f.y;
+          big = fmaxf(big, fmaxf(fabsf(f.x), fabsf(f.y)));
+          sum += f.x + f.y;
         }
 #pragma unroll
         for (int o = 8; o > 0; o >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
@@ -345,7 +441,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
       named_bar_sync(5, kPtSoft);
       const bool valid = row < rows, active = qd * 32 < rows;
       const float f = sh.f[row];
-      const float2 f2 = make_float2(f, f), zq0 = make_float2(sh.zq[0][row], sh.zq[0][row]), zq1 = make_float2(sh.zq[1][row], sh.zq[1][row]);
+      const f2_t f2 = f2_pack(f, f), zq0 = f2_pack(sh.zq[0][row], sh.zq[0][row]), zq1 = f2_pack(sh.zq[1][row], sh.zq[1][row]);
       int qp = 0;
       unsigned long long anc_lo = ~0ull, anc_hi = ~0ull;
       if (valid) {
@@ -363,145 +459,170 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
         anc_hi = r.n <= 64 ? 0ull : r.n < 128 ? anc_hi & ((1ull << (r.n - 64)) - 1) : anc_hi;
       }
       float ref = -INFINITY;
-      float2 l2 = make_float2(0.f, 0.f), oz0 = l2, oz1 = l2;
+      f2_t l2 = f2_pack(0.f, 0.f), oz0 = l2, oz1 = l2;
       for (int j = 0; j < len; ++j) {
         const int u = t + j, s = u & 1;
-        ok = __all_sync(0xffffffffu, ok && mbar_wait(&sh.kv_full[s], (u >> 1) & 1, abort, a.status) &&
-                                         mbar_wait(&sh.s_full[s], (u >> 1) & 1, abort, a.status));
+        ok = __all_sync(0xffffffffu, ok && quiet_wait(&sh.v_full[s], (u >> 1) & 1, abort, a.status) &&
+                                         quiet_wait(&sh.s_full[s], (u >> 1) & 1, abort, a.status));
         tc_fence_after();
         if (active) {
           const int x = x0 + j, key0 = (x < r.sink ? x : x - r.sink + r.lo) * kPtKeys;
-          uint32_t vis = 0xffffffffu;
-          if (valid) vis = sh.bad_kv[s] ? 0u : static_cast<uint32_t>(row_sees(a, r, qp, anc_lo, anc_hi, key0) >> (32 * half));
-          const bool all = __all_sync(0xffffffffu, vis == 0xffffffffu);
-          uint32_t s0[32], s1[32];
-          __syncwarp();
-          tmem_ld32_start(tm + lanes + s * 128 + half * 32, s0);
-          tmem_ld32_start(tm + lanes + s * 128 + 64 + half * 32, s1);
-          tmem_wait();
-          const float(*par)[kPtKeys] = sh.par[s];
-          // scores / f, over s0
-          float top = -INFINITY;
-#pragma unroll
-          for (int k = 0; k < 32; k += 4) {
-            const float4 a0 = *reinterpret_cast<const float4*>(&par[0][half * 32 + k]), a1 = *reinterpret_cast<const float4*>(&par[1][half * 32 + k]);
-            const float4 b0 = *reinterpret_cast<const float4*>(&par[2][half * 32 + k]), b1 = *reinterpret_cast<const float4*>(&par[3][half * 32 + k]);
-            const float4 lg = *reinterpret_cast<const float4*>(&par[8][half * 32 + k]);
-#pragma unroll
-            for (int y = 0; y < 2; ++y) {
-              float2 c = mul2(y ? make_float2(b0.z, b0.w) : make_float2(b0.x, b0.y), zq0);
-              c = fma2(y ? make_float2(b1.z, b1.w) : make_float2(b1.x, b1.y), zq1, c);
-              c = fma2(y ? make_float2(a0.z, a0.w) : make_float2(a0.x, a0.y),
-                       make_float2(__uint_as_float(s0[k + 2 * y]), __uint_as_float(s0[k + 2 * y + 1])), c);
-              c = fma2(y ? make_float2(a1.z, a1.w) : make_float2(a1.x, a1.y),
-                       make_float2(__uint_as_float(s1[k + 2 * y]), __uint_as_float(s1[k + 2 * y + 1])), c);
-              const float2 e = fma2(c, f2, y ? make_float2(lg.z, lg.w) : make_float2(lg.x, lg.y));
-              if (all || (vis >> (k + 2 * y) & 1u)) top = fmaxf(top, e.x);
-              if (all || (vis >> (k + 2 * y + 1) & 1u)) top = fmaxf(top, e.y);
-              s0[k + 2 * y] = __float_as_uint(c.x);
-              s0[k + 2 * y + 1] = __float_as_uint(c.y);
-            }
+          uint32_t vis = 0xffffu;  // bit 4 b + i
+          if (valid && (a.window || key0 + kPtKeys > r.first || sh.bad_kv[s])) {
+            const uint32_t m = sh.bad_kv[s] ? 0u : static_cast<uint32_t>(row_sees(a, r, qp, anc_lo, anc_hi, key0) >> (32 * half)) >> y4;
+            vis = (m & 15u) | (m >> 4 & 0xf0u) | (m >> 8 & 0xf00u) | (m >> 12 & 0xf000u);
           }
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&sh.s_free[s]);
-          // the row's reference rises where a weight times its value's scale would pass 2^15, to leave it at 2^7
-          if (pair_or(pair, top - ref > 15.f)) {
-            sh.top[half][row] = top;
-            named_bar_sync(pair, 64);
-            top = fmaxf(sh.top[0][row], sh.top[1][row]);
-            float al = 1.f;
-            if (top - ref > 15.f) {
-              const float now = top - 7.f;
-              al = ref == -INFINITY ? 1.f : ex2(ref - now);
-              ref = now;
-              l2 = mul2(l2, make_float2(al, al));
-              oz0 = mul2(oz0, make_float2(al, al));
-              oz1 = mul2(oz1, make_float2(al, al));
-            }
-            if (j > 0 && __any_sync(0xffffffffu, al != 1.f)) {
-              ok = __all_sync(0xffffffffu, ok && mbar_wait(&sh.p_free, (u - 1) & 1, abort, a.status));
-              tc_fence_after();
+          const auto page = [&](auto all_tag) {
+            constexpr bool kAll = decltype(all_tag)::value;  // the warp's rows see all of the thread's keys
+            const float* par = &sh.par[s][0][half * 32 + y4];
+            const auto pr = [&](int k, int b) { return *reinterpret_cast<const ulonglong2*>(par + k * kPtKeys + 8 * b); };
+            f2_t c[8];  // scores / f of keys (b, 0..1) and (b, 2..3)
+            {
+              uint32_t s0[16], s1[16];
               __syncwarp();
-              float o[16];
 #pragma unroll
-              for (int c = 0; c < 4; ++c) {
-                const uint32_t at = tm + lanes + 256 + half * 64 + c * 16;
-                tmem_ld16(at, o);
-#pragma unroll
-                for (int i = 0; i < 16; ++i) o[i] *= al;
-                tmem_st16(at, o);
+              for (int b = 0; b < 4; ++b) {
+                tmem_ld4_start(tm + lanes + s * 128 + half * 32 + y4 + 8 * b, s0 + 4 * b);
+                tmem_ld4_start(tm + lanes + s * 128 + 64 + half * 32 + y4 + 8 * b, s1 + 4 * b);
               }
+              tmem_wait();
               tc_fence_before();
-            }
-          }
-          if (u > 0) ok = __all_sync(0xffffffffu, ok && mbar_wait(&sh.p_free, (u - 1) & 1, abort, a.status));
-          // weights: chunk c of the row's P holds, at 2 b + i, key 8 b + 2 c + i of the half
-          const float2 nref = make_float2(-ref, -ref);
-          uint8_t* pd = sp + row * 128;
+              __syncwarp();
+              if (lane == 0) mbar_arrive(&sh.s_free[s]);
 #pragma unroll
-          for (int hc = 0; hc < 2; ++hc) {
-            uint32_t hi[2][2][4], lo[2][2][4];  // [group][chunk 2 hc + y][b]
+              for (int b = 0; b < 4; ++b) {
+                const ulonglong2 a0 = pr(0, b), a1 = pr(1, b), b0 = pr(2, b), b1 = pr(3, b);
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                  const int k = 4 * b + 2 * y;
+                  const f2_t m = f2_pack(__uint_as_float(s0[k]), __uint_as_float(s0[k + 1])), z = f2_pack(__uint_as_float(s1[k]), __uint_as_float(s1[k + 1]));
+                  c[k / 2] = f2_fma(y ? a1.y : a1.x, z, f2_fma(y ? a0.y : a0.x, m, f2_fma(y ? b1.y : b1.x, zq1, f2_mul(y ? b0.y : b0.x, zq0))));
+                }
+              }
+            }
+            float top = -INFINITY;
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
-              const int k = 8 * b + 4 * hc;
-              const float4 v0 = *reinterpret_cast<const float4*>(&par[4][half * 32 + k]), v1 = *reinterpret_cast<const float4*>(&par[5][half * 32 + k]);
-              const float4 w0 = *reinterpret_cast<const float4*>(&par[6][half * 32 + k]), w1 = *reinterpret_cast<const float4*>(&par[7][half * 32 + k]);
+              const ulonglong2 lg = pr(8, b);
 #pragma unroll
               for (int y = 0; y < 2; ++y) {
-                const int kk = k + 2 * y;
-                const float2 e = fma2(make_float2(__uint_as_float(s0[kk]), __uint_as_float(s0[kk + 1])), f2, nref);
-                float2 w = make_float2(ex2(e.x), ex2(e.y));
-                const float2 z0 = y ? make_float2(w0.z, w0.w) : make_float2(w0.x, w0.y), z1 = y ? make_float2(w1.z, w1.w) : make_float2(w1.x, w1.y);
-                const float2 c0 = y ? make_float2(v0.z, v0.w) : make_float2(v0.x, v0.y), c1 = y ? make_float2(v1.z, v1.w) : make_float2(v1.x, v1.y);
-                float2 p0, p1;
-                const float2 down = make_float2(0.0625f, 0.0625f);  // (odd nibbles stand four bits up)
-                if (all) {
-                  l2 = add2(l2, w);
-                  oz0 = fma2(w, z0, oz0);
-                  oz1 = fma2(w, z1, oz1);
-                  if (b & 1) w = mul2(w, down);
-                  p0 = mul2(w, c0);
-                  p1 = mul2(w, c1);
-                } else {  // (what the row does not see may be NaN: selected away, not multiplied)
-                  const bool on0 = vis >> kk & 1u, on1 = vis >> (kk + 1) & 1u;
-                  w = make_float2(on0 ? w.x : 0.f, on1 ? w.y : 0.f);
-                  l2 = add2(l2, w);
-                  oz0 = fma2(w, make_float2(on0 ? z0.x : 0.f, on1 ? z0.y : 0.f), oz0);
-                  oz1 = fma2(w, make_float2(on0 ? z1.x : 0.f, on1 ? z1.y : 0.f), oz1);
-                  if (b & 1) w = mul2(w, down);
-                  p0 = make_float2(on0 ? w.x * c0.x : 0.f, on1 ? w.y * c0.y : 0.f);
-                  p1 = make_float2(on0 ? w.x * c1.x : 0.f, on1 ? w.y * c1.y : 0.f);
+                const int k = 4 * b + 2 * y;
+                const float2 e = f2_unpack(f2_fma(c[k / 2], f2, y ? lg.y : lg.x));
+                if constexpr (kAll) {
+                  top = fmaxf(top, fmaxf(e.x, e.y));
+                } else {
+                  top = fmaxf(top, vis >> k & 1u ? e.x : -INFINITY);
+                  top = fmaxf(top, vis >> (k + 1) & 1u ? e.y : -INFINITY);
                 }
-                const float2 minus = make_float2(-1.f, -1.f);
-                hi[0][y][b] = pack_f16(p0.x, p0.y);
-                hi[1][y][b] = pack_f16(p1.x, p1.y);
-                const float2 r0 = fma2(__half22float2(*reinterpret_cast<const __half2*>(&hi[0][y][b])), minus, p0);
-                const float2 r1 = fma2(__half22float2(*reinterpret_cast<const __half2*>(&hi[1][y][b])), minus, p1);
-                lo[0][y][b] = pack_f16(r0.x, r0.y);
-                lo[1][y][b] = pack_f16(r1.x, r1.y);
               }
             }
+            // the row's reference rises where a weight times its value's scale would pass 2^15, to leave it at 2^7
+            if (quad_or(quad, top - ref > 15.f)) {
+              sh.top[qt][row] = top;
+              named_bar_sync(quad, 128);
+              top = fmaxf(fmaxf(sh.top[0][row], sh.top[1][row]), fmaxf(sh.top[2][row], sh.top[3][row]));
+              float al = 1.f;
+              if (top - ref > 15.f) {
+                const float now = top - 7.f;
+                al = ref == -INFINITY ? 1.f : ex2(ref - now);
+                ref = now;
+                const f2_t al2 = f2_pack(al, al);
+                l2 = f2_mul(l2, al2);
+                oz0 = f2_mul(oz0, al2);
+                oz1 = f2_mul(oz1, al2);
+              }
+              if (j > 0 && __any_sync(0xffffffffu, al != 1.f)) {
+                ok = __all_sync(0xffffffffu, ok && quiet_wait(&sh.p_free, (u - 1) & 1, abort, a.status));
+                tc_fence_after();
+                __syncwarp();
+                float o[16];
+#pragma unroll
+                for (int x2 = 0; x2 < 2; ++x2) {
+                  const uint32_t at = tm + lanes + 256 + qt * 32 + x2 * 16;
+                  tmem_ld16(at, o);
+#pragma unroll
+                  for (int i = 0; i < 16; ++i) o[i] *= al;
+                  tmem_st16(at, o);
+                }
+                tc_fence_before();
+              }
+            }
+            if (u > 0) ok = __all_sync(0xffffffffu, ok && quiet_wait(&sh.p_free, (u - 1) & 1, abort, a.status));
+            // weights: chunk x of a half of the row's P holds, at 2 b + i, key 8 b + 2 x + i; these are x = y4 / 2 + y
+            const f2_t nref = f2_pack(-ref, -ref);
+            uint32_t hi[2][2][4], lo[2][2][4];  // [y][group][b]
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+              const ulonglong2 v0s = pr(4, b), v1s = pr(5, b), z0s = pr(6, b), z1s = pr(7, b);
+#pragma unroll
+              for (int y = 0; y < 2; ++y) {
+                const int k = 4 * b + 2 * y;
+                const float2 e = f2_unpack(f2_fma(c[k / 2], f2, nref));
+                const float2 wf = make_float2(ex2(e.x), ex2(e.y));
+                const f2_t v0 = y ? v0s.y : v0s.x, v1 = y ? v1s.y : v1s.x, z0 = y ? z0s.y : z0s.x, z1 = y ? z1s.y : z1s.x;
+                const f2_t down = f2_pack(0.0625f, 0.0625f);  // (odd nibbles stand four bits up)
+                f2_t p0, p1;
+                if constexpr (kAll) {
+                  f2_t w = f2_pack(wf.x, wf.y);
+                  l2 = f2_add(l2, w);
+                  oz0 = f2_fma(w, z0, oz0);
+                  oz1 = f2_fma(w, z1, oz1);
+                  if (b & 1) w = f2_mul(w, down);
+                  p0 = f2_mul(w, v0);
+                  p1 = f2_mul(w, v1);
+                } else {  // (what the row does not see may be NaN: selected away, not multiplied)
+                  const bool on0 = vis >> k & 1u, on1 = vis >> (k + 1) & 1u;
+                  const auto pick = [&](f2_t m) {
+                    const float2 q = f2_unpack(m);
+                    return f2_pack(on0 ? q.x : 0.f, on1 ? q.y : 0.f);
+                  };
+                  f2_t w = f2_pack(on0 ? wf.x : 0.f, on1 ? wf.y : 0.f);
+                  l2 = f2_add(l2, w);
+                  oz0 = f2_fma(w, pick(z0), oz0);
+                  oz1 = f2_fma(w, pick(z1), oz1);
+                  if (b & 1) w = f2_mul(w, down);
+                  p0 = f2_mul(w, pick(v0));
+                  p1 = f2_mul(w, pick(v1));
+                }
+                const auto split = [&](f2_t m, uint32_t* first, uint32_t* rest) {
+                  const float2 q = f2_unpack(m);
+                  *first = pack_f16(q.x, q.y);
+                  if constexpr (TWO) {
+                    const float2 back = __half22float2(*reinterpret_cast<const __half2*>(first));
+                    const float2 d = f2_unpack(f2_fma(f2_pack(back.x, back.y), f2_pack(-1.f, -1.f), m));
+                    *rest = pack_f16(d.x, d.y);
+                  }
+                };
+                split(p0, &hi[y][0][b], &lo[y][0][b]);
+                split(p1, &hi[y][1][b], &lo[y][1][b]);
+              }
+            }
+            uint8_t* pd = sp + row * 128;
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
-              const int at = ((half * 4 + 2 * hc + y) ^ (row & 7)) << 4;
+              const int at = ((half * 4 + y4 / 2 + y) ^ (row & 7)) << 4;
 #pragma unroll
               for (int g = 0; g < 2; ++g) {
-                *reinterpret_cast<uint4*>(pd + (2 * g) * kPtP + at) = make_uint4(hi[g][y][0], hi[g][y][1], hi[g][y][2], hi[g][y][3]);
-                *reinterpret_cast<uint4*>(pd + (2 * g + 1) * kPtP + at) = make_uint4(lo[g][y][0], lo[g][y][1], lo[g][y][2], lo[g][y][3]);
+                *reinterpret_cast<uint4*>(pd + g * kPtP + at) = make_uint4(hi[y][g][0], hi[y][g][1], hi[y][g][2], hi[y][g][3]);
+                if constexpr (TWO)
+                  *reinterpret_cast<uint4*>(pd + (2 + g) * kPtP + at) = make_uint4(lo[y][g][0], lo[y][g][1], lo[y][g][2], lo[y][g][3]);
               }
             }
-          }
+          };
+          if (__all_sync(0xffffffffu, vis == 0xffffu))
+            page(std::true_type{});
+          else
+            page(std::false_type{});
           fence_async_smem();
         } else {  // no row of the quadrant is in use: the arrivals alone, in step with the others
-          if (u > 0) ok = __all_sync(0xffffffffu, ok && mbar_wait(&sh.p_free, (u - 1) & 1, abort, a.status));
+          if (u > 0) ok = __all_sync(0xffffffffu, ok && quiet_wait(&sh.p_free, (u - 1) & 1, abort, a.status));
           if (lane == 0) mbar_arrive(&sh.s_free[s]);
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(&sh.p_full);
       }
-      // ---- the segment's end ----
-      ok = __all_sync(0xffffffffu, ok && mbar_wait(&sh.o_full, seg & 1, abort, a.status));
+      // ---- the segment's end: 32 dims a thread ----
+      ok = __all_sync(0xffffffffu, ok && quiet_wait(&sh.o_full, seg & 1, abort, a.status));
       tc_fence_after();
       const bool whole = x0 == 0 && len == r.units;
       int c0 = first_cta, c1 = first_cta + splits - 1;
@@ -510,30 +631,40 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
         c1 = cta_of_unit(u0 + t - x0 + r.units - 1, p.total);
       }
       if (active) {
-        sh.part[half][0][row] = l2.x + l2.y;
-        sh.part[half][1][row] = oz0.x + oz0.y;
-        sh.part[half][2][row] = oz1.x + oz1.y;
-        named_bar_sync(pair, 64);
-        const float L = sh.part[0][0][row] + sh.part[1][0][row], z = sh.part[0][1 + half][row] + sh.part[1][1 + half][row];
+        const auto both = [](f2_t x) {
+          const float2 q = f2_unpack(x);
+          return q.x + q.y;
+        };
+        sh.part[qt][0][row] = both(l2);
+        sh.part[qt][1][row] = both(oz0);
+        sh.part[qt][2][row] = both(oz1);
+        named_bar_sync(quad, 128);
+        float L = 0.f, z = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          L += sh.part[i][0][row];
+          z += sh.part[i][1 + half][row];
+        }
         const long long slot = (blockIdx.x * 2 + (x0 == 0 ? 1 : 0)) * static_cast<long long>(kPtRows) + row;
 #pragma unroll 1
-        for (int c = 0; c < 4; ++c) {
+        for (int c = 0; c < 2; ++c) {
           float o[16];
           __syncwarp();
-          tmem_ld16(tm + lanes + 256 + half * 64 + c * 16, o);
+          tmem_ld16(tm + lanes + 256 + qt * 32 + c * 16, o);
           if (!valid) continue;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const float4 x = make_float4(fmaf(o[4 * i], 16777216.f, z), fmaf(o[4 * i + 1], 16777216.f, z), fmaf(o[4 * i + 2], 16777216.f, z),
                                          fmaf(o[4 * i + 3], 16777216.f, z));
-            const int c4 = half * 16 + c * 4 + i;
+            const int c4 = qt * 8 + c * 4 + i;
             if (whole)
               finish_row<kPtD>(a, r, h, row0 + row, c4, ref, L, x);
             else
               __stcg(reinterpret_cast<float4*>(p.part_o + slot * kPtD) + c4, x);
           }
         }
-        if (!whole && valid && half == 0) __stcg(p.part_ml + slot, make_float2(ref, L));
+        if (!whole && valid && qt == 0) __stcg(p.part_ml + slot, make_float2(ref, L));
+        __syncwarp();
         tc_fence_before();
       }
       named_bar_sync(5, kPtSoft);
@@ -543,13 +674,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
           if (sh.last) atomicExch(&p.counters[c0], 0);
         }
         named_bar_sync(5, kPtSoft);
-        if (sh.last)
-          for (int q = sw; q < rows; q += 8) {
-            float M, L;
-            float4 x;
-            gather_partials<kPtD>(p, kPtRows, c0, c1, q, 0, 1, &M, &L, &x);
-            finish_row<kPtD>(a, r, h, row0 + q, lane, M, L, x);
-          }
+        if (sh.last) join_parts(p, sh, sq, sp, r, h, row0, rows, c0, c1, sw, qt, row, lane);
         named_bar_sync(5, kPtSoft);
       }
       t += len;
@@ -567,14 +692,17 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
 }  // namespace
 
 cudaError_t paged_attn_tc_prepare() {
-  return cudaFuncSetAttribute(paged_attn_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kPtSmem));
+  cudaError_t e = cudaFuncSetAttribute(paged_attn_tc_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kPtSmem));
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(paged_attn_tc_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kPtSmem));
+  return e;
 }
 
 cudaError_t launch_paged_attention_tc(PaParams& p, int sms, cudaStream_t s) {
   // (two pages at least, so that the copy, the expansion and the scores of one run under the other's softmax; an
   // item's start and end cost about as much as 6)
   const int grid = pa_cut(p, sms, 2, 6);
-  return launch_k(paged_attn_tc_kernel, dim3(grid), dim3(kPtThreads), kPtSmem, s, true, p);
+  return launch_k(p.a.is_half ? paged_attn_tc_kernel<true> : paged_attn_tc_kernel<false>, dim3(grid), dim3(kPtThreads), kPtSmem, s, true, p);
 }
 
 }  // namespace tss
