@@ -33,19 +33,21 @@ namespace {
 
 __device__ __forceinline__ uint32_t movmatrix_t(uint32_t x) {
   uint32_t y;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
 
-// d = a b (mma_f16_16816 without an accumulator to clear)
-__device__ __forceinline__ void mma_f16_first(float* d, const uint32_t* a, const uint32_t* b) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
-      "{%10, %10, %10, %10};"
+// d += a b and d = a b, fp16 in, fp32 out.  (Not volatile: the compiler may place them among the integer work.)
+__device__ __forceinline__ void mma_next(float* d, const uint32_t* a, const uint32_t* b) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
+}
+__device__ __forceinline__ void mma_first(float* d, const uint32_t* a, const uint32_t* b) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
       : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]), "f"(0.f));
 }
-
 
 // A ring stage holds a page's block (or half of each of its parts).
 template <int D, int NT>
@@ -69,7 +71,8 @@ __device__ __forceinline__ bool sees(const PgAttnArgs& a, const PaReq& r, int i,
   return !a.window || qp - kp < a.window || j < a.sinks;
 }
 
-template <int D, int NT>
+// TWO: weights of two fp16 parts.
+template <int D, int NT, bool TWO>
 __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::kCtas) paged_attn_kernel(const __grid_constant__ PaParams p) {
   using B = PgBlock<D>;
   using S = PaShape<D, NT>;
@@ -280,10 +283,10 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
 #pragma unroll
               for (int nt = 0; nt < NT; ++nt) {
                 if (w == 0)
-                  mma_f16_first(acc[nt][gi], a0, &qf[nt][gi][w][0]);
+                  mma_first(acc[nt][gi], a0, &qf[nt][gi][w][0]);
                 else
-                  mma_f16_16816(acc[nt][gi], a0, &qf[nt][gi][w][0]);
-                mma_f16_16816(acc[nt][gi], a1, &qf[nt][gi][w][2]);
+                  mma_next(acc[nt][gi], a0, &qf[nt][gi][w][0]);
+                mma_next(acc[nt][gi], a1, &qf[nt][gi][w][2]);
               }
             }
           // scores from the codes' sums
@@ -322,7 +325,8 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
           for (int gi = 0; gi < G; ++gi) x = fmaxf(x, vz[mt][x2][gi].x);
           return x;
         };
-        uint32_t pf[NT][G][2][4];  // the weights times the values' scales, fp16 parts hi and lo, [8-key block]
+        constexpr int kParts = TWO ? 2 : 1;
+        uint32_t pf[NT][G][kParts][4];  // the weights times the values' scales in fp16 parts, [8-key block]
         const auto weigh = [&](auto all) {
           constexpr bool kAll = decltype(all)::value;  // every (key, row) pair counts
           uint32_t vis = 0;  // else: bit nt * 8 + mt * 4 + (key half) * 2 + row
@@ -417,10 +421,12 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
                 oz[nt][gi][1] = on1 ? fmaf(w1, sz.y, oz[nt][gi][1]) : oz[nt][gi][1];
                 const float p0 = on0 ? w0 * s2 : 0.f, p1 = on1 ? w1 * s2 : 0.f;
                 const uint32_t hi = pack_f16(p0, p1);
-                const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&hi));
                 pf[nt][gi][0][k] = movmatrix_t(hi);
+                if constexpr (TWO) {
+                const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&hi));
                 const float2 rest = fma2(back, make_float2(-1.f, -1.f), make_float2(p0, p1));
-                pf[nt][gi][1][k] = movmatrix_t(pack_f16(rest.x, rest.y));
+                pf[nt][gi][kParts - 1][k] = movmatrix_t(pack_f16(rest.x, rest.y));
+                }
               }
             }
         };
@@ -440,9 +446,9 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-              for (int part = 0; part < 2; ++part) {
-                mma_f16_16816(o[nt][db][y], a0, &pf[nt][db * 32 / kPgGroup][part][0]);
-                mma_f16_16816(o[nt][db][y], a1, &pf[nt][db * 32 / kPgGroup][part][2]);
+              for (int part = 0; part < kParts; ++part) {
+                mma_next(o[nt][db][y], a0, &pf[nt][db * 32 / kPgGroup][part][0]);
+                mma_next(o[nt][db][y], a1, &pf[nt][db * 32 / kPgGroup][part][2]);
               }
             }
           }
@@ -579,16 +585,16 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
     for (int k = max(0, issued - ST); k < issued; ++k) mbar_drain(&bars[warp][k % ST], (k / ST) & 1);
 }
 
-template <int D, int NT>
+template <int D, int NT, bool TWO>
 cudaError_t pa_launch(PaParams& p, int sms, cudaStream_t s) {
   using S = PaShape<D, NT>;
   // (a run of a unit for each warp at least; ending an item costs about as much as 8 units)
   const int grid = pa_cut(p, sms * S::kCtas, S::kWarps, 8);
-  return launch_k(paged_attn_kernel<D, NT>, dim3(grid), dim3(S::kWarps * 32), S::kSmem, s, true, p);
+  return launch_k(paged_attn_kernel<D, NT, TWO>, dim3(grid), dim3(S::kWarps * 32), S::kSmem, s, true, p);
 }
-template <int D, int NT>
+template <int D, int NT, bool TWO>
 cudaError_t pa_prepare() {
-  return cudaFuncSetAttribute(paged_attn_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+  return cudaFuncSetAttribute(paged_attn_kernel<D, NT, TWO>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                               static_cast<int>(PaShape<D, NT>::kSmem));
 }
 
@@ -599,10 +605,12 @@ size_t pa_partial_rows(int sms, int head_dim) { return static_cast<size_t>(sms) 
 int pa_counters(int sms) { return sms * 3; }
 
 cudaError_t pa_prepare_all() {
-  cudaError_t e = pa_prepare<64, 1>();
-  if (e == cudaSuccess) e = pa_prepare<64, 2>();
-  if (e == cudaSuccess) e = pa_prepare<128, 1>();
-  if (e == cudaSuccess) e = pa_prepare<128, 2>();
+  cudaError_t e = pa_prepare<64, 1, true>();
+  if (e == cudaSuccess) e = pa_prepare<64, 2, false>();
+  if (e == cudaSuccess) e = pa_prepare<64, 2, true>();
+  if (e == cudaSuccess) e = pa_prepare<128, 1, true>();
+  if (e == cudaSuccess) e = pa_prepare<128, 2, false>();
+  if (e == cudaSuccess) e = pa_prepare<128, 2, true>();
   if (e == cudaSuccess) e = paged_attn_tc_prepare();
   return e;
 }
@@ -646,8 +654,11 @@ cudaError_t launch_paged_attention(const tss_paged* h, const PgAttnArgs& a, cons
       *too_large = true;
       return cudaSuccess;
     }
-    const cudaError_t e = h->d == 64 ? (R == 8 ? pa_launch<64, 1>(narrow, h->sms, s) : pa_launch<64, 2>(narrow, h->sms, s))
-                                     : (R == 8 ? pa_launch<128, 1>(narrow, h->sms, s) : pa_launch<128, 2>(narrow, h->sms, s));
+    const auto run = [&](auto dim) {
+      constexpr int D = decltype(dim)::value;
+      return R == 8 ? pa_launch<D, 1, true>(narrow, h->sms, s) : a.is_half ? pa_launch<D, 2, true>(narrow, h->sms, s) : pa_launch<D, 2, false>(narrow, h->sms, s);
+    };
+    const cudaError_t e = h->d == 64 ? run(std::integral_constant<int, 64>{}) : run(std::integral_constant<int, 128>{});
     if (e != cudaSuccess) return e;
   }
   return wide ? launch_paged_attention_tc(p, h->sms, s) : cudaSuccess;
