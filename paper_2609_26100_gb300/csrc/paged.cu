@@ -97,12 +97,24 @@ __device__ __forceinline__ __half2 quantise(const float* x, uint32_t* codes) {
   const float sf = __half2float(s);
   float r;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(sf));
+  // Rounded to an integer by adding 1.5 2^23: the low bits of the sum (ties to even, as rint).  Quotients pass the ends
+  // only where z's own rounding is worth half a step.
+  const bool inside = (lo - zf) * r > -0.49f && (hi - zf) * r < 15.49f;
   uint32_t w = 0;
+  if (__all_sync(0xffffffffu, inside)) {
+    const f2_t nz = f2_pack(-zf, -zf), ns = f2_pack(-sf, -sf), r2 = f2_pack(r, r), magic = f2_pack(12582912.f, 12582912.f);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    // rounded to an integer by adding 1.5 2^23: the low bits of the sum (ties to even, as rint)
-    const float c = fminf(fmaxf(quotient(x[i] - zf, sf, r), 0.f), 15.f);
-    w |= (__float_as_uint(c + 12582912.f) & 15u) << (4 * i);
+    for (int i = 0; i < 4; ++i) {
+      const f2_t d = f2_add(f2_pack(x[2 * i], x[2 * i + 1]), nz), q = f2_mul(d, r2);
+      const float2 c = f2_unpack(f2_add(f2_fma(f2_fma(ns, q, d), r2, q), magic));
+      w |= (__float_as_uint(c.x) & 15u) << (8 * i) | (__float_as_uint(c.y) & 15u) << (8 * i + 4);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float c = fminf(fmaxf(quotient(x[i] - zf, sf, r), 0.f), 15.f);
+      w |= (__float_as_uint(c + 12582912.f) & 15u) << (4 * i);
+    }
   }
   *codes = sf > 0.f && !bad ? w : 0u;
   return bad ? __halves2half2(__ushort_as_half(0x7fff), __ushort_as_half(0)) : __halves2half2(s, z);
@@ -152,25 +164,33 @@ __global__ void __launch_bounds__(kPqThreads) append_kernel(const __grid_constan
   uint8_t* krow = u.block + B::kK + u.tok0 * (D / 2) + at.k_at;
   uint32_t acc[L::kT][4] = {};  // [t][pair of dims]: 16 bits a dim, nibble b
   constexpr int kStep = 4;      // steps whose loads are in flight together: 8 (16) tokens
-#pragma unroll 1
-  for (int j0 = u.lo / (kStep * L::kTokens) * kStep; j0 * L::kTokens < u.hi; j0 += kStep) {
-    float x[kStep][8];
+  Raw8<T> next[kStep];
+  const auto fetch = [&](int j0) {
 #pragma unroll
     for (int j = 0; j < kStep; ++j) {
       const int tok = (j0 + j) * L::kTokens + at.sub;
-      if (tok >= u.lo && tok < u.hi) {
-        load_vec<T, 8>(src + (tok - u.lo) * stride, x[j]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[j][e] = 0.f;
-      }
+      if (tok >= u.lo && tok < u.hi)
+        next[j].load(src + (tok - u.lo) * stride);
+      else
+        next[j].clear();
     }
+  };
+  const int first = u.lo / (kStep * L::kTokens) * kStep;
+  fetch(first);
+#pragma unroll 1
+  for (int j0 = first; j0 * L::kTokens < u.hi; j0 += kStep) {
+    Raw8<T> now[kStep];
+#pragma unroll
+    for (int j = 0; j < kStep; ++j) now[j] = next[j];
+    if ((j0 + kStep) * L::kTokens < u.hi) fetch(j0 + kStep);  // (on their way while these are worked on)
 #pragma unroll
     for (int j = 0; j < kStep; ++j) {
       const int tok0 = (j0 + j) * L::kTokens, tok = tok0 + at.sub;
       if (tok0 + L::kTokens <= u.lo || tok0 >= u.hi) continue;  // (the same for the whole warp)
+      float x[8];
+      now[j].to(x);
       uint32_t w;
-      const __half2 sz = quantise(x[j], &w);
+      const __half2 sz = quantise(x, &w);
       if (tok < u.lo || tok >= u.hi) continue;
       if (at.d0 % kPgGroup == 0) params[tok * B::kGroups] = sz;
       if (u.side) {
@@ -246,34 +266,32 @@ __global__ void __launch_bounds__(kPqThreads) read_kernel(const __grid_constant_
         words[tl][2 * q + 1] = __byte_perm(v.z, v.w, sel);
       }
   }
-  constexpr int kStep = 4;
-#pragma unroll 1
-  for (int j0 = u.lo / (kStep * L::kTokens) * kStep; j0 * L::kTokens < u.hi; j0 += kStep) {
-    uint32_t w[kStep];
-    __half2 sz[kStep];
+  // all of the run's loads first, then its tokens
+  constexpr int kSteps = 32 / L::kTokens;
+  uint32_t w[kSteps];
+  __half2 sz[kSteps];
 #pragma unroll
-    for (int j = 0; j < kStep; ++j) {
-      const int tok = (j0 + j) * L::kTokens + at.sub;
-      w[j] = 0;
-      sz[j] = __half2half2(__ushort_as_half(0));
-      if (tok >= u.lo && tok < u.hi && u.block) {  // (no such page: zeros)
-        sz[j] = params[tok * B::kGroups];
-        if (!u.side) w[j] = *reinterpret_cast<const uint32_t*>(krow + tok * (D / 2));
-      }
+  for (int j = 0; j < kSteps; ++j) {
+    const int tok = j * L::kTokens + at.sub;
+    w[j] = 0;
+    sz[j] = __half2half2(__ushort_as_half(0));
+    if (tok >= u.lo && tok < u.hi && u.block) {  // (no such page: zeros)
+      sz[j] = params[tok * B::kGroups];
+      if (!u.side) w[j] = *reinterpret_cast<const uint32_t*>(krow + tok * (D / 2));
     }
+  }
 #pragma unroll
-    for (int j = 0; j < kStep; ++j) {
-      const int tok = (j0 + j) * L::kTokens + at.sub;
-      if (tok < u.lo || tok >= u.hi) continue;
-      const float2 f = __half22float2(sz[j]);
-      float x[8];
+  for (int j = 0; j < kSteps; ++j) {
+    const int tok = j * L::kTokens + at.sub;
+    if (tok < u.lo || tok >= u.hi) continue;
+    const float2 f = __half22float2(sz[j]);
+    float x[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const uint32_t c = u.side && u.block ? words[j % L::kT][e / 2] >> (16 * (e & 1) + 4 * (tok / 8)) : w[j] >> (4 * e);
-        x[e] = fmaf(static_cast<float>(c & 15u), f.x, f.y);
-      }
-      store_vec<T, 8>(dst + (tok - u.lo) * stride, x);
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t c = u.side && u.block ? words[j % L::kT][e / 2] >> (16 * (e & 1) + 4 * (tok / 8)) : w[j] >> (4 * e);
+      x[e] = fmaf(static_cast<float>(c & 15u), f.x, f.y);
     }
+    store_vec<T, 8>(dst + (tok - u.lo) * stride, x);
   }
 }
 
@@ -484,6 +502,6 @@ extern "C" tss_status tss_paged_attention(tss_paged* h, const tss_paged_cache* c
   p.status = h->status;
   bool too_large = false;
   const cudaError_t e = launch_paged_attention(h, p, b, static_cast<cudaStream_t>(stream), &too_large);
-  if (too_large) return refuse(TSS_ERR_INVALID_ARG, "more than 2^30 (page, head, row tile) units in one call");
+  if (too_large) return refuse(TSS_ERR_INVALID_ARG, "too many (page, head, row tile) units in one call");
   return e == cudaSuccess ? TSS_OK : refuse_cuda(e, "launch");
 }

@@ -492,8 +492,8 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
     const bool whole = x0 == 0 && x1 == r.units;
     int c0 = first_cta, c1 = first_cta + splits - 1;  // CTAs that share the item
     if (!whole && !p.aligned) {
-      c0 = cta_of_unit(u - x0, p.total);
-      c1 = cta_of_unit(u - x0 + r.units - 1, p.total);
+      c0 = cta_of_unit(p, b, u - x0);
+      c1 = cta_of_unit(p, b, u - x0 + r.units - 1);
     }
     // a CTA's two partials: of the item that it begins, and of the one that it ends or runs through
     const int slot = blockIdx.x * 2 + (x0 == 0 ? 1 : 0);
@@ -588,8 +588,9 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
 template <int D, int NT, bool TWO>
 cudaError_t pa_launch(PaParams& p, int sms, cudaStream_t s) {
   using S = PaShape<D, NT>;
-  // (a run of a unit for each warp at least; ending an item costs about as much as 8 units)
-  const int grid = pa_cut(p, sms * S::kCtas, S::kWarps, 8);
+  // A run of a unit for each warp at least.  Leads of 0 / 3 / 6 / 10 / 16 pages, us: six requests of 60 to 30000
+  // tokens 180 / 100 / 66 / 53 / 50, eight of 512 to 4096 45 / 40 / 38 / 37 / 38, equal ones alike at any.
+  const int grid = pa_cut(p, sms * S::kCtas, S::kWarps, 8, 10 * (3 - p.halves));
   return launch_k(paged_attn_kernel<D, NT, TWO>, dim3(grid), dim3(S::kWarps * 32), S::kSmem, s, true, p);
 }
 template <int D, int NT, bool TWO>

@@ -10,7 +10,7 @@ struct PaReq {
   int seq, first, n, row;
   int units;             // of one item: those in sight, [0, sink) and [lo, ...)
   int sink, lo;
-  int off;               // units of all items before the request
+  int off, items0;       // units of all items before the request; those items
   int cta, splits;       // aligned runs: CTAs before the request, CTAs of one item
 };
 struct PaParams {
@@ -18,6 +18,8 @@ struct PaParams {
   int n_req, total;      // units in all
   int aligned;           // a CTA's run lies within one item
   int halves;            // 32-token halves of a unit: 2 (a page) or 1
+  int lead;              // even runs: units that an item counts beside its own, for its start and end
+  int weight;            // even runs: units and leads in all
   float* part_o;         // [grid][2][rows][D]
   float2* part_ml;       // [grid][2][rows]
   int* counters;         // [grid], zero between launches
@@ -30,61 +32,11 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
-// Two fp32 operations in one instruction.
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-  float2 d;
-  asm("{\n\t.reg .b64 x, y, z, w;\n\t"
-      "mov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
-      "fma.rn.f32x2 w, x, y, z;\n\t"
-      "mov.b64 {%0, %1}, w;\n\t}\n"
-      : "=f"(d.x), "=f"(d.y)
-      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-  return d;
-}
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-  float2 d;
-  asm("{\n\t.reg .b64 x, y, w;\n\t"
-      "mov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t"
-      "add.rn.f32x2 w, x, y;\n\t"
-      "mov.b64 {%0, %1}, w;\n\t}\n"
-      : "=f"(d.x), "=f"(d.y)
-      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-  return d;
-}
-
 // The tcgen05 kernel (paged_attn_tc.cu; head_dim 128, planned with R = 128 and whole pages) and the query rows of a KV
 // head from which (exclusive) a request goes there.
 constexpr int kPaTcRows = 32;
 cudaError_t paged_attn_tc_prepare();
 cudaError_t launch_paged_attention_tc(PaParams& p, int sms, cudaStream_t s);
-
-// The same on pairs kept in 64-bit registers (low half first), for loops where a pair is used often.
-using f2_t = unsigned long long;
-__device__ __forceinline__ f2_t f2_pack(float x, float y) {
-  f2_t v;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(x), "f"(y));
-  return v;
-}
-__device__ __forceinline__ float2 f2_unpack(f2_t v) {
-  float2 f;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(v));
-  return f;
-}
-__device__ __forceinline__ f2_t f2_fma(f2_t a, f2_t b, f2_t c) {
-  f2_t d;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-  return d;
-}
-__device__ __forceinline__ f2_t f2_mul(f2_t a, f2_t b) {
-  f2_t d;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
-__device__ __forceinline__ f2_t f2_add(f2_t a, f2_t b) {
-  f2_t d;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
 
 // The power of two that brings a row's largest query value `big` into [2^14, 2^15), where fp16 holds the row exactly
 // (kept within what it and its use in 2^24 / it can be; 1 for a row of zeros, or with an infinity).
@@ -97,11 +49,21 @@ __device__ __forceinline__ float query_scale(float big) {
 constexpr float kTop = 32768.f;
 constexpr float kLeast = 5.9604645e-8f;
 
-// The CTA whose even run of the launch's units holds unit u.
-__device__ __forceinline__ int cta_of_unit(int u, int total) {
-  const long long T = total, G = gridDim.x;
-  int c = static_cast<int>(u * G / T);
-  while ((c + 1) * T / G <= u) ++c;
+// Even runs.  The items' units, each item's led by p.lead more, laid end to end and cut evenly: the first unit at
+// or after place g of them, and the CTA whose run holds unit u (of request b).
+__device__ __forceinline__ int unit_at(const PaParams& p, int g) {
+  int b = 0;
+  while (b + 1 < p.n_req && p.r[b + 1].off + p.lead * p.r[b + 1].items0 <= g) ++b;
+  const PaReq& r = p.r[b];
+  const int v = g - r.off - p.lead * r.items0, item = v / (r.units + p.lead);
+  return r.off + item * r.units + max(0, v - item * (r.units + p.lead) - p.lead);
+}
+__device__ __forceinline__ int cta_of_unit(const PaParams& p, int b, int u) {
+  const PaReq& r = p.r[b];
+  const int g = u + p.lead * (r.items0 + (u - r.off) / r.units + 1);
+  const long long T = p.weight, G = gridDim.x;
+  int c = static_cast<int>(g * G / T);
+  while ((c + 1) * T / G <= g) ++c;
   return c;
 }
 
@@ -118,8 +80,8 @@ __device__ __forceinline__ void cta_run(const PaParams& p, int* u0, int* u1, int
     *first_cta = cta - j;
     *splits = r.splits;
   } else {
-    *u0 = static_cast<int>(static_cast<long long>(p.total) * cta / gridDim.x);
-    *u1 = static_cast<int>(static_cast<long long>(p.total) * (cta + 1) / gridDim.x);
+    *u0 = unit_at(p, static_cast<int>(static_cast<long long>(p.weight) * cta / gridDim.x));
+    *u1 = cta + 1 == static_cast<int>(gridDim.x) ? p.total : unit_at(p, static_cast<int>(static_cast<long long>(p.weight) * (cta + 1) / gridDim.x));
     *first_cta = *splits = 0;
   }
 }
@@ -199,13 +161,14 @@ inline bool pa_plan(PaParams& p, const PgBatch& batch, Take take, int R, int hal
   const PgAttnArgs& a = p.a;
   const int unit = 32 * halves, gq = a.hq / a.hk;
   long long at = 0;
+  int items = 0;
   p.halves = halves;
   p.n_req = 0;
   for (int i = 0; i < batch.n_req; ++i) {
     const PgReq& q = batch.r[i];
     if (q.n == 0 || !take(q)) continue;
     PaReq& r = p.r[p.n_req++];
-    r = PaReq{q.seq, q.first, q.n, q.row, 0, 0, 0, static_cast<int>(at), 0, 1};
+    r = PaReq{q.seq, q.first, q.n, q.row, 0, 0, 0, static_cast<int>(at), items, 0, 1};
     const int end = (q.first + q.n + unit - 1) / unit;
     if (a.window) {
       r.lo = (q.first - a.window + 1 > 0 ? q.first - a.window + 1 : 0) / unit;
@@ -214,17 +177,19 @@ inline bool pa_plan(PaParams& p, const PgBatch& batch, Take take, int R, int hal
       if (r.sink > r.lo) r.sink = r.lo;
     }
     r.units = r.sink + end - r.lo;
-    at += static_cast<long long>(r.units) * a.hk * ((q.n * gq + R - 1) / R);
-    if (at > 0x3fffffff) return false;
+    const int mine = a.hk * ((q.n * gq + R - 1) / R);
+    items += mine;
+    at += static_cast<long long>(r.units) * mine;
+    if (at > 0x1fffffff) return false;
   }
   p.total = static_cast<int>(at);
   return true;
 }
 
-// Cuts the units into runs for at most `most` CTAs and returns their number: even runs, or, where a CTA's run
-// is then at most `slack` units longer, runs that lie within one item each (a CTA ends one item instead of two or
-// three).  Runs have at least `least` units.
-inline int pa_cut(PaParams& p, int most, int least, int slack) {
+// Cuts the units into runs for at most `most` CTAs and returns their number: even runs, every item counting `lead`
+// units beside its own (for its start and end), or, where a CTA's run is then at most `slack` units longer, runs
+// that lie within one item each (a CTA ends one item instead of two or three).  Runs have at least `least` units.
+inline int pa_cut(PaParams& p, int most, int least, int slack, int lead) {
   const int even = (p.total + most - 1) / most;
   const auto items = [&](int i) { return ((i + 1 < p.n_req ? p.r[i + 1].off : p.total) - p.r[i].off) / p.r[i].units; };
   const auto ctas = [&](int len) {
@@ -235,7 +200,11 @@ inline int pa_cut(PaParams& p, int most, int least, int slack) {
   int run = even > least ? even : least;
   while (run <= even + slack && ctas(run) > most) ++run;
   p.aligned = run <= even + slack;
-  if (!p.aligned) return p.total < most ? p.total : most;
+  if (!p.aligned) {
+    p.lead = lead;
+    p.weight = p.total + lead * (p.r[p.n_req - 1].items0 + items(p.n_req - 1));
+    return p.total < most ? p.total : most;
+  }
   int grid = 0;
   for (int i = 0; i < p.n_req; ++i) {
     p.r[i].cta = grid;

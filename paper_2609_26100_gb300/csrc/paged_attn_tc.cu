@@ -394,7 +394,8 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
     const uint32_t lanes = static_cast<uint32_t>(qd * 32) << 16;
     bool ok = true;
     for (int t = 0, seg = 0; t < n; ++seg) {
-      const PaReq& r = p.r[request_of(u0 + t)];
+      const int rb = request_of(u0 + t);
+      const PaReq& r = p.r[rb];
       const int v = u0 + t - r.off, item = v / r.units, x0 = v - item * r.units, len = min(n - t, r.units - x0);
       const int h = item % a.hk, row0 = item / a.hk * kPtRows, rows = min(kPtRows, r.n * gq - row0);
       // Q: 16 lanes a row, 8 dims each, as chunks in the operand's order; the warp's rows in flight together
@@ -627,8 +628,8 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
       const bool whole = x0 == 0 && len == r.units;
       int c0 = first_cta, c1 = first_cta + splits - 1;
       if (!whole && !p.aligned) {
-        c0 = cta_of_unit(u0 + t - x0, p.total);
-        c1 = cta_of_unit(u0 + t - x0 + r.units - 1, p.total);
+        c0 = cta_of_unit(p, rb, u0 + t - x0);
+        c1 = cta_of_unit(p, rb, u0 + t - x0 + r.units - 1);
       }
       if (active) {
         const auto both = [](f2_t x) {
@@ -701,7 +702,7 @@ cudaError_t paged_attn_tc_prepare() {
 cudaError_t launch_paged_attention_tc(PaParams& p, int sms, cudaStream_t s) {
   // (two pages at least, so that the copy, the expansion and the scores of one run under the other's softmax; an
   // item's start and end cost about as much as 6)
-  const int grid = pa_cut(p, sms, 2, 6);
+  const int grid = pa_cut(p, sms, 2, 6, 6);
   return launch_k(p.a.is_half ? paged_attn_tc_kernel<true> : paged_attn_tc_kernel<false>, dim3(grid), dim3(kPtThreads), kPtSmem, s, true, p);
 }
 

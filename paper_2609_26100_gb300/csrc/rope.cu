@@ -55,19 +55,28 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constan
     }
     load_vec<float, 16>(p.table + static_cast<size_t>(pos) * p.rot + 16 * j, cs);
   }
-  const int heads = p.hq + p.hk;
-  for (int h = part * kHeads + sub; h - sub < heads; h += p.splits * kHeads) {
+  const int heads = p.hq + p.hk, step = p.splits * kHeads;
+  // the next head's vectors are on their way while this one is worked on
+  Raw8<T> next[2];
+  const auto fetch = [&](int h) {
+    if (live && h < heads) {
+      const T* x = h < p.hq ? static_cast<const T*>(p.q) + row * p.qs + static_cast<long long>(h) * p.d
+                            : static_cast<const T*>(p.k) + row * p.ks + static_cast<long long>(h - p.hq) * p.d;
+      next[0].load(x + c0);
+      next[1].load(x + c1);
+    }
+  };
+  fetch(part * kHeads + sub);
+#pragma unroll 1
+  for (int h = part * kHeads + sub; h - sub < heads; h += step) {
     const bool on = live && h < heads, isq = h < p.hq;
-    const T* x = isq ? static_cast<const T*>(p.q) + row * p.qs + static_cast<long long>(h) * p.d
-                     : static_cast<const T*>(p.k) + row * p.ks + static_cast<long long>(h - p.hq) * p.d;
     T* y = isq ? static_cast<T*>(p.q_out) + row * p.qos + static_cast<long long>(h) * p.d
                : static_cast<T*>(p.k_out) + row * p.kos + static_cast<long long>(h - p.hq) * p.d;
     const T* gain = static_cast<const T*>(isq ? p.q_gain : p.k_gain);
     float a[16];
-    if (on) {
-      load_vec<T, 8>(x + c0, a);
-      load_vec<T, 8>(x + c1, a + 8);
-    }
+    next[0].to(a);
+    next[1].to(a + 8);
+    fetch(h + step);
     // (every lane of the warp takes part in the butterfly; the condition is the same for all)
     if (p.q_gain || p.k_gain) {
       float ss = 0.f;

@@ -8,6 +8,7 @@ tensors; ``Kv4Cache.allocate`` makes a set that fits together.
 from __future__ import annotations
 
 import ctypes
+from array import array
 from typing import Optional, Sequence
 
 import torch
@@ -49,6 +50,11 @@ def _code(t: torch.Tensor) -> int:
         return _CODES[t.dtype]
     except KeyError:
         raise TypeError(f"bfloat16, float16 or float32 is wanted, not {t.dtype}") from None
+
+
+def _host(values) -> array:
+    """int32 values for a call that reads them before it returns (pass its address, keep it until then)."""
+    return array("i", values)
 
 
 def _ints(t: torch.Tensor, shape, what: str) -> None:
@@ -103,16 +109,19 @@ class PagePool:
         """Pages for tokens[i] tokens of seqs[i] (those it holds stay)."""
         if len(seqs) != len(tokens):
             raise ValueError("seqs and tokens differ in length")
-        check(lib().tss_pages_reserve(self._h, self._ref, len(seqs), _i32(seqs),
-                                      _i32([pages_for(t) for t in tokens]), self._stream(stream)), "tss_pages_reserve")
+        a, b = _host(seqs), _host([-(-t // PAGE_TOKENS) for t in tokens])
+        check(lib().tss_pages_reserve(self._h, self._ref, len(a), a.buffer_info()[0], b.buffer_info()[0], self._stream(stream)),
+              "tss_pages_reserve")
 
     def free(self, seqs: Sequence[int], tokens: Optional[Sequence[int]] = None, stream=None) -> None:
         """Give back the pages of seqs[i] past its first tokens[i] tokens (None: all)."""
         if tokens is not None and len(seqs) != len(tokens):
             raise ValueError("seqs and tokens differ in length")
-        keep = _i32([pages_for(t) for t in tokens]) if tokens is not None else None
-        check(lib().tss_pages_free(self._h, self._ref, len(seqs), _i32(seqs), keep, self._stream(stream)),
-              "tss_pages_free")
+        a, keep = _host(seqs), None
+        if tokens is not None:
+            keep = _host([-(-t // PAGE_TOKENS) for t in tokens])
+        check(lib().tss_pages_free(self._h, self._ref, len(a), a.buffer_info()[0], None if keep is None else keep.buffer_info()[0],
+                                   self._stream(stream)), "tss_pages_free")
 
     def fork(self, src: Sequence[int], dst: Sequence[int], tokens: Sequence[int], stream=None) -> None:
         """dst[i] (which holds nothing) becomes the first tokens[i] tokens of src[i]: full pages are shared, a
@@ -120,9 +129,11 @@ class PagePool:
         n = len(src)
         if len(dst) != n or len(tokens) != n:
             raise ValueError("src, dst and tokens differ in length")
-        check(lib().tss_pages_fork(self._h, self._ref, self._ptrs, self.n_layers, self.page_bytes, n, _i32(src),
-                                   _i32(dst), _i32([int(t) // PAGE_TOKENS for t in tokens]),
-                                   _i32([pages_for(t) for t in tokens]), self._stream(stream)), "tss_pages_fork")
+        a, b = _host(src), _host(dst)
+        c, d = _host([t // PAGE_TOKENS for t in tokens]), _host([-(-t // PAGE_TOKENS) for t in tokens])
+        check(lib().tss_pages_fork(self._h, self._ref, self._ptrs, self.n_layers, self.page_bytes, n, a.buffer_info()[0],
+                                   b.buffer_info()[0], c.buffer_info()[0], d.buffer_info()[0], self._stream(stream)),
+              "tss_pages_fork")
 
     def compact(self, table_out: Optional[torch.Tensor] = None, refs_out: Optional[torch.Tensor] = None, stream=None) -> None:
         """Move the pages in use to the lowest ids; the new table and counts replace the pool's, or go to the
