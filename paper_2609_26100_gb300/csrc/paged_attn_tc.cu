@@ -11,8 +11,8 @@
 // matched in Q and P.
 //
 // Roles (640 threads): warp 0 copies pages (one bulk copy each), warp 1 issues MMAs, warps 2-3 expand codes
-// and parameters, warps 4-19 are the softmax: thread = (row, 16 of the 64 keys).  Two buffers of operands and
-// scores, so that a page's expansion and scores run under the softmax before it.  Runs of pages as in
+// and parameters, warps 4-19 are the softmax: thread = (row, 16 of the 64 keys).  Two buffers of operands, three
+// of scores: a page's expansion and scores run under the softmax of the pages before it.  Runs of pages as in
 // paged_attn.cu, one CTA an SM; partials of shared items are joined by the last CTA in CTA order.
 // Every wait is bounded; on expiry the kernel records a timeout, drains its copies and MMAs and returns.
 #include <cstddef>
@@ -32,13 +32,14 @@ constexpr int kPtQ = kPtRows * 64 * 2;            // one group of Q: 128 rows of
 constexpr int kPtOp = kPtKeys * 64 * 2;           // one group of C or C': 64 rows of 128 bytes
 constexpr int kPtP = kPtRows * kPtKeys * 2;       // one part of one group's weights
 constexpr int kPtParams = 9;                      // arrays of 64: s0 s1 z0 z1 of K, the same of V, log2 of V's larger scale
-constexpr uint32_t kPtTmem = 512;                 // S: 2 buffers x 2 groups x 64 columns; O: 128 from column 256
+constexpr uint32_t kPtTmem = 512;                 // S: 3 buffers x 2 groups x 64 columns; O: 128 from column kPtO
+constexpr uint32_t kPtO = 384;
 
 struct __align__(16) PtShared {
-  float par[2][kPtParams][kPtKeys];                   // (read as 16-byte vectors)
-  uint64_t raw_full[kPtRaw], raw_free[kPtRaw], k_full[2], k_free[2], v_full[2], v_free[2], s_full[2], s_free[2], p_full, p_free, q_full, o_full, drain;
+  float par[4][kPtParams][kPtKeys];                   // (read as 16-byte vectors)
+  uint64_t raw_full[kPtRaw], raw_free[kPtRaw], k_full[2], k_free[2], v_full[2], v_free[2], s_full[3], s_free[3], p_full[2], p_free[2], par_full[4], q_full, o_full, drain;
   uint32_t tmem;
-  int abort, last, bad[kPtRaw], bad_kv[2];
+  int abort, last, bad[kPtRaw], bad_par[4];
   float f[kPtRows], zq[2][kPtRows], top[4][kPtRows];  // per row: factor of the scores, query sums; maxima of its quarters
   float part[4][3][kPtRows];                          // the quarters' sums: p, p z'_0, p z'_1
 };
@@ -50,8 +51,7 @@ __host__ __device__ constexpr uint32_t idesc_f16_m128(int n) {
 }
 
 // mbar_wait, asleep between looks: sixteen warps that poll would take the issue slots of those that work.
-__device__ __forceinline__ bool quiet_wait(uint64_t* bar, uint32_t parity, volatile int* abort, int* status) {
-  if (mbar_try_wait(bar, parity)) return true;
+__device__ __noinline__ bool quiet_wait_slow(uint64_t* bar, uint32_t parity, volatile int* abort, int* status) {
   const uint64_t t0 = globaltimer_ns();
   while (!mbar_try_wait_sleep(bar, parity, 20000)) {
     if (*abort) return false;
@@ -63,6 +63,9 @@ __device__ __forceinline__ bool quiet_wait(uint64_t* bar, uint32_t parity, volat
   }
   return true;
 }
+__device__ __forceinline__ bool quiet_wait(uint64_t* bar, uint32_t parity, volatile int* abort, int* status) {
+  return mbar_try_wait(bar, parity) || quiet_wait_slow(bar, parity, abort, status);
+}
 
 // A word's eight codes as fp16 subnormals.
 __device__ __forceinline__ uint4 expand(uint32_t x) {
@@ -70,11 +73,13 @@ __device__ __forceinline__ uint4 expand(uint32_t x) {
   return make_uint4(x & 0x000f000fu, x & 0x00f000f0u, y & 0x000f000fu, y & 0x00f000f0u);
 }
 
-// 4 columns of a thread's TMEM lane, left in flight: tmem_wait() before they are used.
-__device__ __forceinline__ void tmem_ld4_start(uint32_t taddr, uint32_t* r) {
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%4];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
-               : "r"(taddr));
+// 16 columns of a thread's TMEM lane, left in flight: tmem_wait() before they are used.
+__device__ __forceinline__ void tmem_ld16_start(uint32_t taddr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr));
 }
 __device__ __forceinline__ void tmem_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
@@ -187,7 +192,8 @@ __device__ __forceinline__ void join_parts(const PaParams& p, PtShared& sh, uint
   }
 }
 
-// TWO: weights of two fp16 parts (fp16 outputs); else one (bf16 outputs: its 2^-12 is a fraction of their own 2^-9).
+// TWO: weights of two fp16 parts (fp16 outputs); else one (bf16 outputs: its 2^-12 is a fraction of their own 2^-9),
+// and then two buffers of them.
 template <bool TWO>
 __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __grid_constant__ PaParams p) {
   extern __shared__ uint8_t pt_dyn[];
@@ -195,7 +201,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
   const uint32_t skew = (1024 - (smem_u32(pt_dyn) & 1023)) & 1023;
   uint8_t* sq = pt_dyn + skew;        // Q: group 0, group 1
   uint8_t* skv = sq + 2 * kPtQ;       // [buffer] C_0, C_1, C'_0, C'_1
-  uint8_t* sp = skv + 2 * 4 * kPtOp;  // P s'_0, P s'_1; then their second parts
+  uint8_t* sp = skv + 2 * 4 * kPtOp;  // P s'_0, P s'_1; then their second parts, or the same of the other buffer
   uint8_t* raw = sp + 4 * kPtP;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const PgAttnArgs& a = p.a;
@@ -212,11 +218,14 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
       mbar_init(&sh.k_free[i], 1);
       mbar_init(&sh.v_full[i], kPtExpand);
       mbar_init(&sh.v_free[i], 1);
+      mbar_init(&sh.p_full[i], kPtSoftWarps);
+      mbar_init(&sh.p_free[i], 1);
+    }
+    for (int i = 0; i < 4; ++i) mbar_init(&sh.par_full[i], kPtExpand);
+    for (int i = 0; i < 3; ++i) {
       mbar_init(&sh.s_full[i], 1);
       mbar_init(&sh.s_free[i], kPtSoftWarps);
     }
-    mbar_init(&sh.p_full, kPtSoftWarps);
-    mbar_init(&sh.p_free, 1);
     mbar_init(&sh.q_full, kPtSoftWarps);
     mbar_init(&sh.o_full, 1);
     mbar_init(&sh.drain, 1);
@@ -235,6 +244,11 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
   const uint32_t tm = sh.tmem;
   volatile int* abort = &sh.abort;
   const int n = u1 - u0;  // pages of the run; page t of it is unit u0 + t
+  // P's buffer of page u, and the parity of its barriers' phases: two buffers of one part or one of two parts
+  const auto p_buf = [](int u) { return TWO ? 0 : u & 1; };
+  const auto p_par = [](int u) { return static_cast<uint32_t>(TWO ? u & 1 : (u >> 1) & 1); };
+  constexpr int kPBufs = TWO ? 1 : 2;
+  constexpr int kPBuf = TWO ? 4 * kPtP : 2 * kPtP;
   const auto request_of = [&](int u) {
     int b = 0;
     while (b + 1 < p.n_req && p.r[b + 1].off <= u) ++b;
@@ -276,7 +290,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
     // the copies issued last have landed before the kernel returns
     for (int k = max(0, t - kPtRaw); k < t; ++k) mbar_drain(&sh.raw_full[k % kPtRaw], (k / kPtRaw) & 1);
   } else if (warp == 1) {
-    // ---------------- MMAs: S(t), then O += P(t - 1) C'(t - 1) ----------------
+    // ---------------- MMAs: S two pages ahead, then O += P C' ----------------
     if (lane == 0) {
       constexpr uint32_t id = idesc_f16_m128(64);
       const uint32_t q_a = smem_u32(sq), kv_a = smem_u32(skv), p_a = smem_u32(sp);
@@ -284,44 +298,40 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
       for (int t = 0, seg = 0; t < n && ok; ++seg) {
         const PaReq& r = p.r[request_of(u0 + t)];
         const int len = min(n - t, r.units - (u0 + t - r.off) % r.units);
-        ok = quiet_wait(&sh.q_full, seg & 1, abort, a.status);
-        for (int j = 0; ok && j <= len; ++j) {
-          if (j < len) {
-            const int u = t + j, s = u & 1;
-            if (!quiet_wait(&sh.k_full[s], (u >> 1) & 1, abort, a.status) ||
-                (u >= 2 && !quiet_wait(&sh.s_free[s], ((u >> 1) - 1) & 1, abort, a.status))) {
-              ok = false;
-              break;
-            }
-            tc_fence_after();
+        const auto scores = [&](int u) {
+          const int s = u & 1, b = u % 3;
+          if (!mbar_wait(&sh.k_full[s], (u >> 1) & 1, abort, a.status) ||
+              (u >= 3 && !mbar_wait(&sh.s_free[b], (u / 3 - 1) & 1, abort, a.status)))
+            return false;
+          tc_fence_after();
 #pragma unroll
-            for (int g = 0; g < 2; ++g)
+          for (int g = 0; g < 2; ++g)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              umma_bf16(tm + b * 128 + g * 64, sdesc_sw128(q_a + g * kPtQ + k * 32), sdesc_sw128(kv_a + (s * 4 + g) * kPtOp + k * 32), id,
+                        k ? 1u : 0u);
+          umma_commit(&sh.s_full[b]);
+          umma_commit(&sh.k_free[s]);
+          return true;
+        };
+        ok = mbar_wait(&sh.q_full, seg & 1, abort, a.status) && scores(t) && (len < 2 || scores(t + 1));
+        for (int j = 0; ok && j < len; ++j) {
+          const int u = t + j, s = u & 1;
+          ok = mbar_wait(&sh.v_full[s], (u >> 1) & 1, abort, a.status) && mbar_wait(&sh.p_full[p_buf(u)], p_par(u), abort, a.status);
+          if (!ok) break;
+          tc_fence_after();
+#pragma unroll
+          for (int g = 0; g < 2; ++g)
+#pragma unroll
+            for (int part = 0; part < (TWO ? 2 : 1); ++part)
 #pragma unroll
               for (int k = 0; k < 4; ++k)
-                umma_bf16(tm + s * 128 + g * 64, sdesc_sw128(q_a + g * kPtQ + k * 32), sdesc_sw128(kv_a + (s * 4 + g) * kPtOp + k * 32), id,
-                          k ? 1u : 0u);
-            umma_commit(&sh.s_full[s]);
-            umma_commit(&sh.k_free[s]);
-          }
-          if (j >= 1) {
-            const int u = t + j - 1, s = u & 1;
-            if (!quiet_wait(&sh.v_full[s], (u >> 1) & 1, abort, a.status) || !quiet_wait(&sh.p_full, u & 1, abort, a.status)) {
-              ok = false;
-              break;
-            }
-            tc_fence_after();
-#pragma unroll
-            for (int g = 0; g < 2; ++g)
-#pragma unroll
-              for (int part = 0; part < (TWO ? 2 : 1); ++part)
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                  umma_bf16(tm + 256 + g * 64, sdesc_sw128(p_a + (part * 2 + g) * kPtP + k * 32),
-                            sdesc_sw128(kv_a + (s * 4 + 2 + g) * kPtOp + k * 32), id, (j > 1 || part || k) ? 1u : 0u);
-            umma_commit(&sh.p_free);
-            umma_commit(&sh.v_free[s]);
-            if (j == len) umma_commit(&sh.o_full);
-          }
+                umma_bf16(tm + kPtO + g * 64, sdesc_sw128(p_a + p_buf(u) * kPBuf + (part * 2 + g) * kPtP + k * 32),
+                          sdesc_sw128(kv_a + (s * 4 + 2 + g) * kPtOp + k * 32), id, (j || part || k) ? 1u : 0u);
+          umma_commit(&sh.p_free[p_buf(u)]);
+          umma_commit(&sh.v_free[s]);
+          if (j == len - 1) umma_commit(&sh.o_full);
+          ok = j + 2 >= len || scores(u + 2);
         }
         t += len;
       }
@@ -343,6 +353,17 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
                                        (t < 2 || quiet_wait(&sh.k_free[s], ((t >> 1) - 1) & 1, abort, a.status))))
         break;
       const bool bad = sh.bad[rs];  // without a page: zeros, so that no weight meets a stale operand
+      // Parameters, in a buffer of four: page t - 4's are read out, since S(t - 2), which is complete, was issued after
+      // P V of page t - 4.
+      if (x < kPtKeys) {
+        const uint2 kp = *reinterpret_cast<const uint2*>(blk + PtBlock::kKParams + 8 * x), vp = *reinterpret_cast<const uint2*>(blk + PtBlock::kVParams + 8 * x);
+        const auto pair = [](uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); };
+        const float2 k0 = pair(kp.x), k1 = pair(kp.y), v0 = pair(vp.x), v1 = pair(vp.y);
+        const float all[kPtParams] = {k0.x, k1.x, k0.y, k1.y, v0.x, v1.x, v0.y, v1.y, __log2f(fmaxf(fmaxf(v0.x, v1.x), kLeast))};
+#pragma unroll
+        for (int i = 0; i < kPtParams; ++i) sh.par[t & 3][i][x] = all[i];
+        if (x == 0) sh.bad_par[t & 3] = bad;
+      }
 #pragma unroll
       for (int i = 0; i < kTurns; ++i) {
         // unit w: key w / 4, dims 16 (w % 4) .. + 15 of each group
@@ -356,7 +377,10 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
       }
       fence_async_smem();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&sh.k_full[s]);
+      if (lane == 0) {
+        mbar_arrive(&sh.par_full[t & 3]);
+        mbar_arrive(&sh.k_full[s]);
+      }
       if (!__all_sync(0xffffffffu, t < 2 || quiet_wait(&sh.v_free[s], ((t >> 1) - 1) & 1, abort, a.status))) break;
 #pragma unroll
       for (int i = 0; i < kTurns; ++i) {
@@ -368,16 +392,6 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
 #pragma unroll
         for (int e = 0; e < 4; ++e) *reinterpret_cast<uint4*>(vd + e * 128 + ((vc ^ ((d0 + e) & 7)) << 4)) = expand(vw[e]);
       }
-      // parameters (their readers are done with the buffer's last ones: they precede P V)
-      if (x < kPtKeys) {
-        const uint2 kp = *reinterpret_cast<const uint2*>(blk + PtBlock::kKParams + 8 * x), vp = *reinterpret_cast<const uint2*>(blk + PtBlock::kVParams + 8 * x);
-        const auto pair = [](uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); };
-        const float2 k0 = pair(kp.x), k1 = pair(kp.y), v0 = pair(vp.x), v1 = pair(vp.y);
-        const float all[kPtParams] = {k0.x, k1.x, k0.y, k1.y, v0.x, v1.x, v0.y, v1.y, __log2f(fmaxf(fmaxf(v0.x, v1.x), kLeast))};
-#pragma unroll
-        for (int i = 0; i < kPtParams; ++i) sh.par[s][i][x] = all[i];
-        if (x == 0) sh.bad_kv[s] = bad;
-      }
       fence_async_smem();
       __syncwarp();
       if (lane == 0) {
@@ -387,9 +401,9 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
     }
   } else {
     // ---------------- softmax: thread = (row, a quarter of a page's keys) ----------------
-    // Quarter 2 half + y: keys 8 b + 4 y + {0..3}, b = 0..3, of the half, which are whole chunks of the row's P.
+    // Quarter qt: keys 16 qt .. + 15, which are half of each of four chunks of the row's P.
     // After a wait that gave up the threads go on without waiting, through the same barriers.
-    const int sw = warp - 2 - kPtExpand, qd = warp & 3, qt = sw >> 2, half = qt >> 1, y4 = (qt & 1) * 4;
+    const int sw = warp - 2 - kPtExpand, qd = warp & 3, qt = sw >> 2, half = qt >> 1;
     const int row = qd * 32 + lane, quad = 1 + qd;
     const uint32_t lanes = static_cast<uint32_t>(qd * 32) << 16;
     bool ok = true;
@@ -459,37 +473,43 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
         if (r.n < 64) anc_lo &= (1ull << r.n) - 1;
         anc_hi = r.n <= 64 ? 0ull : r.n < 128 ? anc_hi & ((1ull << (r.n - 64)) - 1) : anc_hi;
       }
+      // pages whose keys every row sees: [0, all0), the sinks', and [all1, all2)
+      int pmax = 0;
+      if (a.window) {
+        pmax = valid ? qp : 0;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) pmax = max(pmax, __shfl_xor_sync(0xffffffffu, pmax, o));
+      }
+      const int all0 = a.window ? min(r.sink, a.sinks / kPtKeys) : 0;
+      const int all1 = r.sink + (a.window ? max(0, (pmax - a.window + kPtKeys) / kPtKeys - r.lo) : 0);
+      const int all2 = r.sink + r.first / kPtKeys - r.lo;
       float ref = -INFINITY;
       f2_t l2 = f2_pack(0.f, 0.f), oz0 = l2, oz1 = l2;
       for (int j = 0; j < len; ++j) {
-        const int u = t + j, s = u & 1;
-        ok = __all_sync(0xffffffffu, ok && quiet_wait(&sh.v_full[s], (u >> 1) & 1, abort, a.status) &&
-                                         quiet_wait(&sh.s_full[s], (u >> 1) & 1, abort, a.status));
+        const int u = t + j, sb = u % 3;
+        ok = ok && quiet_wait(&sh.par_full[u & 3], (u >> 2) & 1, abort, a.status) && quiet_wait(&sh.s_full[sb], (u / 3) & 1, abort, a.status);
         tc_fence_after();
         if (active) {
-          const int x = x0 + j, key0 = (x < r.sink ? x : x - r.sink + r.lo) * kPtKeys;
-          uint32_t vis = 0xffffu;  // bit 4 b + i
-          if (valid && (a.window || key0 + kPtKeys > r.first || sh.bad_kv[s])) {
-            const uint32_t m = sh.bad_kv[s] ? 0u : static_cast<uint32_t>(row_sees(a, r, qp, anc_lo, anc_hi, key0) >> (32 * half)) >> y4;
-            vis = (m & 15u) | (m >> 4 & 0xf0u) | (m >> 8 & 0xf00u) | (m >> 12 & 0xf000u);
-          }
+          const int x = x0 + j;
+          uint32_t vis = 0xffffu;  // bit i: key 16 qt + i
+          if (sh.bad_par[u & 3])
+            vis = valid ? 0u : vis;
+          else if (valid && !(x < all0 || (x >= all1 && x < all2)))
+            vis = static_cast<uint32_t>(row_sees(a, r, qp, anc_lo, anc_hi, (x < r.sink ? x : x - r.sink + r.lo) * kPtKeys) >> (16 * qt)) & 0xffffu;
           const auto page = [&](auto all_tag) {
             constexpr bool kAll = decltype(all_tag)::value;  // the warp's rows see all of the thread's keys
-            const float* par = &sh.par[s][0][half * 32 + y4];
-            const auto pr = [&](int k, int b) { return *reinterpret_cast<const ulonglong2*>(par + k * kPtKeys + 8 * b); };
-            f2_t c[8];  // scores / f of keys (b, 0..1) and (b, 2..3)
+            const float* par = &sh.par[u & 3][0][16 * qt];
+            const auto pr = [&](int k, int b) { return *reinterpret_cast<const ulonglong2*>(par + k * kPtKeys + 4 * b); };
+            f2_t c[8];  // scores / f of keys 2 i, 2 i + 1
             {
               uint32_t s0[16], s1[16];
               __syncwarp();
-#pragma unroll
-              for (int b = 0; b < 4; ++b) {
-                tmem_ld4_start(tm + lanes + s * 128 + half * 32 + y4 + 8 * b, s0 + 4 * b);
-                tmem_ld4_start(tm + lanes + s * 128 + 64 + half * 32 + y4 + 8 * b, s1 + 4 * b);
-              }
+              tmem_ld16_start(tm + lanes + sb * 128 + 16 * qt, s0);
+              tmem_ld16_start(tm + lanes + sb * 128 + 64 + 16 * qt, s1);
               tmem_wait();
               tc_fence_before();
               __syncwarp();
-              if (lane == 0) mbar_arrive(&sh.s_free[s]);
+              if (lane == 0) mbar_arrive(&sh.s_free[sb]);
 #pragma unroll
               for (int b = 0; b < 4; ++b) {
                 const ulonglong2 a0 = pr(0, b), a1 = pr(1, b), b0 = pr(2, b), b1 = pr(3, b);
@@ -533,13 +553,13 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
                 oz1 = f2_mul(oz1, al2);
               }
               if (j > 0 && __any_sync(0xffffffffu, al != 1.f)) {
-                ok = __all_sync(0xffffffffu, ok && quiet_wait(&sh.p_free, (u - 1) & 1, abort, a.status));
+                ok = ok && quiet_wait(&sh.p_free[p_buf(u - 1)], p_par(u - 1), abort, a.status);
                 tc_fence_after();
                 __syncwarp();
                 float o[16];
 #pragma unroll
                 for (int x2 = 0; x2 < 2; ++x2) {
-                  const uint32_t at = tm + lanes + 256 + qt * 32 + x2 * 16;
+                  const uint32_t at = tm + lanes + kPtO + qt * 32 + x2 * 16;
                   tmem_ld16(at, o);
 #pragma unroll
                   for (int i = 0; i < 16; ++i) o[i] *= al;
@@ -548,65 +568,69 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
                 tc_fence_before();
               }
             }
-            if (u > 0) ok = __all_sync(0xffffffffu, ok && quiet_wait(&sh.p_free, (u - 1) & 1, abort, a.status));
-            // weights: chunk x of a half of the row's P holds, at 2 b + i, key 8 b + 2 x + i; these are x = y4 / 2 + y
+            if (u >= kPBufs) ok = ok && quiet_wait(&sh.p_free[p_buf(u)], p_par(u - kPBufs), abort, a.status);
+            // weights: chunk x of a half of the row's P holds, at 2 b + i, key 8 b + 2 x + i; b is 2 (qt & 1) + bb here
             const f2_t nref = f2_pack(-ref, -ref);
-            uint32_t hi[2][2][4], lo[2][2][4];  // [y][group][b]
+            uint8_t* pd = sp + p_buf(u) * kPBuf + row * 128 + (qt & 1) * 8;
 #pragma unroll
-            for (int b = 0; b < 4; ++b) {
-              const ulonglong2 v0s = pr(4, b), v1s = pr(5, b), z0s = pr(6, b), z1s = pr(7, b);
+            for (int xx = 0; xx < 2; ++xx) {  // chunks 2 xx, 2 xx + 1
+              uint32_t hi[2][2][2], lo[2][2][2];  // [y: chunk 2 xx + y][group][bb]
+#pragma unroll
+              for (int bb = 0; bb < 2; ++bb) {
+                // keys 8 bb + 4 xx + {0..3} of the quarter
+                const int q4 = 2 * bb + xx;
+                const ulonglong2 v0s = pr(4, q4), v1s = pr(5, q4), z0s = pr(6, q4), z1s = pr(7, q4);
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                  const int k = 4 * q4 + 2 * y;
+                  const float2 e = f2_unpack(f2_fma(c[k / 2], f2, nref));
+                  const float2 wf = make_float2(ex2(e.x), ex2(e.y));
+                  const f2_t v0 = y ? v0s.y : v0s.x, v1 = y ? v1s.y : v1s.x, z0 = y ? z0s.y : z0s.x, z1 = y ? z1s.y : z1s.x;
+                  const f2_t down = f2_pack(0.0625f, 0.0625f);  // (odd nibbles stand four bits up)
+                  f2_t p0, p1;
+                  if constexpr (kAll) {
+                    f2_t w = f2_pack(wf.x, wf.y);
+                    l2 = f2_add(l2, w);
+                    oz0 = f2_fma(w, z0, oz0);
+                    oz1 = f2_fma(w, z1, oz1);
+                    if (bb) w = f2_mul(w, down);
+                    p0 = f2_mul(w, v0);
+                    p1 = f2_mul(w, v1);
+                  } else {  // (what the row does not see may be NaN: selected away, not multiplied)
+                    const bool on0 = vis >> k & 1u, on1 = vis >> (k + 1) & 1u;
+                    const auto pick = [&](f2_t m) {
+                      const float2 q = f2_unpack(m);
+                      return f2_pack(on0 ? q.x : 0.f, on1 ? q.y : 0.f);
+                    };
+                    f2_t w = f2_pack(on0 ? wf.x : 0.f, on1 ? wf.y : 0.f);
+                    l2 = f2_add(l2, w);
+                    oz0 = f2_fma(w, pick(z0), oz0);
+                    oz1 = f2_fma(w, pick(z1), oz1);
+                    if (bb) w = f2_mul(w, down);
+                    p0 = f2_mul(w, pick(v0));
+                    p1 = f2_mul(w, pick(v1));
+                  }
+                  const auto split = [&](f2_t m, uint32_t* first, uint32_t* rest) {
+                    const float2 q = f2_unpack(m);
+                    *first = pack_f16(q.x, q.y);
+                    if constexpr (TWO) {
+                      const float2 back = __half22float2(*reinterpret_cast<const __half2*>(first));
+                      const float2 d = f2_unpack(f2_fma(f2_pack(back.x, back.y), f2_pack(-1.f, -1.f), m));
+                      *rest = pack_f16(d.x, d.y);
+                    }
+                  };
+                  split(p0, &hi[y][0][bb], &lo[y][0][bb]);
+                  split(p1, &hi[y][1][bb], &lo[y][1][bb]);
+                }
+              }
 #pragma unroll
               for (int y = 0; y < 2; ++y) {
-                const int k = 4 * b + 2 * y;
-                const float2 e = f2_unpack(f2_fma(c[k / 2], f2, nref));
-                const float2 wf = make_float2(ex2(e.x), ex2(e.y));
-                const f2_t v0 = y ? v0s.y : v0s.x, v1 = y ? v1s.y : v1s.x, z0 = y ? z0s.y : z0s.x, z1 = y ? z1s.y : z1s.x;
-                const f2_t down = f2_pack(0.0625f, 0.0625f);  // (odd nibbles stand four bits up)
-                f2_t p0, p1;
-                if constexpr (kAll) {
-                  f2_t w = f2_pack(wf.x, wf.y);
-                  l2 = f2_add(l2, w);
-                  oz0 = f2_fma(w, z0, oz0);
-                  oz1 = f2_fma(w, z1, oz1);
-                  if (b & 1) w = f2_mul(w, down);
-                  p0 = f2_mul(w, v0);
-                  p1 = f2_mul(w, v1);
-                } else {  // (what the row does not see may be NaN: selected away, not multiplied)
-                  const bool on0 = vis >> k & 1u, on1 = vis >> (k + 1) & 1u;
-                  const auto pick = [&](f2_t m) {
-                    const float2 q = f2_unpack(m);
-                    return f2_pack(on0 ? q.x : 0.f, on1 ? q.y : 0.f);
-                  };
-                  f2_t w = f2_pack(on0 ? wf.x : 0.f, on1 ? wf.y : 0.f);
-                  l2 = f2_add(l2, w);
-                  oz0 = f2_fma(w, pick(z0), oz0);
-                  oz1 = f2_fma(w, pick(z1), oz1);
-                  if (b & 1) w = f2_mul(w, down);
-                  p0 = f2_mul(w, pick(v0));
-                  p1 = f2_mul(w, pick(v1));
+                const int at = ((half * 4 + 2 * xx + y) ^ (row & 7)) << 4;
+#pragma unroll
+                for (int g = 0; g < 2; ++g) {
+                  *reinterpret_cast<uint2*>(pd + g * kPtP + at) = make_uint2(hi[y][g][0], hi[y][g][1]);
+                  if constexpr (TWO) *reinterpret_cast<uint2*>(pd + (2 + g) * kPtP + at) = make_uint2(lo[y][g][0], lo[y][g][1]);
                 }
-                const auto split = [&](f2_t m, uint32_t* first, uint32_t* rest) {
-                  const float2 q = f2_unpack(m);
-                  *first = pack_f16(q.x, q.y);
-                  if constexpr (TWO) {
-                    const float2 back = __half22float2(*reinterpret_cast<const __half2*>(first));
-                    const float2 d = f2_unpack(f2_fma(f2_pack(back.x, back.y), f2_pack(-1.f, -1.f), m));
-                    *rest = pack_f16(d.x, d.y);
-                  }
-                };
-                split(p0, &hi[y][0][b], &lo[y][0][b]);
-                split(p1, &hi[y][1][b], &lo[y][1][b]);
-              }
-            }
-            uint8_t* pd = sp + row * 128;
-#pragma unroll
-            for (int y = 0; y < 2; ++y) {
-              const int at = ((half * 4 + y4 / 2 + y) ^ (row & 7)) << 4;
-#pragma unroll
-              for (int g = 0; g < 2; ++g) {
-                *reinterpret_cast<uint4*>(pd + g * kPtP + at) = make_uint4(hi[y][g][0], hi[y][g][1], hi[y][g][2], hi[y][g][3]);
-                if constexpr (TWO)
-                  *reinterpret_cast<uint4*>(pd + (2 + g) * kPtP + at) = make_uint4(lo[y][g][0], lo[y][g][1], lo[y][g][2], lo[y][g][3]);
               }
             }
           };
@@ -616,14 +640,16 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
             page(std::false_type{});
           fence_async_smem();
         } else {  // no row of the quadrant is in use: the arrivals alone, in step with the others
-          if (u > 0) ok = __all_sync(0xffffffffu, ok && quiet_wait(&sh.p_free, (u - 1) & 1, abort, a.status));
-          if (lane == 0) mbar_arrive(&sh.s_free[s]);
+          if (u >= kPBufs) ok = ok && quiet_wait(&sh.p_free[p_buf(u)], p_par(u - kPBufs), abort, a.status);
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sh.s_free[sb]);
         }
         __syncwarp();
-        if (lane == 0) mbar_arrive(&sh.p_full);
+        if (lane == 0) mbar_arrive(&sh.p_full[p_buf(u)]);
       }
       // ---- the segment's end: 32 dims a thread ----
-      ok = __all_sync(0xffffffffu, ok && quiet_wait(&sh.o_full, seg & 1, abort, a.status));
+      ok = ok && quiet_wait(&sh.o_full, seg & 1, abort, a.status);
+      __syncwarp();
       tc_fence_after();
       const bool whole = x0 == 0 && len == r.units;
       int c0 = first_cta, c1 = first_cta + splits - 1;
@@ -651,7 +677,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
         for (int c = 0; c < 2; ++c) {
           float o[16];
           __syncwarp();
-          tmem_ld16(tm + lanes + 256 + qt * 32 + c * 16, o);
+          tmem_ld16(tm + lanes + kPtO + qt * 32 + c * 16, o);
           if (!valid) continue;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
