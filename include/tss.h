@@ -547,7 +547,8 @@ tss_status tss_paged_read(tss_paged* p, const tss_paged_cache* cache, int layer,
  *   lse: DEVICE fp32 [rows][n_q_heads] or NULL: ln sum exp(scale q.k) over the keys seen.
  * A row that sees nothing gets zeros and lse = -infinity.  Values of keys that a row does not see do not
  * reach it, whatever they are.  Scores, sums and accumulators are fp32; the weights enter the second
- * product as two fp16 parts (22 bits).  Asynchronous on `stream`.  Errors: INVALID_ARG, KV_CAPACITY, CUDA. */
+ * product as two fp16 parts (22 bits), or one (11 bits) for bf16 outputs where some request has more than 8 rows
+ * of a KV head.  Asynchronous on `stream`.  Errors: INVALID_ARG, KV_CAPACITY, CUDA. */
 typedef struct {
   const void* q;
   int64_t q_stride;
@@ -562,6 +563,12 @@ typedef struct {
 } tss_paged_attn;
 tss_status tss_paged_attention(tss_paged* p, const tss_paged_cache* cache, int layer, const tss_paged_batch* batch,
                                const tss_paged_attn* args, void* stream);
+
+/* Fault injection for tests, as tss_inject_timeout: in the next n_calls calls of tss_paged_attention that launch
+ * anything, the first warp of the first CTA copies no page (or, for blocks of many rows, the CTA issues no MMA), so
+ * that its wait runs out after 2 s: the call returns on the device, tss_paged_sync_status reports
+ * TSS_ERR_TIMEOUT, that call's outputs are undefined and the next call runs normally.  0 cancels. */
+tss_status tss_paged_inject_timeout(tss_paged* p, int n_calls);
 
 /* Bookkeeping of pages of any content, entirely on the device (no host wait): the caller's arrays
  *   table [n_seqs][max_pages]  page ids of each sequence, -1 past held[seq]

@@ -450,6 +450,12 @@ extern "C" tss_status tss_paged_sync_status(tss_paged* h, void* stream) {
   return TSS_OK;
 }
 
+extern "C" tss_status tss_paged_inject_timeout(tss_paged* h, int n_calls) {
+  if (!h || n_calls < 0) return refuse(TSS_ERR_INVALID_ARG, "NULL argument or n_calls < 0");
+  h->inject = n_calls;
+  return TSS_OK;
+}
+
 extern "C" tss_status tss_paged_append(tss_paged* h, const tss_paged_cache* cache, int layer, const tss_paged_batch* batch, const void* k,
                                        const void* v, int64_t k_stride, int64_t v_stride, int dtype, void* stream) {
   return quant_call(h, cache, layer, batch, k, v, nullptr, nullptr, k_stride, v_stride, dtype, true, stream);

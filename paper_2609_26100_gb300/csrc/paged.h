@@ -10,6 +10,7 @@ struct tss_paged {
   float* part_o;    // device: partial results of items that several CTAs share
   float2* part_ml;
   int* counters;    // device [pa_counters], zero between launches
+  int inject;       // attention launches still to be made to run out of time (tests)
 };
 
 namespace tss {
@@ -32,6 +33,6 @@ size_t pa_partial_rows(int sms, int head_dim);
 int pa_counters(int sms);
 cudaError_t pa_prepare_all();
 // *too_large: more work than one launch counts (nothing was launched).
-cudaError_t launch_paged_attention(const tss_paged* h, const PgAttnArgs& a, const PgBatch& batch, cudaStream_t s, bool* too_large);
+cudaError_t launch_paged_attention(tss_paged* h, const PgAttnArgs& a, const PgBatch& batch, cudaStream_t s, bool* too_large);
 
 }  // namespace tss

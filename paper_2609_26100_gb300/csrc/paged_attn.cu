@@ -8,8 +8,8 @@
 // ANDs and a shift, exactly; the factor 16 of every second pair is taken out of the other operand.  Scales
 // and minima join in fp32: s_t multiplies the sum over a group's dims, z_t the sum of the query's; on the
 // value side s'_t goes into the weight, which enters as two fp16 parts (hi and the rest, 22 bits: one part
-// alone costs the output 4e-4 of its size, as much again as rounding it to fp16), and z'_t is summed by
-// itself.  Queries are scaled by a power of two to fill fp16's range, so they are exact too.
+// alone costs the output 4e-4 of its size, twice what rounding it to fp16 does; a quarter of what rounding to bf16
+// does, so blocks of more than 8 rows with bf16 outputs take one part), and z'_t is summed by itself.  Queries are scaled by a power of two to fill fp16's range, so they are exact too.
 //
 // Tokens take the MMA's 16-row side (S^T = K Q^T, O^T = V^T P^T): a block of 8 query rows (N) fills it,
 // where the usual orientation would pad 1 .. 8 rows to 16.  P^T's operand layout is the transpose of S^T's
@@ -19,11 +19,16 @@
 // need no reduction over tokens.  In terms of p s' rather than p, it keeps the weights in fp16's range
 // whatever the values' scales.
 //
-// Work split.  A unit is 32 tokens (half a page) of one item: a request's row tile and KV head.  CTAs of
-// four warps, three to an SM (two with 16 rows), take runs of units; a run's units go round its warps,
-// each with its own ring of bulk copies.  Several small CTAs rather than one: while one ends an item the
-// others stream.  At an item's end the warps' parts are joined in shared memory; items that several CTAs
-// share leave partials, which the last CTA to arrive joins in CTA order (results do not depend on timing).
+// Work split.  A unit is a page (or half of one, for short launches) of one item: a request's row tile and KV
+// head.  CTAs of four warps, three to an SM (two with 16 rows), take runs of units; a run's units go round its
+// warps, each with its own ring of bulk copies.  Several small CTAs rather than one: while one ends an item the
+// others stream.  At an item's end the warps' parts are joined in shared memory; items that several CTAs share
+// leave partials, which the last CTA to arrive joins in CTA order (results do not depend on timing).
+//
+// Bound: up to 8 rows, instruction issue at half rate and HBM together: 4 x 65536 keys, 32 heads, 1 row in 216 us, 5.6 TB/s
+// (a third of the 555 instructions a warp spends on 32 keys and 8 rows take codes apart; 12 warps an SM, as many as
+// 165 registers allow, issue in half of the cycles); beyond, the warp-level MMA and issue: 9 rows 291 us.  One token over
+// 1024 keys takes 9.8 us: launch, table, page, two joins.
 #include <type_traits>
 
 #include "paged_attn.cuh"
@@ -129,6 +134,7 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
   // a unit's copies: lane 0 K codes, 1 V codes, 2 K parameters, 3 V parameters
   const int piece_half = (lane < 2 ? B::kCodes : B::kParams) / 2, piece = piece_half * halves;
   const int piece_at = lane < 2 ? lane * B::kCodes : B::kKParams + (lane - 2) * B::kParams;
+  const bool withheld = p.withhold && blockIdx.x == 0 && warp == 0;
   const auto issue = [&]() {  // the warp's next unit into stage issued % ST
     if (issued >= mine) return;
     if ((issued & 31) == 0) {
@@ -145,7 +151,7 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
       uint64_t* bar = &bars[warp][s];
       if (lane == 0) mbar_arrive_expect_tx(bar, B::kBytes / 2 * halves);
       __syncwarp();
-      if (lane < 4)
+      if (lane < 4 && !withheld)
         bulk_load(ring + s * B::kBytes + piece_at, a.pool + static_cast<long long>(blk >> 1) * B::kBytes + piece_at + (blk & 1) * piece_half, piece,
                   bar);
     }
@@ -581,7 +587,7 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
     u = seg_end;
   }
   // after a wait gave up: the copies in flight land before the CTA ends
-  if (!ok)
+  if (!ok && !withheld)
     for (int k = max(0, issued - ST); k < issued; ++k) mbar_drain(&bars[warp][k % ST], (k / ST) & 1);
 }
 
@@ -616,13 +622,16 @@ cudaError_t pa_prepare_all() {
   return e;
 }
 
-cudaError_t launch_paged_attention(const tss_paged* h, const PgAttnArgs& a, const PgBatch& batch, cudaStream_t s, bool* too_large) {
+cudaError_t launch_paged_attention(tss_paged* h, const PgAttnArgs& a, const PgBatch& batch, cudaStream_t s, bool* too_large) {
   *too_large = false;
   PaParams p;
   p.a = a;
   p.part_o = h->part_o;
   p.part_ml = h->part_ml;
   p.counters = h->counters;
+  const int withhold = h->inject > 0;
+  if (withhold) --h->inject;
+  p.withhold = withhold;
   // Blocks of more than kPaTcRows query rows of a KV head go to the tcgen05 kernel (head_dim 128).
   const int gq = h->hq / h->hk;
   int most = 0, wide = 0;
@@ -645,6 +654,7 @@ cudaError_t launch_paged_attention(const tss_paged* h, const PgAttnArgs& a, cons
     narrow.part_o = p.part_o;
     narrow.part_ml = p.part_ml;
     narrow.counters = p.counters;
+    narrow.withhold = withhold;
     const int R = most <= 8 ? 8 : 16;
     const auto take = [&](const PgReq& q) { return h->d != 128 || q.n * gq <= kPaTcRows; };
     // Units of a page; of half a page where that leaves the warps less than three pages each (a warp takes

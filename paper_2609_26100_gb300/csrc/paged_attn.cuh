@@ -20,6 +20,7 @@ struct PaParams {
   int halves;            // 32-token halves of a unit: 2 (a page) or 1
   int lead;              // even runs: units that an item counts beside its own, for its start and end
   int weight;            // even runs: units and leads in all
+  int withhold;          // fault injection: the first CTA's first warp copies nothing, or its MMA warp issues none
   float* part_o;         // [grid][2][rows][D]
   float2* part_ml;       // [grid][2][rows]
   int* counters;         // [grid], zero between launches
@@ -33,8 +34,10 @@ __device__ __forceinline__ float ex2(float x) {
 }
 
 // The tcgen05 kernel (paged_attn_tc.cu; head_dim 128, planned with R = 128 and whole pages) and the query rows of a KV
-// head from which (exclusive) a request goes there.
-constexpr int kPaTcRows = 32;
+// head above which a request goes there.  A page costs it the same for any number of rows, the warp-level kernel in
+// proportion to its 16-row tiles; us, warp-level / tcgen05, four requests of 4600 tokens and 32 heads: 24 rows 65 / 108,
+// 48 rows 94 / 115, 64 rows 116 / 116, 128 rows 231 / 137; 8 heads: 32 rows 29 / 40, 48 rows 34 / 42, 64 rows 41 / 43.
+constexpr int kPaTcRows = 48;
 cudaError_t paged_attn_tc_prepare();
 cudaError_t launch_paged_attention_tc(PaParams& p, int sms, cudaStream_t s);
 

@@ -31,7 +31,7 @@ EXPORTS = (
     "tss_linear_static_status", "tss_verify_grouped", "tss_attention_kernel",
     "tss_qk_rope", "tss_rope_frequencies", "tss_rope_table",
     "tss_paged_page_bytes", "tss_paged_create", "tss_paged_destroy", "tss_paged_sync_status", "tss_paged_append",
-    "tss_paged_read", "tss_paged_attention",
+    "tss_paged_read", "tss_paged_attention", "tss_paged_inject_timeout",
     "tss_pages_create", "tss_pages_destroy", "tss_pages_sync_status", "tss_pages_reserve", "tss_pages_free",
     "tss_pages_fork", "tss_pages_compact", "tss_pages_copy",
 )
@@ -174,6 +174,8 @@ def lib() -> ctypes.CDLL:
         L.tss_paged_append.argtypes = [_P, cache, I, batch, _P, _P, L64, L64, I, _P]
         L.tss_paged_read.argtypes = L.tss_paged_append.argtypes
         L.tss_paged_attention.argtypes = [_P, cache, I, batch, ctypes.POINTER(TssPagedAttn), _P]
+        L.tss_paged_inject_timeout.argtypes = [_P, I]
+        L.tss_paged_inject_timeout.restype = I
         L.tss_pages_create.argtypes = [I, I, I, PP]
         L.tss_pages_sync_status.argtypes = [_P, _P]
         L.tss_pages_reserve.argtypes = [_P, tables, I, _P, _P, _P]

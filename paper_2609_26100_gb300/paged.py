@@ -257,5 +257,9 @@ class Kv4Cache:
         if s:
             check(s, "tss_paged_attention")
 
+    def inject_timeout(self, n_calls: int) -> None:
+        """tss_paged_inject_timeout: make a wait of the next n_calls attention calls run out (tests)."""
+        check(lib().tss_paged_inject_timeout(self._h, n_calls), "tss_paged_inject_timeout")
+
     def sync_status(self, stream=None) -> int:
         return lib().tss_paged_sync_status(self._h, current_stream() if stream is None else stream)
