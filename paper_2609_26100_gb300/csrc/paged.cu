@@ -37,11 +37,11 @@ __device__ __forceinline__ int owner_of(const int* off, int n, int u, int lane) 
 }
 
 struct PqUnit {
-  int side, head, tok0, lo, hi;  // 32-token run of the page from token tok0; its tokens [lo, hi) are the batch's
+  int side, head, page, tok0, lo, hi;  // 32-token run of the page from token tok0; its tokens [lo, hi) are the batch's
   long long row;                 // row of token `lo` in the caller's arrays
   uint8_t* block;                // nullptr: the table's entry is no page
 };
-__device__ __forceinline__ bool pq_unit(const PqParams& p, int block_bytes, int lane, PqUnit* u) {
+__device__ __forceinline__ bool pq_unit(const PqParams& p, int lane, PqUnit* u) {
   const long long w = static_cast<long long>(blockIdx.x) * (kPqThreads / 32) + (threadIdx.x >> 5);
   const int per = 2 * p.hk;
   if (w >= static_cast<long long>(p.total) * per) return false;
@@ -56,13 +56,16 @@ __device__ __forceinline__ bool pq_unit(const PqParams& p, int block_bytes, int 
   u->lo = max(r.first - t0, 0);
   u->hi = min(r.first + r.n - t0, 32);
   u->row = static_cast<long long>(r.row) + (t0 + u->lo - r.first);
-  const int page = p.table[static_cast<long long>(r.seq) * p.max_pages + t0 / kPgTokens];
+  u->page = p.table[static_cast<long long>(r.seq) * p.max_pages + t0 / kPgTokens];
+  return true;
+}
+// (apart, so that other loads can follow the table's before its answer is here)
+__device__ __forceinline__ void pq_resolve(const PqParams& p, int block_bytes, int lane, PqUnit* u) {
   u->block = nullptr;
-  if (page >= 0 && page < p.n_pages)
-    u->block = p.pool + (static_cast<long long>(page) * p.hk + u->head) * block_bytes;
+  if (u->page >= 0 && u->page < p.n_pages)
+    u->block = p.pool + (static_cast<long long>(u->page) * p.hk + u->head) * block_bytes;
   else if (lane == 0)
     report(p.status, kStatusCheck);
-  return true;
 }
 
 // a / b rounded as by IEEE division, for a normal b whose reciprocal r approximates to a few ulp: the quotient by
@@ -74,23 +77,56 @@ __device__ __forceinline__ float quotient(float a, float b, float r) {
   return fmaf(fmaf(-b, q, a), r, q);
 }
 
-// Scale and minimum of the group that the lane's 8 values belong to (its lanes are 8 neighbours), and their
-// codes, one to a nibble.
-__device__ __forceinline__ __half2 quantise(const float* x, uint32_t* codes) {
-  float lo = x[0], hi = x[0], odd = 0.f;
+// Largest and smallest value of the group that the lane's 8 values belong to (its lanes are 8 neighbours); both not
+// finite where one of them is not.  16-bit values two at a time, maximum and negated minimum in one register.
+__device__ __forceinline__ void group_range(const Raw8<float>& raw, float* lo, float* hi) {
+  float x[8];
+  raw.to(x);
+  float a = x[0], b = x[0], odd = 0.f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    lo = fminf(lo, x[i]);
-    hi = fmaxf(hi, x[i]);
+    a = fminf(a, x[i]);
+    b = fmaxf(b, x[i]);
     odd = fmaf(x[i], 0.f, odd);  // NaN where a value is NaN or infinite
   }
+  if (odd != 0.f) b = INFINITY;
 #pragma unroll
   for (int o = 4; o > 0; o >>= 1) {
-    lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-    hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+    a = fminf(a, __shfl_xor_sync(0xffffffffu, a, o));
+    b = fmaxf(b, __shfl_xor_sync(0xffffffffu, b, o));
   }
-  // a NaN or an infinity poisons its group
-  const bool bad = (__ballot_sync(0xffffffffu, odd != 0.f) >> (threadIdx.x & 24) & 0xffu) != 0;
+  *lo = a;
+  *hi = b;
+}
+template <typename T2, typename T>
+__device__ __forceinline__ void group_range2(const Raw8<T>& raw, float* lo, float* hi) {
+  T2 x[4];
+  memcpy(x, raw.v, 16);
+  const T2 m = __hmax2_nan(__hmax2_nan(x[0], x[1]), __hmax2_nan(x[2], x[3]));
+  const T2 n = __hmax2_nan(__hmax2_nan(__hneg2(x[0]), __hneg2(x[1])), __hmax2_nan(__hneg2(x[2]), __hneg2(x[3])));
+  uint32_t mb, nb;
+  memcpy(&mb, &m, 4);
+  memcpy(&nb, &n, 4);
+  const uint32_t low = __byte_perm(mb, nb, 0x5410), high = __byte_perm(mb, nb, 0x7632);
+  T2 c, d;
+  memcpy(&c, &low, 4);
+  memcpy(&d, &high, 4);
+  c = __hmax2_nan(c, d);
+#pragma unroll
+  for (int o = 4; o > 0; o >>= 1) c = __hmax2_nan(c, __shfl_xor_sync(0xffffffffu, c, o));
+  *hi = to_f32(c.x);
+  *lo = -to_f32(c.y);
+}
+__device__ __forceinline__ void group_range(const Raw8<__half>& raw, float* lo, float* hi) { group_range2<__half2>(raw, lo, hi); }
+__device__ __forceinline__ void group_range(const Raw8<__nv_bfloat16>& raw, float* lo, float* hi) { group_range2<__nv_bfloat162>(raw, lo, hi); }
+
+// Scale and minimum of the lane's group, and the codes of its 8 values, one to a nibble.
+template <typename T>
+__device__ __forceinline__ __half2 quantise(const Raw8<T>& raw, uint32_t* codes) {
+  float lo, hi, x[8];
+  group_range(raw, &lo, &hi);
+  raw.to(x);
+  const bool bad = !(fabsf(lo) < INFINITY && fabsf(hi) < INFINITY);  // a NaN or an infinity poisons its group
   const __half z = __float2half_rn(fminf(fmaxf(lo, -65504.f), 65504.f));
   const float zf = __half2float(z);
   const __half s = __float2half_rn(fminf(fmaxf(quotient(hi - zf, 15.f, 1.f / 15.f), 0.f), 65504.f));
@@ -103,12 +139,16 @@ __device__ __forceinline__ __half2 quantise(const float* x, uint32_t* codes) {
   uint32_t w = 0;
   if (__all_sync(0xffffffffu, inside)) {
     const f2_t nz = f2_pack(-zf, -zf), ns = f2_pack(-sf, -sf), r2 = f2_pack(r, r), magic = f2_pack(12582912.f, 12582912.f);
+    const f2_t less = f2_pack(-12582912.f, -12582912.f), up = f2_pack(256.f, 256.f);
+    f2_t c[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const f2_t d = f2_add(f2_pack(x[2 * i], x[2 * i + 1]), nz), q = f2_mul(d, r2);
-      const float2 c = f2_unpack(f2_add(f2_fma(f2_fma(ns, q, d), r2, q), magic));
-      w |= (__float_as_uint(c.x) & 15u) << (8 * i) | (__float_as_uint(c.y) & 15u) << (8 * i + 4);
+      c[i] = f2_add(f2_add(f2_fma(f2_fma(ns, q, d), r2, q), magic), less);
     }
+    // four codes to 16 bits by multiply-adds (c0 + 256 c2, c1 + 256 c3; the second times 16), as the low bits of 2^23 + n
+    const float2 a = f2_unpack(f2_fma(c[1], up, c[0])), b = f2_unpack(f2_fma(c[3], up, c[2]));
+    w = __byte_perm(__float_as_uint(fmaf(a.y, 16.f, a.x) + 8388608.f), __float_as_uint(fmaf(b.y, 16.f, b.x) + 8388608.f), 0x5410);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -155,14 +195,12 @@ __global__ void __launch_bounds__(kPqThreads) append_kernel(const __grid_constan
   griddep_wait();
   griddep_launch();
   PqUnit u;
-  if (!pq_unit(p, B::kBytes, lane, &u) || !u.block) return;
+  if (!pq_unit(p, lane, &u)) return;
   const L at(lane);
   const T* src = u.side ? static_cast<const T*>(p.v) + u.row * p.vs : static_cast<const T*>(p.k) + u.row * p.ks;
   const long long stride = u.side ? p.vs : p.ks;
   src += u.head * D + at.d0;
-  __half2* params = reinterpret_cast<__half2*>(u.block + (u.side ? B::kVParams : B::kKParams)) + u.tok0 * B::kGroups + at.d0 / kPgGroup;
-  uint8_t* krow = u.block + B::kK + u.tok0 * (D / 2) + at.k_at;
-  uint32_t acc[L::kT][4] = {};  // [t][pair of dims]: 16 bits a dim, nibble b
+  uint32_t acc[L::kT][4] = {};  // [t]: a byte for each even (odd) dim, nibbles b = 0, 1; the same of b = 2, 3
   constexpr int kStep = 4;      // steps whose loads are in flight together: 8 (16) tokens
   Raw8<T> next[kStep];
   const auto fetch = [&](int j0) {
@@ -177,6 +215,10 @@ __global__ void __launch_bounds__(kPqThreads) append_kernel(const __grid_constan
   };
   const int first = u.lo / (kStep * L::kTokens) * kStep;
   fetch(first);
+  pq_resolve(p, B::kBytes, lane, &u);
+  if (!u.block) return;
+  __half2* params = reinterpret_cast<__half2*>(u.block + (u.side ? B::kVParams : B::kKParams)) + u.tok0 * B::kGroups + at.d0 / kPgGroup;
+  uint8_t* krow = u.block + B::kK + u.tok0 * (D / 2) + at.k_at;
 #pragma unroll 1
   for (int j0 = first; j0 * L::kTokens < u.hi; j0 += kStep) {
     Raw8<T> now[kStep];
@@ -187,24 +229,39 @@ __global__ void __launch_bounds__(kPqThreads) append_kernel(const __grid_constan
     for (int j = 0; j < kStep; ++j) {
       const int tok0 = (j0 + j) * L::kTokens, tok = tok0 + at.sub;
       if (tok0 + L::kTokens <= u.lo || tok0 >= u.hi) continue;  // (the same for the whole warp)
-      float x[8];
-      now[j].to(x);
       uint32_t w;
-      const __half2 sz = quantise(x, &w);
+      const __half2 sz = quantise(now[j], &w);
       if (tok < u.lo || tok >= u.hi) continue;
       if (at.d0 % kPgGroup == 0) params[tok * B::kGroups] = sz;
       if (u.side) {
-        const int shift = 4 * (tok / 8);
-        constexpr int kMod = L::kT;
+        const int b = tok0 / 8, shift = 4 * (b & 1);  // (the same for the whole warp)
+        const uint32_t even = (w & 0x0f0f0f0fu) << shift, odd = (w >> 4 & 0x0f0f0f0fu) << shift;
         // (j0 is a multiple of kStep, a multiple of kT: the word is known at compile time)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[j % kMod][e] |= ((w >> (8 * e) & 15u) | (w >> (8 * e + 4) & 15u) << 16) << shift;
+        uint32_t(&to)[4] = acc[j % L::kT];
+        if (b < 2) {
+          to[0] |= even;
+          to[1] |= odd;
+        } else {
+          to[2] |= even;
+          to[3] |= odd;
+        }
       } else {
         *reinterpret_cast<uint32_t*>(krow + tok * (D / 2)) = w;
       }
     }
   }
   if (!u.side) return;
+  // to pairs of dims, 16 bits a dim, nibble b
+#pragma unroll
+  for (int t = 0; t < L::kT; ++t) {
+    uint32_t(&x)[4] = acc[t];
+    const uint32_t e0 = __byte_perm(x[0], x[2], 0x5140), e1 = __byte_perm(x[0], x[2], 0x7362);
+    const uint32_t o0 = __byte_perm(x[1], x[3], 0x5140), o1 = __byte_perm(x[1], x[3], 0x7362);
+    x[0] = __byte_perm(e0, o0, 0x5410);
+    x[1] = __byte_perm(e0, o0, 0x7632);
+    x[2] = __byte_perm(e1, o1, 0x5410);
+    x[3] = __byte_perm(e1, o1, 0x7632);
+  }
   // A lane of even tokens finishes the first half of its words, one of odd tokens the second.
   constexpr int kHalf = L::kT / 2;
 #pragma unroll
@@ -245,7 +302,8 @@ __global__ void __launch_bounds__(kPqThreads) read_kernel(const __grid_constant_
   griddep_wait();
   griddep_launch();
   PqUnit u;
-  if (!pq_unit(p, B::kBytes, lane, &u)) return;
+  if (!pq_unit(p, lane, &u)) return;
+  pq_resolve(p, B::kBytes, lane, &u);
   T* dst = static_cast<T*>(u.side ? p.vo : p.ko);
   if (!dst) return;
   const L at(lane);
@@ -285,11 +343,20 @@ __global__ void __launch_bounds__(kPqThreads) read_kernel(const __grid_constant_
     const int tok = j * L::kTokens + at.sub;
     if (tok < u.lo || tok >= u.hi) continue;
     const float2 f = __half22float2(sz[j]);
+    const f2_t s2 = f2_pack(f.x, f.x), z2 = f2_pack(f.y, f.y), less = f2_pack(-8388608.f, -8388608.f);
     float x[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint32_t c = u.side && u.block ? words[j % L::kT][e / 2] >> (16 * (e & 1) + 4 * (tok / 8)) : w[j] >> (4 * e);
-      x[e] = fmaf(static_cast<float>(c & 15u), f.x, f.y);
+    for (int e = 0; e < 8; e += 2) {
+      // a code as a float: the low bits of 2^23 + c (the conversion instruction has an eighth of the rate)
+      uint32_t c[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t m = u.side && u.block ? words[j % L::kT][e / 2] >> (16 * i + 4 * (tok / 8)) : w[j] >> (4 * (e + i));
+        c[i] = (m & 15u) | 0x4b000000u;
+      }
+      const float2 y = f2_unpack(f2_fma(f2_add(f2_pack(__uint_as_float(c[0]), __uint_as_float(c[1])), less), s2, z2));
+      x[e] = y.x;
+      x[e + 1] = y.y;
     }
     store_vec<T, 8>(dst + (tok - u.lo) * stride, x);
   }
