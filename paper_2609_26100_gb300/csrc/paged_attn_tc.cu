@@ -6,19 +6,25 @@
 // C, C' are the codes as fp16 subnormals (paged_attn.cu); scales, minima, references and sums are fp32,
 // Q exact in fp16 (scaled by a power of two), the weights one fp16 part (bf16 outputs) or two.
 //
-// A nibble word (8 dims of a key, or 8 keys of a dim) becomes one 16-byte chunk of a K-major operand by four
-// ANDs and a shift; the order of the 8 within it (0, 4, 1, 5, 2, 6, 3, 7) and the factor 16 of odd nibbles are
-// matched in Q and P.
+// A nibble word (8 dims of a key, or 8 keys of a dim) becomes eight values of a K-major operand by four ANDs and a
+// shift; their order and the factor 16 of odd nibbles are matched in Q and P.
 //
 // Roles (640 threads): warp 0 copies pages (one bulk copy each), warp 1 issues MMAs, warps 2-3 expand codes
-// and parameters, warps 4-19 are the softmax: thread = (row, 16 of the 64 keys).  Two buffers of operands, three
-// of scores: a page's expansion and scores run under the softmax of the pages before it.  Runs of pages as in
+// and parameters, warps 4-19 are the softmax.  Scores lie in three buffers of TMEM, read as blocks of 16 rows and 8
+// columns: a thread has 4 rows and 4 of a page's keys (in the shape of a row a thread each thread reads the parameters,
+// nine floats a key, of 16 keys: four times the shared-memory traffic, 81 us where this takes 75).  The weights go back
+// to TMEM, over the scores that they come from, as the second product's first operand.  Operands of K and V are
+// double-buffered, so a page's expansion and scores run under the softmax of the pages before it.  Runs of pages as in
 // paged_attn.cu, one CTA an SM; partials of shared items are joined by the last CTA in CTA order.
 // Every wait is bounded; on expiry the kernel records a timeout, drains its copies and MMAs and returns.
 //
-// Bound: the softmax, 1.7 us a page of 64 keys and 128 rows, of which about 1.2 us are its reads of the keys' parameters from
-// shared memory (nine floats a key, the same for every row, at 128 bytes a clock); the MMAs take 0.3 us of it.  About
-// 20 us more a launch: first page, start and end of an item.  128 rows, 32 heads, four requests of 4600 tokens 137 us.
+// Bound: the latency of a page's way through a softmax warp: load of the scores, 16 scores a thread, the quadrant's vote on
+// its references, exponentials, store of the weights.  1.1 us a page with 32 rows in use, 1.4 us with 128; the MMAs take
+// 0.3 us of it.  About 15 us more a launch: first page, masked pages, end of an item, join.  128 rows, 32 heads, four requests
+// of 4600 tokens 127 us; 4 requests of 2048 .. 8000 tokens, 61 rows, 32 / 8 heads 75 us.
+// Built and slower at the latter size: 8 softmax warps of half a page each (83 us), or of every second page (105); a vote
+// by a barrier that warps wait for only after their exponentials (78); K and V expanded by warps of their own into
+// three buffers (85).
 #include <cstddef>
 #include <type_traits>
 
@@ -34,21 +40,24 @@ constexpr int kPtRaw = 4;                         // pages in the ring of copies
 using PtBlock = PgBlock<kPtD>;
 constexpr int kPtQ = kPtRows * 64 * 2;            // one group of Q: 128 rows of 128 bytes
 constexpr int kPtOp = kPtKeys * 64 * 2;           // one group of C or C': 64 rows of 128 bytes
-constexpr int kPtP = kPtRows * kPtKeys * 2;       // one part of one group's weights
+constexpr int kPtJoin = 128;                      // partials whose weights the joining of an item keeps beside Q's memory
 constexpr int kPtParams = 9;                      // arrays of 64: s0 s1 z0 z1 of K, the same of V, log2 of V's larger scale
 constexpr uint32_t kPtTmem = 512;                 // S: 3 buffers x 2 groups x 64 columns; O: 128 from column kPtO
 constexpr uint32_t kPtO = 384;
 
 struct __align__(16) PtShared {
-  float par[4][kPtParams][kPtKeys];                   // (read as 16-byte vectors)
-  uint64_t raw_full[kPtRaw], raw_free[kPtRaw], k_full[2], k_free[2], v_full[2], v_free[2], s_full[3], s_free[3], p_full[2], p_free[2], par_full[4], q_full, o_full, drain;
+  float par[4][kPtParams][kPtKeys];                   // keys in the order 16 q + 4 x + 2 b + e for 16 q + 8 b + 2 x + e
+  uint64_t raw_full[kPtRaw], raw_free[kPtRaw], k_full[2], k_free[2], v_full[2], v_free[2], s_full[3], p_full[3], o_done[2], par_full[4], q_full, o_full, drain;
   uint32_t tmem;
   int abort, last, bad[kPtRaw], bad_par[4];
-  float f[kPtRows], zq[2][kPtRows], top[4][kPtRows];  // per row: factor of the scores, query sums; maxima of its quarters
+  float4 row[kPtRows];                                // factor of the codes' sums, then of the minima of groups 0 and 1
+  unsigned long long anc[2][kPtRows];                 // the rows of its block that a row sees
+  int qp[kPtRows];                                    // its position
+  float top[4][kPtRows];                              // maxima of its quarters
   float part[4][3][kPtRows];                          // the quarters' sums: p, p z'_0, p z'_1
 };
-static_assert(offsetof(PtShared, par) % 16 == 0 && offsetof(PtShared, raw_full) % 8 == 0, "alignment of vectors and barriers");
-constexpr size_t kPtSmem = 1024 + 2 * kPtQ + 2 * 4 * kPtOp + 4 * kPtP + kPtRaw * PtBlock::kBytes;
+static_assert(offsetof(PtShared, par) % 16 == 0 && offsetof(PtShared, row) % 16 == 0 && offsetof(PtShared, raw_full) % 8 == 0, "alignment of vectors and barriers");
+constexpr size_t kPtSmem = 1024 + 2 * kPtQ + 2 * 4 * kPtOp + kPtJoin * kPtRows * 4 + kPtRaw * PtBlock::kBytes;
 
 __host__ __device__ constexpr uint32_t idesc_f16_m128(int n) {
   return (1u << 4) | (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(128 >> 4) << 24);
@@ -77,15 +86,30 @@ __device__ __forceinline__ uint4 expand(uint32_t x) {
   return make_uint4(x & 0x000f000fu, x & 0x00f000f0u, y & 0x000f000fu, y & 0x00f000f0u);
 }
 
-// 16 columns of a thread's TMEM lane, left in flight: tmem_wait() before they are used.
-__device__ __forceinline__ void tmem_ld16_start(uint32_t taddr, uint32_t* r) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-      : "r"(taddr));
+// 16 TMEM lanes (from taddr's) and 16 columns, left in flight (tmem_wait() before they are used): thread l has, in
+// r[4 b + 2 y + e], lane l / 4 + 8 y and column 8 b + 2 (l % 4) + e.
+__device__ __forceinline__ void tmem_ld_block(uint32_t taddr, uint32_t* r) {
+  asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr));
+}
+// The same layout, 8 columns, stored; tmem_stored() before another thread is told.
+__device__ __forceinline__ void tmem_st_block(uint32_t taddr, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.16x256b.x1.b32 [%0], {%1, %2, %3, %4};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3])
+               : "memory");
 }
 __device__ __forceinline__ void tmem_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// umma_bf16 with its first operand in TMEM: 128 lanes, 8 columns of two 16-bit values.
+__device__ __forceinline__ void umma_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}\n" ::"r"(d_tmem),
+      "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
 
 // OR of v over the 128 threads of named barrier id.
 __device__ __forceinline__ bool quad_or(int id, bool v) {
@@ -132,13 +156,12 @@ __device__ __forceinline__ unsigned long long row_sees(const PgAttnArgs& a, cons
 }
 
 // The softmax team of an item's last CTA joins the partials of CTAs c0..c1: first every row's weights of them (in
-// P's and Q's shared memory: no MMA is in flight), then 4 dims of 8 rows a thread, their loads in flight together.
-__device__ __forceinline__ void join_parts(const PaParams& p, PtShared& sh, uint8_t* sq, uint8_t* sp, const PaReq& r, int h, int row0, int rows,
+// shared memory, some of it Q's: no MMA is in flight), then 4 dims of 8 rows a thread, their loads in flight together.
+__device__ __forceinline__ void join_parts(const PaParams& p, PtShared& sh, uint8_t* sq, uint8_t* sj, const PaReq& r, int h, int row0, int rows,
                                            int c0, int c1, int sw, int qt, int row, int lane) {
   const int parts = c1 - c0 + 1;
-  constexpr int kFirst = 4 * kPtP / (kPtRows * 4);  // weights that P's memory takes: 128 partials
   const auto weight = [&](int x) {
-    return (x < kFirst ? reinterpret_cast<float*>(sp) + x * kPtRows : reinterpret_cast<float*>(sq) + (x - kFirst) * kPtRows);
+    return (x < kPtJoin ? reinterpret_cast<float*>(sj) + x * kPtRows : reinterpret_cast<float*>(sq) + (x - kPtJoin) * kPtRows);
   };
   const auto slot = [&](int x) { return static_cast<long long>((c0 + x) * 2 + (x == 0)) * kPtRows; };
   float M = -INFINITY, L = 0.f;
@@ -205,8 +228,8 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
   const uint32_t skew = (1024 - (smem_u32(pt_dyn) & 1023)) & 1023;
   uint8_t* sq = pt_dyn + skew;        // Q: group 0, group 1
   uint8_t* skv = sq + 2 * kPtQ;       // [buffer] C_0, C_1, C'_0, C'_1
-  uint8_t* sp = skv + 2 * 4 * kPtOp;  // P s'_0, P s'_1; then their second parts, or the same of the other buffer
-  uint8_t* raw = sp + 4 * kPtP;
+  uint8_t* sj = skv + 2 * 4 * kPtOp;  // weights of partials
+  uint8_t* raw = sj + kPtJoin * kPtRows * 4;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const PgAttnArgs& a = p.a;
   const int gq = a.hq / a.hk;
@@ -222,13 +245,12 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
       mbar_init(&sh.k_free[i], 1);
       mbar_init(&sh.v_full[i], kPtExpand);
       mbar_init(&sh.v_free[i], 1);
-      mbar_init(&sh.p_full[i], kPtSoftWarps);
-      mbar_init(&sh.p_free[i], 1);
+      mbar_init(&sh.o_done[i], 1);
     }
     for (int i = 0; i < 4; ++i) mbar_init(&sh.par_full[i], kPtExpand);
     for (int i = 0; i < 3; ++i) {
       mbar_init(&sh.s_full[i], 1);
-      mbar_init(&sh.s_free[i], kPtSoftWarps);
+      mbar_init(&sh.p_full[i], kPtSoftWarps);
     }
     mbar_init(&sh.q_full, kPtSoftWarps);
     mbar_init(&sh.o_full, 1);
@@ -248,11 +270,6 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
   const uint32_t tm = sh.tmem;
   volatile int* abort = &sh.abort;
   const int n = u1 - u0;  // pages of the run; page t of it is unit u0 + t
-  // P's buffer of page u, and the parity of its barriers' phases: two buffers of one part or one of two parts
-  const auto p_buf = [](int u) { return TWO ? 0 : u & 1; };
-  const auto p_par = [](int u) { return static_cast<uint32_t>(TWO ? u & 1 : (u >> 1) & 1); };
-  constexpr int kPBufs = TWO ? 1 : 2;
-  constexpr int kPBuf = TWO ? 4 * kPtP : 2 * kPtP;
   const auto request_of = [&](int u) {
     int b = 0;
     while (b + 1 < p.n_req && p.r[b + 1].off <= u) ++b;
@@ -297,16 +314,15 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
     // ---------------- MMAs: S two pages ahead, then O += P C' ----------------
     if (lane == 0) {
       constexpr uint32_t id = idesc_f16_m128(64);
-      const uint32_t q_a = smem_u32(sq), kv_a = smem_u32(skv), p_a = smem_u32(sp);
+      const uint32_t q_a = smem_u32(sq), kv_a = smem_u32(skv);
       bool ok = true;
       for (int t = 0, seg = 0; t < n && ok; ++seg) {
         const PaReq& r = p.r[request_of(u0 + t)];
         const int len = min(n - t, r.units - (u0 + t - r.off) % r.units);
         const auto scores = [&](int u) {
           const int s = u & 1, b = u % 3;
-          if (!mbar_wait(&sh.k_full[s], (u >> 1) & 1, abort, a.status) ||
-              (u >= 3 && !mbar_wait(&sh.s_free[b], (u / 3 - 1) & 1, abort, a.status)))
-            return false;
+          // (buffer b's last reader, P V of page u - 3, was issued before: MMAs run in the order of their issue)
+          if (!mbar_wait(&sh.k_full[s], (u >> 1) & 1, abort, a.status)) return false;
           tc_fence_after();
 #pragma unroll
           for (int g = 0; g < 2; ++g)
@@ -321,8 +337,8 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
         if (p.withhold && blockIdx.x == 0) break;
         ok = mbar_wait(&sh.q_full, seg & 1, abort, a.status) && scores(t) && (len < 2 || scores(t + 1));
         for (int j = 0; ok && j < len; ++j) {
-          const int u = t + j, s = u & 1;
-          ok = mbar_wait(&sh.v_full[s], (u >> 1) & 1, abort, a.status) && mbar_wait(&sh.p_full[p_buf(u)], p_par(u), abort, a.status);
+          const int u = t + j, s = u & 1, b = u % 3;
+          ok = mbar_wait(&sh.v_full[s], (u >> 1) & 1, abort, a.status) && mbar_wait(&sh.p_full[b], (u / 3) & 1, abort, a.status);
           if (!ok) break;
           tc_fence_after();
 #pragma unroll
@@ -331,9 +347,9 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
             for (int part = 0; part < (TWO ? 2 : 1); ++part)
 #pragma unroll
               for (int k = 0; k < 4; ++k)
-                umma_bf16(tm + kPtO + g * 64, sdesc_sw128(p_a + p_buf(u) * kPBuf + (part * 2 + g) * kPtP + k * 32),
-                          sdesc_sw128(kv_a + (s * 4 + 2 + g) * kPtOp + k * 32), id, (j || part || k) ? 1u : 0u);
-          umma_commit(&sh.p_free[p_buf(u)]);
+                umma_ta(tm + kPtO + g * 64, tm + b * 128 + g * 64 + k * 16 + part * 8, sdesc_sw128(kv_a + (s * 4 + 2 + g) * kPtOp + k * 32), id,
+                        (j || part || k) ? 1u : 0u);
+          umma_commit(&sh.o_done[u & 1]);
           umma_commit(&sh.v_free[s]);
           if (j == len - 1) umma_commit(&sh.o_full);
           ok = j + 2 >= len || scores(u + 2);
@@ -364,9 +380,10 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
         const uint2 kp = *reinterpret_cast<const uint2*>(blk + PtBlock::kKParams + 8 * x), vp = *reinterpret_cast<const uint2*>(blk + PtBlock::kVParams + 8 * x);
         const auto pair = [](uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); };
         const float2 k0 = pair(kp.x), k1 = pair(kp.y), v0 = pair(vp.x), v1 = pair(vp.y);
+        const int at = (x & 48) | (x & 6) << 1 | (x & 8) >> 2 | (x & 1);
         const float all[kPtParams] = {k0.x, k1.x, k0.y, k1.y, v0.x, v1.x, v0.y, v1.y, __log2f(fmaxf(fmaxf(v0.x, v1.x), kLeast))};
 #pragma unroll
-        for (int i = 0; i < kPtParams; ++i) sh.par[t & 3][i][x] = all[i];
+        for (int i = 0; i < kPtParams; ++i) sh.par[t & 3][i][at] = all[i];
         if (x == 0) sh.bad_par[t & 3] = bad;
       }
 #pragma unroll
@@ -389,13 +406,21 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
       if (!__all_sync(0xffffffffu, t < 2 || quiet_wait(&sh.v_free[s], ((t >> 1) - 1) & 1, abort, a.status))) break;
 #pragma unroll
       for (int i = 0; i < kTurns; ++i) {
-        // unit w: half w / 128, dims 4 (w / 4 % 32) .. + 3, tokens 8 b + 2 (w % 4) + i of the half
-        const int w = i * 32 * kPtExpand + x, d0 = ((w >> 2) & 31) * 4, vc = (w >> 7) * 4 + (w & 3);
+        // unit w: half w / 128, dims 4 (w / 4 % 32) .. + 3, tokens 8 b + 2 (w % 4) + i of the half; b = 0, 1 go to the
+        // half's first quarter (16 keys: two chunks of a dim's row), b = 2, 3 to its second, as 8 bytes at w % 4.  (Lanes
+        // of every second pair of dims' groups take the quarters in the other order, to meet other banks.)
+        const int w = i * 32 * kPtExpand + x, d0 = ((w >> 2) & 31) * 4, swap = (w >> 3) & 1;
         const uint4 v = bad ? zero : *reinterpret_cast<const uint4*>(blk + PtBlock::kV + w * 16);
-        uint8_t* vd = op + (2 + d0 / 64) * kPtOp + (d0 % 64) * 128;
+        uint8_t* vd = op + (2 + d0 / 64) * kPtOp + (d0 % 64) * 128 + (w & 1) * 8;
+        const int vc = (w >> 7) * 4 + ((w & 3) >> 1), first = vc + 2 * swap, second = vc + 2 - 2 * swap;
         const uint32_t vw[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) *reinterpret_cast<uint4*>(vd + e * 128 + ((vc ^ ((d0 + e) & 7)) << 4)) = expand(vw[e]);
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t f = vw[e] >> (8 * swap), g = vw[e] >> (8 - 8 * swap);
+          uint8_t* row = vd + e * 128;
+          *reinterpret_cast<uint2*>(row + ((first ^ ((d0 + e) & 7)) << 4)) = make_uint2(f & 0x000f000fu, f & 0x00f000f0u);
+          *reinterpret_cast<uint2*>(row + ((second ^ ((d0 + e) & 7)) << 4)) = make_uint2(g & 0x000f000fu, g & 0x00f000f0u);
+        }
       }
       fence_async_smem();
       __syncwarp();
@@ -405,12 +430,23 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
       }
     }
   } else {
-    // ---------------- softmax: thread = (row, a quarter of a page's keys) ----------------
-    // Quarter qt: keys 16 qt .. + 15, which are half of each of four chunks of the row's P.
+    // ---------------- softmax: warp = (32 rows, a quarter of a page's keys) ----------------
+    // Thread: rows qd * 32 + r4 + 8 i, keys 16 qt + 8 b + 2 x4 + e of a page, so that it reads a quarter of the keys'
+    // parameters.  Its weights go where its quarter's scores were, as the second product's operand in TMEM: words b of
+    // x4 at columns 2 x4 + b.  Queries and outputs: row qd * 32 + lane.
     // After a wait that gave up the threads go on without waiting, through the same barriers.
     const int sw = warp - 2 - kPtExpand, qd = warp & 3, qt = sw >> 2, half = qt >> 1;
-    const int row = qd * 32 + lane, quad = 1 + qd;
+    const int row = qd * 32 + lane, quad = 1 + qd, r4 = lane >> 2, x4 = lane & 3;
     const uint32_t lanes = static_cast<uint32_t>(qd * 32) << 16;
+    const auto of_row = [&](const float* v) {  // row `lane`'s value, from a thread that has it
+      float y = 0.f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float z = __shfl_sync(0xffffffffu, v[i], 4 * (lane & 7));
+        if (i == lane >> 3) y = z;
+      }
+      return y;
+    };
     bool ok = true;
     for (int t = 0, seg = 0; t < n; ++seg) {
       const int rb = request_of(u0 + t);
@@ -452,16 +488,10 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
         const uint4 w = make_uint4(pack_f16(x[0] * up, x[4] * up), pack_f16(x[1] * lo, x[5] * lo), pack_f16(x[2] * up, x[6] * up),
                                    pack_f16(x[3] * lo, x[7] * lo));
         *reinterpret_cast<uint4*>(sq + (c8 >> 3) * kPtQ + qr * 128 + (((c8 & 7) ^ (qr & 7)) << 4)) = w;
-        if (c8 == 0) sh.f[qr] = a.scale_log2 * 16777216.f / up;
-        if ((c8 & 7) == 0) sh.zq[c8 >> 3][qr] = sum * (up * 5.9604645e-8f);
+        const float z1 = __shfl_down_sync(0xffffffffu, sum, 8);
+        if (c8 == 0) sh.row[qr] = make_float4(a.scale_log2 * 16777216.f / up, sum * a.scale_log2, z1 * a.scale_log2, 0.f);
       }
-      fence_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&sh.q_full);
-      named_bar_sync(5, kPtSoft);
       const bool valid = row < rows, active = qd * 32 < rows;
-      const float f = sh.f[row];
-      const f2_t f2 = f2_pack(f, f), zq0 = f2_pack(sh.zq[0][row], sh.zq[0][row]), zq1 = f2_pack(sh.zq[1][row], sh.zq[1][row]);
       int qp = 0;
       unsigned long long anc_lo = ~0ull, anc_hi = ~0ull;
       if (valid) {
@@ -478,6 +508,15 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
         if (r.n < 64) anc_lo &= (1ull << r.n) - 1;
         anc_hi = r.n <= 64 ? 0ull : r.n < 128 ? anc_hi & ((1ull << (r.n - 64)) - 1) : anc_hi;
       }
+      if (qt == 0) {
+        sh.qp[row] = qp;
+        sh.anc[0][row] = anc_lo;
+        sh.anc[1][row] = anc_hi;
+      }
+      fence_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sh.q_full);
+      named_bar_sync(5, kPtSoft);
       // pages whose keys every row sees: [0, all0), the sinks', and [all1, all2)
       int pmax = 0;
       if (a.window) {
@@ -488,130 +527,160 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
       const int all0 = a.window ? min(r.sink, a.sinks / kPtKeys) : 0;
       const int all1 = r.sink + (a.window ? max(0, (pmax - a.window + kPtKeys) / kPtKeys - r.lo) : 0);
       const int all2 = r.sink + r.first / kPtKeys - r.lo;
-      float ref = -INFINITY;
-      f2_t l2 = f2_pack(0.f, 0.f), oz0 = l2, oz1 = l2;
+      float ref[4];
+      f2_t l2[4], oz0[4], oz1[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        ref[i] = -INFINITY;
+        l2[i] = oz0[i] = oz1[i] = f2_pack(0.f, 0.f);
+      }
       for (int j = 0; j < len; ++j) {
         const int u = t + j, sb = u % 3;
         ok = ok && quiet_wait(&sh.par_full[u & 3], (u >> 2) & 1, abort, a.status) && quiet_wait(&sh.s_full[sb], (u / 3) & 1, abort, a.status);
         tc_fence_after();
         if (active) {
           const int x = x0 + j;
-          uint32_t vis = 0xffffu;  // bit i: key 16 qt + i
-          if (sh.bad_par[u & 3])
-            vis = valid ? 0u : vis;
-          else if (valid && !(x < all0 || (x >= all1 && x < all2)))
-            vis = static_cast<uint32_t>(row_sees(a, r, qp, anc_lo, anc_hi, (x < r.sink ? x : x - r.sink + r.lo) * kPtKeys) >> (16 * qt)) & 0xffffu;
-          const auto page = [&](auto all_tag) {
-            constexpr bool kAll = decltype(all_tag)::value;  // the warp's rows see all of the thread's keys
-            const float* par = &sh.par[u & 3][0][16 * qt];
-            const auto pr = [&](int k, int b) { return *reinterpret_cast<const ulonglong2*>(par + k * kPtKeys + 4 * b); };
-            f2_t c[8];  // scores / f of keys 2 i, 2 i + 1
-            {
-              uint32_t s0[16], s1[16];
-              __syncwarp();
-              tmem_ld16_start(tm + lanes + sb * 128 + 16 * qt, s0);
-              tmem_ld16_start(tm + lanes + sb * 128 + 64 + 16 * qt, s1);
-              tmem_wait();
-              tc_fence_before();
-              __syncwarp();
-              if (lane == 0) mbar_arrive(&sh.s_free[sb]);
+          uint32_t vis = 0xffffu;  // bit 4 i + 2 b + e
+          if (sh.bad_par[u & 3]) {
+            vis = 0u;
+          } else if (!(x < all0 || (x >= all1 && x < all2))) {
+            const int key0 = (x < r.sink ? x : x - r.sink + r.lo) * kPtKeys;
 #pragma unroll
-              for (int b = 0; b < 4; ++b) {
-                const ulonglong2 a0 = pr(0, b), a1 = pr(1, b), b0 = pr(2, b), b1 = pr(3, b);
+            for (int i = 0; i < 4; ++i) {
+              const int q = qd * 32 + r4 + 8 * i;
+              if (q >= rows) continue;
+              const uint32_t m = static_cast<uint32_t>(row_sees(a, r, sh.qp[q], sh.anc[0][q], sh.anc[1][q], key0) >> (16 * qt)) >> (2 * x4);
+              vis &= ~(15u << (4 * i)) | (m & 3u) << (4 * i) | (m >> 8 & 3u) << (4 * i + 2);
+            }
+          }
+          const auto page = [&](auto all_tag) {
+            constexpr bool kAll = decltype(all_tag)::value;  // the thread's rows see all of its keys
+            const float* par = &sh.par[u & 3][0][16 * qt + 4 * x4];
+            const auto pr = [&](int k) {  // .x: block 0's keys, .y: block 1's
+              return *reinterpret_cast<const ulonglong2*>(par + k * kPtKeys);
+            };
+            const uint32_t at = tm + lanes + sb * 128 + 16 * qt;
+            f2_t c[4][2];  // scores
+            {
+              const ulonglong2 a0 = pr(0), a1 = pr(1), b0 = pr(2), b1 = pr(3);
+              __syncwarp();
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                uint32_t s0[8], s1[8];
+                tmem_ld_block(at + (static_cast<uint32_t>(16 * h) << 16), s0);
+                tmem_ld_block(at + (static_cast<uint32_t>(16 * h) << 16) + 64, s1);
+                tmem_wait();
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
-                  const int k = 4 * b + 2 * y;
-                  const f2_t m = f2_pack(__uint_as_float(s0[k]), __uint_as_float(s0[k + 1])), z = f2_pack(__uint_as_float(s1[k]), __uint_as_float(s1[k + 1]));
-                  c[k / 2] = f2_fma(y ? a1.y : a1.x, z, f2_fma(y ? a0.y : a0.x, m, f2_fma(y ? b1.y : b1.x, zq1, f2_mul(y ? b0.y : b0.x, zq0))));
+                  const float4 q = sh.row[qd * 32 + r4 + 8 * (2 * h + y)];
+                  const f2_t f2 = f2_pack(q.x, q.x), zq0 = f2_pack(q.y, q.y), zq1 = f2_pack(q.z, q.z);
+#pragma unroll
+                  for (int b = 0; b < 2; ++b) {
+                    const uint32_t *m = &s0[4 * b + 2 * y], *z = &s1[4 * b + 2 * y];
+                    const f2_t m2 = f2_pack(__uint_as_float(m[0]), __uint_as_float(m[1])), z2 = f2_pack(__uint_as_float(z[0]), __uint_as_float(z[1]));
+                    const f2_t code = f2_fma(b ? a1.y : a1.x, z2, f2_mul(b ? a0.y : a0.x, m2));
+                    c[2 * h + y][b] = f2_fma(code, f2, f2_fma(b ? b1.y : b1.x, zq1, f2_mul(b ? b0.y : b0.x, zq0)));
+                  }
                 }
               }
             }
-            float top = -INFINITY;
+            float top[4];
+            bool over = false;
+            {
+              const ulonglong2 lg = pr(8);
 #pragma unroll
-            for (int b = 0; b < 4; ++b) {
-              const ulonglong2 lg = pr(8, b);
+              for (int i = 0; i < 4; ++i) {
+                top[i] = -INFINITY;
 #pragma unroll
-              for (int y = 0; y < 2; ++y) {
-                const int k = 4 * b + 2 * y;
-                const float2 e = f2_unpack(f2_fma(c[k / 2], f2, y ? lg.y : lg.x));
-                if constexpr (kAll) {
-                  top = fmaxf(top, fmaxf(e.x, e.y));
-                } else {
-                  top = fmaxf(top, vis >> k & 1u ? e.x : -INFINITY);
-                  top = fmaxf(top, vis >> (k + 1) & 1u ? e.y : -INFINITY);
+                for (int b = 0; b < 2; ++b) {
+                  const float2 e = f2_unpack(f2_add(c[i][b], b ? lg.y : lg.x));
+                  if constexpr (kAll) {
+                    top[i] = fmaxf(top[i], fmaxf(e.x, e.y));
+                  } else {
+                    top[i] = fmaxf(top[i], vis >> (4 * i + 2 * b) & 1u ? e.x : -INFINITY);
+                    top[i] = fmaxf(top[i], vis >> (4 * i + 2 * b + 1) & 1u ? e.y : -INFINITY);
+                  }
                 }
+                over |= top[i] - ref[i] > 15.f;
               }
             }
-            // the row's reference rises where a weight times its value's scale would pass 2^15, to leave it at 2^7
-            if (quad_or(quad, top - ref > 15.f)) {
-              sh.top[qt][row] = top;
+            // a row's reference rises where a weight times its value's scale would pass 2^15, to leave it at 2^7
+            if (quad_or(quad, over)) {
+              float al[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 1));
+                top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 2));
+                if (x4 == 0) sh.top[qt][qd * 32 + r4 + 8 * i] = top[i];
+              }
               named_bar_sync(quad, 128);
-              top = fmaxf(fmaxf(sh.top[0][row], sh.top[1][row]), fmaxf(sh.top[2][row], sh.top[3][row]));
-              float al = 1.f;
-              if (top - ref > 15.f) {
-                const float now = top - 7.f;
-                al = ref == -INFINITY ? 1.f : ex2(ref - now);
-                ref = now;
-                const f2_t al2 = f2_pack(al, al);
-                l2 = f2_mul(l2, al2);
-                oz0 = f2_mul(oz0, al2);
-                oz1 = f2_mul(oz1, al2);
+              bool moved = false;
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const int q = qd * 32 + r4 + 8 * i;
+                const float most = fmaxf(fmaxf(sh.top[0][q], sh.top[1][q]), fmaxf(sh.top[2][q], sh.top[3][q]));
+                al[i] = 1.f;
+                if (most - ref[i] > 15.f) {
+                  const float now = most - 7.f;
+                  al[i] = ref[i] == -INFINITY ? 1.f : ex2(ref[i] - now);
+                  ref[i] = now;
+                  const f2_t al2 = f2_pack(al[i], al[i]);
+                  l2[i] = f2_mul(l2[i], al2);
+                  oz0[i] = f2_mul(oz0[i], al2);
+                  oz1[i] = f2_mul(oz1[i], al2);
+                }
+                moved |= al[i] != 1.f;
               }
-              if (j > 0 && __any_sync(0xffffffffu, al != 1.f)) {
-                ok = ok && quiet_wait(&sh.p_free[p_buf(u - 1)], p_par(u - 1), abort, a.status);
+              if (j > 0 && __any_sync(0xffffffffu, moved)) {
+                ok = ok && quiet_wait(&sh.o_done[(u - 1) & 1], ((u - 1) >> 1) & 1, abort, a.status);
+                const float mine = of_row(al);
                 tc_fence_after();
                 __syncwarp();
                 float o[16];
 #pragma unroll
                 for (int x2 = 0; x2 < 2; ++x2) {
-                  const uint32_t at = tm + lanes + kPtO + qt * 32 + x2 * 16;
-                  tmem_ld16(at, o);
+                  const uint32_t to = tm + lanes + kPtO + qt * 32 + x2 * 16;
+                  tmem_ld16(to, o);
 #pragma unroll
-                  for (int i = 0; i < 16; ++i) o[i] *= al;
-                  tmem_st16(at, o);
+                  for (int i = 0; i < 16; ++i) o[i] *= mine;
+                  tmem_st16(to, o);
                 }
-                tc_fence_before();
               }
             }
-            if (u >= kPBufs) ok = ok && quiet_wait(&sh.p_free[p_buf(u)], p_par(u - kPBufs), abort, a.status);
-            // weights: chunk x of a half of the row's P holds, at 2 b + i, key 8 b + 2 x + i; b is 2 (qt & 1) + bb here
-            const f2_t nref = f2_pack(-ref, -ref);
-            uint8_t* pd = sp + p_buf(u) * kPBuf + row * 128 + (qt & 1) * 8;
+            const ulonglong2 v0s = pr(4), v1s = pr(5), z0s = pr(6), z1s = pr(7);
+            const f2_t down = f2_pack(0.0625f, 0.0625f);  // (odd nibbles stand four bits up)
 #pragma unroll
-            for (int xx = 0; xx < 2; ++xx) {  // chunks 2 xx, 2 xx + 1
-              uint32_t hi[2][2][2], lo[2][2][2];  // [y: chunk 2 xx + y][group][bb]
+            for (int h = 0; h < 2; ++h) {
+              uint32_t hi[2][4], lo[2][4];  // [group][2 y + b]: row i = 2 h + y
 #pragma unroll
-              for (int bb = 0; bb < 2; ++bb) {
-                // keys 8 bb + 4 xx + {0..3} of the quarter
-                const int q4 = 2 * bb + xx;
-                const ulonglong2 v0s = pr(4, q4), v1s = pr(5, q4), z0s = pr(6, q4), z1s = pr(7, q4);
+              for (int y = 0; y < 2; ++y) {
+                const int i = 2 * h + y;
+                const f2_t nref = f2_pack(-ref[i], -ref[i]);
 #pragma unroll
-                for (int y = 0; y < 2; ++y) {
-                  const int k = 4 * q4 + 2 * y;
-                  const float2 e = f2_unpack(f2_fma(c[k / 2], f2, nref));
+                for (int b = 0; b < 2; ++b) {
+                  const float2 e = f2_unpack(f2_add(c[i][b], nref));
                   const float2 wf = make_float2(ex2(e.x), ex2(e.y));
-                  const f2_t v0 = y ? v0s.y : v0s.x, v1 = y ? v1s.y : v1s.x, z0 = y ? z0s.y : z0s.x, z1 = y ? z1s.y : z1s.x;
-                  const f2_t down = f2_pack(0.0625f, 0.0625f);  // (odd nibbles stand four bits up)
+                  const f2_t v0 = b ? v0s.y : v0s.x, v1 = b ? v1s.y : v1s.x, z0 = b ? z0s.y : z0s.x, z1 = b ? z1s.y : z1s.x;
                   f2_t p0, p1;
                   if constexpr (kAll) {
                     f2_t w = f2_pack(wf.x, wf.y);
-                    l2 = f2_add(l2, w);
-                    oz0 = f2_fma(w, z0, oz0);
-                    oz1 = f2_fma(w, z1, oz1);
-                    if (bb) w = f2_mul(w, down);
+                    l2[i] = f2_add(l2[i], w);
+                    oz0[i] = f2_fma(w, z0, oz0[i]);
+                    oz1[i] = f2_fma(w, z1, oz1[i]);
+                    if (b) w = f2_mul(w, down);
                     p0 = f2_mul(w, v0);
                     p1 = f2_mul(w, v1);
-                  } else {  // (what the row does not see may be NaN: selected away, not multiplied)
-                    const bool on0 = vis >> k & 1u, on1 = vis >> (k + 1) & 1u;
+                  } else {  // (what a row does not see may be NaN: selected away, not multiplied)
+                    const bool on0 = vis >> (4 * i + 2 * b) & 1u, on1 = vis >> (4 * i + 2 * b + 1) & 1u;
                     const auto pick = [&](f2_t m) {
                       const float2 q = f2_unpack(m);
                       return f2_pack(on0 ? q.x : 0.f, on1 ? q.y : 0.f);
                     };
                     f2_t w = f2_pack(on0 ? wf.x : 0.f, on1 ? wf.y : 0.f);
-                    l2 = f2_add(l2, w);
-                    oz0 = f2_fma(w, pick(z0), oz0);
-                    oz1 = f2_fma(w, pick(z1), oz1);
-                    if (bb) w = f2_mul(w, down);
+                    l2[i] = f2_add(l2[i], w);
+                    oz0[i] = f2_fma(w, pick(z0), oz0[i]);
+                    oz1[i] = f2_fma(w, pick(z1), oz1[i]);
+                    if (b) w = f2_mul(w, down);
                     p0 = f2_mul(w, pick(v0));
                     p1 = f2_mul(w, pick(v1));
                   }
@@ -624,33 +693,28 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
                       *rest = pack_f16(d.x, d.y);
                     }
                   };
-                  split(p0, &hi[y][0][bb], &lo[y][0][bb]);
-                  split(p1, &hi[y][1][bb], &lo[y][1][bb]);
+                  split(p0, &hi[0][2 * y + b], &lo[0][2 * y + b]);
+                  split(p1, &hi[1][2 * y + b], &lo[1][2 * y + b]);
                 }
               }
+              const uint32_t to = at + (static_cast<uint32_t>(16 * h) << 16);
+              __syncwarp();
 #pragma unroll
-              for (int y = 0; y < 2; ++y) {
-                const int at = ((half * 4 + 2 * xx + y) ^ (row & 7)) << 4;
-#pragma unroll
-                for (int g = 0; g < 2; ++g) {
-                  *reinterpret_cast<uint2*>(pd + g * kPtP + at) = make_uint2(hi[y][g][0], hi[y][g][1]);
-                  if constexpr (TWO) *reinterpret_cast<uint2*>(pd + (2 + g) * kPtP + at) = make_uint2(lo[y][g][0], lo[y][g][1]);
-                }
+              for (int g = 0; g < 2; ++g) {
+                tmem_st_block(to + g * 64, hi[g]);
+                if constexpr (TWO) tmem_st_block(to + g * 64 + 8, lo[g]);
               }
             }
+            tmem_stored();
           };
           if (__all_sync(0xffffffffu, vis == 0xffffu))
             page(std::true_type{});
           else
             page(std::false_type{});
-          fence_async_smem();
-        } else {  // no row of the quadrant is in use: the arrivals alone, in step with the others
-          if (u >= kPBufs) ok = ok && quiet_wait(&sh.p_free[p_buf(u)], p_par(u - kPBufs), abort, a.status);
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&sh.s_free[sb]);
         }
+        tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&sh.p_full[p_buf(u)]);
+        if (lane == 0) mbar_arrive(&sh.p_full[sb]);  // (of a quadrant without rows: the arrival alone)
       }
       // ---- the segment's end: 32 dims a thread ----
       ok = ok && quiet_wait(&sh.o_full, seg & 1, abort, a.status);
@@ -667,9 +731,17 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
           const float2 q = f2_unpack(x);
           return q.x + q.y;
         };
-        sh.part[qt][0][row] = both(l2);
-        sh.part[qt][1][row] = both(oz0);
-        sh.part[qt][2][row] = both(oz1);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float sums[3] = {both(l2[i]), both(oz0[i]), both(oz1[i])};
+#pragma unroll
+          for (int k = 0; k < 3; ++k) {
+            sums[k] += __shfl_xor_sync(0xffffffffu, sums[k], 1);
+            sums[k] += __shfl_xor_sync(0xffffffffu, sums[k], 2);
+            if (x4 == 0) sh.part[qt][k][qd * 32 + r4 + 8 * i] = sums[k];
+          }
+        }
+        const float my_ref = of_row(ref);
         named_bar_sync(quad, 128);
         float L = 0.f, z = 0.f;
 #pragma unroll
@@ -690,12 +762,12 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
                                          fmaf(o[4 * i + 3], 16777216.f, z));
             const int c4 = qt * 8 + c * 4 + i;
             if (whole)
-              finish_row<kPtD>(a, r, h, row0 + row, c4, ref, L, x);
+              finish_row<kPtD>(a, r, h, row0 + row, c4, my_ref, L, x);
             else
               __stcg(reinterpret_cast<float4*>(p.part_o + slot * kPtD) + c4, x);
           }
         }
-        if (!whole && valid && qt == 0) __stcg(p.part_ml + slot, make_float2(ref, L));
+        if (!whole && valid && qt == 0) __stcg(p.part_ml + slot, make_float2(my_ref, L));
         __syncwarp();
         tc_fence_before();
       }
@@ -706,7 +778,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
           if (sh.last) atomicExch(&p.counters[c0], 0);
         }
         named_bar_sync(5, kPtSoft);
-        if (sh.last) join_parts(p, sh, sq, sp, r, h, row0, rows, c0, c1, sw, qt, row, lane);
+        if (sh.last) join_parts(p, sh, sq, sj, r, h, row0, rows, c0, c1, sw, qt, row, lane);
         named_bar_sync(5, kPtSoft);
       }
       t += len;
