@@ -64,8 +64,6 @@ __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float x) { retu
 template <int BYTES>
 struct RawVec;
 template <>
-struct RawVec<4> { using type = uint32_t; };
-template <>
 struct RawVec<8> { using type = uint2; };
 template <>
 struct RawVec<16> { using type = uint4; };

@@ -77,67 +77,98 @@ __device__ __forceinline__ float quotient(float a, float b, float r) {
   return fmaf(fmaf(-b, q, a), r, q);
 }
 
-// Largest and smallest value of the group that the lane's 8 values belong to (its lanes are 8 neighbours); both not
-// finite where one of them is not.  16-bit values two at a time, maximum and negated minimum in one register.
-__device__ __forceinline__ void group_range(const Raw8<float>& raw, float* lo, float* hi) {
-  float x[8];
-  raw.to(x);
-  float a = x[0], b = x[0], odd = 0.f;
+// Largest and negated smallest of the lane's 8 values; both not finite where one of them is not.  16-bit values two at a
+// time, the two results in one register.
+struct Range32 {
+  float hi, nlo;
+  __device__ __forceinline__ explicit Range32(const Raw8<float>& raw) {
+    float x[8], odd = 0.f;
+    raw.to(x);
+    hi = x[0];
+    nlo = -x[0];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    a = fminf(a, x[i]);
-    b = fmaxf(b, x[i]);
-    odd = fmaf(x[i], 0.f, odd);  // NaN where a value is NaN or infinite
+    for (int i = 0; i < 8; ++i) {
+      hi = fmaxf(hi, x[i]);
+      nlo = fmaxf(nlo, -x[i]);
+      odd = fmaf(x[i], 0.f, odd);  // NaN where a value is NaN or infinite
+    }
+    if (odd != 0.f) hi = INFINITY;
   }
-  if (odd != 0.f) b = INFINITY;
-#pragma unroll
-  for (int o = 4; o > 0; o >>= 1) {
-    a = fminf(a, __shfl_xor_sync(0xffffffffu, a, o));
-    b = fmaxf(b, __shfl_xor_sync(0xffffffffu, b, o));
+  __device__ __forceinline__ void join(const Range32& give, int lanes) {
+    hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, give.hi, lanes));
+    nlo = fmaxf(nlo, __shfl_xor_sync(0xffffffffu, give.nlo, lanes));
   }
-  *lo = a;
-  *hi = b;
-}
-template <typename T2, typename T>
-__device__ __forceinline__ void group_range2(const Raw8<T>& raw, float* lo, float* hi) {
-  T2 x[4];
-  memcpy(x, raw.v, 16);
-  const T2 m = __hmax2_nan(__hmax2_nan(x[0], x[1]), __hmax2_nan(x[2], x[3]));
-  const T2 n = __hmax2_nan(__hmax2_nan(__hneg2(x[0]), __hneg2(x[1])), __hmax2_nan(__hneg2(x[2]), __hneg2(x[3])));
-  uint32_t mb, nb;
-  memcpy(&mb, &m, 4);
-  memcpy(&nb, &n, 4);
-  const uint32_t low = __byte_perm(mb, nb, 0x5410), high = __byte_perm(mb, nb, 0x7632);
-  T2 c, d;
-  memcpy(&c, &low, 4);
-  memcpy(&d, &high, 4);
-  c = __hmax2_nan(c, d);
-#pragma unroll
-  for (int o = 4; o > 0; o >>= 1) c = __hmax2_nan(c, __shfl_xor_sync(0xffffffffu, c, o));
-  *hi = to_f32(c.x);
-  *lo = -to_f32(c.y);
-}
-__device__ __forceinline__ void group_range(const Raw8<__half>& raw, float* lo, float* hi) { group_range2<__half2>(raw, lo, hi); }
-__device__ __forceinline__ void group_range(const Raw8<__nv_bfloat16>& raw, float* lo, float* hi) { group_range2<__nv_bfloat162>(raw, lo, hi); }
-
-// Scale and minimum of the lane's group, and the codes of its 8 values, one to a nibble.
+  __device__ __forceinline__ float2 both() const { return make_float2(hi, nlo); }
+};
+template <typename T, typename T2>
+struct Range16 {
+  T2 m;
+  __device__ __forceinline__ explicit Range16(const Raw8<T>& raw) {
+    T2 x[4];
+    memcpy(x, raw.v, 16);
+    const T2 a = __hmax2_nan(__hmax2_nan(x[0], x[1]), __hmax2_nan(x[2], x[3]));
+    const T2 b = __hmax2_nan(__hmax2_nan(__hneg2(x[0]), __hneg2(x[1])), __hmax2_nan(__hneg2(x[2]), __hneg2(x[3])));
+    uint32_t ab, bb;
+    memcpy(&ab, &a, 4);
+    memcpy(&bb, &b, 4);
+    const uint32_t low = __byte_perm(ab, bb, 0x5410), high = __byte_perm(ab, bb, 0x7632);
+    T2 c, d;
+    memcpy(&c, &low, 4);
+    memcpy(&d, &high, 4);
+    m = __hmax2_nan(c, d);
+  }
+  __device__ __forceinline__ void join(const Range16& give, int lanes) { m = __hmax2_nan(m, __shfl_xor_sync(0xffffffffu, give.m, lanes)); }
+  __device__ __forceinline__ float2 both() const { return make_float2(to_f32(m.x), to_f32(m.y)); }
+};
 template <typename T>
-__device__ __forceinline__ __half2 quantise(const Raw8<T>& raw, uint32_t* codes) {
-  float lo, hi, x[8];
-  group_range(raw, &lo, &hi);
-  raw.to(x);
-  const bool bad = !(fabsf(lo) < INFINITY && fabsf(hi) < INFINITY);  // a NaN or an infinity poisons its group
+struct RangeOf;
+template <>
+struct RangeOf<float> { using type = Range32; };
+template <>
+struct RangeOf<__half> { using type = Range16<__half, __half2>; };
+template <>
+struct RangeOf<__nv_bfloat16> { using type = Range16<__nv_bfloat16, __nv_bfloat162>; };
+
+// The groups of four tokens, 8 lanes and 64 dims each: a lane gets the range of token lane & 3 (each exchange halves the
+// tokens that a lane goes on with), and from it that token's scale and minimum.  *inside: no quotient passes the codes'
+// ends by as much as half a step (they do only where z's own rounding is worth that).
+template <typename T>
+__device__ __forceinline__ __half2 scale_of(const Raw8<T>* raw, int lane, bool* inside) {
+  using R = typename RangeOf<T>::type;
+  const R c0(raw[0]), c1(raw[1]), c2(raw[2]), c3(raw[3]);
+  const bool odd = lane & 1, upper = lane & 2;
+  R a = odd ? c1 : c0, b = odd ? c3 : c2;
+  a.join(odd ? c0 : c1, 1);
+  b.join(odd ? c2 : c3, 1);
+  R m = upper ? b : a;
+  m.join(upper ? a : b, 2);
+  m.join(m, 4);
+  const float2 range = m.both();
+  const float hi = range.x, lo = -range.y;
   const __half z = __float2half_rn(fminf(fmaxf(lo, -65504.f), 65504.f));
   const float zf = __half2float(z);
   const __half s = __float2half_rn(fminf(fmaxf(quotient(hi - zf, 15.f, 1.f / 15.f), 0.f), 65504.f));
   const float sf = __half2float(s);
+  if (!(fabsf(lo) < INFINITY && fabsf(hi) < INFINITY)) {  // a NaN or an infinity poisons its group
+    *inside = true;
+    return __halves2half2(__ushort_as_half(0x7fff), __ushort_as_half(0));
+  }
+  *inside = !(sf > 0.f) || (lo - zf > -0.49f * sf && hi - zf < 15.49f * sf);
+  return __halves2half2(s, z);
+}
+
+// The codes of the lane's 8 values, one to a nibble; zeros where the scale is none.
+template <typename T>
+__device__ __forceinline__ uint32_t codes_of(const Raw8<T>& raw, __half2 sz, bool inside) {
+  float x[8];
+  raw.to(x);
+  const float2 f = __half22float2(sz);
+  const float sf = f.x, zf = f.y;
   float r;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(sf));
-  // Rounded to an integer by adding 1.5 2^23: the low bits of the sum (ties to even, as rint).  Quotients pass the ends
-  // only where z's own rounding is worth half a step.
-  const bool inside = (lo - zf) * r > -0.49f && (hi - zf) * r < 15.49f;
+  // Rounded to an integer by adding 1.5 2^23: the low bits of the sum (ties to even, as rint).
   uint32_t w = 0;
-  if (__all_sync(0xffffffffu, inside)) {
+  if (inside) {
     const f2_t nz = f2_pack(-zf, -zf), ns = f2_pack(-sf, -sf), r2 = f2_pack(r, r), magic = f2_pack(12582912.f, 12582912.f);
     const f2_t less = f2_pack(-12582912.f, -12582912.f), up = f2_pack(256.f, 256.f);
     f2_t c[4];
@@ -156,8 +187,7 @@ __device__ __forceinline__ __half2 quantise(const Raw8<T>& raw, uint32_t* codes)
       w |= (__float_as_uint(c + 12582912.f) & 15u) << (4 * i);
     }
   }
-  *codes = sf > 0.f && !bad ? w : 0u;
-  return bad ? __halves2half2(__ushort_as_half(0x7fff), __ushort_as_half(0)) : __halves2half2(s, z);
+  return sf > 0.f ? w : 0u;
 }
 
 // Nibbles of word t of a run (token 8 b + 2 t + i at nibble b + 4 i) that are tokens [lo, hi).
@@ -201,7 +231,7 @@ __global__ void __launch_bounds__(kPqThreads) append_kernel(const __grid_constan
   const long long stride = u.side ? p.vs : p.ks;
   src += u.head * D + at.d0;
   uint32_t acc[L::kT][4] = {};  // [t]: a byte for each even (odd) dim, nibbles b = 0, 1; the same of b = 2, 3
-  constexpr int kStep = 4;      // steps whose loads are in flight together: 8 (16) tokens
+  constexpr int kStep = 4;      // steps whose loads are in flight together, and whose scales are found together
   Raw8<T> next[kStep];
   const auto fetch = [&](int j0) {
 #pragma unroll
@@ -225,12 +255,15 @@ __global__ void __launch_bounds__(kPqThreads) append_kernel(const __grid_constan
 #pragma unroll
     for (int j = 0; j < kStep; ++j) now[j] = next[j];
     if ((j0 + kStep) * L::kTokens < u.hi) fetch(j0 + kStep);  // (on their way while these are worked on)
+    bool inside;
+    const __half2 scales = scale_of(now, lane, &inside);
+    inside = __all_sync(0xffffffffu, inside);
 #pragma unroll
     for (int j = 0; j < kStep; ++j) {
       const int tok0 = (j0 + j) * L::kTokens, tok = tok0 + at.sub;
       if (tok0 + L::kTokens <= u.lo || tok0 >= u.hi) continue;  // (the same for the whole warp)
-      uint32_t w;
-      const __half2 sz = quantise(now[j], &w);
+      const __half2 sz = __shfl_sync(0xffffffffu, scales, (lane & 24) | j);
+      const uint32_t w = codes_of(now[j], sz, inside);
       if (tok < u.lo || tok >= u.hi) continue;
       if (at.d0 % kPgGroup == 0) params[tok * B::kGroups] = sz;
       if (u.side) {

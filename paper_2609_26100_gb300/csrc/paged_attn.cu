@@ -7,9 +7,10 @@
 // number c 2^-24 (c 2^-20 four bits further up), so a 32-bit word becomes four operand registers with four
 // ANDs and a shift, exactly; the factor 16 of every second pair is taken out of the other operand.  Scales
 // and minima join in fp32: s_t multiplies the sum over a group's dims, z_t the sum of the query's; on the
-// value side s'_t goes into the weight, which enters as two fp16 parts (hi and the rest, 22 bits: one part
-// alone costs the output 4e-4 of its size, twice what rounding it to fp16 does; a quarter of what rounding to bf16
-// does, so blocks of more than 8 rows with bf16 outputs take one part), and z'_t is summed by itself.  Queries are scaled by a power of two to fill fp16's range, so they are exact too.
+// value side s'_t goes into the weight, which enters as two fp16 parts (hi and the rest, 22 bits: one part alone costs
+// the output 4e-4 of its size, twice what rounding it to fp16 does; a quarter of what rounding to bf16 does, so blocks of
+// more than 8 rows with bf16 outputs take one part), and z'_t is summed by itself.  Queries are scaled by a power of two
+// to fill fp16's range, so they are exact too.
 //
 // Tokens take the MMA's 16-row side (S^T = K Q^T, O^T = V^T P^T): a block of 8 query rows (N) fills it,
 // where the usual orientation would pad 1 .. 8 rows to 16.  P^T's operand layout is the transpose of S^T's
@@ -429,9 +430,9 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
                 const uint32_t hi = pack_f16(p0, p1);
                 pf[nt][gi][0][k] = movmatrix_t(hi);
                 if constexpr (TWO) {
-                const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&hi));
-                const float2 rest = fma2(back, make_float2(-1.f, -1.f), make_float2(p0, p1));
-                pf[nt][gi][kParts - 1][k] = movmatrix_t(pack_f16(rest.x, rest.y));
+                  const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+                  const float2 rest = fma2(back, make_float2(-1.f, -1.f), make_float2(p0, p1));
+                  pf[nt][gi][kParts - 1][k] = movmatrix_t(pack_f16(rest.x, rest.y));
                 }
               }
             }
@@ -517,7 +518,8 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
         if (!s_has[wi]) continue;
         const float2 x = s_ml[wi][row];
         const float fw = ex2(x.x - mb);
-        const float4 y = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(pa_dyn + (wi * ST + s_has[wi] - 1) * B::kBytes) + row * D + ((c4 ^ (2 * ((row >> 1) & 3))) << 2));
+        const float* buf = reinterpret_cast<const float*>(pa_dyn + (wi * ST + s_has[wi] - 1) * B::kBytes);
+        const float4 y = *reinterpret_cast<const float4*>(buf + row * D + ((c4 ^ (2 * ((row >> 1) & 3))) << 2));
         L = fmaf(fw, x.y, L);
         sum->x = fmaf(fw, y.x, sum->x);
         sum->y = fmaf(fw, y.y, sum->y);
@@ -667,7 +669,8 @@ cudaError_t launch_paged_attention(tss_paged* h, const PgAttnArgs& a, const PgBa
     }
     const auto run = [&](auto dim) {
       constexpr int D = decltype(dim)::value;
-      return R == 8 ? pa_launch<D, 1, true>(narrow, h->sms, s) : a.is_half ? pa_launch<D, 2, true>(narrow, h->sms, s) : pa_launch<D, 2, false>(narrow, h->sms, s);
+      if (R == 8) return pa_launch<D, 1, true>(narrow, h->sms, s);
+      return a.is_half ? pa_launch<D, 2, true>(narrow, h->sms, s) : pa_launch<D, 2, false>(narrow, h->sms, s);
     };
     const cudaError_t e = h->d == 64 ? run(std::integral_constant<int, 64>{}) : run(std::integral_constant<int, 128>{});
     if (e != cudaSuccess) return e;

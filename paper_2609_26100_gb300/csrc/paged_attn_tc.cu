@@ -47,7 +47,8 @@ constexpr uint32_t kPtO = 384;
 
 struct __align__(16) PtShared {
   float par[4][kPtParams][kPtKeys];                   // keys in the order 16 q + 4 x + 2 b + e for 16 q + 8 b + 2 x + e
-  uint64_t raw_full[kPtRaw], raw_free[kPtRaw], k_full[2], k_free[2], v_full[2], v_free[2], s_full[3], p_full[3], o_done[2], par_full[4], q_full, o_full, drain;
+  uint64_t raw_full[kPtRaw], raw_free[kPtRaw], k_full[2], k_free[2], v_full[2], v_free[2], par_full[4];
+  uint64_t s_full[3], p_full[3], o_done[2], q_full, o_full, drain;
   uint32_t tmem;
   int abort, last, bad[kPtRaw], bad_par[4];
   float4 row[kPtRows];                                // factor of the codes' sums, then of the minima of groups 0 and 1
@@ -56,7 +57,8 @@ struct __align__(16) PtShared {
   float top[4][kPtRows];                              // maxima of its quarters
   float part[4][3][kPtRows];                          // the quarters' sums: p, p z'_0, p z'_1
 };
-static_assert(offsetof(PtShared, par) % 16 == 0 && offsetof(PtShared, row) % 16 == 0 && offsetof(PtShared, raw_full) % 8 == 0, "alignment of vectors and barriers");
+static_assert(offsetof(PtShared, par) % 16 == 0 && offsetof(PtShared, row) % 16 == 0 && offsetof(PtShared, raw_full) % 8 == 0,
+              "alignment of vectors and barriers");
 constexpr size_t kPtSmem = 1024 + 2 * kPtQ + 2 * 4 * kPtOp + kPtJoin * kPtRows * 4 + kPtRaw * PtBlock::kBytes;
 
 __host__ __device__ constexpr uint32_t idesc_f16_m128(int n) {
@@ -377,7 +379,8 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
       // Parameters, in a buffer of four: page t - 4's are read out, since S(t - 2), which is complete, was issued after
       // P V of page t - 4.
       if (x < kPtKeys) {
-        const uint2 kp = *reinterpret_cast<const uint2*>(blk + PtBlock::kKParams + 8 * x), vp = *reinterpret_cast<const uint2*>(blk + PtBlock::kVParams + 8 * x);
+        const uint2 kp = *reinterpret_cast<const uint2*>(blk + PtBlock::kKParams + 8 * x);
+        const uint2 vp = *reinterpret_cast<const uint2*>(blk + PtBlock::kVParams + 8 * x);
         const auto pair = [](uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); };
         const float2 k0 = pair(kp.x), k1 = pair(kp.y), v0 = pair(vp.x), v1 = pair(vp.y);
         const int at = (x & 48) | (x & 6) << 1 | (x & 8) >> 2 | (x & 1);
