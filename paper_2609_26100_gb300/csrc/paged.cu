@@ -2,13 +2,16 @@
 //
 // Quantisation, per token and 64 dims:  z = fp16(min), s = fp16((max - z) / 15), c = rint((x - z) / s).
 // A warp takes one (request, 32-token half page, KV head, K or V).  A lane holds 8 neighbouring dims, a
-// token D / 8 lanes, so a warp's load brings two (four) whole tokens and a group's minimum and maximum
-// are a butterfly over 8 lanes.  A lane's K codes of a token are one 32-bit word.  A word of V codes is 8
-// tokens of a dim: a lane gathers those of even or of odd tokens, 16 bits of each word, and swaps half of
-// them with the lane of the same dims at the other parity.  All words of a half page lie in one warp, so
-// tokens that the call does not bring keep their nibbles and no two warps write one word.
+// token D / 8 lanes, so a warp's load brings two (four) whole tokens.  Of four loads at a time the 8 lanes of a group
+// exchange ranges so that each ends up with one token's, finds its scale and hands it round (one lane's
+// work instead of eight's: 50 us instead of 58 for 7171 rows of 40 heads).  A lane's K codes of a token are one
+// 32-bit word.  A word of V codes is 8 tokens of a dim: a lane gathers those of even or of odd tokens, 16 bits
+// of each word, and swaps half of them with the lane of the same dims at the other parity.  All words of a half
+// page lie in one warp, so tokens that the call does not bring keep their nibbles and no two warps write one word.
 //
-// Bound: HBM for prompts (a token's 2 bytes a value in, half a byte out), latency for a step's few rows.
+// Bound: appending prompts, instruction issue (73 % of the slots, about 20 instructions a value): 7171 rows of 40 heads of
+// 128, bf16, 50 us, 3.8 TB/s of rows read and codes written.  Reading them back, HBM: 36 us, 5.2 TB/s.  A step's 16 rows:
+// 4.4 us, launch and latency.
 #include "paged.h"
 
 namespace tss {

@@ -8,7 +8,9 @@
 // the row.  The mean of squares is a butterfly over the head's lanes (8 at head_dim 128, four heads to a
 // warp).
 //
-// Bound: HBM, each element read and written once.
+// Bound: HBM, each element read and written once: 4096 rows of 64 heads of 128, bf16, with norms 26 us, 5.1 TB/s.  A step of
+// 6 rows 2.3 us: launch and two dependent loads (position, table).  The next head's vectors are held as they come: widened
+// to fp32 while in flight they cost registers and 38 us.
 #include "ops.cuh"
 
 namespace tss {

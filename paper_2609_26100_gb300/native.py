@@ -256,9 +256,9 @@ def dtype_code(t) -> int:
 
 
 def _rows(t, what: str):
-    """(rows, heads, head_dim, row stride) of a tensor [rows][heads][head_dim] whose heads are contiguous."""
-    if t.dim() != 3:
-        raise ValueError(f"{what}: [rows][heads][head_dim] is wanted")
+    """(rows, heads, head_dim, row stride) of a GPU tensor [rows][heads][head_dim] whose heads are contiguous."""
+    if t.dim() != 3 or not t.is_cuda:
+        raise ValueError(f"{what}: [rows][heads][head_dim] on the GPU is wanted")
     n, h, d = t.shape
     if n and h and (t.stride(2) != 1 or (h > 1 and t.stride(1) != d)):
         raise ValueError(f"{what}: the heads of a row must be contiguous")
@@ -280,12 +280,13 @@ def rope_frequencies(rot_dim: int, theta: float = 10000.0, kind: str = "none", f
 
 
 def rope_table(inv_freq: Sequence[float], table, attention_factor: float = 1.0, stream=None) -> None:
-    """tss_rope_table into the float32 device tensor table [positions][len(inv_freq)][2]."""
+    """tss_rope_table into the float32 device tensor table [positions][len(inv_freq)][2], on the given stream (None:
+    torch's current one)."""
     n = len(inv_freq)
-    if tuple(table.shape[1:]) != (n, 2) or dtype_code(table) != TSS_DTYPE_F32 or not table.is_contiguous():
-        raise ValueError("table: contiguous float32 [positions][pairs][2] is wanted")
-    check(lib().tss_rope_table((ctypes.c_double * n)(*inv_freq), n, attention_factor, table.shape[0], table.data_ptr(), stream),
-          "tss_rope_table")
+    if tuple(table.shape[1:]) != (n, 2) or dtype_code(table) != TSS_DTYPE_F32 or not table.is_contiguous() or not table.is_cuda:
+        raise ValueError("table: contiguous float32 [positions][pairs][2] on the GPU is wanted")
+    check(lib().tss_rope_table((ctypes.c_double * n)(*inv_freq), n, attention_factor, table.shape[0], table.data_ptr(),
+                               current_stream() if stream is None else stream), "tss_rope_table")
 
 
 def rope_args(q, k, q_out, k_out, positions, table, q_gain=None, k_gain=None, eps: float = 1e-6, interleaved: bool = False,
@@ -312,16 +313,20 @@ def rope_args(q, k, q_out, k_out, positions, table, q_gain=None, k_gain=None, ep
         setattr(a, name + "_out", y.data_ptr())
         setattr(a, name + "_out_stride", _rows(y, name + "_out")[3])
         if gain is not None:
-            if tuple(gain.shape) != (d,) or gain.dtype != x.dtype or not gain.is_contiguous():
-                raise ValueError(f"{name}_gain: contiguous [head_dim] of the same type is wanted")
+            if tuple(gain.shape) != (d,) or gain.dtype != x.dtype or gain.device != x.device or not gain.is_contiguous():
+                raise ValueError(f"{name}_gain: contiguous [head_dim] of the same type and device is wanted")
             setattr(a, name + "_gain", gain.data_ptr())
     if table is not None:
-        if table.dim() != 3 or table.shape[2] != 2 or dtype_code(table) != TSS_DTYPE_F32 or not table.is_contiguous():
-            raise ValueError("table: contiguous float32 [positions][pairs][2] is wanted")
-        if str(positions.dtype) != "torch.int32" or positions.numel() != a.n_rows or not positions.is_contiguous():
-            raise ValueError("positions: contiguous int32 [rows] is wanted")
+        if (table.dim() != 3 or table.shape[2] != 2 or dtype_code(table) != TSS_DTYPE_F32 or not table.is_contiguous()
+                or not table.is_cuda):
+            raise ValueError("table: contiguous float32 [positions][pairs][2] on the GPU is wanted")
+        if (str(positions.dtype) != "torch.int32" or positions.numel() != a.n_rows or not positions.is_contiguous()
+                or not positions.is_cuda):
+            raise ValueError("positions: contiguous int32 [rows] on the GPU is wanted")
         a.table, a.max_positions, a.rot_dim = table.data_ptr(), table.shape[0], 2 * table.shape[1]
         a.positions = positions.data_ptr()
+    if status is not None and (str(status.dtype) != "torch.int32" or not status.is_cuda):
+        raise ValueError("status: an int32 tensor on the GPU is wanted")
     a.status = _ptr(status)
     a._keep = (q, k, q_out, k_out, positions, table, q_gain, k_gain, status)
     return a

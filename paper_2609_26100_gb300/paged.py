@@ -33,9 +33,9 @@ def pages_for(tokens: int) -> int:
 
 
 def _row_stride(t: torch.Tensor, shape, what: str) -> int:
-    """Elements between the rows of t, which has the given shape and contiguous heads."""
-    if t.shape != shape:
-        raise ValueError(f"{what}: {list(shape)} is wanted")
+    """Elements between the rows of t, a GPU tensor which has the given shape and contiguous heads."""
+    if t.shape != shape or not t.is_cuda:
+        raise ValueError(f"{what}: {list(shape)} on the GPU is wanted")
     row, head, one = t.stride()
     n, h, d = shape
     if n == 0:
@@ -58,14 +58,14 @@ def _host(values) -> array:
 
 
 def _ints(t: torch.Tensor, shape, what: str) -> None:
-    if t.shape != shape or t.dtype != torch.int32 or not t.is_contiguous():
-        raise ValueError(f"{what}: contiguous int32 {list(shape)} is wanted")
+    if t.shape != shape or t.dtype != torch.int32 or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError(f"{what}: contiguous int32 {list(shape)} on the GPU is wanted")
 
 
 def _layers(pool: torch.Tensor):
     """(array of each layer's address, layers, pages, bytes of a page) of a tensor [layers][pages][...]."""
-    if pool.dim() < 3 or not pool.is_contiguous():
-        raise ValueError("pool: contiguous [layers][pages][...] is wanted")
+    if pool.dim() < 3 or not pool.is_contiguous() or not pool.is_cuda:
+        raise ValueError("pool: contiguous [layers][pages][...] on the GPU is wanted")
     n, step = pool.shape[0], pool.stride(0) * pool.element_size()
     ptrs = (_P * n)(*[pool.data_ptr() + i * step for i in range(n)])
     return ptrs, n, pool.shape[1], pool.stride(1) * pool.element_size()
@@ -243,10 +243,11 @@ class Kv4Cache:
         n, h, d = shape = (batch.rows, self.n_q_heads, self.head_dim)
         if out.dtype != q.dtype or out.device != q.device:
             raise ValueError("out: the type and device of q are wanted")
-        if lse is not None and (lse.shape != (n, h) or lse.dtype != torch.float32 or not lse.is_contiguous()):
-            raise ValueError("lse: contiguous float32 [rows][heads] is wanted")
-        if mask is not None and (mask.shape != (n, 2) or mask.dtype not in (torch.int64, torch.uint64) or not mask.is_contiguous()):
-            raise ValueError("mask: contiguous 64-bit [rows][2] is wanted")
+        if lse is not None and (lse.shape != (n, h) or lse.dtype != torch.float32 or not lse.is_contiguous() or not lse.is_cuda):
+            raise ValueError("lse: contiguous float32 [rows][heads] on the GPU is wanted")
+        if mask is not None and (mask.shape != (n, 2) or mask.dtype not in (torch.int64, torch.uint64) or not mask.is_contiguous()
+                                 or not mask.is_cuda):
+            raise ValueError("mask: contiguous 64-bit [rows][2] on the GPU is wanted")
         if positions is not None:
             _ints(positions, (n,), "positions")
         a = native.TssPagedAttn(q.data_ptr(), _row_stride(q, shape, "q"), out.data_ptr(), _row_stride(out, shape, "out"),
