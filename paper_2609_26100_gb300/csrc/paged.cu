@@ -9,7 +9,7 @@
 // of each word, and swaps half of them with the lane of the same dims at the other parity.  All words of a half
 // page lie in one warp, so tokens that the call does not bring keep their nibbles and no two warps write one word.
 //
-// Bound: appending prompts, instruction issue (73 % of the slots, about 20 instructions a value): 7171 rows of 40 heads of
+// Bound: appending prompts, instruction issue (69 % of the slots, 17 instructions a value): 7171 rows of 40 heads of
 // 128, bf16, 50 us, 3.8 TB/s of rows read and codes written.  Reading them back, HBM: 36 us, 5.2 TB/s.  A step's 16 rows:
 // 4.4 us, launch and latency.
 #include "paged.h"
