@@ -12,7 +12,7 @@
 // Roles (640 threads): warp 0 copies pages (one bulk copy each), warp 1 issues MMAs, warps 2-3 expand codes
 // and parameters, warps 4-19 are the softmax.  Scores lie in three buffers of TMEM, read as blocks of 16 rows and 8
 // columns: a thread has 4 rows and 4 of a page's keys (in the shape of a row a thread each thread reads the parameters,
-// nine floats a key, of 16 keys: four times the shared-memory traffic, 81 us where this takes 75).  The weights go back
+// nine floats a key, of 16 keys: four times the shared-memory traffic, 81 us where this took 75).  The weights go back
 // to TMEM, over the scores that they come from, as the second product's first operand.  Operands of K and V are
 // double-buffered, so a page's expansion and scores run under the softmax of the pages before it.  Runs of pages as in
 // paged_attn.cu, one CTA an SM; partials of shared items are joined by the last CTA in CTA order.
@@ -20,9 +20,10 @@
 //
 // Bound: the latency of a page's way through a softmax warp: load of the scores, 16 scores a thread, the quadrant's vote on
 // its references, exponentials, store of the weights.  1.1 us a page with 32 rows in use, 1.4 us with 128; the MMAs take
-// 0.3 us of it.  About 15 us more a launch: first page, masked pages, end of an item, join.  128 rows, 32 heads, four requests
-// of 4600 tokens 127 us; 4 requests of 2048 .. 8000 tokens, 61 rows, 32 / 8 heads 75 us.
-// Built and slower at the latter size: 8 softmax warps of half a page each (83 us), or of every second page (105); a vote
+// 0.3 us of it.  About 12 us more a launch: first page, masked pages, end of an item, join.  128 rows, 32 heads, four requests
+// of 4600 tokens 122 us; 4 requests of 2048 .. 8000 tokens, 61 rows, 32 / 8 heads 70 us.  Outputs written by the threads of
+// their rows, 8 bytes a lane, had cost 5 us an item.
+// Built and slower at the latter size (when this took 75 us): 8 softmax warps of half a page each (83 us), or of every second page (105); a vote
 // by a barrier that warps wait for only after their exponentials (78); K and V expanded by warps of their own into
 // three buffers (85).
 #include <cstddef>
@@ -41,6 +42,7 @@ using PtBlock = PgBlock<kPtD>;
 constexpr int kPtQ = kPtRows * 64 * 2;            // one group of Q: 128 rows of 128 bytes
 constexpr int kPtOp = kPtKeys * 64 * 2;           // one group of C or C': 64 rows of 128 bytes
 constexpr int kPtJoin = 128;                      // partials whose weights the joining of an item keeps beside Q's memory
+static_assert(kPtJoin * kPtRows == kPtRows * kPtD, "the outputs of an item pass through the same memory");
 constexpr int kPtParams = 9;                      // arrays of 64: s0 s1 z0 z1 of K, the same of V, log2 of V's larger scale
 constexpr uint32_t kPtTmem = 512;                 // S: 3 buffers x 2 groups x 64 columns; O: 128 from column kPtO
 constexpr uint32_t kPtO = 384;
@@ -53,7 +55,9 @@ struct __align__(16) PtShared {
   int abort, last, bad[kPtRaw], bad_par[4];
   float4 row[kPtRows];                                // factor of the codes' sums, then of the minima of groups 0 and 1
   unsigned long long anc[2][kPtRows];                 // the rows of its block that a row sees
+  long long out_at[kPtRows];                          // where its output begins
   int qp[kPtRows];                                    // its position
+  float inv[kPtRows];                                 // 1 / sum of its weights
   float top[4][kPtRows];                              // maxima of its quarters
   float part[4][3][kPtRows];                          // the quarters' sums: p, p z'_0, p z'_1
 };
@@ -230,7 +234,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
   const uint32_t skew = (1024 - (smem_u32(pt_dyn) & 1023)) & 1023;
   uint8_t* sq = pt_dyn + skew;        // Q: group 0, group 1
   uint8_t* skv = sq + 2 * kPtQ;       // [buffer] C_0, C_1, C'_0, C'_1
-  uint8_t* sj = skv + 2 * 4 * kPtOp;  // weights of partials
+  uint8_t* sj = skv + 2 * 4 * kPtOp;  // weights of partials; outputs on their way
   uint8_t* raw = sj + kPtJoin * kPtRows * 4;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const PgAttnArgs& a = p.a;
@@ -752,27 +756,49 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
           L += sh.part[i][0][row];
           z += sh.part[i][1 + half][row];
         }
-        const long long slot = (blockIdx.x * 2 + (x0 == 0 ? 1 : 0)) * static_cast<long long>(kPtRows) + row;
+        const long long slot = (blockIdx.x * 2 + (x0 == 0 ? 1 : 0)) * static_cast<long long>(kPtRows);
+        if (qt == 0 && valid) {
+          const int q = row0 + row, head = h * gq + q % gq;
+          const long long tok = r.row + q / gq;
+          sh.out_at[row] = tok * a.os + static_cast<long long>(head) * kPtD;
+          sh.inv[row] = L > 0.f ? 1.f / L : L == 0.f ? 0.f : L;  // (a NaN stays one)
+          if (!whole)
+            __stcg(p.part_ml + slot + row, make_float2(my_ref, L));
+          else if (a.lse)
+            a.lse[tok * a.hq + head] = (my_ref + log2f(L)) * 0.6931471805599453f;
+        }
+        // through shared memory (16-byte chunks permuted by row), so that a warp's store is a row
+        float4* rows_of = reinterpret_cast<float4*>(sj) + qd * 32 * (kPtD / 4);
 #pragma unroll 1
         for (int c = 0; c < 2; ++c) {
           float o[16];
           __syncwarp();
           tmem_ld16(tm + lanes + kPtO + qt * 32 + c * 16, o);
-          if (!valid) continue;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float4 x = make_float4(fmaf(o[4 * i], 16777216.f, z), fmaf(o[4 * i + 1], 16777216.f, z), fmaf(o[4 * i + 2], 16777216.f, z),
-                                         fmaf(o[4 * i + 3], 16777216.f, z));
-            const int c4 = qt * 8 + c * 4 + i;
-            if (whole)
-              finish_row<kPtD>(a, r, h, row0 + row, c4, my_ref, L, x);
+          for (int i = 0; i < 4; ++i)
+            rows_of[lane * (kPtD / 4) + ((qt * 8 + c * 4 + i) ^ lane)] =
+                make_float4(fmaf(o[4 * i], 16777216.f, z), fmaf(o[4 * i + 1], 16777216.f, z), fmaf(o[4 * i + 2], 16777216.f, z),
+                            fmaf(o[4 * i + 3], 16777216.f, z));
+        }
+        tc_fence_before();
+        named_bar_sync(quad, 128);
+#pragma unroll 4
+        for (int i = 0; i < 8; ++i) {
+          const int ql = qt * 8 + i, q = qd * 32 + ql;
+          if (q >= rows) break;
+          const float4 x = rows_of[ql * (kPtD / 4) + (lane ^ ql)];
+          if (whole) {
+            const float inv = sh.inv[q];
+            const float y[4] = {x.x * inv, x.y * inv, x.z * inv, x.w * inv};
+            const long long to = sh.out_at[q] + 4 * lane;
+            if (a.is_half)
+              store_vec<__half, 4>(static_cast<__half*>(a.out) + to, y);
             else
-              __stcg(reinterpret_cast<float4*>(p.part_o + slot * kPtD) + c4, x);
+              store_vec<__nv_bfloat16, 4>(static_cast<__nv_bfloat16*>(a.out) + to, y);
+          } else {
+            __stcg(reinterpret_cast<float4*>(p.part_o + (slot + q) * kPtD) + lane, x);
           }
         }
-        if (!whole && valid && qt == 0) __stcg(p.part_ml + slot, make_float2(my_ref, L));
-        __syncwarp();
-        tc_fence_before();
       }
       named_bar_sync(5, kPtSoft);
       if (!whole) {
