@@ -158,8 +158,10 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
     }
     ++issued;
   };
+  // All stages but one: the last is asked for at the first unit, so that first pages and Q do not queue behind second ones
+  // (eight requests of 4000 tokens, 32 heads, 44.8 -> 43.3 us).
 #pragma unroll
-  for (int i = 0; i < ST; ++i) issue();
+  for (int i = 0; i < ST - 1; ++i) issue();
 
   int done = 0, stage = 0;  // the warp's units so far, the stage of the next
   uint32_t parity = 0;
@@ -247,7 +249,7 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
     const int all2 = r.sink + r.first / unit - r.lo;
     const int done0 = done;
     for (int x = u0 + warp + done * W - u + x0; x < x1; x += W) {
-      if (done > 0) issue();  // into the stage of the unit before (every lane has read it: the last loop's end)
+      issue();  // into the stage of the unit before, if any (every lane has read it: the last loop's end)
       const int s = stage;
       if (!__all_sync(0xffffffffu, mbar_try_wait(&bars[warp][s], parity))) {
         ok = __all_sync(0xffffffffu, ok && mbar_wait(&bars[warp][s], parity, abort, a.status));
