@@ -71,8 +71,8 @@ __device__ __forceinline__ bool sees(const PgAttnArgs& a, const PaReq& r, int i,
   int kp = j;
   if (j >= r.first) {
     const int x = j - r.first;
-    if (anc ? !(__ldg(anc + (x >> 6)) >> (x & 63) & 1ull) : x > i) return false;
-    if (a.positions) kp = max(__ldg(a.positions + r.row + x), r.first);
+    if (anc ? !(__ldcg(anc + (x >> 6)) >> (x & 63) & 1ull) : x > i) return false;
+    if (a.positions) kp = max(__ldcg(a.positions + r.row + x), r.first);
   }
   return !a.window || qp - kp < a.window || j < a.sinks;
 }
@@ -102,7 +102,9 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
   int u0, u1, first_cta, splits;
   cta_run(p, &u0, &u1, &first_cta, &splits);
   __syncthreads();
-  griddep_wait();    // (nothing before this reads or writes what another kernel may)
+  // Nothing before this reads or writes what another kernel may; tables, masks and positions are not read through the
+  // read-only path, since the kernel that writes them may still run while this one begins.
+  griddep_wait();
   griddep_launch();
   volatile int* abort = &abort_s;
 
@@ -122,7 +124,7 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
     const int item = v / r.units, x = v - item * r.units;
     const int h = item % a.hk, at = x < r.sink ? x : x - r.sink + r.lo;
     const int half = halves == 1 ? at & 1 : 0;
-    const int page = __ldg(a.table + static_cast<long long>(r.seq) * a.max_pages + (halves == 1 ? at >> 1 : at));
+    const int page = __ldcg(a.table + static_cast<long long>(r.seq) * a.max_pages + (halves == 1 ? at >> 1 : at));
     if (page < 0 || page >= a.n_pages) {
       report(a.status, kStatusCheck);
       return -1;
@@ -238,7 +240,7 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
     if (a.window) {  // the last position among the tile's rows
       if (lane < rows) {
         const int i = (row0 + lane) / gq;
-        pmax = a.positions ? max(__ldg(a.positions + r.row + i), r.first) : r.first + i;
+        pmax = a.positions ? max(__ldcg(a.positions + r.row + i), r.first) : r.first + i;
       }
 #pragma unroll
       for (int x2 = 16; x2 > 0; x2 >>= 1) pmax = max(pmax, __shfl_xor_sync(0xffffffffu, pmax, x2));
@@ -349,7 +351,7 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
                 if (q >= rows) continue;
                 const int ti = (row0 + q) / gq;
                 const unsigned long long* anc = a.mask ? a.mask + 2LL * (r.row + ti) : nullptr;
-                const int qp = a.positions ? max(__ldg(a.positions + r.row + ti), r.first) : r.first + ti;
+                const int qp = a.positions ? max(__ldcg(a.positions + r.row + ti), r.first) : r.first + ti;
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
                   if (sees(a, r, ti, qp, anc, kb + k * 8 + g)) vis |= 1u << (nt * 8 + k * 2 + i);

@@ -153,7 +153,7 @@ __device__ __forceinline__ unsigned long long row_sees(const PgAttnArgs& a, cons
       near &= ~blk;
       for (unsigned long long x = v & blk; x; x &= x - 1) {
         const int i = __ffsll(static_cast<long long>(x)) - 1;
-        if (qp - max(__ldg(a.positions + r.row + key0 + i - r.first), r.first) < a.window) near |= 1ull << i;
+        if (qp - max(__ldcg(a.positions + r.row + key0 + i - r.first), r.first) < a.window) near |= 1ull << i;
       }
     }
     v &= near | (sinks >= 64 ? ~0ull : sinks <= 0 ? 0ull : (1ull << sinks) - 1);
@@ -292,7 +292,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
         const int u = u0 + t0 + lane;
         const PaReq& r = p.r[request_of(u)];
         const int v = u - r.off, item = v / r.units, x = v - item * r.units, at = x < r.sink ? x : x - r.sink + r.lo;
-        const int page = __ldg(a.table + static_cast<long long>(r.seq) * a.max_pages + at);
+        const int page = __ldcg(a.table + static_cast<long long>(r.seq) * a.max_pages + at);
         if (page >= 0 && page < a.n_pages)
           blk = static_cast<long long>(page) * a.hk + item % a.hk;
         else
@@ -503,10 +503,10 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
       unsigned long long anc_lo = ~0ull, anc_hi = ~0ull;
       if (valid) {
         const int ti = (row0 + row) / gq;
-        qp = a.positions ? max(__ldg(a.positions + r.row + ti), r.first) : r.first + ti;
+        qp = a.positions ? max(__ldcg(a.positions + r.row + ti), r.first) : r.first + ti;
         if (a.mask) {
-          anc_lo = __ldg(a.mask + 2LL * (r.row + ti));
-          anc_hi = __ldg(a.mask + 2LL * (r.row + ti) + 1);
+          anc_lo = __ldcg(a.mask + 2LL * (r.row + ti));
+          anc_hi = __ldcg(a.mask + 2LL * (r.row + ti) + 1);
         } else {
           anc_lo = ti >= 63 ? ~0ull : (2ull << ti) - 1;
           anc_hi = ti < 64 ? 0ull : ti == 127 ? ~0ull : (2ull << (ti - 64)) - 1;
