@@ -88,6 +88,7 @@ class PagePool:
         self._tables = native.TssPageTables(table.data_ptr(), held.data_ptr(), refs.data_ptr())
         self._ref = ctypes.byref(self._tables)
         h = _P()
+        self._c_free, self._c_fork = lib().tss_pages_free, lib().tss_pages_fork
         check(lib().tss_pages_create(self.n_seqs, self.max_pages, self.n_pages, ctypes.byref(h)), "tss_pages_create")
         self._h = h
 
@@ -120,8 +121,10 @@ class PagePool:
         a, keep = _host(seqs), None
         if tokens is not None:
             keep = _host([-(-t // PAGE_TOKENS) for t in tokens])
-        check(lib().tss_pages_free(self._h, self._ref, len(a), a.buffer_info()[0], None if keep is None else keep.buffer_info()[0],
-                                   self._stream(stream)), "tss_pages_free")
+        s = self._c_free(self._h, self._ref, len(a), a.buffer_info()[0], None if keep is None else keep.buffer_info()[0],
+                         current_stream() if stream is None else stream)
+        if s:
+            check(s, "tss_pages_free")
 
     def fork(self, src: Sequence[int], dst: Sequence[int], tokens: Sequence[int], stream=None) -> None:
         """dst[i] (which holds nothing) becomes the first tokens[i] tokens of src[i]: full pages are shared, a
@@ -129,11 +132,13 @@ class PagePool:
         n = len(src)
         if len(dst) != n or len(tokens) != n:
             raise ValueError("src, dst and tokens differ in length")
-        a, b = _host(src), _host(dst)
-        c, d = _host([t // PAGE_TOKENS for t in tokens]), _host([-(-t // PAGE_TOKENS) for t in tokens])
-        check(lib().tss_pages_fork(self._h, self._ref, self._ptrs, self.n_layers, self.page_bytes, n, a.buffer_info()[0],
-                                   b.buffer_info()[0], c.buffer_info()[0], d.buffer_info()[0], self._stream(stream)),
-              "tss_pages_fork")
+        # src, dst, pages to share and pages in all, in one array
+        a = _host((*src, *dst, *[t // PAGE_TOKENS for t in tokens], *[-(-t // PAGE_TOKENS) for t in tokens]))
+        at, step = a.buffer_info()[0], n * a.itemsize
+        s = self._c_fork(self._h, self._ref, self._ptrs, self.n_layers, self.page_bytes, n, at, at + step, at + 2 * step, at + 3 * step,
+                         current_stream() if stream is None else stream)
+        if s:
+            check(s, "tss_pages_fork")
 
     def compact(self, table_out: Optional[torch.Tensor] = None, refs_out: Optional[torch.Tensor] = None, stream=None) -> None:
         """Move the pages in use to the lowest ids; the new table and counts replace the pool's, or go to the
