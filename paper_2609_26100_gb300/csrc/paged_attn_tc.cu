@@ -23,9 +23,9 @@
 // 0.3 us of it.  About 12 us more a launch: first page, masked pages, end of an item, join.  128 rows, 32 heads, four requests
 // of 4600 tokens 122 us; 4 requests of 2048 .. 8000 tokens, 61 rows, 32 / 8 heads 70 us.  Outputs written by the threads of
 // their rows, 8 bytes a lane, had cost 5 us an item.
-// Built and slower at the latter size (when this took 75 us): 8 softmax warps of half a page each (83 us), or of every second page (105); a vote
-// by a barrier that warps wait for only after their exponentials (78); K and V expanded by warps of their own into
-// three buffers (85).
+// Built and slower at the latter size (when this took 75 us): 8 softmax warps of half a page each (83 us), or of every
+// second page (105); a vote by a barrier that warps wait for only after their exponentials (78); K and V expanded by
+// warps of their own into three buffers (85).
 #include <cstddef>
 #include <type_traits>
 
@@ -147,7 +147,8 @@ __device__ __forceinline__ unsigned long long row_sees(const PgAttnArgs& a, cons
     }
   }
   if (a.window) {
-    const int from = qp - a.window + 1 - key0, sinks = a.sinks - key0;
+    // (keys from qp on are near; no difference here leaves 32 bits, whatever the window)
+    const int from = max(qp - key0, 0) - (a.window - 1), sinks = a.sinks - key0;
     unsigned long long near = from <= 0 ? ~0ull : from >= 64 ? 0ull : ~0ull << from;
     if (a.positions && blk) {  // a row of the block stands at its own position
       near &= ~blk;
@@ -225,8 +226,7 @@ __device__ __forceinline__ void join_parts(const PaParams& p, PtShared& sh, uint
   }
 }
 
-// TWO: weights of two fp16 parts (fp16 outputs); else one (bf16 outputs: its 2^-12 is a fraction of their own 2^-9),
-// and then two buffers of them.
+// TWO: weights of two fp16 parts (fp16 outputs); else one (bf16 outputs: its 2^-12 is a fraction of their own 2^-9).
 template <bool TWO>
 __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __grid_constant__ PaParams p) {
   extern __shared__ uint8_t pt_dyn[];
