@@ -100,26 +100,31 @@ __device__ __forceinline__ void gather_partials(const PaParams& p, int R, int c0
     const int c = c0 + slice + k * step;
     return static_cast<long long>(c * 2 + (c == c0)) * R + row;
   };
-  float M = -INFINITY, L = 0.f;
-  for (int k = lane; k < mine; k += 32) M = fmaxf(M, __ldcg(p.part_ml + slot(k)).x);
+  float2 ml;
+  const auto fetch_ml = [&](int k) { ml = k < mine ? __ldcg(p.part_ml + slot(k)) : make_float2(-INFINITY, 0.f); };
+  float4 y[8];
+  const auto fetch = [&](int k) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      y[i] = k + i < mine && lane < D / 4 ? __ldcg(reinterpret_cast<const float4*>(p.part_o + slot(k + i) * D) + lane)
+                                          : make_float4(0.f, 0.f, 0.f, 0.f);
+  };
+  // (the first 32 references and the first 8 parts in flight together)
+  fetch_ml(lane);
+  fetch(0);
+  float M = ml.x, L = 0.f;
+  for (int k = lane + 32; k < mine; k += 32) M = fmaxf(M, __ldcg(p.part_ml + slot(k)).x);
 #pragma unroll
   for (int x = 16; x > 0; x >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, x));
   const float mb = M == -INFINITY ? 0.f : M;
   float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int k0 = 0; k0 < mine; k0 += 32) {
-    float fw = 0.f;
-    if (k0 + lane < mine) {
-      const float2 ml = __ldcg(p.part_ml + slot(k0 + lane));
-      fw = ex2(ml.x - mb);
-      L = fmaf(fw, ml.y, L);
-    }
+    if (k0 > 0) fetch_ml(k0 + lane);
+    const float fw = k0 + lane < mine ? ex2(ml.x - mb) : 0.f;
+    L = fmaf(fw, ml.y, L);
     const int m = min(32, mine - k0);
     for (int k = 0; k < m; k += 8) {
-      float4 y[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        y[i] = k + i < m && lane < D / 4 ? __ldcg(reinterpret_cast<const float4*>(p.part_o + slot(k0 + k + i) * D) + lane)
-                                         : make_float4(0.f, 0.f, 0.f, 0.f);
+      if (k0 + k > 0) fetch(k0 + k);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float x = __shfl_sync(0xffffffffu, fw, (k + i) & 31);
