@@ -102,10 +102,6 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
   int u0, u1, first_cta, splits;
   cta_run(p, &u0, &u1, &first_cta, &splits);
   __syncthreads();
-  // Nothing before this reads or writes what another kernel may; tables, masks and positions are not read through the
-  // read-only path, since the kernel that writes them may still run while this one begins.
-  griddep_wait();
-  griddep_launch();
   volatile int* abort = &abort_s;
 
   const int mine = u0 + warp < u1 ? (u1 - u0 - warp + W - 1) / W : 0;  // the warp's units: u0 + warp + k W
@@ -116,22 +112,33 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
       if (b + s < p.n_req && s_off[b + s] <= u) b += s;
     return b;
   };
-  // Lane l: half block of unit k0 + l in the pool; -1 where the table names no page, -2 past the end.
-  const auto blocks_from = [&](int k0) -> int {
-    if (k0 + lane >= mine) return -2;
+  // Lane l: entry of the table for unit k0 + l (-1 past the end), and its KV head and half of the page.
+  const auto place_of = [&](int k0, int* part) -> long long {
+    if (k0 + lane >= mine) return -1;
     const int u = u0 + warp + (k0 + lane) * W, b = request_of(u), v = u - s_off[b];
     const PaReq& r = p.r[b];
     const int item = v / r.units, x = v - item * r.units;
-    const int h = item % a.hk, at = x < r.sink ? x : x - r.sink + r.lo;
-    const int half = halves == 1 ? at & 1 : 0;
-    const int page = __ldcg(a.table + static_cast<long long>(r.seq) * a.max_pages + (halves == 1 ? at >> 1 : at));
+    const int at = x < r.sink ? x : x - r.sink + r.lo;
+    *part = item % a.hk * 2 + (halves == 1 ? at & 1 : 0);
+    return static_cast<long long>(r.seq) * a.max_pages + (halves == 1 ? at >> 1 : at);
+  };
+  // Half block in the pool; -1 where the table names no page, -2 past the end.
+  const auto block_at = [&](long long place, int part) -> int {
+    if (place < 0) return -2;
+    const int page = __ldcg(a.table + place);
     if (page < 0 || page >= a.n_pages) {
       report(a.status, kStatusCheck);
       return -1;
     }
-    return (page * a.hk + h) * 2 + half;  // (below 2^31: the host checks)
+    return page * a.hk * 2 + part;  // (below 2^31: the host checks)
   };
-  int ids = blocks_from(0), ids_next = -2;
+  int part = 0;
+  const long long place = place_of(0, &part);
+  // Nothing before this reads or writes what another kernel may; tables, masks and positions are not read through the
+  // read-only path, since the kernel that writes them may still run while this one begins.
+  griddep_wait();
+  griddep_launch();
+  int ids = block_at(place, part), ids_next = -2;
   int issued = 0, issue_at = 0;  // units asked for, the stage of the next
   uint32_t no_page = 0;  // bit s: stage s's unit has no page
   // a unit's copies: lane 0 K codes, 1 V codes, 2 K parameters, 3 V parameters
@@ -142,7 +149,10 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
     if (issued >= mine) return;
     if ((issued & 31) == 0) {
       if (issued > 0) ids = ids_next;
-      ids_next = blocks_from(issued + 32);
+      if (issued + 32 < mine) {
+        const long long next = place_of(issued + 32, &part);
+        ids_next = block_at(next, part);
+      }
     }
     const int blk = __shfl_sync(0xffffffffu, ids, issued & 31), s = issue_at;
     issue_at = s + 1 == ST ? 0 : s + 1;
