@@ -29,7 +29,7 @@
 // Bound: up to 8 rows, instruction issue at half rate and HBM together: 4 x 65536 keys, 32 heads, 1 row in 216 us, 5.6 TB/s
 // (a third of the 555 instructions a warp spends on 32 keys and 8 rows take codes apart; 12 warps an SM, as many as
 // 165 registers allow, issue in half of the cycles); beyond, the warp-level MMA and issue: 9 rows 291 us.  One token over
-// 1024 keys takes 9.8 us: launch, table, page, two joins.
+// 1024 keys takes 9.2 us: launch, table, page, two joins.
 #include <type_traits>
 
 #include "paged_attn.cuh"

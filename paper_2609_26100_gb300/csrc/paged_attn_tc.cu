@@ -21,7 +21,7 @@
 // Bound: the latency of a page's way through a softmax warp: load of the scores, 16 scores a thread, the quadrant's vote on
 // its references, exponentials, store of the weights.  1.1 us a page with 32 rows in use, 1.4 us with 128; the MMAs take
 // 0.3 us of it.  About 12 us more a launch: first page, masked pages, end of an item, join.  128 rows, 32 heads, four requests
-// of 4600 tokens 122 us; 4 requests of 2048 .. 8000 tokens, 61 rows, 32 / 8 heads 70 us.  Outputs written by the threads of
+// of 4600 tokens 121 us; 4 requests of 2048 .. 8000 tokens, 61 rows, 32 / 8 heads 70 us.  Outputs written by the threads of
 // their rows, 8 bytes a lane, had cost 5 us an item.
 // Built and slower at the latter size (when this took 75 us): 8 softmax warps of half a page each (83 us), or of every
 // second page (105); a vote by a barrier that warps wait for only after their exponentials (78); K and V expanded by
@@ -271,8 +271,11 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  griddep_wait();
-  griddep_launch();
+  // Each role waits for the kernel before this one: before it meets global memory, and before waits that are bounded.
+  const auto ready = [] {
+    griddep_wait();
+    griddep_launch();
+  };
   const uint32_t tm = sh.tmem;
   volatile int* abort = &sh.abort;
   const int n = u1 - u0;  // pages of the run; page t of it is unit u0 + t
@@ -287,14 +290,20 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
     int t = 0;
     bool ok = true;
     for (int t0 = 0; t0 < n && ok; t0 += 32) {
-      long long blk = -1;
+      long long blk = -1, place = -1;
+      int h = 0;
       if (t0 + lane < n) {
         const int u = u0 + t0 + lane;
         const PaReq& r = p.r[request_of(u)];
         const int v = u - r.off, item = v / r.units, x = v - item * r.units, at = x < r.sink ? x : x - r.sink + r.lo;
-        const int page = __ldcg(a.table + static_cast<long long>(r.seq) * a.max_pages + at);
+        place = static_cast<long long>(r.seq) * a.max_pages + at;
+        h = item % a.hk;
+      }
+      if (t0 == 0) ready();
+      if (place >= 0) {
+        const int page = __ldcg(a.table + place);
         if (page >= 0 && page < a.n_pages)
-          blk = static_cast<long long>(page) * a.hk + item % a.hk;
+          blk = static_cast<long long>(page) * a.hk + h;
         else
           report(a.status, kStatusCheck);
       }
@@ -318,6 +327,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
     for (int k = max(0, t - kPtRaw); k < t; ++k) mbar_drain(&sh.raw_full[k % kPtRaw], (k / kPtRaw) & 1);
   } else if (warp == 1) {
     // ---------------- MMAs: S two pages ahead, then O += P C' ----------------
+    ready();
     if (lane == 0) {
       constexpr uint32_t id = idesc_f16_m128(64);
       const uint32_t q_a = smem_u32(sq), kv_a = smem_u32(skv);
@@ -369,6 +379,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
   } else if (warp < 2 + kPtExpand) {
     // ---------------- codes to operands, parameters to fp32 ----------------
     // A lane's units of a page are 16 keys (dims) apart, so that its chunks' places differ by constants.
+    ready();
     const int x = tid - 64;
     constexpr int kTurns = 256 / (32 * kPtExpand);
     const uint4 zero = make_uint4(0, 0, 0, 0);
@@ -460,6 +471,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
       const PaReq& r = p.r[rb];
       const int v = u0 + t - r.off, item = v / r.units, x0 = v - item * r.units, len = min(n - t, r.units - x0);
       const int h = item % a.hk, row0 = item / a.hk * kPtRows, rows = min(kPtRows, r.n * gq - row0);
+      if (seg == 0) ready();
       // Q: 16 lanes a row, 8 dims each, as chunks in the operand's order; the warp's rows in flight together
       constexpr int kTurns = kPtRows / 2 / kPtSoftWarps;
       uint4 rawq[kTurns];
