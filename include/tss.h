@@ -466,8 +466,9 @@ tss_status tss_qk_rope(const tss_rope_args* args, void* stream);
  *   LINEAR  every frequency divided by factor (position interpolation)
  *   NTK     theta replaced by theta * factor^(rot_dim / (rot_dim - 2))
  *   YARN    pairs that turn more than fast = 32 times within `original` stay, those that turn less than
- *           slow = 1 times are divided by factor, a linear ramp over the pair index between;
- *           attention_factor = 0.1 ln(factor) + 1
+ *           slow = 1 times are divided by factor, a linear ramp over the pair index between, from the floor of the
+ *           index that turns `fast` times to the ceiling of the one that turns `slow` times, kept in
+ *           [0, rot_dim - 1] (a ramp may end past the last pair); attention_factor = 0.1 ln(factor) + 1
  *   BANDS   wavelengths under original / 4 stay, those over `original` are divided by factor, between
  *           them the two are blended in original / wavelength
  * Errors: INVALID_ARG (NULL, rot_dim odd or < 2, theta <= 1, factor < 1, original < 1 where it is used,

@@ -244,7 +244,8 @@ extern "C" tss_status tss_rope_frequencies(int kind, int rot_dim, double theta, 
   if (kind == TSS_ROPE_YARN) {
     const auto index = [&](double t) { return rot_dim * log(original / (turn * t)) / (2 * log(theta)); };
     lo = fmax(0.0, floor(index(32.0)));
-    hi = fmin(static_cast<double>(n - 1), ceil(index(1.0)));
+    // (past the last pair, n - 1, where even that one turns more than once: it is not divided by all of the factor then)
+    hi = fmin(static_cast<double>(rot_dim - 1), ceil(index(1.0)));
     if (hi - lo < 1e-3) hi = lo + 1e-3;
     *attention_factor = 0.1 * log(factor) + 1.0;
   }
