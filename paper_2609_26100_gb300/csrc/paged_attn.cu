@@ -255,10 +255,8 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
 #pragma unroll
       for (int x2 = 16; x2 > 0; x2 >>= 1) pmax = max(pmax, __shfl_xor_sync(0xffffffffu, pmax, x2));
     }
-    // units whose keys every row sees: [0, all0), the sinks, and [all1, all2)
-    const int all0 = a.window ? min(r.sink, a.sinks / unit) : 0;
-    const int all1 = r.sink + (a.window ? max(0, (pmax - a.window + unit) / unit - r.lo) : 0);
-    const int all2 = r.sink + r.first / unit - r.lo;
+    int all0, all1, all2;
+    units_in_sight(a, r, unit, pmax, &all0, &all1, &all2);
     const int done0 = done;
     for (int x = u0 + warp + done * W - u + x0; x < x1; x += W) {
       issue();  // into the stage of the unit before, if any (every lane has read it: the last loop's end)

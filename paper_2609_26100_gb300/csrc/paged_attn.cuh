@@ -89,6 +89,14 @@ __device__ __forceinline__ void cta_run(const PaParams& p, int* u0, int* u1, int
   }
 }
 
+// Units of a request that every row of a tile sees: [0, *all0), the sinks', and [*all1, *all2); pmax: the last position
+// among the rows.  (No difference here leaves 32 bits, whatever the window and the position.)
+__device__ __forceinline__ void units_in_sight(const PgAttnArgs& a, const PaReq& r, int unit, int pmax, int* all0, int* all1, int* all2) {
+  *all0 = a.window ? min(r.sink, a.sinks / unit) : 0;
+  *all1 = r.sink + (a.window && pmax >= a.window ? max(0, (pmax - a.window) / unit + 1 - r.lo) : 0);
+  *all2 = r.sink + r.first / unit - r.lo;
+}
+
 // One warp: the partials that CTAs c0 + slice, c0 + slice + step, ... up to c1 left of a row, joined: the
 // reference and sum (in all lanes) and, in lane l < D / 4, dims 4 l .. 4 l + 3 of the unnormalised output.
 // An item's first CTA left its part in its second slot, the others in their first.

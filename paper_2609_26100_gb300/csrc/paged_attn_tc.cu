@@ -536,16 +536,14 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
       __syncwarp();
       if (lane == 0) mbar_arrive(&sh.q_full);
       named_bar_sync(5, kPtSoft);
-      // pages whose keys every row sees: [0, all0), the sinks', and [all1, all2)
       int pmax = 0;
       if (a.window) {
         pmax = valid ? qp : 0;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) pmax = max(pmax, __shfl_xor_sync(0xffffffffu, pmax, o));
       }
-      const int all0 = a.window ? min(r.sink, a.sinks / kPtKeys) : 0;
-      const int all1 = r.sink + (a.window ? max(0, (pmax - a.window + kPtKeys) / kPtKeys - r.lo) : 0);
-      const int all2 = r.sink + r.first / kPtKeys - r.lo;
+      int all0, all1, all2;
+      units_in_sight(a, r, kPtKeys, pmax, &all0, &all1, &all2);
       float ref[4];
       f2_t l2[4], oz0[4], oz1[4];
 #pragma unroll
