@@ -499,7 +499,8 @@ extern "C" tss_status tss_pages_free(tss_pages* h, const tss_page_tables* t, int
   for (int i = 0; i < n; ++i) {
     if (keep && keep[i] < 0) return refuse(TSS_ERR_INVALID_ARG, "keep must be >= 0");
     list.a[i] = seq[i];
-    list.b[i] = keep ? keep[i] : 0;
+    // (no sequence holds more: the kernel counts up from here, which would wrap near the largest int)
+    list.b[i] = !keep ? 0 : keep[i] < h->max_pages ? keep[i] : h->max_pages;
   }
   return launched(launch_k(free_kernel, dim3(n), dim3(256), 0, static_cast<cudaStream_t>(stream), true, list, pt));
 }
