@@ -258,7 +258,9 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
     int all0, all1, all2;
     units_in_sight(a, r, unit, pmax, &all0, &all1, &all2);
     const int done0 = done;
-    for (int x = u0 + warp + done * W - u + x0; x < x1; x += W) {
+    // (After a wait gave up the warp asks for nothing more and waits for nothing, in this segment and those after it: an
+    // arrival at a stage whose copy is still on its way would be one too many for its barrier.)
+    for (int x = u0 + warp + done * W - u + x0; ok && x < x1; x += W) {
       issue();  // into the stage of the unit before, if any (every lane has read it: the last loop's end)
       const int s = stage;
       if (!__all_sync(0xffffffffu, mbar_try_wait(&bars[warp][s], parity))) {
