@@ -508,6 +508,7 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
           }
         }
       }
+      fence_async_smem();  // (the next segment's first copy goes to this stage: stores before the async proxy's)
     }
     __syncthreads();
     const bool whole = x0 == 0 && x1 == r.units;
