@@ -45,6 +45,17 @@ inline tss_status this_device(int* sms) {
   if (major != 10 || minor != 3) return refuse(TSS_ERR_UNSUPPORTED_ARCH, "needs an sm_103 GPU");
   return TSS_OK;
 }
+// Device memory zeroed when this returns, whatever the calls that use it run on: a memset on the default stream would wait
+// for that stream's work, and streams that do not synchronise with it would not wait for the memset.
+inline cudaError_t zero_now(void* p, size_t bytes) {
+  cudaStream_t s = nullptr;
+  cudaError_t e = cudaStreamCreateWithFlags(&s, cudaStreamNonBlocking);
+  if (e != cudaSuccess) return e;
+  e = cudaMemsetAsync(p, 0, bytes, s);
+  const cudaError_t done = cudaStreamSynchronize(s);
+  cudaStreamDestroy(s);
+  return e == cudaSuccess ? done : e;
+}
 
 // ------------------------------------------------------------------------------------------
 // Vectors of N elements (N * element size a multiple of 4 bytes, addresses aligned to it) as fp32

@@ -518,11 +518,11 @@ extern "C" tss_status tss_paged_create(int n_q_heads, int n_kv_heads, int head_d
   const size_t rows = pa_partial_rows(sms, head_dim);
   cudaError_t e = pa_prepare_all();
   if (e == cudaSuccess) e = cudaMalloc(&h->status, 256);
-  if (e == cudaSuccess) e = cudaMemset(h->status, 0, 256);
+  if (e == cudaSuccess) e = zero_now(h->status, 256);
   if (e == cudaSuccess) e = cudaMalloc(&h->part_o, rows * head_dim * sizeof(float));
   if (e == cudaSuccess) e = cudaMalloc(&h->part_ml, rows * sizeof(float2));
   if (e == cudaSuccess) e = cudaMalloc(&h->counters, pa_counters(sms) * sizeof(int));
-  if (e == cudaSuccess) e = cudaMemset(h->counters, 0, pa_counters(sms) * sizeof(int));
+  if (e == cudaSuccess) e = zero_now(h->counters, pa_counters(sms) * sizeof(int));
   if (e != cudaSuccess) {
     tss_paged_destroy(h);
     const tss_status r = refuse_cuda(e, "workspace");

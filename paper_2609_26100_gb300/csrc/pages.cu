@@ -434,7 +434,7 @@ extern "C" tss_status tss_pages_create(int n_seqs, int max_pages, int n_pages, t
   h->n_pages = n_pages;
   h->sms = sms;
   cudaError_t e = cudaMalloc(&h->status, 256);
-  if (e == cudaSuccess) e = cudaMemset(h->status, 0, 256);
+  if (e == cudaSuccess) e = zero_now(h->status, 256);
   if (e == cudaSuccess) e = cudaMalloc(&h->moves, sizeof(int) * (1 + 2 * static_cast<size_t>(n_pages)));
   if (e == cudaSuccess) e = cudaMalloc(&h->map, sizeof(int) * static_cast<size_t>(n_pages));
   if (e == cudaSuccess) e = cudaFuncSetAttribute(compact_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxPoolPages / 8);
