@@ -405,7 +405,9 @@ tss_status tss_read_trace(tss_ctx* ctx, unsigned long long* host, size_t capacit
 /* ------------------------------------------------------------------------------------------------
  * A KV cache in pages, held in 4 bits, and the operators around it.  The paper keeps its base methods'
  * 16-bit cache; these calls serve the same drafts (chains and trees, App. "Models" heads, grouped
- * heads too) where contexts or hypotheses are too many for it.  They need no tss_ctx.
+ * heads too) where contexts or hypotheses are too many for it.  They need no tss_ctx.  A workspace belongs to the
+ * device that was current when it was made: a call while another one is current returns TSS_ERR_INVALID_ARG.  All
+ * DEVICE pointers and the stream are that device's (of calls without a workspace, the current one's).
  *
  * Page layout.  A page holds TSS_PAGE_TOKENS = 64 tokens of every KV head of one layer: a block of
  * 64 * head_dim + 512 * (head_dim / 64) bytes per head, heads consecutive (head_dim 64 or 128).  The 64

@@ -34,16 +34,23 @@ inline bool known_dtype(int dtype) { return dtype == TSS_DTYPE_BF16 || dtype == 
 inline bool good_stride(int64_t stride, int64_t width, int dtype) {
   return stride >= width && stride < (int64_t(1) << 40) && (stride * dtype_bytes(dtype)) % 16 == 0;
 }
-// The current device's SM count, if it is an sm_103.
-inline tss_status this_device(int* sms) {
-  int dev = 0, major = 0, minor = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev);
-  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, dev);
-  if (e == cudaSuccess) e = cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev);
+// The current device and its SM count, if it is an sm_103.
+inline tss_status this_device(int* dev, int* sms) {
+  int major = 0, minor = 0;
+  cudaError_t e = cudaGetDevice(dev);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, *dev);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, *dev);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, *dev);
   if (e != cudaSuccess) return refuse_cuda(e, "device query");
   if (major != 10 || minor != 3) return refuse(TSS_ERR_UNSUPPORTED_ARCH, "needs an sm_103 GPU");
   return TSS_OK;
+}
+// A workspace is its device's: kernels that use it are launched while that one is current.
+inline tss_status still_on(int dev) {
+  int now = -1;
+  const cudaError_t e = cudaGetDevice(&now);
+  if (e != cudaSuccess) return refuse_cuda(e, "device query");
+  return now == dev ? TSS_OK : refuse(TSS_ERR_INVALID_ARG, "the current device is not the one that the workspace was made on");
 }
 // Device memory zeroed when this returns, whatever the calls that use it run on: a memset on the default stream would wait
 // for that stream's work, and streams that do not synchronise with it would not wait for the memset.

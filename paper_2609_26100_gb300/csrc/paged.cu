@@ -420,6 +420,8 @@ cudaError_t pq_launch(const PqParams& p, bool append, int dtype, unsigned grid, 
 // Checks what every call on the cache has in common and copies the batch.  *rows: rows in all.
 tss_status take_batch(const tss_paged* h, const tss_paged_cache* c, int layer, const tss_paged_batch* b, PgBatch* out, long long* rows) {
   if (!h || !c || !b) return refuse(TSS_ERR_INVALID_ARG, "NULL argument");
+  const tss_status on = still_on(h->dev);
+  if (on != TSS_OK) return on;
   if (!c->layer || c->n_layers < 1 || layer < 0 || layer >= c->n_layers)
     return refuse(TSS_ERR_INVALID_ARG, "layer must be in [0, n_layers)");
   if (!c->layer[layer] || !aligned16(c->layer[layer])) return refuse(TSS_ERR_INVALID_ARG, "the layer's pages must be 16-byte aligned device memory");
@@ -506,14 +508,15 @@ extern "C" tss_status tss_paged_create(int n_q_heads, int n_kv_heads, int head_d
   if (n_kv_heads < 1 || n_kv_heads > 1024) return refuse(TSS_ERR_INVALID_ARG, "n_kv_heads must be in [1, 1024]");
   if (n_q_heads < 1 || n_q_heads % n_kv_heads || n_q_heads / n_kv_heads > 64)
     return refuse(TSS_ERR_INVALID_ARG, "n_q_heads must be a multiple of n_kv_heads, at most 64 times it");
-  int sms = 0;
-  const tss_status st = this_device(&sms);
+  int dev = 0, sms = 0;
+  const tss_status st = this_device(&dev, &sms);
   if (st != TSS_OK) return st;
   tss_paged* h = new (std::nothrow) tss_paged{};
   if (!h) return refuse(TSS_ERR_OUT_OF_MEMORY, "no host memory");
   h->hq = n_q_heads;
   h->hk = n_kv_heads;
   h->d = head_dim;
+  h->dev = dev;
   h->sms = sms;
   const size_t rows = pa_partial_rows(sms, head_dim);
   cudaError_t e = pa_prepare_all();
@@ -543,6 +546,8 @@ extern "C" void tss_paged_destroy(tss_paged* h) {
 
 extern "C" tss_status tss_paged_sync_status(tss_paged* h, void* stream) {
   if (!h) return refuse(TSS_ERR_INVALID_ARG, "NULL argument");
+  const tss_status on = still_on(h->dev);
+  if (on != TSS_OK) return on;
   int v = 0;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   cudaError_t e = cudaMemcpyAsync(&v, h->status, sizeof(int), cudaMemcpyDeviceToHost, s);

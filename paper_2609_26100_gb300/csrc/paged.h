@@ -5,7 +5,7 @@
 
 // (opaque in tss.h)
 struct tss_paged {
-  int hq, hk, d, sms;
+  int hq, hk, d, dev, sms;
   int* status;      // device
   float* part_o;    // device: partial results of items that several CTAs share
   float2* part_ml;

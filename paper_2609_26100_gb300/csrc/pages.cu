@@ -12,7 +12,7 @@
 #include "ops.cuh"
 
 struct tss_pages {
-  int n_seqs, max_pages, n_pages, sms;
+  int n_seqs, max_pages, n_pages, dev, sms;
   int* status;  // device word: first failure
   int* go;      // device word: the last choosing launch found its pages (1) or left everything as it was (0)
   int* moves;   // device [1 + 2 * n_pages]: their number, then sources, then destinations (or chosen pages)
@@ -388,6 +388,8 @@ tss_status take_layers(void* const* layer, int n_layers, size_t page_bytes, Laye
 }
 tss_status take_tables(const tss_pages* h, const tss_page_tables* t, PoolTables* out) {
   if (!h || !t || !t->table || !t->held || !t->refs) return refuse(TSS_ERR_INVALID_ARG, "NULL argument");
+  const tss_status on = still_on(h->dev);
+  if (on != TSS_OK) return on;
   *out = PoolTables{t->table, t->held, t->refs, h->n_seqs, h->max_pages, h->n_pages, h->status};
   return TSS_OK;
 }
@@ -424,14 +426,15 @@ extern "C" tss_status tss_pages_create(int n_seqs, int max_pages, int n_pages, t
   if (n_seqs < 1 || max_pages < 1 || static_cast<long long>(n_seqs) * max_pages > 0x7fffffffLL)
     return refuse(TSS_ERR_INVALID_ARG, "n_seqs and max_pages must be >= 1 and their product below 2^31");
   if (n_pages < 1 || n_pages > kMaxPoolPages) return refuse(TSS_ERR_INVALID_ARG, "n_pages must be in [1, 2^20]");
-  int sms = 0;
-  const tss_status st = this_device(&sms);
+  int dev = 0, sms = 0;
+  const tss_status st = this_device(&dev, &sms);
   if (st != TSS_OK) return st;
   tss_pages* h = new (std::nothrow) tss_pages{};
   if (!h) return refuse(TSS_ERR_OUT_OF_MEMORY, "no host memory");
   h->n_seqs = n_seqs;
   h->max_pages = max_pages;
   h->n_pages = n_pages;
+  h->dev = dev;
   h->sms = sms;
   cudaError_t e = cudaMalloc(&h->status, 256);
   if (e == cudaSuccess) e = zero_now(h->status, 256);
@@ -458,6 +461,8 @@ extern "C" void tss_pages_destroy(tss_pages* h) {
 
 extern "C" tss_status tss_pages_sync_status(tss_pages* h, void* stream) {
   if (!h) return refuse(TSS_ERR_INVALID_ARG, "NULL argument");
+  const tss_status on = still_on(h->dev);
+  if (on != TSS_OK) return on;
   int v = 0;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   cudaError_t e = cudaMemcpyAsync(&v, h->status, sizeof(int), cudaMemcpyDeviceToHost, s);
@@ -561,7 +566,8 @@ extern "C" tss_status tss_pages_copy(tss_pages* h, void* const* layer, int n_lay
                                      const int32_t* dst, void* stream) {
   Layers ly{};
   if (!h) return refuse(TSS_ERR_INVALID_ARG, "NULL argument");
-  const tss_status st = take_layers(layer, n_layers, page_bytes, &ly);
+  tss_status st = still_on(h->dev);
+  if (st == TSS_OK) st = take_layers(layer, n_layers, page_bytes, &ly);
   if (st != TSS_OK) return st;
   if (n < 0) return refuse(TSS_ERR_INVALID_ARG, "n must be >= 0");
   if (n == 0) return TSS_OK;

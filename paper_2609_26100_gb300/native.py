@@ -282,16 +282,19 @@ def rope_frequencies(rot_dim: int, theta: float = 10000.0, kind: str = "none", f
 def rope_table(inv_freq: Sequence[float], table, attention_factor: float = 1.0, stream=None) -> None:
     """tss_rope_table into the float32 device tensor table [positions][len(inv_freq)][2], on the given stream (None:
     torch's current one)."""
+    import torch
     n = len(inv_freq)
     if tuple(table.shape[1:]) != (n, 2) or dtype_code(table) != TSS_DTYPE_F32 or not table.is_contiguous() or not table.is_cuda:
         raise ValueError("table: contiguous float32 [positions][pairs][2] on the GPU is wanted")
+    if table.get_device() != torch.cuda.current_device():
+        raise ValueError("the table's device is not the current one")
     check(lib().tss_rope_table((ctypes.c_double * n)(*inv_freq), n, attention_factor, table.shape[0], table.data_ptr(),
                                current_stream() if stream is None else stream), "tss_rope_table")
 
 
 def rope_args(q, k, q_out, k_out, positions, table, q_gain=None, k_gain=None, eps: float = 1e-6, interleaved: bool = False,
               status=None) -> TssRopeArgs:
-    """Arguments of tss_qk_rope from tensors: q, k [rows][heads][head_dim] (either may be None) and their
+    """Arguments of tss_qk_rope from tensors of one GPU: q, k [rows][heads][head_dim] (either may be None) and their
     outputs (q_out may be q), positions int32 [rows], table [positions][pairs][2] float32 (None: no rotation),
     gains [head_dim] (None: no norm).  The structure keeps the tensors alive."""
     one = q if q is not None else k
@@ -299,6 +302,10 @@ def rope_args(q, k, q_out, k_out, positions, table, q_gain=None, k_gain=None, ep
         raise ValueError("q or k is wanted")
     a = TssRopeArgs()
     a.n_rows, _, a.head_dim, _ = _rows(one, "q")
+    a._device = one.get_device()
+    for x in (k, table, positions, status):
+        if x is not None and x.get_device() != a._device:
+            raise ValueError("q, k, table, positions and status on one GPU are wanted")
     a.dtype, a.interleaved, a.eps = dtype_code(one), int(interleaved), eps
     for name, x, y, gain in (("q", q, q_out, q_gain), ("k", k, k_out, k_gain)):
         if x is None:
@@ -339,8 +346,12 @@ def current_stream() -> int:
 
 
 def qk_rope(args: TssRopeArgs, stream=None) -> None:
-    """tss_qk_rope on the given stream (None: torch's current one)."""
-    s = lib().tss_qk_rope(ctypes.byref(args), current_stream() if stream is None else stream)
+    """tss_qk_rope on the given stream (None: torch's current one) of the tensors' device, which has to be the current one."""
+    import torch
+    device = torch.cuda.current_device()
+    if getattr(args, "_device", device) != device:
+        raise ValueError("the tensors' device is not the current one")
+    s = lib().tss_qk_rope(ctypes.byref(args), torch._C._cuda_getCurrentRawStream(device) if stream is None else stream)
     if s:
         check(s, "tss_qk_rope")
 

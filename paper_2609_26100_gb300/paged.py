@@ -3,7 +3,8 @@ libtss.so (tss_paged_*, tss_pages_*).
 
 ``PagePool`` keeps the books of pages of any content (page table, pages held, reference counts, all on the
 device); ``Kv4Cache`` appends to, reads and attends over pages held in 4 bits.  Both work on the caller's
-tensors; ``Kv4Cache.allocate`` makes a set that fits together.
+tensors; ``Kv4Cache.allocate`` makes a set that fits together.  All tensors are on the pool's GPU, which has to
+be the current device in every call.
 """
 from __future__ import annotations
 
@@ -14,7 +15,7 @@ from typing import Optional, Sequence
 import torch
 
 from . import native
-from .native import _P, _i32, _ptr, check, current_stream, lib
+from .native import _P, _i32, _ptr, check, lib
 
 PAGE_TOKENS = native.PAGE_TOKENS
 _CODES = {torch.bfloat16: native.TSS_DTYPE_BF16, torch.float16: native.TSS_DTYPE_F16, torch.float32: native.TSS_DTYPE_F32}
@@ -32,10 +33,10 @@ def pages_for(tokens: int) -> int:
     return -(-int(tokens) // PAGE_TOKENS)
 
 
-def _row_stride(t: torch.Tensor, shape, what: str) -> int:
-    """Elements between the rows of t, a GPU tensor which has the given shape and contiguous heads."""
-    if t.shape != shape or not t.is_cuda:
-        raise ValueError(f"{what}: {list(shape)} on the GPU is wanted")
+def _row_stride(t: torch.Tensor, shape, device: int, what: str) -> int:
+    """Elements between the rows of t, a tensor on that GPU which has the given shape and contiguous heads."""
+    if t.shape != shape or t.get_device() != device:
+        raise ValueError(f"{what}: {list(shape)} on the pool's GPU is wanted")
     row, head, one = t.stride()
     n, h, d = shape
     if n == 0:
@@ -57,9 +58,16 @@ def _host(values) -> array:
     return array("i", values)
 
 
-def _ints(t: torch.Tensor, shape, what: str) -> None:
-    if t.shape != shape or t.dtype != torch.int32 or not t.is_contiguous() or not t.is_cuda:
-        raise ValueError(f"{what}: contiguous int32 {list(shape)} on the GPU is wanted")
+def _ints(t: torch.Tensor, shape, device: int, what: str) -> None:
+    if t.shape != shape or t.dtype != torch.int32 or not t.is_contiguous() or t.get_device() != device:
+        raise ValueError(f"{what}: contiguous int32 {list(shape)} on the pool's GPU is wanted")
+
+
+def _stream_of(device: int, stream) -> int:
+    """The stream of a call on that device (None: torch's current one), which has to be the current device."""
+    if torch.cuda.current_device() != device:
+        raise ValueError(f"the pool is on cuda:{device}, which is not the current device")
+    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream
 
 
 def _layers(pool: torch.Tensor):
@@ -81,15 +89,17 @@ class PagePool:
         if table.dim() != 2:
             raise ValueError("table: int32 [seqs][max_pages] is wanted")
         self.n_seqs, self.max_pages = table.shape
-        _ints(table, (self.n_seqs, self.max_pages), "table")
-        _ints(held, (self.n_seqs,), "held")
-        _ints(refs, (self.n_pages,), "refs")
+        self._dev = dev = pool.get_device()
+        _ints(table, (self.n_seqs, self.max_pages), dev, "table")
+        _ints(held, (self.n_seqs,), dev, "held")
+        _ints(refs, (self.n_pages,), dev, "refs")
         self.pool, self.table, self.held, self.refs = pool, table, held, refs
         self._tables = native.TssPageTables(table.data_ptr(), held.data_ptr(), refs.data_ptr())
         self._ref = ctypes.byref(self._tables)
         h = _P()
         self._c_free, self._c_fork = lib().tss_pages_free, lib().tss_pages_fork
-        check(lib().tss_pages_create(self.n_seqs, self.max_pages, self.n_pages, ctypes.byref(h)), "tss_pages_create")
+        with torch.cuda.device(dev):
+            check(lib().tss_pages_create(self.n_seqs, self.max_pages, self.n_pages, ctypes.byref(h)), "tss_pages_create")
         self._h = h
 
     def close(self) -> None:
@@ -104,7 +114,7 @@ class PagePool:
             pass
 
     def _stream(self, stream):
-        return current_stream() if stream is None else stream
+        return _stream_of(self._dev, stream)
 
     def reserve(self, seqs: Sequence[int], tokens: Sequence[int], stream=None) -> None:
         """Pages for tokens[i] tokens of seqs[i] (those it holds stay)."""
@@ -122,7 +132,7 @@ class PagePool:
         if tokens is not None:
             keep = _host([-(-t // PAGE_TOKENS) for t in tokens])
         s = self._c_free(self._h, self._ref, len(a), a.buffer_info()[0], None if keep is None else keep.buffer_info()[0],
-                         current_stream() if stream is None else stream)
+                         self._stream(stream))
         if s:
             check(s, "tss_pages_free")
 
@@ -136,7 +146,7 @@ class PagePool:
         a = _host((*src, *dst, *[t // PAGE_TOKENS for t in tokens], *[-(-t // PAGE_TOKENS) for t in tokens]))
         at, step = a.buffer_info()[0], n * a.itemsize
         s = self._c_fork(self._h, self._ref, self._ptrs, self.n_layers, self.page_bytes, n, at, at + step, at + 2 * step, at + 3 * step,
-                         current_stream() if stream is None else stream)
+                         self._stream(stream))
         if s:
             check(s, "tss_pages_fork")
 
@@ -144,15 +154,15 @@ class PagePool:
         """Move the pages in use to the lowest ids; the new table and counts replace the pool's, or go to the
         given tensors."""
         t, r = (self.table if table_out is None else table_out), (self.refs if refs_out is None else refs_out)
-        _ints(t, self.table.shape, "table_out")
-        _ints(r, self.refs.shape, "refs_out")
+        _ints(t, self.table.shape, self._dev, "table_out")
+        _ints(r, self.refs.shape, self._dev, "refs_out")
         check(lib().tss_pages_compact(self._h, self._ref, t.data_ptr(), r.data_ptr(), self._ptrs, self.n_layers,
                                       self.page_bytes, self._stream(stream)), "tss_pages_compact")
 
     def copy(self, src: torch.Tensor, dst: torch.Tensor, stream=None) -> None:
         """Copy page src[i] over page dst[i] in every layer (int32 tensors on the GPU)."""
-        _ints(src, (src.numel(),), "src")
-        _ints(dst, (src.numel(),), "dst")
+        _ints(src, (src.numel(),), self._dev, "src")
+        _ints(dst, (src.numel(),), self._dev, "dst")
         check(lib().tss_pages_copy(self._h, self._ptrs, self.n_layers, self.page_bytes, src.numel(), _ptr(src), _ptr(dst),
                                    self._stream(stream)), "tss_pages_copy")
 
@@ -168,7 +178,8 @@ class Kv4Cache:
             raise ValueError("pool: uint8 [layers][pages][page bytes] is wanted")
         if table.dim() != 2:
             raise ValueError("table: int32 [seqs][max_pages] is wanted")
-        _ints(table, table.shape, "table")
+        self._dev = pool.get_device()
+        _ints(table, table.shape, self._dev, "table")
         self.n_q_heads, self.n_kv_heads, self.head_dim = n_q_heads, n_kv_heads, head_dim
         self.pool, self.table = pool, table
         self._ptrs, n_layers, n_pages, _ = _layers(pool)
@@ -178,7 +189,8 @@ class Kv4Cache:
         self._c_append, self._c_read, self._c_attention = lib().tss_paged_append, lib().tss_paged_read, lib().tss_paged_attention
         self.pages: Optional[PagePool] = None
         h = _P()
-        check(lib().tss_paged_create(n_q_heads, n_kv_heads, head_dim, ctypes.byref(h)), "tss_paged_create")
+        with torch.cuda.device(self._dev):
+            check(lib().tss_paged_create(n_q_heads, n_kv_heads, head_dim, ctypes.byref(h)), "tss_paged_create")
         self._h = h
 
     @classmethod
@@ -219,23 +231,23 @@ class Kv4Cache:
 
     def append(self, layer: int, batch, k: torch.Tensor, v: torch.Tensor, stream=None) -> None:
         """Quantise k, v [rows][kv heads][head_dim] into the pages of the batch's tokens."""
-        shape = (batch.rows, self.n_kv_heads, self.head_dim)
+        shape, dev = (batch.rows, self.n_kv_heads, self.head_dim), self._dev
         if k.dtype != v.dtype:
             raise ValueError("k and v differ in type")
-        s = self._c_append(self._h, self._cache_ref, layer, batch.ref, k.data_ptr(), v.data_ptr(), _row_stride(k, shape, "k"),
-                           _row_stride(v, shape, "v"), _code(k), current_stream() if stream is None else stream)
+        s = self._c_append(self._h, self._cache_ref, layer, batch.ref, k.data_ptr(), v.data_ptr(), _row_stride(k, shape, dev, "k"),
+                           _row_stride(v, shape, dev, "v"), _code(k), _stream_of(self._dev, stream))
         if s:
             check(s, "tss_paged_append")
 
     def read(self, layer: int, batch, k: Optional[torch.Tensor], v: Optional[torch.Tensor], stream=None) -> None:
         """The values that the batch's tokens are held as, to k and v (either may be None)."""
-        shape = (batch.rows, self.n_kv_heads, self.head_dim)
+        shape, dev = (batch.rows, self.n_kv_heads, self.head_dim), self._dev
         one = k if k is not None else v
         if one is None or (k is not None and v is not None and k.dtype != v.dtype):
             raise ValueError("k or v is wanted, of one type")
         s = self._c_read(self._h, self._cache_ref, layer, batch.ref, None if k is None else k.data_ptr(),
-                         None if v is None else v.data_ptr(), 0 if k is None else _row_stride(k, shape, "k"),
-                         0 if v is None else _row_stride(v, shape, "v"), _code(one), current_stream() if stream is None else stream)
+                         None if v is None else v.data_ptr(), 0 if k is None else _row_stride(k, shape, dev, "k"),
+                         0 if v is None else _row_stride(v, shape, dev, "v"), _code(one), _stream_of(self._dev, stream))
         if s:
             check(s, "tss_paged_read")
 
@@ -246,20 +258,21 @@ class Kv4Cache:
         lse float32 [rows][heads]; mask int64 [rows][2] (bits of the block's rows that a row sees; None: a chain);
         window and sinks as in tss_paged_attention, positions int32 [rows]."""
         n, h, d = shape = (batch.rows, self.n_q_heads, self.head_dim)
-        if out.dtype != q.dtype or out.device != q.device:
-            raise ValueError("out: the type and device of q are wanted")
-        if lse is not None and (lse.shape != (n, h) or lse.dtype != torch.float32 or not lse.is_contiguous() or not lse.is_cuda):
-            raise ValueError("lse: contiguous float32 [rows][heads] on the GPU is wanted")
+        dev = self._dev
+        if out.dtype != q.dtype:
+            raise ValueError("out: the type of q is wanted")
+        if lse is not None and (lse.shape != (n, h) or lse.dtype != torch.float32 or not lse.is_contiguous() or lse.get_device() != dev):
+            raise ValueError("lse: contiguous float32 [rows][heads] on the pool's GPU is wanted")
         if mask is not None and (mask.shape != (n, 2) or mask.dtype not in (torch.int64, torch.uint64) or not mask.is_contiguous()
-                                 or not mask.is_cuda):
-            raise ValueError("mask: contiguous 64-bit [rows][2] on the GPU is wanted")
+                                 or mask.get_device() != dev):
+            raise ValueError("mask: contiguous 64-bit [rows][2] on the pool's GPU is wanted")
         if positions is not None:
-            _ints(positions, (n,), "positions")
-        a = native.TssPagedAttn(q.data_ptr(), _row_stride(q, shape, "q"), out.data_ptr(), _row_stride(out, shape, "out"),
+            _ints(positions, (n,), dev, "positions")
+        a = native.TssPagedAttn(q.data_ptr(), _row_stride(q, shape, dev, "q"), out.data_ptr(), _row_stride(out, shape, dev, "out"),
                                 None if lse is None else lse.data_ptr(), _code(q), d ** -0.5 if scale is None else scale, window,
                                 sinks, None if mask is None else mask.data_ptr(), None if positions is None else positions.data_ptr())
         s = self._c_attention(self._h, self._cache_ref, layer, batch.ref, ctypes.byref(a),
-                              current_stream() if stream is None else stream)
+                              _stream_of(self._dev, stream))
         if s:
             check(s, "tss_paged_attention")
 
@@ -268,4 +281,4 @@ class Kv4Cache:
         check(lib().tss_paged_inject_timeout(self._h, n_calls), "tss_paged_inject_timeout")
 
     def sync_status(self, stream=None) -> int:
-        return lib().tss_paged_sync_status(self._h, current_stream() if stream is None else stream)
+        return lib().tss_paged_sync_status(self._h, _stream_of(self._dev, stream))
