@@ -15,7 +15,7 @@ from typing import Optional, Sequence
 import torch
 
 from . import native
-from .native import _P, _i32, _ptr, check, lib
+from .native import _P, _ptr, check, lib
 
 PAGE_TOKENS = native.PAGE_TOKENS
 _CODES = {torch.bfloat16: native.TSS_DTYPE_BF16, torch.float16: native.TSS_DTYPE_F16, torch.float32: native.TSS_DTYPE_F32}
@@ -222,8 +222,8 @@ class Kv4Cache:
         """Request i is the tokens [first[i], first[i] + n_tokens[i]) of sequence seqs[i]."""
         if not len(seqs) == len(first) == len(n_tokens):
             raise ValueError("seqs, first and n_tokens differ in length")
-        keep = [_i32(seqs), _i32(first), _i32(n_tokens)]
-        b = native.TssPagedBatch(len(seqs), *[ctypes.cast(a, _P) for a in keep])
+        keep = [_host(map(int, x)) for x in (seqs, first, n_tokens)]  # (OverflowError past 32 bits)
+        b = native.TssPagedBatch(len(seqs), *[a.buffer_info()[0] for a in keep])
         b._keep = keep
         b.ref = ctypes.byref(b)
         b.rows = sum(int(n) for n in n_tokens)
