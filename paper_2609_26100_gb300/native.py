@@ -262,7 +262,7 @@ def _rows(t, what: str):
     n, h, d = t.shape
     if n and h and (t.stride(2) != 1 or (h > 1 and t.stride(1) != d)):
         raise ValueError(f"{what}: the heads of a row must be contiguous")
-    return n, h, d, t.stride(0) if n > 1 else max(t.stride(0), h * d)
+    return n, h, d, t.stride(0) if n > 1 else h * d  # (nothing steps from a single row)
 
 
 def _same(a, b, what: str) -> None:

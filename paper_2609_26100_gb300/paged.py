@@ -43,7 +43,7 @@ def _row_stride(t: torch.Tensor, shape, device: int, what: str) -> int:
         return h * d
     if one != 1 or (h > 1 and head != d):
         raise ValueError(f"{what}: the heads of a row must be contiguous")
-    return row if n > 1 else max(row, h * d)
+    return row if n > 1 else h * d  # (nothing steps from a single row)
 
 
 def _code(t: torch.Tensor) -> int:
