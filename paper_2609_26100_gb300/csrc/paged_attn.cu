@@ -16,9 +16,11 @@
 // where the usual orientation would pad 1 .. 8 rows to 16.  P^T's operand layout is the transpose of S^T's
 // accumulator: one movmatrix per 8 x 8.
 //
-// ref_r is raised only when some p s' passes 2^15 (fp16's end), to where the largest is 2^7, so most tiles
+// ref_r is raised only when some p s' passes 2^15 (fp16's end), to where the largest is between 2^6 and 2^7, so most tiles
 // need no reduction over tokens.  In terms of p s' rather than p, it keeps the weights in fp16's range
-// whatever the values' scales.
+// whatever the values' scales.  Each group of 64 dims has a reference of its own (as a power of two beside the first
+// group's), since one group's scales may be a millionth of the other's: under the other's reference its weights would be
+// fp16 subnormals, and its dims off by 1e-2.
 //
 // Work split.  A unit is a page (or half of one, for short launches) of one item: a request's row tile and KV
 // head.  CTAs of four warps, three to an SM (two with 16 rows), take runs of units; a run's units go round its
@@ -190,6 +192,7 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
     uint32_t qf[NT][G][2][4];
     float2 f2[NT], ref2[NT], l2[NT];  // (of rows 2t and 2t + 1; the reference negated)
     float zq[NT][G][2], oz[NT][G][2], o[NT][DB][2][4];
+    float2 gx[NT];  // G == 2: what turns weights under the first group's reference into those under the second's
     int pmax = 0;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
@@ -235,6 +238,7 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
       f2[nt] = make_float2(__shfl_sync(0xffffffffu, mul, 8 * t), __shfl_sync(0xffffffffu, mul, 8 * t + 4));
       ref2[nt] = make_float2(INFINITY, INFINITY);
       l2[nt] = make_float2(0.f, 0.f);
+      gx[nt] = make_float2(1.f, 1.f);
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -330,22 +334,18 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
           }
         }
         float2 vz[2][2][G];
-        float smax = kLeast;  // the largest scale among the thread's keys
+        float smax[G];  // the largest scale among the thread's keys
+#pragma unroll
+        for (int gi = 0; gi < G; ++gi) smax[gi] = kLeast;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const __half2* pr = vparams + (k * 8 + g) * G;
 #pragma unroll
           for (int gi = 0; gi < G; ++gi) {
             vz[k >> 1][k & 1][gi] = __half22float2(pr[gi]);
-            smax = fmaxf(smax, vz[k >> 1][k & 1][gi].x);
+            smax[gi] = fmaxf(smax[gi], vz[k >> 1][k & 1][gi].x);
           }
         }
-        const auto key_scale = [&](int mt, int x2) {
-          float x = kLeast;
-#pragma unroll
-          for (int gi = 0; gi < G; ++gi) x = fmaxf(x, vz[mt][x2][gi].x);
-          return x;
-        };
         constexpr int kParts = TWO ? 2 : 1;
         uint32_t pf[NT][G][kParts][4];  // the weights times the values' scales in fp16 parts, [8-key block]
         const auto weigh = [&](auto all) {
@@ -369,11 +369,12 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
           }
           const auto on = [&](int nt, int mt, int i) { return kAll || (vis >> (nt * 8 + mt * 4 + i) & 1u); };
           // weights, in units of 2^ref; again where the reference has to rise first
-          float w[NT][2][4], wmax;
+          float w[NT][2][4];
+          float wmax[G];  // the thread's largest, under each group's reference
           const auto weights = [&]() {
-            wmax = 0.f;
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+            for (int nt = 0; nt < NT; ++nt) {
+              float2 m = make_float2(0.f, 0.f);
 #pragma unroll
               for (int k = 0; k < 4; ++k) {
                 float* sp = &sc[nt][k >> 1][(k & 1) * 2];
@@ -381,44 +382,66 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
                 const float2 e = fma2(make_float2(sp[0], sp[1]), f2[nt], ref2[nt]);
                 wp[0] = on(nt, k >> 1, (k & 1) * 2) ? ex2(e.x) : 0.f;
                 wp[1] = on(nt, k >> 1, (k & 1) * 2 + 1) ? ex2(e.y) : 0.f;
-                wmax = fmaxf(wmax, fmaxf(wp[0], wp[1]));
+                m = make_float2(fmaxf(m.x, wp[0]), fmaxf(m.y, wp[1]));
               }
+              wmax[0] = nt ? fmaxf(wmax[0], fmaxf(m.x, m.y)) : fmaxf(m.x, m.y);
+              if constexpr (G == 2) {
+                const float x = fmaxf(m.x * gx[nt].x, m.y * gx[nt].y);
+                wmax[G - 1] = nt ? fmaxf(wmax[G - 1], x) : x;
+              }
+            }
           };
           weights();
           // (the thread's largest weight and scale may be of different keys: then nothing rises below)
-          if (__any_sync(0xffffffffu, wmax * smax > kTop)) {
+          bool over = false;
+#pragma unroll
+          for (int gi = 0; gi < G; ++gi) over |= wmax[gi] * smax[gi] > kTop;
+          if (__any_sync(0xffffffffu, over)) {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
               for (int i = 0; i < 2; ++i) {
-                float top = -INFINITY;
-                bool up = false;
+                float& ref = i ? ref2[nt].y : ref2[nt].x;
+                float& factor = i ? gx[nt].y : gx[nt].x;
+                float top[G];
+#pragma unroll
+                for (int gi = 0; gi < G; ++gi) top[gi] = -INFINITY;
 #pragma unroll
                 for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
                   for (int x2 = 0; x2 < 2; ++x2)
                     if (on(nt, mt, x2 * 2 + i)) {
-                      top = fmaxf(top, fmaf(sc[nt][mt][2 * x2 + i], i ? f2[nt].y : f2[nt].x, __log2f(key_scale(mt, x2))));
-                      up |= w[nt][mt][2 * x2 + i] * key_scale(mt, x2) > kTop;
+#pragma unroll
+                      for (int gi = 0; gi < G; ++gi)
+                        top[gi] = fmaxf(top[gi], fmaf(sc[nt][mt][2 * x2 + i], i ? f2[nt].y : f2[nt].x, __log2f(fmaxf(vz[mt][x2][gi].x, kLeast))));
                     }
 #pragma unroll
-                for (int x2 = 4; x2 < 32; x2 <<= 1) {
-                  top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x2));
-                  up |= __shfl_xor_sync(0xffffffffu, static_cast<int>(up), x2) != 0;
-                }
-                if (up) {
-                  float& ref = i ? ref2[nt].y : ref2[nt].x;
-                  const float now = 7.f - top, al = ref == INFINITY ? 1.f : ex2(now - ref);
+                for (int x2 = 4; x2 < 32; x2 <<= 1)
+#pragma unroll
+                  for (int gi = 0; gi < G; ++gi) top[gi] = fmaxf(top[gi], __shfl_xor_sync(0xffffffffu, top[gi], x2));
+                // (negated, and whole numbers, so that the factor between the groups is a power of two; infinite until the row's
+                // first keys, which set both)
+                const float last = ref + static_cast<float>((__float_as_int(factor) >> 23) - 127);  // of the last group
+                const bool up = top[0] + ref > 15.f, up_last = top[G - 1] + last > 15.f;
+                if (up || up_last) {
+                  const bool first = ref == INFINITY;
+                  const float now = up ? floorf(7.f - top[0]) : ref, al = first ? 1.f : pow2(now - ref);
+                  float al_last = al;
+                  if constexpr (G == 2) {
+                    const float now_last = up_last ? floorf(7.f - top[G - 1]) : last;
+                    al_last = first ? 1.f : pow2(now_last - last);
+                    factor = pow2(now_last - now);
+                  }
                   ref = now;
                   (i ? l2[nt].y : l2[nt].x) *= al;
 #pragma unroll
                   for (int gi = 0; gi < G; ++gi) oz[nt][gi][i] *= al;
 #pragma unroll
-                  for (int x2 = 0; x2 < DB; ++x2)
+                  for (int db = 0; db < DB; ++db)
 #pragma unroll
                     for (int y = 0; y < 2; ++y) {
-                      o[nt][x2][y][i] *= al;
-                      o[nt][x2][y][2 + i] *= al;
+                      o[nt][db][y][i] *= db * 32 / kPgGroup ? al_last : al;
+                      o[nt][db][y][2 + i] *= db * 32 / kPgGroup ? al_last : al;
                     }
                 }
               }
@@ -433,6 +456,7 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
               const float w0 = w[nt][k >> 1][(k & 1) * 2], w1 = w[nt][k >> 1][(k & 1) * 2 + 1];
               const bool on0 = on(nt, k >> 1, (k & 1) * 2), on1 = on(nt, k >> 1, (k & 1) * 2 + 1);
               l2[nt] = add2(l2[nt], make_float2(w0, w1));
+              const float2 wx = G == 2 ? mul2(make_float2(w0, w1), gx[nt]) : make_float2(0.f, 0.f);
 #pragma unroll
               for (int gi = 0; gi < G; ++gi) {
                 const float2 sz = vz[k >> 1][k & 1][gi];
@@ -440,7 +464,8 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
                 // (what a pair does not see may be NaN: selected away, not multiplied)
                 oz[nt][gi][0] = on0 ? fmaf(w0, sz.y, oz[nt][gi][0]) : oz[nt][gi][0];
                 oz[nt][gi][1] = on1 ? fmaf(w1, sz.y, oz[nt][gi][1]) : oz[nt][gi][1];
-                const float p0 = on0 ? w0 * s2 : 0.f, p1 = on1 ? w1 * s2 : 0.f;
+                const float2 pw = mul2(gi ? wx : make_float2(w0, w1), make_float2(s2, s2));
+                const float p0 = on0 ? pw.x : 0.f, p1 = on1 ? pw.y : 0.f;
                 const uint32_t hi = pack_f16(p0, p1);
                 pf[nt][gi][0][k] = movmatrix_t(hi);
                 if constexpr (TWO) {
@@ -499,10 +524,12 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
           for (int db = 0; db < DB; ++db) {
             float4 x;
             const float z = oz[nt][db * 32 / kPgGroup][i];
-            x.x = fmaf(o[nt][db][0][i], 16777216.f, z);
-            x.y = fmaf(o[nt][db][0][2 + i], 16777216.f, z);
-            x.z = fmaf(o[nt][db][1][i], 16777216.f, z);
-            x.w = fmaf(o[nt][db][1][2 + i], 16777216.f, z);
+            // (2^24 over the group's factor, a power of two)
+            const float m = db * 32 / kPgGroup ? __uint_as_float(((24u + 254u) << 23) - __float_as_uint(i ? gx[nt].y : gx[nt].x)) : 16777216.f;
+            x.x = fmaf(o[nt][db][0][i], m, z);
+            x.y = fmaf(o[nt][db][0][2 + i], m, z);
+            x.z = fmaf(o[nt][db][1][i], m, z);
+            x.w = fmaf(o[nt][db][1][2 + i], m, z);
             // (16-byte chunks permuted by row so that a warp's store meets each bank once)
             *reinterpret_cast<float4*>(buf + row * D + (((db * 8 + g) ^ (2 * t)) << 2)) = x;
           }

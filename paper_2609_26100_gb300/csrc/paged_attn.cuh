@@ -51,6 +51,8 @@ __device__ __forceinline__ float query_scale(float big) {
 // p s' that raises a row's reference, and fp16's smallest scale.
 constexpr float kTop = 32768.f;
 constexpr float kLeast = 5.9604645e-8f;
+// 2^d of a whole d below 128 (0 where that is less than fp32's normal numbers).
+__device__ __forceinline__ float pow2(float d) { return d < -126.f ? 0.f : __int_as_float((static_cast<int>(d) + 127) << 23); }
 
 // Even runs.  The items' units, each item's led by p.lead more, laid end to end and cut evenly: the first unit at
 // or after place g of them, and the CTA whose run holds unit u (of request b).

@@ -6,6 +6,10 @@
 // C, C' are the codes as fp16 subnormals (paged_attn.cu); scales, minima, references and sums are fp32,
 // Q exact in fp16 (scaled by a power of two), the weights one fp16 part (bf16 outputs) or two.
 //
+// References are a row's and group's, as in paged_attn.cu; a row's two are one while they are 2 binades apart at most, so that
+// pages whose groups have scales alike cost one maximum a score and no factor (61 rows over 4600 tokens 71 us, 79 with
+// scales 8 or 10^6 times apart).
+//
 // A nibble word (8 dims of a key, or 8 keys of a dim) becomes eight values of a K-major operand by four ANDs and a
 // shift; their order and the factor 16 of odd nibbles are matched in Q and P.
 //
@@ -26,6 +30,7 @@
 // Built and slower at the latter size (when this took 75 us): 8 softmax warps of half a page each (83 us), or of every
 // second page (105); a vote by a barrier that warps wait for only after their exponentials (78); K and V expanded by
 // warps of their own into three buffers (85).
+#include <cfloat>
 #include <cstddef>
 #include <type_traits>
 
@@ -58,7 +63,7 @@ struct __align__(16) PtShared {
   long long out_at[kPtRows];                          // where its output begins
   int qp[kPtRows];                                    // its position
   float inv[kPtRows];                                 // 1 / sum of its weights
-  float top[4][kPtRows];                              // maxima of its quarters
+  float top[2][4][kPtRows];                           // maxima of its quarters, of scores and V's scales of each group
   float part[4][3][kPtRows];                          // the quarters' sums: p, p z'_0, p z'_1
 };
 static_assert(offsetof(PtShared, par) % 16 == 0 && offsetof(PtShared, row) % 16 == 0 && offsetof(PtShared, raw_full) % 8 == 0,
@@ -175,9 +180,9 @@ __device__ __forceinline__ void join_parts(const PaParams& p, PtShared& sh, uint
   if (row < rows)
 #pragma unroll 4
     for (int x = qt; x < parts; x += 4) M = fmaxf(M, __ldcg(p.part_ml + slot(x) + row).x);
-  sh.top[qt][row] = M;
+  sh.top[0][qt][row] = M;
   named_bar_sync(5, kPtSoft);
-  M = fmaxf(fmaxf(sh.top[0][row], sh.top[1][row]), fmaxf(sh.top[2][row], sh.top[3][row]));
+  M = fmaxf(fmaxf(sh.top[0][0][row], sh.top[0][1][row]), fmaxf(sh.top[0][2][row], sh.top[0][3][row]));
   const float mb = M == -INFINITY ? 0.f : M;
   if (row < rows)
 #pragma unroll 4
@@ -219,7 +224,7 @@ __device__ __forceinline__ void join_parts(const PaParams& p, PtShared& sh, uint
     float m = -INFINITY, l = 0.f;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      m = fmaxf(m, sh.top[k][q]);
+      m = fmaxf(m, sh.top[0][k][q]);
       l += sh.part[k][0][q];
     }
     finish_row<kPtD>(p.a, r, h, row0 + q, lane, m, l, o[i]);
@@ -544,11 +549,14 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
       }
       int all0, all1, all2;
       units_in_sight(a, r, kPtKeys, pmax, &all0, &all1, &all2);
-      float ref[4];
+      float ref[4];  // of the first group of dims, and the factor from weights under it to those under the second's
+      float fx[4];
+      bool split = false;  // some row's factor is not 1
       f2_t l2[4], oz0[4], oz1[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        ref[i] = -INFINITY;
+        ref[i] = -FLT_MAX;  // (nothing seen)
+        fx[i] = 1.f;
         l2[i] = oz0[i] = oz1[i] = f2_pack(0.f, 0.f);
       }
       for (int j = 0; j < len; ++j) {
@@ -601,16 +609,14 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
                 }
               }
             }
-            float top[4];
-            bool over = false;
-            {
-              const ulonglong2 lg = pr(8);
+            // maxima over the thread's keys of a row's scores, each more lg(block).x or .y
+            const auto tops = [&](float* top, auto lg) {
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
                 top[i] = -INFINITY;
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
-                  const float2 e = f2_unpack(f2_add(c[i][b], b ? lg.y : lg.x));
+                  const float2 e = f2_unpack(f2_add(c[i][b], lg(b)));
                   if constexpr (kAll) {
                     top[i] = fmaxf(top[i], fmaxf(e.x, e.y));
                   } else {
@@ -618,36 +624,78 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
                     top[i] = fmaxf(top[i], vis >> (4 * i + 2 * b + 1) & 1u ? e.y : -INFINITY);
                   }
                 }
-                over |= top[i] - ref[i] > 15.f;
               }
-            }
-            // a row's reference rises where a weight times its value's scale would pass 2^15, to leave it at 2^7
-            if (quad_or(quad, over)) {
-              float al[4];
+            };
+            const auto tops_of = [&](float* top, int g) {  // with V's scales of group g
+              const ulonglong2 s = pr(4 + g);
+              const auto log2_of = [](f2_t x) {
+                const float2 q = f2_unpack(x);
+                return f2_pack(__log2f(fmaxf(q.x, kLeast)), __log2f(fmaxf(q.y, kLeast)));
+              };
+              const f2_t lo = log2_of(s.x), hi = log2_of(s.y);
+              tops(top, [&](int b) { return b ? hi : lo; });
+            };
+            const auto second = [&](int i) { return ref[i] - static_cast<float>((__float_as_int(fx[i]) >> 23) - 127); };  // its reference
+            bool over = false;
+            if (split) {
+              float top[4];
+              tops_of(top, 0);
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 1));
-                top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 2));
-                if (x4 == 0) sh.top[qt][qd * 32 + r4 + 8 * i] = top[i];
+              for (int i = 0; i < 4; ++i) over |= top[i] - ref[i] > 15.f;
+              tops_of(top, 1);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) over |= top[i] - second(i) > 15.f;
+            } else {
+              float top[4];
+              const ulonglong2 lg = pr(8);
+              tops(top, [&](int b) { return b ? lg.y : lg.x; });
+#pragma unroll
+              for (int i = 0; i < 4; ++i) over |= top[i] - ref[i] > 15.f;
+            }
+            // A row's references rise where a weight times its value's scale would pass 2^15, to leave each group's largest
+            // between 2^6 and 2^7 (whole numbers, so that the factor between the groups is a power of two; one for both, and a
+            // largest of up to 2^9, where they are 2 apart at most).
+            if (quad_or(quad, over)) {
+              float top[2][4];
+#pragma unroll
+              for (int g = 0; g < 2; ++g) {
+                tops_of(top[g], g);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  top[g][i] = fmaxf(top[g][i], __shfl_xor_sync(0xffffffffu, top[g][i], 1));
+                  top[g][i] = fmaxf(top[g][i], __shfl_xor_sync(0xffffffffu, top[g][i], 2));
+                  if (x4 == 0) sh.top[g][qt][qd * 32 + r4 + 8 * i] = top[g][i];
+                }
               }
               named_bar_sync(quad, 128);
               bool moved = false;
+              float al[4];  // of the group of dims that the thread's outputs are of
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
                 const int q = qd * 32 + r4 + 8 * i;
-                const float most = fmaxf(fmaxf(sh.top[0][q], sh.top[1][q]), fmaxf(sh.top[2][q], sh.top[3][q]));
                 al[i] = 1.f;
-                if (most - ref[i] > 15.f) {
-                  const float now = most - 7.f;
-                  al[i] = ref[i] == -INFINITY ? 1.f : ex2(ref[i] - now);
-                  ref[i] = now;
-                  const f2_t al2 = f2_pack(al[i], al[i]);
-                  l2[i] = f2_mul(l2[i], al2);
-                  oz0[i] = f2_mul(oz0[i], al2);
-                  oz1[i] = f2_mul(oz1[i], al2);
+                float was[2] = {ref[i], second(i)}, now[2];
+                bool up = false;
+#pragma unroll
+                for (int g = 0; g < 2; ++g) {
+                  const float most = fmaxf(fmaxf(sh.top[g][0][q], sh.top[g][1][q]), fmaxf(sh.top[g][2][q], sh.top[g][3][q]));
+                  up |= most - was[g] > 15.f;
+                  now[g] = fmaxf(was[g], ceilf(most - 7.f));
+                }
+                if (up) {
+                  if (fabsf(now[0] - now[1]) <= 2.f) now[0] = now[1] = fminf(now[0], now[1]);
+                  const float down = pow2(was[0] - now[0]);
+                  const f2_t d2 = f2_pack(down, down);
+                  l2[i] = f2_mul(l2[i], d2);
+                  oz0[i] = f2_mul(oz0[i], d2);
+                  oz1[i] = f2_mul(oz1[i], d2);
+                  ref[i] = now[0];
+                  fx[i] = pow2(now[0] - now[1]);
+                  al[i] = half ? pow2(was[1] - now[1]) : down;
                 }
                 moved |= al[i] != 1.f;
               }
+              split = __any_sync(0xffffffffu, fx[0] != 1.f || fx[1] != 1.f || fx[2] != 1.f || fx[3] != 1.f);
               if (j > 0 && __any_sync(0xffffffffu, moved)) {
                 ok = ok && quiet_wait(&sh.o_done[(u - 1) & 1], ((u - 1) >> 1) & 1, abort, a.status);
                 const float mine = of_row(al);
@@ -664,64 +712,72 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
                 }
               }
             }
-            const ulonglong2 v0s = pr(4), v1s = pr(5), z0s = pr(6), z1s = pr(7);
-            const f2_t down = f2_pack(0.0625f, 0.0625f);  // (odd nibbles stand four bits up)
+            const auto weigh = [&](auto split_tag) {
+              constexpr bool kSplit = decltype(split_tag)::value;
+              const ulonglong2 v0s = pr(4), v1s = pr(5), z0s = pr(6), z1s = pr(7);
+              const f2_t down = f2_pack(0.0625f, 0.0625f);  // (odd nibbles stand four bits up)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              uint32_t hi[2][4], lo[2][4];  // [group][2 y + b]: row i = 2 h + y
+              for (int h = 0; h < 2; ++h) {
+                uint32_t hi[2][4], lo[2][4];  // [group][2 y + b]: row i = 2 h + y
 #pragma unroll
-              for (int y = 0; y < 2; ++y) {
-                const int i = 2 * h + y;
-                const f2_t nref = f2_pack(-ref[i], -ref[i]);
+                for (int y = 0; y < 2; ++y) {
+                  const int i = 2 * h + y;
+                  const f2_t nref = f2_pack(-ref[i], -ref[i]);
+                  const f2_t fx2 = f2_pack(fx[i], fx[i]);
 #pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                  const float2 e = f2_unpack(f2_add(c[i][b], nref));
-                  const float2 wf = make_float2(ex2(e.x), ex2(e.y));
-                  const f2_t v0 = b ? v0s.y : v0s.x, v1 = b ? v1s.y : v1s.x, z0 = b ? z0s.y : z0s.x, z1 = b ? z1s.y : z1s.x;
-                  f2_t p0, p1;
-                  if constexpr (kAll) {
-                    f2_t w = f2_pack(wf.x, wf.y);
-                    l2[i] = f2_add(l2[i], w);
-                    oz0[i] = f2_fma(w, z0, oz0[i]);
-                    oz1[i] = f2_fma(w, z1, oz1[i]);
-                    if (b) w = f2_mul(w, down);
-                    p0 = f2_mul(w, v0);
-                    p1 = f2_mul(w, v1);
-                  } else {  // (what a row does not see may be NaN: selected away, not multiplied)
-                    const bool on0 = vis >> (4 * i + 2 * b) & 1u, on1 = vis >> (4 * i + 2 * b + 1) & 1u;
-                    const auto pick = [&](f2_t m) {
-                      const float2 q = f2_unpack(m);
-                      return f2_pack(on0 ? q.x : 0.f, on1 ? q.y : 0.f);
-                    };
-                    f2_t w = f2_pack(on0 ? wf.x : 0.f, on1 ? wf.y : 0.f);
-                    l2[i] = f2_add(l2[i], w);
-                    oz0[i] = f2_fma(w, pick(z0), oz0[i]);
-                    oz1[i] = f2_fma(w, pick(z1), oz1[i]);
-                    if (b) w = f2_mul(w, down);
-                    p0 = f2_mul(w, pick(v0));
-                    p1 = f2_mul(w, pick(v1));
-                  }
-                  const auto split = [&](f2_t m, uint32_t* first, uint32_t* rest) {
-                    const float2 q = f2_unpack(m);
-                    *first = pack_f16(q.x, q.y);
-                    if constexpr (TWO) {
-                      const float2 back = __half22float2(*reinterpret_cast<const __half2*>(first));
-                      const float2 d = f2_unpack(f2_fma(f2_pack(back.x, back.y), f2_pack(-1.f, -1.f), m));
-                      *rest = pack_f16(d.x, d.y);
+                  for (int b = 0; b < 2; ++b) {
+                    const float2 e = f2_unpack(f2_add(c[i][b], nref));
+                    const float2 wf = make_float2(ex2(e.x), ex2(e.y));
+                    const f2_t v0 = b ? v0s.y : v0s.x, v1 = b ? v1s.y : v1s.x, z0 = b ? z0s.y : z0s.x, z1 = b ? z1s.y : z1s.x;
+                    f2_t p0, p1;
+                    if constexpr (kAll) {
+                      f2_t w = f2_pack(wf.x, wf.y);
+                      l2[i] = f2_add(l2[i], w);
+                      oz0[i] = f2_fma(w, z0, oz0[i]);
+                      oz1[i] = f2_fma(w, z1, oz1[i]);
+                      if (b) w = f2_mul(w, down);
+                      p0 = f2_mul(w, v0);
+                      p1 = f2_mul(kSplit ? f2_mul(w, fx2) : w, v1);
+                    } else {  // (what a row does not see may be NaN: selected away, not multiplied)
+                      const bool on0 = vis >> (4 * i + 2 * b) & 1u, on1 = vis >> (4 * i + 2 * b + 1) & 1u;
+                      const auto pick = [&](f2_t m) {
+                        const float2 q = f2_unpack(m);
+                        return f2_pack(on0 ? q.x : 0.f, on1 ? q.y : 0.f);
+                      };
+                      f2_t w = f2_pack(on0 ? wf.x : 0.f, on1 ? wf.y : 0.f);
+                      l2[i] = f2_add(l2[i], w);
+                      oz0[i] = f2_fma(w, pick(z0), oz0[i]);
+                      oz1[i] = f2_fma(w, pick(z1), oz1[i]);
+                      if (b) w = f2_mul(w, down);
+                      p0 = f2_mul(w, pick(v0));
+                      p1 = f2_mul(kSplit ? f2_mul(w, fx2) : w, pick(v1));
                     }
-                  };
-                  split(p0, &hi[0][2 * y + b], &lo[0][2 * y + b]);
-                  split(p1, &hi[1][2 * y + b], &lo[1][2 * y + b]);
+                    const auto split = [&](f2_t m, uint32_t* first, uint32_t* rest) {
+                      const float2 q = f2_unpack(m);
+                      *first = pack_f16(q.x, q.y);
+                      if constexpr (TWO) {
+                        const float2 back = __half22float2(*reinterpret_cast<const __half2*>(first));
+                        const float2 d = f2_unpack(f2_fma(f2_pack(back.x, back.y), f2_pack(-1.f, -1.f), m));
+                        *rest = pack_f16(d.x, d.y);
+                      }
+                    };
+                    split(p0, &hi[0][2 * y + b], &lo[0][2 * y + b]);
+                    split(p1, &hi[1][2 * y + b], &lo[1][2 * y + b]);
+                  }
+                }
+                const uint32_t to = at + (static_cast<uint32_t>(16 * h) << 16);
+                __syncwarp();
+#pragma unroll
+                for (int g = 0; g < 2; ++g) {
+                  tmem_st_block(to + g * 64, hi[g]);
+                  if constexpr (TWO) tmem_st_block(to + g * 64 + 8, lo[g]);
                 }
               }
-              const uint32_t to = at + (static_cast<uint32_t>(16 * h) << 16);
-              __syncwarp();
-#pragma unroll
-              for (int g = 0; g < 2; ++g) {
-                tmem_st_block(to + g * 64, hi[g]);
-                if constexpr (TWO) tmem_st_block(to + g * 64 + 8, lo[g]);
-              }
-            }
+            };
+            if (split)
+              weigh(std::true_type{});
+            else
+              weigh(std::false_type{});
             tmem_stored();
           };
           if (__all_sync(0xffffffffu, vis == 0xffffu))
@@ -758,7 +814,8 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
             if (x4 == 0) sh.part[qt][k][qd * 32 + r4 + 8 * i] = sums[k];
           }
         }
-        const float my_ref = of_row(ref);
+        const float my_ref = of_row(ref), my_fx = of_row(fx);
+        const float m = half ? __uint_as_float(((24u + 254u) << 23) - __float_as_uint(my_fx)) : 16777216.f;  // 2^24 over the group's factor
         named_bar_sync(quad, 128);
         float L = 0.f, z = 0.f;
 #pragma unroll
@@ -787,8 +844,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
 #pragma unroll
           for (int i = 0; i < 4; ++i)
             rows_of[lane * (kPtD / 4) + ((qt * 8 + c * 4 + i) ^ lane)] =
-                make_float4(fmaf(o[4 * i], 16777216.f, z), fmaf(o[4 * i + 1], 16777216.f, z), fmaf(o[4 * i + 2], 16777216.f, z),
-                            fmaf(o[4 * i + 3], 16777216.f, z));
+                make_float4(fmaf(o[4 * i], m, z), fmaf(o[4 * i + 1], m, z), fmaf(o[4 * i + 2], m, z), fmaf(o[4 * i + 3], m, z));
         }
         tc_fence_before();
         named_bar_sync(quad, 128);
