@@ -3,14 +3,16 @@
 //   score_tr = scale q_r . k_t,  k_t = s_t c_t + z_t per 64 dims   (row r, token t)
 //   o_r = sum_t p_tr v_t / sum_t p_tr,  p_tr = 2^(log2e score_tr - ref_r),  v_t = s'_t c'_t + z'_t
 //
-// The codes go to the tensor cores as they are: a nibble in the low bits of an fp16 lane is the subnormal
+// K's codes go to the tensor cores as they are: a nibble in the low bits of an fp16 lane is the subnormal
 // number c 2^-24 (c 2^-20 four bits further up), so a 32-bit word becomes four operand registers with four
 // ANDs and a shift, exactly; the factor 16 of every second pair is taken out of the other operand.  Scales
 // and minima join in fp32: s_t multiplies the sum over a group's dims, z_t the sum of the query's; on the
 // value side s'_t goes into the weight, which enters as two fp16 parts (hi and the rest, 22 bits: one part alone costs
 // the output 4e-4 of its size, twice what rounding it to fp16 does; a quarter of what rounding to bf16 does, so blocks of
-// more than 8 rows with bf16 outputs take one part), and z'_t is summed by itself.  Queries are scaled by a power of two
-// to fill fp16's range, so they are exact too.
+// more than 8 rows with bf16 outputs take one part), and the rest of the value is summed by itself.  V's codes enter centred,
+// v = s' (c' - 7.5) + (z' + 7.5 s') (`centre` says why: sums of terms of one sign drift), one more operation a register, 2 to 5 %
+// of the time; with one weight part, whose own rounding is 2^-12, as they are, 32 keys at a time that are added up by
+// rounding.  Queries are scaled by a power of two to fill fp16's range, exact down to 2^-35 of a row's largest.
 //
 // Tokens take the MMA's 16-row side (S^T = K Q^T, O^T = V^T P^T): a block of 8 query rows (N) fills it,
 // where the usual orientation would pad 1 .. 8 rows to 16.  P^T's operand layout is the transpose of S^T's
@@ -28,10 +30,10 @@
 // others stream.  At an item's end the warps' parts are joined in shared memory; items that several CTAs share
 // leave partials, which the last CTA to arrive joins in CTA order (results do not depend on timing).
 //
-// Bound: up to 8 rows, instruction issue at half rate and HBM together: 4 x 65536 keys, 32 heads, 1 row in 216 us, 5.6 TB/s
-// (a third of the 555 instructions a warp spends on 32 keys and 8 rows take codes apart; 12 warps an SM, as many as
-// 165 registers allow, issue in half of the cycles); beyond, the warp-level MMA and issue: 9 rows 291 us.  One token over
-// 1024 keys takes 9.2 us: launch, table, page, two joins.
+// Bound: up to 8 rows, instruction issue and HBM together: 4 x 65536 keys, 32 heads, 1 row in 234 us, 5.2 TB/s (two fifths of the
+// instructions that a warp spends on 32 keys and 8 rows take codes apart; 12 warps an SM, as many as 168 registers allow,
+// issue in half of the cycles); beyond, neither: eight warps an SM (249 registers) do not hide the steps from load to MMA,
+// 16 x 16384 keys, 9 rows in 315 us.  One token over 1024 keys takes 9.4 us: launch, table, page, two joins.
 #include <type_traits>
 
 #include "paged_attn.cuh"
@@ -343,10 +345,12 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
 #pragma unroll
           for (int gi = 0; gi < G; ++gi) {
             vz[k >> 1][k & 1][gi] = __half22float2(pr[gi]);
+            if constexpr (TWO) vz[k >> 1][k & 1][gi].y = fmaf(vz[k >> 1][k & 1][gi].x, 7.5f, vz[k >> 1][k & 1][gi].y);
             smax[gi] = fmaxf(smax[gi], vz[k >> 1][k & 1][gi].x);
           }
         }
         constexpr int kParts = TWO ? 2 : 1;
+        constexpr bool kCentre = TWO;  // values as s' (c' - 7.5) + (z' + 7.5 s'); else as they are
         uint32_t pf[NT][G][kParts][4];  // the weights times the values' scales in fp16 parts, [8-key block]
         const auto weigh = [&](auto all) {
           constexpr bool kAll = decltype(all)::value;  // every (key, row) pair counts
@@ -460,7 +464,7 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
 #pragma unroll
               for (int gi = 0; gi < G; ++gi) {
                 const float2 sz = vz[k >> 1][k & 1][gi];
-                const float s2 = k & 1 ? sz.x * 0.0625f : sz.x;
+                const float s2 = !kCentre && (k & 1) ? sz.x * 0.0625f : sz.x;
                 // (what a pair does not see may be NaN: selected away, not multiplied)
                 oz[nt][gi][0] = on0 ? fmaf(w0, sz.y, oz[nt][gi][0]) : oz[nt][gi][0];
                 oz[nt][gi][1] = on1 ? fmaf(w1, sz.y, oz[nt][gi][1]) : oz[nt][gi][1];
@@ -487,14 +491,34 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
 #pragma unroll
           for (int y = 0; y < 2; ++y) {
             const uint32_t x0 = x[2 * y], x1 = x[2 * y + 1], y0 = x0 >> 8, y1 = x1 >> 8;
-            const uint32_t a0[4] = {x0 & 0x000f000fu, x1 & 0x000f000fu, x0 & 0x00f000f0u, x1 & 0x00f000f0u};
-            const uint32_t a1[4] = {y0 & 0x000f000fu, y1 & 0x000f000fu, y0 & 0x00f000f0u, y1 & 0x00f000f0u};
+            uint32_t a0[4] = {x0 & 0x000f000fu, x1 & 0x000f000fu, x0 & 0x00f000f0u, x1 & 0x00f000f0u};
+            uint32_t a1[4] = {y0 & 0x000f000fu, y1 & 0x000f000fu, y0 & 0x00f000f0u, y1 & 0x00f000f0u};
+            if constexpr (kCentre) {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                a0[i] = centre(a0[i], i >= 2);
+                a1[i] = centre(a1[i], i >= 2);
+              }
+            }
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
+              const uint32_t(&w)[kParts][4] = pf[nt][db * 32 / kPgGroup];
+              if constexpr (kCentre) {
 #pragma unroll
-              for (int part = 0; part < kParts; ++part) {
-                mma_next(o[nt][db][y], a0, &pf[nt][db * 32 / kPgGroup][part][0]);
-                mma_next(o[nt][db][y], a1, &pf[nt][db * 32 / kPgGroup][part][2]);
+                for (int part = 0; part < kParts; ++part) {
+                  mma_next(o[nt][db][y], a0, &w[part][0]);
+                  mma_next(o[nt][db][y], a1, &w[part][2]);
+                }
+              } else {  // (the 32 keys apart, added to the rest by rounding)
+                float now[4];
+                mma_first(now, a0, &w[0][0]);
+                mma_next(now, a1, &w[0][2]);
+#pragma unroll
+                for (int i = 0; i < 4; i += 2) {
+                  const float2 sum = add2(make_float2(o[nt][db][y][i], o[nt][db][y][i + 1]), make_float2(now[i], now[i + 1]));
+                  o[nt][db][y][i] = sum.x;
+                  o[nt][db][y][i + 1] = sum.y;
+                }
               }
             }
           }
@@ -524,8 +548,10 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
           for (int db = 0; db < DB; ++db) {
             float4 x;
             const float z = oz[nt][db * 32 / kPgGroup][i];
-            // (2^24 over the group's factor, a power of two)
-            const float m = db * 32 / kPgGroup ? __uint_as_float(((24u + 254u) << 23) - __float_as_uint(i ? gx[nt].y : gx[nt].x)) : 16777216.f;
+            // (2^9 or 2^24 over the group's factor, a power of two)
+            constexpr uint32_t kUp = TWO ? 9 : 24;
+            const float m = db * 32 / kPgGroup ? __uint_as_float(((kUp + 254u) << 23) - __float_as_uint(i ? gx[nt].y : gx[nt].x))
+                                               : static_cast<float>(1 << kUp);
             x.x = fmaf(o[nt][db][0][i], m, z);
             x.y = fmaf(o[nt][db][0][2 + i], m, z);
             x.z = fmaf(o[nt][db][1][i], m, z);

@@ -2,16 +2,16 @@
 // head_dim 128: the operation of paged_attn.cu for more than kPaTcRows query rows of a KV head (trees, long
 // chains, grouped heads), which take the MMA's 128-row side.  Per page of 64 tokens, g a group of 64 dims:
 //   S_g [128 rows x 64 keys] = Q_g C_g^T            score = f (s_0 S_0 + s_1 S_1 + z_0 q_0 + z_1 q_1)
-//   O_g [128 rows x 64 dims] += (P s'_g) C'_g       o = (2^24 O_g + sum_t p_t z'_tg) / sum_t p_t
-// C, C' are the codes as fp16 subnormals (paged_attn.cu); scales, minima, references and sums are fp32,
-// Q exact in fp16 (scaled by a power of two), the weights one fp16 part (bf16 outputs) or two.
+//   O_g [128 rows x 64 dims] += (P s'_g) C'_g       o = (2^9 O_g + sum_t p_t (z' + 7.5 s')_tg) / sum_t p_t
+// C is K's codes as fp16 subnormals (paged_attn.cu), C' V's centred, (c - 7.5) 2^-9; scales, minima, references and sums
+// are fp32, Q exact in fp16 (scaled by a power of two), the weights one fp16 part (bf16 outputs) or two.
 //
 // References are a row's and group's, as in paged_attn.cu; a row's two are one while they are 2 binades apart at most, so that
 // pages whose groups have scales alike cost one maximum a score and no factor (61 rows over 4600 tokens 71 us, 79 with
 // scales 8 or 10^6 times apart).
 //
 // A nibble word (8 dims of a key, or 8 keys of a dim) becomes eight values of a K-major operand by four ANDs and a
-// shift; their order and the factor 16 of odd nibbles are matched in Q and P.
+// shift; their order, and in K the factor 16 of odd nibbles, are matched in Q and P.
 //
 // Roles (640 threads): warp 0 copies pages (one bulk copy each), warp 1 issues MMAs, warps 2-3 expand codes
 // and parameters, warps 4-19 are the softmax.  Scores lie in three buffers of TMEM, read as blocks of 16 rows and 8
@@ -25,8 +25,8 @@
 // Bound: the latency of a page's way through a softmax warp: load of the scores, 16 scores a thread, the quadrant's vote on
 // its references, exponentials, store of the weights.  1.1 us a page with 32 rows in use, 1.4 us with 128; the MMAs take
 // 0.3 us of it.  About 12 us more a launch: first page, masked pages, end of an item, join.  128 rows, 32 heads, four requests
-// of 4600 tokens 121 us; 4 requests of 2048 .. 8000 tokens, 61 rows, 32 / 8 heads 70 us.  Outputs written by the threads of
-// their rows, 8 bytes a lane, had cost 5 us an item.
+// of 4600 tokens 123 us; 4 requests of 2048 .. 8000 tokens, 61 rows, 32 / 8 heads 71 us.  (At 640 threads of 96 registers some
+// 64 bytes a thread spill.)  Outputs written by the threads of their rows, 8 bytes a lane, had cost 5 us an item.
 // Built and slower at the latter size (when this took 75 us): 8 softmax warps of half a page each (83 us), or of every
 // second page (105); a vote by a barrier that warps wait for only after their exponentials (78); K and V expanded by
 // warps of their own into three buffers (85).
@@ -404,7 +404,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
         const auto pair = [](uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); };
         const float2 k0 = pair(kp.x), k1 = pair(kp.y), v0 = pair(vp.x), v1 = pair(vp.y);
         const int at = (x & 48) | (x & 6) << 1 | (x & 8) >> 2 | (x & 1);
-        const float all[kPtParams] = {k0.x, k1.x, k0.y, k1.y, v0.x, v1.x, v0.y, v1.y, __log2f(fmaxf(fmaxf(v0.x, v1.x), kLeast))};
+        const float all[kPtParams] = {k0.x, k1.x, k0.y, k1.y, v0.x, v1.x, fmaf(v0.x, 7.5f, v0.y), fmaf(v1.x, 7.5f, v1.y), __log2f(fmaxf(fmaxf(v0.x, v1.x), kLeast))};
 #pragma unroll
         for (int i = 0; i < kPtParams; ++i) sh.par[t & 3][i][at] = all[i];
         if (x == 0) sh.bad_par[t & 3] = bad;
@@ -441,8 +441,8 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
         for (int e = 0; e < 4; ++e) {
           const uint32_t f = vw[e] >> (8 * swap), g = vw[e] >> (8 - 8 * swap);
           uint8_t* row = vd + e * 128;
-          *reinterpret_cast<uint2*>(row + ((first ^ ((d0 + e) & 7)) << 4)) = make_uint2(f & 0x000f000fu, f & 0x00f000f0u);
-          *reinterpret_cast<uint2*>(row + ((second ^ ((d0 + e) & 7)) << 4)) = make_uint2(g & 0x000f000fu, g & 0x00f000f0u);
+          *reinterpret_cast<uint2*>(row + ((first ^ ((d0 + e) & 7)) << 4)) = make_uint2(centre(f & 0x000f000fu, false), centre(f & 0x00f000f0u, true));
+          *reinterpret_cast<uint2*>(row + ((second ^ ((d0 + e) & 7)) << 4)) = make_uint2(centre(g & 0x000f000fu, false), centre(g & 0x00f000f0u, true));
         }
       }
       fence_async_smem();
@@ -715,7 +715,6 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
             const auto weigh = [&](auto split_tag) {
               constexpr bool kSplit = decltype(split_tag)::value;
               const ulonglong2 v0s = pr(4), v1s = pr(5), z0s = pr(6), z1s = pr(7);
-              const f2_t down = f2_pack(0.0625f, 0.0625f);  // (odd nibbles stand four bits up)
 #pragma unroll
               for (int h = 0; h < 2; ++h) {
                 uint32_t hi[2][4], lo[2][4];  // [group][2 y + b]: row i = 2 h + y
@@ -735,7 +734,6 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
                       l2[i] = f2_add(l2[i], w);
                       oz0[i] = f2_fma(w, z0, oz0[i]);
                       oz1[i] = f2_fma(w, z1, oz1[i]);
-                      if (b) w = f2_mul(w, down);
                       p0 = f2_mul(w, v0);
                       p1 = f2_mul(kSplit ? f2_mul(w, fx2) : w, v1);
                     } else {  // (what a row does not see may be NaN: selected away, not multiplied)
@@ -748,7 +746,6 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
                       l2[i] = f2_add(l2[i], w);
                       oz0[i] = f2_fma(w, pick(z0), oz0[i]);
                       oz1[i] = f2_fma(w, pick(z1), oz1[i]);
-                      if (b) w = f2_mul(w, down);
                       p0 = f2_mul(w, pick(v0));
                       p1 = f2_mul(kSplit ? f2_mul(w, fx2) : w, pick(v1));
                     }
@@ -815,7 +812,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
           }
         }
         const float my_ref = of_row(ref), my_fx = of_row(fx);
-        const float m = half ? __uint_as_float(((24u + 254u) << 23) - __float_as_uint(my_fx)) : 16777216.f;  // 2^24 over the group's factor
+        const float m = half ? __uint_as_float(((9u + 254u) << 23) - __float_as_uint(my_fx)) : 512.f;  // 2^9 over the group's factor
         named_bar_sync(quad, 128);
         float L = 0.f, z = 0.f;
 #pragma unroll
