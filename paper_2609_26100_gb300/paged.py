@@ -33,6 +33,11 @@ def pages_for(tokens: int) -> int:
     return -(-int(tokens) // PAGE_TOKENS)
 
 
+def _pages(tokens) -> list:
+    """Pages of each length; -1, which the library refuses, for one below zero (rounding up would make some of them 0)."""
+    return [-(-t // PAGE_TOKENS) if t >= 0 else -1 for t in tokens]
+
+
 def _row_stride(t: torch.Tensor, shape, device: int, what: str) -> int:
     """Elements between the rows of t, a tensor on that GPU which has the given shape and contiguous heads."""
     if t.shape != shape or t.get_device() != device:
@@ -120,7 +125,7 @@ class PagePool:
         """Pages for tokens[i] tokens of seqs[i] (those it holds stay)."""
         if len(seqs) != len(tokens):
             raise ValueError("seqs and tokens differ in length")
-        a, b = _host(seqs), _host([-(-t // PAGE_TOKENS) for t in tokens])
+        a, b = _host(seqs), _host(_pages(tokens))
         check(lib().tss_pages_reserve(self._h, self._ref, len(a), a.buffer_info()[0], b.buffer_info()[0], self._stream(stream)),
               "tss_pages_reserve")
 
@@ -130,7 +135,7 @@ class PagePool:
             raise ValueError("seqs and tokens differ in length")
         a, keep = _host(seqs), None
         if tokens is not None:
-            keep = _host([-(-t // PAGE_TOKENS) for t in tokens])
+            keep = _host(_pages(tokens))
         s = self._c_free(self._h, self._ref, len(a), a.buffer_info()[0], None if keep is None else keep.buffer_info()[0],
                          self._stream(stream))
         if s:
@@ -143,7 +148,7 @@ class PagePool:
         if len(dst) != n or len(tokens) != n:
             raise ValueError("src, dst and tokens differ in length")
         # src, dst, pages to share and pages in all, in one array
-        a = _host((*src, *dst, *[t // PAGE_TOKENS for t in tokens], *[-(-t // PAGE_TOKENS) for t in tokens]))
+        a = _host((*src, *dst, *[t // PAGE_TOKENS for t in tokens], *_pages(tokens)))
         at, step = a.buffer_info()[0], n * a.itemsize
         s = self._c_fork(self._h, self._ref, self._ptrs, self.n_layers, self.page_bytes, n, at, at + step, at + 2 * step, at + 3 * step,
                          self._stream(stream))
