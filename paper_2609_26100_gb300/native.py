@@ -266,7 +266,7 @@ def _rows(t, what: str):
 
 
 def _same(a, b, what: str) -> None:
-    if a.shape != b.shape or a.dtype != b.dtype or a.device != b.device:
+    if b is None or a.shape != b.shape or a.dtype != b.dtype or a.device != b.device:
         raise ValueError(f"{what}: the output's shape, type and device must be the input's")
 
 
@@ -327,7 +327,7 @@ def rope_args(q, k, q_out, k_out, positions, table, q_gain=None, k_gain=None, ep
         if (table.dim() != 3 or table.shape[2] != 2 or dtype_code(table) != TSS_DTYPE_F32 or not table.is_contiguous()
                 or not table.is_cuda):
             raise ValueError("table: contiguous float32 [positions][pairs][2] on the GPU is wanted")
-        if (str(positions.dtype) != "torch.int32" or positions.numel() != a.n_rows or not positions.is_contiguous()
+        if (positions is None or str(positions.dtype) != "torch.int32" or positions.numel() != a.n_rows or not positions.is_contiguous()
                 or not positions.is_cuda):
             raise ValueError("positions: contiguous int32 [rows] on the GPU is wanted")
         a.table, a.max_positions, a.rot_dim = table.data_ptr(), table.shape[0], 2 * table.shape[1]
