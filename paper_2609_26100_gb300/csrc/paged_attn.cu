@@ -30,10 +30,10 @@
 // others stream.  At an item's end the warps' parts are joined in shared memory; items that several CTAs share
 // leave partials, which the last CTA to arrive joins in CTA order (results do not depend on timing).
 //
-// Bound: up to 8 rows, instruction issue and HBM together: 4 x 65536 keys, 32 heads, 1 row in 234 us, 5.2 TB/s (two fifths of the
-// instructions that a warp spends on 32 keys and 8 rows take codes apart; 12 warps an SM, as many as 168 registers allow,
-// issue in half of the cycles); beyond, neither: eight warps an SM (249 registers) do not hide the steps from load to MMA,
-// 16 x 16384 keys, 9 rows in 315 us.  One token over 1024 keys takes 9.4 us: launch, table, page, two joins.
+// Bound: up to 8 rows, instruction issue and HBM together: 4 x 65536 keys, 32 heads, 1 row in 234 us, 5.2 TB/s (over a third of
+// the 608 instructions that a warp spends on 32 keys and 8 rows take codes apart; 12 warps an SM, as many as 168 registers
+// allow, issue in 58 % of the cycles); beyond, neither: eight warps an SM (249 registers) do not hide the steps from load to
+// MMA, 16 x 16384 keys, 9 rows in 315 us.  One token over 1024 keys takes 9.4 us: launch, table, page, two joins.
 #include <type_traits>
 
 #include "paged_attn.cuh"

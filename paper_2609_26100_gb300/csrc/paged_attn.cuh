@@ -35,8 +35,8 @@ __device__ __forceinline__ float ex2(float x) {
 
 // The tcgen05 kernel (paged_attn_tc.cu; head_dim 128, planned with R = 128 and whole pages) and the query rows of a KV
 // head above which a request goes there.  A page costs it the same for any number of rows, the warp-level kernel in
-// proportion to its 16-row tiles; us, warp-level / tcgen05, four requests of 4600 tokens and 32 heads: 24 rows 66 / 101,
-// 48 rows 94 / 108, 56 rows 115 / 109, 128 rows 231 / 127; 8 heads: 32 rows 29 / 39, 48 rows 34 / 41, 64 rows 42 / 43.
+// proportion to its 16-row tiles; us, warp-level / tcgen05, four requests of 4600 tokens and 32 heads: 24 rows 66 / 103,
+// 48 rows 97 / 110, 56 rows 119 / 111, 128 rows 225 / 123; 8 heads: 32 rows 28 / 40, 48 rows 33 / 42, 64 rows 41 / 42.
 constexpr int kPaTcRows = 48;
 cudaError_t paged_attn_tc_prepare();
 cudaError_t launch_paged_attention_tc(PaParams& p, int sms, cudaStream_t s);
