@@ -552,7 +552,7 @@ tss_status tss_paged_read(tss_paged* p, const tss_paged_cache* cache, int layer,
  * reach it, whatever they are.  Scores, sums and accumulators are fp32; the weights (times the values' scales) enter
  * the second product as two fp16 parts (22 bits), or one (11 bits) for bf16 outputs where some request has more than
  * 8 rows of a KV head, scaled by the largest of their row in each group of 64 dims (small ones keep what
- * stands above 2^-27 of it).  Asynchronous on `stream`.  Errors: INVALID_ARG, KV_CAPACITY, CUDA. */
+ * stands above 2^-27 of it; a scale counts as 2^-24 at least there).  Asynchronous on `stream`.  Errors: INVALID_ARG, KV_CAPACITY, CUDA. */
 typedef struct {
   const void* q;
   int64_t q_stride;
