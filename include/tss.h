@@ -532,6 +532,15 @@ typedef struct {
 tss_status tss_paged_append(tss_paged* p, const tss_paged_cache* cache, int layer, const tss_paged_batch* batch,
                             const void* k, const void* v, int64_t k_stride, int64_t v_stride, int dtype, void* stream);
 
+/* tss_qk_rope and tss_paged_append in one launch: the heads of q and k are normed and rotated as rope says; q goes to q_out,
+ * k is rounded to its type and quantised into the pages of the batch's tokens with v [rows][n_kv_heads][head_dim].  The pages
+ * and q_out get the bits that the two calls give.  rope's n_rows are the batch's, its n_k_heads and head_dim the cache's,
+ * n_q_heads any (0: keys alone); k_out may be NULL; rope's dtype is also v's; status NULL: a position outside the table is recorded in
+ * the workspace.  rot_dim 0 without gains appends k as it is.  A sequence may appear once.  Where the page table names no
+ * page the rows still reach q_out and k_out.  Asynchronous on `stream`. */
+tss_status tss_paged_append_rope(tss_paged* p, const tss_paged_cache* cache, int layer, const tss_paged_batch* batch,
+                                 const tss_rope_args* rope, const void* v, int64_t v_stride, void* stream);
+
 /* The reverse: the values of the batch's tokens, s c + z, to k, v (either may be NULL). */
 tss_status tss_paged_read(tss_paged* p, const tss_paged_cache* cache, int layer, const tss_paged_batch* batch, void* k,
                           void* v, int64_t k_stride, int64_t v_stride, int dtype, void* stream);

@@ -29,6 +29,9 @@ struct PgAttnArgs {
   const int* positions;
   int* status;
 };
+// Checks what every call on the cache has in common and copies the batch.  *rows: rows in all.
+tss_status take_batch(const tss_paged* h, const tss_paged_cache* c, int layer, const tss_paged_batch* b, PgBatch* out, long long* rows);
+cudaError_t append_rope_prepare();
 size_t pa_partial_rows(int sms, int head_dim);
 int pa_counters(int sms);
 cudaError_t pa_prepare_all();

@@ -11,107 +11,16 @@
 // Bound: HBM, each element read and written once: 4096 rows of 64 heads of 128, bf16, with norms 26 us, 5.1 TB/s.  A step of
 // 6 rows 2.3 us: launch and two dependent loads (position, table).  The next head's vectors are held as they come: widened
 // to fp32 while in flight they cost registers and 38 us.
-#include "ops.cuh"
+#include "rope.cuh"
 
 namespace tss {
 namespace {
 
-struct RopeParams {
-  int rows, hq, hk, d, rot, max_pos;
-  int splits;  // warps that share a row's head groups
-  const void *q, *k;
-  void *q_out, *k_out;
-  long long qs, ks, qos, kos;
-  const void *q_gain, *k_gain;
-  float eps;
-  const float* table;
-  const int* positions;
-  int* status;
-};
-
-constexpr int kRopeThreads = 128;
-
-// LANES: lanes of one head (a power of two, at least d / 16)
 template <typename T, int LANES, bool INTER>
 __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constant__ RopeParams p) {
-  constexpr int kHeads = 32 / LANES;  // heads of a group: one turn of a warp
   griddep_wait();
   griddep_launch();
-  const int lane = threadIdx.x & 31;
-  const long long w = static_cast<long long>(blockIdx.x) * (kRopeThreads / 32) + (threadIdx.x >> 5);
-  const long long row = w / p.splits;
-  const int part = static_cast<int>(w - row * p.splits);
-  if (row >= p.rows) return;
-  const int j = lane & (LANES - 1), sub = lane / LANES;
-  const bool live = 16 * j < p.d;
-  const bool turns = 16 * j < p.rot;
-  // elements of the lane's two vectors
-  const int rs = p.rot >> 4;
-  const int c0 = INTER || !turns ? 16 * j : 8 * j, c1 = INTER || !turns ? 16 * j + 8 : 8 * (j + rs);
-  float cs[16];
-  if (turns) {
-    int pos = p.positions[row];
-    if (pos < 0 || pos >= p.max_pos) {
-      report(p.status, kStatusCheck);
-      pos = pos < 0 ? 0 : p.max_pos - 1;
-    }
-    load_vec<float, 16>(p.table + static_cast<size_t>(pos) * p.rot + 16 * j, cs);
-  }
-  const int heads = p.hq + p.hk, step = p.splits * kHeads;
-  // the next head's vectors are on their way while this one is worked on
-  Raw8<T> next[2];
-  const auto fetch = [&](int h) {
-    if (live && h < heads) {
-      const T* x = h < p.hq ? static_cast<const T*>(p.q) + row * p.qs + static_cast<long long>(h) * p.d
-                            : static_cast<const T*>(p.k) + row * p.ks + static_cast<long long>(h - p.hq) * p.d;
-      next[0].load(x + c0);
-      next[1].load(x + c1);
-    }
-  };
-  fetch(part * kHeads + sub);
-#pragma unroll 1
-  for (int h = part * kHeads + sub; h - sub < heads; h += step) {
-    const bool on = live && h < heads, isq = h < p.hq;
-    T* y = isq ? static_cast<T*>(p.q_out) + row * p.qos + static_cast<long long>(h) * p.d
-               : static_cast<T*>(p.k_out) + row * p.kos + static_cast<long long>(h - p.hq) * p.d;
-    const T* gain = static_cast<const T*>(isq ? p.q_gain : p.k_gain);
-    float a[16];
-    next[0].to(a);
-    next[1].to(a + 8);
-    fetch(h + step);
-    // (every lane of the warp takes part in the butterfly; the condition is the same for all)
-    if (p.q_gain || p.k_gain) {
-      float ss = 0.f;
-      if (on) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) ss = fmaf(a[i], a[i], ss);
-      }
-#pragma unroll
-      for (int o = LANES / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-      if (on && gain) {
-        const float r = 1.f / sqrtf(ss / static_cast<float>(p.d) + p.eps);
-        float g[16];
-        load_vec<T, 8>(gain + c0, g);
-        load_vec<T, 8>(gain + c1, g + 8);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) a[i] = a[i] * r * g[i];
-      }
-    }
-    if (!on) continue;
-    if (turns) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        float& u = INTER ? a[2 * i] : a[i];
-        float& v = INTER ? a[2 * i + 1] : a[8 + i];
-        const float c = cs[2 * i], s = cs[2 * i + 1];
-        const float u0 = u, v0 = v;
-        u = u0 * c - v0 * s;
-        v = v0 * c + u0 * s;
-      }
-    }
-    store_vec<T, 8>(y + c0, a);
-    store_vec<T, 8>(y + c1, a + 8);
-  }
+  rope_row<T, LANES, INTER>(p, static_cast<long long>(blockIdx.x) * (kRopeThreads / 32) + (threadIdx.x >> 5), threadIdx.x & 31);
 }
 
 struct RopeFreq {
@@ -147,11 +56,9 @@ cudaError_t rope_dispatch(const RopeParams& p, bool inter, unsigned grid, cudaSt
 }
 
 }  // namespace
-}  // namespace tss
 
-using namespace tss;
-
-extern "C" tss_status tss_qk_rope(const tss_rope_args* a, void* stream) {
+tss_status take_rope(const tss_rope_args* a, bool to_pages, RopeParams* p, int* lanes) {
+  *p = RopeParams{};
   if (!a) return refuse(TSS_ERR_INVALID_ARG, "NULL argument");
   if (a->n_rows < 0 || a->n_q_heads < 0 || a->n_k_heads < 0 || a->n_q_heads > (1 << 16) || a->n_k_heads > (1 << 16))
     return refuse(TSS_ERR_INVALID_ARG, "n_rows must be >= 0 and the head counts in [0, 65536]");
@@ -171,10 +78,11 @@ extern "C" tss_status tss_qk_rope(const tss_rope_args* a, void* stream) {
   for (const auto& x : sides) {
     if (x.heads == 0) continue;
     const int64_t width = static_cast<int64_t>(x.heads) * a->head_dim;
-    if (!x.in || !x.out) return refuse(TSS_ERR_INVALID_ARG, "q and k need an input and an output");
+    const bool out = !(to_pages && &x == &sides[1] && !x.out);
+    if (!x.in || (out && !x.out)) return refuse(TSS_ERR_INVALID_ARG, "q and k need an input and an output");
     if (!aligned16(x.in) || !aligned16(x.out) || (x.gain && !aligned16(x.gain)))
       return refuse(TSS_ERR_INVALID_ARG, "q, k, their outputs and gains must be 16-byte aligned");
-    if (!good_stride(x.is, width, a->dtype) || !good_stride(x.os, width, a->dtype))
+    if (!good_stride(x.is, width, a->dtype) || (out && !good_stride(x.os, width, a->dtype)))
       return refuse(TSS_ERR_INVALID_ARG, "row strides must hold the heads and be multiples of 16 bytes");
     if (x.in == x.out && x.is != x.os) return refuse(TSS_ERR_INVALID_ARG, "in place the strides must be equal");
   }
@@ -184,35 +92,41 @@ extern "C" tss_status tss_qk_rope(const tss_rope_args* a, void* stream) {
     if (a->max_positions < 1) return refuse(TSS_ERR_INVALID_ARG, "max_positions must be >= 1");
   }
   if ((a->q_gain || a->k_gain) && !(a->eps >= 0.f)) return refuse(TSS_ERR_INVALID_ARG, "eps must be >= 0");
-  RopeParams p{};
-  p.rows = a->n_rows;
-  p.hq = a->n_q_heads;
-  p.hk = a->n_k_heads;
-  p.d = a->head_dim;
-  p.rot = a->rot_dim;
-  p.max_pos = a->max_positions;
-  p.q = a->q;
-  p.k = a->k;
-  p.q_out = a->q_out;
-  p.k_out = a->k_out;
-  p.qs = a->q_stride;
-  p.ks = a->k_stride;
-  p.qos = a->q_out_stride;
-  p.kos = a->k_out_stride;
-  p.q_gain = a->n_q_heads ? a->q_gain : nullptr;
-  p.k_gain = a->n_k_heads ? a->k_gain : nullptr;
-  p.eps = a->eps;
-  p.table = a->table;
-  p.positions = a->positions;
-  p.status = a->status;
+  p->rows = a->n_rows;
+  p->hq = a->n_q_heads;
+  p->hk = a->n_k_heads;
+  p->d = a->head_dim;
+  p->rot = a->rot_dim;
+  p->max_pos = a->max_positions;
+  p->q = a->q;
+  p->k = a->k;
+  p->q_out = a->q_out;
+  p->k_out = a->k_out;
+  p->qs = a->q_stride;
+  p->ks = a->k_stride;
+  p->qos = a->q_out_stride;
+  p->kos = a->k_out_stride;
+  p->q_gain = a->n_q_heads ? a->q_gain : nullptr;
+  p->k_gain = a->n_k_heads ? a->k_gain : nullptr;
+  p->eps = a->eps;
+  p->table = a->table;
+  p->positions = a->positions;
+  p->status = a->status;
+  *lanes = 1;
+  while (*lanes * 16 < p->d) *lanes *= 2;
+  return TSS_OK;
+}
+
+}  // namespace tss
+
+using namespace tss;
+
+extern "C" tss_status tss_qk_rope(const tss_rope_args* a, void* stream) {
+  RopeParams p;
   int lanes = 1;
-  while (lanes * 16 < p.d) lanes *= 2;
-  // A warp per (row, head group) until there are as many warps as the GPU holds; then fewer warps per
-  // row, each with more groups, so that the table row is read less often.
-  const int groups = (p.hq + p.hk + 32 / lanes - 1) / (32 / lanes);
-  const long long want = 152LL * 64;
-  p.splits = groups;
-  while (p.splits > 1 && static_cast<long long>(p.rows) * ((p.splits + 1) / 2) >= want) p.splits = (p.splits + 1) / 2;
+  const tss_status st = take_rope(a, false, &p, &lanes);
+  if (st != TSS_OK || p.rows == 0) return st;
+  p.splits = rope_splits(p.rows, p.hq + p.hk, lanes);
   const long long warps = static_cast<long long>(p.rows) * p.splits, per = kRopeThreads / 32;
   if ((warps + per - 1) / per > 0x7fffffffLL) return refuse(TSS_ERR_INVALID_ARG, "too many rows for one launch");
   const unsigned grid = static_cast<unsigned>((warps + per - 1) / per);

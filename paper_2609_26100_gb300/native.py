@@ -31,7 +31,7 @@ EXPORTS = (
     "tss_linear_static_status", "tss_verify_grouped", "tss_attention_kernel",
     "tss_qk_rope", "tss_rope_frequencies", "tss_rope_table",
     "tss_paged_page_bytes", "tss_paged_create", "tss_paged_destroy", "tss_paged_sync_status", "tss_paged_append",
-    "tss_paged_read", "tss_paged_attention", "tss_paged_inject_timeout",
+    "tss_paged_append_rope", "tss_paged_read", "tss_paged_attention", "tss_paged_inject_timeout",
     "tss_pages_create", "tss_pages_destroy", "tss_pages_sync_status", "tss_pages_reserve", "tss_pages_free",
     "tss_pages_fork", "tss_pages_compact", "tss_pages_copy",
 )
@@ -172,6 +172,7 @@ def lib() -> ctypes.CDLL:
         L.tss_paged_create.argtypes = [I, I, I, PP]
         L.tss_paged_sync_status.argtypes = [_P, _P]
         L.tss_paged_append.argtypes = [_P, cache, I, batch, _P, _P, L64, L64, I, _P]
+        L.tss_paged_append_rope.argtypes = [_P, cache, I, batch, ctypes.POINTER(TssRopeArgs), _P, L64, _P]
         L.tss_paged_read.argtypes = L.tss_paged_append.argtypes
         L.tss_paged_attention.argtypes = [_P, cache, I, batch, ctypes.POINTER(TssPagedAttn), _P]
         L.tss_paged_inject_timeout.argtypes = [_P, I]
@@ -187,7 +188,7 @@ def lib() -> ctypes.CDLL:
             getattr(L, name).argtypes = [_P]
             getattr(L, name).restype = None
         for name in ("tss_qk_rope", "tss_rope_frequencies", "tss_rope_table", "tss_paged_create", "tss_paged_sync_status",
-                     "tss_paged_append", "tss_paged_read", "tss_paged_attention", "tss_pages_create",
+                     "tss_paged_append", "tss_paged_append_rope", "tss_paged_read", "tss_paged_attention", "tss_pages_create",
                      "tss_pages_sync_status", "tss_pages_reserve", "tss_pages_free", "tss_pages_fork", "tss_pages_compact",
                      "tss_pages_copy"):
             getattr(L, name).restype = ctypes.c_int
@@ -293,10 +294,11 @@ def rope_table(inv_freq: Sequence[float], table, attention_factor: float = 1.0, 
 
 
 def rope_args(q, k, q_out, k_out, positions, table, q_gain=None, k_gain=None, eps: float = 1e-6, interleaved: bool = False,
-              status=None) -> TssRopeArgs:
+              status=None, to_pages: bool = False) -> TssRopeArgs:
     """Arguments of tss_qk_rope from tensors of one GPU: q, k [rows][heads][head_dim] (either may be None) and their
     outputs (q_out may be q), positions int32 [rows], table [positions][pairs][2] float32 (None: no rotation),
-    gains [head_dim] (None: no norm).  The structure keeps the tensors alive."""
+    gains [head_dim] (None: no norm).  to_pages: for Kv4Cache.append_rope, where k_out may be None.  The structure keeps
+    the tensors alive."""
     one = q if q is not None else k
     if one is None:
         raise ValueError("q or k is wanted")
@@ -311,14 +313,16 @@ def rope_args(q, k, q_out, k_out, positions, table, q_gain=None, k_gain=None, ep
         if x is None:
             continue
         n, h, d, stride = _rows(x, name)
-        _same(x, y, name)
+        if y is not None or name == "q" or not to_pages:
+            _same(x, y, name)
         if (n, d, dtype_code(x)) != (a.n_rows, a.head_dim, a.dtype):
             raise ValueError("q and k must agree in rows, head_dim and type")
         setattr(a, f"n_{name}_heads", h)
         setattr(a, name, x.data_ptr())
         setattr(a, name + "_stride", stride)
-        setattr(a, name + "_out", y.data_ptr())
-        setattr(a, name + "_out_stride", _rows(y, name + "_out")[3])
+        if y is not None:
+            setattr(a, name + "_out", y.data_ptr())
+            setattr(a, name + "_out_stride", _rows(y, name + "_out")[3])
         if gain is not None:
             if tuple(gain.shape) != (d,) or gain.dtype != x.dtype or gain.device != x.device or not gain.is_contiguous():
                 raise ValueError(f"{name}_gain: contiguous [head_dim] of the same type and device is wanted")
@@ -335,6 +339,7 @@ def rope_args(q, k, q_out, k_out, positions, table, q_gain=None, k_gain=None, ep
     if status is not None and (str(status.dtype) != "torch.int32" or not status.is_cuda):
         raise ValueError("status: an int32 tensor on the GPU is wanted")
     a.status = _ptr(status)
+    a._to_pages = to_pages
     a._keep = (q, k, q_out, k_out, positions, table, q_gain, k_gain, status)
     return a
 

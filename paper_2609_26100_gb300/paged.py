@@ -192,6 +192,7 @@ class Kv4Cache:
                                            table.shape[0], table.shape[1])
         self._cache_ref = ctypes.byref(self._cache)
         self._c_append, self._c_read, self._c_attention = lib().tss_paged_append, lib().tss_paged_read, lib().tss_paged_attention
+        self._c_append_rope = lib().tss_paged_append_rope
         self.pages: Optional[PagePool] = None
         h = _P()
         with torch.cuda.device(self._dev):
@@ -243,6 +244,18 @@ class Kv4Cache:
                            _row_stride(v, shape, dev, "v"), _code(k), _stream_of(self._dev, stream))
         if s:
             check(s, "tss_paged_append")
+
+    def append_rope(self, layer: int, batch, args: native.TssRopeArgs, v: torch.Tensor, stream=None) -> None:
+        """native.qk_rope and append in one launch: args (native.rope_args with to_pages=True) name the rows of q and k, which
+        are normed and rotated, q to its output, k with v [rows][kv heads][head_dim] into the pages of the batch's tokens."""
+        if getattr(args, "_device", self._dev) != self._dev:
+            raise ValueError("args: tensors on the pool's GPU are wanted")
+        if _code(v) != args.dtype:
+            raise ValueError("v: the type of q and k is wanted")
+        s = self._c_append_rope(self._h, self._cache_ref, layer, batch.ref, ctypes.byref(args), v.data_ptr(),
+                                _row_stride(v, (batch.rows, self.n_kv_heads, self.head_dim), self._dev, "v"), _stream_of(self._dev, stream))
+        if s:
+            check(s, "tss_paged_append_rope")
 
     def read(self, layer: int, batch, k: Optional[torch.Tensor], v: Optional[torch.Tensor], stream=None) -> None:
         """The values that the batch's tokens are held as, to k and v (either may be None)."""
