@@ -619,6 +619,16 @@ tss_status tss_pages_free(tss_pages* h, const tss_page_tables* t, int n, const i
 tss_status tss_pages_fork(tss_pages* h, const tss_page_tables* t, void* const* layer, int n_layers, size_t page_bytes,
                           int n, const int32_t* src, const int32_t* dst, const int32_t* shared, const int32_t* total,
                           void* stream);
+/* Sequences change places as parent says, which is read on the device: after a selection of beams its result, without a host
+ * wait.  seq HOST, distinct; parent int32 DEVICE [n]: sequence seq[i] becomes the first total[p] pages of what seq[p] held,
+ * p = parent[i] in [0, n), or nothing where parent[i] = -1.  shared, total HOST, of the entries as parents: the
+ * first shared[p] pages are the same ones in every place that goes on with p; the rest stay with one of them (p itself if it goes on
+ * with its own pages, else the lowest i) and are copied in every layer for the others, into the lowest pages that were free
+ * before the call, in the order of i.  What no place goes on with is given back.  A page id outside the pool in a shared place is
+ * moved as it is, and recorded. */
+tss_status tss_pages_reorder(tss_pages* h, const tss_page_tables* t, void* const* layer, int n_layers, size_t page_bytes,
+                             int n, const int32_t* seq, const int32_t* parent, const int32_t* shared, const int32_t* total,
+                             void* stream);
 /* Move the pages in use to the ids below their number, in every layer: the lowest page past it to the
  * lowest free one, and so on; the other pages stay.  The new table and counts go to table_out and
  * refs_out, which may be t's own (held does not change). */
@@ -628,6 +638,40 @@ tss_status tss_pages_compact(tss_pages* h, const tss_page_tables* t, int32_t* ta
  * (others are skipped and recorded); no dst is another entry's src or dst. */
 tss_status tss_pages_copy(tss_pages* h, void* const* layer, int n_layers, size_t page_bytes, int n, const int32_t* src,
                           const int32_t* dst, void* stream);
+
+/* Beam search's choice: of each of n_groups groups of n_beams rows the n_keep best continuations (beam b, token t),
+ *   value = score[b] + logits[b][t] - ln sum_u exp(logits[b][u]),
+ * largest first, ties to the lowest b * vocab + t.
+ *   logits [n_groups * n_beams][vocab] DEVICE, TSS_DTYPE_*, stride elements between rows, aligned to an element.
+ *   score [rows] fp32 DEVICE, or NULL (zeros): the beams' values so far; a beam of -infinity offers nothing (all but the first in
+ *     a search's first step).
+ *   done [rows] int32 DEVICE, or NULL: a beam that is not 0 here is finished; it offers itself, with end_token and its score.
+ *   score_out (fp32; may be score where n_keep = n_beams), parent (a row of logits: group * n_beams + beam), token (both int32): [n_groups][n_keep]
+ *     DEVICE.  Where a group offers less than n_keep the rest gets -infinity, -1, -1.
+ * A logit of -1e38 or less is masked.  A row that has a NaN or a logit above 1e38, or whose score is NaN or +infinity,
+ * offers nothing, and TSS_ERR_DEVICE_CHECK is recorded.  Values are right to about 1e-8 (fp32 logits, sums and choice in 64 bits)
+ * and rounded once; equal rows have equal values, and results do not depend on timing.
+ * tss_beam_create makes the workspace for rows of `vocab` logits (at most 2^24), at most max_rows of them (2^20) and n_keep up to
+ * max_keep (128); n_beams is at most 64.  Calls that share one must not overlap on different streams.  Asynchronous on `stream`.
+ * Errors: INVALID_ARG, UNSUPPORTED_ARCH, OUT_OF_MEMORY, CUDA. */
+typedef struct tss_beam tss_beam;
+typedef struct {
+  int n_groups, n_beams, n_keep, dtype;
+  const void* logits;
+  int64_t stride;
+  const float* score;
+  const int32_t* done;
+  int end_token;
+  float* score_out;
+  int32_t* parent;
+  int32_t* token;
+} tss_beam_args;
+tss_status tss_beam_create(int max_rows, int vocab, int max_keep, tss_beam** out);
+/* After the caller's streams are idle; NULL is a no-op. */
+void tss_beam_destroy(tss_beam* h);
+/* Synchronise `stream`, then return and clear the status word. */
+tss_status tss_beam_sync_status(tss_beam* h, void* stream);
+tss_status tss_beam_select(tss_beam* h, const tss_beam_args* args, void* stream);
 
 const char* tss_status_string(tss_status s);
 /* Message of the last error reported to the calling thread ("" if none). */

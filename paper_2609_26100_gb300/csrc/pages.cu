@@ -17,6 +17,7 @@ struct tss_pages {
   int* go;      // device word: the last choosing launch found its pages (1) or left everything as it was (0)
   int* moves;   // device [1 + 2 * n_pages]: their number, then sources, then destinations (or chosen pages)
   int* map;     // device [n_pages]: new id of every page
+  int* plan;    // device [4][64]: a reorder's parents, first copies, pages held before; [3][0] the most held
 };
 
 namespace tss {
@@ -268,6 +269,131 @@ __global__ void __launch_bounds__(kCopyThreads) fork_kernel(const __grid_constan
   }
 }
 
+// reorder.  Entry i takes the first d[p] pages of entry p = parent[i] (a: sequences; c: pages of p that its takers share).
+// The others are the taker's that goes on in p's own place, or else its first, the keeper; the rest get copies.
+//
+// First part: what each entry takes, the copies (sources to src, pages that were free before the call to ids), or nothing.
+__device__ __forceinline__ bool keeps(const int* parent, int n, int i) {
+  const int p = parent[i];
+  if (parent[p] == p) return i == p;
+  for (int j = 0; j < i; ++j)
+    if (parent[j] == p) return false;
+  return true;
+}
+__global__ void __launch_bounds__(kPlanThreads) reorder_choose_kernel(const __grid_constant__ SeqList list, PoolTables t, const int* parents,
+                                                                      int* plan, int* src, int* ids, int* n_copies, int* go) {
+  __shared__ uint32_t bits[kRoundWords];
+  __shared__ int scratch[kPlanThreads / 32], parent[kMaxCalls], off[kMaxCalls + 1], bad, most;
+  const int tid = threadIdx.x;
+  griddep_wait();
+  griddep_launch();
+  if (tid == 0) bad = most = 0;
+  if (tid < list.n) parent[tid] = parents[tid];
+  __syncthreads();
+  int held = 0;
+  if (tid < list.n) {
+    held = t.held[list.a[tid]];
+    const int p = parent[tid];
+    if (held < 0 || held > t.max_pages || p < -1 || p >= list.n) bad = 1;
+    if (p >= 0 && p < list.n && t.held[list.a[p]] < list.d[p]) bad = 1;
+    atomicMax(&most, held);
+  }
+  __syncthreads();
+  if (!bad && tid < list.n) {
+    const int p = parent[tid];
+    off[tid + 1] = p < 0 || keeps(parent, list.n, tid) ? 0 : list.d[p] - list.c[p];
+  }
+  __syncthreads();
+  if (!bad && tid == 0) {
+    off[0] = 0;
+    for (int i = 0; i < list.n; ++i) off[i + 1] = min(off[i] + off[i + 1], t.n_pages + 1);
+  }
+  __syncthreads();
+  const int need = bad ? 0 : off[list.n];
+  if (!bad && need <= t.n_pages)  // every page that will be copied has to be one of the pool that somebody holds
+    for (int i = tid >> 5; i < list.n; i += kPlanThreads / 32) {
+      const int p = parent[i];
+      for (int x = tid & 31; x < off[i + 1] - off[i]; x += 32) {
+        const int page = t.table[static_cast<long long>(list.a[p]) * t.max_pages + list.c[p] + x];
+        if (page < 0 || page >= t.n_pages || t.refs[page] < 1)
+          bad = 1;
+        else
+          src[off[i] + x] = page;
+      }
+    }
+  __syncthreads();
+  if (bad) {
+    if (tid == 0) {
+      report(t.status, kStatusCheck);
+      *go = 0;
+    }
+    return;
+  }
+  const bool room = need <= t.n_pages && (need == 0 || lowest_free(t.refs, t.n_pages, need, ids, bits, scratch) == need);
+  if (tid < list.n) {
+    const int p = parent[tid];
+    plan[tid] = p;
+    plan[kMaxCalls + tid] = off[tid + 1] > off[tid] ? off[tid] : -1;
+    plan[2 * kMaxCalls + tid] = held;
+  }
+  if (tid == 0) {
+    if (!room) report(t.status, TSS_ERR_KV_CAPACITY);
+    plan[3 * kMaxCalls] = most;
+    *n_copies = need;
+    *go = room;
+  }
+}
+
+// Second part: CTAs [0, col_ctas) change 64 columns each of the entries' rows, and the counts of what changes (a column depends
+// on no other, so that rows may change places in place); the others copy pages.
+constexpr int kReorderCols = 64;
+__global__ void __launch_bounds__(kCopyThreads) reorder_kernel(const __grid_constant__ SeqList list, PoolTables t, const __grid_constant__ Layers ly,
+                                                               const int* plan, const int* src, const int* ids, const int* n_copies,
+                                                               const int* go, int col_ctas) {
+  __shared__ int old[kMaxCalls][kReorderCols];
+  griddep_wait();
+  griddep_launch();
+  if (*go == 0) return;
+  const int cta = blockIdx.x, tid = threadIdx.x;
+  if (cta >= col_ctas) {
+    const int pieces = static_cast<int>((ly.page_bytes + kPiece - 1) / kPiece);
+    const long long units = static_cast<long long>(*n_copies) * ly.n * pieces;
+    for (long long u = cta - col_ctas; u < units; u += gridDim.x - col_ctas) {
+      const int c = static_cast<int>(u / (static_cast<long long>(ly.n) * pieces));
+      const int rest = static_cast<int>(u - static_cast<long long>(c) * ly.n * pieces);
+      copy_piece(ly.base[rest / pieces], ly.page_bytes, src[c], ids[c], rest % pieces);
+    }
+    return;
+  }
+  if (cta == 0 && tid < list.n) t.held[list.a[tid]] = plan[tid] < 0 ? 0 : list.d[plan[tid]];
+  constexpr int kStep = kCopyThreads / kReorderCols;
+  const int c = tid % kReorderCols, first = tid / kReorderCols;
+  const auto valid = [&](int page) { return page >= 0 && page < t.n_pages; };
+  for (long long x0 = static_cast<long long>(cta) * kReorderCols; x0 < plan[3 * kMaxCalls]; x0 += static_cast<long long>(col_ctas) * kReorderCols) {
+    const int x = static_cast<int>(x0) + c;
+    for (int i = first; i < list.n; i += kStep)
+      old[i][c] = x < plan[2 * kMaxCalls + i] ? t.table[static_cast<long long>(list.a[i]) * t.max_pages + x] : -1;
+    __syncthreads();
+    for (int i = first; i < list.n; i += kStep) {
+      const int p = plan[i], copy = plan[kMaxCalls + i], was = old[i][c];
+      int now = -1;
+      if (p >= 0 && x < list.d[p]) {
+        now = copy >= 0 && x >= list.c[p] ? ids[copy + x - list.c[p]] : old[p][c];
+        if (!valid(now)) report(t.status, kStatusCheck);
+      }
+      if (x >= plan[2 * kMaxCalls + i] && now < 0) continue;
+      if (now == was && valid(was)) continue;
+      if (x < plan[2 * kMaxCalls + i] && (!valid(was) || atomicSub(&t.refs[was], 1) <= 0)) {
+        if (valid(was)) atomicAdd(&t.refs[was], 1);
+        report(t.status, kStatusCheck);
+      }
+      if (valid(now)) atomicAdd(&t.refs[now], 1);
+      t.table[static_cast<long long>(list.a[i]) * t.max_pages + x] = now;
+    }
+    __syncthreads();
+  }
+}
+
 // compact, first part: moves[0] = number of moves, then their sources and destinations; the map of ids; the
 // new counts
 __global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(PoolTables t, int* refs_out, int* moves, int* map) {
@@ -440,6 +566,7 @@ extern "C" tss_status tss_pages_create(int n_seqs, int max_pages, int n_pages, t
   if (e == cudaSuccess) e = zero_now(h->status, 256);
   if (e == cudaSuccess) e = cudaMalloc(&h->moves, sizeof(int) * (1 + 2 * static_cast<size_t>(n_pages)));
   if (e == cudaSuccess) e = cudaMalloc(&h->map, sizeof(int) * static_cast<size_t>(n_pages));
+  if (e == cudaSuccess) e = cudaMalloc(&h->plan, sizeof(int) * 4 * kMaxCalls);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(compact_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxPoolPages / 8);
   if (e != cudaSuccess) {
     tss_pages_destroy(h);
@@ -456,6 +583,7 @@ extern "C" void tss_pages_destroy(tss_pages* h) {
   cudaFree(h->status);
   cudaFree(h->moves);
   cudaFree(h->map);
+  cudaFree(h->plan);
   delete h;
 }
 
@@ -542,6 +670,38 @@ extern "C" tss_status tss_pages_fork(tss_pages* h, const tss_page_tables* t, voi
   st = launched(launch_k(fork_choose_kernel, dim3(1), dim3(kPlanThreads), 0, s, true, list, pt, static_cast<int>(need), ids, h->go));
   if (st != TSS_OK) return st;
   return launched(launch_k(fork_kernel, dim3(n + copy_grid(need, ly, h->sms)), dim3(kCopyThreads), 0, s, true, list, pt, ly, ids, h->go));
+}
+
+extern "C" tss_status tss_pages_reorder(tss_pages* h, const tss_page_tables* t, void* const* layer, int n_layers, size_t page_bytes, int n,
+                                        const int32_t* seq, const int32_t* parent, const int32_t* shared, const int32_t* total, void* stream) {
+  PoolTables pt;
+  Layers ly{};
+  tss_status st = take_tables(h, t, &pt);
+  if (st == TSS_OK) st = take_seqs(h, n, seq, "seq must be in [0, n_seqs)");
+  if (st == TSS_OK) st = take_layers(layer, n_layers, page_bytes, &ly);
+  if (st != TSS_OK) return st;
+  if (n == 0) return TSS_OK;
+  if (!parent || !shared || !total) return refuse(TSS_ERR_INVALID_ARG, "NULL argument");
+  if (reinterpret_cast<uintptr_t>(parent) & 3u) return refuse(TSS_ERR_INVALID_ARG, "parent is not aligned to its elements");
+  if (!distinct(seq, n)) return refuse(TSS_ERR_INVALID_ARG, "a sequence appears twice");
+  SeqList list{};
+  list.n = n;
+  int tail = 0;
+  for (int i = 0; i < n; ++i) {
+    if (shared[i] < 0 || total[i] < shared[i]) return refuse(TSS_ERR_INVALID_ARG, "0 <= shared <= total is wanted");
+    if (total[i] > h->max_pages) return refuse(TSS_ERR_KV_CAPACITY, "total exceeds max_pages");
+    list.a[i] = seq[i];
+    list.c[i] = shared[i];
+    list.d[i] = total[i];
+    tail = tail > total[i] - shared[i] ? tail : total[i] - shared[i];
+  }
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  int *src = h->moves + 1, *ids = h->moves + 1 + h->n_pages;
+  st = launched(launch_k(reorder_choose_kernel, dim3(1), dim3(kPlanThreads), 0, s, true, list, pt, parent, h->plan, src, ids, h->moves, h->go));
+  if (st != TSS_OK) return st;
+  const int cols = (h->max_pages + kReorderCols - 1) / kReorderCols, col_ctas = cols < h->sms ? cols : h->sms;
+  return launched(launch_k(reorder_kernel, dim3(col_ctas + copy_grid(static_cast<long long>(n - 1) * tail, ly, h->sms)), dim3(kCopyThreads), 0, s,
+                           true, list, pt, ly, h->plan, src, ids, h->moves, h->go, col_ctas));
 }
 
 extern "C" tss_status tss_pages_compact(tss_pages* h, const tss_page_tables* t, int32_t* table_out, int32_t* refs_out, void* const* layer,

@@ -33,7 +33,8 @@ EXPORTS = (
     "tss_paged_page_bytes", "tss_paged_create", "tss_paged_destroy", "tss_paged_sync_status", "tss_paged_append",
     "tss_paged_append_rope", "tss_paged_read", "tss_paged_attention", "tss_paged_inject_timeout",
     "tss_pages_create", "tss_pages_destroy", "tss_pages_sync_status", "tss_pages_reserve", "tss_pages_free",
-    "tss_pages_fork", "tss_pages_compact", "tss_pages_copy",
+    "tss_pages_fork", "tss_pages_reorder", "tss_pages_compact", "tss_pages_copy",
+    "tss_beam_create", "tss_beam_destroy", "tss_beam_sync_status", "tss_beam_select",
 )
 TSS_DTYPE_BF16 = 0
 TSS_DTYPE_F16 = 1
@@ -118,6 +119,12 @@ class TssPageTables(ctypes.Structure):
     _fields_ = [("table", _P), ("held", _P), ("refs", _P)]
 
 
+class TssBeamArgs(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("n_groups", "n_beams", "n_keep", "dtype")] + [
+        ("logits", _P), ("stride", ctypes.c_int64), ("score", _P), ("done", _P), ("end_token", ctypes.c_int), ("score_out", _P),
+        ("parent", _P), ("token", _P)]
+
+
 _lib = None
 
 
@@ -182,15 +189,19 @@ def lib() -> ctypes.CDLL:
         L.tss_pages_reserve.argtypes = [_P, tables, I, _P, _P, _P]
         L.tss_pages_free.argtypes = [_P, tables, I, _P, _P, _P]
         L.tss_pages_fork.argtypes = [_P, tables, PP, I, ctypes.c_size_t, I, _P, _P, _P, _P, _P]
+        L.tss_pages_reorder.argtypes = L.tss_pages_fork.argtypes
         L.tss_pages_compact.argtypes = [_P, tables, _P, _P, PP, I, ctypes.c_size_t, _P]
         L.tss_pages_copy.argtypes = [_P, PP, I, ctypes.c_size_t, I, _P, _P, _P]
-        for name in ("tss_paged_destroy", "tss_pages_destroy"):
+        L.tss_beam_create.argtypes = [I, I, I, PP]
+        L.tss_beam_sync_status.argtypes = [_P, _P]
+        L.tss_beam_select.argtypes = [_P, ctypes.POINTER(TssBeamArgs), _P]
+        for name in ("tss_paged_destroy", "tss_pages_destroy", "tss_beam_destroy"):
             getattr(L, name).argtypes = [_P]
             getattr(L, name).restype = None
         for name in ("tss_qk_rope", "tss_rope_frequencies", "tss_rope_table", "tss_paged_create", "tss_paged_sync_status",
                      "tss_paged_append", "tss_paged_append_rope", "tss_paged_read", "tss_paged_attention", "tss_pages_create",
-                     "tss_pages_sync_status", "tss_pages_reserve", "tss_pages_free", "tss_pages_fork", "tss_pages_compact",
-                     "tss_pages_copy"):
+                     "tss_pages_sync_status", "tss_pages_reserve", "tss_pages_free", "tss_pages_fork", "tss_pages_reorder",
+                     "tss_pages_compact", "tss_pages_copy", "tss_beam_create", "tss_beam_sync_status", "tss_beam_select"):
             getattr(L, name).restype = ctypes.c_int
         for name in ("tss_create", "tss_set_skip_config", "tss_clear_skip_config", "tss_sparsity_ratio",
                      "tss_active_layer_count", "tss_verify", "tss_verify_profiled", "tss_prefill", "tss_sync_status",

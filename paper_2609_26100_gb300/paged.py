@@ -102,7 +102,7 @@ class PagePool:
         self._tables = native.TssPageTables(table.data_ptr(), held.data_ptr(), refs.data_ptr())
         self._ref = ctypes.byref(self._tables)
         h = _P()
-        self._c_free, self._c_fork = lib().tss_pages_free, lib().tss_pages_fork
+        self._c_free, self._c_fork, self._c_reorder = lib().tss_pages_free, lib().tss_pages_fork, lib().tss_pages_reorder
         with torch.cuda.device(dev):
             check(lib().tss_pages_create(self.n_seqs, self.max_pages, self.n_pages, ctypes.byref(h)), "tss_pages_create")
         self._h = h
@@ -154,6 +154,23 @@ class PagePool:
                          self._stream(stream))
         if s:
             check(s, "tss_pages_fork")
+
+    def reorder(self, seqs: Sequence[int], parent: torch.Tensor, tokens: Sequence[int], stream=None) -> None:
+        """seqs[i] becomes the first tokens[p] tokens of what seqs[p] was, p = parent[i] (int32 on the GPU, read there; -1:
+        nothing): full pages are shared, a part-filled last one stays with one of those that go on with p and is copied for the
+        others."""
+        n = len(seqs)
+        if len(tokens) != n:
+            raise ValueError("seqs and tokens differ in length")
+        if parent.numel() != n:
+            raise ValueError("parent: an entry for each of seqs is wanted")
+        _ints(parent, parent.shape, self._dev, "parent")
+        a = _host((*seqs, *[t // PAGE_TOKENS for t in tokens], *_pages(tokens)))  # sequences, pages to share, pages in all
+        at, step = a.buffer_info()[0], n * a.itemsize
+        s = self._c_reorder(self._h, self._ref, self._ptrs, self.n_layers, self.page_bytes, n, at, parent.data_ptr(), at + step,
+                            at + 2 * step, self._stream(stream))
+        if s:
+            check(s, "tss_pages_reorder")
 
     def compact(self, table_out: Optional[torch.Tensor] = None, refs_out: Optional[torch.Tensor] = None, stream=None) -> None:
         """Move the pages in use to the lowest ids; the new table and counts replace the pool's, or go to the
