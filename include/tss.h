@@ -499,6 +499,9 @@ size_t tss_paged_page_bytes(int n_kv_heads, int head_dim);
  * INVALID_ARG, UNSUPPORTED_ARCH, OUT_OF_MEMORY, CUDA. */
 typedef struct tss_paged tss_paged;
 tss_status tss_paged_create(int n_q_heads, int n_kv_heads, int head_dim, tss_paged** out);
+/* The same with room for the results over shared keys of tss_paged_attention_shared calls of up to shared_rows rows (0..8192;
+ * n_q_heads * (4 head_dim + 8) bytes each). */
+tss_status tss_paged_create_shared(int n_q_heads, int n_kv_heads, int head_dim, int shared_rows, tss_paged** out);
 /* After the caller's streams are idle; NULL is a no-op. */
 void tss_paged_destroy(tss_paged* p);
 /* Synchronise `stream`, then return and clear the status word: TSS_OK, TSS_ERR_DEVICE_CHECK (a page table
@@ -577,8 +580,23 @@ typedef struct {
 tss_status tss_paged_attention(tss_paged* p, const tss_paged_cache* cache, int layer, const tss_paged_batch* batch,
                                const tss_paged_attn* args, void* stream);
 
-/* Fault injection for tests, as tss_inject_timeout: in the next n_calls calls of tss_paged_attention that launch
- * anything, the first warp of the first CTA copies no page (or, for blocks of many rows, the CTA issues no MMA), so
+/* tss_paged_attention for sequences that share the pages of their first tokens (tss_pages_fork, _reorder): the keys of the
+ * shared pages are read, and their products taken, once for all rows of a group.  HOST arrays: group g is the batch's next
+ * n_req[g] requests (the groups are the whole batch, in its order), whose sequences have the same pages for the first shared[g]
+ * tokens (rounded down to whole pages); shared[g] is at most the first token of each of them that has rows.  The pages are
+ * looked up in the first such sequence: where the others' differ, that is what their rows see.  Everything else is as in tss_paged_attention; weights take
+ * two fp16 parts or one as there, by the rows of a group for its shared keys.  The workspace is one of tss_paged_create_shared with room
+ * for the batch's rows; else INVALID_ARG. */
+typedef struct {
+  int n_groups;
+  const int32_t* n_req;
+  const int32_t* shared;
+} tss_paged_groups;
+tss_status tss_paged_attention_shared(tss_paged* p, const tss_paged_cache* cache, int layer, const tss_paged_batch* batch,
+                                      const tss_paged_groups* groups, const tss_paged_attn* args, void* stream);
+
+/* Fault injection for tests, as tss_inject_timeout: in the next n_calls calls of tss_paged_attention (or
+ * _shared: its first launch) that launch anything, the first warp of the first CTA copies no page (or, for blocks of many rows, the CTA issues no MMA), so
  * that its wait runs out after 2 s: the call returns on the device, tss_paged_sync_status reports
  * TSS_ERR_TIMEOUT, that call's outputs are undefined and the next call runs normally.  0 cancels. */
 tss_status tss_paged_inject_timeout(tss_paged* p, int n_calls);

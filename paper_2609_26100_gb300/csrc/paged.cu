@@ -207,12 +207,17 @@ extern "C" size_t tss_paged_page_bytes(int n_kv_heads, int head_dim) {
 }
 
 extern "C" tss_status tss_paged_create(int n_q_heads, int n_kv_heads, int head_dim, tss_paged** out) {
+  return tss_paged_create_shared(n_q_heads, n_kv_heads, head_dim, 0, out);
+}
+
+extern "C" tss_status tss_paged_create_shared(int n_q_heads, int n_kv_heads, int head_dim, int shared_rows, tss_paged** out) {
   if (!out) return refuse(TSS_ERR_INVALID_ARG, "out is NULL");
   *out = nullptr;
   if (head_dim != 64 && head_dim != 128) return refuse(TSS_ERR_INVALID_ARG, "head_dim must be 64 or 128");
   if (n_kv_heads < 1 || n_kv_heads > 1024) return refuse(TSS_ERR_INVALID_ARG, "n_kv_heads must be in [1, 1024]");
   if (n_q_heads < 1 || n_q_heads % n_kv_heads || n_q_heads / n_kv_heads > 64)
     return refuse(TSS_ERR_INVALID_ARG, "n_q_heads must be a multiple of n_kv_heads, at most 64 times it");
+  if (shared_rows < 0 || shared_rows > kPgMaxReq * kPgMaxRows) return refuse(TSS_ERR_INVALID_ARG, "shared_rows must be in [0, 8192]");
   int dev = 0, sms = 0;
   const tss_status st = this_device(&dev, &sms);
   if (st != TSS_OK) return st;
@@ -232,6 +237,10 @@ extern "C" tss_status tss_paged_create(int n_q_heads, int n_kv_heads, int head_d
   if (e == cudaSuccess) e = cudaMalloc(&h->part_ml, rows * sizeof(float2));
   if (e == cudaSuccess) e = cudaMalloc(&h->counters, pa_counters(sms) * sizeof(int));
   if (e == cudaSuccess) e = zero_now(h->counters, pa_counters(sms) * sizeof(int));
+  const size_t share = static_cast<size_t>(shared_rows) * n_q_heads;
+  h->share_rows = shared_rows;
+  if (e == cudaSuccess && share) e = cudaMalloc(&h->share_o, share * head_dim * sizeof(float));
+  if (e == cudaSuccess && share) e = cudaMalloc(&h->share_ml, share * sizeof(float2));
   if (e != cudaSuccess) {
     tss_paged_destroy(h);
     const tss_status r = refuse_cuda(e, "workspace");
@@ -247,6 +256,8 @@ extern "C" void tss_paged_destroy(tss_paged* h) {
   cudaFree(h->part_o);
   cudaFree(h->part_ml);
   cudaFree(h->counters);
+  cudaFree(h->share_o);
+  cudaFree(h->share_ml);
   delete h;
 }
 
@@ -280,11 +291,15 @@ extern "C" tss_status tss_paged_read(tss_paged* h, const tss_paged_cache* cache,
   return quant_call(h, cache, layer, batch, nullptr, nullptr, k, v, k_stride, v_stride, dtype, false, stream);
 }
 
-extern "C" tss_status tss_paged_attention(tss_paged* h, const tss_paged_cache* cache, int layer, const tss_paged_batch* batch,
-                                          const tss_paged_attn* a, void* stream) {
-  PgAttnArgs p{};
-  PgBatch b;
-  long long rows = 0;
+namespace tss {
+namespace {
+
+// Checks a call of the attention and lays it out; *rows 0: nothing to do.
+tss_status take_attention(const tss_paged* h, const tss_paged_cache* cache, int layer, const tss_paged_batch* batch, const tss_paged_attn* a,
+                          PgAttnArgs* out, PgBatch* batch_out, long long* rows_out) {
+  PgAttnArgs& p = *out;
+  PgBatch& b = *batch_out;
+  long long& rows = *rows_out;
   const tss_status st = take_batch(h, cache, layer, batch, &b, &rows);
   if (st != TSS_OK) return st;
   if (!a) return refuse(TSS_ERR_INVALID_ARG, "NULL argument");
@@ -320,8 +335,57 @@ extern "C" tss_status tss_paged_attention(tss_paged* h, const tss_paged_cache* c
   p.mask = reinterpret_cast<const unsigned long long*>(a->mask);
   p.positions = a->window ? a->positions : nullptr;
   p.status = h->status;
-  bool too_large = false;
-  const cudaError_t e = launch_paged_attention(h, p, b, static_cast<cudaStream_t>(stream), &too_large);
+  p.share_o = h->share_o;
+  p.share_ml = h->share_ml;
+  return TSS_OK;
+}
+
+tss_status attention_launched(cudaError_t e, bool too_large) {
   if (too_large) return refuse(TSS_ERR_INVALID_ARG, "too many (page, head, row tile) units in one call");
   return e == cudaSuccess ? TSS_OK : refuse_cuda(e, "launch");
+}
+
+}  // namespace
+}  // namespace tss
+
+extern "C" tss_status tss_paged_attention(tss_paged* h, const tss_paged_cache* cache, int layer, const tss_paged_batch* batch,
+                                          const tss_paged_attn* a, void* stream) {
+  PgAttnArgs p{};
+  PgBatch b;
+  long long rows = 0;
+  const tss_status st = take_attention(h, cache, layer, batch, a, &p, &b, &rows);
+  if (st != TSS_OK || rows == 0) return st;
+  bool too_large = false;
+  const cudaError_t e = launch_paged_attention(h, p, b, static_cast<cudaStream_t>(stream), &too_large);
+  return attention_launched(e, too_large);
+}
+
+extern "C" tss_status tss_paged_attention_shared(tss_paged* h, const tss_paged_cache* cache, int layer, const tss_paged_batch* batch,
+                                                 const tss_paged_groups* groups, const tss_paged_attn* a, void* stream) {
+  PgAttnArgs p{};
+  PgBatch b;
+  long long rows = 0;
+  const tss_status st = take_attention(h, cache, layer, batch, a, &p, &b, &rows);
+  if (st != TSS_OK) return st;
+  if (!groups) return refuse(TSS_ERR_INVALID_ARG, "NULL argument");
+  if (groups->n_groups < 1 || groups->n_groups > b.n_req || !groups->n_req || !groups->shared)
+    return refuse(TSS_ERR_INVALID_ARG, "n_groups in [1, the batch's n_req], n_req and shared are wanted");
+  PgGroups g;
+  g.n = groups->n_groups;
+  int at = 0;
+  for (int i = 0; i < g.n; ++i) {
+    if (groups->n_req[i] < 1 || groups->n_req[i] > b.n_req - at) return refuse(TSS_ERR_INVALID_ARG, "the groups' requests must be the batch's");
+    if (groups->shared[i] < 0) return refuse(TSS_ERR_INVALID_ARG, "shared must be >= 0");
+    for (int j = at; j < at + groups->n_req[i]; ++j)
+      if (b.r[j].n && b.r[j].first < groups->shared[i]) return refuse(TSS_ERR_INVALID_ARG, "shared exceeds a request's first token");
+    g.reqs[i] = groups->n_req[i];
+    g.shared[i] = groups->shared[i] / kPgTokens * kPgTokens;
+    at += groups->n_req[i];
+  }
+  if (at != b.n_req) return refuse(TSS_ERR_INVALID_ARG, "the groups' requests must be the batch's");
+  if (rows > h->share_rows) return refuse(TSS_ERR_INVALID_ARG, "more rows than the workspace was made for (shared_rows)");
+  if (rows == 0) return TSS_OK;
+  bool too_large = false;
+  const cudaError_t e = launch_paged_attention_shared(h, p, b, g, static_cast<cudaStream_t>(stream), &too_large);
+  return attention_launched(e, too_large);
 }

@@ -11,6 +11,9 @@ struct tss_paged {
   float2* part_ml;
   int* counters;    // device [pa_counters], zero between launches
   int inject;       // attention launches still to be made to run out of time (tests)
+  int share_rows;   // rows that a shared attention may have
+  float* share_o;   // device [share_rows][hq][d]: results over the shared keys, unnormalised
+  float2* share_ml; // device [share_rows][hq]: their references and sums
 };
 
 namespace tss {
@@ -28,6 +31,10 @@ struct PgAttnArgs {
   const unsigned long long* mask;
   const int* positions;
   int* status;
+  // attention of sequences that share keys, in two passes
+  int own;                  // 0: over the shared keys, results to share_*; 1: over a request's own, joined with those
+  float* share_o;
+  float2* share_ml;
 };
 // Checks what every call on the cache has in common and copies the batch.  *rows: rows in all.
 tss_status take_batch(const tss_paged* h, const tss_paged_cache* c, int layer, const tss_paged_batch* b, PgBatch* out, long long* rows);
@@ -37,5 +44,13 @@ int pa_counters(int sms);
 cudaError_t pa_prepare_all();
 // *too_large: more work than one launch counts (nothing was launched).
 cudaError_t launch_paged_attention(tss_paged* h, const PgAttnArgs& a, const PgBatch& batch, cudaStream_t s, bool* too_large);
+// Groups of requests, one after the other, whose sequences have the same pages for the first `shared` tokens (a multiple of 64, at
+// most the requests' first tokens).
+struct PgGroups {
+  int n;
+  int reqs[kPgMaxReq], shared[kPgMaxReq];
+};
+cudaError_t launch_paged_attention_shared(tss_paged* h, const PgAttnArgs& a, const PgBatch& batch, const PgGroups& groups, cudaStream_t s,
+                                          bool* too_large);
 
 }  // namespace tss

@@ -81,9 +81,10 @@ __device__ __forceinline__ bool sees(const PgAttnArgs& a, const PaReq& r, int i,
   return !a.window || qp - kp < a.window || j < a.sinks;
 }
 
-// TWO: weights of two fp16 parts.
-template <int D, int NT, bool TWO>
-__global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::kCtas) paged_attn_kernel(const __grid_constant__ PaParams p) {
+// TWO: weights of two fp16 parts.  SH: a pass of the attention of sequences that share keys.
+template <int D, int NT, bool TWO, bool SH>
+__global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::kCtas)
+    paged_attn_kernel(const __grid_constant__ typename PaParamsOf<SH>::type p) {
   using B = PgBlock<D>;
   using S = PaShape<D, NT>;
   constexpr int G = B::kGroups, W = S::kWarps, ST = S::kStages, R = S::kRows, DB = D / 32;
@@ -255,8 +256,7 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
     }
     if (a.window) {  // the last position among the tile's rows
       if (lane < rows) {
-        const int i = (row0 + lane) / gq;
-        pmax = a.positions ? max(__ldcg(a.positions + r.row + i), r.first) : r.first + i;
+        pmax = row_position(p, r, (row0 + lane) / gq);
       }
 #pragma unroll
       for (int x2 = 16; x2 > 0; x2 >>= 1) pmax = max(pmax, __shfl_xor_sync(0xffffffffu, pmax, x2));
@@ -365,7 +365,7 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
                 if (q >= rows) continue;
                 const int ti = (row0 + q) / gq;
                 const unsigned long long* anc = a.mask ? a.mask + 2LL * (r.row + ti) : nullptr;
-                const int qp = a.positions ? max(__ldcg(a.positions + r.row + ti), r.first) : r.first + ti;
+                const int qp = row_position(p, r, ti);
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
                   if (sees(a, r, ti, qp, anc, kb + k * 8 + g)) vis |= 1u << (nt * 8 + k * 2 + i);
@@ -572,7 +572,7 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
     }
     // a CTA's two partials: of the item that it begins, and of the one that it ends or runs through
     const int slot = blockIdx.x * 2 + (x0 == 0 ? 1 : 0);
-    const auto finish = [&](int row, int c4, float M, float L, float4 x) { finish_row<D>(a, r, h, row0 + row, c4, M, L, x); };
+    const auto finish = [&](int row, int c4, float M, float L, float4 x) { finish_row<D>(p, r, h, row0 + row, c4, M, L, x); };
     // the parts of (row, 4 dims), with the rows' references and sums
     const auto joined = [&](int row, int c4, float2* ml, float4* sum) {
       float M = -INFINITY, L = 0.f;
@@ -662,17 +662,75 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
 }
 
 template <int D, int NT, bool TWO>
-cudaError_t pa_launch(PaParams& p, int sms, cudaStream_t s) {
+cudaError_t pa_launch(PaShared& p, bool shared, int sms, cudaStream_t s) {
   using S = PaShape<D, NT>;
   // A run of a unit for each warp at least.  Leads of 0 / 3 / 6 / 10 / 16 pages, us: six requests of 60 to 30000
   // tokens 180 / 100 / 66 / 53 / 50, eight of 512 to 4096 45 / 40 / 38 / 37 / 38, equal ones alike at any.
   const int grid = pa_cut(p, sms * S::kCtas, S::kWarps, 8, 10 * (3 - p.halves));
-  return launch_k(paged_attn_kernel<D, NT, TWO>, dim3(grid), dim3(S::kWarps * 32), S::kSmem, s, true, p);
+  const dim3 g(grid), b(S::kWarps * 32);
+  return shared ? launch_k(paged_attn_kernel<D, NT, TWO, true>, g, b, S::kSmem, s, true, p)
+                : launch_k(paged_attn_kernel<D, NT, TWO, false>, g, b, S::kSmem, s, true, static_cast<PaParams&>(p));
 }
 template <int D, int NT, bool TWO>
 cudaError_t pa_prepare() {
-  return cudaFuncSetAttribute(paged_attn_kernel<D, NT, TWO>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              static_cast<int>(PaShape<D, NT>::kSmem));
+  const int bytes = static_cast<int>(PaShape<D, NT>::kSmem);
+  const cudaError_t e = cudaFuncSetAttribute(paged_attn_kernel<D, NT, TWO, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  return e == cudaSuccess ? cudaFuncSetAttribute(paged_attn_kernel<D, NT, TWO, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) : e;
+}
+
+// The launches of a pass: blocks of more than kPaTcRows query rows of a KV head go to the tcgen05 kernel (head_dim 128), the others
+// to the one above.
+cudaError_t pa_pass(tss_paged* h, const PgAttnArgs& a, const PaTask* tasks, int n_tasks, const int2* mem, int withhold, bool shared, cudaStream_t s,
+                    bool* too_large) {
+  const int gq = h->hq / h->hk;
+  int most = 0, wide = 0;
+  for (int i = 0; i < n_tasks; ++i) {
+    const int rows = tasks[i].q.n * gq;
+    if (h->d == 128 && rows > kPaTcRows)
+      ++wide;
+    else
+      most = rows > most ? rows : most;
+  }
+  PaShared p, narrow;
+  const auto begin = [&](PaShared& x) {
+    x.a = a;
+    x.part_o = h->part_o;
+    x.part_ml = h->part_ml;
+    x.counters = h->counters;
+    x.withhold = withhold;
+    if (mem)
+      for (int i = 0; i < kPgMaxReq; ++i) x.mem[i] = mem[i];
+  };
+  if (wide) {
+    begin(p);
+    if (!pa_plan(p, tasks, n_tasks, [&](const PgReq& q) { return q.n * gq > kPaTcRows; }, 128, 2)) {
+      *too_large = true;
+      return cudaSuccess;
+    }
+  }
+  if (most) {
+    begin(narrow);
+    const int R = most <= 8 ? 8 : 16;
+    const auto take = [&](const PgReq& q) { return h->d != 128 || q.n * gq <= kPaTcRows; };
+    // Units of a page; of half a page where that leaves the warps less than three pages each (a warp takes
+    // about 2 us for a page, so a short launch is as long as its longest warp).
+    bool fits = pa_plan(narrow, tasks, n_tasks, take, R, 2);
+    if (fits && narrow.total < 3LL * h->sms * (R == 8 ? 12 : 8)) fits = pa_plan(narrow, tasks, n_tasks, take, R, 1);
+    if (!fits) {
+      *too_large = true;
+      return cudaSuccess;
+    }
+    const auto run = [&](auto dim) {
+      constexpr int D = decltype(dim)::value;
+      if (R == 8) return pa_launch<D, 1, true>(narrow, shared, h->sms, s);
+      return a.is_half ? pa_launch<D, 2, true>(narrow, shared, h->sms, s) : pa_launch<D, 2, false>(narrow, shared, h->sms, s);
+    };
+    if (narrow.n_req) {
+      const cudaError_t e = h->d == 64 ? run(std::integral_constant<int, 64>{}) : run(std::integral_constant<int, 128>{});
+      if (e != cudaSuccess) return e;
+    }
+  }
+  return wide && p.n_req ? launch_paged_attention_tc(p, shared, h->sms, s) : cudaSuccess;
 }
 
 }  // namespace
@@ -694,56 +752,62 @@ cudaError_t pa_prepare_all() {
 
 cudaError_t launch_paged_attention(tss_paged* h, const PgAttnArgs& a, const PgBatch& batch, cudaStream_t s, bool* too_large) {
   *too_large = false;
-  PaParams p;
-  p.a = a;
-  p.part_o = h->part_o;
-  p.part_ml = h->part_ml;
-  p.counters = h->counters;
   const int withhold = h->inject > 0;
   if (withhold) --h->inject;
-  p.withhold = withhold;
-  // Blocks of more than kPaTcRows query rows of a KV head go to the tcgen05 kernel (head_dim 128).
-  const int gq = h->hq / h->hk;
-  int most = 0, wide = 0;
+  PaTask tasks[kPgMaxReq];
   for (int i = 0; i < batch.n_req; ++i) {
-    const int rows = batch.r[i].n * gq;
-    if (h->d == 128 && rows > kPaTcRows)
-      ++wide;
-    else
-      most = rows > most ? rows : most;
+    const PgReq& q = batch.r[i];
+    tasks[i] = PaTask{q, 0, q.first + q.n, q.first, 0, 0, 0};
   }
-  if (wide) {
-    if (!pa_plan(p, batch, [&](const PgReq& q) { return q.n * gq > kPaTcRows; }, 128, 2)) {
-      *too_large = true;
-      return cudaSuccess;
+  return pa_pass(h, a, tasks, batch.n_req, nullptr, withhold, false, s, too_large);
+}
+
+// A pass over the groups' shared keys, for all rows of a group at once, then one over every request's own.
+cudaError_t launch_paged_attention_shared(tss_paged* h, const PgAttnArgs& args, const PgBatch& batch, const PgGroups& groups, cudaStream_t s,
+                                          bool* too_large) {
+  *too_large = false;
+  const int withhold = h->inject > 0;
+  if (withhold) --h->inject;
+  PgAttnArgs a = args;
+  PaTask common[kPgMaxReq], mine[kPgMaxReq];
+  int2 mem[kPgMaxReq];
+  int n_common = 0, at = 0, n_mem = 0;
+  for (int g = 0; g < groups.n; ++g) {
+    PaTask t{PgReq{0, groups.shared[g], 0, 0}, 0, groups.shared[g], 0, 0, n_mem, 0};
+    for (int i = at; i < at + groups.reqs[g]; ++i) {
+      const PgReq& q = batch.r[i];
+      mine[i] = PaTask{q, 0, q.first + q.n, q.first, 0, 0, 0};
+      if (q.n == 0) continue;
+      if (t.members == 0) {
+        t.q.seq = q.seq;
+        t.q.row = q.row;
+        t.from = q.first;
+      }
+      t.q.n += q.n;
+      t.from = q.first < t.from ? q.first : t.from;
+      mem[n_mem++] = make_int2(q.row, q.first);
+      ++t.members;
     }
-  }
-  PaParams narrow;
-  if (most) {
-    narrow.a = a;
-    narrow.part_o = p.part_o;
-    narrow.part_ml = p.part_ml;
-    narrow.counters = p.counters;
-    narrow.withhold = withhold;
-    const int R = most <= 8 ? 8 : 16;
-    const auto take = [&](const PgReq& q) { return h->d != 128 || q.n * gq <= kPaTcRows; };
-    // Units of a page; of half a page where that leaves the warps less than three pages each (a warp takes
-    // about 2 us for a page, so a short launch is as long as its longest warp).
-    bool fits = pa_plan(narrow, batch, take, R, 2);
-    if (fits && narrow.total < 3LL * h->sms * (R == 8 ? 12 : 8)) fits = pa_plan(narrow, batch, take, R, 1);
-    if (!fits) {
-      *too_large = true;
-      return cudaSuccess;
+    if (t.members > 1 && groups.shared[g] > 0) {  // (alone, a request has no one to share with)
+      PaReq r;
+      pa_units(a, t, kPgTokens, &r);
+      for (int i = at; i < at + groups.reqs[g]; ++i) {
+        mine[i].k0 = groups.shared[g];
+        mine[i].joins = r.units > 0;
+      }
+      if (r.units > 0) common[n_common++] = t;
+    } else {
+      n_mem -= t.members;
     }
-    const auto run = [&](auto dim) {
-      constexpr int D = decltype(dim)::value;
-      if (R == 8) return pa_launch<D, 1, true>(narrow, h->sms, s);
-      return a.is_half ? pa_launch<D, 2, true>(narrow, h->sms, s) : pa_launch<D, 2, false>(narrow, h->sms, s);
-    };
-    const cudaError_t e = h->d == 64 ? run(std::integral_constant<int, 64>{}) : run(std::integral_constant<int, 128>{});
-    if (e != cudaSuccess) return e;
+    at += groups.reqs[g];
   }
-  return wide ? launch_paged_attention_tc(p, h->sms, s) : cudaSuccess;
+  cudaError_t e = cudaSuccess;
+  if (n_common) {
+    a.own = 0;
+    e = pa_pass(h, a, common, n_common, mem, withhold, true, s, too_large);
+  }
+  a.own = 1;
+  return e == cudaSuccess && !*too_large ? pa_pass(h, a, mine, batch.n_req, mem, withhold && !n_common, true, s, too_large) : e;
 }
 
 }  // namespace tss

@@ -26,6 +26,32 @@ struct PaParams {
   int* counters;         // [grid], zero between launches
   PaReq r[kPgMaxReq];
 };
+// A pass of the attention over shared keys.  The pass over the shared keys has a group where the others have a request: its rows
+// are those of its requests, `first` and the keys in all are the shared tokens.
+struct PaShared : PaParams {
+  int joins[kPgMaxReq];                   // own keys: the request's rows have results over shared ones
+  int member[kPgMaxReq], members[kPgMaxReq];  // shared keys: the group's requests, in mem
+  int2 mem[kPgMaxReq];                    // first row, first token
+};
+template <bool SH>
+struct PaParamsOf { using type = PaParams; };
+template <>
+struct PaParamsOf<true> { using type = PaShared; };
+// Index of a request among the parameters' (its arrays beside r).
+__device__ __forceinline__ int index_of(const PaParams& p, const PaReq& r) { return static_cast<int>(&r - p.r); }
+
+// Position of row ti of a request (or of a group, whose rows stand at their requests' tokens).
+__device__ __forceinline__ int row_position(const PaParams& p, const PaReq& r, int ti) {
+  return p.a.positions ? max(__ldcg(p.a.positions + r.row + ti), r.first) : r.first + ti;
+}
+__device__ __forceinline__ int row_position(const PaShared& p, const PaReq& r, int ti) {
+  const PgAttnArgs& a = p.a;
+  if (a.own) return row_position(static_cast<const PaParams&>(p), r, ti);
+  const int b = index_of(p, r), row = r.row + ti;
+  int m = p.member[b];
+  while (m + 1 < p.member[b] + p.members[b] && p.mem[m + 1].x <= row) ++m;
+  return a.positions ? max(__ldcg(a.positions + row), p.mem[m].y) : p.mem[m].y + row - p.mem[m].x;
+}
 
 __device__ __forceinline__ float ex2(float x) {
   float y;
@@ -39,7 +65,7 @@ __device__ __forceinline__ float ex2(float x) {
 // 48 rows 97 / 110, 56 rows 119 / 111, 128 rows 225 / 123; 8 heads: 32 rows 28 / 40, 48 rows 33 / 42, 64 rows 41 / 42.
 constexpr int kPaTcRows = 48;
 cudaError_t paged_attn_tc_prepare();
-cudaError_t launch_paged_attention_tc(PaParams& p, int sms, cudaStream_t s);
+cudaError_t launch_paged_attention_tc(PaShared& p, bool shared, int sms, cudaStream_t s);
 
 // The power of two that brings a row's largest query value `big` into [2^14, 2^15), where fp16 holds the row exactly
 // (kept within what it and its use in 2^24 / it can be; 1 for a row of zeros, or with an infinity).
@@ -165,7 +191,8 @@ __device__ __forceinline__ void gather_partials(const PaParams& p, int R, int c0
 
 // Four dims (from 4 c4) of the output of query row qr (token qr / group, query head of KV head h), and its lse.
 template <int D>
-__device__ __forceinline__ void finish_row(const PgAttnArgs& a, const PaReq& r, int h, int qr, int c4, float M, float L, float4 x) {
+__device__ __forceinline__ void finish_row(const PaParams& p, const PaReq& r, int h, int qr, int c4, float M, float L, float4 x) {
+  const PgAttnArgs& a = p.a;
   const int gq = a.hq / a.hk;
   const float inv = L > 0.f ? 1.f / L : L == 0.f ? 0.f : L;  // (a NaN stays one)
   const float y[4] = {x.x * inv, x.y * inv, x.z * inv, x.w * inv};
@@ -179,32 +206,77 @@ __device__ __forceinline__ void finish_row(const PgAttnArgs& a, const PaReq& r, 
   if (c4 == 0 && a.lse) a.lse[tok * a.hq + head] = (M + log2f(L)) * 0.6931471805599453f;
 }
 
+// The same in a pass of the shared attention: left for the other pass, or joined with what that one left.
+template <int D>
+__device__ __forceinline__ void finish_row(const PaShared& p, const PaReq& r, int h, int qr, int c4, float M, float L, float4 x) {
+  const PgAttnArgs& a = p.a;
+  const int gq = a.hq / a.hk;
+  const long long at = static_cast<long long>(r.row + qr / gq) * a.hq + h * gq + qr % gq;
+  float4* other = reinterpret_cast<float4*>(a.share_o + at * D) + c4;
+  if (!a.own) {
+    __stcg(other, x);
+    if (c4 == 0) __stcg(a.share_ml + at, make_float2(M, L));
+    return;
+  }
+  if (p.joins[index_of(p, r)]) {
+    const float2 ml = __ldcg(a.share_ml + at);
+    const float4 y = __ldcg(other);
+    const float top = fmaxf(M, ml.x), mb = top == -INFINITY ? 0.f : top, w = ex2(M - mb), v = ex2(ml.x - mb);
+    M = top;
+    L = fmaf(v, ml.y, w * L);
+    x = make_float4(fmaf(v, y.x, w * x.x), fmaf(v, y.y, w * x.y), fmaf(v, y.z, w * x.z), fmaf(v, y.w, w * x.w));
+  }
+  finish_row<D>(static_cast<const PaParams&>(p), r, h, qr, c4, M, L, x);
+}
+
 // ------------------------------------------------------------------------------------------
 // Host: the plan of a launch
 // ------------------------------------------------------------------------------------------
-// The requests of the batch that `take` picks, in row tiles of R query rows and units of `halves` 32-token
-// halves; false where the units pass 2^30.
+// What a launch has to do for a request: its rows over its keys [k0, k1) (k0 a multiple of a page).
+struct PaTask {
+  PgReq q;
+  int k0, k1;
+  int from;                    // the smallest index of its rows in the sequence
+  int joins, member, members;  // as in PaShared
+};
+
+// Units of a task, with those past the first tokens and before the window left out.
+inline void pa_units(const PgAttnArgs& a, const PaTask& t, int unit, PaReq* r) {
+  const int begin = t.k0 / unit, end = (t.k1 + unit - 1) / unit;
+  r->lo = begin;
+  r->sink = 0;
+  if (a.window) {
+    const int sinks = ((a.sinks < t.k1 ? a.sinks : t.k1) + unit - 1) / unit;
+    const int lo = (t.from - a.window + 1 > 0 ? t.from - a.window + 1 : 0) / unit;
+    if (sinks <= begin || begin == 0) {  // (first tokens that reach past a shared part: all units, and the masks)
+      if (lo > begin) r->lo = lo < end ? lo : end;
+      if (begin == 0) r->sink = sinks < r->lo ? sinks : r->lo;
+    }
+  }
+  r->units = r->sink + end - r->lo;
+}
+
+// The tasks that `take` picks, in row tiles of R query rows and units of `halves` 32-token halves; false where the units pass
+// 2^30.
 template <typename Take>
-inline bool pa_plan(PaParams& p, const PgBatch& batch, Take take, int R, int halves) {
+inline bool pa_plan(PaShared& p, const PaTask* tasks, int n_tasks, Take take, int R, int halves) {
   const PgAttnArgs& a = p.a;
   const int unit = 32 * halves, gq = a.hq / a.hk;
   long long at = 0;
   int items = 0;
   p.halves = halves;
   p.n_req = 0;
-  for (int i = 0; i < batch.n_req; ++i) {
-    const PgReq& q = batch.r[i];
+  for (int i = 0; i < n_tasks; ++i) {
+    const PaTask& t = tasks[i];
+    const PgReq& q = t.q;
     if (q.n == 0 || !take(q)) continue;
-    PaReq& r = p.r[p.n_req++];
-    r = PaReq{q.seq, q.first, q.n, q.row, 0, 0, 0, static_cast<int>(at), items, 0, 1};
-    const int end = (q.first + q.n + unit - 1) / unit;
-    if (a.window) {
-      r.lo = (q.first - a.window + 1 > 0 ? q.first - a.window + 1 : 0) / unit;
-      const int sinks = a.sinks < q.first + q.n ? a.sinks : q.first + q.n;
-      r.sink = (sinks + unit - 1) / unit;
-      if (r.sink > r.lo) r.sink = r.lo;
-    }
-    r.units = r.sink + end - r.lo;
+    PaReq r{q.seq, q.first, q.n, q.row, 0, 0, 0, static_cast<int>(at), items, 0, 1};
+    pa_units(a, t, unit, &r);
+    if (r.units == 0) continue;
+    p.joins[p.n_req] = t.joins;
+    p.member[p.n_req] = t.member;
+    p.members[p.n_req] = t.members;
+    p.r[p.n_req++] = r;
     const int mine = a.hk * ((q.n * gq + R - 1) / R);
     items += mine;
     at += static_cast<long long>(r.units) * mine;

@@ -63,6 +63,7 @@ struct __align__(16) PtShared {
   long long out_at[kPtRows];                          // where its output begins
   int qp[kPtRows];                                    // its position
   float inv[kPtRows];                                 // 1 / sum of its weights
+  float other[kPtRows];                               // what its results over shared keys are multiplied by
   float top[2][4][kPtRows];                           // maxima of its quarters, of scores and V's scales of each group
   float part[4][3][kPtRows];                          // the quarters' sums: p, p z'_0, p z'_1
 };
@@ -169,7 +170,8 @@ __device__ __forceinline__ unsigned long long row_sees(const PgAttnArgs& a, cons
 
 // The softmax team of an item's last CTA joins the partials of CTAs c0..c1: first every row's weights of them (in
 // shared memory, some of it Q's: no MMA is in flight), then 4 dims of 8 rows a thread, their loads in flight together.
-__device__ __forceinline__ void join_parts(const PaParams& p, PtShared& sh, uint8_t* sq, uint8_t* sj, const PaReq& r, int h, int row0, int rows,
+template <typename P>
+__device__ __forceinline__ void join_parts(const P& p, PtShared& sh, uint8_t* sq, uint8_t* sj, const PaReq& r, int h, int row0, int rows,
                                            int c0, int c1, int sw, int qt, int row, int lane) {
   const int parts = c1 - c0 + 1;
   const auto weight = [&](int x) {
@@ -227,13 +229,14 @@ __device__ __forceinline__ void join_parts(const PaParams& p, PtShared& sh, uint
       m = fmaxf(m, sh.top[0][k][q]);
       l += sh.part[k][0][q];
     }
-    finish_row<kPtD>(p.a, r, h, row0 + q, lane, m, l, o[i]);
+    finish_row<kPtD>(p, r, h, row0 + q, lane, m, l, o[i]);
   }
 }
 
-// TWO: weights of two fp16 parts (fp16 outputs); else one (bf16 outputs: its 2^-12 is a fraction of their own 2^-9).
-template <bool TWO>
-__global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __grid_constant__ PaParams p) {
+// TWO: weights of two fp16 parts (fp16 outputs); else one (bf16 outputs: its 2^-12 is a fraction of their own 2^-9).  SH: a pass
+// of the attention of sequences that share keys.
+template <bool TWO, bool SH>
+__global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __grid_constant__ typename PaParamsOf<SH>::type p) {
   extern __shared__ uint8_t pt_dyn[];
   __shared__ PtShared sh;
   const uint32_t skew = (1024 - (smem_u32(pt_dyn) & 1023)) & 1023;
@@ -520,15 +523,16 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
       unsigned long long anc_lo = ~0ull, anc_hi = ~0ull;
       if (valid) {
         const int ti = (row0 + row) / gq;
-        qp = a.positions ? max(__ldcg(a.positions + r.row + ti), r.first) : r.first + ti;
-        if (a.mask) {
+        qp = row_position(p, r, ti);
+        if (SH && !a.own) {  // (no shared key is of a row's block)
+        } else if (a.mask) {
           anc_lo = __ldcg(a.mask + 2LL * (r.row + ti));
           anc_hi = __ldcg(a.mask + 2LL * (r.row + ti) + 1);
         } else {
           anc_lo = ti >= 63 ? ~0ull : (2ull << ti) - 1;
           anc_hi = ti < 64 ? 0ull : ti == 127 ? ~0ull : (2ull << (ti - 64)) - 1;
         }
-        // (rows that the block does not have are not seen, whatever the mask says)
+        // (rows that the block does not have are not seen, whatever the mask says; a group's rows may be more than 128)
         if (r.n < 64) anc_lo &= (1ull << r.n) - 1;
         anc_hi = r.n <= 64 ? 0ull : r.n < 128 ? anc_hi & ((1ull << (r.n - 64)) - 1) : anc_hi;
       }
@@ -825,11 +829,32 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
           const int q = row0 + row, head = h * gq + q % gq;
           const long long tok = r.row + q / gq;
           sh.out_at[row] = tok * a.os + static_cast<long long>(head) * kPtD;
-          sh.inv[row] = L > 0.f ? 1.f / L : L == 0.f ? 0.f : L;  // (a NaN stays one)
-          if (!whole)
-            __stcg(p.part_ml + slot + row, make_float2(my_ref, L));
-          else if (a.lse)
-            a.lse[tok * a.hq + head] = (my_ref + log2f(L)) * 0.6931471805599453f;
+          if constexpr (SH) {
+            float M = my_ref, sum = L, w = 1.f, v = 0.f;
+            if (whole && !a.own) {
+              __stcg(a.share_ml + tok * a.hq + head, make_float2(my_ref, L));
+              sh.out_at[row] = (tok * a.hq + head) * kPtD;
+            } else if (whole && p.joins[rb]) {
+              const float2 ml = __ldcg(a.share_ml + tok * a.hq + head);
+              M = fmaxf(my_ref, ml.x);
+              w = ex2(my_ref - M);
+              v = ex2(ml.x - M);
+              sum = fmaf(v, ml.y, w * L);
+            }
+            const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;
+            sh.inv[row] = w * inv;
+            sh.other[row] = v * inv;
+            if (!whole)
+              __stcg(p.part_ml + slot + row, make_float2(my_ref, L));
+            else if (a.own && a.lse)
+              a.lse[tok * a.hq + head] = (M + log2f(sum)) * 0.6931471805599453f;
+          } else {
+            sh.inv[row] = L > 0.f ? 1.f / L : L == 0.f ? 0.f : L;  // (a NaN stays one)
+            if (!whole)
+              __stcg(p.part_ml + slot + row, make_float2(my_ref, L));
+            else if (a.lse)
+              a.lse[tok * a.hq + head] = (my_ref + log2f(L)) * 0.6931471805599453f;
+          }
         }
         // through shared memory (16-byte chunks permuted by row), so that a warp's store is a row
         float4* rows_of = reinterpret_cast<float4*>(sj) + qd * 32 * (kPtD / 4);
@@ -850,10 +875,24 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
           const int ql = qt * 8 + i, q = qd * 32 + ql;
           if (q >= rows) break;
           const float4 x = rows_of[ql * (kPtD / 4) + (lane ^ ql)];
-          if (whole) {
+          if (SH && whole && !a.own) {
+            __stcg(reinterpret_cast<float4*>(a.share_o + sh.out_at[q]) + lane, x);
+          } else if (whole) {
             const float inv = sh.inv[q];
-            const float y[4] = {x.x * inv, x.y * inv, x.z * inv, x.w * inv};
+            float y[4] = {x.x * inv, x.y * inv, x.z * inv, x.w * inv};
             const long long to = sh.out_at[q] + 4 * lane;
+            if constexpr (SH) {
+              if (p.joins[rb]) {
+                const int q2 = row0 + q;
+                const long long at = (static_cast<long long>(r.row + q2 / gq) * a.hq + h * gq + q2 % gq) * kPtD;
+                const float4 z = __ldcg(reinterpret_cast<const float4*>(a.share_o + at) + lane);
+                const float v = sh.other[q];
+                y[0] = fmaf(v, z.x, y[0]);
+                y[1] = fmaf(v, z.y, y[1]);
+                y[2] = fmaf(v, z.z, y[2]);
+                y[3] = fmaf(v, z.w, y[3]);
+              }
+            }
             if (a.is_half)
               store_vec<__half, 4>(static_cast<__half*>(a.out) + to, y);
             else
@@ -887,18 +926,25 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
 
 }  // namespace
 
+template <bool TWO>
+cudaError_t pt_prepare() {
+  const int bytes = static_cast<int>(kPtSmem);
+  const cudaError_t e = cudaFuncSetAttribute(paged_attn_tc_kernel<TWO, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  return e == cudaSuccess ? cudaFuncSetAttribute(paged_attn_tc_kernel<TWO, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) : e;
+}
 cudaError_t paged_attn_tc_prepare() {
-  cudaError_t e = cudaFuncSetAttribute(paged_attn_tc_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kPtSmem));
-  if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(paged_attn_tc_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kPtSmem));
-  return e;
+  const cudaError_t e = pt_prepare<false>();
+  return e == cudaSuccess ? pt_prepare<true>() : e;
 }
 
-cudaError_t launch_paged_attention_tc(PaParams& p, int sms, cudaStream_t s) {
+cudaError_t launch_paged_attention_tc(PaShared& p, bool shared, int sms, cudaStream_t s) {
   // (two pages at least, so that the copy, the expansion and the scores of one run under the other's softmax; an
   // item's start and end cost about as much as 6)
   const int grid = pa_cut(p, sms, 2, 6, 6);
-  return launch_k(p.a.is_half ? paged_attn_tc_kernel<true> : paged_attn_tc_kernel<false>, dim3(grid), dim3(kPtThreads), kPtSmem, s, true, p);
+  const dim3 g(grid), b(kPtThreads);
+  if (shared) return launch_k(p.a.is_half ? paged_attn_tc_kernel<true, true> : paged_attn_tc_kernel<false, true>, g, b, kPtSmem, s, true, p);
+  return launch_k(p.a.is_half ? paged_attn_tc_kernel<true, false> : paged_attn_tc_kernel<false, false>, g, b, kPtSmem, s, true,
+                  static_cast<PaParams&>(p));
 }
 
 }  // namespace tss

@@ -32,6 +32,7 @@ EXPORTS = (
     "tss_qk_rope", "tss_rope_frequencies", "tss_rope_table",
     "tss_paged_page_bytes", "tss_paged_create", "tss_paged_destroy", "tss_paged_sync_status", "tss_paged_append",
     "tss_paged_append_rope", "tss_paged_read", "tss_paged_attention", "tss_paged_inject_timeout",
+    "tss_paged_create_shared", "tss_paged_attention_shared",
     "tss_pages_create", "tss_pages_destroy", "tss_pages_sync_status", "tss_pages_reserve", "tss_pages_free",
     "tss_pages_fork", "tss_pages_reorder", "tss_pages_compact", "tss_pages_copy",
     "tss_beam_create", "tss_beam_destroy", "tss_beam_sync_status", "tss_beam_select",
@@ -115,6 +116,10 @@ class TssPagedAttn(ctypes.Structure):
                 ("mask", _P), ("positions", _P)]
 
 
+class TssPagedGroups(ctypes.Structure):
+    _fields_ = [("n_groups", ctypes.c_int), ("n_req", _P), ("shared", _P)]
+
+
 class TssPageTables(ctypes.Structure):
     _fields_ = [("table", _P), ("held", _P), ("refs", _P)]
 
@@ -182,6 +187,8 @@ def lib() -> ctypes.CDLL:
         L.tss_paged_append_rope.argtypes = [_P, cache, I, batch, ctypes.POINTER(TssRopeArgs), _P, L64, _P]
         L.tss_paged_read.argtypes = L.tss_paged_append.argtypes
         L.tss_paged_attention.argtypes = [_P, cache, I, batch, ctypes.POINTER(TssPagedAttn), _P]
+        L.tss_paged_create_shared.argtypes = [I, I, I, I, PP]
+        L.tss_paged_attention_shared.argtypes = [_P, cache, I, batch, ctypes.POINTER(TssPagedGroups), ctypes.POINTER(TssPagedAttn), _P]
         L.tss_paged_inject_timeout.argtypes = [_P, I]
         L.tss_paged_inject_timeout.restype = I
         L.tss_pages_create.argtypes = [I, I, I, PP]
@@ -200,6 +207,7 @@ def lib() -> ctypes.CDLL:
             getattr(L, name).restype = None
         for name in ("tss_qk_rope", "tss_rope_frequencies", "tss_rope_table", "tss_paged_create", "tss_paged_sync_status",
                      "tss_paged_append", "tss_paged_append_rope", "tss_paged_read", "tss_paged_attention", "tss_pages_create",
+                     "tss_paged_create_shared", "tss_paged_attention_shared",
                      "tss_pages_sync_status", "tss_pages_reserve", "tss_pages_free", "tss_pages_fork", "tss_pages_reorder",
                      "tss_pages_compact", "tss_pages_copy", "tss_beam_create", "tss_beam_sync_status", "tss_beam_select"):
             getattr(L, name).restype = ctypes.c_int

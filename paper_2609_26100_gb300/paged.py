@@ -193,9 +193,10 @@ class PagePool:
 
 
 class Kv4Cache:
-    """A KV cache in 4 bits: pool uint8 [layers][pages][page bytes], table int32 [seqs][max_pages]."""
+    """A KV cache in 4 bits: pool uint8 [layers][pages][page bytes], table int32 [seqs][max_pages].  shared_rows: the most rows of
+    an attention_shared call."""
 
-    def __init__(self, pool: torch.Tensor, table: torch.Tensor, *, n_q_heads: int, n_kv_heads: int, head_dim: int):
+    def __init__(self, pool: torch.Tensor, table: torch.Tensor, *, n_q_heads: int, n_kv_heads: int, head_dim: int, shared_rows: int = 0):
         if pool.dtype != torch.uint8 or pool.dim() != 3 or pool.shape[2] != page_bytes(n_kv_heads, head_dim):
             raise ValueError("pool: uint8 [layers][pages][page bytes] is wanted")
         if table.dim() != 2:
@@ -209,20 +210,20 @@ class Kv4Cache:
                                            table.shape[0], table.shape[1])
         self._cache_ref = ctypes.byref(self._cache)
         self._c_append, self._c_read, self._c_attention = lib().tss_paged_append, lib().tss_paged_read, lib().tss_paged_attention
-        self._c_append_rope = lib().tss_paged_append_rope
+        self._c_append_rope, self._c_shared = lib().tss_paged_append_rope, lib().tss_paged_attention_shared
         self.pages: Optional[PagePool] = None
         h = _P()
         with torch.cuda.device(self._dev):
-            check(lib().tss_paged_create(n_q_heads, n_kv_heads, head_dim, ctypes.byref(h)), "tss_paged_create")
+            check(lib().tss_paged_create_shared(n_q_heads, n_kv_heads, head_dim, shared_rows, ctypes.byref(h)), "tss_paged_create")
         self._h = h
 
     @classmethod
     def allocate(cls, *, n_layers: int, n_pages: int, n_seqs: int, max_pages: int, n_q_heads: int, n_kv_heads: int,
-                 head_dim: int, device: str = "cuda") -> "Kv4Cache":
+                 head_dim: int, device: str = "cuda", shared_rows: int = 0) -> "Kv4Cache":
         """An empty cache with its page books (the result's `pages`)."""
         pool = torch.zeros((n_layers, n_pages, page_bytes(n_kv_heads, head_dim)), dtype=torch.uint8, device=device)
         table = torch.full((n_seqs, max_pages), -1, dtype=torch.int32, device=device)
-        c = cls(pool, table, n_q_heads=n_q_heads, n_kv_heads=n_kv_heads, head_dim=head_dim)
+        c = cls(pool, table, n_q_heads=n_q_heads, n_kv_heads=n_kv_heads, head_dim=head_dim, shared_rows=shared_rows)
         c.pages = PagePool(pool, table, torch.zeros(n_seqs, dtype=torch.int32, device=device),
                            torch.zeros(n_pages, dtype=torch.int32, device=device))
         return c
@@ -292,6 +293,33 @@ class Kv4Cache:
         """Attention of the batch's rows (already appended) over their sequences: q, out [rows][heads][head_dim];
         lse float32 [rows][heads]; mask int64 [rows][2] (bits of the block's rows that a row sees; None: a chain);
         window and sinks as in tss_paged_attention, positions int32 [rows]."""
+        a = self._attention(batch, q, out, lse, scale, window, sinks, mask, positions)
+        s = self._c_attention(self._h, self._cache_ref, layer, batch.ref, ctypes.byref(a), _stream_of(self._dev, stream))
+        if s:
+            check(s, "tss_paged_attention")
+
+    @staticmethod
+    def groups(sizes: Sequence[int], shared: Sequence[int]) -> native.TssPagedGroups:
+        """Of a batch the next sizes[g] requests share the pages of their first shared[g] tokens (whole pages of them)."""
+        if len(sizes) != len(shared):
+            raise ValueError("sizes and shared differ in length")
+        keep = [_host(map(int, x)) for x in (sizes, shared)]
+        g = native.TssPagedGroups(len(sizes), *[a.buffer_info()[0] for a in keep])
+        g._keep = keep
+        g.ref = ctypes.byref(g)
+        return g
+
+    def attention_shared(self, layer: int, batch, groups, q: torch.Tensor, out: torch.Tensor, lse: Optional[torch.Tensor] = None, *,
+                         scale: Optional[float] = None, window: int = 0, sinks: int = 0, mask: Optional[torch.Tensor] = None,
+                         positions: Optional[torch.Tensor] = None, stream=None) -> None:
+        """attention() of sequences that share the pages of their first tokens (PagePool.fork, reorder), whose keys are read once for all
+        rows of a group of self.groups().  The cache was made with shared_rows of at least the batch's rows."""
+        a = self._attention(batch, q, out, lse, scale, window, sinks, mask, positions)
+        s = self._c_shared(self._h, self._cache_ref, layer, batch.ref, groups.ref, ctypes.byref(a), _stream_of(self._dev, stream))
+        if s:
+            check(s, "tss_paged_attention_shared")
+
+    def _attention(self, batch, q, out, lse, scale, window, sinks, mask, positions) -> native.TssPagedAttn:
         n, h, d = shape = (batch.rows, self.n_q_heads, self.head_dim)
         dev = self._dev
         if out.dtype != q.dtype:
@@ -303,13 +331,9 @@ class Kv4Cache:
             raise ValueError("mask: contiguous 64-bit [rows][2] on the pool's GPU is wanted")
         if positions is not None:
             _ints(positions, (n,), dev, "positions")
-        a = native.TssPagedAttn(q.data_ptr(), _row_stride(q, shape, dev, "q"), out.data_ptr(), _row_stride(out, shape, dev, "out"),
-                                None if lse is None else lse.data_ptr(), _code(q), d ** -0.5 if scale is None else scale, window,
-                                sinks, None if mask is None else mask.data_ptr(), None if positions is None else positions.data_ptr())
-        s = self._c_attention(self._h, self._cache_ref, layer, batch.ref, ctypes.byref(a),
-                              _stream_of(self._dev, stream))
-        if s:
-            check(s, "tss_paged_attention")
+        return native.TssPagedAttn(q.data_ptr(), _row_stride(q, shape, dev, "q"), out.data_ptr(), _row_stride(out, shape, dev, "out"),
+                                   None if lse is None else lse.data_ptr(), _code(q), d ** -0.5 if scale is None else scale, window,
+                                   sinks, None if mask is None else mask.data_ptr(), None if positions is None else positions.data_ptr())
 
     def inject_timeout(self, n_calls: int) -> None:
         """tss_paged_inject_timeout: make a wait of the next n_calls attention calls run out (tests)."""
