@@ -2,15 +2,16 @@
 //
 //   value(b, t) = score_b + x_bt - ln sum_u exp x_bu,  largest first, ties to the lowest b vocab + t
 //
-// One pass over the logits.  A CTA holds a chunk of a row in registers.  The k-th largest of its threads' maxima is at most the
-// chunk's k-th largest, and only k threads have elements above it, so a scan of the registers against it leaves few candidates,
-// which are ranked by (value, index).  With them goes the chunk's sum of exponentials.  The last CTA of a group to arrive joins
-// the rows' sums and picks from the chunks' sorted lists in the same way: first the k-th largest head, then what is above it.
+// One pass over the logits.  A CTA holds a chunk of a row in registers.  At least n_keep of its elements reach the least of its
+// warps' ceil(n_keep / 8)-th largest thread maxima, and few more do: those are ranked by (value, index).  With them goes the
+// chunk's sum of exponentials.  The last CTA of a group to arrive joins the rows' sums and picks from the chunks' sorted lists in
+// the same way: a bound from one entry of each list, then what reaches it.
 //
-// Between rows the order goes by the last bits of the rows' sums.  Terms are 2^((x - m) log2e), m the chunk's largest logit and
-// log2e in two parts, sums are 64-bit from a thread's own on, and a chunk's n_keep largest terms are put in again in 64 bits (the
-// fast exponential is off by 2^-22, which a few likely tokens would leave in the sum): values are right to about 1e-8, compared in
-// 64 bits and rounded once.  The order of all sums is the elements', whatever their alignment: equal rows have equal values.
+// Between rows the order goes by the last bits of the rows' sums.  Terms are 2^((x - m) log2e + f), m the chunk's largest logit,
+// log2e in two parts, f what its product with m leaves of a whole number, so that chunks' sums differ by powers of two.  The
+// candidates' terms, most of the sum, are computed to 2^-28 (the fast exponential's 2^-22 is for the others), and sums of
+// threads are whole numbers, whose order does not matter: values are right to about 1e-8, compared in 64 bits and rounded once, and
+// equal rows have equal values, whatever their alignment (elements go to threads by their index).
 #include "ops.cuh"
 
 struct tss_beam {
@@ -19,7 +20,7 @@ struct tss_beam {
   int* status;        // device
   int* counters;      // device [max_rows]: chunks of each group that are done, zero between launches
   uint2* part;        // device [lists][max_keep]: a chunk's largest, (value's bits, token)
-  double2* sums;      // device [lists]: (largest logit m, sum of e^(x - m))
+  longlong2* sums;    // device [lists]: sum of its terms in units of 2^(R - kBmBits); its largest logit m, and 2^32 if it has none to use
 };
 
 namespace tss {
@@ -41,7 +42,7 @@ struct BmParams {
   int *parent, *token;
   int* counters;
   uint2* part;
-  double2* sums;
+  longlong2* sums;
   int* status;
 };
 
@@ -61,17 +62,44 @@ __device__ __forceinline__ double double_of(unsigned long long o) {
 // (value, index): larger values first, then lower indices
 __device__ __forceinline__ bool ahead(unsigned long long a, uint32_t ai, unsigned long long b, uint32_t bi) { return a > b || (a == b && ai < bi); }
 
-__device__ __forceinline__ float bm_ex2(float x) {
+// e^x = 2^(R + t): R whole (of two floats, as it may pass 2^24) and of the chunk's largest logit m, t = (x - m) log2e + f.
+constexpr float kLog2eHi = 1.44269502162933349609f, kLog2eLo = 1.92596299112661746887e-8f;
+struct BmBase {
+  float hi, lo, f;
+  __device__ __forceinline__ explicit BmBase(float m) {
+    const float t = m * kLog2eHi, rest = fmaf(m, kLog2eHi, -t) + m * kLog2eLo;
+    hi = rintf(t);
+    lo = rintf(rest);
+    f = (t - hi) + (rest - lo);
+  }
+};
+// 2^t by the fast exponential (2^-22 of it).
+__device__ __forceinline__ float bm_term(float x, float m, float f) {
+  const float d = x - m;
   float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(fmaf(d, kLog2eHi, fmaf(d, kLog2eLo, f))));
   return y;
 }
-// e^(x - m): the difference is exact for 16-bit logits, log2e in two parts
-constexpr float kLog2eHi = 1.44269502162933349609f, kLog2eLo = 1.92596299112661746887e-8f;
-__device__ __forceinline__ float bm_term(float x, float m) {
-  const float d = x - m;
-  return bm_ex2(fmaf(d, kLog2eHi, d * kLog2eLo));
+// 2^t to about 2^-28 of it, times 2^kBmBits and rounded to a whole number: 2^n e^u with u in two floats, e^u = 1 + u + u^2 q(u).
+constexpr int kBmBits = 37;  // 2^24 terms of up to 2 stay below 2^63
+__device__ __forceinline__ long long bm_fixed(float x, float m, float f) {
+  constexpr float kLn2Hi = 0.693147182464599609375f, kLn2Lo = -1.90465429995776804525e-9f;
+  const float d = x - m, t = d * kLog2eHi, rest = fmaf(d, kLog2eHi, -t) + fmaf(d, kLog2eLo, f);
+  const float n = rintf(t + rest), v = t - n;  // (exact)
+  const float v1 = v + rest, v2 = rest - (v1 - v);
+  const float u = v1 * kLn2Hi, w = fmaf(v1, kLn2Hi, -u) + fmaf(v1, kLn2Lo, v2 * kLn2Hi);
+  float q = 1.f / 5040.f;
+  q = fmaf(q, u, 1.f / 720.f);
+  q = fmaf(q, u, 1.f / 120.f);
+  q = fmaf(q, u, 1.f / 24.f);
+  q = fmaf(q, u, 1.f / 6.f);
+  q = fmaf(q, u, 0.5f);
+  const float e = fmaf(u * u, q, fmaf(u, w, w));  // all but 1 + u
+  if (n < -static_cast<float>(kBmBits) - 2.f) return 0;
+  const float scale = __uint_as_float(static_cast<uint32_t>(static_cast<int>(n) + kBmBits + 127) << 23);
+  return __float2ll_rn(scale) + __float2ll_rn(u * scale) + __float2ll_rn(e * scale);
 }
+__device__ __forceinline__ long long bm_fixed(float y) { return __float2ll_rn(y * static_cast<float>(1ll << kBmBits)); }
 
 // The first k of n entries (value, index) in shared memory, which has room for the next power of two from n on, in the order of
 // `before`, to `put(rank, value, index)`; all threads.
@@ -79,14 +107,20 @@ template <typename Before, typename Put>
 __device__ __forceinline__ void pick(unsigned long long* val, uint32_t* idx, int n, int k, Before before, Put put) {
   const int tid = threadIdx.x;
   __syncthreads();
-  if (n <= kBmThreads) {  // by counting who comes before
-    if (tid < n) {
-      const unsigned long long v = val[tid];
-      const uint32_t x = idx[tid];
-      int rank = 0;
-      for (int j = 0; j < n; ++j) rank += before(val[j], idx[j], v, x);
-      if (rank < k) put(rank, v, x);
+  if (n <= kBmThreads) {  // by counting who comes before: up to 8 threads an entry
+    int per = 8;
+    while (per > 1 && n * per > kBmThreads) per /= 2;
+    const int e = tid / per, part = tid & (per - 1);
+    unsigned long long v = 0;
+    uint32_t x = 0;
+    int rank = 0;
+    if (e < n) {
+      v = val[e];
+      x = idx[e];
+      for (int j = part; j < n; j += per) rank += before(val[j], idx[j], v, x);
     }
+    for (int o = per / 2; o > 0; o /= 2) rank += __shfl_xor_sync(0xffffffffu, rank, o);
+    if (e < n && part == 0 && rank < k) put(rank, v, x);
   } else {  // bitonic sort
     int size = 2 * kBmThreads;
     while (size < n) size *= 2;
@@ -114,18 +148,34 @@ __device__ __forceinline__ void pick(unsigned long long* val, uint32_t* idx, int
 }
 
 struct BmShared {
-  unsigned long long top[kBmThreads];  // the threads' maxima
+  unsigned long long top[kBmThreads];
   uint32_t top_idx[kBmThreads];
-  double sum[kBmWarps];
-  double again[kBmKeep];
+  long long sum[kBmWarps];
   double base[kBmBeams];               // score - ln sum of each row
-  float most[kBmWarps];
+  float most[kBmWarps], least[kBmWarps];
+  unsigned long long bound[kBmWarps], last_of[kBmWarps];
+  long long row_sum[kBmBeams];
+  float2 row_base[kBmBeams];
   int n, last;
 };
 
-// The k-th of the threads' own largest entries: at least k entries are at or before it (the last one where fewer than k have any).
+// The m-th largest of a warp's values, m in [1, 32] (in all lanes).
+template <typename V>
+__device__ __forceinline__ V nth_of(V v, int m, int lane) {
+  int rank = 0;
+#pragma unroll
+  for (int j = 0; j < 32; ++j) {
+    const V o = __shfl_sync(0xffffffffu, v, j);
+    rank += o > v || (o == v && j < lane);
+  }
+  return __shfl_sync(0xffffffffu, v, __ffs(__ballot_sync(0xffffffffu, rank == m - 1)) - 1);
+}
+
+// The k-th of the threads' own largest entries: at least k entries are at or before it, and no others than those threads' are
+// before it.
 __device__ __forceinline__ void bound_of(BmShared& sh, unsigned long long v, uint32_t x, int k, unsigned long long* tv, uint32_t* tx) {
   const int tid = threadIdx.x;
+  __syncthreads();
   sh.top[tid] = v;
   sh.top_idx[tid] = x;
   __syncthreads();
@@ -160,63 +210,101 @@ __device__ __forceinline__ void bm_chunk(const BmParams& p, BmShared& sh, unsign
       for (int j = 0; j < VEC; ++j) x[i * VEC + j] = at + j < n ? to_f32(src[at + j]) : -INFINITY;
     }
   }
-  float most = -INFINITY;
-  int where = 0;
-  bool bad = false;
+  if (tid == 0) sh.n = 0;
+  float mv[NV], most = -INFINITY;  // the vectors' maxima
 #pragma unroll
-  for (int i = 0; i < EPT; ++i) {
-    if (x[i] <= -kBmMost) x[i] = -INFINITY;
-    bad |= !(x[i] < kBmMost);
-    if (x[i] > most) {
-      most = x[i];
-      where = i;
-    }
+  for (int i = 0; i < NV; ++i) {
+    mv[i] = x[i * VEC];
+#pragma unroll
+    for (int j = 1; j < VEC; ++j) mv[i] = fmaxf(mv[i], x[i * VEC + j]);
+    most = fmaxf(most, mv[i]);
   }
   const auto token = [&](int i) { return static_cast<uint32_t>(e0 + (tid + i / VEC * kBmThreads) * VEC + i % VEC); };
-  float m = most;
+  // A bound that at least n_keep elements reach: of every warp the ceil(n_keep / 8)-th largest of its threads' maxima, the least
+  // of these.
+  float m = most, least;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  if (lane == 0) sh.most[warp] = m;
-  if (tid == 0) sh.n = 0;
-  bad = __syncthreads_or(bad);
+  least = p.keep <= kBmWarps ? m : nth_of(most, (p.keep + kBmWarps - 1) / kBmWarps, lane);
+  if (lane == 0) {
+    sh.most[warp] = m;
+    sh.least[warp] = least;
+  }
+  __syncthreads();
 #pragma unroll
-  for (int i = 0; i < kBmWarps; ++i) m = fmaxf(m, sh.most[i]);
+  for (int i = 0; i < kBmWarps; ++i) {
+    m = fmaxf(m, sh.most[i]);
+    least = fminf(least, sh.least[i]);
+  }
   const long long list = row * p.chunks + chunk;
-  if (bad || m == -INFINITY) {  // nothing to offer
-    if (tid == 0) __stcg(p.sums + list, make_double2(0., bad ? NAN : 0.));
-    if (tid < p.keep) __stcg(p.part + list * p.keep + tid, make_uint2(order_of(-INFINITY), 0u));
+  uint2* part = p.part + list * p.keep;
+  const auto offer_nothing = [&](bool bad) {
+    if (tid == 0) __stcg(p.sums + list, make_longlong2(0, (bad ? 1ll << 32 : 0ll) | __float_as_uint(-INFINITY)));
+    if (tid < p.keep) __stcg(part + tid, make_uint2(order_of(-INFINITY), 0u));
+  };
+  const BmBase base(m);
+  // Elements that reach the bound become candidates, whose terms are added up apart; a NaN shows in the sum of the others.
+  float s[2] = {0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < EPT; ++i) {
+    const float y = bm_term(x[i], m, base.f);
+    if (!(x[i] >= least)) s[i & 1] += y;
+  }
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+    if (mv[i] >= least) {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j)
+        if (x[i * VEC + j] >= least && x[i * VEC + j] > -kBmMost) {
+          const int at = atomicAdd(&sh.n, 1);
+          if (at < kBmPool) {
+            val[at] = order_of(x[i * VEC + j]);
+            idx[at] = token(i * VEC + j);
+          }
+        }
+    }
+  const float odd = s[0] + s[1];
+  if (__syncthreads_or(odd != odd || !(m < kBmMost)) || m <= -kBmMost) {
+    // (where all are masked the difference from the largest is a NaN too)
+    bool bad = !(m < kBmMost);
+#pragma unroll
+    for (int i = 0; i < EPT; ++i) bad |= x[i] != x[i];
+    offer_nothing(__syncthreads_or(bad));
     return;
   }
-  float s[4] = {0.f, 0.f, 0.f, 0.f};
+  int found = sh.n;
+  long long sum = bm_fixed(s[0]) + bm_fixed(s[1]);
+  if (found > kBmPool / 4) {
+    // Too many (a run of masked elements, or of equal ones): the n_keep-th of the threads' best is the bound, which n_keep
+    // threads' elements reach at most; the candidates' terms are taken as the others' are.
+    __syncthreads();  // (all have read how many)
+    int where = 0;
+    float s2 = 0.f;
 #pragma unroll
-  for (int i = 0; i < EPT; ++i) s[i & 3] += bm_term(x[i], m);
-  double sum = static_cast<double>(s[0] + s[1]) + static_cast<double>(s[2] + s[3]);
-  // candidates
-  unsigned long long tv;
-  uint32_t tx;
-  bound_of(sh, order_of(most), most > -INFINITY ? token(where) : 0xffffffffu, p.keep, &tv, &tx);
-  const float least = float_of(static_cast<uint32_t>(tv));
-#pragma unroll
-  for (int i = 0; i < EPT; ++i)
-    if (x[i] >= least && x[i] > -INFINITY) {
-      const unsigned long long v = order_of(x[i]);
-      const uint32_t t = token(i);
-      if (!ahead(tv, tx, v, t)) {
-        const int at = atomicAdd(&sh.n, 1);
-        val[at] = v;
-        idx[at] = t;
-      }
+    for (int i = EPT - 1; i >= 0; --i) {
+      if (x[i] == most) where = i;
+      if (x[i] >= least) s2 += bm_term(x[i], m, base.f);
     }
-  __syncthreads();
-  const int found = sh.n;
-  pick(val, idx, found, p.keep, ahead, [&](int rank, unsigned long long v, uint32_t t) {
-    __stcg(p.part + list * p.keep + rank, make_uint2(static_cast<uint32_t>(v), t));
-    // the term again, in 64 bits
-    const float y = float_of(static_cast<uint32_t>(v));
-    sh.again[rank] = exp(static_cast<double>(y) - static_cast<double>(m)) - static_cast<double>(bm_term(y, m));
-  });
-  if (tid < min(found, p.keep)) sum += sh.again[tid];  // (by rank, so that the sum's order does not depend on timing)
-  for (int r = found + tid; r < p.keep; r += kBmThreads) __stcg(p.part + list * p.keep + r, make_uint2(order_of(-INFINITY), 0u));
+    sum += bm_fixed(s2);
+    if (tid == 0) sh.n = 0;
+    unsigned long long tv;
+    uint32_t tx;
+    bound_of(sh, order_of(most), most > -kBmMost ? token(where) : 0xffffffffu, p.keep, &tv, &tx);
+    const float from = float_of(static_cast<uint32_t>(tv));
+#pragma unroll
+    for (int i = 0; i < EPT; ++i)
+      if (x[i] >= from && x[i] > -kBmMost && !ahead(tv, tx, order_of(x[i]), token(i))) {
+        const int at = atomicAdd(&sh.n, 1);
+        val[at] = order_of(x[i]);
+        idx[at] = token(i);
+      }
+    __syncthreads();
+    found = sh.n;
+  } else {
+    for (int j = tid; j < found; j += kBmThreads) sum += bm_fixed(float_of(static_cast<uint32_t>(val[j])), m, base.f);
+  }
+  pick(val, idx, found, p.keep, ahead, [&](int rank, unsigned long long v, uint32_t t) { __stcg(part + rank, make_uint2(static_cast<uint32_t>(v), t)); });
+  for (int r = found + tid; r < p.keep; r += kBmThreads) __stcg(part + r, make_uint2(order_of(-INFINITY), 0u));
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
   if (lane == 0) sh.sum[warp] = sum;
@@ -224,7 +312,7 @@ __device__ __forceinline__ void bm_chunk(const BmParams& p, BmShared& sh, unsign
   if (tid == 0) {
 #pragma unroll
     for (int i = 1; i < kBmWarps; ++i) sum += sh.sum[i];
-    __stcg(p.sums + list, make_double2(static_cast<double>(m), sum));
+    __stcg(p.sums + list, make_longlong2(sum, __float_as_uint(m)));
   }
 }
 
@@ -234,41 +322,73 @@ __device__ __forceinline__ void bm_join(const BmParams& p, BmShared& sh, unsigne
   const long long row0 = static_cast<long long>(group) * p.beams;
   const int lists = p.beams * p.chunks;
   const double none = -static_cast<double>(INFINITY);
-  // rows: score - ln sum
-  for (int b = warp; b < p.beams; b += kBmWarps) {
+  // rows' sums: a warp takes every eighth row, its lanes chunks; the rows' first chunks are on their way together
+  constexpr int kRows = kBmBeams / kBmWarps;
+  const auto alive = [&](int b) {
     const float s = p.score ? __ldcg(p.score + row0 + b) : 0.f;
-    const bool fine = s > -INFINITY && s < INFINITY;
-    if (lane == 0 && !(s < INFINITY)) report(p.status, kStatusCheck);
-    double base = none;
-    if (fine && !(p.done && __ldcg(p.done + row0 + b))) {
-      const double2* sums = p.sums + (row0 + b) * p.chunks;
-      double ref = none, sum = 0.;
-      for (int c = lane; c < p.chunks; c += 32) {
-        const double2 x = __ldcg(sums + c);
-        if (x.y != x.y) sum = x.y;  // (a NaN stays one)
-        if (!(x.y > 0.)) continue;
-        const double r = fmax(ref, x.x);
-        sum = (sum == 0. ? 0. : sum * exp(ref - r)) + x.y * exp(x.x - r);
-        ref = r;
-      }
+    return s > -INFINITY && s < INFINITY && !(p.done && __ldcg(p.done + row0 + b));
+  };
+  longlong2 first[kRows];
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) {
-        const double r2 = __shfl_xor_sync(0xffffffffu, ref, o), s2 = __shfl_xor_sync(0xffffffffu, sum, o), r = fmax(ref, r2);
-        sum = (ref > none ? sum * exp(ref - r) : sum) + (r2 > none ? s2 * exp(r2 - r) : s2);
-        ref = r;
-      }
-      if (sum != sum) {
-        if (lane == 0) report(p.status, kStatusCheck);
-      } else if (sum > 0.) {
-        base = static_cast<double>(s) - (ref + log(sum));
+  for (int i = 0; i < kRows; ++i) {
+    const int b = warp + i * kBmWarps;
+    first[i] = make_longlong2(0, __float_as_uint(-INFINITY));
+    if (b < p.beams && lane < p.chunks && alive(b)) first[i] = __ldcg(p.sums + (row0 + b) * p.chunks + lane);
+  }
+#pragma unroll
+  for (int i = 0; i < kRows; ++i) {
+    const int b = warp + i * kBmWarps;
+    if (b >= p.beams) break;
+    const bool on = alive(b);
+    float m = -INFINITY;
+    bool bad = false;
+    for (int c = lane; c < p.chunks; c += 32) {
+      const longlong2 x = c < 32 ? first[i] : on ? __ldcg(p.sums + (row0 + b) * p.chunks + c) : make_longlong2(0, __float_as_uint(-INFINITY));
+      m = fmaxf(m, __uint_as_float(static_cast<uint32_t>(x.y)));
+      bad |= x.y >> 32 != 0;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    bad = __any_sync(0xffffffffu, bad);
+    const BmBase top(m);
+    long long sum = 0;
+    for (int c = lane; c < p.chunks; c += 32) {
+      const longlong2 x = c < 32 ? first[i] : on ? __ldcg(p.sums + (row0 + b) * p.chunks + c) : make_longlong2(0, __float_as_uint(-INFINITY));
+      if (x.x == 0) continue;
+      const BmBase mine(__uint_as_float(static_cast<uint32_t>(x.y)));
+      const float down = (top.hi - mine.hi) + (top.lo - mine.lo);  // (whole; below 2^24 exact, beyond that nothing is left)
+      if (down < 62.f) {
+        const int k = max(static_cast<int>(down), 0);
+        sum += k > 0 ? (x.x + (1ll << (k - 1))) >> k : x.x;
       }
     }
-    if (lane == 0) sh.base[b] = base;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (lane == 0) {
+      sh.row_sum[b] = bad ? 0 : sum;
+      sh.row_base[b] = make_float2(m, top.f);
+      if (bad) report(p.status, kStatusCheck);
+    }
   }
+  __syncthreads();
+  bool goes_on = false;  // the thread's row is finished and goes on as it is
+  float score = 0.f;
+  if (tid < p.beams) {
+    score = p.score ? __ldcg(p.score + row0 + tid) : 0.f;
+    if (!(score < INFINITY)) report(p.status, kStatusCheck);
+    const bool fine = score > -INFINITY && score < INFINITY, done = p.done && __ldcg(p.done + row0 + tid);
+    goes_on = fine && done;
+    const long long sum = sh.row_sum[tid];
+    // (ln sum e^x = m + ln(2^-f sum of the terms): what R is does not come in)
+    const float2 top = sh.row_base[tid];
+    const double lse = static_cast<double>(top.x) + (log(static_cast<double>(sum)) - (static_cast<double>(top.y) + kBmBits) * 0.6931471805599453);
+    sh.base[tid] = !fine || done || sum == 0 ? none : static_cast<double>(score) - lse;
+  }
+  if (tid == 0) sh.n = 0;
   __syncthreads();
   // An entry of the lists goes by its place among them, a finished beam by lists * keep + beam.
   const uint2* part = p.part + row0 * p.chunks * p.keep;
-  const auto value = [&](int list, int rank) { return order_of(sh.base[list / p.chunks] + static_cast<double>(float_of(__ldcg(part + list * p.keep + rank).x))); };
+  const auto value_of = [&](int list, uint32_t x) { return order_of(sh.base[list / p.chunks] + static_cast<double>(float_of(x))); };
   const uint32_t finished = static_cast<uint32_t>(lists) * p.keep, of_row = static_cast<uint32_t>(p.chunks) * p.keep;
   const auto row_of = [&](uint32_t x) { return x >= finished ? x - finished : x / of_row; };
   // Equal values: the lower row; in a row the larger logit (which 64 bits of the value may not show), then the lower token.
@@ -281,50 +401,53 @@ __device__ __forceinline__ void bm_join(const BmParams& p, BmShared& sh, unsigne
   };
   const unsigned long long nothing = order_of(none);
   const auto offers = [&](int list) { return sh.base[list / p.chunks] > none; };
-  // what comes before the k-th of the threads' best heads, and before every list's k-th
-  unsigned long long bv = nothing, lv = nothing;
-  for (int l = tid; l < lists; l += kBmThreads)
+  // A bound that at least n_keep entries reach, as in a chunk: of the lists' `deep`-th entries (lists go round the warps); and the
+  // largest of their last ones.
+  const int deep = min(p.keep, (2 * p.keep + lists - 1) / lists);
+  const int nth = ((p.keep + deep - 1) / deep + kBmWarps - 1) / kBmWarps;
+  unsigned long long tv = nothing, lv = nothing;
+  const int mine = warp + lane * kBmWarps;
+  for (int l = mine; l < lists; l += kBmThreads)
     if (offers(l)) {
-      bv = max(bv, value(l, 0));
-      lv = max(lv, value(l, p.keep - 1));
+      const uint32_t a = __ldcg(part + l * p.keep + deep - 1).x, z = __ldcg(part + l * p.keep + p.keep - 1).x;
+      tv = max(tv, value_of(l, a));
+      lv = max(lv, value_of(l, z));
     }
-  unsigned long long tv;
-  uint32_t tx;
-  bound_of(sh, bv, 0u, p.keep, &tv, &tx);
-  sh.top[tid] = lv;
-  __syncthreads();
-  for (int o = kBmThreads / 2; o > 0; o >>= 1) {
-    if (tid < o) sh.top[tid] = max(sh.top[tid], sh.top[tid + o]);
-    __syncthreads();
+  tv = nth_of(tv, nth, lane);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) lv = max(lv, __shfl_xor_sync(0xffffffffu, lv, o));
+  if (lane == 0) {
+    sh.bound[warp] = tv;
+    sh.last_of[warp] = lv;
   }
-  tv = max(max(tv, sh.top[0]), nothing + 1);
-  // finished beams go on as they are
-  int n = 0;  // entries in the pool; the first ones are the best so far
-  if (tid == 0) sh.n = 0;
   __syncthreads();
-  if (tid < p.beams && p.done && __ldcg(p.done + row0 + tid)) {
-    const float s = p.score ? __ldcg(p.score + row0 + tid) : 0.f;
-    if (s > -INFINITY && s < INFINITY) {
-      const int at = atomicAdd(&sh.n, 1);
-      val[at] = order_of(static_cast<double>(s));
-      idx[at] = finished + tid;
-    }
+#pragma unroll
+  for (int i = 0; i < kBmWarps; ++i) {
+    tv = min(tv, sh.bound[i]);
+    lv = max(lv, sh.last_of[i]);
   }
-  // Lists in turns of one a thread; where the pool could overflow, what it has is cut to the best and the bound raised.
+  tv = max(max(tv, lv), nothing + 1);
+  int n = 0;  // entries in the pool
+  if (goes_on) {
+    const int at = atomicAdd(&sh.n, 1);
+    val[at] = order_of(static_cast<double>(score));
+    idx[at] = finished + tid;
+  }
+  // The lists' entries that reach it, four of a list at a time; where the pool could overflow, what it has is cut to the best and
+  // the bound raised.
+  constexpr int kStep = 4;
   for (int l0 = 0; l0 < lists; l0 += kBmThreads) {
-    const int l = l0 + tid;
+    const int l = l0 + mine;
     bool more = l < lists && offers(l);
-    for (int r0 = 0; r0 < p.keep && __syncthreads_or(more); r0 += 8) {
+    for (int r0 = 0; r0 < p.keep && __syncthreads_or(more); r0 += kStep) {
       n = sh.n;
       __syncthreads();
-      if (n > kBmPool - 8 * kBmThreads) {
+      if (n > kBmPool - kStep * kBmThreads) {
         unsigned long long kept_v = 0;
         uint32_t kept_x = 0;
         bool kept = false;
         int at = 0;
-        pick(val, idx, n, p.keep, first_of, [&](int rank, unsigned long long v, uint32_t x) {
-          kept_v = v, kept_x = x, kept = true, at = rank;
-        });
+        pick(val, idx, n, p.keep, first_of, [&](int rank, unsigned long long v, uint32_t x) { kept_v = v, kept_x = x, kept = true, at = rank; });
         if (kept) {
           val[at] = kept_v;
           idx[at] = kept_x;
@@ -333,13 +456,19 @@ __device__ __forceinline__ void bm_join(const BmParams& p, BmShared& sh, unsigne
         __syncthreads();
         if (n >= p.keep) tv = max(tv, val[p.keep - 1]);
       }
-      for (int r = r0; more && r < min(r0 + 8, p.keep); ++r) {
-        const unsigned long long v = value(l, r);
-        more = v >= tv;
-        if (more) {
-          const int to = atomicAdd(&sh.n, 1);
-          val[to] = v;
-          idx[to] = static_cast<uint32_t>(l) * p.keep + r;
+      if (more) {
+        uint32_t e[kStep];
+#pragma unroll
+        for (int r = 0; r < kStep; ++r) e[r] = r0 + r < p.keep ? __ldcg(part + l * p.keep + r0 + r).x : order_of(-INFINITY);
+#pragma unroll
+        for (int r = 0; r < kStep; ++r) {
+          const unsigned long long v = value_of(l, e[r]);
+          more = more && v >= tv;
+          if (more) {
+            const int to = atomicAdd(&sh.n, 1);
+            val[to] = v;
+            idx[to] = static_cast<uint32_t>(l) * p.keep + r0 + r;
+          }
         }
       }
     }
@@ -359,7 +488,7 @@ __device__ __forceinline__ void bm_join(const BmParams& p, BmShared& sh, unsigne
 }
 
 template <typename T, int EPT>
-__global__ void __launch_bounds__(kBmThreads) beam_kernel(const __grid_constant__ BmParams p) {
+__global__ void __launch_bounds__(kBmThreads, 3) beam_kernel(const __grid_constant__ BmParams p) {
   extern __shared__ __align__(16) uint8_t bm_dyn[];
   __shared__ BmShared sh;
   unsigned long long* val = reinterpret_cast<unsigned long long*>(bm_dyn);
@@ -431,7 +560,7 @@ extern "C" tss_status tss_beam_create(int max_rows, int vocab, int max_keep, tss
   if (e == cudaSuccess) e = cudaMalloc(&h->counters, sizeof(int) * static_cast<size_t>(max_rows));
   if (e == cudaSuccess) e = zero_now(h->counters, sizeof(int) * static_cast<size_t>(max_rows));
   if (e == cudaSuccess) e = cudaMalloc(&h->part, sizeof(uint2) * static_cast<size_t>(h->lists) * max_keep);
-  if (e == cudaSuccess) e = cudaMalloc(&h->sums, sizeof(double2) * static_cast<size_t>(h->lists));
+  if (e == cudaSuccess) e = cudaMalloc(&h->sums, sizeof(longlong2) * static_cast<size_t>(h->lists));
   if (e != cudaSuccess) {
     tss_beam_destroy(h);
     const tss_status r = refuse_cuda(e, "workspace");
