@@ -28,7 +28,7 @@ namespace {
 
 constexpr int kBmThreads = 256, kBmWarps = kBmThreads / 32;
 constexpr int kBmKeep = 128, kBmBeams = 64;
-constexpr int kBmPool = 4096;     // candidates that the join holds at once
+constexpr int kBmPool = 2048;     // candidates that are held at once: at least 1024 beside 512
 constexpr float kBmMost = 1e38f;  // logits from here on count as infinite, those from minus that on down as masked
 
 struct BmParams {
@@ -59,6 +59,24 @@ __device__ __forceinline__ unsigned long long order_of(double x) {
 __device__ __forceinline__ double double_of(unsigned long long o) {
   return __longlong_as_double(static_cast<long long>(o >> 63 ? o & 0x7fffffffffffffffull : ~o));
 }
+// A CTA's dynamic shared memory: candidates (value, index); of a chunk's groups the largest element, the sum, and those that are
+// looked at again.
+constexpr int kBmTiles = 8, kBmGroups = kBmTiles * kBmThreads;
+struct BmSpace {
+  unsigned long long* val;
+  uint32_t* idx;
+  float *most, *sum;
+  uint16_t* group;
+  static constexpr int kBytes = kBmPool * 12 + kBmGroups * 10;
+  __device__ __forceinline__ explicit BmSpace(uint8_t* at) {
+    val = reinterpret_cast<unsigned long long*>(at);
+    idx = reinterpret_cast<uint32_t*>(val + kBmPool);
+    most = reinterpret_cast<float*>(idx + kBmPool);
+    sum = most + kBmGroups;
+    group = reinterpret_cast<uint16_t*>(sum + kBmGroups);
+  }
+};
+
 // (value, index): larger values first, then lower indices
 __device__ __forceinline__ bool ahead(unsigned long long a, uint32_t ai, unsigned long long b, uint32_t bi) { return a > b || (a == b && ai < bi); }
 
@@ -74,11 +92,14 @@ struct BmBase {
   }
 };
 // 2^t by the fast exponential (2^-22 of it).
+__device__ __forceinline__ float bm_ex2(float t) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(t));
+  return y;
+}
 __device__ __forceinline__ float bm_term(float x, float m, float f) {
   const float d = x - m;
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(fmaf(d, kLog2eHi, fmaf(d, kLog2eLo, f))));
-  return y;
+  return bm_ex2(fmaf(d, kLog2eHi, fmaf(d, kLog2eLo, f)));
 }
 // 2^t to about 2^-28 of it, times 2^kBmBits and rounded to a whole number: 2^n e^u with u in two floats, e^u = 1 + u + u^2 q(u).
 constexpr int kBmBits = 37;  // 2^24 terms of up to 2 stay below 2^63
@@ -99,28 +120,46 @@ __device__ __forceinline__ long long bm_fixed(float x, float m, float f) {
   const float scale = __uint_as_float(static_cast<uint32_t>(static_cast<int>(n) + kBmBits + 127) << 23);
   return __float2ll_rn(scale) + __float2ll_rn(u * scale) + __float2ll_rn(e * scale);
 }
+// A sum relative to another base, of a larger logit: a shift, rounded.
+__device__ __forceinline__ long long bm_down(long long sum, const BmBase& from, const BmBase& to) {
+  const float down = (to.hi - from.hi) + (to.lo - from.lo);  // (whole; below 2^24 exact, beyond that nothing is left)
+  if (!(down < 62.f)) return 0;
+  const int k = max(static_cast<int>(down), 0);
+  return k > 0 ? (sum + (1ll << (k - 1))) >> k : sum;
+}
 __device__ __forceinline__ long long bm_fixed(float y) { return __float2ll_rn(y * static_cast<float>(1ll << kBmBits)); }
 
-// The first k of n entries (value, index) in shared memory, which has room for the next power of two from n on, in the order of
-// `before`, to `put(rank, value, index)`; all threads.
+// n entries (value, index) in shared memory, which has room for the next power of two from n on, in the order of `before` to
+// `put(rank, value, index)`; all threads (one of the first 256 ranks goes to a thread at most).
 template <typename Before, typename Put>
-__device__ __forceinline__ void pick(unsigned long long* val, uint32_t* idx, int n, int k, Before before, Put put) {
+__device__ __forceinline__ void pick(unsigned long long* val, uint32_t* idx, int n, Before before, Put put) {
   const int tid = threadIdx.x;
   __syncthreads();
-  if (n <= kBmThreads) {  // by counting who comes before: up to 8 threads an entry
+  if (n <= kBmThreads) {  // by counting who comes before: up to 8 threads an entry; indices only where values are equal
     int per = 8;
     while (per > 1 && n * per > kBmThreads) per /= 2;
     const int e = tid / per, part = tid & (per - 1);
     unsigned long long v = 0;
-    uint32_t x = 0;
-    int rank = 0;
+    int rank = 0, same = 0;
     if (e < n) {
       v = val[e];
-      x = idx[e];
-      for (int j = part; j < n; j += per) rank += before(val[j], idx[j], v, x);
+#pragma unroll 4
+      for (int j = part; j < n; j += per) {
+        const unsigned long long o = val[j];
+        rank += o > v;
+        same += o == v;
+      }
     }
-    for (int o = per / 2; o > 0; o /= 2) rank += __shfl_xor_sync(0xffffffffu, rank, o);
-    if (e < n && part == 0 && rank < k) put(rank, v, x);
+    for (int o = per / 2; o > 0; o /= 2) {
+      rank += __shfl_xor_sync(0xffffffffu, rank, o);
+      same += __shfl_xor_sync(0xffffffffu, same, o);
+    }
+    if (e < n && part == 0) {
+      const uint32_t x = idx[e];
+      if (same > 1)
+        for (int j = 0; j < n; ++j) rank += val[j] == v && before(v, idx[j], v, x);
+      put(rank, v, x);
+    }
   } else {  // bitonic sort
     int size = 2 * kBmThreads;
     while (size < n) size *= 2;
@@ -142,169 +181,246 @@ __device__ __forceinline__ void pick(unsigned long long* val, uint32_t* idx, int
         }
       }
     __syncthreads();
-    for (int j = tid; j < min(n, k); j += kBmThreads) put(j, val[j], idx[j]);
+    for (int j = tid; j < n; j += kBmThreads) put(j, val[j], idx[j]);
   }
   __syncthreads();
+}
+
+// The pool's entries cut to the k best, in order; their number.
+template <typename Before>
+__device__ __forceinline__ int cut(unsigned long long* val, uint32_t* idx, int n, int k, int* count, Before before) {
+  unsigned long long kept_v = 0;
+  uint32_t kept_x = 0;
+  int at = -1;
+  pick(val, idx, n, before, [&](int rank, unsigned long long v, uint32_t x) {
+    if (rank < k) kept_v = v, kept_x = x, at = rank;
+  });
+  if (at >= 0) {
+    val[at] = kept_v;
+    idx[at] = kept_x;
+  }
+  if (threadIdx.x == 0) *count = min(n, k);
+  __syncthreads();
+  return min(n, k);
 }
 
 struct BmShared {
-  unsigned long long top[kBmThreads];
-  uint32_t top_idx[kBmThreads];
   long long sum[kBmWarps];
   double base[kBmBeams];               // score - ln sum of each row
-  float most[kBmWarps], least[kBmWarps];
-  unsigned long long bound[kBmWarps], last_of[kBmWarps];
   long long row_sum[kBmBeams];
-  float2 row_base[kBmBeams];
-  int n, last;
+  float2 row_base[kBmBeams];           // its largest logit m, and f
+  float2 near[kBmBeams];               // base in 32 bits, and how far off that may be
+  float sorted[kBmWarps][32], most[kBmWarps], kth;
+  float score[kBmBeams];
+  int alive[kBmBeams];                 // 1: the row's logits count; 2: it is finished
+  int n, groups, tiny, last;
 };
 
-// The m-th largest of a warp's values, m in [1, 32] (in all lanes).
-template <typename V>
-__device__ __forceinline__ V nth_of(V v, int m, int lane) {
-  int rank = 0;
+// The k-th largest of the threads' values, k in [1, 256]: every warp sorts its own, and each finds its place among the others'.
+// (The caller has a barrier before the next call.)
+__device__ __forceinline__ float kth_of(BmShared& sh, float v, int k) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
-  for (int j = 0; j < 32; ++j) {
-    const V o = __shfl_sync(0xffffffffu, v, j);
-    rank += o > v || (o == v && j < lane);
+  for (int run = 2; run <= 32; run *= 2)
+#pragma unroll
+    for (int step = run / 2; step > 0; step /= 2) {
+      const float o = __shfl_xor_sync(0xffffffffu, v, step);
+      v = ((lane & step) == 0) == ((lane & run) == 0) ? fmaxf(v, o) : fminf(v, o);  // (descending; the last run is of all)
+    }
+  sh.sorted[warp][lane] = v;
+  __syncthreads();
+  int rank = lane;
+#pragma unroll
+  for (int i = 1; i < kBmWarps; ++i) {
+    const int w = (warp + i) % kBmWarps;
+    int at = 0;  // of the warp's values those that come before
+#pragma unroll
+    for (int step = 16; step > 0; step /= 2) {
+      const float o = sh.sorted[w][at + step - 1];
+      if (o > v || (o == v && w < warp)) at += step;
+    }
+    const float o = sh.sorted[w][min(at, 31)];
+    rank += at + (at < 32 && (o > v || (o == v && w < warp)));
   }
-  return __shfl_sync(0xffffffffu, v, __ffs(__ballot_sync(0xffffffffu, rank == m - 1)) - 1);
+  if (rank == k - 1) sh.kth = v;
+  __syncthreads();
+  return sh.kth;
 }
 
-// The k-th of the threads' own largest entries: at least k entries are at or before it, and no others than those threads' are
-// before it.
-__device__ __forceinline__ void bound_of(BmShared& sh, unsigned long long v, uint32_t x, int k, unsigned long long* tv, uint32_t* tx) {
-  const int tid = threadIdx.x;
-  __syncthreads();
-  sh.top[tid] = v;
-  sh.top_idx[tid] = x;
-  __syncthreads();
-  int rank = 0;
-  for (int j = 0; j < kBmThreads; ++j) rank += ahead(sh.top[j], sh.top_idx[j], v, x) || (sh.top[j] == v && sh.top_idx[j] == x && j < tid);
-  __syncthreads();
-  if (rank == k - 1) {
-    sh.top[0] = v;
-    sh.top_idx[0] = x;
+template <typename T>
+struct Pair { using type = __half2; };
+template <>
+struct Pair<__nv_bfloat16> { using type = __nv_bfloat162; };
+
+// A tile is EPT elements a thread, in vectors of 16 bytes that go round the threads; a thread's part of one is a group.
+template <typename T, int EPT>
+struct BmTile {
+  static constexpr int VEC = 16 / sizeof(T), NV = EPT / VEC, kElems = kBmThreads * EPT;
+  // Place in the tile of element i of thread tid's group.
+  static __device__ __forceinline__ int at(int tid, int i) { return (tid + i / VEC * kBmThreads) * VEC + i % VEC; }
+  // The group's elements of src, which has n, on their way; `whole`: src is aligned to 16 bytes.
+  uint4 raw[NV];
+  __device__ __forceinline__ void fetch(const T* src, int n, bool whole) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int a = at(threadIdx.x, i * VEC);
+      if (whole && a + VEC <= n) {
+        raw[i] = *reinterpret_cast<const uint4*>(src + a);
+      } else {
+        T t[VEC];
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) t[j] = a + j < n ? src[a + j] : from_f32<T>(-INFINITY);
+        memcpy(&raw[i], t, 16);
+      }
+    }
   }
-  __syncthreads();
-  *tv = sh.top[0];
-  *tx = sh.top_idx[0];
-}
+  __device__ __forceinline__ float get(int i) const {
+    T t[VEC];
+    memcpy(t, &raw[i / VEC], 16);
+    return to_f32(t[i % VEC]);
+  }
+  // The largest (16-bit ones two at a time).
+  __device__ __forceinline__ float most() const {
+    if constexpr (sizeof(T) == 4) {
+      float m = get(0);
+#pragma unroll
+      for (int i = 1; i < EPT; ++i) m = fmaxf(m, get(i));
+      return m;
+    } else {
+      using T2 = typename Pair<T>::type;
+      T2 t[NV * 4];
+      memcpy(t, raw, sizeof(raw));
+#pragma unroll
+      for (int i = 1; i < NV * 4; ++i) t[0] = __hmax2(t[0], t[i]);
+      return fmaxf(to_f32(t[0].x), to_f32(t[0].y));
+    }
+  }
+};
 
 // A chunk of a live row: its largest entries and its sum.
 template <typename T, int EPT>
-__device__ __forceinline__ void bm_chunk(const BmParams& p, BmShared& sh, unsigned long long* val, uint32_t* idx, long long row, int chunk) {
-  constexpr int VEC = 16 / sizeof(T), NV = EPT / VEC;
+__device__ __forceinline__ void bm_chunk(const BmParams& p, BmShared& sh, const BmSpace& sp, long long row, int chunk) {
+  using Tile = BmTile<T, EPT>;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int e0 = chunk * p.len, n = min(p.len, p.vocab - e0);
+  const int e0 = chunk * p.len, n_el = min(p.len, p.vocab - e0);
   const T* src = static_cast<const T*>(p.logits) + row * p.stride + e0;
   const bool whole = (reinterpret_cast<uintptr_t>(src) & 15u) == 0;
-  float x[EPT];
+  if (tid == 0) sh.n = sh.groups = 0;
+  // ---- the groups' largest elements, and their sums relative to them; the next tile is on its way meanwhile ----
+  float best = -INFINITY;
+  bool odd = false;
+  int tiles = 0;
+  Tile next;
+  next.fetch(src, n_el, whole);
+  for (int t0 = 0; t0 < n_el; t0 += Tile::kElems, ++tiles) {
+    const Tile now = next;
+    if (t0 + Tile::kElems < n_el) next.fetch(src + t0 + Tile::kElems, n_el - t0 - Tile::kElems, whole);
+    const float g = now.most(), m = g > -kBmMost ? g : 0.f;
+    const BmBase base(m);
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    if (fabsf(m) < 1e6f) {  // (R is one float, and what x log2e loses is less than 2^-22 beside it)
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int at = (tid + i * kBmThreads) * VEC;
-    if (whole && at + VEC <= n) {
-      load_vec<T, VEC>(src + at, x + i * VEC);
+      for (int i = 0; i < EPT; ++i) {
+        const float x = now.get(i);
+        s[i & 3] += bm_ex2(fmaf(x, kLog2eLo, fmaf(x, kLog2eHi, -base.hi)));
+      }
     } else {
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) x[i * VEC + j] = at + j < n ? to_f32(src[at + j]) : -INFINITY;
+      for (int i = 0; i < EPT; ++i) s[i & 3] += bm_term(now.get(i), m, base.f);
     }
+    const float sum = (s[0] + s[1]) + (s[2] + s[3]);
+    sp.most[tiles * kBmThreads + tid] = g;
+    sp.sum[tiles * kBmThreads + tid] = sum;
+    best = fmaxf(best, g);
+    odd |= sum != sum || !(g < kBmMost);
   }
-  if (tid == 0) sh.n = 0;
-  float mv[NV], most = -INFINITY;  // the vectors' maxima
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    mv[i] = x[i * VEC];
-#pragma unroll
-    for (int j = 1; j < VEC; ++j) mv[i] = fmaxf(mv[i], x[i * VEC + j]);
-    most = fmaxf(most, mv[i]);
-  }
-  const auto token = [&](int i) { return static_cast<uint32_t>(e0 + (tid + i / VEC * kBmThreads) * VEC + i % VEC); };
-  // A bound that at least n_keep elements reach: of every warp the ceil(n_keep / 8)-th largest of its threads' maxima, the least
-  // of these.
-  float m = most, least;
+  // ---- the chunk's largest, and a bound that at least n_keep elements reach: the n_keep-th largest of the threads' own, or, of
+  // up to 8, the least of the warps' ----
+  float m = best;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  least = p.keep <= kBmWarps ? m : nth_of(most, (p.keep + kBmWarps - 1) / kBmWarps, lane);
-  if (lane == 0) {
-    sh.most[warp] = m;
-    sh.least[warp] = least;
-  }
-  __syncthreads();
+  float least = m;
+  if (lane == 0) sh.most[warp] = m;
+  odd = __syncthreads_or(odd);
 #pragma unroll
   for (int i = 0; i < kBmWarps; ++i) {
     m = fmaxf(m, sh.most[i]);
-    least = fminf(least, sh.least[i]);
+    least = fminf(least, sh.most[i]);
   }
+  if (p.keep > kBmWarps) least = kth_of(sh, best, p.keep);
   const long long list = row * p.chunks + chunk;
   uint2* part = p.part + list * p.keep;
-  const auto offer_nothing = [&](bool bad) {
-    if (tid == 0) __stcg(p.sums + list, make_longlong2(0, (bad ? 1ll << 32 : 0ll) | __float_as_uint(-INFINITY)));
+  if (odd || m <= -kBmMost) {  // nothing to offer
+    if (tid == 0) __stcg(p.sums + list, make_longlong2(0, (odd ? 1ll << 32 : 0ll) | __float_as_uint(-INFINITY)));
     if (tid < p.keep) __stcg(part + tid, make_uint2(order_of(-INFINITY), 0u));
-  };
-  const BmBase base(m);
-  // Elements that reach the bound become candidates, whose terms are added up apart; a NaN shows in the sum of the others.
-  float s[2] = {0.f, 0.f};
-#pragma unroll
-  for (int i = 0; i < EPT; ++i) {
-    const float y = bm_term(x[i], m, base.f);
-    if (!(x[i] >= least)) s[i & 1] += y;
-  }
-#pragma unroll
-  for (int i = 0; i < NV; ++i)
-    if (mv[i] >= least) {
-#pragma unroll
-      for (int j = 0; j < VEC; ++j)
-        if (x[i * VEC + j] >= least && x[i * VEC + j] > -kBmMost) {
-          const int at = atomicAdd(&sh.n, 1);
-          if (at < kBmPool) {
-            val[at] = order_of(x[i * VEC + j]);
-            idx[at] = token(i * VEC + j);
-          }
-        }
-    }
-  const float odd = s[0] + s[1];
-  if (__syncthreads_or(odd != odd || !(m < kBmMost)) || m <= -kBmMost) {
-    // (where all are masked the difference from the largest is a NaN too)
-    bool bad = !(m < kBmMost);
-#pragma unroll
-    for (int i = 0; i < EPT; ++i) bad |= x[i] != x[i];
-    offer_nothing(__syncthreads_or(bad));
     return;
   }
-  int found = sh.n;
-  long long sum = bm_fixed(s[0]) + bm_fixed(s[1]);
-  if (found > kBmPool / 4) {
-    // Too many (a run of masked elements, or of equal ones): the n_keep-th of the threads' best is the bound, which n_keep
-    // threads' elements reach at most; the candidates' terms are taken as the others' are.
-    __syncthreads();  // (all have read how many)
-    int where = 0;
-    float s2 = 0.f;
-#pragma unroll
-    for (int i = EPT - 1; i >= 0; --i) {
-      if (x[i] == most) where = i;
-      if (x[i] >= least) s2 += bm_term(x[i], m, base.f);
-    }
-    sum += bm_fixed(s2);
-    if (tid == 0) sh.n = 0;
-    unsigned long long tv;
-    uint32_t tx;
-    bound_of(sh, order_of(most), most > -kBmMost ? token(where) : 0xffffffffu, p.keep, &tv, &tx);
-    const float from = float_of(static_cast<uint32_t>(tv));
-#pragma unroll
-    for (int i = 0; i < EPT; ++i)
-      if (x[i] >= from && x[i] > -kBmMost && !ahead(tv, tx, order_of(x[i]), token(i))) {
-        const int at = atomicAdd(&sh.n, 1);
-        val[at] = order_of(x[i]);
-        idx[at] = token(i);
-      }
-    __syncthreads();
-    found = sh.n;
-  } else {
-    for (int j = tid; j < found; j += kBmThreads) sum += bm_fixed(float_of(static_cast<uint32_t>(val[j])), m, base.f);
+  // ---- groups that reach the bound are looked at again, the others' sums added up ----
+  const BmBase base(m);
+  long long sum = 0;
+  for (int t = 0; t < tiles; ++t) {
+    const int id = t * kBmThreads + tid;
+    const float g = sp.most[id];
+    if (!(g > -kBmMost)) continue;
+    if (g >= least)
+      sp.group[atomicAdd(&sh.groups, 1)] = static_cast<uint16_t>(id);
+    else
+      sum += bm_down(bm_fixed(sp.sum[id]), BmBase(g), base);
   }
-  pick(val, idx, found, p.keep, ahead, [&](int rank, unsigned long long v, uint32_t t) { __stcg(part + rank, make_uint2(static_cast<uint32_t>(v), t)); });
-  for (int r = found + tid; r < p.keep; r += kBmThreads) __stcg(part + r, make_uint2(order_of(-INFINITY), 0u));
+  __syncthreads();
+  const int groups = sh.groups;
+  // An element a lane: its term, and itself into the pool if it reaches the bound; where the pool could overflow it is cut to the
+  // n_keep best, and others have to come before the last of them.
+  constexpr int kAt = kBmThreads / EPT, kRound = 4, kFlight = 8;  // groups of a pass; passes of a round, and whose loads are in flight
+  unsigned long long cv = 0;
+  uint32_t cx = 0;
+  int n = 0;
+  for (int g0 = 0; g0 < groups; g0 += kAt * kFlight) {
+    float x[kFlight];
+    uint32_t at[kFlight];
+#pragma unroll
+    for (int u = 0; u < kFlight; ++u) {
+      const int g = g0 + u * kAt + tid / EPT;
+      x[u] = -INFINITY;
+      at[u] = 0;
+      if (g < groups) {
+        const int id = sp.group[g];
+        at[u] = id / kBmThreads * Tile::kElems + Tile::at(id % kBmThreads, tid % EPT);
+        if (static_cast<int>(at[u]) < n_el) x[u] = to_f32(src[at[u]]);
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < kFlight; r += kRound) {
+      if (g0 + kAt * r >= groups) break;
+#pragma unroll
+      for (int u = r; u < r + kRound; ++u) {
+        if (!(x[u] > -kBmMost)) continue;
+        sum += bm_fixed(x[u], m, base.f);
+        const unsigned long long v = order_of(x[u]);
+        if (x[u] >= least && !ahead(cv, cx, v, e0 + at[u])) {
+          const int to = atomicAdd(&sh.n, 1);
+          sp.val[to] = v;
+          sp.idx[to] = e0 + at[u];
+        }
+      }
+      __syncthreads();
+      n = sh.n;
+      if (g0 + kAt * (r + kRound) >= groups) break;
+      __syncthreads();
+      if (n > kBmPool / 4) {
+        n = cut(sp.val, sp.idx, n, p.keep, &sh.n, ahead);
+        if (n == p.keep) {
+          cv = sp.val[n - 1];
+          cx = sp.idx[n - 1];
+        }
+        __syncthreads();
+      }
+    }
+  }
+  pick(sp.val, sp.idx, n, ahead, [&](int rank, unsigned long long v, uint32_t t) {
+    if (rank < p.keep) __stcg(part + rank, make_uint2(static_cast<uint32_t>(v), t));
+  });
+  for (int r = n + tid; r < p.keep; r += kBmThreads) __stcg(part + r, make_uint2(order_of(-INFINITY), 0u));
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
   if (lane == 0) sh.sum[warp] = sum;
@@ -317,169 +433,182 @@ __device__ __forceinline__ void bm_chunk(const BmParams& p, BmShared& sh, unsign
 }
 
 // The group's chunks are done: its best.
-__device__ __forceinline__ void bm_join(const BmParams& p, BmShared& sh, unsigned long long* val, uint32_t* idx, int group) {
+__device__ __forceinline__ void bm_join(const BmParams& p, BmShared& sh, const BmSpace& sp, int group) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const long long row0 = static_cast<long long>(group) * p.beams;
   const int lists = p.beams * p.chunks;
   const double none = -static_cast<double>(INFINITY);
-  // rows' sums: a warp takes every eighth row, its lanes chunks; the rows' first chunks are on their way together
-  constexpr int kRows = kBmBeams / kBmWarps;
-  const auto alive = [&](int b) {
-    const float s = p.score ? __ldcg(p.score + row0 + b) : 0.f;
-    return s > -INFINITY && s < INFINITY && !(p.done && __ldcg(p.done + row0 + b));
-  };
+  const uint2* part = p.part + row0 * p.chunks * p.keep;
+  const longlong2* sums = p.sums + row0 * p.chunks;
+  // The thread's first list's first entries, those that the bound comes from and the first chunks' sums are on their way together
+  // (lists go round the warps; what rows without logits that count have left there is not used).
+  constexpr int kStep = 4, kHead = 2 * kStep, kRows = kBmBeams / kBmWarps;
+  const int deep = min(p.keep, (2 * p.keep + lists - 1) / lists), mine = warp + lane * kBmWarps;
+  const auto entry = [&](int l, int r) { return l < lists && r < p.keep ? __ldcg(part + l * p.keep + r) : make_uint2(order_of(-INFINITY), 0u); };
+  uint2 head[kHead];
+#pragma unroll
+  for (int r = 0; r < kHead; ++r) head[r] = entry(mine, r);
+  const uint32_t deep_x = entry(mine, deep - 1).x, last_x = entry(mine, p.keep - 1).x;
   longlong2 first[kRows];
 #pragma unroll
   for (int i = 0; i < kRows; ++i) {
     const int b = warp + i * kBmWarps;
-    first[i] = make_longlong2(0, __float_as_uint(-INFINITY));
-    if (b < p.beams && lane < p.chunks && alive(b)) first[i] = __ldcg(p.sums + (row0 + b) * p.chunks + lane);
+    if (b < p.beams && lane < p.chunks) first[i] = __ldcg(sums + b * p.chunks + lane);
   }
+  if (tid < p.beams) {
+    const float s = p.score ? __ldcg(p.score + row0 + tid) : 0.f;
+    const int done = p.done ? __ldcg(p.done + row0 + tid) : 0;
+    sh.score[tid] = s;
+    sh.alive[tid] = !(s > -INFINITY && s < INFINITY) ? 0 : done ? 2 : 1;
+    if (!(s < INFINITY)) report(p.status, kStatusCheck);
+  }
+  if (tid == 0) sh.n = sh.tiny = 0;
+  __syncthreads();
+  // ---- rows: a warp takes every eighth, its lanes the chunks ----
 #pragma unroll
   for (int i = 0; i < kRows; ++i) {
     const int b = warp + i * kBmWarps;
     if (b >= p.beams) break;
-    const bool on = alive(b);
     float m = -INFINITY;
     bool bad = false;
-    for (int c = lane; c < p.chunks; c += 32) {
-      const longlong2 x = c < 32 ? first[i] : on ? __ldcg(p.sums + (row0 + b) * p.chunks + c) : make_longlong2(0, __float_as_uint(-INFINITY));
-      m = fmaxf(m, __uint_as_float(static_cast<uint32_t>(x.y)));
-      bad |= x.y >> 32 != 0;
+    long long sum = 0;
+    if (sh.alive[b] == 1) {
+      for (int c = lane; c < p.chunks; c += 32) {
+        const longlong2 x = c < 32 ? first[i] : __ldcg(sums + b * p.chunks + c);
+        m = fmaxf(m, __uint_as_float(static_cast<uint32_t>(x.y)));
+        bad |= x.y >> 32 != 0;
+      }
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
     bad = __any_sync(0xffffffffu, bad);
     const BmBase top(m);
-    long long sum = 0;
-    for (int c = lane; c < p.chunks; c += 32) {
-      const longlong2 x = c < 32 ? first[i] : on ? __ldcg(p.sums + (row0 + b) * p.chunks + c) : make_longlong2(0, __float_as_uint(-INFINITY));
-      if (x.x == 0) continue;
-      const BmBase mine(__uint_as_float(static_cast<uint32_t>(x.y)));
-      const float down = (top.hi - mine.hi) + (top.lo - mine.lo);  // (whole; below 2^24 exact, beyond that nothing is left)
-      if (down < 62.f) {
-        const int k = max(static_cast<int>(down), 0);
-        sum += k > 0 ? (x.x + (1ll << (k - 1))) >> k : x.x;
+    if (m > -kBmMost)
+      for (int c = lane; c < p.chunks; c += 32) {
+        const longlong2 x = c < 32 ? first[i] : __ldcg(sums + b * p.chunks + c);
+        if (x.x != 0) sum += bm_down(x.x, BmBase(__uint_as_float(static_cast<uint32_t>(x.y))), top);
       }
-    }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     if (lane == 0) {
-      sh.row_sum[b] = bad ? 0 : sum;
+      if (bad) sum = 0;
+      sh.row_sum[b] = sum;
       sh.row_base[b] = make_float2(m, top.f);
+      const float s = sh.score[b];
+      sh.near[b] = sum > 0 ? make_float2(s - (m + (log2f(static_cast<float>(sum)) - top.f - kBmBits) * 0.69314718f), (fabsf(s) + fabsf(m) + 64.f) * 0x1p-20f)
+                           : make_float2(-INFINITY, 0.f);
       if (bad) report(p.status, kStatusCheck);
     }
   }
   __syncthreads();
-  bool goes_on = false;  // the thread's row is finished and goes on as it is
-  float score = 0.f;
+  // An entry goes by its place: row * of_row + chunk * keep + rank, a finished beam's by the row's last.
+  const uint32_t in_row = static_cast<uint32_t>(p.chunks) * p.keep, of_row = in_row + 1;
   if (tid < p.beams) {
-    score = p.score ? __ldcg(p.score + row0 + tid) : 0.f;
-    if (!(score < INFINITY)) report(p.status, kStatusCheck);
-    const bool fine = score > -INFINITY && score < INFINITY, done = p.done && __ldcg(p.done + row0 + tid);
-    goes_on = fine && done;
-    const long long sum = sh.row_sum[tid];
     // (ln sum e^x = m + ln(2^-f sum of the terms): what R is does not come in)
     const float2 top = sh.row_base[tid];
-    const double lse = static_cast<double>(top.x) + (log(static_cast<double>(sum)) - (static_cast<double>(top.y) + kBmBits) * 0.6931471805599453);
-    sh.base[tid] = !fine || done || sum == 0 ? none : static_cast<double>(score) - lse;
-  }
-  if (tid == 0) sh.n = 0;
-  __syncthreads();
-  // An entry of the lists goes by its place among them, a finished beam by lists * keep + beam.
-  const uint2* part = p.part + row0 * p.chunks * p.keep;
-  const auto value_of = [&](int list, uint32_t x) { return order_of(sh.base[list / p.chunks] + static_cast<double>(float_of(x))); };
-  const uint32_t finished = static_cast<uint32_t>(lists) * p.keep, of_row = static_cast<uint32_t>(p.chunks) * p.keep;
-  const auto row_of = [&](uint32_t x) { return x >= finished ? x - finished : x / of_row; };
-  // Equal values: the lower row; in a row the larger logit (which 64 bits of the value may not show), then the lower token.
-  const auto first_of = [&](unsigned long long a, uint32_t ax, unsigned long long b, uint32_t bx) {
-    if (a != b) return a > b;
-    const uint32_t ar = row_of(ax), br = row_of(bx);
-    if (ar != br || ax >= finished) return ar < br;
-    const uint32_t av = __ldcg(part + ax).x, bv = __ldcg(part + bx).x;
-    return av > bv || (av == bv && ax < bx);  // (places of a row go by token where logits are equal)
-  };
-  const unsigned long long nothing = order_of(none);
-  const auto offers = [&](int list) { return sh.base[list / p.chunks] > none; };
-  // A bound that at least n_keep entries reach, as in a chunk: of the lists' `deep`-th entries (lists go round the warps); and the
-  // largest of their last ones.
-  const int deep = min(p.keep, (2 * p.keep + lists - 1) / lists);
-  const int nth = ((p.keep + deep - 1) / deep + kBmWarps - 1) / kBmWarps;
-  unsigned long long tv = nothing, lv = nothing;
-  const int mine = warp + lane * kBmWarps;
-  for (int l = mine; l < lists; l += kBmThreads)
-    if (offers(l)) {
-      const uint32_t a = __ldcg(part + l * p.keep + deep - 1).x, z = __ldcg(part + l * p.keep + p.keep - 1).x;
-      tv = max(tv, value_of(l, a));
-      lv = max(lv, value_of(l, z));
+    const long long sum = sh.row_sum[tid];
+    double base = none;
+    if (sum > 0)
+      base = static_cast<double>(sh.score[tid]) -
+             (static_cast<double>(top.x) + (log(static_cast<double>(sum)) - (static_cast<double>(top.y) + kBmBits) * 0.6931471805599453));
+    sh.base[tid] = base;
+    if (sh.alive[tid] == 2) {  // a finished beam goes on as it is
+      const int at = atomicAdd(&sh.n, 1);
+      sp.val[at] = order_of(static_cast<double>(sh.score[tid]));
+      sp.idx[at] = tid * of_row + in_row;
     }
-  tv = nth_of(tv, nth, lane);
+  }
+  // A bound that at least n_keep entries reach: of the lists' `deep`-th ones the ceil(n_keep / deep)-th largest, or the largest of
+  // their last ones; of values in 32 bits, less what these may be off (64-bit logarithms take their time meanwhile).
+  const auto least_of = [&](int l, uint32_t x) {
+    const float2 b = sh.near[l / p.chunks];
+    const float y = float_of(x);
+    return y > -INFINITY ? (b.x + y) - (b.y + fabsf(y) * 0x1p-20f) : -INFINITY;
+  };
+  float tf = mine < lists ? least_of(mine, deep_x) : -INFINITY, lf = mine < lists ? least_of(mine, last_x) : -INFINITY;
+  for (int l = mine + kBmThreads; l < lists; l += kBmThreads) {
+    tf = fmaxf(tf, least_of(l, entry(l, deep - 1).x));
+    lf = fmaxf(lf, least_of(l, entry(l, p.keep - 1).x));
+  }
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) lv = max(lv, __shfl_xor_sync(0xffffffffu, lv, o));
-  if (lane == 0) {
-    sh.bound[warp] = tv;
-    sh.last_of[warp] = lv;
-  }
-  __syncthreads();
+  for (int o = 16; o > 0; o >>= 1) lf = fmaxf(lf, __shfl_xor_sync(0xffffffffu, lf, o));
+  if (lane == 0) sh.most[warp] = lf;
+  tf = kth_of(sh, tf, (p.keep + deep - 1) / deep);
 #pragma unroll
-  for (int i = 0; i < kBmWarps; ++i) {
-    tv = min(tv, sh.bound[i]);
-    lv = max(lv, sh.last_of[i]);
-  }
-  tv = max(max(tv, lv), nothing + 1);
-  int n = 0;  // entries in the pool
-  if (goes_on) {
-    const int at = atomicAdd(&sh.n, 1);
-    val[at] = order_of(static_cast<double>(score));
-    idx[at] = finished + tid;
-  }
-  // The lists' entries that reach it, four of a list at a time; where the pool could overflow, what it has is cut to the best and
-  // the bound raised.
-  constexpr int kStep = 4;
+  for (int i = 0; i < kBmWarps; ++i) tf = fmaxf(tf, sh.most[i]);
+  const unsigned long long nothing = order_of(none);
+  unsigned long long tv = max(order_of(static_cast<double>(tf)), nothing + 1);
+  const auto value_of = [&](int list, uint32_t x) { return order_of(sh.base[list / p.chunks] + static_cast<double>(float_of(x))); };
+  const auto offers = [&](int list) { return list < lists && sh.base[list / p.chunks] > none; };
+  // Equal values: the lower row, then the lower token, which is the order of places; but where logits are so small that 64 bits of
+  // a value may not show their difference, the larger one of a row first.
+  const auto by_place = [](unsigned long long a, uint32_t ax, unsigned long long b, uint32_t bx) { return a > b || (a == b && ax < bx); };
+  const auto by_logit = [&](unsigned long long a, uint32_t ax, unsigned long long b, uint32_t bx) {
+    if (a != b || ax / of_row != bx / of_row || ax % of_row == in_row || ax == bx) return by_place(a, ax, b, bx);
+    const uint32_t av = __ldcg(part + ax - ax / of_row).x, bv = __ldcg(part + bx - bx / of_row).x;
+    return av > bv || (av == bv && ax < bx);
+  };
+  const auto sorted = [&](int n, auto put) {
+    if (sh.tiny)
+      pick(sp.val, sp.idx, n, by_logit, put);
+    else
+      pick(sp.val, sp.idx, n, by_place, put);
+  };
+  // ---- the lists' entries that reach it, a few of a list at a time; where the pool could overflow it is cut to the best and the
+  // bound raised ----
+  int n = 0;
+  const auto take = [&](int l, int r, uint2 e, bool* more) {
+    const unsigned long long v = value_of(l, e.x);
+    *more = *more && v >= tv;
+    if (*more) {
+      const int to = atomicAdd(&sh.n, 1);
+      sp.val[to] = v;
+      sp.idx[to] = static_cast<uint32_t>(l) * p.keep + r + l / p.chunks;
+      const float y = fabsf(float_of(e.x));
+      if (y < 1e-6f * fabsf(static_cast<float>(double_of(v)))) sh.tiny = 1;
+    }
+  };
   for (int l0 = 0; l0 < lists; l0 += kBmThreads) {
     const int l = l0 + mine;
-    bool more = l < lists && offers(l);
-    for (int r0 = 0; r0 < p.keep && __syncthreads_or(more); r0 += kStep) {
+    bool more = offers(l);
+    for (int r0 = 0;; r0 += kStep) {
+      const bool any = __syncthreads_or(more && r0 < p.keep);
       n = sh.n;
       __syncthreads();
       if (n > kBmPool - kStep * kBmThreads) {
         unsigned long long kept_v = 0;
         uint32_t kept_x = 0;
-        bool kept = false;
-        int at = 0;
-        pick(val, idx, n, p.keep, first_of, [&](int rank, unsigned long long v, uint32_t x) { kept_v = v, kept_x = x, kept = true, at = rank; });
-        if (kept) {
-          val[at] = kept_v;
-          idx[at] = kept_x;
+        int at = -1;
+        sorted(n, [&](int rank, unsigned long long v, uint32_t x) {
+          if (rank < p.keep) kept_v = v, kept_x = x, at = rank;
+        });
+        if (at >= 0) {
+          sp.val[at] = kept_v;
+          sp.idx[at] = kept_x;
         }
-        if (tid == 0) sh.n = min(n, p.keep);
+        n = min(n, p.keep);
+        if (tid == 0) sh.n = n;
         __syncthreads();
-        if (n >= p.keep) tv = max(tv, val[p.keep - 1]);
+        if (n == p.keep) tv = max(tv, sp.val[n - 1]);
+        __syncthreads();
       }
-      if (more) {
-        uint32_t e[kStep];
+      if (!any) break;
+      if (more && r0 < p.keep) {
+        uint2 e[kStep];
 #pragma unroll
-        for (int r = 0; r < kStep; ++r) e[r] = r0 + r < p.keep ? __ldcg(part + l * p.keep + r0 + r).x : order_of(-INFINITY);
+        for (int r = 0; r < kStep; ++r) e[r] = l0 > 0 || r0 >= kHead ? entry(l, r0 + r) : r0 ? head[kStep + r] : head[r];
 #pragma unroll
-        for (int r = 0; r < kStep; ++r) {
-          const unsigned long long v = value_of(l, e[r]);
-          more = more && v >= tv;
-          if (more) {
-            const int to = atomicAdd(&sh.n, 1);
-            val[to] = v;
-            idx[to] = static_cast<uint32_t>(l) * p.keep + r0 + r;
-          }
-        }
+        for (int r = 0; r < kStep; ++r) take(l, r0 + r, e[r], &more);
       }
     }
   }
-  __syncthreads();
-  n = sh.n;
   const long long out = static_cast<long long>(group) * p.keep;
-  pick(val, idx, n, p.keep, first_of, [&](int rank, unsigned long long v, uint32_t x) {
+  sorted(n, [&](int rank, unsigned long long v, uint32_t x) {
+    if (rank >= p.keep) return;
+    const uint32_t row = x / of_row;
     p.score_out[out + rank] = static_cast<float>(double_of(v));
-    p.parent[out + rank] = static_cast<int>(row0) + static_cast<int>(row_of(x));
-    p.token[out + rank] = x >= finished ? p.end_token : static_cast<int>(__ldcg(part + x).y);
+    p.parent[out + rank] = static_cast<int>(row0 + row);
+    p.token[out + rank] = x - row * of_row == in_row ? p.end_token : static_cast<int>(__ldcg(part + x - row).y);
   });
   for (int r = n + tid; r < p.keep; r += kBmThreads) {
     p.score_out[out + r] = -INFINITY;
@@ -487,47 +616,36 @@ __device__ __forceinline__ void bm_join(const BmParams& p, BmShared& sh, unsigne
   }
 }
 
+// Tiles of 2048 elements (small calls) or of 16 KiB.
+constexpr int kBmSmall = 8;
 template <typename T, int EPT>
 __global__ void __launch_bounds__(kBmThreads, 3) beam_kernel(const __grid_constant__ BmParams p) {
   extern __shared__ __align__(16) uint8_t bm_dyn[];
   __shared__ BmShared sh;
-  unsigned long long* val = reinterpret_cast<unsigned long long*>(bm_dyn);
-  uint32_t* idx = reinterpret_cast<uint32_t*>(val + kBmPool);
+  const BmSpace sp(bm_dyn);
   const int tid = threadIdx.x;
   const long long row = blockIdx.x / p.chunks;
   const int chunk = static_cast<int>(blockIdx.x - row * p.chunks), group = static_cast<int>(row / p.beams);
   griddep_wait();
   griddep_launch();
   const float s = p.score ? __ldcg(p.score + row) : 0.f;
-  if (s > -INFINITY && s < INFINITY && !(p.done && __ldcg(p.done + row))) bm_chunk<T, EPT>(p, sh, val, idx, row, chunk);
+  if (s > -INFINITY && s < INFINITY && !(p.done && __ldcg(p.done + row))) bm_chunk<T, EPT>(p, sh, sp, row, chunk);
   __syncthreads();
   if (tid == 0) {
     sh.last = atom_add_acq_rel_gpu(&p.counters[group], 1) == p.beams * p.chunks - 1;
     if (sh.last) atomicExch(&p.counters[group], 0);
   }
   __syncthreads();
-  if (sh.last) bm_join(p, sh, val, idx, group);
+  if (sh.last) bm_join(p, sh, sp, group);
 }
 
-constexpr int kBmSmem = kBmPool * 12;
 
 template <typename T>
-cudaError_t bm_launch(const BmParams& p, int ept, unsigned grid, cudaStream_t s) {
-  switch (ept) {
-    case 8: return launch_k(beam_kernel<T, 8>, dim3(grid), dim3(kBmThreads), kBmSmem, s, true, p);
-    case 16: return launch_k(beam_kernel<T, 16>, dim3(grid), dim3(kBmThreads), kBmSmem, s, true, p);
-    default: return launch_k(beam_kernel<T, 32>, dim3(grid), dim3(kBmThreads), kBmSmem, s, true, p);
-  }
-}
-template <typename T>
-cudaError_t bm_prepare() {
-  cudaError_t e = cudaFuncSetAttribute(beam_kernel<T, 8>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBmSmem);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(beam_kernel<T, 16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBmSmem);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(beam_kernel<T, 32>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBmSmem);
-  return e;
+cudaError_t bm_launch(const BmParams& p, bool small, unsigned grid, cudaStream_t s) {
+  return launch_k(small ? beam_kernel<T, kBmSmall> : beam_kernel<T, 64 / sizeof(T)>, dim3(grid), dim3(kBmThreads), BmSpace::kBytes, s, true, p);
 }
 
-long long chunks_of(int vocab, int ept) { return (vocab + kBmThreads * ept - 1) / (kBmThreads * ept); }
+long long chunks_of(int vocab, int len) { return (vocab + len - 1) / len; }
 
 }  // namespace
 }  // namespace tss
@@ -550,12 +668,9 @@ extern "C" tss_status tss_beam_create(int max_rows, int vocab, int max_keep, tss
   h->max_keep = max_keep;
   h->dev = dev;
   h->sms = sms;
-  h->lists = max_rows * chunks_of(vocab, 32);
-  if (h->lists < 4LL * sms) h->lists = 4LL * sms;
-  cudaError_t e = bm_prepare<float>();
-  if (e == cudaSuccess) e = bm_prepare<__half>();
-  if (e == cudaSuccess) e = bm_prepare<__nv_bfloat16>();
-  if (e == cudaSuccess) e = cudaMalloc(&h->status, 256);
+  h->lists = max_rows * chunks_of(vocab, 16 * kBmThreads);  // (the most that a call of fp32 logits has)
+  if (h->lists < 2LL * sms) h->lists = 2LL * sms;
+  cudaError_t e = cudaMalloc(&h->status, 256);
   if (e == cudaSuccess) e = zero_now(h->status, 256);
   if (e == cudaSuccess) e = cudaMalloc(&h->counters, sizeof(int) * static_cast<size_t>(max_rows));
   if (e == cudaSuccess) e = zero_now(h->counters, sizeof(int) * static_cast<size_t>(max_rows));
@@ -627,18 +742,23 @@ extern "C" tss_status tss_beam_select(tss_beam* h, const tss_beam_args* a, void*
   p.part = h->part;
   p.sums = h->sums;
   p.status = h->status;
-  // Chunks of 2048, 4096 or 8192 elements: the smallest that give no more CTAs than two an SM.
-  int ept = 8;
-  while (ept < 32 && rows * chunks_of(h->vocab, ept) > 2LL * h->sms) ept *= 2;
-  p.chunks = static_cast<int>(chunks_of(h->vocab, ept));
-  p.len = (h->vocab + p.chunks - 1) / p.chunks;
-  p.len = (p.len + 7) / 8 * 8;
+  // Chunks of a tile of 2048 elements where that makes two CTAs an SM at most; else of 8 tiles of 16 KiB, or less, down to one,
+  // where that leaves fewer CTAs than four times what the GPU holds.
+  int len = kBmSmall * kBmThreads;
+  const bool small = rows * chunks_of(h->vocab, len) <= 2LL * h->sms;
+  if (!small) {
+    const int tile = 64 / dtype_bytes(a->dtype) * kBmThreads;
+    len = kBmTiles * tile;
+    while (len > tile && rows * chunks_of(h->vocab, len) < 12LL * h->sms) len /= 2;
+  }
+  p.chunks = static_cast<int>(chunks_of(h->vocab, len));
+  p.len = ((h->vocab + p.chunks - 1) / p.chunks + 7) / 8 * 8;
   const long long grid = rows * p.chunks;
   if (grid > 0x7fffffffLL) return refuse(TSS_ERR_INVALID_ARG, "too many rows for one launch");
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const unsigned g = static_cast<unsigned>(grid);
-  const cudaError_t e = a->dtype == TSS_DTYPE_BF16  ? bm_launch<__nv_bfloat16>(p, ept, g, s)
-                        : a->dtype == TSS_DTYPE_F16 ? bm_launch<__half>(p, ept, g, s)
-                                                    : bm_launch<float>(p, ept, g, s);
+  const cudaError_t e = a->dtype == TSS_DTYPE_BF16  ? bm_launch<__nv_bfloat16>(p, small, g, s)
+                        : a->dtype == TSS_DTYPE_F16 ? bm_launch<__half>(p, small, g, s)
+                                                    : bm_launch<float>(p, small, g, s);
   return e == cudaSuccess ? TSS_OK : refuse_cuda(e, "launch");
 }
