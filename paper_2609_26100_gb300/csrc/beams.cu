@@ -358,15 +358,19 @@ __device__ __forceinline__ void bm_chunk(const BmParams& p, BmShared& sh, const 
   // ---- groups that reach the bound are looked at again, the others' sums added up ----
   const BmBase base(m);
   long long sum = 0;
+  float others = 0.f;
   for (int t = 0; t < tiles; ++t) {
     const int id = t * kBmThreads + tid;
     const float g = sp.most[id];
     if (!(g > -kBmMost)) continue;
     if (g >= least)
       sp.group[atomicAdd(&sh.groups, 1)] = static_cast<uint16_t>(id);
+    else if (fabsf(g) < 1e6f && fabsf(m) < 1e6f)
+      others = fmaf(sp.sum[id], bm_ex2(rintf(g * kLog2eHi) - base.hi), others);  // (a power of two)
     else
       sum += bm_down(bm_fixed(sp.sum[id]), BmBase(g), base);
   }
+  sum += bm_fixed(others);
   __syncthreads();
   const int groups = sh.groups;
   // An element a lane: its term, and itself into the pool if it reaches the bound; where the pool could overflow it is cut to the
@@ -442,19 +446,19 @@ __device__ __forceinline__ void bm_join(const BmParams& p, BmShared& sh, const B
   const longlong2* sums = p.sums + row0 * p.chunks;
   // The thread's first list's first entries, those that the bound comes from and the first chunks' sums are on their way together
   // (lists go round the warps; what rows without logits that count have left there is not used).
-  constexpr int kStep = 4, kHead = 2 * kStep, kRows = kBmBeams / kBmWarps;
+  constexpr int kStep = 4, kHead = 2 * kStep;
   const int deep = min(p.keep, (2 * p.keep + lists - 1) / lists), mine = warp + lane * kBmWarps;
   const auto entry = [&](int l, int r) { return l < lists && r < p.keep ? __ldcg(part + l * p.keep + r) : make_uint2(order_of(-INFINITY), 0u); };
   uint2 head[kHead];
 #pragma unroll
   for (int r = 0; r < kHead; ++r) head[r] = entry(mine, r);
   const uint32_t deep_x = entry(mine, deep - 1).x, last_x = entry(mine, p.keep - 1).x;
-  longlong2 first[kRows];
-#pragma unroll
-  for (int i = 0; i < kRows; ++i) {
-    const int b = warp + i * kBmWarps;
-    if (b < p.beams && lane < p.chunks) first[i] = __ldcg(sums + b * p.chunks + lane);
-  }
+  // (a row's chunks lie in `wide` lanes, a power of two)
+  int wide = 1;
+  while (wide < 32 && wide < p.chunks) wide *= 2;
+  const int c0 = lane & (wide - 1), b0 = tid / wide, b_step = kBmThreads / wide;
+  const auto sum_of = [&](int b, int c) { return b < p.beams && c < p.chunks ? __ldcg(sums + b * p.chunks + c) : make_longlong2(0, __float_as_uint(-INFINITY)); };
+  longlong2 first = sum_of(b0, c0);
   if (tid < p.beams) {
     const float s = p.score ? __ldcg(p.score + row0 + tid) : 0.f;
     const int done = p.done ? __ldcg(p.done + row0 + tid) : 0;
@@ -464,33 +468,32 @@ __device__ __forceinline__ void bm_join(const BmParams& p, BmShared& sh, const B
   }
   if (tid == 0) sh.n = sh.tiny = 0;
   __syncthreads();
-  // ---- rows: a warp takes every eighth, its lanes the chunks ----
-#pragma unroll
-  for (int i = 0; i < kRows; ++i) {
-    const int b = warp + i * kBmWarps;
-    if (b >= p.beams) break;
+  // ---- rows' sums ----
+  for (int b_first = 0; b_first < p.beams; b_first += b_step) {
+    const int b = b_first + b0;
+    if (b_first > 0) first = sum_of(b, c0);
+    const bool on = b < p.beams && sh.alive[b] == 1;
     float m = -INFINITY;
     bool bad = false;
     long long sum = 0;
-    if (sh.alive[b] == 1) {
-      for (int c = lane; c < p.chunks; c += 32) {
-        const longlong2 x = c < 32 ? first[i] : __ldcg(sums + b * p.chunks + c);
+    if (on)
+      for (int c = c0; c < p.chunks; c += wide) {
+        const longlong2 x = c == c0 ? first : sum_of(b, c);
         m = fmaxf(m, __uint_as_float(static_cast<uint32_t>(x.y)));
         bad |= x.y >> 32 != 0;
       }
+    for (int o = wide / 2; o > 0; o /= 2) {
+      m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+      bad |= __shfl_xor_sync(0xffffffffu, static_cast<int>(bad), o);
     }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    bad = __any_sync(0xffffffffu, bad);
     const BmBase top(m);
     if (m > -kBmMost)
-      for (int c = lane; c < p.chunks; c += 32) {
-        const longlong2 x = c < 32 ? first[i] : __ldcg(sums + b * p.chunks + c);
+      for (int c = c0; c < p.chunks; c += wide) {
+        const longlong2 x = c == c0 ? first : sum_of(b, c);
         if (x.x != 0) sum += bm_down(x.x, BmBase(__uint_as_float(static_cast<uint32_t>(x.y))), top);
       }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if (lane == 0) {
+    for (int o = wide / 2; o > 0; o /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (c0 == 0 && b < p.beams) {
       if (bad) sum = 0;
       sh.row_sum[b] = sum;
       sh.row_base[b] = make_float2(m, top.f);
@@ -538,8 +541,6 @@ __device__ __forceinline__ void bm_join(const BmParams& p, BmShared& sh, const B
   for (int i = 0; i < kBmWarps; ++i) tf = fmaxf(tf, sh.most[i]);
   const unsigned long long nothing = order_of(none);
   unsigned long long tv = max(order_of(static_cast<double>(tf)), nothing + 1);
-  const auto value_of = [&](int list, uint32_t x) { return order_of(sh.base[list / p.chunks] + static_cast<double>(float_of(x))); };
-  const auto offers = [&](int list) { return list < lists && sh.base[list / p.chunks] > none; };
   // Equal values: the lower row, then the lower token, which is the order of places; but where logits are so small that 64 bits of
   // a value may not show their difference, the larger one of a row first.
   const auto by_place = [](unsigned long long a, uint32_t ax, unsigned long long b, uint32_t bx) { return a > b || (a == b && ax < bx); };
@@ -557,48 +558,62 @@ __device__ __forceinline__ void bm_join(const BmParams& p, BmShared& sh, const B
   // ---- the lists' entries that reach it, a few of a list at a time; where the pool could overflow it is cut to the best and the
   // bound raised ----
   int n = 0;
-  const auto take = [&](int l, int r, uint2 e, bool* more) {
-    const unsigned long long v = value_of(l, e.x);
+  const auto take = [&](int l, int row, double base, int r, uint2 e, bool* more) {
+    const unsigned long long v = order_of(base + static_cast<double>(float_of(e.x)));
     *more = *more && v >= tv;
     if (*more) {
       const int to = atomicAdd(&sh.n, 1);
       sp.val[to] = v;
-      sp.idx[to] = static_cast<uint32_t>(l) * p.keep + r + l / p.chunks;
+      sp.idx[to] = static_cast<uint32_t>(l) * p.keep + r + row;
       const float y = fabsf(float_of(e.x));
       if (y < 1e-6f * fabsf(static_cast<float>(double_of(v)))) sh.tiny = 1;
     }
   };
-  for (int l0 = 0; l0 < lists; l0 += kBmThreads) {
-    const int l = l0 + mine;
-    bool more = offers(l);
-    for (int r0 = 0;; r0 += kStep) {
-      const bool any = __syncthreads_or(more && r0 < p.keep);
-      n = sh.n;
-      __syncthreads();
-      if (n > kBmPool - kStep * kBmThreads) {
-        unsigned long long kept_v = 0;
-        uint32_t kept_x = 0;
-        int at = -1;
-        sorted(n, [&](int rank, unsigned long long v, uint32_t x) {
-          if (rank < p.keep) kept_v = v, kept_x = x, at = rank;
-        });
-        if (at >= 0) {
-          sp.val[at] = kept_v;
-          sp.idx[at] = kept_x;
-        }
-        n = min(n, p.keep);
-        if (tid == 0) sh.n = n;
-        __syncthreads();
-        if (n == p.keep) tv = max(tv, sp.val[n - 1]);
-        __syncthreads();
+  // (the same for all threads; n becomes what the pool has)
+  const auto keep_room = [&](bool mine_more) {
+    const bool any = __syncthreads_or(mine_more);
+    n = sh.n;
+    __syncthreads();
+    if (n > kBmPool / 2) {
+      unsigned long long kept_v = 0;
+      uint32_t kept_x = 0;
+      int at = -1;
+      sorted(n, [&](int rank, unsigned long long v, uint32_t x) {
+        if (rank < p.keep) kept_v = v, kept_x = x, at = rank;
+      });
+      if (at >= 0) {
+        sp.val[at] = kept_v;
+        sp.idx[at] = kept_x;
       }
-      if (!any) break;
-      if (more && r0 < p.keep) {
-        uint2 e[kStep];
+      n = min(n, p.keep);
+      if (tid == 0) sh.n = n;
+      __syncthreads();
+      if (n == p.keep) tv = max(tv, sp.val[n - 1]);
+      __syncthreads();
+    }
+    return any;
+  };
+  static_assert(kStep * kBmThreads <= kBmPool / 2 && kBmWarps * kBmKeep <= kBmPool / 2, "room for a turn");
+  for (int l0 = 0; l0 < lists; l0 += kBmThreads) {
+    const int l = l0 + mine, row = l / p.chunks;
+    const double base = l < lists ? sh.base[row] : none;
+    bool more = base > none;
 #pragma unroll
-        for (int r = 0; r < kStep; ++r) e[r] = l0 > 0 || r0 >= kHead ? entry(l, r0 + r) : r0 ? head[kStep + r] : head[r];
+    for (int r0 = 0; r0 < kHead; r0 += kStep) {
+      if (!keep_room(more)) break;
+      if (more) {
 #pragma unroll
-        for (int r = 0; r < kStep; ++r) take(l, r0 + r, e[r], &more);
+        for (int r = r0; r < r0 + kStep; ++r) take(l, row, base, r, l0 > 0 ? entry(l, r) : head[r], &more);
+      }
+    }
+    // what is left of a list is a warp's
+    for (uint32_t rest = __ballot_sync(0xffffffffu, more && p.keep > kHead); keep_room(rest != 0); rest &= rest - 1) {
+      if (rest == 0) continue;
+      const int from = __shfl_sync(0xffffffffu, l, __ffs(rest) - 1), from_row = from / p.chunks;
+      const double from_base = sh.base[from_row];
+      for (int r = kHead + lane; r < p.keep; r += 32) {
+        bool here = true;
+        take(from, from_row, from_base, r, entry(from, r), &here);
       }
     }
   }
@@ -617,9 +632,9 @@ __device__ __forceinline__ void bm_join(const BmParams& p, BmShared& sh, const B
 }
 
 // Tiles of 2048 elements (small calls) or of 16 KiB.
-constexpr int kBmSmall = 8;
+constexpr int kBmSmall = 8, kBmCtas = 4;
 template <typename T, int EPT>
-__global__ void __launch_bounds__(kBmThreads, 3) beam_kernel(const __grid_constant__ BmParams p) {
+__global__ void __launch_bounds__(kBmThreads, kBmCtas) beam_kernel(const __grid_constant__ BmParams p) {
   extern __shared__ __align__(16) uint8_t bm_dyn[];
   __shared__ BmShared sh;
   const BmSpace sp(bm_dyn);
@@ -742,14 +757,22 @@ extern "C" tss_status tss_beam_select(tss_beam* h, const tss_beam_args* a, void*
   p.part = h->part;
   p.sums = h->sums;
   p.status = h->status;
-  // Chunks of a tile of 2048 elements where that makes two CTAs an SM at most; else of 8 tiles of 16 KiB, or less, down to one,
-  // where that leaves fewer CTAs than four times what the GPU holds.
+  // Chunks of a tile of 2048 elements where that makes two CTAs an SM at most.  Else of 1 to 8 tiles of 16 KiB: a CTA takes about
+  // 1.2 us a tile, 3 us more and as many again for 32 kept, and an SM holds kBmCtas.
   int len = kBmSmall * kBmThreads;
   const bool small = rows * chunks_of(h->vocab, len) <= 2LL * h->sms;
   if (!small) {
     const int tile = 64 / dtype_bytes(a->dtype) * kBmThreads;
-    len = kBmTiles * tile;
-    while (len > tile && rows * chunks_of(h->vocab, len) < 12LL * h->sms) len /= 2;
+    const double start = 3. + a->n_keep / 10.;
+    double least = 1e30;
+    for (int t = 1; t <= kBmTiles; ++t) {
+      const long long ctas = rows * chunks_of(h->vocab, t * tile), waves = (ctas + kBmCtas * h->sms - 1) / (kBmCtas * h->sms);
+      const double us = waves * (start + 1.2 * t);
+      if (us < least) {
+        least = us;
+        len = t * tile;
+      }
+    }
   }
   p.chunks = static_cast<int>(chunks_of(h->vocab, len));
   p.len = ((h->vocab + p.chunks - 1) / p.chunks + 7) / 8 * 8;
