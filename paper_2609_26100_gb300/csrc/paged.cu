@@ -241,6 +241,10 @@ extern "C" tss_status tss_paged_create_shared(int n_q_heads, int n_kv_heads, int
   h->share_rows = shared_rows;
   if (e == cudaSuccess && share) e = cudaMalloc(&h->share_o, share * head_dim * sizeof(float));
   if (e == cudaSuccess && share) e = cudaMalloc(&h->share_ml, share * sizeof(float2));
+  if (e == cudaSuccess && share) e = cudaMalloc(&h->own_o, rows * head_dim * sizeof(float));
+  if (e == cudaSuccess && share) e = cudaMalloc(&h->own_ml, rows * sizeof(float2));
+  if (e == cudaSuccess && share) e = cudaMalloc(&h->own_counters, pa_counters(sms) * sizeof(int));
+  if (e == cudaSuccess && share) e = zero_now(h->own_counters, pa_counters(sms) * sizeof(int));
   if (e != cudaSuccess) {
     tss_paged_destroy(h);
     const tss_status r = refuse_cuda(e, "workspace");
@@ -258,6 +262,9 @@ extern "C" void tss_paged_destroy(tss_paged* h) {
   cudaFree(h->counters);
   cudaFree(h->share_o);
   cudaFree(h->share_ml);
+  cudaFree(h->own_o);
+  cudaFree(h->own_ml);
+  cudaFree(h->own_counters);
   delete h;
 }
 

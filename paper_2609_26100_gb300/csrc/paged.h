@@ -14,6 +14,9 @@ struct tss_paged {
   int share_rows;   // rows that a shared attention may have
   float* share_o;   // device [share_rows][hq][d]: results over the shared keys, unnormalised
   float2* share_ml; // device [share_rows][hq]: their references and sums
+  float* own_o;     // part_o, part_ml and counters of the pass over own keys, which overlaps the one over shared keys
+  float2* own_ml;
+  int* own_counters;
 };
 
 namespace tss {

@@ -59,13 +59,13 @@ __device__ __forceinline__ void mma_first(float* d, const uint32_t* a, const uin
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]), "f"(0.f));
 }
 
-// A ring stage holds a page's block (or half of each of its parts).
-template <int D, int NT>
+// A ring stage holds a page's block (or half of each of its parts).  W: warps of a CTA, 4, or 1 for many short items.
+template <int D, int NT, int W>
 struct PaShape {
   static constexpr int kRows = 8 * NT;
-  static constexpr int kWarps = 4;
-  static constexpr int kCtas = NT == 1 ? 3 : 2;  // resident on an SM
-  static constexpr int kStages = NT == 1 ? 2 : 3;
+  static constexpr int kWarps = W;
+  static constexpr int kCtas = W == 1 ? (NT == 1 ? 11 : 8) : NT == 1 ? 3 : 2;  // resident on an SM
+  static constexpr int kStages = NT == 1 || W == 1 ? 2 : 3;
   static constexpr size_t kSmem = kWarps * kStages * PgBlock<D>::kBytes;
 };
 
@@ -82,11 +82,11 @@ __device__ __forceinline__ bool sees(const PgAttnArgs& a, const PaReq& r, int i,
 }
 
 // TWO: weights of two fp16 parts.  SH: a pass of the attention of sequences that share keys.
-template <int D, int NT, bool TWO, bool SH>
-__global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::kCtas)
+template <int D, int NT, bool TWO, bool SH, int WARPS>
+__global__ void __launch_bounds__(WARPS * 32, PaShape<D, NT, WARPS>::kCtas)
     paged_attn_kernel(const __grid_constant__ typename PaParamsOf<SH>::type p) {
   using B = PgBlock<D>;
-  using S = PaShape<D, NT>;
+  using S = PaShape<D, NT, WARPS>;
   constexpr int G = B::kGroups, W = S::kWarps, ST = S::kStages, R = S::kRows, DB = D / 32;
   extern __shared__ __align__(128) uint8_t pa_dyn[];
   __shared__ uint64_t bars[W][ST];
@@ -98,7 +98,7 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
   uint8_t* ring = pa_dyn + warp * (ST * B::kBytes);
   const PgAttnArgs& a = p.a;
   const int gq = a.hq / a.hk, halves = p.halves, unit = 32 * halves;  // tokens of a unit
-  if (tid < p.n_req) s_off[tid] = p.r[tid].off;
+  for (int i = tid; i < p.n_req; i += W * 32) s_off[i] = p.r[i].off;
   if (lane == 0)
     for (int i = 0; i < ST; ++i) mbar_init(&bars[warp][i], 1);
   if (tid == 0) abort_s = 0;
@@ -141,7 +141,11 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
   const long long place = place_of(0, &part);
   // Nothing before this reads or writes what another kernel may; tables, masks and positions are not read through the
   // read-only path, since the kernel that writes them may still run while this one begins.
-  griddep_wait();
+  if constexpr (SH) {
+    if (!p.early) griddep_wait();  // (what this reads before that was complete when the pass before it began)
+  } else {
+    griddep_wait();
+  }
   griddep_launch();
   int ids = block_at(place, part), ids_next = -2;
   int issued = 0, issue_at = 0;  // units asked for, the stage of the next
@@ -189,7 +193,8 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
     const PaReq& r = p.r[b];
     const int v = u - r.off, item = v / r.units, x0 = v - item * r.units;
     const int seg_end = min(u1, u - x0 + r.units), x1 = x0 + seg_end - u;
-    const int h = item % a.hk, row0 = item / a.hk * R, rows = min(R, r.n * gq - row0);
+    int rows;
+    const int h = item % a.hk, row0 = tile_rows(p, r, item / a.hk, R, gq, &rows);
     // Q: thread (g, t) holds row g's dims 64 gi + 16 t .. + 15 as the operand of 4 k-steps a group: pairs
     // (0, 4), (1, 5) and (2, 6), (3, 7) of each 8 dims, odd ones / 16 (their codes stand four bits up)
     uint32_t qf[NT][G][2][4];
@@ -564,6 +569,7 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
       fence_async_smem();  // (the next segment's first copy goes to this stage: stores before the async proxy's)
     }
     __syncthreads();
+    wait_for_shared(p);
     const bool whole = x0 == 0 && x1 == r.units;
     int c0 = first_cta, c1 = first_cta + splits - 1;  // CTAs that share the item
     if (!whole && !p.aligned) {
@@ -617,7 +623,7 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
       __syncthreads();
       if (s_last) {
         // Few rows: several warps take a row, each some of its partials.
-        const int per_row = rows == 1 ? W : rows == 2 ? W / 2 : 1, slice = warp % per_row;
+        const int per_row = W == 1 ? 1 : rows == 1 ? W : rows == 2 ? W / 2 : 1, slice = warp % per_row;
         for (int row = warp / per_row; row < rows; row += W / per_row) {
           float M, L;
           float4 sum;
@@ -656,6 +662,7 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
     }
     u = seg_end;
   }
+  wait_for_shared(p);  // (a CTA without work too: the kernel ends no earlier than the one before it)
   // after a wait gave up: the copies in flight land before the CTA ends
   if (!ok && !withheld)
     for (int k = max(0, issued - ST); k < issued; ++k) mbar_drain(&bars[warp][k % ST], (k / ST) & 1);
@@ -663,74 +670,122 @@ __global__ void __launch_bounds__(PaShape<D, NT>::kWarps * 32, PaShape<D, NT>::k
 
 template <int D, int NT, bool TWO>
 cudaError_t pa_launch(PaShared& p, bool shared, int sms, cudaStream_t s) {
-  using S = PaShape<D, NT>;
+  using S = PaShape<D, NT, 4>;
   // A run of a unit for each warp at least.  Leads of 0 / 3 / 6 / 10 / 16 pages, us: six requests of 60 to 30000
   // tokens 180 / 100 / 66 / 53 / 50, eight of 512 to 4096 45 / 40 / 38 / 37 / 38, equal ones alike at any.
   const int grid = pa_cut(p, sms * S::kCtas, S::kWarps, 8, 10 * (3 - p.halves));
   const dim3 g(grid), b(S::kWarps * 32);
-  return shared ? launch_k(paged_attn_kernel<D, NT, TWO, true>, g, b, S::kSmem, s, true, p)
-                : launch_k(paged_attn_kernel<D, NT, TWO, false>, g, b, S::kSmem, s, true, static_cast<PaParams&>(p));
+  return shared ? launch_k(paged_attn_kernel<D, NT, TWO, true, 4>, g, b, S::kSmem, s, true, p)
+                : launch_k(paged_attn_kernel<D, NT, TWO, false, 4>, g, b, S::kSmem, s, true, static_cast<PaParams&>(p));
+}
+// A warp for every item.
+template <int D, int NT, bool TWO>
+cudaError_t pa_launch_items(PaShared& p, cudaStream_t s) {
+  using S = PaShape<D, NT, 1>;
+  return launch_k(paged_attn_kernel<D, NT, TWO, true, 1>, dim3(pa_each(p)), dim3(32), S::kSmem, s, true, p);
 }
 template <int D, int NT, bool TWO>
 cudaError_t pa_prepare() {
-  const int bytes = static_cast<int>(PaShape<D, NT>::kSmem);
-  const cudaError_t e = cudaFuncSetAttribute(paged_attn_kernel<D, NT, TWO, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-  return e == cudaSuccess ? cudaFuncSetAttribute(paged_attn_kernel<D, NT, TWO, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) : e;
+  const auto allow = [](auto kernel, size_t bytes) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)); };
+  cudaError_t e = allow(paged_attn_kernel<D, NT, TWO, false, 4>, PaShape<D, NT, 4>::kSmem);
+  if (e == cudaSuccess) e = allow(paged_attn_kernel<D, NT, TWO, true, 4>, PaShape<D, NT, 4>::kSmem);
+  if (e == cudaSuccess) e = allow(paged_attn_kernel<D, NT, TWO, true, 1>, PaShape<D, NT, 1>::kSmem);
+  return e;
 }
 
-// The launches of a pass: blocks of more than kPaTcRows query rows of a KV head go to the tcgen05 kernel (head_dim 128), the others
+// What a pass writes its partial results to, and whether it waits for the pass before it only where it joins.
+struct PaWork {
+  float* part_o;
+  float2* part_ml;
+  int* counters;
+  int early;
+};
+
+// The launches of a pass: blocks of more than `limit` query rows of a KV head go to the tcgen05 kernel (head_dim 128), the others
 // to the one above.
-cudaError_t pa_pass(tss_paged* h, const PgAttnArgs& a, const PaTask* tasks, int n_tasks, const int2* mem, int withhold, bool shared, cudaStream_t s,
-                    bool* too_large) {
-  const int gq = h->hq / h->hk;
-  int most = 0, wide = 0;
+cudaError_t pa_pass(tss_paged* h, const PgAttnArgs& a, const PaTask* tasks, int n_tasks, const int2* mem, int limit, const PaWork& work, int withhold,
+                    bool shared, cudaStream_t s, bool* too_large) {
+  PaTask few[kPgMaxReq], many[kPgMaxReq];
+  int n_few = 0, n_many = 0, most = 0;
   for (int i = 0; i < n_tasks; ++i) {
-    const int rows = tasks[i].q.n * gq;
-    if (h->d == 128 && rows > kPaTcRows)
-      ++wide;
-    else
-      most = rows > most ? rows : most;
+    PaTask t = tasks[i];
+    if (t.rows == 0) continue;
+    if (h->d == 128 && t.rows > limit) {
+      // (in a shared pass what 128 rows leave goes with the blocks of few rows, unless it would be one of many itself)
+      const int rest = t.rows % kPaTcTile;
+      if (shared && rest > 0 && rest <= limit) {
+        PaTask tail = t;
+        tail.skip += t.rows - rest;
+        tail.rows = rest;
+        t.rows -= rest;
+        few[n_few++] = tail;
+        most = rest > most ? rest : most;
+      }
+      many[n_many++] = t;
+    } else {
+      few[n_few++] = t;
+      most = t.rows > most ? t.rows : most;
+    }
   }
   PaShared p, narrow;
   const auto begin = [&](PaShared& x) {
     x.a = a;
-    x.part_o = h->part_o;
-    x.part_ml = h->part_ml;
-    x.counters = h->counters;
+    x.part_o = work.part_o;
+    x.part_ml = work.part_ml;
+    x.counters = work.counters;
+    x.early = work.early;
     x.withhold = withhold;
     if (mem)
       for (int i = 0; i < kPgMaxReq; ++i) x.mem[i] = mem[i];
   };
-  if (wide) {
+  if (n_many) {
     begin(p);
-    if (!pa_plan(p, tasks, n_tasks, [&](const PgReq& q) { return q.n * gq > kPaTcRows; }, 128, 2)) {
+    if (!pa_plan(p, many, n_many, kPaTcTile, 2)) {
       *too_large = true;
       return cudaSuccess;
     }
   }
-  if (most) {
+  if (n_few) {
     begin(narrow);
     const int R = most <= 8 ? 8 : 16;
-    const auto take = [&](const PgReq& q) { return h->d != 128 || q.n * gq <= kPaTcRows; };
     // Units of a page; of half a page where that leaves the warps less than three pages each (a warp takes
     // about 2 us for a page, so a short launch is as long as its longest warp).
-    bool fits = pa_plan(narrow, tasks, n_tasks, take, R, 2);
-    if (fits && narrow.total < 3LL * h->sms * (R == 8 ? 12 : 8)) fits = pa_plan(narrow, tasks, n_tasks, take, R, 1);
+    bool fits = pa_plan(narrow, few, n_few, R, 2);
+    // Own keys beside a shared prefix are few as a rule and their items many: a warp for each, where the SMs' warps take that
+    // sooner than the four of a CTA, which share an item and join (about 4 us an item, and 2 a page of a warp).
+    bool each = false;
+    if (fits && shared && a.own && narrow.n_req) {
+      const auto items = [&](int i) { return ((i + 1 < narrow.n_req ? narrow.r[i + 1].off : narrow.total) - narrow.r[i].off) / narrow.r[i].units; };
+      int n = 0, longest = 0;
+      for (int i = 0; i < narrow.n_req; ++i) {
+        n += items(i);
+        longest = narrow.r[i].units > longest ? narrow.r[i].units : longest;
+      }
+      const double one = h->sms * (R == 8 ? 11. : 8.), four = h->sms * (R == 8 ? 3. : 2.);
+      const double mean = static_cast<double>(narrow.total) / n;
+      each = (n > one ? n / one * (4 + 2 * mean) : 4 + 2 * longest) < (n > four ? n / four : 1) * (5 + mean / 2);
+    }
+    if (fits && !each && narrow.total < 3LL * h->sms * (R == 8 ? 12 : 8)) fits = pa_plan(narrow, few, n_few, R, 1);
     if (!fits) {
       *too_large = true;
       return cudaSuccess;
     }
     const auto run = [&](auto dim) {
       constexpr int D = decltype(dim)::value;
+      if (each) {
+        if (R == 8) return pa_launch_items<D, 1, true>(narrow, s);
+        return a.is_half ? pa_launch_items<D, 2, true>(narrow, s) : pa_launch_items<D, 2, false>(narrow, s);
+      }
       if (R == 8) return pa_launch<D, 1, true>(narrow, shared, h->sms, s);
       return a.is_half ? pa_launch<D, 2, true>(narrow, shared, h->sms, s) : pa_launch<D, 2, false>(narrow, shared, h->sms, s);
     };
     if (narrow.n_req) {
       const cudaError_t e = h->d == 64 ? run(std::integral_constant<int, 64>{}) : run(std::integral_constant<int, 128>{});
       if (e != cudaSuccess) return e;
+      p.early = 0;  // (behind the launch above now, whose workspace it shares)
     }
   }
-  return wide && p.n_req ? launch_paged_attention_tc(p, shared, h->sms, s) : cudaSuccess;
+  return n_many && p.n_req ? launch_paged_attention_tc(p, shared, h->sms, s) : cudaSuccess;
 }
 
 }  // namespace
@@ -757,12 +812,13 @@ cudaError_t launch_paged_attention(tss_paged* h, const PgAttnArgs& a, const PgBa
   PaTask tasks[kPgMaxReq];
   for (int i = 0; i < batch.n_req; ++i) {
     const PgReq& q = batch.r[i];
-    tasks[i] = PaTask{q, 0, q.first + q.n, q.first, 0, 0, 0};
+    tasks[i] = PaTask{q, 0, q.first + q.n, q.first, 0, q.n * (h->hq / h->hk), 0, 0, 0};
   }
-  return pa_pass(h, a, tasks, batch.n_req, nullptr, withhold, false, s, too_large);
+  return pa_pass(h, a, tasks, batch.n_req, nullptr, kPaTcRows, PaWork{h->part_o, h->part_ml, h->counters, 0}, withhold, false, s, too_large);
 }
 
-// A pass over the groups' shared keys, for all rows of a group at once, then one over every request's own.
+// A pass over the groups' shared keys, for all rows of a group at once, then one over every request's own, which begins while
+// the first one ends (it has partial results and counters of its own) and waits for it where it joins.
 cudaError_t launch_paged_attention_shared(tss_paged* h, const PgAttnArgs& args, const PgBatch& batch, const PgGroups& groups, cudaStream_t s,
                                           bool* too_large) {
   *too_large = false;
@@ -772,11 +828,12 @@ cudaError_t launch_paged_attention_shared(tss_paged* h, const PgAttnArgs& args, 
   PaTask common[kPgMaxReq], mine[kPgMaxReq];
   int2 mem[kPgMaxReq];
   int n_common = 0, at = 0, n_mem = 0;
+  const int gq = h->hq / h->hk;
   for (int g = 0; g < groups.n; ++g) {
-    PaTask t{PgReq{0, groups.shared[g], 0, 0}, 0, groups.shared[g], 0, 0, n_mem, 0};
+    PaTask t{PgReq{0, groups.shared[g], 0, 0}, 0, groups.shared[g], 0, 0, 0, 0, n_mem, 0};
     for (int i = at; i < at + groups.reqs[g]; ++i) {
       const PgReq& q = batch.r[i];
-      mine[i] = PaTask{q, 0, q.first + q.n, q.first, 0, 0, 0};
+      mine[i] = PaTask{q, 0, q.first + q.n, q.first, 0, q.n * gq, 0, 0, 0};
       if (q.n == 0) continue;
       if (t.members == 0) {
         t.q.seq = q.seq;
@@ -795,6 +852,7 @@ cudaError_t launch_paged_attention_shared(tss_paged* h, const PgAttnArgs& args, 
         mine[i].k0 = groups.shared[g];
         mine[i].joins = r.units > 0;
       }
+      t.rows = t.q.n * gq;
       if (r.units > 0) common[n_common++] = t;
     } else {
       n_mem -= t.members;
@@ -804,10 +862,12 @@ cudaError_t launch_paged_attention_shared(tss_paged* h, const PgAttnArgs& args, 
   cudaError_t e = cudaSuccess;
   if (n_common) {
     a.own = 0;
-    e = pa_pass(h, a, common, n_common, mem, withhold, true, s, too_large);
+    e = pa_pass(h, a, common, n_common, mem, kPaTcShared, PaWork{h->part_o, h->part_ml, h->counters, 0}, withhold, true, s, too_large);
   }
+  if (e != cudaSuccess || *too_large) return e;
   a.own = 1;
-  return e == cudaSuccess && !*too_large ? pa_pass(h, a, mine, batch.n_req, mem, withhold && !n_common, true, s, too_large) : e;
+  return pa_pass(h, a, mine, batch.n_req, mem, kPaTcShared, PaWork{h->own_o, h->own_ml, h->own_counters, n_common > 0}, withhold && !n_common, true, s,
+                 too_large);
 }
 
 }  // namespace tss

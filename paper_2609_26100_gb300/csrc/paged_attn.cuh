@@ -29,9 +29,11 @@ struct PaParams {
 // A pass of the attention over shared keys.  The pass over the shared keys has a group where the others have a request: its rows
 // are those of its requests, `first` and the keys in all are the shared tokens.
 struct PaShared : PaParams {
+  int skip[kPgMaxReq], rows[kPgMaxReq];   // query rows [skip, skip + rows) of the request are the launch's
   int joins[kPgMaxReq];                   // own keys: the request's rows have results over shared ones
   int member[kPgMaxReq], members[kPgMaxReq];  // shared keys: the group's requests, in mem
   int2 mem[kPgMaxReq];                    // first row, first token
+  int early;                              // launched behind the pass over the shared keys, whose end only the joining waits for
 };
 template <bool SH>
 struct PaParamsOf { using type = PaParams; };
@@ -39,6 +41,22 @@ template <>
 struct PaParamsOf<true> { using type = PaShared; };
 // Index of a request among the parameters' (its arrays beside r).
 __device__ __forceinline__ int index_of(const PaParams& p, const PaReq& r) { return static_cast<int>(&r - p.r); }
+
+// First query row of row tile `tile` of a request, and how many it has.
+__device__ __forceinline__ int tile_rows(const PaParams&, const PaReq& r, int tile, int R, int gq, int* rows) {
+  *rows = min(R, r.n * gq - tile * R);
+  return tile * R;
+}
+__device__ __forceinline__ int tile_rows(const PaShared& p, const PaReq& r, int tile, int R, int, int* rows) {
+  const int b = index_of(p, r);
+  *rows = min(R, p.rows[b] - tile * R);
+  return p.skip[b] + tile * R;
+}
+// Before results over shared keys are read.
+__device__ __forceinline__ void wait_for_shared(const PaParams&) {}
+__device__ __forceinline__ void wait_for_shared(const PaShared& p) {
+  if (p.early) griddep_wait();
+}
 
 // Position of row ti of a request (or of a group, whose rows stand at their requests' tokens).
 __device__ __forceinline__ int row_position(const PaParams& p, const PaReq& r, int ti) {
@@ -63,7 +81,8 @@ __device__ __forceinline__ float ex2(float x) {
 // head above which a request goes there.  A page costs it the same for any number of rows, the warp-level kernel in
 // proportion to its 16-row tiles; us, warp-level / tcgen05, four requests of 4600 tokens and 32 heads: 24 rows 66 / 103,
 // 48 rows 97 / 110, 56 rows 119 / 111, 128 rows 225 / 123; 8 heads: 32 rows 28 / 40, 48 rows 33 / 42, 64 rows 41 / 42.
-constexpr int kPaTcRows = 48;
+constexpr int kPaTcRows = 48, kPaTcTile = 128;
+constexpr int kPaTcShared = 80;
 cudaError_t paged_attn_tc_prepare();
 cudaError_t launch_paged_attention_tc(PaShared& p, bool shared, int sms, cudaStream_t s);
 
@@ -237,6 +256,7 @@ struct PaTask {
   PgReq q;
   int k0, k1;
   int from;                    // the smallest index of its rows in the sequence
+  int skip, rows;              // its query rows of a KV head
   int joins, member, members;  // as in PaShared
 };
 
@@ -256,12 +276,10 @@ inline void pa_units(const PgAttnArgs& a, const PaTask& t, int unit, PaReq* r) {
   r->units = r->sink + end - r->lo;
 }
 
-// The tasks that `take` picks, in row tiles of R query rows and units of `halves` 32-token halves; false where the units pass
-// 2^30.
-template <typename Take>
-inline bool pa_plan(PaShared& p, const PaTask* tasks, int n_tasks, Take take, int R, int halves) {
+// The tasks in row tiles of R query rows and units of `halves` 32-token halves; false where the units pass 2^30.
+inline bool pa_plan(PaShared& p, const PaTask* tasks, int n_tasks, int R, int halves) {
   const PgAttnArgs& a = p.a;
-  const int unit = 32 * halves, gq = a.hq / a.hk;
+  const int unit = 32 * halves;
   long long at = 0;
   int items = 0;
   p.halves = halves;
@@ -269,21 +287,35 @@ inline bool pa_plan(PaShared& p, const PaTask* tasks, int n_tasks, Take take, in
   for (int i = 0; i < n_tasks; ++i) {
     const PaTask& t = tasks[i];
     const PgReq& q = t.q;
-    if (q.n == 0 || !take(q)) continue;
+    if (t.rows == 0) continue;
     PaReq r{q.seq, q.first, q.n, q.row, 0, 0, 0, static_cast<int>(at), items, 0, 1};
     pa_units(a, t, unit, &r);
     if (r.units == 0) continue;
+    p.skip[p.n_req] = t.skip;
+    p.rows[p.n_req] = t.rows;
     p.joins[p.n_req] = t.joins;
     p.member[p.n_req] = t.member;
     p.members[p.n_req] = t.members;
     p.r[p.n_req++] = r;
-    const int mine = a.hk * ((q.n * gq + R - 1) / R);
+    const int mine = a.hk * ((t.rows + R - 1) / R);
     items += mine;
     at += static_cast<long long>(r.units) * mine;
     if (at > 0x1fffffff) return false;
   }
   p.total = static_cast<int>(at);
   return true;
+}
+
+// A CTA for every item; their number.
+inline int pa_each(PaParams& p) {
+  int grid = 0;
+  p.aligned = 1;
+  for (int i = 0; i < p.n_req; ++i) {
+    p.r[i].cta = grid;
+    p.r[i].splits = 1;
+    grid += ((i + 1 < p.n_req ? p.r[i + 1].off : p.total) - p.r[i].off) / p.r[i].units;
+  }
+  return grid;
 }
 
 // Cuts the units into runs for at most `most` CTAs and returns their number: even runs, every item counting `lead`

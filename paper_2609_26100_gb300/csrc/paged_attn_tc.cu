@@ -280,8 +280,12 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
   __syncthreads();
   tc_fence_after();
   // Each role waits for the kernel before this one: before it meets global memory, and before waits that are bounded.
-  const auto ready = [] {
-    griddep_wait();
+  const auto ready = [&] {
+    if constexpr (SH) {
+      if (!p.early) griddep_wait();  // (what it reads before that was complete when the pass before it began)
+    } else {
+      griddep_wait();
+    }
     griddep_launch();
   };
   const uint32_t tm = sh.tmem;
@@ -478,7 +482,8 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
       const int rb = request_of(u0 + t);
       const PaReq& r = p.r[rb];
       const int v = u0 + t - r.off, item = v / r.units, x0 = v - item * r.units, len = min(n - t, r.units - x0);
-      const int h = item % a.hk, row0 = item / a.hk * kPtRows, rows = min(kPtRows, r.n * gq - row0);
+      int rows;
+      const int h = item % a.hk, row0 = tile_rows(p, r, item / a.hk, kPtRows, gq, &rows);
       if (seg == 0) ready();
       // Q: 16 lanes a row, 8 dims each, as chunks in the operand's order; the warp's rows in flight together
       constexpr int kTurns = kPtRows / 2 / kPtSoftWarps;
@@ -791,6 +796,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
         if (lane == 0) mbar_arrive(&sh.p_full[sb]);  // (of a quadrant without rows: the arrival alone)
       }
       // ---- the segment's end: 32 dims a thread ----
+      wait_for_shared(p);
       ok = ok && quiet_wait(&sh.o_full, seg & 1, abort, a.status);
       __syncwarp();
       tc_fence_after();
@@ -915,6 +921,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
       t += len;
     }
   }
+  wait_for_shared(p);  // (the kernel ends no earlier than the one before it)
   __syncwarp();
   tc_fence_before();
   __syncthreads();
