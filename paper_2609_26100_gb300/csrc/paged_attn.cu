@@ -90,7 +90,7 @@ __global__ void __launch_bounds__(WARPS * 32, PaShape<D, NT, WARPS>::kCtas)
   constexpr int G = B::kGroups, W = S::kWarps, ST = S::kStages, R = S::kRows, DB = D / 32;
   extern __shared__ __align__(128) uint8_t pa_dyn[];
   __shared__ uint64_t bars[W][ST];
-  __shared__ int s_off[kPgMaxReq];
+  __shared__ int s_off[kPgMaxReq], s_qp[W][R];  // s_qp: positions of the rows that the warp works on
   __shared__ float2 s_ml[W][R];
   __shared__ int s_has[W], abort_s, s_last;  // s_has: the stage of a warp's part, plus one; 0 without
   __shared__ __align__(16) float s_x[W][D];  // parts of rows that several warps gather from other CTAs' partials
@@ -193,8 +193,7 @@ __global__ void __launch_bounds__(WARPS * 32, PaShape<D, NT, WARPS>::kCtas)
     const PaReq& r = p.r[b];
     const int v = u - r.off, item = v / r.units, x0 = v - item * r.units;
     const int seg_end = min(u1, u - x0 + r.units), x1 = x0 + seg_end - u;
-    int rows;
-    const int h = item % a.hk, row0 = tile_rows(p, r, item / a.hk, R, gq, &rows);
+    const int h = item % a.hk, row0 = item / a.hk * R, rows = min(R, r.n * gq - row0);
     // Q: thread (g, t) holds row g's dims 64 gi + 16 t .. + 15 as the operand of 4 k-steps a group: pairs
     // (0, 4), (1, 5) and (2, 6), (3, 7) of each 8 dims, odd ones / 16 (their codes stand four bits up)
     uint32_t qf[NT][G][2][4];
@@ -262,6 +261,7 @@ __global__ void __launch_bounds__(WARPS * 32, PaShape<D, NT, WARPS>::kCtas)
     if (a.window) {  // the last position among the tile's rows
       if (lane < rows) {
         pmax = row_position(p, r, (row0 + lane) / gq);
+        if constexpr (SH) s_qp[warp][lane] = pmax;
       }
 #pragma unroll
       for (int x2 = 16; x2 > 0; x2 >>= 1) pmax = max(pmax, __shfl_xor_sync(0xffffffffu, pmax, x2));
@@ -370,7 +370,11 @@ __global__ void __launch_bounds__(WARPS * 32, PaShape<D, NT, WARPS>::kCtas)
                 if (q >= rows) continue;
                 const int ti = (row0 + q) / gq;
                 const unsigned long long* anc = a.mask ? a.mask + 2LL * (r.row + ti) : nullptr;
-                const int qp = row_position(p, r, ti);
+                int qp;
+                if constexpr (SH)
+                  qp = a.window ? s_qp[warp][q] : 0;  // (read only under a window)
+                else
+                  qp = row_position(p, r, ti);
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
                   if (sees(a, r, ti, qp, anc, kb + k * 8 + g)) vis |= 1u << (nt * 8 + k * 2 + i);
@@ -708,19 +712,9 @@ cudaError_t pa_pass(tss_paged* h, const PgAttnArgs& a, const PaTask* tasks, int 
   PaTask few[kPgMaxReq], many[kPgMaxReq];
   int n_few = 0, n_many = 0, most = 0;
   for (int i = 0; i < n_tasks; ++i) {
-    PaTask t = tasks[i];
+    const PaTask& t = tasks[i];
     if (t.rows == 0) continue;
     if (h->d == 128 && t.rows > limit) {
-      // (in a shared pass what 128 rows leave goes with the blocks of few rows, unless it would be one of many itself)
-      const int rest = t.rows % kPaTcTile;
-      if (shared && rest > 0 && rest <= limit) {
-        PaTask tail = t;
-        tail.skip += t.rows - rest;
-        tail.rows = rest;
-        t.rows -= rest;
-        few[n_few++] = tail;
-        most = rest > most ? rest : most;
-      }
       many[n_many++] = t;
     } else {
       few[n_few++] = t;
@@ -812,7 +806,7 @@ cudaError_t launch_paged_attention(tss_paged* h, const PgAttnArgs& a, const PgBa
   PaTask tasks[kPgMaxReq];
   for (int i = 0; i < batch.n_req; ++i) {
     const PgReq& q = batch.r[i];
-    tasks[i] = PaTask{q, 0, q.first + q.n, q.first, 0, q.n * (h->hq / h->hk), 0, 0, 0};
+    tasks[i] = PaTask{q, 0, q.first + q.n, q.first, q.n * (h->hq / h->hk), 0, 0, 0};
   }
   return pa_pass(h, a, tasks, batch.n_req, nullptr, kPaTcRows, PaWork{h->part_o, h->part_ml, h->counters, 0}, withhold, false, s, too_large);
 }
@@ -830,10 +824,10 @@ cudaError_t launch_paged_attention_shared(tss_paged* h, const PgAttnArgs& args, 
   int n_common = 0, at = 0, n_mem = 0;
   const int gq = h->hq / h->hk;
   for (int g = 0; g < groups.n; ++g) {
-    PaTask t{PgReq{0, groups.shared[g], 0, 0}, 0, groups.shared[g], 0, 0, 0, 0, n_mem, 0};
+    PaTask t{PgReq{0, groups.shared[g], 0, 0}, 0, groups.shared[g], 0, 0, 0, n_mem, 0};
     for (int i = at; i < at + groups.reqs[g]; ++i) {
       const PgReq& q = batch.r[i];
-      mine[i] = PaTask{q, 0, q.first + q.n, q.first, 0, q.n * gq, 0, 0, 0};
+      mine[i] = PaTask{q, 0, q.first + q.n, q.first, q.n * gq, 0, 0, 0};
       if (q.n == 0) continue;
       if (t.members == 0) {
         t.q.seq = q.seq;

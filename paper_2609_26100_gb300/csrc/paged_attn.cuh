@@ -29,7 +29,6 @@ struct PaParams {
 // A pass of the attention over shared keys.  The pass over the shared keys has a group where the others have a request: its rows
 // are those of its requests, `first` and the keys in all are the shared tokens.
 struct PaShared : PaParams {
-  int skip[kPgMaxReq], rows[kPgMaxReq];   // query rows [skip, skip + rows) of the request are the launch's
   int joins[kPgMaxReq];                   // own keys: the request's rows have results over shared ones
   int member[kPgMaxReq], members[kPgMaxReq];  // shared keys: the group's requests, in mem
   int2 mem[kPgMaxReq];                    // first row, first token
@@ -42,16 +41,6 @@ struct PaParamsOf<true> { using type = PaShared; };
 // Index of a request among the parameters' (its arrays beside r).
 __device__ __forceinline__ int index_of(const PaParams& p, const PaReq& r) { return static_cast<int>(&r - p.r); }
 
-// First query row of row tile `tile` of a request, and how many it has.
-__device__ __forceinline__ int tile_rows(const PaParams&, const PaReq& r, int tile, int R, int gq, int* rows) {
-  *rows = min(R, r.n * gq - tile * R);
-  return tile * R;
-}
-__device__ __forceinline__ int tile_rows(const PaShared& p, const PaReq& r, int tile, int R, int, int* rows) {
-  const int b = index_of(p, r);
-  *rows = min(R, p.rows[b] - tile * R);
-  return p.skip[b] + tile * R;
-}
 // Before results over shared keys are read.
 __device__ __forceinline__ void wait_for_shared(const PaParams&) {}
 __device__ __forceinline__ void wait_for_shared(const PaShared& p) {
@@ -256,7 +245,7 @@ struct PaTask {
   PgReq q;
   int k0, k1;
   int from;                    // the smallest index of its rows in the sequence
-  int skip, rows;              // its query rows of a KV head
+  int rows;                    // its query rows of a KV head
   int joins, member, members;  // as in PaShared
 };
 
@@ -291,8 +280,6 @@ inline bool pa_plan(PaShared& p, const PaTask* tasks, int n_tasks, int R, int ha
     PaReq r{q.seq, q.first, q.n, q.row, 0, 0, 0, static_cast<int>(at), items, 0, 1};
     pa_units(a, t, unit, &r);
     if (r.units == 0) continue;
-    p.skip[p.n_req] = t.skip;
-    p.rows[p.n_req] = t.rows;
     p.joins[p.n_req] = t.joins;
     p.member[p.n_req] = t.member;
     p.members[p.n_req] = t.members;

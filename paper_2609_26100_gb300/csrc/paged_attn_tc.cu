@@ -62,6 +62,7 @@ struct __align__(16) PtShared {
   unsigned long long anc[2][kPtRows];                 // the rows of its block that a row sees
   long long out_at[kPtRows];                          // where its output begins
   int qp[kPtRows];                                    // its position
+  int bp[kPgMaxRows];                                 // under a window, the positions of the block's rows
   float inv[kPtRows];                                 // 1 / sum of its weights
   float other[kPtRows];                               // what its results over shared keys are multiplied by
   float top[2][4][kPtRows];                           // maxima of its quarters, of scores and V's scales of each group
@@ -138,8 +139,8 @@ __device__ __forceinline__ bool quad_or(int id, bool v) {
 }
 
 // Keys of the tile from key0 that a row sees (position qp; lo, hi: the rows of its block that it sees).
-__device__ __forceinline__ unsigned long long row_sees(const PgAttnArgs& a, const PaReq& r, int qp, unsigned long long lo, unsigned long long hi,
-                                                       int key0) {
+__device__ __forceinline__ unsigned long long row_sees(const PgAttnArgs& a, const PaReq& r, const int* bp, int qp, unsigned long long lo,
+                                                       unsigned long long hi, int key0) {
   unsigned long long v = ~0ull, blk = 0;  // blk: bits that are rows of the block
   if (key0 + kPtKeys > r.first) {
     if (key0 < r.first) {
@@ -160,7 +161,7 @@ __device__ __forceinline__ unsigned long long row_sees(const PgAttnArgs& a, cons
       near &= ~blk;
       for (unsigned long long x = v & blk; x; x &= x - 1) {
         const int i = __ffsll(static_cast<long long>(x)) - 1;
-        if (qp - max(__ldcg(a.positions + r.row + key0 + i - r.first), r.first) < a.window) near |= 1ull << i;
+        if (qp - bp[key0 + i - r.first] < a.window) near |= 1ull << i;
       }
     }
     v &= near | (sinks >= 64 ? ~0ull : sinks <= 0 ? 0ull : (1ull << sinks) - 1);
@@ -482,8 +483,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
       const int rb = request_of(u0 + t);
       const PaReq& r = p.r[rb];
       const int v = u0 + t - r.off, item = v / r.units, x0 = v - item * r.units, len = min(n - t, r.units - x0);
-      int rows;
-      const int h = item % a.hk, row0 = tile_rows(p, r, item / a.hk, kPtRows, gq, &rows);
+      const int h = item % a.hk, row0 = item / a.hk * kPtRows, rows = min(kPtRows, r.n * gq - row0);
       if (seg == 0) ready();
       // Q: 16 lanes a row, 8 dims each, as chunks in the operand's order; the warp's rows in flight together
       constexpr int kTurns = kPtRows / 2 / kPtSoftWarps;
@@ -541,6 +541,9 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
         if (r.n < 64) anc_lo &= (1ull << r.n) - 1;
         anc_hi = r.n <= 64 ? 0ull : r.n < 128 ? anc_hi & ((1ull << (r.n - 64)) - 1) : anc_hi;
       }
+      // (four trees of 33 rows in a window over a shared prefix: 144 us where every masked page's rows read them from memory, 118 so)
+      if (a.positions && sw * 32 + lane < min(r.n, kPgMaxRows))
+        sh.bp[sw * 32 + lane] = max(__ldcg(a.positions + r.row + sw * 32 + lane), r.first);
       if (qt == 0) {
         sh.qp[row] = qp;
         sh.anc[0][row] = anc_lo;
@@ -583,7 +586,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
             for (int i = 0; i < 4; ++i) {
               const int q = qd * 32 + r4 + 8 * i;
               if (q >= rows) continue;
-              const uint32_t m = static_cast<uint32_t>(row_sees(a, r, sh.qp[q], sh.anc[0][q], sh.anc[1][q], key0) >> (16 * qt)) >> (2 * x4);
+              const uint32_t m = static_cast<uint32_t>(row_sees(a, r, sh.bp, sh.qp[q], sh.anc[0][q], sh.anc[1][q], key0) >> (16 * qt)) >> (2 * x4);
               vis &= ~(15u << (4 * i)) | (m & 3u) << (4 * i) | (m >> 8 & 3u) << (4 * i + 2);
             }
           }
