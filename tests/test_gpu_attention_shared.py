@@ -4,7 +4,8 @@ request.
 Tolerances.  The output's half step (eps / 2 of it).  Weights of one fp16 part, bf16 outputs where some request or group of the call
 has more than 8 rows of a KV head: of v = s c + z the sum of p s c takes p s rounded by up to 2^-12 of it, while that of p z does not,
 so the output is off by up to 2^-12 of the mean of s c = v - z.  As z is the least value of its group, that is at most the
-largest value less the smallest, twice the largest magnitude.  Scores and sums in fp32: a score's error of 2^-20 of the largest
+largest value less the smallest, twice the largest magnitude.  Many rows over shared keys take v itself in fp16: 2^-12 of it more,
+three times 2^-12 of the largest magnitude in all.  Scores and sums in fp32: a score's error of 2^-20 of the largest
 score's size or one moves the weights by as much, and with them the output by that share of the largest value, twice."""
 import math
 import random
@@ -77,7 +78,7 @@ def run_and_check(c, k, v, sizes, shared, first, n, *, dtype=BF, window=0, sinks
     for m in sizes:
         rows += [sum(n[at:at + m])] + n[at:at + m]
         at += m
-    one_part = 2.0 ** -11 if dtype == BF and max(rows) * gq > 8 else 0.0
+    one_part = 3 * 2.0 ** -12 if dtype == BF and max(rows) * gq > 8 else 0.0
     at = 0
     for b, m in enumerate(n):
         if m == 0:
@@ -182,6 +183,44 @@ def test_flat_and_steep_scores(dtype, spread):
     first = [3000 + 31 * i for i in range(20)]
     c, k, v = shared_cache(sizes, shared, first, n, 4, 1, 128, seed=8)
     run_and_check(c, k, v, sizes, shared, first, n, dtype=dtype, scale=spread * 128 ** -0.5)
+
+
+@pytest.mark.parametrize("rows", [9, 16, 31, 33, 64, 65, 80, 97, 128, 129, 200])
+@pytest.mark.parametrize("tokens", [64, 128, 192, 1088])
+def test_row_counts(rows, tokens):
+    """Every width of the kernel for many rows: tiles of an odd page, one tile for two teams, teams of their own rows."""
+    m = min(rows, 64)
+    n = [rows // m + (i < rows % m) for i in range(m)]
+    c, k, v = shared_cache([m], [tokens], [tokens] * m, n, 2, 2, 128, seed=rows)
+    run_and_check(c, k, v, [m], [tokens], [tokens] * m, n)
+
+
+@pytest.mark.parametrize("size", [1e-7, 1e-3, 300.0, 2e4, 6e4, 3e5])
+@pytest.mark.parametrize("rows", [12, 90])
+def test_magnitudes_of_values(size, rows):
+    """Values over the whole range that pages hold, a few tokens much larger than the rest."""
+    first, n = [330, 320], [rows // 2, rows // 2]
+    c, k, v = shared_cache([2], [320], first, n, 2, 2, 128, seed=20)
+    g = torch.Generator(device="cuda").manual_seed(21)
+    kk = torch.randn(320, 2, 128, generator=g, device="cuda").to(BF)
+    vv = torch.randn(320, 2, 128, generator=g, device="cuda") * min(size, 1.0)
+    vv[::7] *= max(size, 1.0)
+    c.append(0, c.batch([0], [0], [320]), kk, vv.to(BF))
+    k, v = ([R.sequence_values(c.pool[0], c.table, b, f + m, 2, 128, side) for b, (f, m) in enumerate(zip(first, n))] for side in (0, 1))
+    run_and_check(c, k, v, [2], [320], first, n, scale=0.02)
+
+
+def test_scores_that_rise_page_by_page():
+    """Keys ever nearer to the queries: references rise at nearly every tile, the outputs so far are scaled each time."""
+    for rows in (16, 100):
+        first, n = [2048, 2048], [rows // 2, rows // 2]
+        c, k, v = shared_cache([2], [2048], first, n, 2, 2, 128, seed=22)
+        g = torch.Generator(device="cuda").manual_seed(23)
+        kk = torch.randn(1, 2, 128, generator=g, device="cuda") * torch.linspace(-3, 3, 2048, device="cuda")[:, None, None]
+        vv = torch.randn(2048, 2, 128, generator=g, device="cuda")
+        c.append(0, c.batch([0], [0], [2048]), kk.to(BF), vv.to(BF))
+        k, v = ([R.sequence_values(c.pool[0], c.table, b, f + m, 2, 128, side) for b, (f, m) in enumerate(zip(first, n))] for side in (0, 1))
+        run_and_check(c, k, v, [2], [2048], first, n, scale=0.5)
 
 
 def test_as_the_attention_of_each():
