@@ -9,7 +9,7 @@
 // Keys take the MMA's 128-row side, so a softmax thread is a key: what belongs to a key (s, z) is in its registers, what belongs to a
 // row (f, a, b, ref) comes as broadcasts for two rows at a time, and the weights of eight rows leave as one vector.  In the
 // orientation of paged_attn_tc.cu (a thread four rows and four keys) the latency of a page's way through a softmax warp bounds the
-// kernel; here a tile's is of twice the keys, and two teams of four warps are at different tiles (up to 64 rows) or at different
+// kernel; here a tile's is of twice the keys, and two teams of eight warps are at different tiles (up to 64 rows) or at different
 // rows of a tile (more).  A thread's sums of p are its key's; they are joined over the keys at the end.
 //
 // The order of a page's keys in the operands is that in which V's words hold them: a word's eight tokens are a vector of an operand
@@ -19,7 +19,8 @@
 // finds the rows' maxima, scales what it has and takes the tile again.  Values of more than 2^15 (a token whose quantised range
 // passes that) enter as 2^-5 of themselves and their weights 2^5 times as large.
 //
-// Roles (448 threads): warp 0 copies pages, warp 1 issues MMAs, warps 2-9 are the teams, warps 10-13 make operands.  Runs of tiles
+// Roles (768 threads): warp 0 copies pages, warp 1 issues MMAs, warps 2-17 are the teams (of eight warps: a quarter of the keys and
+// half of the team's rows each), warps 18-19 make operands of K, 20-23 of V.  Runs of tiles
 // within one item, one CTA an SM; partials of a CTA's teams are joined by the item's last CTA.  Every wait is bounded, as in
 // paged_attn_tc.cu.
 #include <cfloat>
@@ -32,13 +33,14 @@ namespace tss {
 namespace {
 
 constexpr int kPgrD = 128, kPgrTeam = 64, kPgrRows = 2 * kPgrTeam, kPgrKeys = 128;
-constexpr int kPgrSoft = 8, kPgrMake = 4, kPgrThreads = 32 * (2 + kPgrSoft + kPgrMake);
-constexpr int kPgrRaw = 5;                      // pages in the ring of copies
+constexpr int kPgrSoft = 16, kPgrMakeK = 2, kPgrMakeV = 4, kPgrThreads = 32 * (2 + kPgrSoft + kPgrMakeK + kPgrMakeV);
+constexpr int kPgrRaw = 4;                      // pages in the ring of copies
+constexpr int kPgrVals = 3;                     // pages of V's operands
 constexpr int kPgrQ = kPgrTeam * 128;           // a team's rows, one group of dims
 constexpr int kPgrK = kPgrKeys * 128;           // a tile's keys, one group of dims
 constexpr int kPgrV = kPgrD * 128;              // 128 dims, a page's keys
 constexpr int kPgrP = kPgrKeys * 128;           // a tile's keys, a team's rows
-constexpr uint32_t kPgrTmem = 512, kPgrO = 256; // S: team * 128 + group * 64; O: kPgrO + team * 64
+constexpr uint32_t kPgrTmem = 512, kPgrO = 256;  // S: team * 128 + group * 64; O: kPgrO + team * 64
 constexpr float kPgrTop = 512.f;                // weights that raise a reference
 using PgrBlock = PgBlock<kPgrD>;
 
@@ -46,20 +48,51 @@ struct __align__(16) PgrShared {
   float4 rc[2][kPgrTeam / 2][2];                // [team][pair of rows]: f, a of both; b, -ref of both
   uint2 par[4][kPgrKeys];                       // K's (s, z) of both groups, by place
   float vk[4][kPgrKeys];                        // what a key's weights are multiplied by for its values
-  uint64_t raw_full[kPgrRaw], raw_free[kPgrRaw], k_full, k_free, v_full[2], v_free[2], par_full[4], s_full[2], p_full[2], pv_done[2], q_full, drain;
+  uint64_t raw_full[kPgrRaw], raw_free[kPgrRaw], k_full[2], k_free[2], v_full[kPgrVals], v_free[kPgrVals], par_full[4], s_full[2], p_full[2], pv_done[2], q_full, drain;
   float ref[2][kPgrTeam], fac[2][kPgrTeam];
   float wmax[2][4][kPgrTeam], lsum[2][4][kPgrTeam];
   uint32_t tmem;
-  int abort, last, bad_raw[kPgrRaw], bad[4][2], big[4][kPgrMake];
+  int abort, last, bad_raw[kPgrRaw], bad[4][2];
 };
 static_assert(offsetof(PgrShared, par) % 16 == 0 && offsetof(PgrShared, raw_full) % 8 == 0, "alignment of vectors and barriers");
-constexpr size_t kPgrSmem = 1024 + 4 * kPgrQ + 2 * kPgrK + 4 * kPgrV + 2 * kPgrP + kPgrRaw * PgrBlock::kBytes;
+constexpr size_t kPgrSmem = 1024 + 4 * kPgrQ + 4 * kPgrK + kPgrVals * kPgrV + 2 * kPgrP + kPgrRaw * PgrBlock::kBytes;
 
-// 32 lanes x 8 columns of TMEM, left in flight.
+// 32 lanes x 8 columns of TMEM, left in flight until tmem_here() of the registers; stored (tmem_stored()).
 __device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t* r) {
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
                : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_here(uint32_t* a) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(a[0]), "+r"(a[1]), "+r"(a[2]), "+r"(a[3]), "+r"(a[4]), "+r"(a[5]), "+r"(a[6]), "+r"(a[7]));
+}
+__device__ __forceinline__ void tmem_here(uint32_t* a, uint32_t* b) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(a[0]), "+r"(a[1]), "+r"(a[2]), "+r"(a[3]), "+r"(a[4]), "+r"(a[5]), "+r"(a[6]), "+r"(a[7]), "+r"(b[0]), "+r"(b[1]), "+r"(b[2]),
+                 "+r"(b[3]), "+r"(b[4]), "+r"(b[5]), "+r"(b[6]), "+r"(b[7]));
+}
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};\n\ttcgen05.wait::st.sync.aligned;" ::"r"(taddr), "r"(r[0]),
+               "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
+}
+// OR of v over the threads of a team's named barrier.
+__device__ __forceinline__ bool team_or(int id, bool v) {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.u32 q, %1, 0;\n\t"
+      "bar.red.or.pred p, %2, 256, q;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}\n"
+      : "=r"(r)
+      : "r"(v ? 1u : 0u), "r"(id)
+      : "memory");
+  return r != 0;
+}
+// Two pairs from shared memory.  Not volatile, so that they may be loaded ahead of stores to other places; `when` keeps them
+// behind what it depends on.
+__device__ __forceinline__ void pairs_at(uint32_t addr, int when, f2_t* x, f2_t* y) {
+  asm("ld.shared.v2.u64 {%0, %1}, [%2];  // %3" : "=l"(*x), "=l"(*y) : "r"(addr), "r"(when));
 }
 
 // Place of a page's token among the operands' keys.
@@ -78,9 +111,9 @@ __global__ void __launch_bounds__(kPgrThreads, 1) paged_attn_group_kernel(const 
   __shared__ PgrShared sh;
   const uint32_t skew = (1024 - (smem_u32(pgr_dyn) & 1023)) & 1023;
   uint8_t* sq = pgr_dyn + skew;      // [team][group] rows
-  uint8_t* sk = sq + 4 * kPgrQ;      // [group] keys
-  uint8_t* sv = sk + 2 * kPgrK;      // [buffer][page] dims
-  uint8_t* sp = sv + 4 * kPgrV;      // [team] keys
+  uint8_t* sk = sq + 4 * kPgrQ;      // [buffer][group] keys
+  uint8_t* sv = sk + 4 * kPgrK;      // [page] dims
+  uint8_t* sp = sv + kPgrVals * kPgrV;  // [team] keys
   uint8_t* raw = sp + 2 * kPgrP;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const PgAttnArgs& a = p.a;
@@ -97,18 +130,20 @@ __global__ void __launch_bounds__(kPgrThreads, 1) paged_attn_group_kernel(const 
   if (tid == 0) {
     for (int i = 0; i < kPgrRaw; ++i) {
       mbar_init(&sh.raw_full[i], 1);
-      mbar_init(&sh.raw_free[i], kPgrMake);
+      mbar_init(&sh.raw_free[i], kPgrMakeK + kPgrMakeV);
     }
-    mbar_init(&sh.k_full, kPgrMake);
-    mbar_init(&sh.k_free, 1);
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(&sh.v_full[i], kPgrMake);
+    for (int i = 0; i < kPgrVals; ++i) {
+      mbar_init(&sh.v_full[i], kPgrMakeV);
       mbar_init(&sh.v_free[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&sh.k_full[i], kPgrMakeK);
+      mbar_init(&sh.k_free[i], 1);
       mbar_init(&sh.s_full[i], 1);
       mbar_init(&sh.p_full[i], 1);
       mbar_init(&sh.pv_done[i], 1);
     }
-    for (int i = 0; i < 4; ++i) mbar_init(&sh.par_full[i], kPgrMake);
+    for (int i = 0; i < 4; ++i) mbar_init(&sh.par_full[i], kPgrMakeK);
     mbar_init(&sh.q_full, kPgrSoft);
     mbar_init(&sh.drain, 1);
     sh.abort = 0;
@@ -169,68 +204,72 @@ __global__ void __launch_bounds__(kPgrThreads, 1) paged_attn_group_kernel(const 
       const uint32_t q_a = smem_u32(sq), k_a = smem_u32(sk), v_a = smem_u32(sv), p_a = smem_u32(sp);
       constexpr uint32_t id_pv = idesc_f16_m128(kPgrTeam) | (1u << 16);  // (P: rows contiguous)
       const auto wait = [&](uint64_t* bar, int phase) { return mbar_wait(bar, phase & 1, abort, a.status); };
-      const auto scores = [&](int team) {
+      const auto scores = [&](int team, int t) {
         const uint32_t id = idesc_f16_m128(team ? width1 : width0);
         const int rows_of = two ? team : 0;
 #pragma unroll
         for (int g = 0; g < 2; ++g)
 #pragma unroll
           for (int k = 0; k < 4; ++k)
-            umma_bf16(tm + team * 128 + g * 64, sdesc_sw128(k_a + g * kPgrK + k * 32), sdesc_sw128(q_a + (rows_of * 2 + g) * kPgrQ + k * 32), id,
-                      k ? 1u : 0u);
+            umma_bf16(tm + team * 128 + g * 64, sdesc_sw128(k_a + ((t & 1) * 2 + g) * kPgrK + k * 32),
+                      sdesc_sw128(q_a + (rows_of * 2 + g) * kPgrQ + k * 32), id, k ? 1u : 0u);
         umma_commit(&sh.s_full[team]);
       };
-      const auto outputs = [&](int team, int t, bool first) {
+      const auto values = [&](int t) { return wait(&sh.v_full[2 * t % kPgrVals], 2 * t / kPgrVals) && wait(&sh.v_full[(2 * t + 1) % kPgrVals], (2 * t + 1) / kPgrVals); };
+      const auto outputs = [&](int team, int t, bool first, bool last) {  // last: V's last use
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-          umma_bf16(tm + kPgrO + team * 64, sdesc_sw128(v_a + ((t & 1) * 2 + (k >> 2)) * kPgrV + (k & 3) * 32),
-                    sdesc_sw128_mn(p_a + team * kPgrP + k * 16 * 128, kPgrP), id_pv, first && k == 0 ? 0u : 1u);
+        for (int pg = 0; pg < 2; ++pg) {
+          const int s = (2 * t + pg) % kPgrVals;
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            umma_bf16(tm + kPgrO + team * 64, sdesc_sw128(v_a + s * kPgrV + k * 32), sdesc_sw128_mn(p_a + team * kPgrP + (pg * 4 + k) * 16 * 128, kPgrP),
+                      id_pv, first && pg == 0 && k == 0 ? 0u : 1u);
+          if (last) umma_commit(&sh.v_free[s]);
+        }
         umma_commit(&sh.pv_done[team]);
       };
       bool ok = !(p.withhold && blockIdx.x == 0) && wait(&sh.q_full, 0);
       if (two) {
-        ok = ok && wait(&sh.k_full, 0);
+        ok = ok && wait(&sh.k_full[0], 0);
         if (ok) {
           tc_fence_after();
-          scores(0);
-          scores(1);
-          umma_commit(&sh.k_free);
+          scores(0, 0);
+          scores(1, 0);
+          umma_commit(&sh.k_free[0]);
         }
         for (int t = 0; t < n && ok; ++t) {
           const bool more = t + 1 < n;
-          ok = wait(&sh.v_full[t & 1], t >> 1) && wait(&sh.p_full[0], t);
+          ok = values(t) && wait(&sh.p_full[0], t);
           if (!ok) break;
           tc_fence_after();
-          outputs(0, t, t == 0);
-          ok = !more || wait(&sh.k_full, t + 1);
+          outputs(0, t, t == 0, false);
+          ok = !more || wait(&sh.k_full[(t + 1) & 1], (t + 1) >> 1);
           if (!ok) break;
           tc_fence_after();
-          if (more) scores(0);
+          if (more) scores(0, t + 1);
           ok = wait(&sh.p_full[1], t);
           if (!ok) break;
           tc_fence_after();
-          outputs(1, t, t == 0);
-          umma_commit(&sh.v_free[t & 1]);
+          outputs(1, t, t == 0, true);
           if (more) {
-            scores(1);
-            umma_commit(&sh.k_free);
+            scores(1, t + 1);
+            umma_commit(&sh.k_free[(t + 1) & 1]);
           }
         }
       } else {
         const auto tile = [&](int t) {
-          if (!wait(&sh.k_full, t)) return false;
+          if (!wait(&sh.k_full[t & 1], t >> 1)) return false;
           tc_fence_after();
-          scores(t & 1);  // (its team's last tile but one was read out before its P was)
-          umma_commit(&sh.k_free);
+          scores(t & 1, t);  // (its team's last tile but one was read out before its P was)
+          umma_commit(&sh.k_free[t & 1]);
           return true;
         };
         ok = ok && tile(0) && (n < 2 || tile(1));
         for (int t = 0; t < n && ok; ++t) {
-          ok = wait(&sh.v_full[t & 1], t >> 1) && wait(&sh.p_full[t & 1], t >> 1);
+          ok = values(t) && wait(&sh.p_full[t & 1], t >> 1);
           if (!ok) break;
           tc_fence_after();
-          outputs(t & 1, t, t < 2);
-          umma_commit(&sh.v_free[t & 1]);
+          outputs(t & 1, t, t < 2, true);
           ok = t + 2 >= n || tile(t + 2);
         }
       }
@@ -240,107 +279,127 @@ __global__ void __launch_bounds__(kPgrThreads, 1) paged_attn_group_kernel(const 
     }
   } else if (warp >= 2 + kPgrSoft) {
     // ---------------- operands ----------------
+    // A thread reads all that it needs of the pages before it stores anything, so that the loads are on their way together.
     griddep_wait();
     griddep_launch();
-    const int x = tid - 32 * (2 + kPgrSoft), cw = x >> 5;
+    const bool is_k = warp < 2 + kPgrSoft + kPgrMakeK;
+    const int x = tid - 32 * (2 + kPgrSoft + (is_k ? 0 : kPgrMakeK));
     const uint4 zero = make_uint4(0, 0, 0, 0);
-    for (int t = 0; t < n; ++t) {
-      const int s0 = (2 * t) % kPgrRaw, s1 = (2 * t + 1) % kPgrRaw;
-      if (!__all_sync(0xffffffffu, quiet_wait(&sh.raw_full[s0], (2 * t / kPgrRaw) & 1, abort, a.status) &&
-                                       quiet_wait(&sh.raw_full[s1], ((2 * t + 1) / kPgrRaw) & 1, abort, a.status) &&
-                                       (t < 1 || quiet_wait(&sh.k_free, (t - 1) & 1, abort, a.status))))
-        break;
-      const uint8_t* blk[2] = {raw + s0 * PgrBlock::kBytes, raw + s1 * PgrBlock::kBytes};
-      const bool bad[2] = {sh.bad_raw[s0] != 0, sh.bad_raw[s1] != 0};
-      // What belongs to keys, in a buffer of four: S(t - 1), which is complete, was issued after the team of tile t - 3 was done.
-      {
-        const int pg = x >> 6, tok = x & 63, at = pg * 64 + place_of(tok);
-        const uint2 vp = *reinterpret_cast<const uint2*>(blk[pg] + PgrBlock::kVParams + 8 * tok);
-        const bool large = !bad[pg] && (passes(vp.x) || passes(vp.y));
-        sh.par[t & 3][at] = bad[pg] ? make_uint2(0, 0) : *reinterpret_cast<const uint2*>(blk[pg] + PgrBlock::kKParams + 8 * tok);
-        sh.vk[t & 3][at] = large ? 32.f : 1.f;
-        const bool any = __any_sync(0xffffffffu, large);
-        if (lane == 0) sh.big[t & 3][cw] = any;
-        if (tok == 0) sh.bad[t & 3][pg] = bad[pg];
-      }
-      // K: unit w is key w / 4, dims 16 (w % 4) .. + 15 of each group of a page
+    if (is_k) {
+      // Keys x / 4 + 16 i, dims 16 (x % 4) .. + 15 of each group; and what belongs to key x of each page, in a buffer of four
+      // (S(t - 2), which is complete, was issued after the team of tile t - 4 was done).
+      for (int t = 0; t < n; ++t) {
+        bool here = true;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int pg = i >> 1, w = (i & 1) * 128 + x, row = pg * 64 + place_of(w >> 2), c = 2 * (w & 3);
-        const uint4 k = bad[pg] ? zero : *reinterpret_cast<const uint4*>(blk[pg] + PgrBlock::kK + w * 16);
-        uint8_t *k0 = sk + row * 128 + ((c ^ (row & 7)) << 4), *k1 = sk + row * 128 + (((c + 1) ^ (row & 7)) << 4);
-        *reinterpret_cast<uint4*>(k0) = expand(k.x);
-        *reinterpret_cast<uint4*>(k1) = expand(k.y);
-        *reinterpret_cast<uint4*>(k0 + kPgrK) = expand(k.z);
-        *reinterpret_cast<uint4*>(k1 + kPgrK) = expand(k.w);
+        for (int pg = 0; pg < 2; ++pg) here = here && quiet_wait(&sh.raw_full[(2 * t + pg) % kPgrRaw], ((2 * t + pg) / kPgrRaw) & 1, abort, a.status);
+        if (!__all_sync(0xffffffffu, here)) break;
+        uint4 k[2][4];
+        uint2 kp[2], vp[2];
+        bool bad[2];
+#pragma unroll
+        for (int pg = 0; pg < 2; ++pg) {
+          const int s = (2 * t + pg) % kPgrRaw;
+          const uint8_t* blk = raw + s * PgrBlock::kBytes;
+          bad[pg] = sh.bad_raw[s] != 0;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) k[pg][i] = *reinterpret_cast<const uint4*>(blk + PgrBlock::kK + (x + 64 * i) * 16);
+          kp[pg] = *reinterpret_cast<const uint2*>(blk + PgrBlock::kKParams + 8 * x);
+          vp[pg] = *reinterpret_cast<const uint2*>(blk + PgrBlock::kVParams + 8 * x);
+        }
+        if (!__all_sync(0xffffffffu, t < 2 || quiet_wait(&sh.k_free[t & 1], ((t >> 1) - 1) & 1, abort, a.status))) break;
+        uint8_t* op = sk + (t & 1) * 2 * kPgrK;
+#pragma unroll
+        for (int pg = 0; pg < 2; ++pg) {
+          const bool over = !bad[pg] && (passes(vp[pg].x) || passes(vp[pg].y));
+          sh.par[t & 3][pg * 64 + place_of(x)] = bad[pg] ? make_uint2(0, 0) : kp[pg];
+          sh.vk[t & 3][pg * 64 + place_of(x)] = over ? 32.f : 1.f;
+          if (x == 0) sh.bad[t & 3][pg] = bad[pg];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int row = pg * 64 + place_of((x >> 2) + 16 * i), c = 2 * (x & 3);
+            const uint4 w = bad[pg] ? zero : k[pg][i];
+            uint8_t *to0 = op + row * 128 + ((c ^ (row & 7)) << 4), *to1 = op + row * 128 + (((c + 1) ^ (row & 7)) << 4);
+            *reinterpret_cast<uint4*>(to0) = expand(w.x);
+            *reinterpret_cast<uint4*>(to1) = expand(w.y);
+            *reinterpret_cast<uint4*>(to0 + kPgrK) = expand(w.z);
+            *reinterpret_cast<uint4*>(to1 + kPgrK) = expand(w.w);
+          }
+        }
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(&sh.par_full[t & 3]);
+          mbar_arrive(&sh.k_full[t & 1]);
+          mbar_arrive(&sh.raw_free[(2 * t) % kPgrRaw]);
+          mbar_arrive(&sh.raw_free[(2 * t + 1) % kPgrRaw]);
+        }
       }
-      fence_async_smem();
-      __syncwarp();
-      if (lane == 0) {
-        mbar_arrive(&sh.par_full[t & 3]);
-        mbar_arrive(&sh.k_full);
-      }
-      if (!__all_sync(0xffffffffu, t < 2 || quiet_wait(&sh.v_free[t & 1], ((t >> 1) - 1) & 1, abort, a.status))) break;
-      // V: the thread's dims 4 (x / 4) .. + 3, of each half page the tokens 8 b + 2 (x % 4) + i: a vector of a dim's row
-      const int d0 = (x >> 2) * 4, t4 = x & 3;
+    } else {
+      // V, a page at a time: of half a page the tokens 8 b + 2 t4 + i, a vector of a dim's row; of dims d0 .. + 3 and d0 + 32 .. + 35
+      const int t4 = x & 3, half = (x >> 5) & 1, group = x >> 6, d0 = group * 64 + ((x >> 2) & 7) * 4;
       const __half2 sixteenth = __half2half2(__ushort_as_half(0x2c00)), m64 = __half2half2(__ushort_as_half(0xd400)),
                     m1024 = __half2half2(__ushort_as_half(0xe400));
+      for (int q = 0; q < 2 * n; ++q) {
+        const int rs = q % kPgrRaw, vs = q % kPgrVals;
+        if (!__all_sync(0xffffffffu, quiet_wait(&sh.raw_full[rs], (q / kPgrRaw) & 1, abort, a.status))) break;
+        const uint8_t* blk = raw + rs * PgrBlock::kBytes;
+        const bool bad = sh.bad_raw[rs] != 0;
+        uint4 v[2];
+        uint2 ev[4], od[4];
 #pragma unroll
-      for (int pg = 0; pg < 2; ++pg) {
-        const uint2 v0 = *reinterpret_cast<const uint2*>(blk[pg] + PgrBlock::kVParams + 8 * lane),
-                    v1 = *reinterpret_cast<const uint2*>(blk[pg] + PgrBlock::kVParams + 8 * (lane + 32));
-        const bool large = __any_sync(0xffffffffu, passes(v0.x) || passes(v0.y) || passes(v1.x) || passes(v1.y));
-        uint8_t* op = sv + ((t & 1) * 2 + pg) * kPgrV;
+        for (int i = 0; i < 2; ++i) v[i] = *reinterpret_cast<const uint4*>(blk + PgrBlock::kV + (half * 128 + (d0 / 4 + 8 * i) * 4 + t4) * 16);
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const uint4 v = *reinterpret_cast<const uint4*>(blk[pg] + PgrBlock::kV + (half * 128 + x) * 16);
-          const uint8_t* vp = blk[pg] + PgrBlock::kVParams + 8 * (32 * half + 2 * t4) + 4 * (d0 / 64);
-          __half2 s[4], z[4];
+        for (int i = 0; i < 4; ++i) {
+          ev[i] = *reinterpret_cast<const uint2*>(blk + PgrBlock::kVParams + 8 * (32 * half + 8 * i + 2 * t4));
+          od[i] = *reinterpret_cast<const uint2*>(blk + PgrBlock::kVParams + 8 * (32 * half + 8 * i + 2 * t4 + 1));
+        }
+        __half2 s[4], z[4];
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            uint32_t e = *reinterpret_cast<const uint32_t*>(vp + 64 * q), o = *reinterpret_cast<const uint32_t*>(vp + 64 * q + 8);
-            if (large) {  // (the tokens' other group decides too)
-              const __half2 down = __half2half2(__ushort_as_half(0x2800));  // 2^-5
-              const int other = 4 - 8 * (d0 / 64);
-              const uint32_t e2 = *reinterpret_cast<const uint32_t*>(vp + 64 * q + other), o2 = *reinterpret_cast<const uint32_t*>(vp + 64 * q + 8 + other);
-              if (passes(e) || passes(e2)) e = u32(__hmul2(h2(e), down));
-              if (passes(o) || passes(o2)) o = u32(__hmul2(h2(o), down));
-            }
-            s[q] = h2(__byte_perm(e, o, 0x5410));
-            z[q] = h2(__byte_perm(e, o, 0x7632));
-          }
-          const uint32_t vw[4] = {v.x, v.y, v.z, v.w};
+        for (int i = 0; i < 4; ++i) {
+          uint32_t e = group ? ev[i].y : ev[i].x, o = group ? od[i].y : od[i].x;
+          // (either group's values decide)
+          const __half2 down = __half2half2(__ushort_as_half(0x2800));  // 2^-5
+          if (passes(ev[i].x) || passes(ev[i].y)) e = u32(__hmul2(h2(e), down));
+          if (passes(od[i].x) || passes(od[i].y)) o = u32(__hmul2(h2(o), down));
+          s[i] = h2(__byte_perm(e, o, 0x5410));
+          z[i] = h2(__byte_perm(e, o, 0x7632));
+        }
+        if (!__all_sync(0xffffffffu, q < kPgrVals || quiet_wait(&sh.v_free[vs], (q / kPgrVals - 1) & 1, abort, a.status))) break;
+        uint8_t* op = sv + vs * kPgrV + d0 * 128;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const uint32_t vw[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const uint32_t lo = vw[e], hi = vw[e] >> 8;
             // codes as 1024 + c, or 1024 + 16 c from nibbles four bits up; to c exactly
-            const __half2 c0 = __hadd2(h2((lo & 0x000f000fu) | 0x64006400u), m1024), c1 = __hfma2(h2((lo & 0x00f000f0u) | 0x64006400u), sixteenth, m64);
-            const __half2 c2 = __hadd2(h2((hi & 0x000f000fu) | 0x64006400u), m1024), c3 = __hfma2(h2((hi & 0x00f000f0u) | 0x64006400u), sixteenth, m64);
-            const uint4 y = make_uint4(u32(__hfma2(c0, s[0], z[0])), u32(__hfma2(c1, s[1], z[1])), u32(__hfma2(c2, s[2], z[2])), u32(__hfma2(c3, s[3], z[3])));
-            *reinterpret_cast<uint4*>(op + (d0 + e) * 128 + (((4 * half + t4) ^ ((d0 + e) & 7)) << 4)) = bad[pg] ? zero : y;
+            const __half2 k0 = __hadd2(h2((lo & 0x000f000fu) | 0x64006400u), m1024), k1 = __hfma2(h2((lo & 0x00f000f0u) | 0x64006400u), sixteenth, m64);
+            const __half2 k2 = __hadd2(h2((hi & 0x000f000fu) | 0x64006400u), m1024), k3 = __hfma2(h2((hi & 0x00f000f0u) | 0x64006400u), sixteenth, m64);
+            const uint4 y = make_uint4(u32(__hfma2(k0, s[0], z[0])), u32(__hfma2(k1, s[1], z[1])), u32(__hfma2(k2, s[2], z[2])), u32(__hfma2(k3, s[3], z[3])));
+            *reinterpret_cast<uint4*>(op + (32 * i + e) * 128 + (((4 * half + t4) ^ ((d0 + e) & 7)) << 4)) = bad ? zero : y;
           }
         }
-      }
-      fence_async_smem();
-      __syncwarp();
-      if (lane == 0) {
-        mbar_arrive(&sh.v_full[t & 1]);
-        mbar_arrive(&sh.raw_free[s0]);
-        mbar_arrive(&sh.raw_free[s1]);
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(&sh.v_full[vs]);
+          mbar_arrive(&sh.raw_free[rs]);
+        }
       }
     }
   } else {
-    // ---------------- teams: a thread is a key ----------------
+    // ---------------- teams: a thread is a key, for half of the team's rows ----------------
     // After a wait that gave up the threads go on without waiting, through the same barriers.
-    const int sw = warp - 2, team = sw >> 2, qd = warp & 3, wt = (sw & 3) * 32 + lane, key = qd * 32 + lane, bar = 1 + team;
+    constexpr int kTeamThreads = 16 * kPgrSoft;
+    const int sw = warp - 2, team = sw >> 3, side = (sw >> 2) & 1, qd = warp & 3, wt = (sw & 7) * 32 + lane, key = qd * 32 + lane, bar = 1 + team;
     const uint32_t lanes = static_cast<uint32_t>(qd * 32) << 16;
-    const int width = team ? width1 : width0;
+    const int width = team ? width1 : width0, c0 = side * (width / 16), c1 = c0 + width / 16;  // the thread's rows, in eights
     griddep_wait();
     griddep_launch();
     // Q: 16 lanes a row, 8 dims each, as vectors in the operand's order; a team its own rows, or half of the common ones
     {
       const int mine = two ? kPgrTeam : kPgrTeam / 2, from = two ? 0 : team * (kPgrTeam / 2), c8 = lane & 15;
-      for (int i = (sw & 3) * 2 + (lane >> 4); i < mine; i += 8) {
+      for (int i = (sw & 7) * 2 + (lane >> 4); i < mine; i += kPgrSoft) {
         const int qr = from + i, row = (two ? team * kPgrTeam : 0) + qr, q = row0 + row;
         uint4 in = make_uint4(0, 0, 0, 0);
         if (row < rows)
@@ -380,11 +439,12 @@ __global__ void __launch_bounds__(kPgrThreads, 1) paged_attn_group_kernel(const 
     __syncwarp();
     if (lane == 0) mbar_arrive(&sh.q_full);
     named_bar_sync(3, 32 * kPgrSoft);
-    f2_t l[kPgrTeam / 2];  // the key's sums of p, by pairs of rows
+    constexpr int kEights = kPgrTeam / 16;  // of a thread's rows
+    f2_t l[4 * kEights];                    // the key's sums of p, by pairs of rows
 #pragma unroll
-    for (int i = 0; i < kPgrTeam / 2; ++i) l[i] = f2_pack(0.f, 0.f);
+    for (int i = 0; i < 4 * kEights; ++i) l[i] = f2_pack(0.f, 0.f);
     uint8_t* prow = sp + team * kPgrP + key * 128;
-    const uint32_t s_at = tm + lanes + team * 128, o_at = tm + lanes + kPgrO + team * 64;
+    const uint32_t s_at = tm + lanes + team * 128, o_at = tm + lanes + kPgrO + team * 64, rc_at = smem_u32(&sh.rc[team][0][0]);
     bool ok = true;
     int used = 0;
     for (int t = two ? 0 : team; t < n; t += two ? 1 : 2, ++used) {
@@ -394,127 +454,130 @@ __global__ void __launch_bounds__(kPgrThreads, 1) paged_attn_group_kernel(const 
       __syncwarp();
       tc_fence_after();
       const bool none = sh.bad[pb][qd >> 1] != 0;  // no such page
-      const bool big = (sh.big[pb][0] | sh.big[pb][1] | sh.big[pb][2] | sh.big[pb][3]) != 0;
       const uint2 kp = sh.par[pb][key];
       const float vk = sh.vk[pb][key];
       const float2 sz0 = __half22float2(h2(kp.x)), sz1 = __half22float2(h2(kp.y));
       const f2_t ks0 = f2_pack(sz0.x, sz0.x), kz0 = f2_pack(sz0.y, sz0.y), ks1 = f2_pack(sz1.x, sz1.x), kz1 = f2_pack(sz1.y, sz1.y);
-      // every eight rows' exponents e - ref to use(rows / 8, four pairs)
-      const auto each = [&](auto use) {
+      // every eight rows' exponents e - ref to use(eight, four pairs)
+      const auto each = [&](int when, auto use) {
 #pragma unroll
-        for (int c = 0; c < kPgrTeam / 8; ++c) {
-          if (c * 8 >= width) break;
-          uint32_t now[2][8];
-          tmem_ld8(s_at + c * 8, now[0]);
-          tmem_ld8(s_at + 64 + c * 8, now[1]);
-          tmem_wait();
+        for (int cc = 0; cc < kEights; ++cc) {
+          const int c = c0 + cc;
+          if (c >= c1) break;
+          uint32_t s0[8], s1[8];
+          tmem_ld8(s_at + c * 8, s0);
+          tmem_ld8(s_at + 64 + c * 8, s1);
+          tmem_here(s0, s1);
           f2_t e[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const ulonglong2 fa = *reinterpret_cast<const ulonglong2*>(&sh.rc[team][c * 4 + i][0]);
-            const ulonglong2 bn = *reinterpret_cast<const ulonglong2*>(&sh.rc[team][c * 4 + i][1]);
-            const f2_t x0 = f2_pack(__uint_as_float(now[0][2 * i]), __uint_as_float(now[0][2 * i + 1]));
-            const f2_t x1 = f2_pack(__uint_as_float(now[1][2 * i]), __uint_as_float(now[1][2 * i + 1]));
+          for (int q = 0; q < 4; ++q) {
+            f2_t f, ra, rb, nref;
+            pairs_at(rc_at + (c * 4 + q) * 32, when, &f, &ra);
+            pairs_at(rc_at + (c * 4 + q) * 32 + 16, when, &rb, &nref);
+            const f2_t x0 = f2_pack(__uint_as_float(s0[2 * q]), __uint_as_float(s0[2 * q + 1]));
+            const f2_t x1 = f2_pack(__uint_as_float(s1[2 * q]), __uint_as_float(s1[2 * q + 1]));
             const f2_t code = f2_fma(ks1, x1, f2_mul(ks0, x0));
-            e[i] = f2_fma(code, fa.x, f2_fma(kz0, fa.y, f2_fma(kz1, bn.x, bn.y)));
+            e[q] = f2_fma(code, f, f2_fma(kz0, ra, f2_fma(kz1, rb, nref)));
           }
-          use(c, e);
+          use(cc, e);
         }
       };
       // the tile's weights, into P and the sums; whether one passes kPgrTop
-      const auto weigh = [&](auto big_tag) {
-        constexpr bool kBig = decltype(big_tag)::value;
+      const auto weights = [&](int when) {
+        if (none) return false;
         __half2 top = __half2half2(__ushort_as_half(0));
-        float most = -INFINITY;
-        each([&](int c, const f2_t* e) {
+        const f2_t vk2 = f2_pack(vk, vk);
+        each(when, [&](int cc, const f2_t* e) {
           uint32_t w[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const float2 x = f2_unpack(e[i]);
-            float2 y = make_float2(ex2(x.x), ex2(x.y));
-            l[c * 4 + i] = f2_add(l[c * 4 + i], f2_pack(y.x, y.y));
-            if constexpr (kBig) {
-              most = fmaxf(most, fmaxf(x.x, x.y));
-              y.x *= vk;
-              y.y *= vk;
-            }
-            w[i] = pack_f16(y.x, y.y);
-            if constexpr (!kBig) top = __hmax2(top, h2(w[i]));
+            const f2_t y = f2_pack(ex2(x.x), ex2(x.y));
+            l[cc * 4 + i] = f2_add(l[cc * 4 + i], y);
+            const float2 v = f2_unpack(f2_mul(y, vk2));
+            w[i] = pack_f16(v.x, v.y);
+            top = __hmax2(top, h2(w[i]));
           }
-          *reinterpret_cast<uint4*>(prow + ((c ^ (key & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+          *reinterpret_cast<uint4*>(prow + (((c0 + cc) ^ (key & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
         });
-        if constexpr (kBig) return most > 9.f;
         const float2 m = __half22float2(top);
-        return fmaxf(m.x, m.y) > kPgrTop;
+        return fmaxf(m.x, m.y) > kPgrTop * vk;
       };
-      const auto weights = [&]() { return none ? false : big ? weigh(std::true_type{}) : weigh(std::false_type{}); };
       if (none)
-        for (int c = 0; c < kPgrTeam / 8; ++c) *reinterpret_cast<uint4*>(prow + (c << 4)) = make_uint4(0, 0, 0, 0);
-      bool over = weights();
+        for (int c = c0; c < c1; ++c) *reinterpret_cast<uint4*>(prow + ((c ^ (key & 7)) << 4)) = make_uint4(0, 0, 0, 0);
+      const bool over = weights(2 * t);
       fence_async_smem();
       tc_fence_before();
-      if (quad_or(bar, over)) {
+      if (team_or(bar, over)) {
         // References rise.  The tile's sums are taken back (what an infinite weight leaves is scaled to nothing), the rows' maxima
         // over the keys found.
         tc_fence_after();
         if (!none) {
-          each([&](int c, const f2_t* e) {
+          each(2 * t, [&](int cc, const f2_t* e) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const float2 x = f2_unpack(e[i]), was = f2_unpack(l[c * 4 + i]);
+              const float2 x = f2_unpack(e[i]), was = f2_unpack(l[cc * 4 + i]);
               const float2 y = make_float2(ex2(x.x), ex2(x.y));
-              l[c * 4 + i] = f2_pack(y.x == INFINITY ? 0.f : was.x - y.x, y.y == INFINITY ? 0.f : was.y - y.y);
+              l[cc * 4 + i] = f2_pack(y.x == INFINITY ? 0.f : was.x - y.x, y.y == INFINITY ? 0.f : was.y - y.y);
             }
           });
           // (scores without the references: the first tile's are the largest float)
-          for (int q = 0; q < kPgrTeam; ++q) {
-            if (q >= width) break;
-            uint32_t s[2];
-            asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(s[0]) : "r"(s_at + q));
-            asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(s[1]) : "r"(s_at + 64 + q));
-            tmem_wait();
-            const float* rc = reinterpret_cast<const float*>(&sh.rc[team][q >> 1][0]) + (q & 1);
-            const float code = fmaf(sz1.x, __uint_as_float(s[1]), sz0.x * __uint_as_float(s[0]));
-            float e = fmaf(code, rc[0], fmaf(sz0.y, rc[2], sz1.y * rc[4]));
+#pragma unroll 1
+          for (int c = c0; c < c1; ++c) {
+            uint32_t s0[8], s1[8];
+            tmem_ld8(s_at + c * 8, s0);
+            tmem_ld8(s_at + 64 + c * 8, s1);
+            tmem_here(s0, s1);
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1) e = fmaxf(e, __shfl_xor_sync(0xffffffffu, e, o));
-            if (lane == 0) sh.wmax[team][sw & 3][q] = e;
+            for (int i = 0; i < 8; ++i) {
+              const int q = c * 8 + i;
+              const float* rc = reinterpret_cast<const float*>(&sh.rc[team][q >> 1][0]) + (q & 1);
+              const float code = fmaf(sz1.x, __uint_as_float(s1[i]), sz0.x * __uint_as_float(s0[i]));
+              float e = fmaf(code, rc[0], fmaf(sz0.y, rc[2], sz1.y * rc[4]));
+#pragma unroll
+              for (int o = 16; o > 0; o >>= 1) e = fmaxf(e, __shfl_xor_sync(0xffffffffu, e, o));
+              if (lane == 0) sh.wmax[team][qd][q] = e;
+            }
           }
         } else {
-          for (int q = lane; q < kPgrTeam; q += 32) sh.wmax[team][sw & 3][q] = -INFINITY;
+          for (int q = c0 * 8 + lane; q < c1 * 8; q += 32) sh.wmax[team][qd][q] = -INFINITY;
         }
         tc_fence_before();
-        named_bar_sync(bar, 128);
+        named_bar_sync(bar, kTeamThreads);
         if (wt < kPgrTeam) {
           const int row = (two ? team * kPgrTeam : 0) + wt;
-          const float most = fmaxf(fmaxf(sh.wmax[team][0][wt], sh.wmax[team][1][wt]), fmaxf(sh.wmax[team][2][wt], sh.wmax[team][3][wt]));
-          const float ref = sh.ref[team][wt];
           float fac = 1.f;
-          if (row < rows && wt < width && most - ref > 9.f) {
-            const float now = ceilf(most);
-            fac = ref == -FLT_MAX ? 0.f : pow2(ref - now);
-            sh.ref[team][wt] = now;
-            (reinterpret_cast<float*>(&sh.rc[team][wt >> 1][1]) + (wt & 1))[2] = -now;
+          if (row < rows) {
+            const float most = fmaxf(fmaxf(sh.wmax[team][0][wt], sh.wmax[team][1][wt]), fmaxf(sh.wmax[team][2][wt], sh.wmax[team][3][wt]));
+            const float ref = sh.ref[team][wt];
+            if (most - ref > 9.f) {
+              const float now = ceilf(most);
+              fac = ref == -FLT_MAX ? 0.f : pow2(ref - now);
+              sh.ref[team][wt] = now;
+              (reinterpret_cast<float*>(&sh.rc[team][wt >> 1][1]) + (wt & 1))[2] = -now;
+            }
           }
           sh.fac[team][wt] = fac;
         }
-        named_bar_sync(bar, 128);
+        named_bar_sync(bar, kTeamThreads);
         tc_fence_after();
 #pragma unroll
-        for (int i = 0; i < kPgrTeam / 2; ++i) l[i] = f2_mul(l[i], *reinterpret_cast<const f2_t*>(&sh.fac[team][2 * i]));
+        for (int i = 0; i < 4 * kEights; ++i)
+          if (i < (c1 - c0) * 4) l[i] = f2_mul(l[i], *reinterpret_cast<const f2_t*>(&sh.fac[team][c0 * 8 + 2 * i]));
         if (j > 0)
-          for (int c = 0; c < width; c += 16) {
-            float o[16];
-            __syncwarp();
-            tmem_ld16(o_at + c, o);
+#pragma unroll 1
+          for (int c = c0; c < c1; ++c) {
+            uint32_t o[8];
+            tmem_ld8(o_at + c * 8, o);
+            tmem_here(o);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) o[i] *= sh.fac[team][c + i];
-            tmem_st16(o_at + c, o);
+            for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * sh.fac[team][c * 8 + i]);
+            tmem_st8(o_at + c * 8, o);
           }
-        weights();
+        weights(2 * t + 1);
         fence_async_smem();
         tc_fence_before();
-        named_bar_sync(bar, 128);
+        named_bar_sync(bar, kTeamThreads);
       }
       if (wt == 0) mbar_arrive(&sh.p_full[team]);
     }
@@ -523,31 +586,32 @@ __global__ void __launch_bounds__(kPgrThreads, 1) paged_attn_group_kernel(const 
     __syncwarp();
     tc_fence_after();
 #pragma unroll
-    for (int i = 0; i < kPgrTeam / 2; ++i) {
+    for (int i = 0; i < 4 * kEights; ++i) {
       float2 y = f2_unpack(l[i]);
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) {
         y.x += __shfl_xor_sync(0xffffffffu, y.x, o);
         y.y += __shfl_xor_sync(0xffffffffu, y.y, o);
       }
-      if (lane == 0) *reinterpret_cast<float2*>(&sh.lsum[team][sw & 3][2 * i]) = y;
+      if (lane == 0 && i < (c1 - c0) * 4) *reinterpret_cast<float2*>(&sh.lsum[team][qd][c0 * 8 + 2 * i]) = y;
     }
     const int mine = two && !team ? kPgrTeam : rows - (two ? kPgrTeam : 0);  // the team's rows
     const long long slot = (static_cast<long long>(blockIdx.x) * 2 + team) * kPgrTeam;
-    named_bar_sync(bar, 128);
+    named_bar_sync(bar, kTeamThreads);
     if (wt < mine) {
       const float sum = (sh.lsum[team][0][wt] + sh.lsum[team][1][wt]) + (sh.lsum[team][2][wt] + sh.lsum[team][3][wt]);
       const float ref = sh.ref[team][wt];
       __stcg(p.part_ml + slot + wt, make_float2(ref == -FLT_MAX ? -INFINITY : ref, sum));
     }
     if (used > 0)
-      for (int c = 0; c < mine; c += 16) {
-        float o[16];
-        __syncwarp();
-        tmem_ld16(o_at + c, o);
+#pragma unroll 1
+      for (int c = c0; c < c1; ++c) {
+        uint32_t o[8];
+        tmem_ld8(o_at + c * 8, o);
+        tmem_here(o);
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (c + i < mine) __stcg(p.part_o + (slot + c + i) * kPgrD + key, o[i]);
+        for (int i = 0; i < 8; ++i)
+          if (c * 8 + i < mine) __stcg(p.part_o + (slot + c * 8 + i) * kPgrD + key, __uint_as_float(o[i]));
       }
     tc_fence_before();
     named_bar_sync(3, 32 * kPgrSoft);
