@@ -34,7 +34,7 @@ namespace {
 
 constexpr int kPgrD = 128, kPgrTeam = 64, kPgrRows = 2 * kPgrTeam, kPgrKeys = 128;
 constexpr int kPgrSoft = 16, kPgrMakeK = 2, kPgrMakeV = 4, kPgrThreads = 32 * (2 + kPgrSoft + kPgrMakeK + kPgrMakeV);
-constexpr int kPgrRaw = 4;                      // pages in the ring of copies
+constexpr int kPgrRaw = 4;                      // pages in the rings of copies, of K's parts and of V's
 constexpr int kPgrVals = 3;                     // pages of V's operands
 constexpr int kPgrQ = kPgrTeam * 128;           // a team's rows, one group of dims
 constexpr int kPgrK = kPgrKeys * 128;           // a tile's keys, one group of dims
@@ -43,19 +43,21 @@ constexpr int kPgrP = kPgrKeys * 128;           // a tile's keys, a team's rows
 constexpr uint32_t kPgrTmem = 512, kPgrO = 256;  // S: team * 128 + group * 64; O: kPgrO + team * 64
 constexpr float kPgrTop = 512.f;                // weights that raise a reference
 using PgrBlock = PgBlock<kPgrD>;
+constexpr int kPgrRawK = PgrBlock::kCodes + 2 * PgrBlock::kParams;  // of a page K's codes, and the parameters of K and V
+constexpr int kPgrRawV = PgrBlock::kCodes + PgrBlock::kParams;      // V's codes and parameters
 
 struct __align__(16) PgrShared {
   float4 rc[2][kPgrTeam / 2][2];                // [team][pair of rows]: f, a of both; b, -ref of both
-  uint2 par[4][kPgrKeys];                       // K's (s, z) of both groups, by place
-  float vk[4][kPgrKeys];                        // what a key's weights are multiplied by for its values
-  uint64_t raw_full[kPgrRaw], raw_free[kPgrRaw], k_full[2], k_free[2], v_full[kPgrVals], v_free[kPgrVals], par_full[4], s_full[2], p_full[2], pv_done[2], q_full, drain;
+  uint2 par[4][kPgrKeys];                       // K's (s, z) of both groups, by place; the first sign: the key's values are large
+  uint64_t raw_full[2][kPgrRaw], raw_free[2][kPgrRaw], k_full[2], k_free[2], v_full[kPgrVals], v_free[kPgrVals], par_full[4], s_full[2], p_full[2], pv_done[2], q_full, drain;
   float ref[2][kPgrTeam], fac[2][kPgrTeam];
   float wmax[2][4][kPgrTeam], lsum[2][4][kPgrTeam];
   uint32_t tmem;
-  int abort, last, bad_raw[kPgrRaw], bad[4][2];
+  int abort, last, bad_raw[2][kPgrRaw], bad[4][2];
 };
+static_assert(PgrBlock::kKParams + PgrBlock::kParams == PgrBlock::kVParams, "one copy brings the parameters of both");
 static_assert(offsetof(PgrShared, par) % 16 == 0 && offsetof(PgrShared, raw_full) % 8 == 0, "alignment of vectors and barriers");
-constexpr size_t kPgrSmem = 1024 + 4 * kPgrQ + 4 * kPgrK + kPgrVals * kPgrV + 2 * kPgrP + kPgrRaw * PgrBlock::kBytes;
+constexpr size_t kPgrSmem = 1024 + 4 * kPgrQ + 4 * kPgrK + kPgrVals * kPgrV + 2 * kPgrP + kPgrRaw * (kPgrRawK + kPgrRawV);
 
 // 32 lanes x 8 columns of TMEM, left in flight until tmem_here() of the registers; stored (tmem_stored()).
 __device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t* r) {
@@ -114,7 +116,8 @@ __global__ void __launch_bounds__(kPgrThreads, 1) paged_attn_group_kernel(const 
   uint8_t* sk = sq + 4 * kPgrQ;      // [buffer][group] keys
   uint8_t* sv = sk + 4 * kPgrK;      // [page] dims
   uint8_t* sp = sv + kPgrVals * kPgrV;  // [team] keys
-  uint8_t* raw = sp + 2 * kPgrP;
+  uint8_t* raw_k = sp + 2 * kPgrP;
+  uint8_t* raw_v = raw_k + kPgrRaw * kPgrRawK;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const PgAttnArgs& a = p.a;
   const int gq = a.hq / a.hk;
@@ -128,10 +131,11 @@ __global__ void __launch_bounds__(kPgrThreads, 1) paged_attn_group_kernel(const 
   const bool two = rows > kPgrTeam;  // the teams have rows of their own; else every second tile
   const int width0 = two ? kPgrTeam : (rows + 15) & ~15, width1 = two ? (rows - kPgrTeam + 15) & ~15 : width0;  // teams' rows, in 16s
   if (tid == 0) {
-    for (int i = 0; i < kPgrRaw; ++i) {
-      mbar_init(&sh.raw_full[i], 1);
-      mbar_init(&sh.raw_free[i], kPgrMakeK + kPgrMakeV);
-    }
+    for (int i = 0; i < kPgrRaw; ++i)
+      for (int side = 0; side < 2; ++side) {
+        mbar_init(&sh.raw_full[side][i], 1);
+        mbar_init(&sh.raw_free[side][i], side ? kPgrMakeV : kPgrMakeK);
+      }
     for (int i = 0; i < kPgrVals; ++i) {
       mbar_init(&sh.v_full[i], kPgrMakeV);
       mbar_init(&sh.v_free[i], 1);
@@ -160,42 +164,69 @@ __global__ void __launch_bounds__(kPgrThreads, 1) paged_attn_group_kernel(const 
   volatile int* abort = &sh.abort;
 
   if (warp == 0) {
-    // ---------------- pages: the table's entries 32 at a time, one bulk copy a page ----------------
+    // ---------------- pages: K's parts and V's, each as far ahead as its ring goes (K's operands are made earlier) ----------------
     const int pages = r.first / kPgTokens, slots = 2 * n;  // (the last tile's second page may be none)
-    int q = 0;
-    bool ok = true;
-    for (int q0 = 0; q0 < slots && ok; q0 += 32) {
+    griddep_wait();
+    griddep_launch();
+    int at[2] = {0, 0}, from = 0;  // parts asked for; the first page whose places the lanes hold
+    const auto places = [&](int q0) {
       const int at = 2 * x0 + q0 + lane;
-      long long blk = -1;
-      if (q0 == 0) {
-        griddep_wait();
-        griddep_launch();
-      }
-      if (q0 + lane < slots && at < pages) {
-        const int page = __ldcg(a.table + static_cast<long long>(r.seq) * a.max_pages + at);
-        if (page >= 0 && page < a.n_pages)
-          blk = static_cast<long long>(page) * a.hk + h;
-        else
-          report(a.status, kStatusCheck);
-      }
-      for (int k = 0; k < 32 && q < slots; ++k, ++q) {
-        const long long src = __shfl_sync(0xffffffffu, blk, k);
-        const int s = q % kPgrRaw;
-        ok = __all_sync(0xffffffffu, q < kPgrRaw || quiet_wait(&sh.raw_free[s], ((q / kPgrRaw) - 1) & 1, abort, a.status));
-        if (!ok) break;
+      if (q0 + lane >= slots || at >= pages) return -1;
+      const int page = __ldcg(a.table + static_cast<long long>(r.seq) * a.max_pages + at);
+      if (page >= 0 && page < a.n_pages) return page;
+      report(a.status, kStatusCheck);
+      return -1;
+    };
+    int now = places(0), later = places(32);
+    uint64_t moved = globaltimer_ns();
+    bool ok = true;
+    while (ok && at[1] < slots) {
+      bool any = false;
+#pragma unroll
+      for (int side = 0; side < 2; ++side) {
+        const int q = at[side], s = q % kPgrRaw;
+        // (K's ring is at most some pages ahead of V's, within the 64 that the lanes hold)
+        if (q >= slots || q >= from + 64 || (q >= kPgrRaw && !__any_sync(0xffffffffu, mbar_test(&sh.raw_free[side][s], ((q / kPgrRaw) - 1) & 1)))) continue;
+        const int page = __shfl_sync(0xffffffffu, q - from < 32 ? now : later, (q - from) & 31);
         if (lane == 0) {
-          sh.bad_raw[s] = src < 0;
-          if (src < 0) {
-            mbar_arrive(&sh.raw_full[s]);
+          uint64_t* bar = &sh.raw_full[side][s];
+          sh.bad_raw[side][s] = page < 0;
+          if (page < 0) {
+            mbar_arrive(bar);
           } else {
-            mbar_arrive_expect_tx(&sh.raw_full[s], PgrBlock::kBytes);
-            bulk_load(raw + s * PgrBlock::kBytes, a.pool + src * PgrBlock::kBytes, PgrBlock::kBytes, &sh.raw_full[s]);
+            const uint8_t* src = a.pool + (static_cast<long long>(page) * a.hk + h) * PgrBlock::kBytes;
+            uint8_t* to = side ? raw_v + s * kPgrRawV : raw_k + s * kPgrRawK;
+            mbar_arrive_expect_tx(bar, side ? kPgrRawV : kPgrRawK);
+            bulk_load(to, src + (side ? PgrBlock::kV : PgrBlock::kK), PgrBlock::kCodes, bar);
+            bulk_load(to + PgrBlock::kCodes, src + (side ? PgrBlock::kVParams : PgrBlock::kKParams), side ? PgrBlock::kParams : 2 * PgrBlock::kParams, bar);
           }
+        }
+        __syncwarp();
+        ++at[side];
+        any = true;
+      }
+      if (at[1] >= from + 32) {
+        from += 32;
+        now = later;
+        later = places(from + 32);
+      }
+      if (any) {
+        moved = globaltimer_ns();
+      } else {
+        __nanosleep(40);
+        const bool late = globaltimer_ns() - moved > kWaitLimitNs;
+        if (__any_sync(0xffffffffu, late || *abort != 0)) {
+          if (lane == 0 && *abort == 0) {
+            *abort = 1;
+            report(a.status, kStatusTimeout);
+          }
+          ok = false;
         }
       }
     }
     // the copies issued last have landed before the kernel returns
-    for (int k = max(0, q - kPgrRaw); k < q; ++k) mbar_drain(&sh.raw_full[k % kPgrRaw], (k / kPgrRaw) & 1);
+    for (int side = 0; side < 2; ++side)
+      for (int k = max(0, at[side] - kPgrRaw); k < at[side]; ++k) mbar_drain(&sh.raw_full[side][k % kPgrRaw], (k / kPgrRaw) & 1);
   } else if (warp == 1) {
     // ---------------- MMAs ----------------
     griddep_wait();
@@ -291,28 +322,27 @@ __global__ void __launch_bounds__(kPgrThreads, 1) paged_attn_group_kernel(const 
       for (int t = 0; t < n; ++t) {
         bool here = true;
 #pragma unroll
-        for (int pg = 0; pg < 2; ++pg) here = here && quiet_wait(&sh.raw_full[(2 * t + pg) % kPgrRaw], ((2 * t + pg) / kPgrRaw) & 1, abort, a.status);
+        for (int pg = 0; pg < 2; ++pg) here = here && quiet_wait(&sh.raw_full[0][(2 * t + pg) % kPgrRaw], ((2 * t + pg) / kPgrRaw) & 1, abort, a.status);
         if (!__all_sync(0xffffffffu, here)) break;
         uint4 k[2][4];
-        uint2 kp[2], vp[2];
+        uint2 kp[2];
         bool bad[2];
 #pragma unroll
         for (int pg = 0; pg < 2; ++pg) {
           const int s = (2 * t + pg) % kPgrRaw;
-          const uint8_t* blk = raw + s * PgrBlock::kBytes;
-          bad[pg] = sh.bad_raw[s] != 0;
+          const uint8_t* blk = raw_k + s * kPgrRawK;
+          bad[pg] = sh.bad_raw[0][s] != 0;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) k[pg][i] = *reinterpret_cast<const uint4*>(blk + PgrBlock::kK + (x + 64 * i) * 16);
-          kp[pg] = *reinterpret_cast<const uint2*>(blk + PgrBlock::kKParams + 8 * x);
-          vp[pg] = *reinterpret_cast<const uint2*>(blk + PgrBlock::kVParams + 8 * x);
+          for (int i = 0; i < 4; ++i) k[pg][i] = *reinterpret_cast<const uint4*>(blk + (x + 64 * i) * 16);
+          kp[pg] = *reinterpret_cast<const uint2*>(blk + PgrBlock::kCodes + 8 * x);
+          const uint2 vp = *reinterpret_cast<const uint2*>(blk + PgrBlock::kCodes + PgrBlock::kParams + 8 * x);
+          kp[pg].x = (kp[pg].x & 0xffff7fffu) | (passes(vp.x) || passes(vp.y) ? 0x8000u : 0u);  // (scales are not negative)
         }
         if (!__all_sync(0xffffffffu, t < 2 || quiet_wait(&sh.k_free[t & 1], ((t >> 1) - 1) & 1, abort, a.status))) break;
         uint8_t* op = sk + (t & 1) * 2 * kPgrK;
 #pragma unroll
         for (int pg = 0; pg < 2; ++pg) {
-          const bool over = !bad[pg] && (passes(vp[pg].x) || passes(vp[pg].y));
           sh.par[t & 3][pg * 64 + place_of(x)] = bad[pg] ? make_uint2(0, 0) : kp[pg];
-          sh.vk[t & 3][pg * 64 + place_of(x)] = over ? 32.f : 1.f;
           if (x == 0) sh.bad[t & 3][pg] = bad[pg];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
@@ -330,8 +360,8 @@ __global__ void __launch_bounds__(kPgrThreads, 1) paged_attn_group_kernel(const 
         if (lane == 0) {
           mbar_arrive(&sh.par_full[t & 3]);
           mbar_arrive(&sh.k_full[t & 1]);
-          mbar_arrive(&sh.raw_free[(2 * t) % kPgrRaw]);
-          mbar_arrive(&sh.raw_free[(2 * t + 1) % kPgrRaw]);
+          mbar_arrive(&sh.raw_free[0][(2 * t) % kPgrRaw]);
+          mbar_arrive(&sh.raw_free[0][(2 * t + 1) % kPgrRaw]);
         }
       }
     } else {
@@ -341,17 +371,17 @@ __global__ void __launch_bounds__(kPgrThreads, 1) paged_attn_group_kernel(const 
                     m1024 = __half2half2(__ushort_as_half(0xe400));
       for (int q = 0; q < 2 * n; ++q) {
         const int rs = q % kPgrRaw, vs = q % kPgrVals;
-        if (!__all_sync(0xffffffffu, quiet_wait(&sh.raw_full[rs], (q / kPgrRaw) & 1, abort, a.status))) break;
-        const uint8_t* blk = raw + rs * PgrBlock::kBytes;
-        const bool bad = sh.bad_raw[rs] != 0;
+        if (!__all_sync(0xffffffffu, quiet_wait(&sh.raw_full[1][rs], (q / kPgrRaw) & 1, abort, a.status))) break;
+        const uint8_t* blk = raw_v + rs * kPgrRawV;
+        const bool bad = sh.bad_raw[1][rs] != 0;
         uint4 v[2];
         uint2 ev[4], od[4];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) v[i] = *reinterpret_cast<const uint4*>(blk + PgrBlock::kV + (half * 128 + (d0 / 4 + 8 * i) * 4 + t4) * 16);
+        for (int i = 0; i < 2; ++i) v[i] = *reinterpret_cast<const uint4*>(blk + (half * 128 + (d0 / 4 + 8 * i) * 4 + t4) * 16);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          ev[i] = *reinterpret_cast<const uint2*>(blk + PgrBlock::kVParams + 8 * (32 * half + 8 * i + 2 * t4));
-          od[i] = *reinterpret_cast<const uint2*>(blk + PgrBlock::kVParams + 8 * (32 * half + 8 * i + 2 * t4 + 1));
+          ev[i] = *reinterpret_cast<const uint2*>(blk + PgrBlock::kCodes + 8 * (32 * half + 8 * i + 2 * t4));
+          od[i] = *reinterpret_cast<const uint2*>(blk + PgrBlock::kCodes + 8 * (32 * half + 8 * i + 2 * t4 + 1));
         }
         __half2 s[4], z[4];
 #pragma unroll
@@ -383,7 +413,7 @@ __global__ void __launch_bounds__(kPgrThreads, 1) paged_attn_group_kernel(const 
         __syncwarp();
         if (lane == 0) {
           mbar_arrive(&sh.v_full[vs]);
-          mbar_arrive(&sh.raw_free[rs]);
+          mbar_arrive(&sh.raw_free[1][rs]);
         }
       }
     }
@@ -455,8 +485,8 @@ __global__ void __launch_bounds__(kPgrThreads, 1) paged_attn_group_kernel(const 
       tc_fence_after();
       const bool none = sh.bad[pb][qd >> 1] != 0;  // no such page
       const uint2 kp = sh.par[pb][key];
-      const float vk = sh.vk[pb][key];
-      const float2 sz0 = __half22float2(h2(kp.x)), sz1 = __half22float2(h2(kp.y));
+      const float vk = kp.x & 0x8000u ? 32.f : 1.f;  // what the key's weights are multiplied by for its values
+      const float2 sz0 = __half22float2(h2(kp.x & 0xffff7fffu)), sz1 = __half22float2(h2(kp.y));
       const f2_t ks0 = f2_pack(sz0.x, sz0.x), kz0 = f2_pack(sz0.y, sz0.y), ks1 = f2_pack(sz1.x, sz1.x), kz1 = f2_pack(sz1.y, sz1.y);
       // every eight rows' exponents e - ref to use(eight, four pairs)
       const auto each = [&](int when, auto use) {
