@@ -11,7 +11,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libtss.so")
 SOURCES = ("api.cu", "gemm.cu", "attention.cu", "attn_tc.cu", "attn_rows.cu", "misc.cu", "noalloc.cu", "prefill.cu", "verify_mk.cu", "rope.cu",
-           "paged.cu", "append_rope.cu", "paged_attn.cu", "paged_attn_tc.cu", "paged_attn_group.cu", "pages.cu", "beams.cu")
+           "paged.cu", "append_rope.cu", "paged_attn.cu", "paged_attn_tc.cu", "pages.cu", "beams.cu")
 HEADERS = ("common.cuh", "internal.h", "attn_body.cuh", "ops.cuh", "rope.cuh", "paged.h", "paged_quant.cuh", "paged_attn.cuh")
 ARCH = ("-gencode", "arch=compute_103a,code=sm_103a")
 FLAGS = ("-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr")

@@ -166,19 +166,6 @@ __device__ __forceinline__ bool mbar_try_wait(uint64_t* bar, uint32_t parity) {
   return ok != 0;
 }
 
-// Whether the phase with the given parity is complete, without waiting.
-__device__ __forceinline__ bool mbar_test(uint64_t* bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}\n"
-      : "=r"(ok)
-      : "r"(smem_u32(bar)), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
-
 // Bounded wait for the phase with the given parity.  On expiry (or if *abort is already set) it
 // raises *abort, records TIMEOUT and returns false.
 __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, volatile int* abort, int* status) {
@@ -367,6 +354,18 @@ __host__ __device__ constexpr uint32_t idesc_bf16_m128(int n) {
          | (1u << 10)                            // B format: bf16
          | (static_cast<uint32_t>(n >> 3) << 17)  // N >> 3
          | (static_cast<uint32_t>(128 >> 4) << 24);  // M >> 4
+}
+
+// One of the warp's threads.  Code behind this, unlike code behind a comparison of lane numbers, is known to be run by one thread:
+// descriptors stay in the registers that MMAs take them from.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "elect.sync _|p, 0xffffffff;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}\n"
+      : "=r"(r));
+  return r != 0;
 }
 
 __device__ __forceinline__ void umma_bf16(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc,

@@ -711,6 +711,16 @@ cudaError_t pa_pass(tss_paged* h, const PgAttnArgs& a, const PaTask* tasks, int 
                     bool shared, cudaStream_t s, bool* too_large) {
   PaTask few[kPgMaxReq], many[kPgMaxReq];
   int n_few = 0, n_many = 0, most = 0;
+  for (int i = 0; i < n_tasks; ++i) {
+    const PaTask& t = tasks[i];
+    if (t.rows == 0) continue;
+    if (h->d == 128 && t.rows > limit) {
+      many[n_many++] = t;
+    } else {
+      few[n_few++] = t;
+      most = t.rows > most ? t.rows : most;
+    }
+  }
   PaShared p, narrow;
   const auto begin = [&](PaShared& x) {
     x.a = a;
@@ -722,36 +732,6 @@ cudaError_t pa_pass(tss_paged* h, const PgAttnArgs& a, const PaTask* tasks, int 
     if (mem)
       for (int i = 0; i < kPgMaxReq; ++i) x.mem[i] = mem[i];
   };
-  // Shared keys that all rows see: groups of more than kPaGroup rows have a kernel of their own.
-  const bool group = shared && !a.own && h->d == 128 && !a.is_half && !a.window;
-  if (group) {
-    PaTask wide[kPgMaxReq];
-    int n_wide = 0, grid = 0;
-    for (int i = 0; i < n_tasks; ++i)
-      if (tasks[i].rows > kPaGroup) wide[n_wide++] = tasks[i];
-    if (n_wide) {
-      begin(p);
-      if (plan_paged_attention_group(p, wide, n_wide, h->sms, &grid)) {
-        if (grid) {
-          const cudaError_t e = launch_paged_attention_group(p, grid, s);
-          if (e != cudaSuccess) return e;
-        }
-      } else {
-        n_wide = 0;
-      }
-    }
-    if (n_wide) limit = 0;  // (marks them as done)
-  }
-  for (int i = 0; i < n_tasks; ++i) {
-    const PaTask& t = tasks[i];
-    if (t.rows == 0 || (limit == 0 && t.rows > kPaGroup)) continue;
-    if (h->d == 128 && limit && t.rows > limit) {
-      many[n_many++] = t;
-    } else {
-      few[n_few++] = t;
-      most = t.rows > most ? t.rows : most;
-    }
-  }
   if (n_many) {
     begin(p);
     if (!pa_plan(p, many, n_many, kPaTcTile, 2)) {
@@ -816,7 +796,6 @@ cudaError_t pa_prepare_all() {
   if (e == cudaSuccess) e = pa_prepare<128, 2, false>();
   if (e == cudaSuccess) e = pa_prepare<128, 2, true>();
   if (e == cudaSuccess) e = paged_attn_tc_prepare();
-  if (e == cudaSuccess) e = paged_attn_group_prepare();
   return e;
 }
 

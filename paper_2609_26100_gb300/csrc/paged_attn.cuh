@@ -71,11 +71,7 @@ __device__ __forceinline__ float ex2(float x) {
 // proportion to its 16-row tiles; us, warp-level / tcgen05, four requests of 4600 tokens and 32 heads: 24 rows 66 / 103,
 // 48 rows 97 / 110, 56 rows 119 / 111, 128 rows 225 / 123; 8 heads: 32 rows 28 / 40, 48 rows 33 / 42, 64 rows 41 / 42.
 constexpr int kPaTcRows = 48, kPaTcTile = 128;
-// (In the passes of the shared attention, which have fewer items: us of such a call, warp-level / tcgen05, 32 heads over 8192
-// shared keys, 64 rows 74 / 85, 80 rows 77 / 79, 96 rows 89 / 84; 8 heads over 32768, 64 rows 61 / 70, 96 rows 82 / 73.)
 constexpr int kPaTcShared = 80;
-// Rows of a KV head above which shared keys that all rows see go to paged_attn_group.cu.
-constexpr int kPaGroup = 8;
 cudaError_t paged_attn_tc_prepare();
 cudaError_t launch_paged_attention_tc(PaShared& p, bool shared, int sms, cudaStream_t s);
 
@@ -242,52 +238,6 @@ __device__ __forceinline__ void finish_row(const PaShared& p, const PaReq& r, in
 }
 
 // ------------------------------------------------------------------------------------------
-// What the tcgen05 kernels share
-// ------------------------------------------------------------------------------------------
-__host__ __device__ constexpr uint32_t idesc_f16_m128(int n) {
-  return (1u << 4) | (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(128 >> 4) << 24);
-}
-
-// mbar_wait, asleep between looks: sixteen warps that poll would take the issue slots of those that work.
-static __device__ __noinline__ bool quiet_wait_slow(uint64_t* bar, uint32_t parity, volatile int* abort, int* status) {
-  const uint64_t t0 = globaltimer_ns();
-  while (!mbar_try_wait_sleep(bar, parity, 20000)) {
-    if (*abort) return false;
-    if (globaltimer_ns() - t0 > kWaitLimitNs) {
-      *abort = 1;
-      report(status, kStatusTimeout);
-      return false;
-    }
-  }
-  return true;
-}
-__device__ __forceinline__ bool quiet_wait(uint64_t* bar, uint32_t parity, volatile int* abort, int* status) {
-  return mbar_try_wait(bar, parity) || quiet_wait_slow(bar, parity, abort, status);
-}
-
-// A word's eight codes as fp16 subnormals.
-__device__ __forceinline__ uint4 expand(uint32_t x) {
-  const uint32_t y = x >> 8;
-  return make_uint4(x & 0x000f000fu, x & 0x00f000f0u, y & 0x000f000fu, y & 0x00f000f0u);
-}
-
-__device__ __forceinline__ void tmem_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-
-// OR of v over the 128 threads of named barrier id.
-__device__ __forceinline__ bool quad_or(int id, bool v) {
-  uint32_t r;
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\t"
-      "setp.ne.u32 q, %1, 0;\n\t"
-      "bar.red.or.pred p, %2, 128, q;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}\n"
-      : "=r"(r)
-      : "r"(v ? 1u : 0u), "r"(id)
-      : "memory");
-  return r != 0;
-}
-
-// ------------------------------------------------------------------------------------------
 // Host: the plan of a launch
 // ------------------------------------------------------------------------------------------
 // What a launch has to do for a request: its rows over its keys [k0, k1) (k0 a multiple of a page).
@@ -354,12 +304,6 @@ inline int pa_each(PaParams& p) {
   }
   return grid;
 }
-
-// The kernel for many rows over shared keys (paged_attn_group.cu): plans the tasks for it (false where they do not fit; *grid 0: no
-// work) and launches.
-cudaError_t paged_attn_group_prepare();
-bool plan_paged_attention_group(PaShared& p, const PaTask* tasks, int n_tasks, int sms, int* grid);
-cudaError_t launch_paged_attention_group(const PaShared& p, int grid, cudaStream_t s);
 
 // Cuts the units into runs for at most `most` CTAs and returns their number: even runs, every item counting `lead`
 // units beside its own (for its start and end), or, where a CTA's run is then at most `slack` units longer, runs

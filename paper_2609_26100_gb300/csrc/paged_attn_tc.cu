@@ -72,6 +72,33 @@ static_assert(offsetof(PtShared, par) % 16 == 0 && offsetof(PtShared, row) % 16 
               "alignment of vectors and barriers");
 constexpr size_t kPtSmem = 1024 + 2 * kPtQ + 2 * 4 * kPtOp + kPtJoin * kPtRows * 4 + kPtRaw * PtBlock::kBytes;
 
+__host__ __device__ constexpr uint32_t idesc_f16_m128(int n) {
+  return (1u << 4) | (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(128 >> 4) << 24);
+}
+
+// mbar_wait, asleep between looks: sixteen warps that poll would take the issue slots of those that work.
+__device__ __noinline__ bool quiet_wait_slow(uint64_t* bar, uint32_t parity, volatile int* abort, int* status) {
+  const uint64_t t0 = globaltimer_ns();
+  while (!mbar_try_wait_sleep(bar, parity, 20000)) {
+    if (*abort) return false;
+    if (globaltimer_ns() - t0 > kWaitLimitNs) {
+      *abort = 1;
+      report(status, kStatusTimeout);
+      return false;
+    }
+  }
+  return true;
+}
+__device__ __forceinline__ bool quiet_wait(uint64_t* bar, uint32_t parity, volatile int* abort, int* status) {
+  return mbar_try_wait(bar, parity) || quiet_wait_slow(bar, parity, abort, status);
+}
+
+// A word's eight codes as fp16 subnormals.
+__device__ __forceinline__ uint4 expand(uint32_t x) {
+  const uint32_t y = x >> 8;
+  return make_uint4(x & 0x000f000fu, x & 0x00f000f0u, y & 0x000f000fu, y & 0x00f000f0u);
+}
+
 // 16 TMEM lanes (from taddr's) and 16 columns, left in flight (tmem_wait() before they are used): thread l has, in
 // r[4 b + 2 y + e], lane l / 4 + 8 y and column 8 b + 2 (l % 4) + e.
 __device__ __forceinline__ void tmem_ld_block(uint32_t taddr, uint32_t* r) {
@@ -84,6 +111,7 @@ __device__ __forceinline__ void tmem_st_block(uint32_t taddr, const uint32_t* r)
   asm volatile("tcgen05.st.sync.aligned.16x256b.x1.b32 [%0], {%1, %2, %3, %4};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3])
                : "memory");
 }
+__device__ __forceinline__ void tmem_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // umma_bf16 with its first operand in TMEM: 128 lanes, 8 columns of two 16-bit values.
@@ -94,6 +122,20 @@ __device__ __forceinline__ void umma_ta(uint32_t d_tmem, uint32_t a_tmem, uint64
       "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}\n" ::"r"(d_tmem),
       "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
       : "memory");
+}
+
+// OR of v over the 128 threads of named barrier id.
+__device__ __forceinline__ bool quad_or(int id, bool v) {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.u32 q, %1, 0;\n\t"
+      "bar.red.or.pred p, %2, 128, q;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}\n"
+      : "=r"(r)
+      : "r"(v ? 1u : 0u), "r"(id)
+      : "memory");
+  return r != 0;
 }
 
 // Keys of the tile from key0 that a row sees (position qp; lo, hi: the rows of its block that it sees).
@@ -299,7 +341,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
   } else if (warp == 1) {
     // ---------------- MMAs: S two pages ahead, then O += P C' ----------------
     ready();
-    if (lane == 0) {
+    if (elect_one()) {
       constexpr uint32_t id = idesc_f16_m128(64);
       const uint32_t q_a = smem_u32(sq), kv_a = smem_u32(skv);
       bool ok = true;
