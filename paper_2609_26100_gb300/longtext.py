@@ -1,6 +1,7 @@
 """Example: several continuations of one long prompt over a paged 4-bit KV cache.
 
     python -m paper_2609_26100_gb300.longtext [--prompt 3000] [--steps 6] [--hypotheses 4] [--layers 4]
+    python -m paper_2609_26100_gb300.longtext --beams 8 [--texts 2] [--prompt 3000] [--steps 6] [--layers 4]
 
 A stack of attention layers with random weights (head norms, rotary positions stretched for a long
 context, grouped heads; every second layer sees a window and the first tokens) decodes speculatively:
@@ -13,6 +14,11 @@ context, grouped heads; every second layer sees a window and the first tokens) d
   * every second step the worse half is dropped and forked from the better half; at the end the pool is
     made dense (tss_pages_compact).
 
+With --beams it searches instead: every text's beams share its prompt's pages; a step norms, rotates and appends in
+one launch (tss_paged_append_rope), attends with the shared keys read once (tss_paged_attention_shared), picks the
+best continuations over beams and vocabulary (tss_beam_select) and lets page rows follow their parents
+(tss_pages_reorder), all without a host wait.
+
 It checks the attention against a plain computation on the values read back (tss_paged_read) and prints the
 error and the time of a step.
 """
@@ -24,7 +30,7 @@ import time
 
 import torch
 
-from . import native, paged
+from . import beams, native, paged
 
 WINDOW, SINKS = 512, 4
 
@@ -46,22 +52,29 @@ class Stack:
         native.rope_table(freq, self.table, factor, native.current_stream())
         self.error = 0.0
 
-    def run(self, cache: paged.Kv4Cache, batch, x, positions, mask=None, check=None):
+    def run(self, cache: paged.Kv4Cache, batch, x, positions, mask=None, check=None, joined=False, groups=None):
         """Rows x of the batch's blocks through all layers, their keys and values appended on the way; the
-        outputs and each layer's rotated keys and values.  check: a request whose first layer is compared with
-        a plain computation."""
+        outputs and each layer's keys (rotated, unless joined) and values.  check: a request whose first layer is compared
+        with a plain computation; joined: rotated and appended in one launch; groups: requests that share pages."""
         kept = []
         for layer in range(self.layers):
             n = x.shape[0]
             rows = torch.nn.functional.linear(x / x.float().square().mean(-1, keepdim=True).sqrt().bfloat16(), self.wqkv[layer])
             rows = rows.view(n, self.hq + 2 * self.hk, self.d)
             q, k, v = rows[:, :self.hq], rows[:, self.hq:self.hq + self.hk], rows[:, self.hq + self.hk:]
-            native.qk_rope(native.rope_args(q, k, q, k, positions, self.table, q_gain=self.gains[layer][0],
-                                            k_gain=self.gains[layer][1]))
-            cache.append(layer, batch, k, v)
+            args = native.rope_args(q, k, q, None if joined else k, positions, self.table, q_gain=self.gains[layer][0],
+                                    k_gain=self.gains[layer][1], to_pages=joined)
+            if joined:
+                cache.append_rope(layer, batch, args, v)
+            else:
+                native.qk_rope(args)
+                cache.append(layer, batch, k, v)
             out = torch.empty(n, self.hq, self.d, dtype=x.dtype, device=x.device)
             near = {"window": WINDOW, "sinks": SINKS} if layer % 2 else {}
-            cache.attention(layer, batch, q, out, mask=mask, positions=positions, **near)
+            if groups is not None:
+                cache.attention_shared(layer, batch, groups, q, out, mask=mask, positions=positions, **near)
+            else:
+                cache.attention(layer, batch, q, out, mask=mask, positions=positions, **near)
             if check is not None and layer < 2:
                 self.compare(cache, layer, check, q, out, near)
             x = x + torch.nn.functional.linear(out.view(n, -1), self.wo[layer])
@@ -100,6 +113,88 @@ def mask_words(sets):
     return [[signed(s & (1 << 64) - 1), signed(s >> 64)] for s in sets]
 
 
+def search(a) -> dict:
+    """Beam search of a.texts texts, a.beams beams each; end token 0."""
+    texts, n, rows = a.texts, a.beams, a.texts * a.beams
+    prompts = [max(1, a.prompt - 100 * i) for i in range(texts)]
+    stack, pages = Stack(a.layers, 16, 4, 128, a.prompt + a.steps + 1, a.seed), paged.PAGE_TOKENS
+    # (while rows change places a text's beams hold at most what they held, and a tail and a new page each)
+    cache = paged.Kv4Cache.allocate(n_layers=a.layers, n_pages=sum(-(-p // pages) for p in prompts) + rows * (3 + a.steps // pages),
+                                    n_seqs=rows, max_pages=-(-(a.prompt + a.steps + 1) // pages) + 1, n_q_heads=16, n_kv_heads=4,
+                                    head_dim=128, shared_rows=rows)
+    g = torch.Generator(device="cuda").manual_seed(a.seed)
+    head, embed = ((torch.randn(a.vocab, stack.width, generator=g, device="cuda") * w).bfloat16() for w in (4 * stack.width ** -0.5, 1.0))
+    first, step_of = beams.BeamSelector(texts, a.vocab, n), beams.BeamSelector(rows, a.vocab, n)
+
+    def normal(x):
+        return x / x.float().square().mean(-1, keepdim=True).sqrt().bfloat16()
+
+    # the prompts, each in the row of its text's first beam
+    ends = []
+    for t, prompt in enumerate(prompts):
+        x = torch.randn(prompt, stack.width, generator=g, device="cuda").bfloat16()
+        cache.pages.reserve([t * n], [prompt])
+        for at in range(0, prompt, 128):
+            m = min(128, prompt - at)
+            positions = torch.arange(at, at + m, dtype=torch.int32, device="cuda")
+            check = (t * n, at, m, 0, [(2 << i) - 1 for i in range(m)], list(range(at, at + m)))
+            last, _ = stack.run(cache, cache.batch([t * n], [at], [m]), x[at:at + m], positions, check=check, joined=True)
+        ends.append(last[-1])
+        cache.pages.fork([t * n] * (n - 1), [t * n + i for i in range(1, n)], [prompt] * (n - 1))
+
+    def chosen(selector, logits, was, done, width):
+        """A step's choice, compared with a plain one of the same logits."""
+        out = torch.empty(texts, n, device="cuda"), *(torch.empty(texts, n, dtype=torch.int32, device="cuda") for _ in range(2))
+        selector.select(logits, was, *out, n_beams=width, done=done, end_token=0)
+        return out
+
+    def off(logits, was, done, width, score):
+        value = logits.double().log_softmax(-1)
+        if done is not None:  # (finished beams go on with the end token, at no cost)
+            value[done != 0] = -torch.inf
+            value[done != 0, 0] = 0.0
+        value = (value if was is None else value + was.double()[:, None]).view(texts, width * a.vocab)
+        return float((value.topk(n).values - score.double()).abs().max())
+
+    logits = torch.nn.functional.linear(normal(torch.stack(ends)), head)
+    score, _, token = chosen(first, logits, None, None, 1)
+    error, taken = off(logits, None, None, 1, score), 0.0
+    done = (token.view(-1) == 0).int()
+    parents, tokens, seqs = [], [token.view(-1)], list(range(rows))
+    for step in range(a.steps):
+        length = [p + step for p in prompts for _ in range(n)]
+        torch.cuda.synchronize()
+        began = time.perf_counter()
+        cache.pages.reserve(seqs, [c + 1 for c in length])
+        positions = torch.tensor(length, dtype=torch.int32, device="cuda")
+        check = (rows - 1, length[-1], 1, rows - 1, [1], [length[-1]]) if step % 2 else None
+        out, _ = stack.run(cache, cache.batch(seqs, length, [1] * rows), embed[tokens[-1].long()], positions, check=check, joined=True,
+                           groups=cache.groups([n] * texts, prompts))
+        logits, was, over = torch.nn.functional.linear(normal(out), head), score.view(-1), done
+        score, parent, token = chosen(step_of, logits, was, over, n)
+        cache.pages.reorder(seqs, parent.view(-1), [c + 1 for c in length])
+        parents.append(parent.view(-1))
+        tokens.append(token.view(-1))
+        done = done[parent.view(-1).long()] | (token.view(-1) == 0).int()
+        torch.cuda.synchronize()
+        taken += time.perf_counter() - began
+        error = max(error, off(logits, was, over, n, score))
+    held = int((cache.pages.refs > 0).sum())
+    for status in (cache.sync_status(), cache.pages.sync_status(), first.sync_status(), step_of.sync_status()):
+        native.check(status, "longtext")
+    # every beam's tokens, from its last one back
+    row, found = torch.arange(rows, device="cuda"), [tokens[-1]]
+    for parent, token in zip(reversed(parents), reversed(tokens[:-1])):
+        row = parent[row].long()
+        found.append(token[row])
+    found = torch.stack(found[::-1], 1).view(texts, n, -1).tolist()
+    full = sum(n * -(-(p + a.steps) // pages) for p in prompts)
+    print(f"{texts} x {n} beams, best {score[0, 0].item():.2f} with {found[0][0][:8]}, {held} pages ({full} unshared), "
+          f"{taken / max(a.steps, 1) * 1e3:.2f} ms a step, attention off by {stack.error:.1e}, values by {error:.1e}")
+    cache.close()
+    return {"error": stack.error, "held": held, "unshared": full, "values": error, "score": score.tolist(), "tokens": found}
+
+
 def main(argv=None) -> dict:
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     ap.add_argument("--prompt", type=int, default=3000)
@@ -108,7 +203,12 @@ def main(argv=None) -> dict:
     ap.add_argument("--layers", type=int, default=4)
     ap.add_argument("--nodes", type=int, default=12, help="rows of a draft tree, its root included")
     ap.add_argument("--seed", type=int, default=1)
+    ap.add_argument("--beams", type=int, default=0, help="beams of a text; 0: draft trees instead")
+    ap.add_argument("--texts", type=int, default=1, help="texts that are searched together")
+    ap.add_argument("--vocab", type=int, default=8000)
     a = ap.parse_args(argv)
+    if a.beams:
+        return search(a)
     rng = random.Random(a.seed)
     n, longest = a.hypotheses, a.prompt + a.steps * a.nodes + a.nodes
     stack = Stack(a.layers, 16, 4, 128, longest, a.seed)
