@@ -314,3 +314,12 @@ def test_refusals():
     # a request without rows does not bound the shared tokens
     c.attention_shared(0, c.batch([0, 1, 2], [130, 5, 64], [2, 0, 1]), c.groups(sizes, shared), q[:3], out[:3])
     assert c.sync_status() == native.TSS_OK
+
+
+def test_no_requests():
+    c, _, _ = shared_cache([1], [64], [64], [1], 2, 2, 128, seed=14)
+    q = torch.zeros(0, 2, 128, dtype=BF, device="cuda")
+    c.attention_shared(0, c.batch([], [], []), c.groups([], []), q, q.clone())
+    with pytest.raises(native.TssError):
+        c.attention_shared(0, c.batch([], [], []), c.groups([0], [0]), q, q.clone())
+    assert c.sync_status() == native.TSS_OK
