@@ -76,8 +76,9 @@ __device__ __forceinline__ void rope_run(const RopeParams& r, const PqUnit& u, T
   __syncwarp();
 }
 
+// (of 16-bit rows five CTAs an SM: 7171 rows of 32 heads 99 us, 109 with four, 106 with six, whose registers spill)
 template <typename T, int D, bool INTER>
-__global__ void __launch_bounds__(kPqThreads) append_rope_kernel(const __grid_constant__ ArParams a) {
+__global__ void __launch_bounds__(kPqThreads, sizeof(T) == 4 ? 4 : 5) append_rope_kernel(const __grid_constant__ ArParams a) {
   extern __shared__ __align__(16) uint8_t ar_dyn[];
   const int lane = threadIdx.x & 31;
   griddep_wait();

@@ -45,13 +45,14 @@ __device__ __forceinline__ int rope_position(const RopeParams& p, long long row)
 }
 
 // x rsqrt(mean(x^2) + eps) gain of the lane's elements; ss: the head's sum of squares.
+__device__ __forceinline__ float rope_scale(float ss, const RopeParams& p) { return 1.f / sqrtf(ss / static_cast<float>(p.d) + p.eps); }
 __device__ __forceinline__ void rope_norm(float* a, const float* g, float ss, const RopeParams& p) {
-  const float r = 1.f / sqrtf(ss / static_cast<float>(p.d) + p.eps);
+  const float r = rope_scale(ss, p);
 #pragma unroll
   for (int i = 0; i < 16; ++i) a[i] = a[i] * r * g[i];
 }
 
-// The rotation of the lane's eight pairs by their (cos, sin).
+// The rotation of the lane's eight pairs by their (cos, sin); the second products are rounded, the first are not.
 template <bool INTER>
 __device__ __forceinline__ void rope_turn(float* a, const float* cs) {
 #pragma unroll
@@ -59,8 +60,8 @@ __device__ __forceinline__ void rope_turn(float* a, const float* cs) {
     float& u = INTER ? a[2 * i] : a[i];
     float& v = INTER ? a[2 * i + 1] : a[8 + i];
     const float c = cs[2 * i], s = cs[2 * i + 1], u0 = u, v0 = v;
-    u = u0 * c - v0 * s;
-    v = v0 * c + u0 * s;
+    u = fmaf(u0, c, -__fmul_rn(v0, s));
+    v = fmaf(u0, s, __fmul_rn(v0, c));
   }
 }
 
