@@ -375,8 +375,8 @@ extern "C" tss_status tss_paged_attention_shared(tss_paged* h, const tss_paged_c
   const tss_status st = take_attention(h, cache, layer, batch, a, &p, &b, &rows);
   if (st != TSS_OK) return st;
   if (!groups) return refuse(TSS_ERR_INVALID_ARG, "NULL argument");
-  if (groups->n_groups < 0 || groups->n_groups > b.n_req || (groups->n_groups && (!groups->n_req || !groups->shared)))
-    return refuse(TSS_ERR_INVALID_ARG, "n_groups in [0, the batch's n_req], n_req and shared are wanted");
+  if (groups->n_groups < 1 || groups->n_groups > b.n_req || !groups->n_req || !groups->shared)
+    return refuse(TSS_ERR_INVALID_ARG, "n_groups in [1, the batch's n_req], n_req and shared are wanted");
   PgGroups g;
   g.n = groups->n_groups;
   int at = 0;

@@ -317,9 +317,9 @@ def test_refusals():
 
 
 def test_no_requests():
+    """Refused, as by the other calls on a batch."""
     c, _, _ = shared_cache([1], [64], [64], [1], 2, 2, 128, seed=14)
     q = torch.zeros(0, 2, 128, dtype=BF, device="cuda")
-    c.attention_shared(0, c.batch([], [], []), c.groups([], []), q, q.clone())
     with pytest.raises(native.TssError):
-        c.attention_shared(0, c.batch([], [], []), c.groups([0], [0]), q, q.clone())
+        c.attention_shared(0, c.batch([], [], []), c.groups([], []), q, q.clone())
     assert c.sync_status() == native.TSS_OK
