@@ -9,6 +9,12 @@
 // Warps that quantise K take a (request, 32-token half page, KV head) as in paged_quant.cuh: a lane rotates 16 elements of a
 // token, which lie where its pairs do, and leaves them in shared memory, from where the warp picks up 8 neighbouring dims a
 // lane to quantise.  Warps of V read the caller's rows, those after them rotate the rows' query heads.
+//
+// Bound: of few rows the launch and three dependent loads (position or page, table row, rows): 16 rows of 32 heads 4.3 us, where the
+// two calls are two launches.  Of many rows issue slots and latency, with 20 warps an SM: 7171 rows of 32 heads, bf16, 93 us (3.0
+// TB/s; the two calls 94), 72 of them for K and V, of which the pass through shared memory is 18 and norms and rotation 8.
+// Slower for the same rows: K's partners by shuffles in the lanes that quantise, without shared memory (156 us: 4 shuffles a vector and
+// norms taken twice), the next table row or two turns' rows in flight (registers: 103, 109).
 #include "paged_quant.cuh"
 #include "rope.cuh"
 
@@ -29,10 +35,10 @@ __device__ __forceinline__ void rope_run(const RopeParams& r, const PqUnit& u, T
   const int sub = lane / LANES, n = u.hi - u.lo;
   int my_pos = 0;
   if (r.rot > 0 && lane < n) my_pos = rope_position(r, u.row + lane);
-  float g[16];
+  Raw8<T> gain[2];
   if (r.k_gain) {
-    load_vec<T, 8>(static_cast<const T*>(r.k_gain) + at.c0, g);
-    load_vec<T, 8>(static_cast<const T*>(r.k_gain) + at.c1, g + 8);
+    gain[0].load(static_cast<const T*>(r.k_gain) + at.c0);
+    gain[1].load(static_cast<const T*>(r.k_gain) + at.c1);
   }
   const T* src = static_cast<const T*>(r.k) + u.row * r.ks + static_cast<long long>(u.head) * D;
   T* out = r.k_out ? static_cast<T*>(r.k_out) + u.row * r.kos + static_cast<long long>(u.head) * D : nullptr;
@@ -62,7 +68,11 @@ __device__ __forceinline__ void rope_run(const RopeParams& r, const PqUnit& u, T
       }
 #pragma unroll
       for (int o = LANES / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-      if (on) rope_norm(a, g, ss, r);
+      const float scale = rope_scale(ss, r);
+      float g[16];
+      gain[0].to(g);
+      gain[1].to(g + 8);
+      rope_norm(a, g, scale);
     }
     if (!on) continue;
     if (at.turns) rope_turn<INTER>(a, cs);
@@ -76,7 +86,7 @@ __device__ __forceinline__ void rope_run(const RopeParams& r, const PqUnit& u, T
   __syncwarp();
 }
 
-// (of 16-bit rows five CTAs an SM: 7171 rows of 32 heads 99 us, 109 with four, 106 with six, whose registers spill)
+// (of 16-bit rows five CTAs an SM: 7171 rows of 32 heads 93 us, with six 97, with seven 107: registers spill)
 template <typename T, int D, bool INTER>
 __global__ void __launch_bounds__(kPqThreads, sizeof(T) == 4 ? 4 : 5) append_rope_kernel(const __grid_constant__ ArParams a) {
   extern __shared__ __align__(16) uint8_t ar_dyn[];

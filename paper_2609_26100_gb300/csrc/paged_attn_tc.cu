@@ -341,7 +341,9 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
   } else if (warp == 1) {
     // ---------------- MMAs: S two pages ahead, then O += P C' ----------------
     ready();
-    if (elect_one()) {
+    // (issued behind elect.sync: 4 trees of 33 rows over a shared prefix 117 -> 108 us; not so in the kernel of single requests, where
+    // 4 trees of 61 rows took 74 us instead of 72)
+    if (SH ? elect_one() : lane == 0) {
       constexpr uint32_t id = idesc_f16_m128(64);
       const uint32_t q_a = smem_u32(sq), kv_a = smem_u32(skv);
       bool ok = true;

@@ -44,10 +44,9 @@ __device__ __forceinline__ int rope_position(const RopeParams& p, long long row)
   return pos < 0 ? 0 : p.max_pos - 1;
 }
 
-// x rsqrt(mean(x^2) + eps) gain of the lane's elements; ss: the head's sum of squares.
+// 1 / sqrt(mean(x^2) + eps) of a head whose sum of squares is ss, and x r gain of the lane's elements.
 __device__ __forceinline__ float rope_scale(float ss, const RopeParams& p) { return 1.f / sqrtf(ss / static_cast<float>(p.d) + p.eps); }
-__device__ __forceinline__ void rope_norm(float* a, const float* g, float ss, const RopeParams& p) {
-  const float r = rope_scale(ss, p);
+__device__ __forceinline__ void rope_norm(float* a, const float* g, float r) {
 #pragma unroll
   for (int i = 0; i < 16; ++i) a[i] = a[i] * r * g[i];
 }
@@ -109,10 +108,11 @@ __device__ __forceinline__ void rope_row(const RopeParams& p, long long w, int l
 #pragma unroll
       for (int o = LANES / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
       if (on && gain) {
+        const float r = rope_scale(ss, p);
         float g[16];
         load_vec<T, 8>(gain + c0, g);
         load_vec<T, 8>(gain + c1, g + 8);
-        rope_norm(a, g, ss, p);
+        rope_norm(a, g, r);
       }
     }
     if (!on) continue;
