@@ -573,8 +573,8 @@ __global__ void __launch_bounds__(WARPS * 32, PaShape<D, NT, WARPS>::kCtas)
       fence_async_smem();  // (the next segment's first copy goes to this stage: stores before the async proxy's)
     }
     __syncthreads();
-    wait_for_shared(p);
     const bool whole = x0 == 0 && x1 == r.units;
+    if (whole) wait_for_shared(p);  // (else the join does)
     int c0 = first_cta, c1 = first_cta + splits - 1;  // CTAs that share the item
     if (!whole && !p.aligned) {
       c0 = cta_of_unit(p, b, u - x0);
@@ -633,6 +633,7 @@ __global__ void __launch_bounds__(WARPS * 32, PaShape<D, NT, WARPS>::kCtas)
           float4 sum;
           gather_partials<D>(p, R, c0, c1, row, slice, per_row, &M, &L, &sum);
           if (per_row == 1) {
+            wait_for_shared(p);
             if (lane < D / 4) finish(row, lane, M, L, sum);
           } else {
             const int at = slice * rows + row;  // (at most W)
@@ -642,6 +643,7 @@ __global__ void __launch_bounds__(WARPS * 32, PaShape<D, NT, WARPS>::kCtas)
         }
         __syncthreads();
         if (per_row > 1) {
+          wait_for_shared(p);
           for (int x = tid; x < rows * (D / 4); x += W * 32) {
             const int row = x / (D / 4), c4 = x % (D / 4);
             float M = -INFINITY, L = 0.f;

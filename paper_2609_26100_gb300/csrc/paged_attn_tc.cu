@@ -220,6 +220,7 @@ __device__ __forceinline__ void join_parts(const P& p, PtShared& sh, uint8_t* sq
       o[i].w = fmaf(w, y[i].w, o[i].w);
     }
   }
+  wait_for_shared(p);
 #pragma unroll
   for (int i = 0; i < kRowsOf; ++i) {
     const int q = sw + i * kPtSoftWarps;
@@ -801,11 +802,11 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
         if (lane == 0) mbar_arrive(&sh.p_full[sb]);  // (of a quadrant without rows: the arrival alone)
       }
       // ---- the segment's end: 32 dims a thread ----
-      wait_for_shared(p);
       ok = ok && quiet_wait(&sh.o_full, seg & 1, abort, a.status);
       __syncwarp();
       tc_fence_after();
       const bool whole = x0 == 0 && len == r.units;
+      if (whole) wait_for_shared(p);  // (else the join does)
       int c0 = first_cta, c1 = first_cta + splits - 1;
       if (!whole && !p.aligned) {
         c0 = cta_of_unit(p, rb, u0 + t - x0);
@@ -926,8 +927,8 @@ __global__ void __launch_bounds__(kPtThreads, 1) paged_attn_tc_kernel(const __gr
       t += len;
     }
   }
+  __syncwarp();  // (lanes that wait for the other kernel would keep the one that issues MMAs from running)
   wait_for_shared(p);  // (the kernel ends no earlier than the one before it)
-  __syncwarp();
   tc_fence_before();
   __syncthreads();
   if (warp == 1) {
