@@ -10,7 +10,7 @@
 // token, which lie where its pairs do, and leaves them in shared memory, from where the warp picks up 8 neighbouring dims a
 // lane to quantise.  Warps of V read the caller's rows, those after them rotate the rows' query heads.
 //
-// Bound: of few rows the launch and three dependent loads (position or page, table row, rows): 16 rows of 32 heads 4.3 us, where the
+// Bound: of few rows the launch and three dependent loads (position or page, table row, rows): 16 rows of 32 heads 5.7 us cold, where the
 // two calls are two launches.  Of many rows issue slots and latency, with 20 warps an SM: 7171 rows of 32 heads, bf16, 93 us (3.0
 // TB/s; the two calls 94), 72 of them for K and V, of which the pass through shared memory is 18 and norms and rotation 8.
 // Slower for the same rows: K's partners by shuffles in the lanes that quantise, without shared memory (156 us: 4 shuffles a vector and

@@ -2,10 +2,16 @@
 //
 //   value(b, t) = score_b + x_bt - ln sum_u exp x_bu,  largest first, ties to the lowest b vocab + t
 //
-// One pass over the logits.  A CTA holds a chunk of a row in registers.  At least n_keep of its elements reach the least of its
-// warps' ceil(n_keep / 8)-th largest thread maxima, and few more do: those are ranked by (value, index).  With them goes the
-// chunk's sum of exponentials.  The last CTA of a group to arrive joins the rows' sums and picks from the chunks' sorted lists in
-// the same way: a bound from one entry of each list, then what reaches it.
+// One pass over the logits.  A CTA takes a chunk of a row in tiles, the next one on its way while one is worked on.  A thread's part of
+// a tile is a group, which leaves its largest element and its sum of exponentials.  At least n_keep elements reach the n_keep-th largest
+// of the threads' largest (of up to 8: the least of the warps'): groups that reach it, few, are looked at again, an element a lane, and
+// what reaches it is ranked by (value, index).  The last CTA of a group of beams to arrive joins the rows' sums and picks from the
+// chunks' sorted lists in the same way: a bound from one entry of each list, then what reaches it.
+//
+// Bound: of large calls the exponentials, 16 a cycle and SM (the reading goes at 7.9 TB/s meanwhile), then the chunks' ends; 512 rows of
+// 131072, bf16, 32 kept, 59.5 us in two waves, each 10 us of reading and 8 of its end (the bound 2.2, the groups' sums 1.5, the second
+// look 3.2, the order 1.2), the last joins 14.  Of small ones chains of barriers: 4 rows of 32000 12.5 us (a chunk 4, the join 8), 64 of
+// 50021, fp32, 20.5.
 //
 // Between rows the order goes by the last bits of the rows' sums.  Terms are 2^((x - m) log2e + f), m the chunk's largest logit,
 // log2e in two parts, f what its product with m leaves of a whole number, so that chunks' sums differ by powers of two.  The
