@@ -8,10 +8,10 @@
 // what reaches it is ranked by (value, index).  The last CTA of a group of beams to arrive joins the rows' sums and picks from the
 // chunks' sorted lists in the same way: a bound from one entry of each list, then what reaches it.
 //
-// Bound: of large calls the exponentials, 16 a cycle and SM (the reading goes at 7.9 TB/s meanwhile), then the chunks' ends; 512 rows of
-// 131072, bf16, 32 kept, 59.5 us in two waves, each 10 us of reading and 8 of its end (the bound 2.2, the groups' sums 1.5, the second
-// look 3.2, the order 1.2), the last joins 14.  Of small ones chains of barriers: 4 rows of 32000 12.5 us (a chunk 4, the join 8), 64 of
-// 50021, fp32, 20.5.
+// Bound: of large calls the exponentials, 16 a cycle and SM, and the reading (5 TB/s while four CTAs of an SM read), then the chunks' ends;
+// 512 rows of 131072, bf16, 32 kept, 51 us in one wave of chunks of 16 tiles: 19 to 25 us of reading, 10 of a chunk's end (the bound
+// 2.3, the groups' sums 2.3, the second look 4.3, the order 1.1), the last joins 13; in two waves of half as long chunks 59.5.  Of small
+// ones chains of barriers: 4 rows of 32000 12.4 us (a chunk 4, the join 8), 64 of 50021, fp32, 19.6.
 //
 // Between rows the order goes by the last bits of the rows' sums.  Terms are 2^((x - m) log2e + f), m the chunk's largest logit,
 // log2e in two parts, f what its product with m leaves of a whole number, so that chunks' sums differ by powers of two.  The
@@ -34,7 +34,7 @@ namespace {
 
 constexpr int kBmThreads = 256, kBmWarps = kBmThreads / 32;
 constexpr int kBmKeep = 128, kBmBeams = 64;
-constexpr int kBmPool = 2048;     // candidates that are held at once: at least 1024 beside 512
+constexpr int kBmPool = 2048, kBmPoolOf = 1024;  // candidates that are held at once, by the join and by a chunk
 constexpr float kBmMost = 1e38f;  // logits from here on count as infinite, those from minus that on down as masked
 
 struct BmParams {
@@ -65,23 +65,24 @@ __device__ __forceinline__ unsigned long long order_of(double x) {
 __device__ __forceinline__ double double_of(unsigned long long o) {
   return __longlong_as_double(static_cast<long long>(o >> 63 ? o & 0x7fffffffffffffffull : ~o));
 }
-// A CTA's dynamic shared memory: candidates (value, index); of a chunk's groups the largest element, the sum, and those that are
-// looked at again.
-constexpr int kBmTiles = 8, kBmGroups = kBmTiles * kBmThreads;
+// A CTA's dynamic shared memory: candidates (value, index); of a chunk's groups the largest element and the sum, in whose place comes
+// the list of those that are looked at again.
+constexpr int kBmTiles = 16, kBmGroups = kBmTiles * kBmThreads;
 struct BmSpace {
   unsigned long long* val;
   uint32_t* idx;
   float *most, *sum;
   uint16_t* group;
-  static constexpr int kBytes = kBmPool * 12 + kBmGroups * 10;
-  __device__ __forceinline__ explicit BmSpace(uint8_t* at) {
+  static constexpr int kBytes = kBmPoolOf * 12 + kBmGroups * 8;
+  __device__ __forceinline__ BmSpace(uint8_t* at, int pool) {
     val = reinterpret_cast<unsigned long long*>(at);
-    idx = reinterpret_cast<uint32_t*>(val + kBmPool);
-    most = reinterpret_cast<float*>(idx + kBmPool);
+    idx = reinterpret_cast<uint32_t*>(val + pool);
+    most = reinterpret_cast<float*>(idx + pool);
     sum = most + kBmGroups;
-    group = reinterpret_cast<uint16_t*>(sum + kBmGroups);
+    group = reinterpret_cast<uint16_t*>(sum);
   }
 };
+static_assert(kBmPool * 12 <= BmSpace::kBytes && kBmGroups <= 65536 && kBmTiles <= 32, "room for the join's, groups' numbers and a thread's mask");
 
 // (value, index): larger values first, then lower indices
 __device__ __forceinline__ bool ahead(unsigned long long a, uint32_t ai, unsigned long long b, uint32_t bi) { return a > b || (a == b && ai < bi); }
@@ -365,12 +366,13 @@ __device__ __forceinline__ void bm_chunk(const BmParams& p, BmShared& sh, const 
   const BmBase base(m);
   long long sum = 0;
   float others = 0.f;
+  uint32_t again = 0;
   for (int t = 0; t < tiles; ++t) {
     const int id = t * kBmThreads + tid;
     const float g = sp.most[id];
     if (!(g > -kBmMost)) continue;
     if (g >= least)
-      sp.group[atomicAdd(&sh.groups, 1)] = static_cast<uint16_t>(id);
+      again |= 1u << t;
     else if (fabsf(g) < 1e6f && fabsf(m) < 1e6f)
       others = fmaf(sp.sum[id], bm_ex2(rintf(g * kLog2eHi) - base.hi), others);  // (a power of two)
     else
@@ -378,10 +380,12 @@ __device__ __forceinline__ void bm_chunk(const BmParams& p, BmShared& sh, const 
   }
   sum += bm_fixed(others);
   __syncthreads();
+  for (; again; again &= again - 1) sp.group[atomicAdd(&sh.groups, 1)] = static_cast<uint16_t>((__ffs(again) - 1) * kBmThreads + tid);
+  __syncthreads();
   const int groups = sh.groups;
   // An element a lane: its term, and itself into the pool if it reaches the bound; where the pool could overflow it is cut to the
   // n_keep best, and others have to come before the last of them.
-  constexpr int kAt = kBmThreads / EPT, kRound = 4, kFlight = 8;  // groups of a pass; passes of a round, and whose loads are in flight
+  constexpr int kAt = kBmThreads / EPT, kRound = 2, kFlight = 8;  // groups of a pass; passes of a round, and whose loads are in flight
   unsigned long long cv = 0;
   uint32_t cx = 0;
   int n = 0;
@@ -417,7 +421,7 @@ __device__ __forceinline__ void bm_chunk(const BmParams& p, BmShared& sh, const 
       n = sh.n;
       if (g0 + kAt * (r + kRound) >= groups) break;
       __syncthreads();
-      if (n > kBmPool / 4) {
+      if (n > kBmPoolOf / 4) {
         n = cut(sp.val, sp.idx, n, p.keep, &sh.n, ahead);
         if (n == p.keep) {
           cv = sp.val[n - 1];
@@ -643,21 +647,20 @@ template <typename T, int EPT>
 __global__ void __launch_bounds__(kBmThreads, kBmCtas) beam_kernel(const __grid_constant__ BmParams p) {
   extern __shared__ __align__(16) uint8_t bm_dyn[];
   __shared__ BmShared sh;
-  const BmSpace sp(bm_dyn);
   const int tid = threadIdx.x;
   const long long row = blockIdx.x / p.chunks;
   const int chunk = static_cast<int>(blockIdx.x - row * p.chunks), group = static_cast<int>(row / p.beams);
   griddep_wait();
   griddep_launch();
   const float s = p.score ? __ldcg(p.score + row) : 0.f;
-  if (s > -INFINITY && s < INFINITY && !(p.done && __ldcg(p.done + row))) bm_chunk<T, EPT>(p, sh, sp, row, chunk);
+  if (s > -INFINITY && s < INFINITY && !(p.done && __ldcg(p.done + row))) bm_chunk<T, EPT>(p, sh, BmSpace(bm_dyn, kBmPoolOf), row, chunk);
   __syncthreads();
   if (tid == 0) {
     sh.last = atom_add_acq_rel_gpu(&p.counters[group], 1) == p.beams * p.chunks - 1;
     if (sh.last) atomicExch(&p.counters[group], 0);
   }
   __syncthreads();
-  if (sh.last) bm_join(p, sh, sp, group);
+  if (sh.last) bm_join(p, sh, BmSpace(bm_dyn, kBmPool), group);
 }
 
 
@@ -763,7 +766,7 @@ extern "C" tss_status tss_beam_select(tss_beam* h, const tss_beam_args* a, void*
   p.part = h->part;
   p.sums = h->sums;
   p.status = h->status;
-  // Chunks of a tile of 2048 elements where that makes two CTAs an SM at most.  Else of 1 to 8 tiles of 16 KiB: a CTA takes about
+  // Chunks of a tile of 2048 elements where that makes two CTAs an SM at most.  Else of 1 to 16 tiles of 16 KiB: a CTA takes about
   // 1.2 us a tile, 3 us more and as many again for 32 kept, and an SM holds kBmCtas.
   int len = kBmSmall * kBmThreads;
   const bool small = rows * chunks_of(h->vocab, len) <= 2LL * h->sms;
