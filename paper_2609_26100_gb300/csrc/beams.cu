@@ -8,8 +8,8 @@
 // what reaches it is ranked by (value, index).  The last CTA of a group of beams to arrive joins the rows' sums and picks from the
 // chunks' sorted lists in the same way: a bound from one entry of each list, then what reaches it.
 //
-// Bound: of large calls the exponentials, 16 a cycle and SM, and the reading (5 TB/s while four CTAs of an SM read), then the chunks' ends;
-// 512 rows of 131072, bf16, 32 kept, 51 us in one wave of chunks of 16 tiles: 19 to 25 us of reading, 10 of a chunk's end (the bound
+// Bound: of large calls HBM while the CTAs read (6.5 TB/s until those of SMs with three are through; the exponentials take 11 of the 16
+// places a cycle and SM), then the chunks' ends; 512 rows of 131072, bf16, 32 kept, 51 us in one wave of chunks of 16 tiles: 19 to 25 us of reading, 10 of a chunk's end (the bound
 // 2.3, the groups' sums 2.3, the second look 4.3, the order 1.1), the last joins 13; in two waves of half as long chunks 59.5.  Of small
 // ones chains of barriers: 4 rows of 32000 12.4 us (a chunk 4, the join 8), 64 of 50021, fp32, 19.6.
 //
