@@ -222,6 +222,16 @@ def test_scores_that_rise_page_by_page():
         run_and_check(c, k, v, [2], [2048], first, n, scale=0.5)
 
 
+@pytest.mark.parametrize("d,n,dtype", [(128, 1, BF), (64, 1, HF), (64, 9, HF), (128, 9, BF)])
+@pytest.mark.parametrize("window", [0, 130])
+def test_more_items_of_own_keys_than_warps(d, n, dtype, window):
+    """64 requests of 32 heads: more items of few keys than warps that run at a time."""
+    rng = random.Random(d + n)
+    first = [64 + rng.randrange(260) for _ in range(64)]
+    c, k, v = shared_cache([64], [64], first, [n] * 64, 32, 32, d, seed=15)
+    run_and_check(c, k, v, [64], [64], first, [n] * 64, dtype=dtype, window=window, sinks=3 if window else 0)
+
+
 def test_as_the_attention_of_each():
     """The same as tss_paged_attention, up to the weights' bits and the order of sums; and twice the same bits."""
     sizes, shared, n = [12, 5], [1500, 777], [1] * 17
