@@ -11,8 +11,8 @@
 // lane to quantise.  Warps of V read the caller's rows, those after them rotate the rows' query heads.
 //
 // Bound: of few rows the launch and three dependent loads (position or page, table row, rows): 16 rows of 32 heads 5.7 us cold, where the
-// two calls are two launches.  Of many rows issue slots and latency, with 20 warps an SM: 7171 rows of 32 heads, bf16, 93 us (3.0
-// TB/s; the two calls 94), 72 of them for K and V, of which the pass through shared memory is 18 and norms and rotation 8.
+// two calls are two launches.  Of many rows issue slots and latency, with 20 warps an SM: 7171 rows of 32 heads, bf16, 89 us (3.0
+// TB/s; the two calls 94), 68 of them for K and V (46 where neither is rotated by the call).
 // Slower for the same rows: K's partners by shuffles in the lanes that quantise, without shared memory (156 us: 4 shuffles a vector and
 // norms taken twice), the next table row or two turns' rows in flight (registers: 103, 109).
 #include "paged_quant.cuh"
@@ -86,8 +86,93 @@ __device__ __forceinline__ void rope_run(const RopeParams& r, const PqUnit& u, T
   __syncwarp();
 }
 
-// (of 16-bit rows five CTAs an SM: 7171 rows of 32 heads 93 us, with six 97, with seven 107: registers spill)
-template <typename T, int D, bool INTER>
+// Heads of 128 that turn as a whole, in the half layout: a lane's two vectors of a token are of one group of 64 dims each, 8 lanes a
+// token, as the codes want them (scale_of: of two tokens at a time, both groups), so that nothing goes through shared memory (K and V of 7171 rows
+// of 32 heads 68 us, 72 through it).
+template <typename T>
+__device__ __forceinline__ void rope_and_quantise(const PqParams& p, const RopeParams& r, PqUnit& u, int lane) {
+  constexpr int D = 128;
+  using B = PgBlock<D>;
+  const RopeLane<8, false> at(r, lane);
+  const int sub = lane >> 3, n = u.hi - u.lo;
+  const T* src = static_cast<const T*>(r.k) + u.row * r.ks + static_cast<long long>(u.head) * D;
+  T* out = r.k_out ? static_cast<T*>(r.k_out) + u.row * r.kos + static_cast<long long>(u.head) * D : nullptr;
+  Raw8<T> next[2][2], gain[2];
+  const auto fetch = [&](int i, int tok) {
+    if (tok < n) {
+      next[i][0].load(src + tok * r.ks + at.c0);
+      next[i][1].load(src + tok * r.ks + at.c1);
+    }
+  };
+  fetch(0, sub);
+  fetch(1, sub + 4);
+  const int my_pos = lane < n ? rope_position(r, u.row + lane) : 0;
+  if (r.k_gain) {
+    gain[0].load(static_cast<const T*>(r.k_gain) + at.c0);
+    gain[1].load(static_cast<const T*>(r.k_gain) + at.c1);
+  }
+  pq_resolve(p, B::kBytes, lane, &u);
+  if (!u.block && !out) return;
+  const int tok0 = u.tok0 + u.lo;
+  __half2* params = reinterpret_cast<__half2*>(u.block + B::kKParams) + tok0 * B::kGroups;
+  uint8_t* krow = u.block + B::kK + tok0 * (D / 2) + PqLane<D>(at.j).k_at;
+#pragma unroll 1
+  for (int t0 = 0; t0 < n; t0 += 8) {
+    Raw8<T> now[4];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int tok = t0 + 4 * i + sub;
+      const bool on = tok < n;
+      const int pos = __shfl_sync(0xffffffffu, my_pos, tok & 31);
+      float cs[16], x[16];
+      if (on) load_vec<float, 16>(r.table + static_cast<size_t>(pos) * D + 16 * at.j, cs);
+      next[i][0].to(x);
+      next[i][1].to(x + 8);
+      fetch(i, tok + 8);
+      if (r.k_gain) {
+        float ss = 0.f;
+        if (on) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) ss = fmaf(x[e], x[e], ss);
+        }
+#pragma unroll
+        for (int o = 4; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+        const float scale = rope_scale(ss, r);
+        float g[16];
+        gain[0].to(g);
+        gain[1].to(g + 8);
+        rope_norm(x, g, scale);
+      }
+      now[2 * i].clear();
+      now[2 * i + 1].clear();
+      if (!on) continue;
+      rope_turn<false>(x, cs);
+      store_vec<T, 8>(reinterpret_cast<T*>(now[2 * i].v), x);
+      store_vec<T, 8>(reinterpret_cast<T*>(now[2 * i + 1].v), x + 8);
+      if (out) {
+        *reinterpret_cast<uint4*>(out + tok * r.kos + at.c0) = now[2 * i].v[0];
+        *reinterpret_cast<uint4*>(out + tok * r.kos + at.c1) = now[2 * i + 1].v[0];
+      }
+    }
+    if (!u.block) continue;
+    bool inside;
+    const __half2 scales = scale_of(now, lane, &inside);
+    inside = __all_sync(0xffffffffu, inside);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int tok = t0 + 4 * (k >> 1) + sub;
+      const __half2 sz = __shfl_sync(0xffffffffu, scales, (lane & 24) | k);
+      const uint32_t w = codes_of(now[k], sz, inside);
+      if (tok >= n) continue;
+      if (at.j == 0) params[tok * B::kGroups + (k & 1)] = sz;
+      *reinterpret_cast<uint32_t*>(krow + tok * (D / 2) + (k & 1) * 8) = w;
+    }
+  }
+}
+
+// WHOLE: K by rope_and_quantise.  (Of 16-bit rows five CTAs an SM: 7171 rows of 32 heads through shared memory 93 us, with six 97, with
+// seven 107: registers spill.)
+template <typename T, int D, bool INTER, bool WHOLE>
 __global__ void __launch_bounds__(kPqThreads, sizeof(T) == 4 ? 4 : 5) append_rope_kernel(const __grid_constant__ ArParams a) {
   extern __shared__ __align__(16) uint8_t ar_dyn[];
   const int lane = threadIdx.x & 31;
@@ -102,6 +187,8 @@ __global__ void __launch_bounds__(kPqThreads, sizeof(T) == 4 ? 4 : 5) append_rop
   if (!pq_unit(a.p, w, lane, &u)) return;
   if (u.side) {
     quantise_run<T, D>(a.p, u, static_cast<const T*>(a.p.v) + u.row * a.p.vs + u.head * D, a.p.vs, lane);
+  } else if constexpr (WHOLE) {
+    rope_and_quantise<T>(a.p, a.r, u, lane);
   } else {
     T* tile = reinterpret_cast<T*>(ar_dyn) + (threadIdx.x >> 5) * (32 * D);
     rope_run<T, D, INTER>(a.r, u, tile, lane);
@@ -113,8 +200,10 @@ constexpr int ar_smem(int bytes, int d) { return kPqThreads / 32 * 32 * d * byte
 
 template <typename T, int D>
 cudaError_t ar_launch(const ArParams& a, bool inter, unsigned grid, cudaStream_t s) {
-  return launch_k(inter ? append_rope_kernel<T, D, true> : append_rope_kernel<T, D, false>, dim3(grid), dim3(kPqThreads), ar_smem(sizeof(T), D), s,
-                  true, a);
+  if constexpr (sizeof(T) == 2 && D == 128)
+    if (!inter && a.r.rot == D) return launch_k(append_rope_kernel<T, D, false, true>, dim3(grid), dim3(kPqThreads), 0, s, true, a);
+  return launch_k(inter ? append_rope_kernel<T, D, true, false> : append_rope_kernel<T, D, false, false>, dim3(grid), dim3(kPqThreads),
+                  ar_smem(sizeof(T), D), s, true, a);
 }
 template <typename T>
 cudaError_t ar_dispatch(const ArParams& a, bool inter, int d, unsigned grid, cudaStream_t s) {
@@ -126,8 +215,8 @@ cudaError_t ar_dispatch(const ArParams& a, bool inter, int d, unsigned grid, cud
 // (of fp32 rows of 128 dims the tiles pass the 48 KiB that need no asking)
 cudaError_t append_rope_prepare() {
   const int bytes = ar_smem(4, 128);
-  const cudaError_t e = cudaFuncSetAttribute(append_rope_kernel<float, 128, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-  return e == cudaSuccess ? cudaFuncSetAttribute(append_rope_kernel<float, 128, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) : e;
+  const cudaError_t e = cudaFuncSetAttribute(append_rope_kernel<float, 128, false, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  return e == cudaSuccess ? cudaFuncSetAttribute(append_rope_kernel<float, 128, true, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) : e;
 }
 
 }  // namespace tss
