@@ -203,3 +203,40 @@ def test_refusals():
     none = native.rope_args(q[:0], k[:0], qo[:0], None, pos[:0], t, to_pages=True)
     cache.append_rope(0, cache.batch([0], [0], [0]), none, v[:0])    # no rows: nothing to do
     assert torch.equal(cache.pool, before)
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("norm", [False, True])
+@pytest.mark.parametrize("way", ["no k_out", "k_out", "in place"])
+def test_heads_that_turn_as_a_whole(dtype, norm, way):
+    """128 dims, half layout, 16 bits, with runs that begin and end anywhere in a half page, values of all sizes, NaN and infinities."""
+    first, n = (5, 63, 31, 40, 96, 0), (3, 2, 70, 33, 1, 32)
+    lens, rows, hq, hk, d = [f + m for f, m in zip(first, n)], sum(n), 6, 3, 128
+    one, two = (make(lens, hq, hk, d) for _ in range(2))
+    q, k, v = (x.clone() for x in rows_of(rows, hq, hk, d, dtype, 12))
+    k[7, 1] *= 1e-6
+    k[9, 0] *= 500.0
+    k[11, 2] = 0.0
+    k[20, 1, 77], k[21, 2, 3] = float("nan"), float("inf")
+    qg, kg = gains(d, dtype, 12) if norm else (None, None)
+    t = table_of(128, 200)
+    pos = torch.cat([torch.arange(f, f + m, device="cuda") for f, m in zip(first, n)]).to(torch.int32)
+    qr, kr = torch.empty_like(q), torch.empty_like(k)
+    native.qk_rope(native.rope_args(q, k, qr, kr, pos, t, q_gain=qg, k_gain=kg))
+    batch = one.batch(range(6), first, n)
+    two.append(0, batch, kr, v)
+    qo = torch.empty_like(q)
+    ko = {"no k_out": None, "k_out": torch.empty_like(k), "in place": k}[way]
+    one.append_rope(0, batch, native.rope_args(q, k, qo, ko, pos, t, q_gain=qg, k_gain=kg, to_pages=True), v)
+    assert one.sync_status() == native.TSS_OK and two.sync_status() == native.TSS_OK
+    assert torch.equal(one.pool, two.pool) and torch.equal(qo, qr)
+    if ko is not None:
+        assert torch.equal(ko.view(torch.int16), kr.view(torch.int16))
+    # without their pages the rows still reach q_out and k_out
+    if way == "k_out":
+        one.table[2, 0], one.table[3, 1] = -1, 10 ** 6
+        before = one.pool.clone()
+        ko.zero_()
+        one.append_rope(0, batch, native.rope_args(q, k, qo, ko, pos, t, q_gain=qg, k_gain=kg, to_pages=True), v)
+        assert one.sync_status() == native.TSS_ERR_DEVICE_CHECK
+        assert torch.equal(one.pool, before) and torch.equal(ko.view(torch.int16), kr.view(torch.int16))
