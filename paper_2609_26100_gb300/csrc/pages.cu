@@ -8,8 +8,8 @@
 //
 // Bounds: the choosing launch is latency (one CTA, one read of the counts up to the last page taken): twelve sequences
 // freed and forked again with a tail page in 8 layers each, 9 us in all.  The copies are HBM, each byte read and written
-// once: 900 pages of 128 KB moved in each of 2 layers (472 MB) in 81 us, 5.8 TB/s.  A reorder of 64 beams over 32 layers: the choice 11 us
-// (parents read, takers and free pages found), rows and copies of 60 tails a layer 22 us, 3.2 TB/s of DRAM; of 8 beams over 8 layers 10 us in all.
+// once: 900 pages of 128 KB moved in each of 2 layers (472 MB) in 81 us, 5.8 TB/s.  A reorder of 64 beams over 32 layers: the choice 10 us
+// (parents read, takers and free pages found), rows and copies of 60 tails a layer 20 us; of 8 beams over 8 layers 9 us in all.
 #include "ops.cuh"
 
 struct tss_pages {
@@ -274,21 +274,15 @@ __global__ void __launch_bounds__(kCopyThreads) fork_kernel(const __grid_constan
 // The others are the taker's that goes on in p's own place, or else its first, the keeper; the rest get copies.
 //
 // First part: what each entry takes, the copies (sources to src, pages that were free before the call to ids), or nothing.
-__device__ __forceinline__ bool keeps(const int* parent, int n, int i) {
-  const int p = parent[i];
-  if (parent[p] == p) return i == p;
-  for (int j = 0; j < i; ++j)
-    if (parent[j] == p) return false;
-  return true;
-}
 __global__ void __launch_bounds__(kPlanThreads) reorder_choose_kernel(const __grid_constant__ SeqList list, PoolTables t, const int* parents,
                                                                       int* plan, int* src, int* ids, int* n_copies, int* go) {
   __shared__ uint32_t bits[kRoundWords];
-  __shared__ int scratch[kPlanThreads / 32], parent[kMaxCalls], off[kMaxCalls + 1], bad, most;
+  __shared__ int scratch[kPlanThreads / 32], parent[kMaxCalls], keeper[kMaxCalls], off[kMaxCalls + 1], bad, most;  // keeper: -1 for p itself
   const int tid = threadIdx.x;
   griddep_wait();
   griddep_launch();
   if (tid == 0) bad = most = 0;
+  if (tid < kMaxCalls) keeper[tid] = kMaxCalls;
   if (tid < list.n) parent[tid] = parents[tid];
   __syncthreads();
   int held = 0;
@@ -296,18 +290,31 @@ __global__ void __launch_bounds__(kPlanThreads) reorder_choose_kernel(const __gr
     held = t.held[list.a[tid]];
     const int p = parent[tid];
     if (held < 0 || held > t.max_pages || p < -1 || p >= list.n) bad = 1;
-    if (p >= 0 && p < list.n && t.held[list.a[p]] < list.d[p]) bad = 1;
+    if (p >= 0 && p < list.n) {
+      atomicMin(&keeper[p], p == tid ? -1 : tid);
+      if (t.held[list.a[p]] < list.d[p]) bad = 1;
+    }
     atomicMax(&most, held);
   }
   __syncthreads();
   if (!bad && tid < list.n) {
     const int p = parent[tid];
-    off[tid + 1] = p < 0 || keeps(parent, list.n, tid) ? 0 : list.d[p] - list.c[p];
+    off[tid + 1] = p < 0 || keeper[p] == (p == tid ? -1 : tid) ? 0 : list.d[p] - list.c[p];
   }
   __syncthreads();
-  if (!bad && tid == 0) {
-    off[0] = 0;
-    for (int i = 0; i < list.n; ++i) off[i + 1] = min(off[i] + off[i + 1], t.n_pages + 1);
+  if (!bad && tid < 32) {  // sums of the entries before, two a lane, up to one more than there are pages
+    static_assert(kMaxCalls == 64, "two entries a lane");
+    const int cap = t.n_pages + 1, a = 2 * tid < list.n ? min(off[2 * tid + 1], cap) : 0, b = 2 * tid + 1 < list.n ? min(off[2 * tid + 2], cap) : 0;
+    int all = min(a + b, cap);
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+      const int y = __shfl_up_sync(0xffffffffu, all, o);
+      if (tid >= o) all = min(all + y, cap);
+    }
+    int before = __shfl_up_sync(0xffffffffu, all, 1);
+    if (tid == 0) before = off[0] = 0;
+    off[2 * tid + 1] = min(before + a, cap);
+    off[2 * tid + 2] = all;
   }
   __syncthreads();
   const int need = bad ? 0 : off[list.n];
