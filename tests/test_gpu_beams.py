@@ -261,3 +261,28 @@ def test_refusals():
         with pytest.raises(native.TssError):
             beams.BeamSelector(*bad)
     assert s.sync_status() == native.TSS_OK
+
+
+@pytest.mark.parametrize("rows,n_beams,vocab,keep,dtype", [(512, 32, 70001, 32, BF), (640, 16, 66000, 128, HF), (320, 8, 66001, 7, FL), (2048, 64, 9000, 64, BF)])
+def test_many_long_rows(rows, n_beams, vocab, keep, dtype):
+    """Chunks of up to sixteen tiles: random rows, flat ones, of which every element is as large as the bound, rising and falling ones.  The
+    reference on the GPU, in 64 bits; candidates of equal value may come in either order where the logits are random."""
+    g = torch.Generator(device="cuda").manual_seed(31)
+    x = torch.randn(rows, vocab, generator=g, device="cuda").mul_(3).to(dtype)
+    score = torch.randn(rows, generator=g, device="cuda")
+    x[:n_beams] = 0.5
+    score[:n_beams] = -1.0
+    x[n_beams:2 * n_beams] = torch.linspace(-9, 9, vocab, device="cuda").to(dtype)
+    x[2 * n_beams:3 * n_beams] = torch.linspace(9, -9, vocab, device="cuda").to(dtype)
+    x[3 * n_beams + 1, vocab // 3:] = -math.inf
+    (value, parent, token), s = chosen(x, score, n_beams, keep)
+    assert s.sync_status() == native.TSS_OK
+    for at in range(0, rows, n_beams):
+        v = x[at:at + n_beams].double().log_softmax(-1) + score[at:at + n_beams].double()[:, None]
+        top, i = v.reshape(-1).topk(keep), at // n_beams
+        place = (parent[i].long() - at) * vocab + token[i].long()
+        assert place.unique().numel() == keep and (place >= 0).all()
+        # (a float's half step, and 1e-7 of the sum)
+        assert ((value[i].double() - top.values).abs() <= top.values.abs() * 2.0 ** -24 + 2e-7).all()
+        assert ((v.reshape(-1)[place] - top.values).abs() <= 2e-7).all()
+    assert (parent[0] == 0).all() and torch.equal(token[0].long(), torch.arange(keep, device="cuda"))
