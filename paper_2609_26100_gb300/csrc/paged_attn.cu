@@ -7,12 +7,14 @@
 // number c 2^-24 (c 2^-20 four bits further up), so a 32-bit word becomes four operand registers with four
 // ANDs and a shift, exactly; the factor 16 of every second pair is taken out of the other operand.  Scales
 // and minima join in fp32: s_t multiplies the sum over a group's dims, z_t the sum of the query's; on the
-// value side s'_t goes into the weight, which enters as two fp16 parts (hi and the rest, 22 bits: one part alone costs
-// the output 4e-4 of its size, twice what rounding it to fp16 does; a quarter of what rounding to bf16 does, so blocks of
-// more than 8 rows with bf16 outputs take one part), and the rest of the value is summed by itself.  V's codes enter centred,
-// v = s' (c' - 7.5) + (z' + 7.5 s') (`centre` says why: sums of terms of one sign drift), one more operation a register, 2 to 5 %
-// of the time; with one weight part, whose own rounding is 2^-12, as they are, 32 keys at a time that are added up by
-// rounding.  Queries are scaled by a power of two to fill fp16's range, exact down to 2^-35 of a row's largest.
+// value side s'_t goes into the weight, which enters as two fp16 parts (hi and the rest, 22 bits) or, in blocks of more than
+// 8 rows with bf16 outputs, as one (11 bits): beside bf16's own rounding errors, of 8 bits, it makes those of an output 0.8 %
+// larger (of 2000, 9000 or 32768 keys alike), which the second part would buy back for an eighth of the time (64 samples over 32768 keys
+// 202 -> 225 us); fp16's would be doubled.  The rest of the value is summed by itself, in fp32.  V's codes enter centred,
+// v = s' (c' - 7.5) + (z' + 7.5 s'), one more operation a register, 2 to 5 % of the time: sums of terms of one sign drift (`centre`),
+// and a rounded weight's error is multiplied by what it weighs: by codes as they are, whose mean square is six times that of
+// centred ones, where the output is a mean over many keys and small.  Queries are scaled by a power of two to fill fp16's range, exact
+// down to 2^-35 of a row's largest.
 //
 // Tokens take the MMA's 16-row side (S^T = K Q^T, O^T = V^T P^T): a block of 8 query rows (N) fills it,
 // where the usual orientation would pad 1 .. 8 rows to 16.  P^T's operand layout is the transpose of S^T's
@@ -33,7 +35,7 @@
 // Bound: up to 8 rows, instruction issue and HBM together: 4 x 65536 keys, 32 heads, 1 row in 234 us, 5.2 TB/s (over a third of
 // the 608 instructions that a warp spends on 32 keys and 8 rows take codes apart; 12 warps an SM, as many as 168 registers
 // allow, issue in 58 % of the cycles); beyond, neither: eight warps an SM (249 registers) do not hide the steps from load to
-// MMA, 16 x 16384 keys, 9 rows in 315 us.  One token over 1024 keys takes 9.4 us: launch, table, page, two joins.
+// MMA, 16 x 16384 keys, 9 rows in 332 us.  One token over 1024 keys takes 9.4 us: launch, table, page, two joins.
 #include <type_traits>
 
 #include "paged_attn.cuh"
@@ -350,12 +352,11 @@ __global__ void __launch_bounds__(WARPS * 32, PaShape<D, NT, WARPS>::kCtas)
 #pragma unroll
           for (int gi = 0; gi < G; ++gi) {
             vz[k >> 1][k & 1][gi] = __half22float2(pr[gi]);
-            if constexpr (TWO) vz[k >> 1][k & 1][gi].y = fmaf(vz[k >> 1][k & 1][gi].x, 7.5f, vz[k >> 1][k & 1][gi].y);
+            vz[k >> 1][k & 1][gi].y = fmaf(vz[k >> 1][k & 1][gi].x, 7.5f, vz[k >> 1][k & 1][gi].y);  // (v = s' (c' - 7.5) + (z' + 7.5 s'))
             smax[gi] = fmaxf(smax[gi], vz[k >> 1][k & 1][gi].x);
           }
         }
         constexpr int kParts = TWO ? 2 : 1;
-        constexpr bool kCentre = TWO;  // values as s' (c' - 7.5) + (z' + 7.5 s'); else as they are
         uint32_t pf[NT][G][kParts][4];  // the weights times the values' scales in fp16 parts, [8-key block]
         const auto weigh = [&](auto all) {
           constexpr bool kAll = decltype(all)::value;  // every (key, row) pair counts
@@ -473,11 +474,10 @@ __global__ void __launch_bounds__(WARPS * 32, PaShape<D, NT, WARPS>::kCtas)
 #pragma unroll
               for (int gi = 0; gi < G; ++gi) {
                 const float2 sz = vz[k >> 1][k & 1][gi];
-                const float s2 = !kCentre && (k & 1) ? sz.x * 0.0625f : sz.x;
                 // (what a pair does not see may be NaN: selected away, not multiplied)
                 oz[nt][gi][0] = on0 ? fmaf(w0, sz.y, oz[nt][gi][0]) : oz[nt][gi][0];
                 oz[nt][gi][1] = on1 ? fmaf(w1, sz.y, oz[nt][gi][1]) : oz[nt][gi][1];
-                const float2 pw = mul2(gi ? wx : make_float2(w0, w1), make_float2(s2, s2));
+                const float2 pw = mul2(gi ? wx : make_float2(w0, w1), make_float2(sz.x, sz.x));
                 const float p0 = on0 ? pw.x : 0.f, p1 = on1 ? pw.y : 0.f;
                 const uint32_t hi = pack_f16(p0, p1);
                 pf[nt][gi][0][k] = movmatrix_t(hi);
@@ -502,32 +502,18 @@ __global__ void __launch_bounds__(WARPS * 32, PaShape<D, NT, WARPS>::kCtas)
             const uint32_t x0 = x[2 * y], x1 = x[2 * y + 1], y0 = x0 >> 8, y1 = x1 >> 8;
             uint32_t a0[4] = {x0 & 0x000f000fu, x1 & 0x000f000fu, x0 & 0x00f000f0u, x1 & 0x00f000f0u};
             uint32_t a1[4] = {y0 & 0x000f000fu, y1 & 0x000f000fu, y0 & 0x00f000f0u, y1 & 0x00f000f0u};
-            if constexpr (kCentre) {
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                a0[i] = centre(a0[i], i >= 2);
-                a1[i] = centre(a1[i], i >= 2);
-              }
+            for (int i = 0; i < 4; ++i) {
+              a0[i] = centre(a0[i], i >= 2);
+              a1[i] = centre(a1[i], i >= 2);
             }
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
               const uint32_t(&w)[kParts][4] = pf[nt][db * 32 / kPgGroup];
-              if constexpr (kCentre) {
 #pragma unroll
-                for (int part = 0; part < kParts; ++part) {
-                  mma_next(o[nt][db][y], a0, &w[part][0]);
-                  mma_next(o[nt][db][y], a1, &w[part][2]);
-                }
-              } else {  // (the 32 keys apart, added to the rest by rounding)
-                float now[4];
-                mma_first(now, a0, &w[0][0]);
-                mma_next(now, a1, &w[0][2]);
-#pragma unroll
-                for (int i = 0; i < 4; i += 2) {
-                  const float2 sum = add2(make_float2(o[nt][db][y][i], o[nt][db][y][i + 1]), make_float2(now[i], now[i + 1]));
-                  o[nt][db][y][i] = sum.x;
-                  o[nt][db][y][i + 1] = sum.y;
-                }
+              for (int part = 0; part < kParts; ++part) {
+                mma_next(o[nt][db][y], a0, &w[part][0]);
+                mma_next(o[nt][db][y], a1, &w[part][2]);
               }
             }
           }
@@ -557,8 +543,8 @@ __global__ void __launch_bounds__(WARPS * 32, PaShape<D, NT, WARPS>::kCtas)
           for (int db = 0; db < DB; ++db) {
             float4 x;
             const float z = oz[nt][db * 32 / kPgGroup][i];
-            // (2^9 or 2^24 over the group's factor, a power of two)
-            constexpr uint32_t kUp = TWO ? 9 : 24;
+            // (2^9 over the group's factor, a power of two)
+            constexpr uint32_t kUp = 9;
             const float m = db * 32 / kPgGroup ? __uint_as_float(((kUp + 254u) << 23) - __float_as_uint(i ? gx[nt].y : gx[nt].x))
                                                : static_cast<float>(1 << kUp);
             x.x = fmaf(o[nt][db][0][i], m, z);

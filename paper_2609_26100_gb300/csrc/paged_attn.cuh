@@ -68,12 +68,12 @@ __device__ __forceinline__ float ex2(float x) {
 
 // The tcgen05 kernel (paged_attn_tc.cu; head_dim 128, planned with R = 128 and whole pages) and the query rows of a KV
 // head above which a request goes there.  A page costs it the same for any number of rows, the warp-level kernel in
-// proportion to its 16-row tiles; us, warp-level / tcgen05, four requests of 4600 tokens and 32 heads: 24 rows 66 / 103,
-// 48 rows 97 / 110, 56 rows 119 / 111, 128 rows 225 / 123; 8 heads: 32 rows 28 / 40, 48 rows 33 / 42, 64 rows 41 / 42.
+// proportion to its 16-row tiles; us, warp-level / tcgen05, four requests of 4600 tokens and 32 heads: 24 rows 68 / 103,
+// 48 rows 101 / 109, 56 rows 124 / 110, 128 rows 234 / 122; 8 heads: 32 rows 29 / 40, 48 rows 35 / 42, 64 rows 44 / 42.
 constexpr int kPaTcRows = 48, kPaTcTile = 128;
 // In the passes of the shared attention, which have fewer items: us of such a call, warp-level / tcgen05, bf16, 32 heads over 8192
-// shared keys, 64 rows 72 / 82, 96 rows 87 / 81; over 32768, 64 rows 187 / 196, 96 rows 249 / 197; 8 heads over 32768, 64 rows 59 / 68,
-// 96 rows 81 / 71.
+// shared keys, 64 rows 74 / 81, 80 rows 78 / 74, 96 rows 90 / 80; over 32768, 64 rows 195 / 197, 96 rows 261 / 197; 8 heads over 8192,
+// 80 rows 35 / 40, 96 rows 40 / 42; over 32768, 64 rows 61 / 69, 80 rows 71 / 70, 96 rows 83 / 72.
 constexpr int kPaTcShared = 80;
 cudaError_t paged_attn_tc_prepare();
 cudaError_t launch_paged_attention_tc(PaShared& p, bool shared, int sms, cudaStream_t s);
