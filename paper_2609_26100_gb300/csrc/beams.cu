@@ -535,8 +535,8 @@ __device__ __forceinline__ void bm_join(const BmParams& p, BmShared& sh, const B
   // their last ones; of values in 32 bits, less what these may be off (64-bit logarithms take their time meanwhile).
   const auto least_of = [&](int l, uint32_t x) {
     const float2 b = sh.near[l / p.chunks];
-    const float y = float_of(x);
-    return y > -INFINITY ? (b.x + y) - (b.y + fabsf(y) * 0x1p-20f) : -INFINITY;
+    const float y = float_of(x);  // (of a row without logits that count whatever lay there, infinite or NaN too)
+    return b.x > -INFINITY && y > -INFINITY ? (b.x + y) - (b.y + fabsf(y) * 0x1p-20f) : -INFINITY;
   };
   float tf = mine < lists ? least_of(mine, deep_x) : -INFINITY, lf = mine < lists ? least_of(mine, last_x) : -INFINITY;
   for (int l = mine + kBmThreads; l < lists; l += kBmThreads) {
