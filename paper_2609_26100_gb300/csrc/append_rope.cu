@@ -180,7 +180,8 @@ __global__ void __launch_bounds__(kPqThreads, sizeof(T) == 4 ? 4 : 5) append_rop
   griddep_launch();
   const long long w = pq_warp();
   if (w >= a.quant) {
-    rope_row<T, D / 16, INTER>(a.r, w - a.quant, lane);
+    // (without query heads the last CTA's spare warps come here, and a row has no splits)
+    if (a.r.hq > 0) rope_row<T, D / 16, INTER>(a.r, w - a.quant, lane);
     return;
   }
   PqUnit u;
