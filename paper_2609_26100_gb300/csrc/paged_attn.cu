@@ -267,6 +267,7 @@ __global__ void __launch_bounds__(WARPS * 32, PaShape<D, NT, WARPS>::kCtas)
       }
 #pragma unroll
       for (int x2 = 16; x2 > 0; x2 >>= 1) pmax = max(pmax, __shfl_xor_sync(0xffffffffu, pmax, x2));
+      if constexpr (SH) __syncwarp();  // (the positions, before other lanes read them: shuffles order no memory)
     }
     int all0, all1, all2;
     units_in_sight(a, r, unit, pmax, &all0, &all1, &all2);
