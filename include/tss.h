@@ -667,8 +667,9 @@ tss_status tss_pages_copy(tss_pages* h, void* const* layer, int n_layers, size_t
  *   score_out (fp32; may be score where n_keep = n_beams), parent (a row of logits: group * n_beams + beam), token (both int32): [n_groups][n_keep]
  *     DEVICE.  Where a group offers less than n_keep the rest gets -infinity, -1, -1.
  * A logit of -1e38 or less is masked.  A row that has a NaN or a logit above 1e38, or whose score is NaN or +infinity,
- * offers nothing, and TSS_ERR_DEVICE_CHECK is recorded.  Values are right to about 1e-8 (fp32 logits, sums and choice in 64 bits)
- * and rounded once; equal rows have equal values, and results do not depend on timing.
+ * offers nothing, and TSS_ERR_DEVICE_CHECK is recorded.  Values are right to 2^-19 (to about 3e-8 where a row's logits are many
+ * different numbers), chosen in 64 bits and rounded once: the order of candidates closer than 2^-18 is not the definition's for certain, but in
+ * a row it is that of the logits, equal rows of a call have equal values, and results do not depend on timing.
  * tss_beam_create makes the workspace for rows of `vocab` logits (at most 2^24), at most max_rows of them (2^20) and n_keep up to
  * max_keep (128); n_beams is at most 64.  Calls that share one must not overlap on different streams.  Asynchronous on `stream`.
  * Errors: INVALID_ARG, UNSUPPORTED_ARCH, OUT_OF_MEMORY, CUDA. */

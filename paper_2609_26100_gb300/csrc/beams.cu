@@ -15,9 +15,11 @@
 //
 // Between rows the order goes by the last bits of the rows' sums.  Terms are 2^((x - m) log2e + f), m the chunk's largest logit,
 // log2e in two parts, f what its product with m leaves of a whole number, so that chunks' sums differ by powers of two.  The
-// candidates' terms, most of the sum, are computed to 2^-28 (the fast exponential's 2^-22 is for the others), and sums of
-// threads are whole numbers, whose order does not matter: values are right to about 1e-8, compared in 64 bits and rounded once, and
-// equal rows have equal values, whatever their alignment (elements go to threads by their index).
+// candidates' terms are computed to 2^-27, the others' by the fast exponential (2^-22 of a term, and as much by its argument), in
+// fp32 sums of a thread's (24 additions at most); sums of threads are whole numbers, whose order does not matter.  So ln sum and a
+// value are off by less than 2^-19 (4e-7 at the most that was seen, fp32 rows of one value but for a few; 3e-8 where logits are many different
+// numbers); rounding the value to fp32 leaves as much from 32 on.  Values are compared in 64 bits and rounded once, and equal rows of a call have
+// equal values, whatever their alignment (elements go to threads by their index).
 #include "ops.cuh"
 
 struct tss_beam {
@@ -108,7 +110,8 @@ __device__ __forceinline__ float bm_term(float x, float m, float f) {
   const float d = x - m;
   return bm_ex2(fmaf(d, kLog2eHi, fmaf(d, kLog2eLo, f)));
 }
-// 2^t to about 2^-28 of it, times 2^kBmBits and rounded to a whole number: 2^n e^u with u in two floats, e^u = 1 + u + u^2 q(u).
+// 2^t to 2^-27 of it, times 2^kBmBits and rounded to a whole number: 2^n e^u with u in two floats, e^u = 1 + u + u^2 q(u) (what q leaves
+// out is u^8 / 8!, at |u| = ln 2 / 2 5e-9).
 constexpr int kBmBits = 37;  // 2^24 terms of up to 2 stay below 2^63
 __device__ __forceinline__ long long bm_fixed(float x, float m, float f) {
   constexpr float kLn2Hi = 0.693147182464599609375f, kLn2Lo = -1.90465429995776804525e-9f;
