@@ -643,7 +643,8 @@ tss_status tss_pages_fork(tss_pages* h, const tss_page_tables* t, void* const* l
  * first shared[p] pages are the same ones in every place that goes on with p; the rest stay with one of them (p itself if it goes on
  * with its own pages, else the lowest i) and are copied in every layer for the others, into the lowest pages that were free
  * before the call, in the order of i.  What no place goes on with is given back.  A page id outside the pool in a shared place is
- * moved as it is, and recorded. */
+ * moved as it is, and recorded.  n is at most 64, as everywhere here: more sequences take several calls, a text's beams in one and
+ * its parents counted from that call's first. */
 tss_status tss_pages_reorder(tss_pages* h, const tss_page_tables* t, void* const* layer, int n_layers, size_t page_bytes,
                              int n, const int32_t* seq, const int32_t* parent, const int32_t* shared, const int32_t* total,
                              void* stream);
@@ -671,7 +672,8 @@ tss_status tss_pages_copy(tss_pages* h, void* const* layer, int n_layers, size_t
  * different numbers), chosen in 64 bits and rounded once: the order of candidates closer than 2^-18 is not the definition's for certain, but in
  * a row it is that of the logits, equal rows of a call have equal values, and results do not depend on timing.
  * tss_beam_create makes the workspace for rows of `vocab` logits (at most 2^24), at most max_rows of them (2^20) and n_keep up to
- * max_keep (128); n_beams is at most 64.  Calls that share one must not overlap on different streams.  Asynchronous on `stream`.
+ * max_keep (128); n_beams is at most 64.  (The calls on pages take 64 requests or sequences each: wider searches take several of them
+ * to one selection.)  Calls that share one must not overlap on different streams.  Asynchronous on `stream`.
  * Errors: INVALID_ARG, UNSUPPORTED_ARCH, OUT_OF_MEMORY, CUDA. */
 typedef struct tss_beam tss_beam;
 typedef struct {

@@ -2,7 +2,8 @@
 libtss.so (tss_beam_*).
 
 ``BeamSelector.select`` picks every group's best continuations on the device; its ``parent`` is what
-``paged.PagePool.reorder`` takes to move the beams' pages, without a host wait between the two.  All tensors are on the
+``paged.PagePool.reorder`` takes to move the beams' pages, without a host wait between the two (64 sequences a call: of more
+rows, each call gets the parents of its texts less its first row's number).  All tensors are on the
 selector's GPU, which has to be the current device in every call.
 """
 from __future__ import annotations
